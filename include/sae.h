@@ -324,6 +324,62 @@ int sae_sign_compress_noalloc(const float *v, int64_t n, uint32_t *words, float 
                               void *stream);
 int64_t sae_noalloc_max_elements(void);
 
+/*
+ * Gradient sets.  (The paper has no counterpart; it stands in Algorithm 1 where "compute stochastic gradient"
+ * hands the gradient over.)  A model's gradient is T tensors, often of 16-bit types; sae_step takes one float row
+ * a worker.  A sae_grads holds the parameter list's tile table and scratch and does what lies between:
+ *
+ *   norm_k = (sum over row k of |g|^q)^(1/q), q = 1 or 2, or the largest |g|;   coef_k = min(1, max_norm / (norm_k + 1e-6))
+ *   sae_grads_norm    norms[k] = norm_k
+ *   sae_grads_clip    g *= coef_k, in place, each element rounded once to its type
+ *   sae_grads_pack    out[k][0..d) = coef_k * (the row's T tensors, concatenated in list order), the caller layout of sae_step
+ *   sae_grads_unpack  the T tensors of row k = in[k][0..d), rounded to their types (the step-ahead point back to a model)
+ *
+ * tensors: HOST array of num_rows * num_tensors DEVICE pointers, row k's at tensors[k * T .. ); read before the call
+ *   returns.  Tensor j has n_j elements without gaps, of type tensor_types[j], aligned to its type; the tensors that a
+ *   call writes must not overlap one another, its output or its input.  A tensor with n_j = 0 may be NULL.
+ * norms: DEVICE, num_rows floats, NULL where it is not wanted (not for sae_grads_norm).
+ * out / in: DEVICE; row k starts at element k * stride.  in_stride = 0 gives every row the same vector.
+ * SAE_NORM_NONE (sae_grads_pack only, norms NULL): no norm is taken and coef_k = 1.
+ *
+ * Squares and sums are accumulated in double (groups of eight in float), in a fixed order: the same input gives the
+ * same bits, and no finite float row overflows.  As the formula has it, a row whose norm is infinite gets coef_k = 0
+ * (its infinities become NaN) and a NaN anywhere makes the norm and the row NaN; sae_sync reports either after the step.
+ * Where coef_k = 1, sae_grads_clip writes nothing.
+ * All calls only enqueue kernels on the configuration's stream, allocate nothing, may be captured, and share the
+ * handle's scratch: one handle is for one stream and one host thread at a time.
+ * Returns SAE_OK or a sae_status; sae_grads_last_cuda_error as sae_last_cuda_error (NULL: of the last sae_grads_init).
+ */
+#define SAE_TYPE_FLOAT 0
+#define SAE_TYPE_BFLOAT 1 /* bfloat16 */
+#define SAE_TYPE_HALF 2   /* IEEE binary16 */
+
+#define SAE_NORM_NONE 0
+#define SAE_NORM_ONE 1
+#define SAE_NORM_TWO 2
+#define SAE_NORM_MAX 3
+
+typedef struct sae_grads sae_grads; /* opaque, library-owned */
+
+typedef struct {
+  uint32_t abi_version;        /* must be SAE_ABI_VERSION                                               */
+  int32_t num_rows;            /* K, 1..1024                                                            */
+  int32_t num_tensors;         /* T >= 1                                                                */
+  const int64_t *tensor_sizes; /* HOST, T entries, 0 <= n_j <= 2^30; copied                             */
+  const int32_t *tensor_types; /* HOST, T SAE_TYPE_* codes, copied; NULL = all SAE_TYPE_FLOAT           */
+  int32_t device;              /* CUDA device ordinal                                                   */
+  void *stream;                /* cudaStream_t (NULL = default stream)                                  */
+} sae_grads_config;
+
+int sae_grads_init(const sae_grads_config *cfg, sae_grads **out);
+int sae_grads_norm(sae_grads *h, const void *const *tensors, int32_t norm_kind, float *norms);
+int sae_grads_clip(sae_grads *h, void *const *tensors, int32_t norm_kind, float max_norm, float *norms);
+int sae_grads_pack(sae_grads *h, const void *const *tensors, int32_t norm_kind, float max_norm, float *out,
+                   int64_t out_stride, float *norms);
+int sae_grads_unpack(sae_grads *h, const float *in, int64_t in_stride, void *const *tensors);
+int sae_grads_last_cuda_error(const sae_grads *h);
+void sae_grads_destroy(sae_grads *h);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,7 +26,12 @@ EXPORTS = ["sae_init", "sae_step", "sae_step_host", "sae_get_params", "sae_get_p
            "sae_last_cuda_error", "sae_sign_compress_noalloc", "sae_noalloc_max_elements", "sae_state_bytes",
            "sae_save_state", "sae_load_state", "sae_get_mismatch", "sae_init_shard", "sae_shard_export",
            "sae_shard_attach", "sae_shard_detach", "sae_step_begin", "sae_step_end", "sae_shard_set_avg_mode", "sae_avg_due",
-           "sae_num_padded", "sae_avg_local_sum", "sae_avg_set", "sae_set_local_steps"]
+           "sae_num_padded", "sae_avg_local_sum", "sae_avg_set", "sae_set_local_steps",
+           "sae_grads_init", "sae_grads_norm", "sae_grads_clip", "sae_grads_pack", "sae_grads_unpack",
+           "sae_grads_last_cuda_error", "sae_grads_destroy"]
+
+TYPE_FLOAT, TYPE_BFLOAT, TYPE_HALF = 0, 1, 2
+NORM_NONE, NORM_ONE, NORM_TWO, NORM_MAX = 0, 1, 2, 3
 
 SHARD_BLOB_BYTES = 1024
 
@@ -36,6 +41,12 @@ class SaeConfig(C.Structure):
                 ("tensor_sizes", C.POINTER(C.c_int64)), ("compressor", C.c_int32), ("server_compress", C.c_int32),
                 ("mode", C.c_int32), ("avg_period", C.c_int32), ("momentum", C.c_float), ("weight_decay", C.c_float),
                 ("topk_num", C.c_uint32), ("topk_den", C.c_uint32), ("device", C.c_int32), ("stream", C.c_void_p)]
+
+
+class SaeGradsConfig(C.Structure):
+    _fields_ = [("abi_version", C.c_uint32), ("num_rows", C.c_int32), ("num_tensors", C.c_int32),
+                ("tensor_sizes", C.POINTER(C.c_int64)), ("tensor_types", C.POINTER(C.c_int32)), ("device", C.c_int32),
+                ("stream", C.c_void_p)]
 
 
 class SaeError(RuntimeError):
@@ -100,6 +111,14 @@ def lib():
         L.sae_sign_compress_noalloc.argtypes = [vp, i64, vp, vp, vp, vp]
         L.sae_noalloc_max_elements.argtypes = []
         L.sae_noalloc_max_elements.restype = i64
+        L.sae_grads_init.argtypes = [C.POINTER(SaeGradsConfig), C.POINTER(vp)]
+        L.sae_grads_norm.argtypes = [vp, vp, i32, vp]
+        L.sae_grads_clip.argtypes = [vp, vp, i32, f32, vp]
+        L.sae_grads_pack.argtypes = [vp, vp, i32, f32, vp, i64, vp]
+        L.sae_grads_unpack.argtypes = [vp, vp, i64, vp]
+        L.sae_grads_last_cuda_error.argtypes = [vp]
+        L.sae_grads_destroy.argtypes = [vp]
+        L.sae_grads_destroy.restype = None
         _lib = L
     return _lib
 
