@@ -380,6 +380,56 @@ int sae_grads_unpack(sae_grads *h, const float *in, int64_t in_stride, void *con
 int sae_grads_last_cuda_error(const sae_grads *h);
 void sae_grads_destroy(sae_grads *h);
 
+/*
+ * Group norm with an activation, channels last.  (The paper's models use batch norm.  Its running statistics are no
+ * parameters, so no compressor sends them, and at a worker's share of a batch they are noisy; group norm has the same
+ * two parameter vectors a layer, the same parameter list, and neither defect.)
+ *
+ * x: [samples][pixels][channels] with the channels of a pixel neighbours in memory; group j is the Cg = channels / groups
+ * channels from j * Cg on, over all pixels of its sample:
+ *   xhat = (x - mean) / sqrt(var + eps);  z = xhat * weight_c + bias_c (+ residual);  y = act(z)
+ * backward, from dL/dy:  dz = dy * act'(z);  dresidual = dz;  dbias_c = sum dz;  dweight_c = sum dz * xhat;
+ *   g = dz * weight_c;  dx = rstd * (g - mean_group(g) - xhat * mean_group(g * xhat))
+ *
+ * All pointers are DEVICE pointers, all work goes to `stream` of the CURRENT device and is asynchronous; nothing is
+ * allocated and nothing is kept between calls.
+ * x, residual, dy: type `type`, sample n's pixel p at n * *_sample + p * *_pixel elements (strides >= 0; 0 repeats).
+ * y, dx, dresidual: type `type`, without gaps; they must not overlap any input.  weight, bias, dweight, dbias: `channels`
+ *   values of type `param_type`; weight NULL = 1, bias NULL = 0.  residual NULL = none; dresidual, dweight, dbias NULL = not wanted.
+ * mean, rstd: [samples][groups] floats, written by the forward call, read by the backward call.
+ * workspace: at least sae_group_norm_workspace(desc) bytes, 16-byte aligned, the call's own until it has run.
+ * Arithmetic is in float (statistics and sums joined in double), one rounding to `type` at each output; z is the same bits
+ * in both directions, so relu's mask (z > 0) is the forward call's.  The sums' order is fixed: same input, same bits.
+ * samples or pixels = 0: mean and rstd are NaN (0 / 0), dweight and dbias 0.
+ * Errors: SAE_ERR_INVALID_ARG for a null or misaligned pointer, groups that do not divide channels, a size out of range
+ * (samples <= 2^24, pixels <= 2^30, channels <= 2^20, samples * groups < 2^31), a workspace too small; SAE_ERR_CUDA.
+ */
+#define SAE_ACT_NONE 0
+#define SAE_ACT_RELU 1
+#define SAE_ACT_SILU 2 /* z / (1 + exp(-z))            */
+#define SAE_ACT_GELU 3 /* z * (1 + erf(z / sqrt(2))) / 2 */
+
+typedef struct {
+  int32_t type, param_type;           /* SAE_TYPE_*                                                           */
+  int32_t activation;                 /* SAE_ACT_*                                                            */
+  int32_t groups;
+  int64_t samples, pixels, channels;
+  int64_t x_sample, x_pixel;          /* strides in elements                                                  */
+  int64_t residual_sample, residual_pixel; /* 0 without a residual                                            */
+  int64_t dy_sample, dy_pixel;        /* 0 for a forward call                                                 */
+  float eps;                          /* >= 0                                                                 */
+} sae_group_norm_desc;
+
+/* Bytes of workspace either call needs on the current device; -1 for a bad description or without a device. */
+int64_t sae_group_norm_workspace(const sae_group_norm_desc *desc);
+int sae_group_norm_forward(const sae_group_norm_desc *desc, const void *x, const void *residual, const void *weight,
+                           const void *bias, void *y, float *mean, float *rstd, void *workspace, size_t workspace_bytes,
+                           void *stream);
+int sae_group_norm_backward(const sae_group_norm_desc *desc, const void *dy, const void *x, const void *residual,
+                            const float *mean, const float *rstd, const void *weight, const void *bias, void *dx,
+                            void *dresidual, void *dweight, void *dbias, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,10 +28,12 @@ EXPORTS = ["sae_init", "sae_step", "sae_step_host", "sae_get_params", "sae_get_p
            "sae_shard_attach", "sae_shard_detach", "sae_step_begin", "sae_step_end", "sae_shard_set_avg_mode", "sae_avg_due",
            "sae_num_padded", "sae_avg_local_sum", "sae_avg_set", "sae_set_local_steps",
            "sae_grads_init", "sae_grads_norm", "sae_grads_clip", "sae_grads_pack", "sae_grads_unpack",
-           "sae_grads_last_cuda_error", "sae_grads_destroy"]
+           "sae_grads_last_cuda_error", "sae_grads_destroy", "sae_group_norm_workspace", "sae_group_norm_forward",
+           "sae_group_norm_backward"]
 
 TYPE_FLOAT, TYPE_BFLOAT, TYPE_HALF = 0, 1, 2
 NORM_NONE, NORM_ONE, NORM_TWO, NORM_MAX = 0, 1, 2, 3
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
 
 SHARD_BLOB_BYTES = 1024
 
@@ -47,6 +49,13 @@ class SaeGradsConfig(C.Structure):
     _fields_ = [("abi_version", C.c_uint32), ("num_rows", C.c_int32), ("num_tensors", C.c_int32),
                 ("tensor_sizes", C.POINTER(C.c_int64)), ("tensor_types", C.POINTER(C.c_int32)), ("device", C.c_int32),
                 ("stream", C.c_void_p)]
+
+
+class SaeGroupNormDesc(C.Structure):
+    _fields_ = [("type", C.c_int32), ("param_type", C.c_int32), ("activation", C.c_int32), ("groups", C.c_int32),
+                ("samples", C.c_int64), ("pixels", C.c_int64), ("channels", C.c_int64), ("x_sample", C.c_int64),
+                ("x_pixel", C.c_int64), ("residual_sample", C.c_int64), ("residual_pixel", C.c_int64),
+                ("dy_sample", C.c_int64), ("dy_pixel", C.c_int64), ("eps", C.c_float)]
 
 
 class SaeError(RuntimeError):
@@ -119,6 +128,10 @@ def lib():
         L.sae_grads_last_cuda_error.argtypes = [vp]
         L.sae_grads_destroy.argtypes = [vp]
         L.sae_grads_destroy.restype = None
+        L.sae_group_norm_workspace.argtypes = [C.POINTER(SaeGroupNormDesc)]
+        L.sae_group_norm_workspace.restype = i64
+        L.sae_group_norm_forward.argtypes = [C.POINTER(SaeGroupNormDesc)] + [vp] * 8 + [C.c_size_t, vp]
+        L.sae_group_norm_backward.argtypes = [C.POINTER(SaeGroupNormDesc)] + [vp] * 12 + [C.c_size_t, vp]
         _lib = L
     return _lib
 

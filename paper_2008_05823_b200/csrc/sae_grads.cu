@@ -6,15 +6,13 @@
 // Everything here is bound by HBM: a norm reads each element once; clipping and packing need the finished norm
 // before the first store, so they are a second pass whose reads come from L2 as far as it still holds the row.
 #include "../../include/sae.h"
-
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-#include <cuda_runtime.h>
-#include <stdint.h>
+#include "sae_vec.cuh"
 
 #include <algorithm>
 #include <new>
 #include <vector>
+
+using namespace sae;
 
 namespace {
 
@@ -55,52 +53,25 @@ __global__ void k_upload_ptrs(const __grid_constant__ UploadChunk c, void** tabl
   if (i < n) table[i] = c.p[i];
 }
 
-// ---- eight elements of any type as floats, and back ----------------------------------------------------------
-__device__ __forceinline__ float2 unpack2(u32 w, const __nv_bfloat16*) {
-  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-}
-__device__ __forceinline__ float2 unpack2(u32 w, const __half*) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
-__device__ __forceinline__ u32 pack2(float a, float b, const __nv_bfloat16*) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const u32*>(&v);
-}
-__device__ __forceinline__ u32 pack2(float a, float b, const __half*) {
-  const __half2 v = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const u32*>(&v);
-}
-
-template <typename T> struct Raw8 { uint4 a; };
-template <> struct Raw8<float> { float4 a, b; };
-
-template <typename T> __device__ __forceinline__ Raw8<T> load8(const T* p) { return {__ldg(reinterpret_cast<const uint4*>(p))}; }
-template <> __device__ __forceinline__ Raw8<float> load8<float>(const float* p) {
-  return {__ldg(reinterpret_cast<const float4*>(p)), __ldg(reinterpret_cast<const float4*>(p) + 1)};
-}
-template <typename T> __device__ __forceinline__ void widen(const Raw8<T>& r, float (&v)[8]) {
-  const u32 w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { const float2 f = unpack2(w[i], (const T*)nullptr); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
-}
-template <> __device__ __forceinline__ void widen<float>(const Raw8<float>& r, float (&v)[8]) {
-  v[0] = r.a.x; v[1] = r.a.y; v[2] = r.a.z; v[3] = r.a.w; v[4] = r.b.x; v[5] = r.b.y; v[6] = r.b.z; v[7] = r.b.w;
-}
-template <typename T> __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
-  uint4 w;
-  w.x = pack2(v[0], v[1], (const T*)nullptr); w.y = pack2(v[2], v[3], (const T*)nullptr);
-  w.z = pack2(v[4], v[5], (const T*)nullptr); w.w = pack2(v[6], v[7], (const T*)nullptr);
-  *reinterpret_cast<uint4*>(p) = w;
-}
-template <> __device__ __forceinline__ void store8<float>(float* p, const float (&v)[8]) {
-  *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ float to_f(float v) { return v; }
-__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
-template <typename T> __device__ __forceinline__ T from_f(float v);
-template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
+// Eight elements of any type: one piece of 16 bytes, or two.
+template <typename T> struct Eight {
+  Raw<T, 8> a;
+  __device__ __forceinline__ void load(const T* p) { a.load(p); }
+  __device__ __forceinline__ void store(T* p) const { a.store(p); }
+  __device__ __forceinline__ void widen(float (&v)[8]) const { a.widen(v); }
+  __device__ __forceinline__ void round(const float (&v)[8]) { a.round(v); }
+};
+template <> struct Eight<float> {
+  Raw<float, 4> a, b;
+  __device__ __forceinline__ void load(const float* p) { a.load(p); b.load(p + 4); }
+  __device__ __forceinline__ void store(float* p) const { a.store(p); b.store(p + 4); }
+  __device__ __forceinline__ void widen(float (&v)[8]) const {
+    a.widen(*reinterpret_cast<float (*)[4]>(&v[0])); b.widen(*reinterpret_cast<float (*)[4]>(&v[4]));
+  }
+  __device__ __forceinline__ void round(const float (&v)[8]) {
+    a.round(*reinterpret_cast<const float (*)[4]>(&v[0])); b.round(*reinterpret_cast<const float (*)[4]>(&v[4]));
+  }
+};
 
 // ---- the running value of a norm: a double (q = 1, 2), or the bits of the largest magnitude -------------------
 // Eight elements are added in float first and the sum goes to the double accumulator: the float part rounds at most
@@ -165,14 +136,14 @@ template <int KIND, typename T>
 __device__ __forceinline__ void tile_norm(Running<KIND>& r, const T* p, u32 cnt) {
   if ((reinterpret_cast<uintptr_t>(p) & 15) == 0) {
     if (cnt == GT_TILE) {
-      Raw8<T> raw[GT_TILE / (GT_THREADS * GT_VEC)];
+      Eight<T> raw[GT_TILE / (GT_THREADS * GT_VEC)];
 #pragma unroll
-      for (int i = 0; i < GT_TILE / (GT_THREADS * GT_VEC); ++i) raw[i] = load8(p + (i * GT_THREADS + threadIdx.x) * GT_VEC);
+      for (int i = 0; i < GT_TILE / (GT_THREADS * GT_VEC); ++i) raw[i].load(p + (i * GT_THREADS + threadIdx.x) * GT_VEC);
 #pragma unroll
-      for (int i = 0; i < GT_TILE / (GT_THREADS * GT_VEC); ++i) { float v[8]; widen<T>(raw[i], v); r.eight(v); }
+      for (int i = 0; i < GT_TILE / (GT_THREADS * GT_VEC); ++i) { float v[8]; raw[i].widen(v); r.eight(v); }
     } else {
       const u32 whole = cnt / GT_VEC;
-      for (u32 i = threadIdx.x; i < whole; i += GT_THREADS) { float v[8]; widen<T>(load8(p + i * GT_VEC), v); r.eight(v); }
+      for (u32 i = threadIdx.x; i < whole; i += GT_THREADS) { Eight<T> raw; raw.load(p + i * GT_VEC); float v[8]; raw.widen(v); r.eight(v); }
       const u32 e = whole * GT_VEC + threadIdx.x;
       if (e < cnt) r.one(to_f(p[e]));
     }
@@ -228,23 +199,26 @@ template <typename S, typename D>
 __device__ __forceinline__ void tile_scale(const S* s, D* d, u32 cnt, float coef) {
   if (((reinterpret_cast<uintptr_t>(s) | reinterpret_cast<uintptr_t>(d)) & 15) == 0) {
     if (cnt == GT_TILE) {
-      Raw8<S> raw[GT_TILE / (GT_THREADS * GT_VEC)];
+      Eight<S> raw[GT_TILE / (GT_THREADS * GT_VEC)];
 #pragma unroll
-      for (int i = 0; i < GT_TILE / (GT_THREADS * GT_VEC); ++i) raw[i] = load8(s + (i * GT_THREADS + threadIdx.x) * GT_VEC);
+      for (int i = 0; i < GT_TILE / (GT_THREADS * GT_VEC); ++i) raw[i].load(s + (i * GT_THREADS + threadIdx.x) * GT_VEC);
 #pragma unroll
       for (int i = 0; i < GT_TILE / (GT_THREADS * GT_VEC); ++i) {
-        float v[8]; widen<S>(raw[i], v);
+        float v[8]; raw[i].widen(v);
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = __fmul_rn(v[q], coef);
-        store8<D>(d + (i * GT_THREADS + threadIdx.x) * GT_VEC, v);
+        Eight<D> o; o.round(v);
+        o.store(d + (i * GT_THREADS + threadIdx.x) * GT_VEC);
       }
     } else {
       const u32 whole = cnt / GT_VEC;
       for (u32 i = threadIdx.x; i < whole; i += GT_THREADS) {
-        float v[8]; widen<S>(load8(s + i * GT_VEC), v);
+        Eight<S> raw; raw.load(s + i * GT_VEC);
+        float v[8]; raw.widen(v);
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = __fmul_rn(v[q], coef);
-        store8<D>(d + i * GT_VEC, v);
+        Eight<D> o; o.round(v);
+        o.store(d + i * GT_VEC);
       }
       const u32 e = whole * GT_VEC + threadIdx.x;
       if (e < cnt) d[e] = from_f<D>(__fmul_rn(to_f(s[e]), coef));

@@ -1,0 +1,601 @@
+// Group norm with an activation, channels last, forward and backward.  Declarations and contract: include/sae.h.
+//
+// x is [N][P][C] (P pixels, the channels of a pixel neighbours in memory); group j is the Cg channels from j * Cg on, over
+// all P pixels of a sample, M = P * Cg values:
+//   mean = sum x / M,  var = sum (x - mean)^2 / M,  rstd = 1 / sqrt(var + eps)
+//   xhat = (x - mean) * rstd,  z = xhat * w_c + b_c (+ residual),  y = act(z)
+//   dz = dy * act'(z),  db_c = sum dz,  dw_c = sum dz * xhat,  g = dz * w_c,
+//   dx = rstd * (g - mean_group(g) - xhat * mean_group(g * xhat))
+// z is computed by the same separately rounded operations in both directions, so that relu's mask in the backward pass is
+// the forward pass's own.
+//
+// Everything is bound by HBM.  A group of neighbouring channels is a column of short runs, so a thread takes 16 bytes of a
+// pixel, always the same channels, and walks down the pixels; the threads of a block stand side by side over the channels
+// first, which makes a block's loads whole lines whatever the group size is.
+#include "../../include/sae.h"
+#include "sae_vec.cuh"
+
+#include <algorithm>
+
+using namespace sae;
+
+namespace {
+
+constexpr int GN_THREADS = 256;
+constexpr int GN_BATCH = 4;              // pixels a thread has in flight
+
+struct Args {
+  const void *x, *res, *dy, *w, *b;
+  void *out, *dres;                      // y or dx; dense
+  float *mean, *rstd;                    // [N][G]: written forwards, read backwards
+  void *dw, *db;
+  long long x_n, x_p, r_n, r_p, d_n, d_p;   // strides of a sample and of a pixel, in elements
+  int N, P, C, G, Cg;
+  int act, ptype;
+  float eps;
+  int slices, cvt;                       // runs of pixels a sample is cut into; vectors of a pixel a block takes
+  float *part_a, *part_b;                // [N][slices][C] values of each channel's run (forwards: mean and squares about it;
+                                         // backwards: sum dz and sum dz * xhat)
+  float *mean_g, *mean_gx;               // [N][G] backwards: mean_group(g), mean_group(g * xhat)
+};
+
+__device__ __forceinline__ float param(const void* p, int type, int c, float none) {
+  if (!p) return none;
+  if (type == SAE_TYPE_FLOAT) return __ldg((const float*)p + c);
+  if (type == SAE_TYPE_BFLOAT) return to_f(((const __nv_bfloat16*)p)[c]);
+  return to_f(((const __half*)p)[c]);
+}
+__device__ __forceinline__ void put_param(void* p, int type, int c, float v) {
+  if (type == SAE_TYPE_FLOAT) ((float*)p)[c] = v;
+  else if (type == SAE_TYPE_BFLOAT) ((__nv_bfloat16*)p)[c] = from_f<__nv_bfloat16>(v);
+  else ((__half*)p)[c] = from_f<__half>(v);
+}
+
+// ---- activations ------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+// Exact enough for float32 results: expf and a true division.  (__expf's error grows with |z|.)
+__device__ __forceinline__ float sigmoid_exact(float z) { return __fdiv_rn(1.0f, 1.0f + expf(-z)); }
+
+template <typename T>
+__device__ __forceinline__ float sigmoid_for(float z) { return sizeof(T) == 4 ? sigmoid_exact(z) : sigmoid(z); }
+
+template <typename T, int V>
+__device__ __forceinline__ void activate(float (&z)[V], int act) {
+  if (act == SAE_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] = z[i] < 0.0f ? 0.0f : z[i];          // a NaN stays
+  } else if (act == SAE_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] *= sigmoid_for<T>(z[i]);
+  } else if (act == SAE_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] *= 0.5f * (1.0f + erff(z[i] * 0.70710678f));
+  }
+}
+
+// dz[i] = dy[i] * act'(z[i])
+template <typename T, int V>
+__device__ __forceinline__ void slope(float (&dz)[V], const float (&z)[V], int act) {
+  if (act == SAE_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) dz[i] = z[i] > 0.0f ? dz[i] : 0.0f;
+  } else if (act == SAE_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float s = sigmoid_for<T>(z[i]);
+      dz[i] *= s * (1.0f + z[i] * (1.0f - s));
+    }
+  } else if (act == SAE_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float cdf = 0.5f * (1.0f + erff(z[i] * 0.70710678f));
+      dz[i] *= cdf + z[i] * (0.39894228f * expf(-0.5f * z[i] * z[i]));
+    }
+  }
+}
+
+// ---- what a thread stands for: V channels from c on, pixels p0 + row, p0 + row + rows, .. below p1 ----------------
+struct Place {
+  int n, slice, c, p, p1, rows, row, tid_in;
+  bool on;
+};
+template <int V>
+__device__ __forceinline__ Place place(const Args& a) {
+  Place q;
+  q.n = blockIdx.x / a.slices;
+  q.slice = blockIdx.x - q.n * a.slices;
+  q.rows = GN_THREADS / a.cvt;
+  q.row = threadIdx.x / a.cvt;
+  const int cv = threadIdx.x - q.row * a.cvt;
+  q.c = (blockIdx.y * a.cvt + cv) * V;
+  q.on = q.row < q.rows && q.c < a.C;
+  const int p0 = (int)((long long)a.P * q.slice / a.slices);
+  q.p1 = (int)((long long)a.P * (q.slice + 1) / a.slices);
+  q.p = p0 + q.row;
+  return q;
+}
+
+template <int V>
+struct Channels {                        // a thread's channels: their group's statistics, weight and bias
+  float mean[V], rstd[V], w[V], b[V];
+  __device__ __forceinline__ void load(const Args& a, int n, int c) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int g = (c + i) / a.Cg;
+      mean[i] = a.mean[(long long)n * a.G + g];
+      rstd[i] = a.rstd[(long long)n * a.G + g];
+      w[i] = param(a.w, a.ptype, c + i, 1.0f);
+      b[i] = param(a.b, a.ptype, c + i, 0.0f);
+    }
+  }
+  __device__ __forceinline__ float xhat(int i, float x) const { return __fmul_rn(__fsub_rn(x, mean[i]), rstd[i]); }
+  __device__ __forceinline__ float z(int i, float xh) const { return __fadd_rn(__fmul_rn(xh, w[i]), b[i]); }
+};
+
+// ---- forward, two passes over x -----------------------------------------------------------------------------------
+// A run's count, mean and squares about it; joining two runs by the update of Chan, Golub and LeVeque.
+__device__ __forceinline__ void join(float& n, float& mean, float& m2, float on, float omean, float om2) {
+  if (on == 0.0f) return;
+  const float t = n + on, d = omean - mean, f = on / t;
+  mean = __fmaf_rn(d, f, mean);
+  m2 += om2 + d * d * (n * f);
+  n = t;
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(GN_THREADS) k_gn_statistics(const Args a) {
+  extern __shared__ float sh[];           // [2][V][GN_THREADS], then [GN_THREADS] counts
+  const Place q = place<V>(a);
+  float n = 0.0f, mean[V], m2[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) { mean[i] = 0.0f; m2[i] = 0.0f; }
+  if (q.on) {
+    const T* x = (const T*)a.x + q.n * a.x_n + q.c;
+    for (int p = q.p; p < q.p1; p += GN_BATCH * q.rows) {
+      Raw<T, V> raw[GN_BATCH];
+      float v[GN_BATCH][V];
+      int m = 0;
+#pragma unroll
+      for (int k = 0; k < GN_BATCH; ++k)
+        if (p + k * q.rows < q.p1) { raw[k].load(x + (long long)(p + k * q.rows) * a.x_p); m = k + 1; }
+      // the batch's own mean and squares about it, then joined to what came before
+      const float fm = (float)m, inv = 1.0f / fm, t = n + fm, f = fm / t, nf = n * f;
+#pragma unroll
+      for (int k = 0; k < GN_BATCH; ++k) {
+        if (k < m) raw[k].widen(v[k]);
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float s = v[0][i];
+#pragma unroll
+        for (int k = 1; k < GN_BATCH; ++k) if (k < m) s += v[k][i];
+        const float bm = s * inv;
+        float b2 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < GN_BATCH; ++k) if (k < m) { const float d = v[k][i] - bm; b2 = __fmaf_rn(d, d, b2); }
+        const float d = bm - mean[i];
+        mean[i] = __fmaf_rn(d, f, mean[i]);
+        m2[i] += __fmaf_rn(d * d, nf, b2);
+      }
+      n = t;
+    }
+  }
+  float *sm = sh, *s2 = sh + V * GN_THREADS, *sn = sh + 2 * V * GN_THREADS;
+#pragma unroll
+  for (int i = 0; i < V; ++i) { sm[i * GN_THREADS + threadIdx.x] = mean[i]; s2[i * GN_THREADS + threadIdx.x] = m2[i]; }
+  sn[threadIdx.x] = n;
+  for (int w = q.rows; w > 1;) {          // rows join pairwise, always the same pairs
+    const int half = (w + 1) / 2;
+    __syncthreads();
+    const bool take = q.on && q.row + half < w;
+    if (take) {
+      const int o = threadIdx.x + half * a.cvt;
+      const float on = sn[o];
+      float t = n;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        t = n;
+        join(t, mean[i], m2[i], on, sm[i * GN_THREADS + o], s2[i * GN_THREADS + o]);
+        sm[i * GN_THREADS + threadIdx.x] = mean[i]; s2[i * GN_THREADS + threadIdx.x] = m2[i];
+      }
+      n = t;
+      sn[threadIdx.x] = n;
+    }
+    w = half;
+  }
+  if (q.on && q.row == 0) {
+    const long long at = ((long long)q.n * a.slices + q.slice) * a.C + q.c;
+#pragma unroll
+    for (int i = 0; i < V; ++i) { a.part_a[at + i] = mean[i]; a.part_b[at + i] = m2[i]; }
+  }
+}
+
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+__device__ __forceinline__ int slice_count(const Args& a, int s) {
+  return (int)((long long)a.P * (s + 1) / a.slices) - (int)((long long)a.P * s / a.slices);
+}
+
+// One warp a group: its channels' runs joined about the group's own mean, in double.
+__global__ void __launch_bounds__(GN_THREADS) k_gn_finish_statistics(const Args a) {
+  const long long g = ((long long)blockIdx.x * GN_THREADS + threadIdx.x) >> 5;
+  const int lane = threadIdx.x & 31;
+  if (g >= (long long)a.N * a.G) return;
+  const int n = (int)(g / a.G), j = (int)(g - (long long)n * a.G);
+  const long long base = (long long)n * a.slices * a.C + (long long)j * a.Cg;
+  const int E = a.slices * a.Cg;
+  double s = 0.0, q = 0.0;
+  for (int e = lane; e < E; e += 32) {
+    const int sl = e / a.Cg, c = e - sl * a.Cg;
+    s += (double)slice_count(a, sl) * (double)a.part_a[base + (long long)sl * a.C + c];
+  }
+  const double M = (double)a.P * a.Cg, mean = warp_sum(s) / M;
+  for (int e = lane; e < E; e += 32) {
+    const int sl = e / a.Cg, c = e - sl * a.Cg;
+    const double d = (double)a.part_a[base + (long long)sl * a.C + c] - mean;
+    q += (double)a.part_b[base + (long long)sl * a.C + c] + (double)slice_count(a, sl) * d * d;
+  }
+  const double var = warp_sum(q) / M;
+  if (lane == 0) {
+    a.mean[g] = (float)mean;
+    a.rstd[g] = (float)(1.0 / sqrt(var + (double)a.eps));
+  }
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(GN_THREADS) k_gn_apply(const Args a) {
+  const Place q = place<V>(a);
+  if (!q.on) return;
+  Channels<V> ch;
+  ch.load(a, q.n, q.c);
+  const T* x = (const T*)a.x + q.n * a.x_n + q.c;
+  const T* r = a.res ? (const T*)a.res + q.n * a.r_n + q.c : nullptr;
+  T* y = (T*)a.out + (long long)q.n * a.P * a.C + q.c;
+  for (int p = q.p; p < q.p1; p += GN_BATCH * q.rows) {
+    Raw<T, V> xr[GN_BATCH], rr[GN_BATCH];
+#pragma unroll
+    for (int k = 0; k < GN_BATCH; ++k) {
+      const long long pk = p + (long long)k * q.rows;
+      if (pk < q.p1) { xr[k].load(x + pk * a.x_p); if (r) rr[k].load(r + pk * a.r_p); }
+    }
+#pragma unroll
+    for (int k = 0; k < GN_BATCH; ++k) {
+      const long long pk = p + (long long)k * q.rows;
+      if (pk < q.p1) {
+        float v[V], z[V];
+        xr[k].widen(v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) z[i] = ch.z(i, ch.xhat(i, v[i]));
+        if (r) {
+          rr[k].widen(v);
+#pragma unroll
+          for (int i = 0; i < V; ++i) z[i] = __fadd_rn(z[i], v[i]);
+        }
+        activate<T, V>(z, a.act);
+        Raw<T, V> o;
+        o.round(z);
+        o.store(y + pk * a.C);
+      }
+    }
+  }
+}
+
+// ---- backward, two passes over dy and x ----------------------------------------------------------------------------
+template <typename T, int V>
+__device__ __forceinline__ void grad_z(const Channels<V>& ch, const Raw<T, V>& xr, const Raw<T, V>& dr, const Raw<T, V>* rr, int act,
+                                       float (&xh)[V], float (&dz)[V]) {
+  float v[V], z[V];
+  xr.widen(v);
+  dr.widen(dz);
+#pragma unroll
+  for (int i = 0; i < V; ++i) { xh[i] = ch.xhat(i, v[i]); z[i] = ch.z(i, xh[i]); }
+  if (rr) {
+    rr->widen(v);
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] = __fadd_rn(z[i], v[i]);
+  }
+  slope<T, V>(dz, z, act);
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(GN_THREADS) k_gn_grad_sums(const Args a) {
+  extern __shared__ float sh[];           // [2][V][GN_THREADS]
+  const Place q = place<V>(a);
+  float s[V], sx[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) { s[i] = 0.0f; sx[i] = 0.0f; }
+  if (q.on) {
+    Channels<V> ch;
+    ch.load(a, q.n, q.c);
+    const T* x = (const T*)a.x + q.n * a.x_n + q.c;
+    const T* d = (const T*)a.dy + q.n * a.d_n + q.c;
+    const T* r = a.res ? (const T*)a.res + q.n * a.r_n + q.c : nullptr;
+    T* dres = a.dres ? (T*)a.dres + (long long)q.n * a.P * a.C + q.c : nullptr;
+    for (int p = q.p; p < q.p1; p += GN_BATCH * q.rows) {
+      Raw<T, V> xr[GN_BATCH], dr[GN_BATCH], rr[GN_BATCH];
+#pragma unroll
+      for (int k = 0; k < GN_BATCH; ++k) {
+        const long long pk = p + (long long)k * q.rows;
+        if (pk < q.p1) { xr[k].load(x + pk * a.x_p); dr[k].load(d + pk * a.d_p); if (r) rr[k].load(r + pk * a.r_p); }
+      }
+#pragma unroll
+      for (int k = 0; k < GN_BATCH; ++k) {
+        const long long pk = p + (long long)k * q.rows;
+        if (pk < q.p1) {
+          float xh[V], dz[V];
+          grad_z<T, V>(ch, xr[k], dr[k], r ? &rr[k] : nullptr, a.act, xh, dz);
+#pragma unroll
+          for (int i = 0; i < V; ++i) { s[i] += dz[i]; sx[i] = __fmaf_rn(dz[i], xh[i], sx[i]); }
+          if (dres) { Raw<T, V> o; o.round(dz); o.store(dres + pk * a.C); }
+        }
+      }
+    }
+  }
+  float *s1 = sh, *s2 = sh + V * GN_THREADS;
+#pragma unroll
+  for (int i = 0; i < V; ++i) { s1[i * GN_THREADS + threadIdx.x] = s[i]; s2[i * GN_THREADS + threadIdx.x] = sx[i]; }
+  for (int w = q.rows; w > 1;) {
+    const int half = (w + 1) / 2;
+    __syncthreads();
+    if (q.on && q.row + half < w) {
+      const int o = threadIdx.x + half * a.cvt;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        s[i] += s1[i * GN_THREADS + o]; sx[i] += s2[i * GN_THREADS + o];
+        s1[i * GN_THREADS + threadIdx.x] = s[i]; s2[i * GN_THREADS + threadIdx.x] = sx[i];
+      }
+    }
+    w = half;
+  }
+  if (q.on && q.row == 0) {
+    const long long at = ((long long)q.n * a.slices + q.slice) * a.C + q.c;
+#pragma unroll
+    for (int i = 0; i < V; ++i) { a.part_a[at + i] = s[i]; a.part_b[at + i] = sx[i]; }
+  }
+}
+
+// One warp a group: mean_group(g) and mean_group(g * xhat) from the channels' sums.
+__global__ void __launch_bounds__(GN_THREADS) k_gn_finish_grad(const Args a) {
+  const long long g = ((long long)blockIdx.x * GN_THREADS + threadIdx.x) >> 5;
+  const int lane = threadIdx.x & 31;
+  if (g >= (long long)a.N * a.G) return;
+  const int n = (int)(g / a.G), j = (int)(g - (long long)n * a.G);
+  const long long base = (long long)n * a.slices * a.C + (long long)j * a.Cg;
+  const int E = a.slices * a.Cg;
+  double s = 0.0, q = 0.0;
+  for (int e = lane; e < E; e += 32) {
+    const int sl = e / a.Cg, c = e - sl * a.Cg;
+    const double w = (double)param(a.w, a.ptype, j * a.Cg + c, 1.0f);
+    s += w * (double)a.part_a[base + (long long)sl * a.C + c];
+    q += w * (double)a.part_b[base + (long long)sl * a.C + c];
+  }
+  s = warp_sum(s); q = warp_sum(q);
+  if (lane == 0) {
+    const double M = (double)a.P * a.Cg;
+    a.mean_g[g] = (float)(s / M);
+    a.mean_gx[g] = (float)(q / M);
+  }
+}
+
+// dw and db: the channels' sums over samples and runs, 32 channels a block, in a fixed order.
+__global__ void __launch_bounds__(1024) k_gn_param_grads(const Args a, int rows) {
+  __shared__ float sa[32][33], sb[32][33];
+  const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5, c = blockIdx.x * 32 + cx;
+  float s = 0.0f, q = 0.0f;
+  if (c < a.C)
+    for (int r = ry; r < rows; r += 32) { s += a.part_a[(long long)r * a.C + c]; q += a.part_b[(long long)r * a.C + c]; }
+  sa[ry][cx] = s; sb[ry][cx] = q;
+  __syncthreads();
+  s = sa[cx][ry]; q = sb[cx][ry];         // a warp now holds one channel's 32 sums
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) { s += __shfl_xor_sync(0xffffffffu, s, o); q += __shfl_xor_sync(0xffffffffu, q, o); }
+  const int cc = blockIdx.x * 32 + ry;
+  if (cx == 0 && cc < a.C) {
+    if (a.db) put_param(a.db, a.ptype, cc, s);
+    if (a.dw) put_param(a.dw, a.ptype, cc, q);
+  }
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(GN_THREADS) k_gn_grad_apply(const Args a) {
+  const Place q = place<V>(a);
+  if (!q.on) return;
+  Channels<V> ch;
+  ch.load(a, q.n, q.c);
+  float mg[V], mx[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const long long g = (long long)q.n * a.G + (q.c + i) / a.Cg;
+    mg[i] = a.mean_g[g]; mx[i] = a.mean_gx[g];
+  }
+  const T* x = (const T*)a.x + q.n * a.x_n + q.c;
+  const T* d = (const T*)a.dy + q.n * a.d_n + q.c;
+  const T* r = a.res ? (const T*)a.res + q.n * a.r_n + q.c : nullptr;
+  T* dx = (T*)a.out + (long long)q.n * a.P * a.C + q.c;
+  for (int p = q.p; p < q.p1; p += GN_BATCH * q.rows) {
+    Raw<T, V> xr[GN_BATCH], dr[GN_BATCH], rr[GN_BATCH];
+#pragma unroll
+    for (int k = 0; k < GN_BATCH; ++k) {
+      const long long pk = p + (long long)k * q.rows;
+      if (pk < q.p1) { xr[k].load(x + pk * a.x_p); dr[k].load(d + pk * a.d_p); if (r) rr[k].load(r + pk * a.r_p); }
+    }
+#pragma unroll
+    for (int k = 0; k < GN_BATCH; ++k) {
+      const long long pk = p + (long long)k * q.rows;
+      if (pk < q.p1) {
+        float xh[V], dz[V];
+        grad_z<T, V>(ch, xr[k], dr[k], r ? &rr[k] : nullptr, a.act, xh, dz);
+#pragma unroll
+        for (int i = 0; i < V; ++i) dz[i] = ch.rstd[i] * (__fmul_rn(dz[i], ch.w[i]) - mg[i] - xh[i] * mx[i]);
+        Raw<T, V> o;
+        o.round(dz);
+        o.store(dx + pk * a.C);
+      }
+    }
+  }
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------
+struct Plan {
+  int vec, cvt, ctiles, slices;
+  size_t bytes;
+};
+
+int elem(int type) { return type == SAE_TYPE_FLOAT ? 4 : 2; }
+bool type_ok(int t) { return t == SAE_TYPE_FLOAT || t == SAE_TYPE_BFLOAT || t == SAE_TYPE_HALF; }
+
+bool desc_ok(const sae_group_norm_desc* d) {
+  if (!d || !type_ok(d->type) || !type_ok(d->param_type) || d->activation < SAE_ACT_NONE || d->activation > SAE_ACT_GELU) return false;
+  if (d->samples < 0 || d->samples > (1 << 24) || d->pixels < 0 || d->pixels > (1ll << 30) || d->channels < 1 || d->channels > (1 << 20)) return false;
+  if (d->groups < 1 || d->channels % d->groups || !(d->eps >= 0.0f) || d->samples * d->groups > 0x7fffffffll) return false;
+  const long long s[6] = {d->x_sample, d->x_pixel, d->residual_sample, d->residual_pixel, d->dy_sample, d->dy_pixel};
+  for (long long v : s) if (v < 0) return false;
+  return true;
+}
+
+// Sixteen bytes at a time where every tensor of the call lets it (base, strides and the channel count), else one element.
+int vector_width(const sae_group_norm_desc* d, const void* const* ptrs, int n) {
+  const int es = elem(d->type), V = 16 / es;
+  uintptr_t m = 0;
+  for (int i = 0; i < n; ++i) m |= reinterpret_cast<uintptr_t>(ptrs[i]);
+  const long long s = d->x_sample | d->x_pixel | d->residual_sample | d->residual_pixel | d->dy_sample | d->dy_pixel | d->channels;
+  return (m & 15) == 0 && s % V == 0 ? V : 1;
+}
+
+// The caller's workspace is asked for before the tensors' alignment is known: both widths have to fit in it.
+Plan make_plan(const sae_group_norm_desc* d, int vec, int sms) {
+  Plan p;
+  p.vec = vec;
+  const int cv = (int)((d->channels + vec - 1) / vec);
+  p.ctiles = (cv + GN_THREADS - 1) / GN_THREADS;
+  p.cvt = (cv + p.ctiles - 1) / p.ctiles;
+  const int rows = GN_THREADS / p.cvt;
+  const long long blocks = (long long)d->samples * p.ctiles;
+  // enough blocks to fill the SMs, but at least four batches of pixels for a thread
+  const long long want = std::max<long long>(1, ((long long)sms * 8 + blocks - 1) / std::max<long long>(1, blocks));
+  const long long most = std::max<long long>(1, d->pixels / ((long long)rows * GN_BATCH * 4));
+  p.slices = (int)std::min<long long>(1024, std::min(want, most));
+  p.bytes = (size_t)2 * 4 * ((size_t)d->samples * p.slices * d->channels + (size_t)d->samples * d->groups);
+  return p;
+}
+
+int device_sms() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  return sms;
+}
+
+Args make_args(const sae_group_norm_desc* d, const Plan& p, void* ws) {
+  Args a = {};
+  a.x_n = d->x_sample; a.x_p = d->x_pixel; a.r_n = d->residual_sample; a.r_p = d->residual_pixel; a.d_n = d->dy_sample; a.d_p = d->dy_pixel;
+  a.N = (int)d->samples; a.P = (int)d->pixels; a.C = (int)d->channels; a.G = d->groups; a.Cg = a.C / a.G;
+  a.act = d->activation; a.ptype = d->param_type; a.eps = d->eps;
+  a.slices = p.slices; a.cvt = p.cvt;
+  float* f = (float*)ws;
+  const size_t n = (size_t)a.N * a.slices * a.C, g = (size_t)a.N * a.G;
+  a.part_a = f; a.part_b = f + n; a.mean_g = f + 2 * n; a.mean_gx = f + 2 * n + g;
+  return a;
+}
+
+int launched() {
+  return cudaGetLastError() == cudaSuccess ? SAE_OK : SAE_ERR_CUDA;
+}
+
+template <typename T, int V>
+int forward(const Args& a, const Plan& p, cudaStream_t st) {
+  const dim3 grid((unsigned)(a.N * p.slices), (unsigned)p.ctiles);
+  const long long warps = (long long)a.N * a.G;
+  k_gn_statistics<T, V><<<grid, GN_THREADS, (2 * V + 1) * GN_THREADS * sizeof(float), st>>>(a);
+  k_gn_finish_statistics<<<(unsigned)((warps * 32 + GN_THREADS - 1) / GN_THREADS), GN_THREADS, 0, st>>>(a);
+  k_gn_apply<T, V><<<grid, GN_THREADS, 0, st>>>(a);
+  return launched();
+}
+
+template <typename T, int V>
+int backward(const Args& a, const Plan& p, cudaStream_t st) {
+  const dim3 grid((unsigned)(a.N * p.slices), (unsigned)p.ctiles);
+  const long long warps = (long long)a.N * a.G;
+  k_gn_grad_sums<T, V><<<grid, GN_THREADS, 2 * V * GN_THREADS * sizeof(float), st>>>(a);
+  k_gn_finish_grad<<<(unsigned)((warps * 32 + GN_THREADS - 1) / GN_THREADS), GN_THREADS, 0, st>>>(a);
+  if (a.dw || a.db) k_gn_param_grads<<<(unsigned)((a.C + 31) / 32), 1024, 0, st>>>(a, a.N * a.slices);
+  k_gn_grad_apply<T, V><<<grid, GN_THREADS, 0, st>>>(a);
+  return launched();
+}
+
+// An element type and a vector width as template arguments.
+#define GN_DISPATCH(fn, type, vec, ...)                                                                               \
+  ((type) == SAE_TYPE_FLOAT ? ((vec) > 1 ? fn<float, 4>(__VA_ARGS__) : fn<float, 1>(__VA_ARGS__))                      \
+   : (type) == SAE_TYPE_BFLOAT ? ((vec) > 1 ? fn<__nv_bfloat16, 8>(__VA_ARGS__) : fn<__nv_bfloat16, 1>(__VA_ARGS__))   \
+                               : ((vec) > 1 ? fn<__half, 8>(__VA_ARGS__) : fn<__half, 1>(__VA_ARGS__)))
+
+bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+
+}  // namespace
+
+extern "C" {
+
+int64_t sae_group_norm_workspace(const sae_group_norm_desc* d) {
+  if (!desc_ok(d)) return -1;
+  const int sms = device_sms();
+  if (sms < 1) return -1;
+  if (d->samples == 0 || d->pixels == 0) return 0;
+  return (int64_t)std::max(make_plan(d, 16 / elem(d->type), sms).bytes, make_plan(d, 1, sms).bytes);
+}
+
+int sae_group_norm_forward(const sae_group_norm_desc* d, const void* x, const void* residual, const void* weight, const void* bias,
+                           void* y, float* mean, float* rstd, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!desc_ok(d)) return SAE_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (d->samples == 0) return SAE_OK;
+  if (!mean || !rstd) return SAE_ERR_INVALID_ARG;
+  if (d->pixels == 0) {                     // the mean of nothing
+    const size_t g = (size_t)d->samples * d->groups * sizeof(float);
+    return cudaMemsetAsync(mean, 0xff, g, st) == cudaSuccess && cudaMemsetAsync(rstd, 0xff, g, st) == cudaSuccess ? SAE_OK : SAE_ERR_CUDA;
+  }
+  const int es = elem(d->type);
+  if (!x || !y || !aligned_to(x, es) || !aligned_to(y, es) || !aligned_to(residual, es) || !aligned_to(weight, elem(d->param_type)) ||
+      !aligned_to(bias, elem(d->param_type))) return SAE_ERR_INVALID_ARG;
+  const int sms = device_sms();
+  if (sms < 1) return SAE_ERR_CUDA;
+  const void* ptrs[3] = {x, y, residual};
+  const Plan p = make_plan(d, vector_width(d, ptrs, 3), sms);
+  if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < p.bytes || (long long)d->samples * p.slices > 0x7fffffffll) return SAE_ERR_INVALID_ARG;
+  Args a = make_args(d, p, workspace);
+  a.x = x; a.res = residual; a.w = weight; a.b = bias; a.out = y; a.mean = mean; a.rstd = rstd;
+  return GN_DISPATCH(forward, d->type, p.vec, a, p, st);
+}
+
+int sae_group_norm_backward(const sae_group_norm_desc* d, const void* dy, const void* x, const void* residual, const float* mean,
+                            const float* rstd, const void* weight, const void* bias, void* dx, void* dresidual, void* dweight,
+                            void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!desc_ok(d)) return SAE_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (d->samples == 0 || d->pixels == 0) {  // sums of nothing
+    const size_t c = (size_t)d->channels * elem(d->param_type);
+    if (dweight && cudaMemsetAsync(dweight, 0, c, st) != cudaSuccess) return SAE_ERR_CUDA;
+    if (dbias && cudaMemsetAsync(dbias, 0, c, st) != cudaSuccess) return SAE_ERR_CUDA;
+    return SAE_OK;
+  }
+  const int es = elem(d->type), ps = elem(d->param_type);
+  if (!dy || !x || !mean || !rstd || !dx || !aligned_to(dy, es) || !aligned_to(x, es) || !aligned_to(residual, es) || !aligned_to(dx, es) ||
+      !aligned_to(dresidual, es) || !aligned_to(weight, ps) || !aligned_to(bias, ps) || !aligned_to(dweight, ps) || !aligned_to(dbias, ps))
+    return SAE_ERR_INVALID_ARG;
+  const int sms = device_sms();
+  if (sms < 1) return SAE_ERR_CUDA;
+  const void* ptrs[5] = {dy, x, residual, dx, dresidual};
+  const Plan p = make_plan(d, vector_width(d, ptrs, 5), sms);
+  if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < p.bytes || (long long)d->samples * p.slices > 0x7fffffffll) return SAE_ERR_INVALID_ARG;
+  Args a = make_args(d, p, workspace);
+  a.x = x; a.dy = dy; a.res = residual; a.w = weight; a.b = bias; a.out = dx; a.dres = dresidual; a.dw = dweight; a.db = dbias;
+  a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
+  return GN_DISPATCH(backward, d->type, p.vec, a, p, st);
+}
+
+}  // extern "C"

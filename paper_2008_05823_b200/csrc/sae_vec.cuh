@@ -1,0 +1,71 @@
+// Vectors of 1 to 8 elements of float, bfloat16 or half in registers: loads, stores, widening to float and rounding back.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace sae {
+
+template <int BYTES> struct Bits;
+template <> struct Bits<2> { typedef unsigned short type; };
+template <> struct Bits<4> { typedef unsigned int type; };
+template <> struct Bits<8> { typedef uint2 type; };
+template <> struct Bits<16> { typedef uint4 type; };
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
+
+// Two 16-bit elements of one word; a bfloat16 is the upper half of its float.
+__device__ __forceinline__ float2 widen2(unsigned int w, const __nv_bfloat16*) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ float2 widen2(unsigned int w, const __half*) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ unsigned int round2(float a, float b, const __nv_bfloat16*) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const unsigned int*>(&v);
+}
+__device__ __forceinline__ unsigned int round2(float a, float b, const __half*) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const unsigned int*>(&v);
+}
+
+// V elements as they lie in memory; V * sizeof(T) is 2, 4, 8 or 16 bytes and the address a multiple of it.
+template <typename T, int V>
+struct Raw {
+  typedef typename Bits<V * (int)sizeof(T)>::type B;
+  B b;
+  __device__ __forceinline__ void load(const T* p) { b = __ldg(reinterpret_cast<const B*>(p)); }
+  __device__ __forceinline__ void load_stream(const T* p) { b = __ldcs(reinterpret_cast<const B*>(p)); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<B*>(p) = b; }
+  __device__ __forceinline__ void store_stream(T* p) const { __stcs(reinterpret_cast<B*>(p), b); }
+  __device__ __forceinline__ void widen(float (&v)[V]) const {
+    if constexpr (sizeof(T) == 4 || V == 1) {
+      const T* e = reinterpret_cast<const T*>(&b);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = to_f(e[i]);
+    } else {
+      const unsigned int* w = reinterpret_cast<const unsigned int*>(&b);
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) { const float2 f = widen2(w[i], (const T*)nullptr); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
+    }
+  }
+  __device__ __forceinline__ void round(const float (&v)[V]) {
+    if constexpr (sizeof(T) == 4 || V == 1) {
+      T* e = reinterpret_cast<T*>(&b);
+#pragma unroll
+      for (int i = 0; i < V; ++i) e[i] = from_f<T>(v[i]);
+    } else {
+      unsigned int* w = reinterpret_cast<unsigned int*>(&b);
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) w[i] = round2(v[2 * i], v[2 * i + 1], (const T*)nullptr);
+    }
+  }
+};
+
+}  // namespace sae
