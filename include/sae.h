@@ -331,7 +331,8 @@ int64_t sae_noalloc_max_elements(void);
  *
  *   norm_k = (sum over row k of |g|^q)^(1/q), q = 1 or 2, or the largest |g|;   coef_k = min(1, max_norm / (norm_k + 1e-6))
  *   sae_grads_norm    norms[k] = norm_k
- *   sae_grads_clip    g *= coef_k, in place, each element rounded once to its type
+ *   sae_grads_clip    g *= coef_k, in place, each element rounded once to its type.  A 16-bit tensor takes coef_k rounded to
+ *                     its own type (as long as that is a normal number there), as torch's in-place clipping does
  *   sae_grads_pack    out[k][0..d) = coef_k * (the row's T tensors, concatenated in list order), the caller layout of sae_step
  *   sae_grads_unpack  the T tensors of row k = in[k][0..d), rounded to their types (the step-ahead point back to a model)
  *
@@ -397,7 +398,7 @@ void sae_grads_destroy(sae_grads *h);
  * y, dx, dresidual: type `type`, without gaps; they must not overlap any input.  weight, bias, dweight, dbias: `channels`
  *   values of type `param_type`; weight NULL = 1, bias NULL = 0.  residual NULL = none; dresidual, dweight, dbias NULL = not wanted.
  * mean, rstd: [samples][groups] floats, written by the forward call, read by the backward call.
- * workspace: at least sae_group_norm_workspace(desc) bytes, 16-byte aligned, the call's own until it has run.
+ * workspace: at least sae_group_norm_workspace(desc, ..) bytes, 16-byte aligned, the call's own until it has run.
  * Arithmetic is in float (statistics and sums joined in double), one rounding to `type` at each output; z is the same bits
  * in both directions, so relu's mask (z > 0) is the forward call's.  The sums' order is fixed: same input, same bits.
  * samples or pixels = 0: mean and rstd are NaN (0 / 0), dweight and dbias 0.
@@ -420,8 +421,9 @@ typedef struct {
   float eps;                          /* >= 0                                                                 */
 } sae_group_norm_desc;
 
-/* Bytes of workspace either call needs on the current device; -1 for a bad description or without a device. */
-int64_t sae_group_norm_workspace(const sae_group_norm_desc *desc);
+/* Bytes of workspace the forward (backward = 0) or backward call needs on the current device, 0: none, NULL will do;
+ * -1 for a bad description or without a device. */
+int64_t sae_group_norm_workspace(const sae_group_norm_desc *desc, int32_t backward);
 int sae_group_norm_forward(const sae_group_norm_desc *desc, const void *x, const void *residual, const void *weight,
                            const void *bias, void *y, float *mean, float *rstd, void *workspace, size_t workspace_bytes,
                            void *stream);

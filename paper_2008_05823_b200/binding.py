@@ -128,12 +128,30 @@ def lib():
         L.sae_grads_last_cuda_error.argtypes = [vp]
         L.sae_grads_destroy.argtypes = [vp]
         L.sae_grads_destroy.restype = None
-        L.sae_group_norm_workspace.argtypes = [C.POINTER(SaeGroupNormDesc)]
+        L.sae_group_norm_workspace.argtypes = [C.POINTER(SaeGroupNormDesc), i32]
         L.sae_group_norm_workspace.restype = i64
         L.sae_group_norm_forward.argtypes = [C.POINTER(SaeGroupNormDesc)] + [vp] * 8 + [C.c_size_t, vp]
         L.sae_group_norm_backward.argtypes = [C.POINTER(SaeGroupNormDesc)] + [vp] * 12 + [C.c_size_t, vp]
         _lib = L
     return _lib
+
+
+_host = None
+
+
+def host():
+    """The C++ side of `grads` and `group_norm` (argument checks and allocation against torch), built beside libsae.so."""
+    global _host
+    if _host is None:
+        lib()
+        try:
+            import torch  # noqa: F401  (its libraries are what the module links to)
+            from . import _host as module
+        except ImportError as e:
+            raise RuntimeError("_host.so is missing or does not fit this torch: run `python -m paper_2008_05823_b200.build --force`; "
+                               "there is no fallback path") from e
+        _host = module
+    return _host
 
 
 def _check(status, what, handle=None):

@@ -2,6 +2,7 @@
 
   libsae.so        -- the C-ABI library declared in include/sae.h
   libsae_synth.so  -- the seeded synthetic-gradient generator used by tests and the benchmark
+  _host.so         -- the Python side of gradient sets and group norm (argument checks, allocation), C++ against torch
 
 Usage: python -m paper_2008_05823_b200.build [--force] [--verbose]
 """
@@ -19,7 +20,22 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 TARGETS = {
     "libsae.so": (["sae.cu", "sae_noalloc.cu", "sae_grads.cu", "sae_group_norm.cu"], ["sae_vec.cuh", "sae_kernels.cuh", "sae_worker_tma.cuh", "sae_worker_fused.cuh", "sae_worker_small.cuh", "sae_topk.cuh", "sae_shard_topk.cuh", "sae_device.cuh", os.path.join(INCLUDE, "sae.h")]),
     "libsae_synth.so": (["synth_gen.cu"], []),
+    "_host.so": (["host_torch.cpp"], [os.path.join(INCLUDE, "sae.h")]),
 }
+
+
+def _host_command(out, sources):
+    """g++ against the installed torch's headers; libsae.so is found beside the module."""
+    import sysconfig
+    from torch.utils import cpp_extension
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-DTORCH_EXTENSION_NAME=_host"]
+    for inc in cpp_extension.include_paths() + [os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]:
+        cmd += ["-isystem", inc]
+    cmd += ["-o", out] + sources + ["-L" + HERE, "-l:libsae.so", "-Wl,-rpath,$ORIGIN"]
+    for lib in cpp_extension.library_paths() + [os.path.join(cuda, "lib64")]:
+        cmd.append("-L" + lib)
+    return cmd + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python", "-lcudart"]
 
 
 def _stale(out, deps):
@@ -38,6 +54,10 @@ def build(force: bool = False, verbose: bool = False):
         dep_paths = src_paths + [h if os.path.isabs(h) else os.path.join(CSRC, h) for h in hdrs]
         if force or _stale(out, dep_paths):
             extra = os.environ.get("SAE_NVCC_EXTRA", "").split()
+            if src_paths[0].endswith(".cpp"):
+                subprocess.check_call(_host_command(out, src_paths))
+                outs.append(out)
+                continue
             cmd = [nvcc] + NVCC_FLAGS + extra + (["-Xptxas", "-v"] if verbose else []) + ["-o", out] + src_paths
             subprocess.check_call(cmd)
         outs.append(out)

@@ -238,10 +238,17 @@ __device__ __forceinline__ void tile_scale(const S* s, D* d, u32 cnt, float coef
 
 enum { MODE_CLIP, MODE_PACK, MODE_UNPACK };
 
+// In place, a 16-bit tensor is scaled by the coefficient rounded to its own type, which is what torch's in-place product with
+// a scalar tensor does: replacing a torch clipping changes no bit.  Not below the type's normal numbers (a half's end at
+// 2^-14), where the rounding would cost digits or leave zero.
+template <typename T> __device__ __forceinline__ float coef_for(float c) { return c; }
+template <> __device__ __forceinline__ float coef_for<__nv_bfloat16>(float c) { return c >= 1.17549435e-38f ? to_f(from_f<__nv_bfloat16>(c)) : c; }
+template <> __device__ __forceinline__ float coef_for<__half>(float c) { return c >= 6.103515625e-5f ? to_f(from_f<__half>(c)) : c; }
+
 template <int MODE, typename T>
 __device__ __forceinline__ void tile_move(void* base, const Tile& ti, float* vec, float coef) {
   T* g = (T*)base + ti.start;
-  if (MODE == MODE_CLIP) tile_scale<T, T>(g, g, ti.count, coef);
+  if (MODE == MODE_CLIP) tile_scale<T, T>(g, g, ti.count, coef_for<T>(coef));
   else if (MODE == MODE_PACK) tile_scale<T, float>(g, vec + ti.at, ti.count, coef);
   else tile_scale<float, T>(vec + ti.at, g, ti.count, 1.0f);
 }

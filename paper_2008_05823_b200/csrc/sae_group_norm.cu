@@ -541,7 +541,8 @@ bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(
 
 extern "C" {
 
-int64_t sae_group_norm_workspace(const sae_group_norm_desc* d) {
+int64_t sae_group_norm_workspace(const sae_group_norm_desc* d, int32_t backward) {
+  (void)backward;
   if (!desc_ok(d)) return -1;
   const int sms = device_sms();
   if (sms < 1) return -1;

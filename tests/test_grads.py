@@ -4,7 +4,8 @@ float64 computation.
 Tolerances, with u = 2^-24: eight squares (or magnitudes) are summed in float, at most 8 roundings of positive terms,
 then in double, so a sum is within 8u and its square root within 4u; rounding the norm to float adds u.  The scale
 is taken from the double norm (8u for q = 1) and rounded (u); the product rounds once more: u to float32, 2^-8 to
-bfloat16, 2^-11 to float16 (half a unit of the last place, relative), or half the smallest subnormal, absolute."""
+bfloat16, 2^-11 to float16 (half a unit of the last place, relative), or half the smallest subnormal, absolute.  Clipping
+in place rounds the scale to the tensor's type as well: once more the same."""
 import ctypes as C
 import math
 
@@ -90,10 +91,10 @@ def assert_norms(got, rows, q):
         assert abs(got[k] - want) <= (SUM_TOL[q] + U) * want, (k, got[k], want)
 
 
-def assert_scaled(got, before, scale, dtype, q):
-    """got ~ before * scale, rounded once to dtype."""
+def assert_scaled(got, before, scale, dtype, q, in_place=False):
+    """got ~ before * scale, rounded once to dtype; in place the scale is rounded to dtype too."""
     want = before * scale
-    tol = np.abs(want) * (SUM_TOL[q] + 2 * U + ROUND[dtype]) + TINY[dtype]
+    tol = np.abs(want) * (SUM_TOL[q] + 2 * U + (2 if in_place else 1) * ROUND[dtype]) + TINY[dtype]
     bad = np.abs(got - want) > tol
     assert not bad.any(), (np.flatnonzero(bad)[:5], got[bad][:5], want[bad][:5])
 
@@ -166,9 +167,30 @@ def test_norm_pack_clip_unpack(case, q):
         assert abs(float(got[k]) - norms[k]) <= (SUM_TOL[q] + U) * norms[k]
         at = 0
         for t, dt in zip(rows[k], dtypes):
-            assert_scaled(t.double().cpu().numpy(), before[k][at:at + t.numel()], coef64(norms[k], max_norm), dt, q)
+            assert_scaled(t.double().cpu().numpy(), before[k][at:at + t.numel()], coef64(norms[k], max_norm), dt, q, in_place=True)
             at += t.numel()
     s.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("share", [0.3, 0.7, 0.9999, 1.5, 1e-7])
+def test_clip_has_the_bits_of_a_product_in_place(dtype, share):
+    """The tensors after clip_ are those of torch's in-place product with the float32 coefficient (here of the same norm)."""
+    row = make(1, [7, 8192, 30011], [dtype] * 3, 8)[0]
+    s = gset(1, [7, 8192, 30011], [dtype] * 3)
+    norm = s.norm(row)
+    max_norm = share * float(norm)
+    want = [t.clone() for t in row]
+    coef = (max_norm / (norm.double() + 1e-6)).clamp(max=1.0).float()[0]
+    if share > 1e-6 or dtype != F16:                   # below a half's normal numbers the coefficient stays as it is
+        for t in want:
+            t.mul_(coef)
+    else:
+        want = [(t.float() * coef).half() for t in want]
+    s.clip_(row, max_norm)
+    near = torch.equal if dtype != F32 else (lambda a, b: torch.allclose(a, b, rtol=(4 + 3) * U, atol=0))
+    assert all(near(a, b) for a, b in zip(row, want))
 
 
 @pytest.mark.gpu

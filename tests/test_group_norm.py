@@ -42,7 +42,7 @@ BAD = [dict(type=3), dict(type=-1), dict(param_type=5), dict(activation=4), dict
 def test_bad_descriptions_are_refused(kw):
     L, p = sb.lib(), C.c_void_p(256)          # never dereferenced: the checks fail first
     d = C.byref(desc(**kw))
-    assert L.sae_group_norm_workspace(d) == -1
+    assert L.sae_group_norm_workspace(d, 0) == -1
     assert L.sae_group_norm_forward(d, p, None, p, p, p, p, p, p, 1 << 20, None) == sb.ERR_INVALID_ARG
     assert L.sae_group_norm_backward(d, p, p, None, p, p, p, p, p, None, p, p, p, 1 << 20, None) == sb.ERR_INVALID_ARG
 
@@ -50,7 +50,7 @@ def test_bad_descriptions_are_refused(kw):
 def test_null_and_misaligned_pointers_are_refused():
     L, p, odd = sb.lib(), C.c_void_p(256), C.c_void_p(258)
     d = C.byref(desc())
-    assert L.sae_group_norm_workspace(None) == -1
+    assert L.sae_group_norm_workspace(None, 1) == -1
     for i in (0, 4, 5, 6):
         args = [p, None, p, p, p, p, p, p]
         args[i] = None
