@@ -16,8 +16,10 @@
 #include "sae_vec.cuh"
 
 #include <algorithm>
+#include <cooperative_groups.h>
 
 using namespace sae;
+namespace cg = cooperative_groups;
 
 namespace {
 
@@ -63,7 +65,7 @@ template <typename T, int V>
 __device__ __forceinline__ void activate(float (&z)[V], int act) {
   if (act == SAE_ACT_RELU) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) z[i] = z[i] < 0.0f ? 0.0f : z[i];          // a NaN stays
+    for (int i = 0; i < V; ++i) asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(z[i]) : "f"(z[i]));
   } else if (act == SAE_ACT_SILU) {
 #pragma unroll
     for (int i = 0; i < V; ++i) z[i] *= sigmoid_for<T>(z[i]);
@@ -439,10 +441,368 @@ __global__ void __launch_bounds__(GN_THREADS) k_gn_grad_apply(const Args a) {
   }
 }
 
+// ---- one pass: a unit (a sample's channels of one or more whole groups) stays in shared memory --------------------
+// A cluster of S blocks takes a unit, each its run of pixels.  Every thread copies its own vectors into shared memory
+// asynchronously (slots that nobody else reads: no barrier for the data), so the inputs are read from HBM once; the
+// blocks' sums meet through distributed shared memory.
+struct Unit {
+  int log_cvt;                           // vectors of a pixel that stand side by side in a block: a power of two
+  int cc, chunks;                        // channels of a unit (whole groups, whole vectors); units a sample has
+  int px, S;                             // pixels a block takes; blocks of a cluster
+  int slots;                             // vectors a thread holds of each tensor
+};
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+  const unsigned int s = (unsigned int)__cvta_generic_to_shared(to);
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(from) : "memory");
+  else if constexpr (BYTES >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(s), "l"(from), "n"(BYTES) : "memory");
+  else *(unsigned short*)to = __ldg((const unsigned short*)from);
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A thread's `turns` vectors, `step` elements apart, into its slots.
+template <typename T, int V>
+__device__ __forceinline__ void fetch(typename Raw<T, V>::B* to, const T* from, long long step, int pitch, int turns) {
+#pragma unroll 4
+  for (int k = 0; k < turns; ++k, from += step) copy_async<V * (int)sizeof(T)>(to + k * pitch, from);
+}
+
+// A thread's V channel sums as one, or as they are.
+template <int V, int SL>
+__device__ __forceinline__ void narrow(const float (&v)[V], float (&o)[SL]) {
+  if constexpr (SL == V) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = v[i];
+  } else {
+    float t = v[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) t += v[i];
+    o[0] = t;
+  }
+}
+
+// Adds up v over the rows of a block, column by column: afterwards sh[r * pitch + column * SL + i] holds the sums of row r's
+// warp (columns fewer than a warp's lanes: those are joined here) and `rows` such rows are left to add.  Ends with a barrier.
+template <int SL>
+__device__ __forceinline__ int fold_rows(float (&v)[SL], float* sh, int log_cvt) {
+  const int cvt = 1 << log_cvt, tid = threadIdx.x;
+  int rows = (int)blockDim.x >> log_cvt, row = tid >> log_cvt;
+  bool write = true;
+  if (log_cvt < 5) {
+    for (int o = 16; o >= cvt; o >>= 1) {
+#pragma unroll
+      for (int i = 0; i < SL; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    }
+    rows = (int)blockDim.x >> 5;
+    row = tid >> 5;
+    write = (tid & 31) < cvt;
+  }
+  if (write) {
+    float* to = sh + (row * cvt + (tid & (cvt - 1))) * SL;
+#pragma unroll
+    for (int i = 0; i < SL; ++i) to[i] = v[i];
+  }
+  __syncthreads();
+  return rows;
+}
+
+// The folded values of each group: one warp a group, `per` neighbouring values of it in a row.  out[j] is written by lane 0.
+template <typename F>
+__device__ __forceinline__ void fold_groups(const float* sh, int rows, int pitch, int per, int groups, F out) {
+  const int lane = threadIdx.x & 31;
+  const float inv_per = 1.0f / (float)per;
+  for (int j = threadIdx.x >> 5; j < groups; j += (int)blockDim.x >> 5) {
+    float s = 0.0f;
+    for (int e = lane; e < rows * per; e += 32) {
+      const int r = (int)(((float)e + 0.5f) * inv_per);
+      s += sh[r * pitch + j * per + (e - r * per)];
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0) out(j, s);
+  }
+}
+
+// V neighbouring parameters at once: c is a multiple of V, and the parameters' own alignment is checked here.
+template <int V>
+__device__ __forceinline__ void params(const void* p, int type, int c, float none, float (&o)[V]) {
+  if (!p) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = none;
+  } else if (V >= 4 && type == SAE_TYPE_FLOAT && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+#pragma unroll
+    for (int i = 0; i + 3 < V; i += 4) {
+      const float4 f = __ldg(reinterpret_cast<const float4*>((const float*)p + c + i));
+      o[i] = f.x; o[i + 1] = f.y; o[i + 2] = f.z; o[i + 3] = f.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = param(p, type, c + i, none);
+  }
+}
+
+// Small non-negative integers (below 2^20) over a divisor, by its reciprocal.
+__device__ __forceinline__ int quotient(int a, float inv) { return (int)(((float)a + 0.5f) * inv); }
+
+// WHOLE: a vector lies within one group, so one value a thread is enough for a statistic; else one a channel.
+template <typename T, int V, bool WHOLE>
+__global__ void __launch_bounds__(GN_THREADS, 3) k_gn_unit(const Args a, const Unit u) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  typedef typename Raw<T, V>::B B;
+  constexpr int SL = WHOLE ? 1 : V;
+  const int TH = blockDim.x, tid = threadIdx.x, cvt = 1 << u.log_cvt, rows = TH >> u.log_cvt, row = tid >> u.log_cvt;
+  const int rank = blockIdx.x % u.S, unit = blockIdx.x / u.S, n = unit / u.chunks, c0 = (unit - n * u.chunks) * u.cc;
+  const int cc = min(u.cc, a.C - c0), groups = cc / a.Cg, co = (tid & (cvt - 1)) * V, c = c0 + co;
+  const int p0 = rank * u.px, all = max(0, min(u.px, a.P - p0)), cnt = co < cc ? all : 0;
+  const int turns = cnt > row ? (cnt - row - 1) / rows + 1 : 0;                 // vectors this thread has
+  const float inv_cg = 1.0f / (float)a.Cg;
+  B* const xs = (B*)smem + tid;                                                 // slot k at k * TH
+  B* const rs = xs + u.slots * TH;
+  float* sh = (float*)((B*)smem + (size_t)u.slots * TH * (a.res ? 2 : 1));      // [rows or warps][cvt * SL]
+  float2* stat = (float2*)(sh + (u.log_cvt < 5 ? TH >> 5 : rows) * cvt * SL);   // [groups]: mean and squares, then mean and rstd
+  float2* mine = stat + u.cc / a.Cg;                                            // [groups]: what the cluster's others read
+  fetch<T, V>(xs, (const T*)a.x + n * a.x_n + (p0 + row) * a.x_p + c, rows * a.x_p, TH, turns);
+  copies_commit();
+  if (a.res) fetch<T, V>(rs, (const T*)a.res + n * a.r_n + (p0 + row) * a.r_p + c, rows * a.r_p, TH, turns);
+  copies_commit();
+  float w[V], b[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) { w[i] = 0.0f; b[i] = 0.0f; }
+  if (co < cc) { params<V>(a.w, a.ptype, c, 1.0f, w); params<V>(a.b, a.ptype, c, 0.0f, b); }
+  // the block's mean of each group
+  float acc[V], fold[SL];
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+  copies_wait<1>();
+#pragma unroll 4
+  for (int k = 0; k < turns; ++k) {
+    float v[V];
+    Raw<T, V> r;
+    r.b = xs[k * TH];
+    r.widen(v);
+    vadd<V>(acc, acc, v);
+  }
+  const int per = WHOLE ? a.Cg / V : a.Cg, pitch = cvt * SL;
+  narrow<V, SL>(acc, fold);
+  int left = fold_rows<SL>(fold, sh, u.log_cvt);
+  const float inv = all > 0 ? 1.0f / ((float)all * (float)a.Cg) : 0.0f;
+  fold_groups(sh, left, pitch, per, groups, [&](int j, float s) { stat[j].x = s * inv; });
+  __syncthreads();
+  // the squares about it
+  Per<V, WHOLE> mean, rstd;
+  mean.set([&](int i) { return co < cc ? stat[quotient(co + i, inv_cg)].x : 0.0f; });
+  float less[V];
+  mean.all(less);
+#pragma unroll
+  for (int i = 0; i < V; ++i) { less[i] = -less[i]; acc[i] = 0.0f; }
+#pragma unroll 4
+  for (int k = 0; k < turns; ++k) {
+    float v[V];
+    Raw<T, V> r;
+    r.b = xs[k * TH];
+    r.widen(v);
+    vadd<V>(v, v, less);
+    vfma<V>(acc, v, v, acc);
+  }
+  narrow<V, SL>(acc, fold);
+  left = fold_rows<SL>(fold, sh, u.log_cvt);
+  fold_groups(sh, left, pitch, per, groups, [&](int j, float s) { mine[j] = make_float2(stat[j].x, s); });
+  // joined over the cluster
+  cg::cluster_group cluster = cg::this_cluster();
+  if (u.S > 1) cluster.sync(); else __syncthreads();
+  const float M = (float)a.P * (float)a.Cg;
+  for (int j = tid; j < groups; j += TH) {
+    float2 r = mine[j];
+    if (u.S > 1) {
+      float s = 0.0f;
+      for (int k = 0; k < u.S; ++k) s += (float)max(0, min(u.px, a.P - k * u.px)) * cluster.map_shared_rank(mine, k)[j].x;
+      const float m = s * (float)a.Cg / M;
+      float q = 0.0f;
+      for (int k = 0; k < u.S; ++k) {
+        const float2 o = cluster.map_shared_rank(mine, k)[j];
+        const float d = o.x - m;
+        q += o.y + (float)max(0, min(u.px, a.P - k * u.px)) * (float)a.Cg * d * d;
+      }
+      r = make_float2(m, q);
+    }
+    r.y = __fdiv_rn(1.0f, __fsqrt_rn(r.y / M + a.eps));
+    stat[j] = r;
+    if (rank == 0) { const long long g = (long long)n * a.G + c0 / a.Cg + j; a.mean[g] = r.x; a.rstd[g] = r.y; }
+  }
+  __syncthreads();
+  if (u.S > 1) cluster.barrier_arrive();            // this block has read what it needs of the others
+  copies_wait<0>();
+  mean.set([&](int i) { return co < cc ? stat[quotient(co + i, inv_cg)].x : 0.0f; });
+  rstd.set([&](int i) { return co < cc ? stat[quotient(co + i, inv_cg)].y : 0.0f; });
+  float scale[V];
+  mean.all(less);
+  rstd.all(scale);
+#pragma unroll
+  for (int i = 0; i < V; ++i) less[i] = -less[i];
+  T* y = (T*)a.out + ((long long)n * a.P + p0 + row) * a.C + c;
+  const long long step = (long long)rows * a.C;
+  const int act = a.act;
+#pragma unroll 2
+  for (int k = 0; k < turns; ++k, y += step) {
+    float z[V];
+    Raw<T, V> r;
+    r.b = xs[k * TH];
+    r.widen(z);
+    vadd<V>(z, z, less);
+    vmul<V>(z, z, scale);
+    vmul<V>(z, z, w);
+    vadd<V>(z, z, b);
+    if (a.res) {
+      float v[V];
+      r.b = rs[k * TH];
+      r.widen(v);
+      vadd<V>(z, z, v);
+    }
+    activate<T, V>(z, act);
+    r.round(z);
+    r.store(y);
+  }
+  if (u.S > 1) cluster.barrier_wait();              // nobody leaves while another may still read its sums
+}
+
+// What both passes of the backward unit kernel make of a vector: xhat and dz.
+template <typename T, int V>
+__device__ __forceinline__ void unit_grad(Raw<T, V> x, Raw<T, V> d, const typename Raw<T, V>::B* res, const float (&less)[V], const float (&scale)[V],
+                                          const float (&w)[V], const float (&b)[V], int act, float (&xh)[V], float (&dz)[V]) {
+  float z[V];
+  x.widen(xh);
+  d.widen(dz);
+  vadd<V>(xh, xh, less);
+  vmul<V>(xh, xh, scale);
+  if (act == SAE_ACT_NONE) return;
+  vmul<V>(z, xh, w);
+  vadd<V>(z, z, b);
+  if (res) {
+    Raw<T, V> r;
+    float v[V];
+    r.b = *res;
+    r.widen(v);
+    vadd<V>(z, z, v);
+  }
+  slope<T, V>(dz, z, act);
+}
+
+template <typename T, int V, bool WHOLE>
+__global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_unit(const Args a, const Unit u) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  typedef typename Raw<T, V>::B B;
+  const int TH = blockDim.x, tid = threadIdx.x, cvt = 1 << u.log_cvt, rows = TH >> u.log_cvt, row = tid >> u.log_cvt;
+  const int rank = blockIdx.x % u.S, unit = blockIdx.x / u.S, n = unit / u.chunks, c0 = (unit - n * u.chunks) * u.cc;
+  const int cc = min(u.cc, a.C - c0), groups = cc / a.Cg, co = (tid & (cvt - 1)) * V, c = c0 + co;
+  const int p0 = rank * u.px, cnt = co < cc ? max(0, min(u.px, a.P - p0)) : 0;
+  const int turns = cnt > row ? (cnt - row - 1) / rows + 1 : 0;
+  const float inv_cg = 1.0f / (float)a.Cg;
+  B* const xs = (B*)smem + tid;
+  B* const ds = xs + u.slots * TH;
+  B* const rs = ds + u.slots * TH;
+  float* sh = (float*)((B*)smem + (size_t)u.slots * TH * (a.res ? 3 : 2));      // [rows or warps][cvt * V], twice
+  const int span = (u.log_cvt < 5 ? TH >> 5 : rows) * cvt * V;
+  float2* mine = (float2*)(sh + 2 * span);                                      // [cc]: the block's sums of each channel
+  float2* chan = mine + u.cc;                                                   // [cc]: the unit's, times the weight
+  float2* grp = chan + u.cc;                                                    // [groups]: the two means
+  fetch<T, V>(xs, (const T*)a.x + n * a.x_n + (p0 + row) * a.x_p + c, rows * a.x_p, TH, turns);
+  fetch<T, V>(ds, (const T*)a.dy + n * a.d_n + (p0 + row) * a.d_p + c, rows * a.d_p, TH, turns);
+  if (a.res) fetch<T, V>(rs, (const T*)a.res + n * a.r_n + (p0 + row) * a.r_p + c, rows * a.r_p, TH, turns);
+  copies_commit();
+  Per<V, WHOLE> mean, rstd;
+  float w[V], b[V], less[V], scale[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) { w[i] = 0.0f; b[i] = 0.0f; }
+  if (co < cc) { params<V>(a.w, a.ptype, c, 1.0f, w); params<V>(a.b, a.ptype, c, 0.0f, b); }
+  const float* const gm = a.mean + (long long)n * a.G + c0 / a.Cg;
+  const float* const gr = a.rstd + (long long)n * a.G + c0 / a.Cg;
+  mean.set([&](int i) { return co < cc ? __ldg(gm + quotient(co + i, inv_cg)) : 0.0f; });
+  rstd.set([&](int i) { return co < cc ? __ldg(gr + quotient(co + i, inv_cg)) : 0.0f; });
+  mean.all(less);
+  rstd.all(scale);
+#pragma unroll
+  for (int i = 0; i < V; ++i) less[i] = -less[i];
+  const int act = a.act;
+  float s[V], sx[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) { s[i] = 0.0f; sx[i] = 0.0f; }
+  copies_wait<0>();
+#pragma unroll 2
+  for (int k = 0; k < turns; ++k) {
+    float xh[V], dz[V];
+    Raw<T, V> x, d;
+    x.b = xs[k * TH];
+    d.b = ds[k * TH];
+    unit_grad<T, V>(x, d, a.res ? rs + k * TH : nullptr, less, scale, w, b, act, xh, dz);
+    vadd<V>(s, s, dz);
+    vfma<V>(sx, dz, xh, sx);
+  }
+  fold_rows<V>(s, sh, u.log_cvt);
+  const int left = fold_rows<V>(sx, sh + span, u.log_cvt);
+  for (int i = tid; i < cc; i += TH) {
+    float2 t = make_float2(0.0f, 0.0f);
+    for (int r = 0; r < left; ++r) { t.x += sh[r * cvt * V + i]; t.y += sh[span + r * cvt * V + i]; }
+    mine[i] = t;
+  }
+  cg::cluster_group cluster = cg::this_cluster();
+  if (u.S > 1) cluster.sync(); else __syncthreads();
+  for (int i = tid; i < cc; i += TH) {
+    float2 t = mine[i];
+    if (u.S > 1) {
+      t = make_float2(0.0f, 0.0f);
+      for (int k = 0; k < u.S; ++k) { const float2 o = cluster.map_shared_rank(mine, k)[i]; t.x += o.x; t.y += o.y; }
+    }
+    if (rank == 0 && a.part_a) { const long long at = (long long)n * a.C + c0 + i; a.part_a[at] = t.x; a.part_b[at] = t.y; }
+    const float wi = param(a.w, a.ptype, c0 + i, 1.0f);
+    chan[i] = make_float2(t.x * wi, t.y * wi);
+  }
+  __syncthreads();
+  if (u.S > 1) cluster.barrier_arrive();
+  const float M = (float)a.P * (float)a.Cg;
+  for (int j = tid >> 5; j < groups; j += TH >> 5) {
+    float p = 0.0f, q = 0.0f;
+    for (int i = tid & 31; i < a.Cg; i += 32) { const float2 t = chan[j * a.Cg + i]; p += t.x; q += t.y; }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) { p += __shfl_xor_sync(0xffffffffu, p, o); q += __shfl_xor_sync(0xffffffffu, q, o); }
+    if ((tid & 31) == 0) grp[j] = make_float2(-(p / M), -(q / M));
+  }
+  __syncthreads();
+  Per<V, WHOLE> m1, m2;
+  m1.set([&](int i) { return co < cc ? grp[quotient(co + i, inv_cg)].x : 0.0f; });
+  m2.set([&](int i) { return co < cc ? grp[quotient(co + i, inv_cg)].y : 0.0f; });
+  const long long base = ((long long)n * a.P + p0 + row) * a.C + c, step = (long long)rows * a.C;
+  T* dx = (T*)a.out + base;
+  T* dres = a.dres ? (T*)a.dres + base : nullptr;
+#pragma unroll 2
+  for (int k = 0; k < turns; ++k, dx += step) {
+    float xh[V], dz[V], mg[V], mx[V];
+    Raw<T, V> x, d;
+    x.b = xs[k * TH];
+    d.b = ds[k * TH];
+    unit_grad<T, V>(x, d, a.res ? rs + k * TH : nullptr, less, scale, w, b, act, xh, dz);
+    if (dres) { d.round(dz); d.store(dres); dres += step; }
+    m1.all(mg);
+    m2.all(mx);
+    vmul<V>(dz, dz, w);                             // rstd * (g - mean(g) - xhat * mean(g * xhat)), the means negated
+    vadd<V>(dz, dz, mg);
+    vfma<V>(dz, xh, mx, dz);
+    vmul<V>(dz, dz, scale);
+    x.round(dz);
+    x.store(dx);
+  }
+  if (u.S > 1) cluster.barrier_wait();
+}
+
 // ---- host -----------------------------------------------------------------------------------------------------------
 struct Plan {
   int vec, cvt, ctiles, slices;
-  size_t bytes;
+  bool unit;                             // one pass: `u`, `threads` and `smem`; else two
+  Unit u;
+  int threads;
+  size_t smem, bytes;
 };
 
 int elem(int type) { return type == SAE_TYPE_FLOAT ? 4 : 2; }
@@ -457,19 +817,79 @@ bool desc_ok(const sae_group_norm_desc* d) {
   return true;
 }
 
-// Sixteen bytes at a time where every tensor of the call lets it (base, strides and the channel count), else one element.
+// Sixteen bytes at a time where every tensor of the call lets it (base, strides and the channel count), else four, else one element.
 int vector_width(const sae_group_norm_desc* d, const void* const* ptrs, int n) {
-  const int es = elem(d->type), V = 16 / es;
+  const int es = elem(d->type);
   uintptr_t m = 0;
   for (int i = 0; i < n; ++i) m |= reinterpret_cast<uintptr_t>(ptrs[i]);
   const long long s = d->x_sample | d->x_pixel | d->residual_sample | d->residual_pixel | d->dy_sample | d->dy_pixel | d->channels;
-  return (m & 15) == 0 && s % V == 0 ? V : 1;
+  m |= (uintptr_t)(s * es);
+  return (m & 15) == 0 ? 16 / es : es == 2 && (m & 3) == 0 ? 2 : 1;
 }
 
-// The caller's workspace is asked for before the tensors' alignment is known: both widths have to fit in it.
-Plan make_plan(const sae_group_norm_desc* d, int vec, int sms) {
-  Plan p;
+#ifdef SAE_GN_TUNE
+#include <cstdlib>
+int tune(const char* name, int otherwise) { const char* v = getenv(name); return v ? atoi(v) : otherwise; }
+#else
+int tune(const char*, int otherwise) { return otherwise; }
+#endif
+
+constexpr int SMEM_BLOCK = 227 * 1024;
+
+// One pass over a unit of `seg` bytes a pixel or a little less (whole groups, whole vectors), in clusters of up to `most` blocks
+// of up to `room` bytes; false if the unit does not fit.
+bool unit_plan(const sae_group_norm_desc* d, int vec, int tensors, bool backward, int seg, int most, size_t room, int sms, Plan& p) {
+  const int es = elem(d->type), VB = vec * es, cg_ = (int)(d->channels / d->groups);
+  int step = cg_;
+  while (step % vec) step += cg_;                                  // whole groups and whole vectors
+  if (step > d->channels) return false;
+  long long cc = std::max(1, seg / (step * es)) * (long long)step;
+  cc = std::min<long long>(cc, d->channels);
+  int log = 0;
+  while ((1ll << log) * vec < cc) ++log;
+  const int cvt = 1 << log;
+  if (cvt > GN_THREADS) return false;
+  cc = std::min<long long>(d->channels, (long long)cvt * vec / step * step);      // fill the lanes
+  const long long vectors = d->pixels * cvt;
+  int th = tune("GN_THREADS", 256);
+  while (th > 64 && vectors < th * 2ll) th /= 2;
+  th = std::max(th, cvt);
+  if (th < 32) th = 32;
+  const int rows = th >> log, SL = vec;
+  const size_t fixed = (size_t)(log < 5 ? th / 32 : rows) * cvt * SL * 4 * (backward ? 2 : 1) + (size_t)cc * 8 * 3 + 64;
+  if (fixed >= room) return false;
+  const long long slots_most = (long long)((room - fixed) / ((size_t)th * VB * tensors));
+  if (slots_most < 1) return false;
+  long long S = (d->pixels + slots_most * rows - 1) / (slots_most * rows);
+  if (S > most) return false;
+  // few units: shorter runs over more blocks, as long as a thread keeps two vectors
+  const int chunks = (int)((d->channels + cc - 1) / cc);
+  const long long units = (long long)d->samples * chunks;
+  while (S * 2 <= std::min(most, 8) && units * S * 2 <= sms * 2 && d->pixels >= S * 2 * rows * 2) S *= 2;
+  Unit& u = p.u;
+  u.log_cvt = log; u.cc = (int)cc; u.chunks = chunks; u.S = (int)S;
+  u.px = (int)((d->pixels + S - 1) / S);
+  u.slots = (u.px + rows - 1) / rows;
+  if (units * S > 0x7fffffffll) return false;
+  p.unit = true;
+  p.threads = th;
+  p.smem = fixed + (size_t)u.slots * th * VB * tensors;
+  return true;
+}
+
+Plan make_plan(const sae_group_norm_desc* d, int vec, bool backward, bool residual, int sms) {
+  Plan p = {};
   p.vec = vec;
+  const int tensors = (backward ? 2 : 1) + (residual ? 1 : 0);
+  const int segs[3] = {tune("GN_SEG", 128), 64, 32};
+  for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, (size_t)tune("GN_ROOM", 72) * 1024, sms, p);
+  for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, (size_t)SMEM_BLOCK / 2 - 1024, sms, p);
+  if (tune("GN_SPLIT", 0)) p.unit = false;
+  if (p.unit) {
+    p.slices = 1;
+    p.bytes = backward ? (size_t)2 * 4 * d->samples * d->channels : 0;
+    return p;
+  }
   const int cv = (int)((d->channels + vec - 1) / vec);
   p.ctiles = (cv + GN_THREADS - 1) / GN_THREADS;
   p.cvt = (cv + p.ctiles - 1) / p.ctiles;
@@ -508,8 +928,36 @@ int launched() {
   return cudaGetLastError() == cudaSuccess ? SAE_OK : SAE_ERR_CUDA;
 }
 
+// A unit kernel in clusters of S blocks.  Its shared memory needs an opt-in above 48 KB, once a device and kernel.
+template <void (*KERNEL)(const Args, const Unit)>
+int launch_units(const Args& a, const Plan& p, cudaStream_t st) {
+  static thread_local int opted = -1;               // one variable for each kernel
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
+  if (opted != dev) {
+    if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BLOCK) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
+    opted = dev;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((long long)a.N * p.u.chunks * p.u.S));
+  cfg.blockDim = dim3((unsigned)p.threads);
+  cfg.dynamicSmemBytes = p.smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim = {(unsigned)p.u.S, 1, 1};
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, KERNEL, a, p.u) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
+  return SAE_OK;
+}
+
 template <typename T, int V>
 int forward(const Args& a, const Plan& p, cudaStream_t st) {
+  if (p.unit) {
+    if (V > 1 && a.Cg % V == 0) return launch_units<k_gn_unit<T, V, true>>(a, p, st);
+    return launch_units<k_gn_unit<T, V, false>>(a, p, st);
+  }
   const dim3 grid((unsigned)(a.N * p.slices), (unsigned)p.ctiles);
   const long long warps = (long long)a.N * a.G;
   k_gn_statistics<T, V><<<grid, GN_THREADS, (2 * V + 1) * GN_THREADS * sizeof(float), st>>>(a);
@@ -520,6 +968,12 @@ int forward(const Args& a, const Plan& p, cudaStream_t st) {
 
 template <typename T, int V>
 int backward(const Args& a, const Plan& p, cudaStream_t st) {
+  if (p.unit) {
+    const int rc = V > 1 && a.Cg % V == 0 ? launch_units<k_gn_grad_unit<T, V, true>>(a, p, st) : launch_units<k_gn_grad_unit<T, V, false>>(a, p, st);
+    if (rc != SAE_OK) return rc;
+    if (a.dw || a.db) k_gn_param_grads<<<(unsigned)((a.C + 31) / 32), 1024, 0, st>>>(a, a.N);
+    return launched();
+  }
   const dim3 grid((unsigned)(a.N * p.slices), (unsigned)p.ctiles);
   const long long warps = (long long)a.N * a.G;
   k_gn_grad_sums<T, V><<<grid, GN_THREADS, 2 * V * GN_THREADS * sizeof(float), st>>>(a);
@@ -530,10 +984,10 @@ int backward(const Args& a, const Plan& p, cudaStream_t st) {
 }
 
 // An element type and a vector width as template arguments.
-#define GN_DISPATCH(fn, type, vec, ...)                                                                               \
-  ((type) == SAE_TYPE_FLOAT ? ((vec) > 1 ? fn<float, 4>(__VA_ARGS__) : fn<float, 1>(__VA_ARGS__))                      \
-   : (type) == SAE_TYPE_BFLOAT ? ((vec) > 1 ? fn<__nv_bfloat16, 8>(__VA_ARGS__) : fn<__nv_bfloat16, 1>(__VA_ARGS__))   \
-                               : ((vec) > 1 ? fn<__half, 8>(__VA_ARGS__) : fn<__half, 1>(__VA_ARGS__)))
+#define GN_DISPATCH16(fn, T, vec, ...) ((vec) == 8 ? fn<T, 8>(__VA_ARGS__) : (vec) == 2 ? fn<T, 2>(__VA_ARGS__) : fn<T, 1>(__VA_ARGS__))
+#define GN_DISPATCH(fn, type, vec, ...)                                                                  \
+  ((type) == SAE_TYPE_FLOAT ? ((vec) == 4 ? fn<float, 4>(__VA_ARGS__) : fn<float, 1>(__VA_ARGS__))        \
+   : (type) == SAE_TYPE_BFLOAT ? GN_DISPATCH16(fn, __nv_bfloat16, vec, __VA_ARGS__) : GN_DISPATCH16(fn, __half, vec, __VA_ARGS__))
 
 bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
 
@@ -542,12 +996,18 @@ bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(
 extern "C" {
 
 int64_t sae_group_norm_workspace(const sae_group_norm_desc* d, int32_t backward) {
-  (void)backward;
   if (!desc_ok(d)) return -1;
   const int sms = device_sms();
   if (sms < 1) return -1;
   if (d->samples == 0 || d->pixels == 0) return 0;
-  return (int64_t)std::max(make_plan(d, 16 / elem(d->type), sms).bytes, make_plan(d, 1, sms).bytes);
+  // the tensors' alignment and whether there is a residual are not known yet: the most that any form needs
+  size_t most = 0;
+  const int widths[3] = {16 / elem(d->type), 2, 1};
+  for (int i = 0; i < 3; ++i) {
+    if ((i == 1 && elem(d->type) == 4) || d->channels % widths[i]) continue;
+    for (int r = 0; r < 2; ++r) most = std::max(most, make_plan(d, widths[i], backward != 0, r != 0, sms).bytes);
+  }
+  return (int64_t)most;
 }
 
 int sae_group_norm_forward(const sae_group_norm_desc* d, const void* x, const void* residual, const void* weight, const void* bias,
@@ -566,8 +1026,8 @@ int sae_group_norm_forward(const sae_group_norm_desc* d, const void* x, const vo
   const int sms = device_sms();
   if (sms < 1) return SAE_ERR_CUDA;
   const void* ptrs[3] = {x, y, residual};
-  const Plan p = make_plan(d, vector_width(d, ptrs, 3), sms);
-  if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < p.bytes || (long long)d->samples * p.slices > 0x7fffffffll) return SAE_ERR_INVALID_ARG;
+  const Plan p = make_plan(d, vector_width(d, ptrs, 3), false, residual != nullptr, sms);
+  if ((p.bytes && !workspace) || !aligned_to(workspace, 16) || workspace_bytes < p.bytes || (long long)d->samples * p.slices > 0x7fffffffll) return SAE_ERR_INVALID_ARG;
   Args a = make_args(d, p, workspace);
   a.x = x; a.res = residual; a.w = weight; a.b = bias; a.out = y; a.mean = mean; a.rstd = rstd;
   return GN_DISPATCH(forward, d->type, p.vec, a, p, st);
@@ -591,8 +1051,8 @@ int sae_group_norm_backward(const sae_group_norm_desc* d, const void* dy, const 
   const int sms = device_sms();
   if (sms < 1) return SAE_ERR_CUDA;
   const void* ptrs[5] = {dy, x, residual, dx, dresidual};
-  const Plan p = make_plan(d, vector_width(d, ptrs, 5), sms);
-  if (!workspace || !aligned_to(workspace, 16) || workspace_bytes < p.bytes || (long long)d->samples * p.slices > 0x7fffffffll) return SAE_ERR_INVALID_ARG;
+  const Plan p = make_plan(d, vector_width(d, ptrs, 5), true, residual != nullptr, sms);
+  if ((p.bytes && !workspace) || !aligned_to(workspace, 16) || workspace_bytes < p.bytes || (long long)d->samples * p.slices > 0x7fffffffll) return SAE_ERR_INVALID_ARG;
   Args a = make_args(d, p, workspace);
   a.x = x; a.dy = dy; a.res = residual; a.w = weight; a.b = bias; a.out = dx; a.dres = dresidual; a.dw = dweight; a.db = dbias;
   a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);

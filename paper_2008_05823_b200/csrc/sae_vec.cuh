@@ -68,4 +68,80 @@ struct Raw {
   }
 };
 
+// Lane-wise arithmetic on V floats, two at a time where V is even: sm_100a adds, multiplies and fuses pairs of floats in one
+// instruction, each half rounded as the single operation rounds.
+__device__ __forceinline__ unsigned long long pair(float a, float b) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair(unsigned long long r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+
+template <int V>
+__device__ __forceinline__ void vadd(float (&o)[V], const float (&a)[V], const float (&b)[V]) {
+  if constexpr (V % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      unsigned long long r;
+      asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(a[i], a[i + 1])), "l"(pair(b[i], b[i + 1])));
+      unpair(r, o[i], o[i + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = __fadd_rn(a[i], b[i]);
+  }
+}
+template <int V>
+__device__ __forceinline__ void vmul(float (&o)[V], const float (&a)[V], const float (&b)[V]) {
+  if constexpr (V % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      unsigned long long r;
+      asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair(a[i], a[i + 1])), "l"(pair(b[i], b[i + 1])));
+      unpair(r, o[i], o[i + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = __fmul_rn(a[i], b[i]);
+  }
+}
+// o = a * b + c
+template <int V>
+__device__ __forceinline__ void vfma(float (&o)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V]) {
+  if constexpr (V % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      unsigned long long r;
+      asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair(a[i], a[i + 1])), "l"(pair(b[i], b[i + 1])), "l"(pair(c[i], c[i + 1])));
+      unpair(r, o[i], o[i + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = __fmaf_rn(a[i], b[i], c[i]);
+  }
+}
+// The same value in all lanes: a group's statistic where the V channels lie in one group, else one value a channel.
+template <int V, bool WHOLE> struct Per;
+template <int V> struct Per<V, true> {
+  float v;
+  template <typename F> __device__ __forceinline__ void set(F f) { v = f(0); }
+  __device__ __forceinline__ float at(int) const { return v; }
+  __device__ __forceinline__ void all(float (&o)[V]) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = v;
+  }
+};
+template <int V> struct Per<V, false> {
+  float v[V];
+  template <typename F> __device__ __forceinline__ void set(F f) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = f(i);
+  }
+  __device__ __forceinline__ float at(int i) const { return v[i]; }
+  __device__ __forceinline__ void all(float (&o)[V]) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = v[i];
+  }
+};
+
 }  // namespace sae
