@@ -547,106 +547,151 @@ __device__ __forceinline__ void params(const void* p, int type, int c, float non
 // Small non-negative integers (below 2^20) over a divisor, by its reciprocal.
 __device__ __forceinline__ int quotient(int a, float inv) { return (int)(((float)a + 0.5f) * inv); }
 
+// A block's place: a cluster is one unit (chunk blockIdx.x / S of sample n), a block the rank-th run of its pixels.
+struct Spot {
+  int n, rank, cc, groups, c0, co, c, p0, all, row, rows, turns;
+  bool on;                                // this thread's channels exist
+};
+template <int V>
+__device__ __forceinline__ Spot spot(const Args& a, const Unit& u) {
+  Spot q;
+  q.n = blockIdx.y + gridDim.y * blockIdx.z;
+  unsigned int rank, chunk;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm("mov.u32 %0, %%clusterid.x;" : "=r"(chunk));
+  q.rank = (int)rank;
+  q.c0 = (int)chunk * u.cc;
+  q.cc = min(u.cc, a.C - q.c0);
+  q.groups = q.cc / a.Cg;
+  q.co = ((int)threadIdx.x & ((1 << u.log_cvt) - 1)) * V;
+  q.c = q.c0 + q.co;
+  q.row = (int)threadIdx.x >> u.log_cvt;
+  q.rows = (int)blockDim.x >> u.log_cvt;
+  q.p0 = q.rank * u.px;
+  q.all = max(0, min(u.px, a.P - q.p0));
+  q.on = q.co < q.cc;
+  q.turns = q.on && q.all > q.row ? (q.all - q.row - 1) / q.rows + 1 : 0;
+  return q;
+}
+
 // WHOLE: a vector lies within one group, so one value a thread is enough for a statistic; else one a channel.
+// Statistics in one pass: a thread sums x - k and its square, k being its own first value (WHOLE: its first vector's mean).
+// As k is one of the values, (mean - k)^2 is at most their squares' sum about the mean, so taking the squares about the mean
+// from those about k loses at most the thread's count of values, in units of rounding: no large mean cancels.
 template <typename T, int V, bool WHOLE>
 __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_unit(const Args a, const Unit u) {
   extern __shared__ __align__(16) unsigned char smem[];
   typedef typename Raw<T, V>::B B;
   constexpr int SL = WHOLE ? 1 : V;
-  const int TH = blockDim.x, tid = threadIdx.x, cvt = 1 << u.log_cvt, rows = TH >> u.log_cvt, row = tid >> u.log_cvt;
-  const int rank = blockIdx.x % u.S, unit = blockIdx.x / u.S, n = unit / u.chunks, c0 = (unit - n * u.chunks) * u.cc;
-  const int cc = min(u.cc, a.C - c0), groups = cc / a.Cg, co = (tid & (cvt - 1)) * V, c = c0 + co;
-  const int p0 = rank * u.px, all = max(0, min(u.px, a.P - p0)), cnt = co < cc ? all : 0;
-  const int turns = cnt > row ? (cnt - row - 1) / rows + 1 : 0;                 // vectors this thread has
+  const Spot q = spot<V>(a, u);
+  if (q.n >= a.N) return;                                                       // the whole cluster
+  const int TH = blockDim.x, tid = threadIdx.x, cvt = 1 << u.log_cvt;
   const float inv_cg = 1.0f / (float)a.Cg;
   B* const xs = (B*)smem + tid;                                                 // slot k at k * TH
   B* const rs = xs + u.slots * TH;
   float* sh = (float*)((B*)smem + (size_t)u.slots * TH * (a.res ? 2 : 1));      // [rows or warps][cvt * SL]
-  float2* stat = (float2*)(sh + (u.log_cvt < 5 ? TH >> 5 : rows) * cvt * SL);   // [groups]: mean and squares, then mean and rstd
+  float2* stat = (float2*)(sh + (u.log_cvt < 5 ? TH >> 5 : q.rows) * cvt * SL); // [groups]: mean and squares, then mean and rstd
   float2* mine = stat + u.cc / a.Cg;                                            // [groups]: what the cluster's others read
-  fetch<T, V>(xs, (const T*)a.x + n * a.x_n + (p0 + row) * a.x_p + c, rows * a.x_p, TH, turns);
+  fetch<T, V>(xs, (const T*)a.x + q.n * a.x_n + (q.p0 + q.row) * a.x_p + q.c, q.rows * a.x_p, TH, q.turns);
   copies_commit();
-  if (a.res) fetch<T, V>(rs, (const T*)a.res + n * a.r_n + (p0 + row) * a.r_p + c, rows * a.r_p, TH, turns);
+  if (a.res) fetch<T, V>(rs, (const T*)a.res + q.n * a.r_n + (q.p0 + q.row) * a.r_p + q.c, q.rows * a.r_p, TH, q.turns);
   copies_commit();
   float w[V], b[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) { w[i] = 0.0f; b[i] = 0.0f; }
-  if (co < cc) { params<V>(a.w, a.ptype, c, 1.0f, w); params<V>(a.b, a.ptype, c, 0.0f, b); }
-  // the block's mean of each group
-  float acc[V], fold[SL];
+  if (q.on) { params<V>(a.w, a.ptype, q.c, 1.0f, w); params<V>(a.b, a.ptype, q.c, 0.0f, b); }
+  float s1[V], s2[V], less[V], fold[SL], k1[SL], k2[SL], shift[SL];
 #pragma unroll
-  for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+  for (int i = 0; i < V; ++i) { s1[i] = 0.0f; s2[i] = 0.0f; less[i] = 0.0f; }
   copies_wait<1>();
-#pragma unroll 4
-  for (int k = 0; k < turns; ++k) {
-    float v[V];
+  if (q.turns > 0) {
     Raw<T, V> r;
-    r.b = xs[k * TH];
-    r.widen(v);
-    vadd<V>(acc, acc, v);
-  }
-  const int per = WHOLE ? a.Cg / V : a.Cg, pitch = cvt * SL;
-  narrow<V, SL>(acc, fold);
-  int left = fold_rows<SL>(fold, sh, u.log_cvt);
-  const float inv = all > 0 ? 1.0f / ((float)all * (float)a.Cg) : 0.0f;
-  fold_groups(sh, left, pitch, per, groups, [&](int j, float s) { stat[j].x = s * inv; });
-  __syncthreads();
-  // the squares about it
-  Per<V, WHOLE> mean, rstd;
-  mean.set([&](int i) { return co < cc ? stat[quotient(co + i, inv_cg)].x : 0.0f; });
-  float less[V];
-  mean.all(less);
+    r.b = xs[0];
+    r.widen(less);
+    if constexpr (WHOLE) {
+      float t = less[0];
 #pragma unroll
-  for (int i = 0; i < V; ++i) { less[i] = -less[i]; acc[i] = 0.0f; }
+      for (int i = 1; i < V; ++i) t += less[i];
+#pragma unroll
+      for (int i = 0; i < V; ++i) less[i] = t * (1.0f / V);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) less[i] = fabsf(less[i]) <= 3e38f ? -less[i] : 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < SL; ++i) shift[i] = -less[i];
 #pragma unroll 4
-  for (int k = 0; k < turns; ++k) {
+  for (int k = 0; k < q.turns; ++k) {
     float v[V];
     Raw<T, V> r;
     r.b = xs[k * TH];
     r.widen(v);
     vadd<V>(v, v, less);
-    vfma<V>(acc, v, v, acc);
+    vadd<V>(s1, s1, v);
+    vfma<V>(s2, v, v, s2);
   }
-  narrow<V, SL>(acc, fold);
+  // k1: the thread's mean about its shift, k2: its squares about that mean; the block's mean of each group
+  const int per = WHOLE ? a.Cg / V : a.Cg, pitch = cvt * SL;
+  const float count = (float)(WHOLE ? q.turns * V : q.turns), inv_count = q.turns > 0 ? 1.0f / count : 0.0f;
+  narrow<V, SL>(s1, k1);
+  narrow<V, SL>(s2, k2);
+#pragma unroll
+  for (int i = 0; i < SL; ++i) {
+    fold[i] = __fmaf_rn(count, shift[i], k1[i]);
+    const float m = k1[i] * inv_count;
+    k2[i] = __fmaf_rn(-m, k1[i], k2[i]);
+    k1[i] = m;
+  }
+  int left = fold_rows<SL>(fold, sh, u.log_cvt);
+  const float inv = q.all > 0 ? 1.0f / ((float)q.all * (float)a.Cg) : 0.0f;
+  fold_groups(sh, left, pitch, per, q.groups, [&](int j, float s) { stat[j].x = s * inv; });
+  __syncthreads();
+  // the squares about it
+#pragma unroll
+  for (int i = 0; i < SL; ++i) {
+    const float d = q.on ? (shift[i] - stat[quotient(q.co + i, inv_cg)].x) + k1[i] : 0.0f;
+    fold[i] = __fmaf_rn(count * d, d, k2[i]);
+  }
   left = fold_rows<SL>(fold, sh, u.log_cvt);
-  fold_groups(sh, left, pitch, per, groups, [&](int j, float s) { mine[j] = make_float2(stat[j].x, s); });
+  fold_groups(sh, left, pitch, per, q.groups, [&](int j, float s) { mine[j] = make_float2(stat[j].x, s); });
   // joined over the cluster
   cg::cluster_group cluster = cg::this_cluster();
   if (u.S > 1) cluster.sync(); else __syncthreads();
   const float M = (float)a.P * (float)a.Cg;
-  for (int j = tid; j < groups; j += TH) {
+  for (int j = tid; j < q.groups; j += TH) {
     float2 r = mine[j];
     if (u.S > 1) {
       float s = 0.0f;
       for (int k = 0; k < u.S; ++k) s += (float)max(0, min(u.px, a.P - k * u.px)) * cluster.map_shared_rank(mine, k)[j].x;
       const float m = s * (float)a.Cg / M;
-      float q = 0.0f;
+      float m2 = 0.0f;
       for (int k = 0; k < u.S; ++k) {
         const float2 o = cluster.map_shared_rank(mine, k)[j];
         const float d = o.x - m;
-        q += o.y + (float)max(0, min(u.px, a.P - k * u.px)) * (float)a.Cg * d * d;
+        m2 += o.y + (float)max(0, min(u.px, a.P - k * u.px)) * (float)a.Cg * d * d;
       }
-      r = make_float2(m, q);
+      r = make_float2(m, m2);
     }
     r.y = __fdiv_rn(1.0f, __fsqrt_rn(r.y / M + a.eps));
     stat[j] = r;
-    if (rank == 0) { const long long g = (long long)n * a.G + c0 / a.Cg + j; a.mean[g] = r.x; a.rstd[g] = r.y; }
+    if (q.rank == 0) { const long long g = (long long)q.n * a.G + q.c0 / a.Cg + j; a.mean[g] = r.x; a.rstd[g] = r.y; }
   }
   __syncthreads();
   if (u.S > 1) cluster.barrier_arrive();            // this block has read what it needs of the others
   copies_wait<0>();
-  mean.set([&](int i) { return co < cc ? stat[quotient(co + i, inv_cg)].x : 0.0f; });
-  rstd.set([&](int i) { return co < cc ? stat[quotient(co + i, inv_cg)].y : 0.0f; });
+  Per<V, WHOLE> mean, rstd;
+  mean.set([&](int i) { return q.on ? stat[quotient(q.co + i, inv_cg)].x : 0.0f; });
+  rstd.set([&](int i) { return q.on ? stat[quotient(q.co + i, inv_cg)].y : 0.0f; });
   float scale[V];
   mean.all(less);
   rstd.all(scale);
 #pragma unroll
   for (int i = 0; i < V; ++i) less[i] = -less[i];
-  T* y = (T*)a.out + ((long long)n * a.P + p0 + row) * a.C + c;
-  const long long step = (long long)rows * a.C;
+  T* y = (T*)a.out + ((long long)q.n * a.P + q.p0 + q.row) * a.C + q.c;
+  const long long step = (long long)q.rows * a.C;
   const int act = a.act;
 #pragma unroll 2
-  for (int k = 0; k < turns; ++k, y += step) {
+  for (int k = 0; k < q.turns; ++k, y += step) {
     float z[V];
     Raw<T, V> r;
     r.b = xs[k * TH];
@@ -668,7 +713,38 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_unit(const Args a, const U
   if (u.S > 1) cluster.barrier_wait();              // nobody leaves while another may still read its sums
 }
 
-// What both passes of the backward unit kernel make of a vector: xhat and dz.
+// V floats of a 16-bit type's slots, half of their bytes in each of two.
+template <typename T, int V>
+__device__ __forceinline__ void hold(typename Raw<T, V>::B* lo, typename Raw<T, V>::B* hi, const float (&v)[V]) {
+  if constexpr (sizeof(T) == 2) {
+    typename Raw<T, V>::B b[2];
+    if constexpr (V == 8) {
+      b[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+      b[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+    } else if constexpr (V == 2) {
+      b[0] = __float_as_uint(v[0]); b[1] = __float_as_uint(v[1]);
+    } else {
+      b[0] = (unsigned short)(__float_as_uint(v[0]) & 0xffffu); b[1] = (unsigned short)(__float_as_uint(v[0]) >> 16);
+    }
+    *lo = b[0]; *hi = b[1];
+  }
+}
+template <typename T, int V>
+__device__ __forceinline__ void held(const typename Raw<T, V>::B* lo, const typename Raw<T, V>::B* hi, float (&v)[V]) {
+  if constexpr (sizeof(T) == 2) {
+    const typename Raw<T, V>::B a = *lo, b = *hi;
+    if constexpr (V == 8) {
+      v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
+      v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
+    } else if constexpr (V == 2) {
+      v[0] = __uint_as_float(a); v[1] = __uint_as_float(b);
+    } else {
+      v[0] = __uint_as_float((unsigned int)a | ((unsigned int)b << 16));
+    }
+  }
+}
+
+// xhat and dz of a vector.
 template <typename T, int V>
 __device__ __forceinline__ void unit_grad(Raw<T, V> x, Raw<T, V> d, const typename Raw<T, V>::B* res, const float (&less)[V], const float (&scale)[V],
                                           const float (&w)[V], const float (&b)[V], int act, float (&xh)[V], float (&dz)[V]) {
@@ -690,106 +766,160 @@ __device__ __forceinline__ void unit_grad(Raw<T, V> x, Raw<T, V> d, const typena
   slope<T, V>(dz, z, act);
 }
 
+// Adds up 2 V values a lane over the lanes whose numbers differ in the bits above log_cvt: in each round a lane hands half of
+// its values to the partner and takes the partner's other half, so the work halves from round to round.  Afterwards values
+// v[0 .. left) of a lane are the sums of the values from `from` on; `left` is returned.  The order is fixed.
+template <int W>
+__device__ __forceinline__ int scatter_sum(float (&v)[W], int log_cvt, int& from) {
+  const int lane = threadIdx.x & 31;
+  int left = W;
+  from = 0;
+#pragma unroll
+  for (int r = 0; r < 5; ++r) {
+    const int o = 16 >> r;
+    if (o < (1 << log_cvt)) break;
+    const bool upper = (lane & o) != 0;
+    if ((W >> r) >= 2) {
+#pragma unroll
+      for (int i = 0; i < W / 2; ++i) {
+        if (i < (W >> r) / 2) {
+          const float keep = upper ? v[i + (W >> r) / 2] : v[i], give = upper ? v[i] : v[i + (W >> r) / 2];
+          v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+      }
+      left = (W >> r) / 2;
+      if (upper) from += left;
+    } else {
+      v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    }
+  }
+  return left;
+}
+
+// After the first pass a thread's dz stays in its slots: a 16-bit dz that rounding does not change (relu's, none's) in dy's
+// place, else in float, which for 16-bit types takes a second slot (the residual's, if there is one).
 template <typename T, int V, bool WHOLE>
 __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_unit(const Args a, const Unit u) {
   extern __shared__ __align__(16) unsigned char smem[];
   typedef typename Raw<T, V>::B B;
-  const int TH = blockDim.x, tid = threadIdx.x, cvt = 1 << u.log_cvt, rows = TH >> u.log_cvt, row = tid >> u.log_cvt;
-  const int rank = blockIdx.x % u.S, unit = blockIdx.x / u.S, n = unit / u.chunks, c0 = (unit - n * u.chunks) * u.cc;
-  const int cc = min(u.cc, a.C - c0), groups = cc / a.Cg, co = (tid & (cvt - 1)) * V, c = c0 + co;
-  const int p0 = rank * u.px, cnt = co < cc ? max(0, min(u.px, a.P - p0)) : 0;
-  const int turns = cnt > row ? (cnt - row - 1) / rows + 1 : 0;
+  const Spot q = spot<V>(a, u);
+  if (q.n >= a.N) return;
+  const int TH = blockDim.x, tid = threadIdx.x, cvt = 1 << u.log_cvt, groups = q.groups;
   const float inv_cg = 1.0f / (float)a.Cg;
+  const int act = a.act;
+  const bool wide = sizeof(T) == 2 && act >= SAE_ACT_SILU, second = wide || a.res != nullptr;
   B* const xs = (B*)smem + tid;
   B* const ds = xs + u.slots * TH;
   B* const rs = ds + u.slots * TH;
-  float* sh = (float*)((B*)smem + (size_t)u.slots * TH * (a.res ? 3 : 2));      // [rows or warps][cvt * V], twice
-  const int span = (u.log_cvt < 5 ? TH >> 5 : rows) * cvt * V;
+  float* sh = (float*)((B*)smem + (size_t)u.slots * TH * (second ? 3 : 2));     // [2][rows or warps][cvt * V]
+  const int left = u.log_cvt < 5 ? TH >> 5 : q.rows, pitch = cvt * V, span = left * pitch;
   float2* mine = (float2*)(sh + 2 * span);                                      // [cc]: the block's sums of each channel
   float2* chan = mine + u.cc;                                                   // [cc]: the unit's, times the weight
   float2* grp = chan + u.cc;                                                    // [groups]: the two means
-  fetch<T, V>(xs, (const T*)a.x + n * a.x_n + (p0 + row) * a.x_p + c, rows * a.x_p, TH, turns);
-  fetch<T, V>(ds, (const T*)a.dy + n * a.d_n + (p0 + row) * a.d_p + c, rows * a.d_p, TH, turns);
-  if (a.res) fetch<T, V>(rs, (const T*)a.res + n * a.r_n + (p0 + row) * a.r_p + c, rows * a.r_p, TH, turns);
+  fetch<T, V>(xs, (const T*)a.x + q.n * a.x_n + (q.p0 + q.row) * a.x_p + q.c, q.rows * a.x_p, TH, q.turns);
+  fetch<T, V>(ds, (const T*)a.dy + q.n * a.d_n + (q.p0 + q.row) * a.d_p + q.c, q.rows * a.d_p, TH, q.turns);
+  if (a.res) fetch<T, V>(rs, (const T*)a.res + q.n * a.r_n + (q.p0 + q.row) * a.r_p + q.c, q.rows * a.r_p, TH, q.turns);
   copies_commit();
   Per<V, WHOLE> mean, rstd;
   float w[V], b[V], less[V], scale[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) { w[i] = 0.0f; b[i] = 0.0f; }
-  if (co < cc) { params<V>(a.w, a.ptype, c, 1.0f, w); params<V>(a.b, a.ptype, c, 0.0f, b); }
-  const float* const gm = a.mean + (long long)n * a.G + c0 / a.Cg;
-  const float* const gr = a.rstd + (long long)n * a.G + c0 / a.Cg;
-  mean.set([&](int i) { return co < cc ? __ldg(gm + quotient(co + i, inv_cg)) : 0.0f; });
-  rstd.set([&](int i) { return co < cc ? __ldg(gr + quotient(co + i, inv_cg)) : 0.0f; });
+  if (q.on) { params<V>(a.w, a.ptype, q.c, 1.0f, w); params<V>(a.b, a.ptype, q.c, 0.0f, b); }
+  const float* const gm = a.mean + (long long)q.n * a.G + q.c0 / a.Cg;
+  const float* const gr = a.rstd + (long long)q.n * a.G + q.c0 / a.Cg;
+  mean.set([&](int i) { return q.on ? __ldg(gm + quotient(q.co + i, inv_cg)) : 0.0f; });
+  rstd.set([&](int i) { return q.on ? __ldg(gr + quotient(q.co + i, inv_cg)) : 0.0f; });
   mean.all(less);
   rstd.all(scale);
 #pragma unroll
   for (int i = 0; i < V; ++i) less[i] = -less[i];
-  const int act = a.act;
-  float s[V], sx[V];
+  float s[2 * V];                                   // sum dz, then sum dz * xhat
+  {
+    float s0[V], sx[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) { s[i] = 0.0f; sx[i] = 0.0f; }
-  copies_wait<0>();
+    for (int i = 0; i < V; ++i) { s0[i] = 0.0f; sx[i] = 0.0f; }
+    T* dres = a.dres ? (T*)a.dres + ((long long)q.n * a.P + q.p0 + q.row) * a.C + q.c : nullptr;
+    const long long step = (long long)q.rows * a.C;
+    copies_wait<0>();
 #pragma unroll 2
-  for (int k = 0; k < turns; ++k) {
-    float xh[V], dz[V];
-    Raw<T, V> x, d;
-    x.b = xs[k * TH];
-    d.b = ds[k * TH];
-    unit_grad<T, V>(x, d, a.res ? rs + k * TH : nullptr, less, scale, w, b, act, xh, dz);
-    vadd<V>(s, s, dz);
-    vfma<V>(sx, dz, xh, sx);
+    for (int k = 0; k < q.turns; ++k) {
+      float xh[V], dz[V];
+      Raw<T, V> x, d;
+      x.b = xs[k * TH];
+      d.b = ds[k * TH];
+      unit_grad<T, V>(x, d, a.res ? rs + k * TH : nullptr, less, scale, w, b, act, xh, dz);
+      vadd<V>(s0, s0, dz);
+      vfma<V>(sx, dz, xh, sx);
+      if (act != SAE_ACT_NONE) {
+        d.round(dz);
+        if (wide) hold<T, V>(ds + k * TH, rs + k * TH, dz);
+        else ds[k * TH] = d.b;
+      }
+      if (dres) { d.store(dres); dres += step; }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) { s[i] = s0[i]; s[V + i] = sx[i]; }
   }
-  fold_rows<V>(s, sh, u.log_cvt);
-  const int left = fold_rows<V>(sx, sh + span, u.log_cvt);
-  for (int i = tid; i < cc; i += TH) {
-    float2 t = make_float2(0.0f, 0.0f);
-    for (int r = 0; r < left; ++r) { t.x += sh[r * cvt * V + i]; t.y += sh[span + r * cvt * V + i]; }
-    mine[i] = t;
+  {
+    int from, n = scatter_sum<2 * V>(s, u.log_cvt, from);
+    const int at = (u.log_cvt < 5 ? tid >> 5 : q.row) * pitch + (tid & (cvt - 1)) * V;
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i)
+      if (i < n) { const int j = from + i; sh[(j >= V ? span - V : 0) + at + j] = s[i]; }
+  }
+  __syncthreads();
+  for (int i = tid; i < 2 * pitch; i += TH) {       // one thread a sum
+    const bool x = i >= pitch;
+    const int j = x ? i - pitch : i;
+    const float* from = sh + (x ? span : 0) + j;
+    float t = 0.0f;
+#pragma unroll 4
+    for (int r = 0; r < left; ++r) t += from[r * pitch];
+    if (j < q.cc) ((float*)&mine[j])[x ? 1 : 0] = t;
   }
   cg::cluster_group cluster = cg::this_cluster();
   if (u.S > 1) cluster.sync(); else __syncthreads();
-  for (int i = tid; i < cc; i += TH) {
+  for (int i = tid; i < q.cc; i += TH) {
     float2 t = mine[i];
     if (u.S > 1) {
       t = make_float2(0.0f, 0.0f);
       for (int k = 0; k < u.S; ++k) { const float2 o = cluster.map_shared_rank(mine, k)[i]; t.x += o.x; t.y += o.y; }
     }
-    if (rank == 0 && a.part_a) { const long long at = (long long)n * a.C + c0 + i; a.part_a[at] = t.x; a.part_b[at] = t.y; }
-    const float wi = param(a.w, a.ptype, c0 + i, 1.0f);
+    if (q.rank == 0) { const long long at = (long long)q.n * a.C + q.c0 + i; a.part_a[at] = t.x; a.part_b[at] = t.y; }
+    const float wi = param(a.w, a.ptype, q.c0 + i, 1.0f);
     chan[i] = make_float2(t.x * wi, t.y * wi);
   }
   __syncthreads();
   if (u.S > 1) cluster.barrier_arrive();
   const float M = (float)a.P * (float)a.Cg;
   for (int j = tid >> 5; j < groups; j += TH >> 5) {
-    float p = 0.0f, q = 0.0f;
-    for (int i = tid & 31; i < a.Cg; i += 32) { const float2 t = chan[j * a.Cg + i]; p += t.x; q += t.y; }
+    float p = 0.0f, t = 0.0f;
+    for (int i = tid & 31; i < a.Cg; i += 32) { const float2 o = chan[j * a.Cg + i]; p += o.x; t += o.y; }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) { p += __shfl_xor_sync(0xffffffffu, p, o); q += __shfl_xor_sync(0xffffffffu, q, o); }
-    if ((tid & 31) == 0) grp[j] = make_float2(-(p / M), -(q / M));
+    for (int o = 16; o > 0; o >>= 1) { p += __shfl_xor_sync(0xffffffffu, p, o); t += __shfl_xor_sync(0xffffffffu, t, o); }
+    if ((tid & 31) == 0) grp[j] = make_float2(-(p / M), -(t / M));
   }
   __syncthreads();
+  // dx = rstd * (dz * w - mean(g) - xhat * mean(g * xhat)) = dz * (w rstd) + ((x - mean) * (-rstd^2 mean(g xhat)) - rstd mean(g))
   Per<V, WHOLE> m1, m2;
-  m1.set([&](int i) { return co < cc ? grp[quotient(co + i, inv_cg)].x : 0.0f; });
-  m2.set([&](int i) { return co < cc ? grp[quotient(co + i, inv_cg)].y : 0.0f; });
-  const long long base = ((long long)n * a.P + p0 + row) * a.C + c, step = (long long)rows * a.C;
-  T* dx = (T*)a.out + base;
-  T* dres = a.dres ? (T*)a.dres + base : nullptr;
+  m1.set([&](int i) { return q.on ? grp[quotient(q.co + i, inv_cg)].x * rstd.at(i) : 0.0f; });
+  m2.set([&](int i) { return q.on ? grp[quotient(q.co + i, inv_cg)].y * rstd.at(i) * rstd.at(i) : 0.0f; });
+  vmul<V>(w, w, scale);
+  T* dx = (T*)a.out + ((long long)q.n * a.P + q.p0 + q.row) * a.C + q.c;
+  const long long step = (long long)q.rows * a.C;
 #pragma unroll 2
-  for (int k = 0; k < turns; ++k, dx += step) {
-    float xh[V], dz[V], mg[V], mx[V];
+  for (int k = 0; k < q.turns; ++k, dx += step) {
+    float v[V], dz[V], p[V], t[V];
     Raw<T, V> x, d;
     x.b = xs[k * TH];
-    d.b = ds[k * TH];
-    unit_grad<T, V>(x, d, a.res ? rs + k * TH : nullptr, less, scale, w, b, act, xh, dz);
-    if (dres) { d.round(dz); d.store(dres); dres += step; }
-    m1.all(mg);
-    m2.all(mx);
-    vmul<V>(dz, dz, w);                             // rstd * (g - mean(g) - xhat * mean(g * xhat)), the means negated
-    vadd<V>(dz, dz, mg);
-    vfma<V>(dz, xh, mx, dz);
-    vmul<V>(dz, dz, scale);
+    x.widen(v);
+    if (wide) held<T, V>(ds + k * TH, rs + k * TH, dz);
+    else { d.b = ds[k * TH]; d.widen(dz); }
+    m2.all(p);
+    m1.all(t);
+    vadd<V>(v, v, less);
+    vfma<V>(v, v, p, t);
+    vfma<V>(dz, dz, w, v);
     x.round(dz);
     x.store(dx);
   }
@@ -870,7 +1000,6 @@ bool unit_plan(const sae_group_norm_desc* d, int vec, int tensors, bool backward
   u.log_cvt = log; u.cc = (int)cc; u.chunks = chunks; u.S = (int)S;
   u.px = (int)((d->pixels + S - 1) / S);
   u.slots = (u.px + rows - 1) / rows;
-  if (units * S > 0x7fffffffll) return false;
   p.unit = true;
   p.threads = th;
   p.smem = fixed + (size_t)u.slots * th * VB * tensors;
@@ -880,7 +1009,9 @@ bool unit_plan(const sae_group_norm_desc* d, int vec, int tensors, bool backward
 Plan make_plan(const sae_group_norm_desc* d, int vec, bool backward, bool residual, int sms) {
   Plan p = {};
   p.vec = vec;
-  const int tensors = (backward ? 2 : 1) + (residual ? 1 : 0);
+  // backward: a second slot for dz in float where its type cannot hold it
+  const bool second = residual || (backward && elem(d->type) == 2 && d->activation >= SAE_ACT_SILU);
+  const int tensors = (backward ? 2 : 1) + (second ? 1 : 0);
   const int segs[3] = {tune("GN_SEG", 128), 64, 32};
   for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, (size_t)tune("GN_ROOM", 72) * 1024, sms, p);
   for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, (size_t)SMEM_BLOCK / 2 - 1024, sms, p);
@@ -939,7 +1070,8 @@ int launch_units(const Args& a, const Plan& p, cudaStream_t st) {
     opted = dev;
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((long long)a.N * p.u.chunks * p.u.S));
+  const int ny = std::min(a.N, 32768);
+  cfg.gridDim = dim3((unsigned)(p.u.chunks * p.u.S), (unsigned)ny, (unsigned)((a.N + ny - 1) / ny));
   cfg.blockDim = dim3((unsigned)p.threads);
   cfg.dynamicSmemBytes = p.smem;
   cfg.stream = st;
