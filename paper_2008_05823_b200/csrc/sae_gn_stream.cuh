@@ -1,0 +1,450 @@
+// Group norm in two passes: streaming kernels for groups too large to stay on chip.  The second pass finds in L2 what the
+// first one read: the host cuts the samples into portions that fit there.
+#pragma once
+#include "sae_gn_common.cuh"
+
+namespace sae {
+
+struct Stream {
+  int n0;                                // first sample of this launch
+  int slices, px;                        // runs of pixels a sample is cut into, pixels of one
+  int cvt, tiles, tile_groups;           // vectors of a pixel a block takes, tiles of them in a pixel, groups a tile touches at most
+  int param_z;                           // backward apply: leading layers of the grid that sum up dw and db
+  bool held;                             // backward sums: the second pass reads dresidual instead of dy and the residual
+};
+
+// Vectors of each tensor that a thread has in flight: eight for the statistics, which read one tensor, four for the rest of the
+// forward pass; backwards, with two or three tensors, two, which keeps three blocks an SM without spills.
+constexpr int GN_STAT_BATCH = 8, GN_BATCH = 4, GN_GRAD_BATCH = 2;
+
+// What a thread stands for: V channels from c on, pixels p, p + rows, .. below p1.  grid: (slices, tiles, samples).
+struct Place {
+  int n, slice, c, p, p1, rows, row;
+  bool on;
+};
+template <int V>
+__device__ __forceinline__ Place place(const Args& a, const Stream& s) {
+  Place q;
+  q.n = s.n0 + (int)blockIdx.z - s.param_z;
+  q.slice = blockIdx.x;
+  q.rows = GN_THREADS / s.cvt;
+  q.row = threadIdx.x / s.cvt;
+  q.c = (blockIdx.y * s.cvt + (threadIdx.x - q.row * s.cvt)) * V;
+  q.on = q.row < q.rows && q.c < a.C;
+  q.p = q.slice * s.px + q.row;
+  q.p1 = min(a.P, (q.slice + 1) * s.px);
+  return q;
+}
+__device__ __forceinline__ int slice_count(const Args& a, const Stream& s, int i) { return min(s.px, a.P - i * s.px); }
+
+// A stream kernel lets its successor start as soon as all its blocks run, and itself waits, before it touches what another
+// kernel of the call has written, for all of its predecessor.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// Calls f(k) for each of a thread's pixels, batch by batch: get(k, pixel) loads, use(k, pixel) computes.
+template <int BATCH, typename G, typename U>
+__device__ __forceinline__ void walk(const Place& q, G get, U use) {
+  int p = q.p;
+  for (; p + (BATCH - 1) * q.rows < q.p1; p += BATCH * q.rows) {
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) get(k, (long long)(p + k * q.rows));
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) use(k, (long long)(p + k * q.rows));
+  }
+  for (; p < q.p1; p += q.rows) { get(0, (long long)p); use(0, (long long)p); }
+}
+
+// The same from the last batch to the first: the second pass begins with what the first one read last.
+template <int BATCH, typename G, typename U>
+__device__ __forceinline__ void walk_back(const Place& q, G get, U use) {
+  if (q.p >= q.p1) return;
+  const int whole = ((q.p1 - q.p - 1) / q.rows + 1) / BATCH * BATCH;            // pixels in whole batches
+  for (int p = q.p + whole * q.rows; p < q.p1; p += q.rows) { get(0, (long long)p); use(0, (long long)p); }
+  for (int p = q.p + (whole - BATCH) * q.rows; p >= q.p; p -= BATCH * q.rows) {
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) get(k, (long long)(p + k * q.rows));
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) use(k, (long long)(p + k * q.rows));
+  }
+}
+
+// ---- a tile's groups ----------------------------------------------------------------------------------------------
+struct Tile {                            // the tile's channels [lo, hi), the groups they touch
+  int lo, hi, g0, groups;
+};
+__device__ __forceinline__ Tile tile_of(const Args& a, const Stream& s, int tile, int vec) {
+  Tile t;
+  t.lo = tile * s.cvt * vec;
+  t.hi = min(a.C, t.lo + s.cvt * vec);
+  t.g0 = t.lo / a.Cg;
+  t.groups = (t.hi - 1) / a.Cg - t.g0 + 1;
+  return t;
+}
+
+// Few values a group: as many groups as fit share a warp.  The lanes a group gets: a power of two, 32 at most.
+__device__ __forceinline__ int lanes_for(int entries) { return entries > 16 ? 32 : entries > 8 ? 16 : entries > 4 ? 8 : entries > 2 ? 4 : 2; }
+
+// Calls f(j, lane, lanes) for each group j of a tile with the lanes that share it (j may be past the end: take part in shuffles).
+template <typename F>
+__device__ __forceinline__ void each_group(const Tile& t, int entries, F f) {
+  const int lanes = lanes_for(entries), sub = threadIdx.x / lanes, lane = threadIdx.x & (lanes - 1);
+  for (int j0 = 0; j0 < t.groups; j0 += GN_THREADS / lanes) f(j0 + sub, lane, lanes);
+}
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+  for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// Sums of each group's values in sh[rows][pitch], SL of them a vector of V channels: out(j, sum, channels).
+template <int SL, int V, typename F>
+__device__ __forceinline__ void fold_tile(const Args& a, const Tile& t, const float* sh, int rows, int pitch, F out) {
+  each_group(t, rows * (a.Cg * SL / V), [&](int j, int lane, int lanes) {
+    const int lo = max((t.g0 + j) * a.Cg, t.lo), hi = min((t.g0 + j + 1) * a.Cg, t.hi), len = (hi - lo) * SL / V;
+    float s = 0.0f;
+    if (j < t.groups) {
+      const float* p = sh + (lo - t.lo) * SL / V;
+      if (len == 1) {
+        for (int e = lane; e < rows; e += lanes) s += p[e * pitch];
+      } else {
+        const float inv = __frcp_rn((float)len);
+        for (int e = lane; e < rows * len; e += lanes) {
+          const int r = quotient(e, inv);
+          s += p[r * pitch + (e - r * len)];
+        }
+      }
+    }
+    s = lanes_sum(s, lanes);
+    if (j < t.groups && lane == 0) out(j, s, hi - lo);
+  });
+}
+
+// The runs' pairs of group g of sample n, dealt to the lanes that share it: f(pixels * channels of the run, pair).
+template <typename F>
+__device__ __forceinline__ void each_run(const Args& a, const Stream& s, int n, int g, int vec, int lane, int lanes, F f) {
+  const float2* part = a.part_s + (long long)n * s.slices * s.tiles * s.tile_groups;
+  if (s.tiles == 1) {
+    for (int i = lane; i < s.slices; i += lanes)
+      f((float)slice_count(a, s, i) * (float)a.Cg, __ldcg(part + i * s.tile_groups + g));
+    return;
+  }
+  const int tile_c = s.cvt * vec, t0 = g * a.Cg / tile_c, tiles = (g * a.Cg + a.Cg - 1) / tile_c - t0 + 1;
+  for (int e = lane; e < s.slices * tiles; e += lanes) {
+    const int i = tiles == 1 ? e : e / tiles, t = t0 + (e - i * tiles);
+    const int lo = max(g * a.Cg, t * tile_c), hi = min(min((g + 1) * a.Cg, (t + 1) * tile_c), a.C);
+    f((float)slice_count(a, s, i) * (float)(hi - lo), __ldcg(part + ((long long)i * s.tiles + t) * s.tile_groups + g - t * tile_c / a.Cg));
+  }
+}
+__device__ __forceinline__ float2* run_out(const Args& a, const Stream& s, const Place& q) {
+  return a.part_s + (((long long)q.n * s.slices + q.slice) * s.tiles + blockIdx.y) * s.tile_groups;
+}
+
+// ---- forward ------------------------------------------------------------------------------------------------------
+// A thread sums x - k and its square over at most 32 vectors, k being the first one's value (WHOLE: mean), then joins count, mean
+// and squares to what came before (Chan, Golub and LeVeque's update).
+template <typename T, int V, bool WHOLE>
+__global__ void __launch_bounds__(GN_THREADS, WHOLE ? 4 : 3) k_gn_statistics(const Args a, const Stream st) {
+  extern __shared__ float sh[];           // [rows][cvt * SL], then [tile_groups]
+  constexpr int SL = WHOLE ? 1 : V;
+  let_next_start();
+  const Place q = place<V>(a, st);
+  const float inv_cg = 1.0f / (float)a.Cg;
+  float count = 0.0f, mean[SL], m2[SL];
+#pragma unroll
+  for (int i = 0; i < SL; ++i) { mean[i] = 0.0f; m2[i] = 0.0f; }
+  if (q.on) {
+    const T* x = (const T*)a.x + q.n * a.x_n + q.c;
+    const long long step = q.rows * a.x_p;
+    int left = q.p < q.p1 ? (q.p1 - q.p - 1) / q.rows + 1 : 0;                  // vectors to come
+    x += q.p * a.x_p;
+    Raw<T, V> raw[GN_STAT_BATCH];
+    while (left > 0) {                                                          // a run
+      float s1[V], s2[V], less[V];
+      int run = 0;
+      do {
+        const int m = min(left, GN_STAT_BATCH);
+        if (m == GN_STAT_BATCH) {
+#pragma unroll
+          for (int k = 0; k < GN_STAT_BATCH; ++k) raw[k].load(x + k * step);
+        } else {
+#pragma unroll
+          for (int k = 0; k < GN_STAT_BATCH - 1; ++k) if (k < m) raw[k].load(x + k * step);
+        }
+        x += m * step;
+        left -= m;
+        if (run == 0) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) { s1[i] = 0.0f; s2[i] = 0.0f; }
+          raw[0].widen(less);
+          if constexpr (WHOLE) {
+            float t = less[0];
+#pragma unroll
+            for (int i = 1; i < V; ++i) t += less[i];
+#pragma unroll
+            for (int i = 0; i < V; ++i) less[i] = t * (1.0f / V);
+          }
+#pragma unroll
+          for (int i = 0; i < V; ++i) less[i] = fabsf(less[i]) <= 3e38f ? -less[i] : 0.0f;
+        }
+        run += m;
+#pragma unroll
+        for (int k = 0; k < GN_STAT_BATCH; ++k) {
+          if (k < m) {
+            float v[V];
+            raw[k].widen(v);
+            vadd<V>(v, v, less);
+            vadd<V>(s1, s1, v);
+            vfma<V>(s2, v, v, s2);
+          }
+        }
+      } while (left > 0 && run < 32);
+      float k1[SL], k2[SL];
+      narrow<V, SL>(s1, k1);
+      narrow<V, SL>(s2, k2);
+      const float n = (float)(WHOLE ? run * V : run), inv = 1.0f / n, t = count + n, f = n / t;
+#pragma unroll
+      for (int i = 0; i < SL; ++i) {
+        const float m = k1[i] * inv, d = (m - less[i]) - mean[i];
+        m2[i] += __fmaf_rn(-m, k1[i], k2[i]) + d * d * (count * f);
+        mean[i] = __fmaf_rn(d, f, mean[i]);
+      }
+      count = t;
+    }
+  }
+  // the block's mean of each group of its tile, then the squares about it
+  const Tile tile = tile_of(a, st, blockIdx.y, V);
+  const int pitch = st.cvt * SL, slot = q.row * pitch + (threadIdx.x - q.row * st.cvt) * SL;
+  const float inv_pixels = 1.0f / (float)slice_count(a, st, q.slice);
+  float* const gmean = sh + q.rows * pitch;
+  if (q.row < q.rows) {
+#pragma unroll
+    for (int i = 0; i < SL; ++i) sh[slot + i] = q.on ? count * mean[i] : 0.0f;
+  }
+  __syncthreads();
+  fold_tile<SL, V>(a, tile, sh, q.rows, pitch, [&](int j, float s, int channels) { gmean[j] = s * inv_pixels * __frcp_rn((float)channels); });
+  __syncthreads();
+  if (q.row < q.rows) {
+#pragma unroll
+    for (int i = 0; i < SL; ++i) {
+      float v = 0.0f;
+      if (q.on) { const float d = mean[i] - gmean[quotient(q.c + i, inv_cg) - tile.g0]; v = __fmaf_rn(count * d, d, m2[i]); }
+      sh[slot + i] = v;
+    }
+  }
+  __syncthreads();
+  wait_for_previous();
+  float2* const out = run_out(a, st, q);
+  fold_tile<SL, V>(a, tile, sh, q.rows, pitch, [&](int j, float s, int) { out[j] = make_float2(gmean[j], s); });
+}
+
+template <typename T, int V, bool WHOLE, bool RES>
+__global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_apply(const Args a, const Stream st) {
+  extern __shared__ float2 stat[];        // [tile_groups]
+  let_next_start();
+  const Place q = place<V>(a, st);
+  const float inv_cg = 1.0f / (float)a.Cg;
+  float w[V], b[V], less[V], scale[V];
+  if (q.on) { params<V>(a.w, a.ptype, q.c, 1.0f, w); params<V>(a.b, a.ptype, q.c, 0.0f, b); }
+  wait_for_previous();
+  // the tile's groups: their runs joined about the group's own mean
+  const Tile tile = tile_of(a, st, blockIdx.y, V);
+  const float inv_m = 1.0f / ((float)a.P * (float)a.Cg);
+  each_group(tile, st.slices, [&](int j, int lane, int lanes) {
+    const int g = tile.g0 + j;
+    const bool on = j < tile.groups;
+    float s = 0.0f, m2 = 0.0f;
+    if (on) each_run(a, st, q.n, g, V, lane, lanes, [&](float m, float2 v) { s = __fmaf_rn(m * inv_m, v.x, s); });
+    s = lanes_sum(s, lanes);
+    if (on) each_run(a, st, q.n, g, V, lane, lanes, [&](float m, float2 v) { const float d = v.x - s; m2 += __fmaf_rn(m * d, d, v.y); });
+    m2 = lanes_sum(m2, lanes);
+    if (on && lane == 0) {
+      const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(m2 * inv_m + a.eps));
+      stat[j] = make_float2(s, rstd);
+      if (q.slice == 0) { a.mean[(long long)q.n * a.G + g] = s; a.rstd[(long long)q.n * a.G + g] = rstd; }   // tiles that share a group agree
+    }
+  });
+  __syncthreads();
+  if (!q.on) return;
+  {
+    Per<V, WHOLE> mean, rstd;
+    mean.set([&](int i) { return stat[quotient(q.c + i, inv_cg) - tile.g0].x; });
+    rstd.set([&](int i) { return stat[quotient(q.c + i, inv_cg) - tile.g0].y; });
+    mean.all(less);
+    rstd.all(scale);
+#pragma unroll
+    for (int i = 0; i < V; ++i) less[i] = -less[i];
+  }
+  const T* x = (const T*)a.x + q.n * a.x_n + q.c;
+  const T* r = RES ? (const T*)a.res + q.n * a.r_n + q.c : nullptr;
+  T* y = (T*)a.out + (long long)q.n * a.P * a.C + q.c;
+  Raw<T, V> xr[GN_BATCH], rr[RES ? GN_BATCH : 1];
+  const int act = a.act;
+  walk_back<GN_BATCH>(q, [&](int k, long long p) { xr[k].load_stream(x + p * a.x_p); if (RES) rr[k].load_stream(r + p * a.r_p); },
+       [&](int k, long long p) {
+         float z[V];
+         xr[k].widen(z);
+         vadd<V>(z, z, less);
+         vmul<V>(z, z, scale);
+         vmul<V>(z, z, w);
+         vadd<V>(z, z, b);
+         if (RES) { float v[V]; rr[k].widen(v); vadd<V>(z, z, v); }
+         activate<T, V>(z, act);
+         Raw<T, V> o;
+         o.round(z);
+         o.store_stream(y + p * a.C);
+       });
+}
+
+// ---- backward ------------------------------------------------------------------------------------------------------
+// ACT: none, relu, or (2) the one that a.act names.  Backwards the residual only enters through act', so without an
+// activation there is none.
+template <int ACT>
+__device__ __forceinline__ int act_of(const Args& a) { return ACT == 2 ? a.act : ACT == 1 ? SAE_ACT_RELU : SAE_ACT_NONE; }
+
+template <typename T, int V, bool WHOLE, int ACT, bool RES>
+__global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(const Args a, const Stream st) {
+  extern __shared__ float sh[];           // [2][rows][cvt * V]; the first rows take the sums, times the weight
+  let_next_start();
+  const Place q = place<V>(a, st);
+  const float inv_cg = 1.0f / (float)a.Cg;
+  const int pitch = st.cvt * V, span = q.rows * pitch, slot = (threadIdx.x - q.row * st.cvt) * V;
+  if (q.row < q.rows) {
+    float s[V], sx[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) { s[i] = 0.0f; sx[i] = 0.0f; }
+    if (q.on) {
+      float w[V], b[V], less[V], scale[V];
+      params<V>(a.w, a.ptype, q.c, 1.0f, w);
+      params<V>(a.b, a.ptype, q.c, 0.0f, b);
+      Per<V, WHOLE> mean, rstd;
+      const long long g = (long long)q.n * a.G;
+      mean.set([&](int i) { return __ldg(a.mean + g + quotient(q.c + i, inv_cg)); });
+      rstd.set([&](int i) { return __ldg(a.rstd + g + quotient(q.c + i, inv_cg)); });
+      mean.all(less);
+      rstd.all(scale);
+#pragma unroll
+      for (int i = 0; i < V; ++i) less[i] = -less[i];
+      const T* x = (const T*)a.x + q.n * a.x_n + q.c;
+      const T* d = (const T*)a.dy + q.n * a.d_n + q.c;
+      const T* r = RES ? (const T*)a.res + q.n * a.r_n + q.c : nullptr;
+      T* dres = a.dres ? (T*)a.dres + (long long)q.n * a.P * a.C + q.c : nullptr;
+      Raw<T, V> xr[GN_GRAD_BATCH], dr[GN_GRAD_BATCH], rr[RES ? GN_GRAD_BATCH : 1];
+      const int act = act_of<ACT>(a);
+      const unsigned long long once = l2_policy(st.held);                       // what the second pass will not read again
+      walk<GN_GRAD_BATCH>(q, [&](int k, long long p) { xr[k].load(x + p * a.x_p); dr[k].load(d + p * a.d_p, once); if (RES) rr[k].load(r + p * a.r_p, once); },
+           [&](int k, long long p) {
+             float xh[V], dz[V];
+             vector_grad<T, V>(xr[k], dr[k], RES ? &rr[k] : nullptr, less, scale, w, b, act, xh, dz);
+             vadd<V>(s, s, dz);
+             vfma<V>(sx, dz, xh, sx);
+             if (dres) { Raw<T, V> o; o.round(dz); o.store(dres + p * a.C); }
+           });
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) { sh[q.row * pitch + slot + i] = s[i]; sh[span + q.row * pitch + slot + i] = sx[i]; }
+  }
+  __syncthreads();
+  wait_for_previous();
+  const Tile tile = tile_of(a, st, blockIdx.y, V);
+  const long long at = ((long long)q.n * st.slices + q.slice) * a.C + tile.lo;
+  for (int i = threadIdx.x; i < pitch; i += GN_THREADS) {
+    float s = 0.0f, sx = 0.0f, w = 0.0f;
+    for (int r = 0; r < q.rows; ++r) { s += sh[r * pitch + i]; sx += sh[span + r * pitch + i]; }
+    if (tile.lo + i < tile.hi) { a.part_a[at + i] = s; a.part_b[at + i] = sx; w = param(a.w, a.ptype, tile.lo + i, 1.0f); }
+    sh[i] = s * w;
+    sh[span + i] = sx * w;
+  }
+  __syncthreads();
+  float2* const out = run_out(a, st, q);
+  fold_tile<V, V>(a, tile, sh, 1, pitch, [&](int j, float s, int) { out[j].x = s; });
+  fold_tile<V, V>(a, tile, sh + span, 1, pitch, [&](int j, float s, int) { out[j].y = s; });
+}
+
+// The channels' sums over `rows` runs, 32 channels a block of 256 threads, in a fixed order: dw and db.
+__device__ __forceinline__ void param_grads(const Args& a, int block, long long rows) {
+  __shared__ float sa[8][33], sb[8][33];
+  const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5, c = block * 32 + cx;
+  float s = 0.0f, q = 0.0f;
+  if (c < a.C) {
+#pragma unroll 4
+    for (long long r = ry; r < rows; r += 8) { s += __ldcg(a.part_a + r * a.C + c); q += __ldcg(a.part_b + r * a.C + c); }
+  }
+  sa[ry][cx] = s; sb[ry][cx] = q;
+  __syncthreads();
+  if (ry == 0 && c < a.C) {
+    for (int i = 1; i < 8; ++i) { s += sa[i][cx]; q += sb[i][cx]; }
+    if (a.db) put_param(a.db, a.ptype, c, s);
+    if (a.dw) put_param(a.dw, a.ptype, c, q);
+  }
+}
+__global__ void __launch_bounds__(GN_THREADS) k_gn_param_grads(const Args a, long long rows) {
+  wait_for_previous();
+  param_grads(a, blockIdx.x, rows);
+}
+
+template <typename T, int V, bool WHOLE, int ACT, bool RES>
+__global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_apply(const Args a, const Stream st) {
+  extern __shared__ float2 stat[];        // [tile_groups]
+  let_next_start();
+  if ((int)blockIdx.z < st.param_z) {     // dw and db, beside the rest
+    wait_for_previous();
+    const int block = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+    if (block * 32 < a.C) param_grads(a, block, (long long)a.N * st.slices);
+    return;
+  }
+  const Place q = place<V>(a, st);
+  const float inv_cg = 1.0f / (float)a.Cg;
+  float w[V], b[V], less[V], scale[V], p1[V], p2[V], gw[V];
+  if (q.on) {
+    params<V>(a.w, a.ptype, q.c, 1.0f, w);
+    params<V>(a.b, a.ptype, q.c, 0.0f, b);
+    Per<V, WHOLE> mean, rstd;
+    const long long g = (long long)q.n * a.G;
+    mean.set([&](int i) { return __ldg(a.mean + g + quotient(q.c + i, inv_cg)); });
+    rstd.set([&](int i) { return __ldg(a.rstd + g + quotient(q.c + i, inv_cg)); });
+    mean.all(less);
+    rstd.all(scale);
+#pragma unroll
+    for (int i = 0; i < V; ++i) less[i] = -less[i];
+  }
+  wait_for_previous();
+  // the tile's groups: mean(g) and mean(g * xhat), negated
+  const Tile tile = tile_of(a, st, blockIdx.y, V);
+  const float inv_m = 1.0f / ((float)a.P * (float)a.Cg);
+  each_group(tile, st.slices, [&](int j, int lane, int lanes) {
+    float s = 0.0f, sx = 0.0f;
+    if (j < tile.groups) each_run(a, st, q.n, tile.g0 + j, V, lane, lanes, [&](float, float2 v) { s += v.x; sx += v.y; });
+    s = lanes_sum(s, lanes);
+    sx = lanes_sum(sx, lanes);
+    if (j < tile.groups && lane == 0) stat[j] = make_float2(-s * inv_m, -sx * inv_m);
+  });
+  __syncthreads();
+  if (!q.on) return;
+  {
+    // dx = rstd * (dz * w - mean(g) - xhat * mean(g * xhat)) = dz * (w rstd) + (xhat * (-rstd mean(g xhat)) - rstd mean(g))
+    Per<V, WHOLE> m1, m2;
+    m1.set([&](int i) { return scale[i] * stat[quotient(q.c + i, inv_cg) - tile.g0].x; });
+    m2.set([&](int i) { return scale[i] * stat[quotient(q.c + i, inv_cg) - tile.g0].y; });
+    m1.all(p1);
+    m2.all(p2);
+    vmul<V>(gw, w, scale);
+  }
+  const T* x = (const T*)a.x + q.n * a.x_n + q.c;
+  const T* d = (const T*)a.dy + q.n * a.d_n + q.c;
+  const T* r = RES ? (const T*)a.res + q.n * a.r_n + q.c : nullptr;
+  T* dx = (T*)a.out + (long long)q.n * a.P * a.C + q.c;
+  Raw<T, V> xr[GN_GRAD_BATCH], dr[GN_GRAD_BATCH], rr[RES ? GN_GRAD_BATCH : 1];
+  const int act = act_of<ACT>(a);
+  walk_back<GN_GRAD_BATCH>(q, [&](int k, long long p) { xr[k].load_stream(x + p * a.x_p); dr[k].load_stream(d + p * a.d_p); if (RES) rr[k].load_stream(r + p * a.r_p); },
+       [&](int k, long long p) {
+         float xh[V], dz[V];
+         vector_grad<T, V>(xr[k], dr[k], RES ? &rr[k] : nullptr, less, scale, w, b, act, xh, dz);
+         vfma<V>(xh, xh, p2, p1);
+         vfma<V>(dz, dz, gw, xh);
+         Raw<T, V> o;
+         o.round(dz);
+         o.store_stream(dx + p * a.C);
+       });
+}
+
+}  // namespace sae

@@ -35,12 +35,36 @@ __device__ __forceinline__ unsigned int round2(float a, float b, const __half*) 
   return *reinterpret_cast<const unsigned int*>(&v);
 }
 
+// How a load is to be kept in L2: first to go, or as usual.
+__device__ __forceinline__ unsigned long long l2_policy(bool evict_first) {
+  unsigned long long first, usual;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(first));
+  asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(usual));
+  return evict_first ? first : usual;
+}
+__device__ __forceinline__ uint4 load_hint(const uint4* p, unsigned long long policy) {
+  uint4 v;
+  asm volatile("ld.global.nc.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p), "l"(policy));
+  return v;
+}
+__device__ __forceinline__ unsigned int load_hint(const unsigned int* p, unsigned long long policy) {
+  unsigned int v;
+  asm volatile("ld.global.nc.L2::cache_hint.u32 %0, [%1], %2;" : "=r"(v) : "l"(p), "l"(policy));
+  return v;
+}
+__device__ __forceinline__ unsigned short load_hint(const unsigned short* p, unsigned long long policy) {
+  unsigned short v;
+  asm volatile("ld.global.nc.L2::cache_hint.u16 %0, [%1], %2;" : "=h"(v) : "l"(p), "l"(policy));
+  return v;
+}
+
 // V elements as they lie in memory; V * sizeof(T) is 2, 4, 8 or 16 bytes and the address a multiple of it.
 template <typename T, int V>
 struct Raw {
   typedef typename Bits<V * (int)sizeof(T)>::type B;
   B b;
   __device__ __forceinline__ void load(const T* p) { b = __ldg(reinterpret_cast<const B*>(p)); }
+  __device__ __forceinline__ void load(const T* p, unsigned long long policy) { b = load_hint(reinterpret_cast<const B*>(p), policy); }
   __device__ __forceinline__ void load_stream(const T* p) { b = __ldcs(reinterpret_cast<const B*>(p)); }
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<B*>(p) = b; }
   __device__ __forceinline__ void store_stream(T* p) const { __stcs(reinterpret_cast<B*>(p), b); }
