@@ -99,7 +99,7 @@ __device__ __forceinline__ int quotient(int a, float inv) { return (int)(((float
 
 // xhat and dz of a vector.
 template <typename T, int V>
-__device__ __forceinline__ void vector_grad(Raw<T, V> x, Raw<T, V> d, const Raw<T, V>* res, const float (&less)[V], const float (&scale)[V],
+__device__ __forceinline__ void vector_grad(const Raw<T, V>& x, const Raw<T, V>& d, const Raw<T, V>* res, const float (&less)[V], const float (&scale)[V],
                                           const float (&w)[V], const float (&b)[V], int act, float (&xh)[V], float (&dz)[V]) {
   float z[V];
   x.widen(xh);

@@ -13,10 +13,6 @@ struct Stream {
   bool held;                             // backward sums: the second pass reads dresidual instead of dy and the residual
 };
 
-// Vectors of each tensor that a thread has in flight: eight for the statistics, which read one tensor, four for the rest of the
-// forward pass; backwards, with two or three tensors, two, which keeps three blocks an SM without spills.
-constexpr int GN_STAT_BATCH = 8, GN_BATCH = 4, GN_GRAD_BATCH = 2;
-
 // What a thread stands for: V channels from c on, pixels p, p + rows, .. below p1.  grid: (slices, tiles, samples).
 struct Place {
   int n, slice, c, p, p1, rows, row;
@@ -42,32 +38,88 @@ __device__ __forceinline__ int slice_count(const Args& a, const Stream& s, int i
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// Calls f(k) for each of a thread's pixels, batch by batch: get(k, pixel) loads, use(k, pixel) computes.
-template <int BATCH, typename G, typename U>
-__device__ __forceinline__ void walk(const Place& q, G get, U use) {
-  int p = q.p;
-  for (; p + (BATCH - 1) * q.rows < q.p1; p += BATCH * q.rows) {
-#pragma unroll
-    for (int k = 0; k < BATCH; ++k) get(k, (long long)(p + k * q.rows));
-#pragma unroll
-    for (int k = 0; k < BATCH; ++k) use(k, (long long)(p + k * q.rows));
-  }
-  for (; p < q.p1; p += q.rows) { get(0, (long long)p); use(0, (long long)p); }
-}
+// How many of its pixels a thread has on their way: 64 KB of a block's shared memory, three blocks an SM.
+__host__ __device__ constexpr int ring_depth(int bytes, int tensors) { return bytes < 4 ? 8 : 256 / (bytes * tensors) < 24 ? 256 / (bytes * tensors) : 24; }
+__host__ __device__ constexpr size_t ring_bytes(int bytes, int tensors) { return bytes < 4 ? 0 : (size_t)ring_depth(bytes, tensors) * tensors * bytes * GN_THREADS; }
 
-// The same from the last batch to the first: the second pass begins with what the first one read last.
-template <int BATCH, typename G, typename U>
-__device__ __forceinline__ void walk_back(const Place& q, G get, U use) {
-  if (q.p >= q.p1) return;
-  const int whole = ((q.p1 - q.p - 1) / q.rows + 1) / BATCH * BATCH;            // pixels in whole batches
-  for (int p = q.p + whole * q.rows; p < q.p1; p += q.rows) { get(0, (long long)p); use(0, (long long)p); }
-  for (int p = q.p + (whole - BATCH) * q.rows; p >= q.p; p -= BATCH * q.rows) {
-#pragma unroll
-    for (int k = 0; k < BATCH; ++k) get(k, (long long)(p + k * q.rows));
-#pragma unroll
-    for (int k = 0; k < BATCH; ++k) use(k, (long long)(p + k * q.rows));
+// A thread's walk over its pixels of NT tensors, first to last or (BACK) last to first: the second pass begins with what the
+// first one read last.  Copies run ahead through a ring of slots of the thread's own in shared memory, so no barrier is
+// needed and the loads in flight do not depend on registers; single 16-bit elements, which have no asynchronous copy, are
+// loaded in batches instead.
+template <typename T, int V, int NT, bool BACK>
+struct Walk {
+  typedef typename Raw<T, V>::B B;
+  static constexpr int D = ring_depth(sizeof(B), NT);
+  const T* next[NT];
+  long long step[NT];
+  unsigned long long policy[NT];
+  B* slots;
+  int turns, ahead;
+
+  __device__ __forceinline__ void set(const Place& q, void* smem) {
+    turns = q.on && q.p < q.p1 ? (q.p1 - q.p - 1) / q.rows + 1 : 0;
+    ahead = 0;
+    slots = (B*)smem + threadIdx.x;
   }
-}
+  __device__ __forceinline__ int first(const Place& q) const { return BACK ? q.p + (turns - 1) * q.rows : q.p; }
+  // Tensor t: element (n, c) of it and the stride of a pixel; `once`: nobody reads it again, so it goes from L2 first.
+  __device__ __forceinline__ void tensor(int t, const Place& q, const T* from, long long pixel, bool once) {
+    next[t] = from + first(q) * pixel;
+    step[t] = (BACK ? -q.rows : q.rows) * pixel;
+    policy[t] = l2_policy(once);
+  }
+  __device__ __forceinline__ void fetch(int slot) {
+    if constexpr (sizeof(B) >= 4) {
+      if (ahead < turns) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          copy_async<sizeof(B)>(slots + (slot * NT + t) * GN_THREADS, next[t], policy[t]);
+          next[t] += step[t];
+        }
+      }
+      ++ahead;
+      copies_commit();
+    }
+  }
+  __device__ __forceinline__ void start() {
+    if constexpr (sizeof(B) >= 4) {
+#pragma unroll
+      for (int k = 0; k < D - 1; ++k) fetch(k);
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void run(F use) {
+    if constexpr (sizeof(B) >= 4) {
+      int to = D - 1, from = 0;
+#pragma unroll 2
+      for (int k = 0; k < turns; ++k) {
+        fetch(to);
+        to = to + 1 == D ? 0 : to + 1;
+        copies_wait<D - 1>();
+        Raw<T, V> r[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) r[t].b = slots[(from * NT + t) * GN_THREADS];
+        from = from + 1 == D ? 0 : from + 1;
+        use(r, k);
+      }
+      copies_wait<0>();
+    } else {
+      for (int k0 = 0; k0 < turns; k0 += D) {
+        Raw<T, V> r[D][NT];
+#pragma unroll
+        for (int k = 0; k < D; ++k) {
+          if (k0 + k < turns) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) { r[k][t].load(next[t]); next[t] += step[t]; }
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < D; ++k)
+          if (k0 + k < turns) use(r[k], k0 + k);
+      }
+    }
+  }
+};
 
 // ---- a tile's groups ----------------------------------------------------------------------------------------------
 struct Tile {                            // the tile's channels [lo, hi), the groups they touch
@@ -143,74 +195,55 @@ __device__ __forceinline__ float2* run_out(const Args& a, const Stream& s, const
 // A thread sums x - k and its square over at most 32 vectors, k being the first one's value (WHOLE: mean), then joins count, mean
 // and squares to what came before (Chan, Golub and LeVeque's update).
 template <typename T, int V, bool WHOLE>
-__global__ void __launch_bounds__(GN_THREADS, WHOLE ? 4 : 3) k_gn_statistics(const Args a, const Stream st) {
-  extern __shared__ float sh[];           // [rows][cvt * SL], then [tile_groups]
+__global__ void __launch_bounds__(GN_THREADS, 3) k_gn_statistics(const Args a, const Stream st) {
+  extern __shared__ __align__(16) unsigned char smem[];
   constexpr int SL = WHOLE ? 1 : V;
+  float* const sh = (float*)(smem + ring_bytes(V * sizeof(T), 1));              // [rows][cvt * SL], then [tile_groups]
   let_next_start();
   const Place q = place<V>(a, st);
   const float inv_cg = 1.0f / (float)a.Cg;
-  float count = 0.0f, mean[SL], m2[SL];
+  float count = 0.0f, mean[SL], m2[SL], s1[V], s2[V], less[V];
 #pragma unroll
   for (int i = 0; i < SL; ++i) { mean[i] = 0.0f; m2[i] = 0.0f; }
-  if (q.on) {
-    const T* x = (const T*)a.x + q.n * a.x_n + q.c;
-    const long long step = q.rows * a.x_p;
-    int left = q.p < q.p1 ? (q.p1 - q.p - 1) / q.rows + 1 : 0;                  // vectors to come
-    x += q.p * a.x_p;
-    Raw<T, V> raw[GN_STAT_BATCH];
-    while (left > 0) {                                                          // a run
-      float s1[V], s2[V], less[V];
-      int run = 0;
-      do {
-        const int m = min(left, GN_STAT_BATCH);
-        if (m == GN_STAT_BATCH) {
+  Walk<T, V, 1, false> walk;
+  walk.set(q, smem);
+  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p, false);
+  walk.start();
+  auto join = [&](int run) {
+    float k1[SL], k2[SL];
+    narrow<V, SL>(s1, k1);
+    narrow<V, SL>(s2, k2);
+    const float n = (float)(WHOLE ? run * V : run), inv = __frcp_rn(n), t = count + n, f = n * __frcp_rn(t);
 #pragma unroll
-          for (int k = 0; k < GN_STAT_BATCH; ++k) raw[k].load(x + k * step);
-        } else {
-#pragma unroll
-          for (int k = 0; k < GN_STAT_BATCH - 1; ++k) if (k < m) raw[k].load(x + k * step);
-        }
-        x += m * step;
-        left -= m;
-        if (run == 0) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) { s1[i] = 0.0f; s2[i] = 0.0f; }
-          raw[0].widen(less);
-          if constexpr (WHOLE) {
-            float t = less[0];
-#pragma unroll
-            for (int i = 1; i < V; ++i) t += less[i];
-#pragma unroll
-            for (int i = 0; i < V; ++i) less[i] = t * (1.0f / V);
-          }
-#pragma unroll
-          for (int i = 0; i < V; ++i) less[i] = fabsf(less[i]) <= 3e38f ? -less[i] : 0.0f;
-        }
-        run += m;
-#pragma unroll
-        for (int k = 0; k < GN_STAT_BATCH; ++k) {
-          if (k < m) {
-            float v[V];
-            raw[k].widen(v);
-            vadd<V>(v, v, less);
-            vadd<V>(s1, s1, v);
-            vfma<V>(s2, v, v, s2);
-          }
-        }
-      } while (left > 0 && run < 32);
-      float k1[SL], k2[SL];
-      narrow<V, SL>(s1, k1);
-      narrow<V, SL>(s2, k2);
-      const float n = (float)(WHOLE ? run * V : run), inv = 1.0f / n, t = count + n, f = n / t;
-#pragma unroll
-      for (int i = 0; i < SL; ++i) {
-        const float m = k1[i] * inv, d = (m - less[i]) - mean[i];
-        m2[i] += __fmaf_rn(-m, k1[i], k2[i]) + d * d * (count * f);
-        mean[i] = __fmaf_rn(d, f, mean[i]);
-      }
-      count = t;
+    for (int i = 0; i < SL; ++i) {
+      const float m = k1[i] * inv, d = (m - less[i]) - mean[i];
+      m2[i] += __fmaf_rn(-m, k1[i], k2[i]) + d * d * (count * f);
+      mean[i] = __fmaf_rn(d, f, mean[i]);
     }
-  }
+    count = t;
+  };
+  walk.run([&](const Raw<T, V> (&r)[1], int k) {
+    float v[V];
+    r[0].widen(v);
+    if ((k & 31) == 0) {
+      if (k) join(32);
+#pragma unroll
+      for (int i = 0; i < V; ++i) { s1[i] = 0.0f; s2[i] = 0.0f; less[i] = v[i]; }
+      if constexpr (WHOLE && V > 1) {
+        float t = v[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i) t += v[i];
+#pragma unroll
+        for (int i = 0; i < V; ++i) less[i] = t * (1.0f / V);
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) less[i] = fabsf(less[i]) <= 3e38f ? -less[i] : 0.0f;
+    }
+    vadd<V>(v, v, less);
+    vadd<V>(s1, s1, v);
+    vfma<V>(s2, v, v, s2);
+  });
+  if (walk.turns > 0) join(((walk.turns - 1) & 31) + 1);
   // the block's mean of each group of its tile, then the squares about it
   const Tile tile = tile_of(a, st, blockIdx.y, V);
   const int pitch = st.cvt * SL, slot = q.row * pitch + (threadIdx.x - q.row * st.cvt) * SL;
@@ -238,10 +271,17 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 4 : 3) k_gn_statistics(con
 }
 
 template <typename T, int V, bool WHOLE, bool RES>
-__global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_apply(const Args a, const Stream st) {
-  extern __shared__ float2 stat[];        // [tile_groups]
+__global__ void __launch_bounds__(GN_THREADS, 3) k_gn_apply(const Args a, const Stream st) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int NT = RES ? 2 : 1;
+  float2* const stat = (float2*)(smem + ring_bytes(V * sizeof(T), NT));         // [tile_groups]
   let_next_start();
   const Place q = place<V>(a, st);
+  Walk<T, V, NT, true> walk;
+  walk.set(q, smem);
+  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p, true);
+  if constexpr (RES) walk.tensor(1, q, (const T*)a.res + q.n * a.r_n + q.c, a.r_p, true);
+  walk.start();                           // no kernel of the call has written these
   const float inv_cg = 1.0f / (float)a.Cg;
   float w[V], b[V], less[V], scale[V];
   if (q.on) { params<V>(a.w, a.ptype, q.c, 1.0f, w); params<V>(a.b, a.ptype, q.c, 0.0f, b); }
@@ -274,25 +314,23 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_apply(const Ar
 #pragma unroll
     for (int i = 0; i < V; ++i) less[i] = -less[i];
   }
-  const T* x = (const T*)a.x + q.n * a.x_n + q.c;
-  const T* r = RES ? (const T*)a.res + q.n * a.r_n + q.c : nullptr;
-  T* y = (T*)a.out + (long long)q.n * a.P * a.C + q.c;
-  Raw<T, V> xr[GN_BATCH], rr[RES ? GN_BATCH : 1];
+  T* y = (T*)a.out + ((long long)q.n * a.P + walk.first(q)) * a.C + q.c;
+  const long long step = (long long)q.rows * a.C;
   const int act = a.act;
-  walk_back<GN_BATCH>(q, [&](int k, long long p) { xr[k].load_stream(x + p * a.x_p); if (RES) rr[k].load_stream(r + p * a.r_p); },
-       [&](int k, long long p) {
-         float z[V];
-         xr[k].widen(z);
-         vadd<V>(z, z, less);
-         vmul<V>(z, z, scale);
-         vmul<V>(z, z, w);
-         vadd<V>(z, z, b);
-         if (RES) { float v[V]; rr[k].widen(v); vadd<V>(z, z, v); }
-         activate<T, V>(z, act);
-         Raw<T, V> o;
-         o.round(z);
-         o.store_stream(y + p * a.C);
-       });
+  walk.run([&](const Raw<T, V> (&r)[NT], int) {
+    float z[V];
+    r[0].widen(z);
+    vadd<V>(z, z, less);
+    vmul<V>(z, z, scale);
+    vmul<V>(z, z, w);
+    vadd<V>(z, z, b);
+    if constexpr (RES) { float v[V]; r[1].widen(v); vadd<V>(z, z, v); }
+    activate<T, V>(z, act);
+    Raw<T, V> o;
+    o.round(z);
+    o.store_stream(y);
+    y -= step;
+  });
 }
 
 // ---- backward ------------------------------------------------------------------------------------------------------
@@ -303,10 +341,18 @@ __device__ __forceinline__ int act_of(const Args& a) { return ACT == 2 ? a.act :
 
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(const Args a, const Stream st) {
-  extern __shared__ float sh[];           // [2][rows][cvt * V]; the first rows take the sums, times the weight
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int NT = RES ? 3 : 2;
+  float* const sh = (float*)(smem + ring_bytes(V * sizeof(T), NT));             // [2][rows][cvt * V]; the first rows take the sums, times the weight
   let_next_start();
   const Place q = place<V>(a, st);
   const float inv_cg = 1.0f / (float)a.Cg;
+  Walk<T, V, NT, false> walk;
+  walk.set(q, smem);
+  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p, false);
+  walk.tensor(1, q, (const T*)a.dy + q.n * a.d_n + q.c, a.d_p, st.held);
+  if constexpr (RES) walk.tensor(2, q, (const T*)a.res + q.n * a.r_n + q.c, a.r_p, st.held);
+  walk.start();
   const int pitch = st.cvt * V, span = q.rows * pitch, slot = (threadIdx.x - q.row * st.cvt) * V;
   if (q.row < q.rows) {
     float s[V], sx[V];
@@ -324,21 +370,16 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(cons
       rstd.all(scale);
 #pragma unroll
       for (int i = 0; i < V; ++i) less[i] = -less[i];
-      const T* x = (const T*)a.x + q.n * a.x_n + q.c;
-      const T* d = (const T*)a.dy + q.n * a.d_n + q.c;
-      const T* r = RES ? (const T*)a.res + q.n * a.r_n + q.c : nullptr;
-      T* dres = a.dres ? (T*)a.dres + (long long)q.n * a.P * a.C + q.c : nullptr;
-      Raw<T, V> xr[GN_GRAD_BATCH], dr[GN_GRAD_BATCH], rr[RES ? GN_GRAD_BATCH : 1];
+      T* dres = a.dres ? (T*)a.dres + ((long long)q.n * a.P + q.p) * a.C + q.c : nullptr;
+      const long long step = (long long)q.rows * a.C;
       const int act = act_of<ACT>(a);
-      const unsigned long long once = l2_policy(st.held);                       // what the second pass will not read again
-      walk<GN_GRAD_BATCH>(q, [&](int k, long long p) { xr[k].load(x + p * a.x_p); dr[k].load(d + p * a.d_p, once); if (RES) rr[k].load(r + p * a.r_p, once); },
-           [&](int k, long long p) {
-             float xh[V], dz[V];
-             vector_grad<T, V>(xr[k], dr[k], RES ? &rr[k] : nullptr, less, scale, w, b, act, xh, dz);
-             vadd<V>(s, s, dz);
-             vfma<V>(sx, dz, xh, sx);
-             if (dres) { Raw<T, V> o; o.round(dz); o.store(dres + p * a.C); }
-           });
+      walk.run([&](const Raw<T, V> (&r)[NT], int) {
+        float xh[V], dz[V];
+        vector_grad<T, V>(r[0], r[1], RES ? &r[NT - 1] : nullptr, less, scale, w, b, act, xh, dz);
+        vadd<V>(s, s, dz);
+        vfma<V>(sx, dz, xh, sx);
+        if (dres) { Raw<T, V> o; o.round(dz); o.store(dres); dres += step; }
+      });
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) { sh[q.row * pitch + slot + i] = s[i]; sh[span + q.row * pitch + slot + i] = sx[i]; }
@@ -384,7 +425,9 @@ __global__ void __launch_bounds__(GN_THREADS) k_gn_param_grads(const Args a, lon
 
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_apply(const Args a, const Stream st) {
-  extern __shared__ float2 stat[];        // [tile_groups]
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int NT = RES ? 3 : 2;
+  float2* const stat = (float2*)(smem + ring_bytes(V * sizeof(T), NT));         // [tile_groups]
   let_next_start();
   if ((int)blockIdx.z < st.param_z) {     // dw and db, beside the rest
     wait_for_previous();
@@ -394,6 +437,12 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_apply(con
   }
   const Place q = place<V>(a, st);
   const float inv_cg = 1.0f / (float)a.Cg;
+  Walk<T, V, NT, true> walk;
+  walk.set(q, smem);
+  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p, true);
+  walk.tensor(1, q, (const T*)a.dy + q.n * a.d_n + q.c, a.d_p, true);
+  if constexpr (RES) walk.tensor(2, q, (const T*)a.res + q.n * a.r_n + q.c, a.r_p, true);
+  if (!st.held) walk.start();             // held: the first pass writes what is read here
   float w[V], b[V], less[V], scale[V], p1[V], p2[V], gw[V];
   if (q.on) {
     params<V>(a.w, a.ptype, q.c, 1.0f, w);
@@ -408,6 +457,7 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_apply(con
     for (int i = 0; i < V; ++i) less[i] = -less[i];
   }
   wait_for_previous();
+  if (st.held) walk.start();
   // the tile's groups: mean(g) and mean(g * xhat), negated
   const Tile tile = tile_of(a, st, blockIdx.y, V);
   const float inv_m = 1.0f / ((float)a.P * (float)a.Cg);
@@ -429,22 +479,19 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_apply(con
     m2.all(p2);
     vmul<V>(gw, w, scale);
   }
-  const T* x = (const T*)a.x + q.n * a.x_n + q.c;
-  const T* d = (const T*)a.dy + q.n * a.d_n + q.c;
-  const T* r = RES ? (const T*)a.res + q.n * a.r_n + q.c : nullptr;
-  T* dx = (T*)a.out + (long long)q.n * a.P * a.C + q.c;
-  Raw<T, V> xr[GN_GRAD_BATCH], dr[GN_GRAD_BATCH], rr[RES ? GN_GRAD_BATCH : 1];
+  T* dx = (T*)a.out + ((long long)q.n * a.P + walk.first(q)) * a.C + q.c;
+  const long long step = (long long)q.rows * a.C;
   const int act = act_of<ACT>(a);
-  walk_back<GN_GRAD_BATCH>(q, [&](int k, long long p) { xr[k].load_stream(x + p * a.x_p); dr[k].load_stream(d + p * a.d_p); if (RES) rr[k].load_stream(r + p * a.r_p); },
-       [&](int k, long long p) {
-         float xh[V], dz[V];
-         vector_grad<T, V>(xr[k], dr[k], RES ? &rr[k] : nullptr, less, scale, w, b, act, xh, dz);
-         vfma<V>(xh, xh, p2, p1);
-         vfma<V>(dz, dz, gw, xh);
-         Raw<T, V> o;
-         o.round(dz);
-         o.store_stream(dx + p * a.C);
-       });
+  walk.run([&](const Raw<T, V> (&r)[NT], int) {
+    float xh[V], dz[V];
+    vector_grad<T, V>(r[0], r[1], RES ? &r[NT - 1] : nullptr, less, scale, w, b, act, xh, dz);
+    vfma<V>(xh, xh, p2, p1);
+    vfma<V>(dz, dz, gw, xh);
+    Raw<T, V> o;
+    o.round(dz);
+    o.store_stream(dx);
+    dx -= step;
+  });
 }
 
 }  // namespace sae

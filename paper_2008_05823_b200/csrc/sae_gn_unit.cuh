@@ -19,17 +19,6 @@ struct Unit {
   int slots;                             // vectors a thread holds of each tensor
 };
 
-template <int BYTES>
-__device__ __forceinline__ void copy_async(void* to, const void* from) {
-  const unsigned int s = (unsigned int)__cvta_generic_to_shared(to);
-  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(from) : "memory");
-  else if constexpr (BYTES >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(s), "l"(from), "n"(BYTES) : "memory");
-  else *(unsigned short*)to = __ldg((const unsigned short*)from);
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // A thread's `turns` vectors, `step` elements apart, into its slots.
 template <typename T, int V>
 __device__ __forceinline__ void fetch(typename Raw<T, V>::B* to, const T* from, long long step, int pitch, int turns) {

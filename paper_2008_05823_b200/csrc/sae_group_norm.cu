@@ -64,6 +64,7 @@ int tune(const char*, int otherwise) { return otherwise; }
 #endif
 
 constexpr int SMEM_BLOCK = 227 * 1024;
+constexpr int SMEM_MOST = SMEM_BLOCK / 2;           // no kernel here takes more: two blocks an SM at least
 
 // One pass over a unit of `seg` bytes a pixel or a little less (whole groups, whole vectors), in clusters of up to `most` blocks
 // of up to `room` bytes; false if the unit does not fit.
@@ -120,8 +121,8 @@ void stream_plan(const sae_group_norm_desc* d, int vec, bool backward, bool resi
   const long long parts = (d->samples + p.portion - 1) / p.portion;
   p.portion = (int)((d->samples + parts - 1) / parts);
   const long long wave = (long long)sms * tune("GN_WAVE", 3), blocks = (long long)p.portion * s.tiles;
-  // one wave of blocks, but at least two batches of pixels for a thread
-  const long long most = std::max<long long>(1, d->pixels / ((long long)rows * GN_BATCH * 2));
+  // one wave of blocks, but at least eight vectors for a thread
+  const long long most = std::max<long long>(1, d->pixels / ((long long)rows * 8));
   s.slices = (int)std::min<long long>(1024, std::min(std::max<long long>(1, wave / blocks), most));
   s.px = (int)((d->pixels + s.slices - 1) / s.slices);
   s.slices = (int)((d->pixels + s.px - 1) / s.px);
@@ -165,16 +166,24 @@ Args make_args(const sae_group_norm_desc* d, const Plan& p, void* ws) {
   return a;
 }
 
-// A unit kernel in clusters of S blocks.  Its shared memory needs an opt-in above 48 KB, once a device and kernel.
-template <void (*KERNEL)(const Args, const Unit)>
-int launch_units(const Args& a, const Plan& p, cudaStream_t st) {
+// Dynamic shared memory above 48 KB needs an opt-in, once a device and kernel.
+template <auto KERNEL>
+int opt_in() {
   static thread_local int opted = -1;               // one variable for each kernel
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
   if (opted != dev) {
-    if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BLOCK) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
+    if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
     opted = dev;
   }
+  return SAE_OK;
+}
+
+// A unit kernel in clusters of S blocks.
+template <void (*KERNEL)(const Args, const Unit)>
+int launch_units(const Args& a, const Plan& p, cudaStream_t st) {
+  const int rc = opt_in<KERNEL>();
+  if (rc != SAE_OK) return rc;
   cudaLaunchConfig_t cfg = {};
   const int ny = std::min(a.N, 32768);
   cfg.gridDim = dim3((unsigned)(p.u.chunks * p.u.S), (unsigned)ny, (unsigned)((a.N + ny - 1) / ny));
@@ -191,8 +200,12 @@ int launch_units(const Args& a, const Plan& p, cudaStream_t st) {
 }
 
 // One of a call's streaming kernels: all but the first may start before their predecessor's end (they wait for it themselves).
-template <typename... P, typename... A>
-int launch(void (*kernel)(P...), dim3 grid, size_t smem, cudaStream_t st, bool first, A... args) {
+template <auto KERNEL, typename... A>
+int launch(dim3 grid, size_t smem, cudaStream_t st, bool first, A... args) {
+  if (smem > 48 * 1024) {
+    const int rc = opt_in<KERNEL>();
+    if (rc != SAE_OK) return rc;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(GN_THREADS);
@@ -203,7 +216,7 @@ int launch(void (*kernel)(P...), dim3 grid, size_t smem, cudaStream_t st, bool f
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = first ? 0 : 1;
-  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
+  if (cudaLaunchKernelEx(&cfg, KERNEL, args...) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
   return SAE_OK;
 }
 
@@ -213,23 +226,26 @@ int forward_as(const Args& a, const Plan& p, cudaStream_t st) {
   Stream s = p.s;
   const int rows = GN_THREADS / s.cvt;
   const size_t stat = s.tile_groups * sizeof(float2);
+  constexpr int VB = V * (int)sizeof(T);
   int rc = SAE_OK;
   for (s.n0 = 0; s.n0 < a.N && rc == SAE_OK; s.n0 += p.portion) {
     const unsigned n = (unsigned)std::min(p.portion, a.N - s.n0);
     const dim3 grid((unsigned)s.slices, (unsigned)s.tiles, n);
-    rc = launch(k_gn_statistics<T, V, WHOLE>, grid, (size_t)(rows * s.cvt * (WHOLE ? 1 : V) + s.tile_groups) * 4, st, s.n0 == 0, a, s);
-    if (rc == SAE_OK) rc = launch(a.res ? k_gn_apply<T, V, WHOLE, true> : k_gn_apply<T, V, WHOLE, false>, grid, stat, st, false, a, s);
+    rc = launch<k_gn_statistics<T, V, WHOLE>>(grid, ring_bytes(VB, 1) + (size_t)(rows * s.cvt * (WHOLE ? 1 : V) + s.tile_groups) * 4, st, s.n0 == 0, a, s);
+    if (rc != SAE_OK) break;
+    if (a.res) rc = launch<k_gn_apply<T, V, WHOLE, true>>(grid, ring_bytes(VB, 2) + stat, st, false, a, s);
+    else rc = launch<k_gn_apply<T, V, WHOLE, false>>(grid, ring_bytes(VB, 1) + stat, st, false, a, s);
   }
   return rc;
 }
 
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 int grad_sums(const Args& a, const Stream& s, dim3 grid, cudaStream_t st, bool first) {
-  return launch(k_gn_grad_sums<T, V, WHOLE, ACT, RES>, grid, (size_t)2 * (GN_THREADS / s.cvt) * s.cvt * V * 4, st, first, a, s);
+  return launch<k_gn_grad_sums<T, V, WHOLE, ACT, RES>>(grid, ring_bytes(V * sizeof(T), RES ? 3 : 2) + (size_t)2 * (GN_THREADS / s.cvt) * s.cvt * V * 4, st, first, a, s);
 }
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 int grad_apply(const Args& a, const Stream& s, dim3 grid, cudaStream_t st, bool) {
-  return launch(k_gn_grad_apply<T, V, WHOLE, ACT, RES>, grid, s.tile_groups * sizeof(float2), st, false, a, s);
+  return launch<k_gn_grad_apply<T, V, WHOLE, ACT, RES>>(grid, ring_bytes(V * sizeof(T), RES ? 3 : 2) + s.tile_groups * sizeof(float2), st, false, a, s);
 }
 #define GN_ACT(fn, ...)                                                                                              \
   (a.act == SAE_ACT_NONE ? fn<T, V, WHOLE, 0, false>(__VA_ARGS__)                                                     \
@@ -242,7 +258,7 @@ int backward_as(const Args& all, const Plan& p, cudaStream_t st) {
   int rc = SAE_OK;
   if (p.unit) {
     rc = launch_units<k_gn_grad_unit<T, V, WHOLE>>(all, p, st);
-    if (rc == SAE_OK && param_blocks) rc = launch(k_gn_param_grads, dim3(param_blocks), 0, st, false, all, (long long)all.N);
+    if (rc == SAE_OK && param_blocks) rc = launch<k_gn_param_grads>(dim3(param_blocks), 0, st, false, all, (long long)all.N);
     return rc;
   }
   Stream s = p.s;

@@ -42,21 +42,23 @@ __device__ __forceinline__ unsigned long long l2_policy(bool evict_first) {
   asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(usual));
   return evict_first ? first : usual;
 }
-__device__ __forceinline__ uint4 load_hint(const uint4* p, unsigned long long policy) {
-  uint4 v;
-  asm volatile("ld.global.nc.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p), "l"(policy));
-  return v;
+// Copies to shared memory that a thread waits for itself.  Two bytes have no asynchronous form.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+  const unsigned int s = (unsigned int)__cvta_generic_to_shared(to);
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(from) : "memory");
+  else if constexpr (BYTES >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(s), "l"(from), "n"(BYTES) : "memory");
+  else *(unsigned short*)to = __ldg((const unsigned short*)from);
 }
-__device__ __forceinline__ unsigned int load_hint(const unsigned int* p, unsigned long long policy) {
-  unsigned int v;
-  asm volatile("ld.global.nc.L2::cache_hint.u32 %0, [%1], %2;" : "=r"(v) : "l"(p), "l"(policy));
-  return v;
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* to, const void* from, unsigned long long policy) {
+  const unsigned int s = (unsigned int)__cvta_generic_to_shared(to);
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(s), "l"(from), "l"(policy) : "memory");
+  else asm volatile("cp.async.ca.shared.global.L2::cache_hint [%0], [%1], %2, %3;" ::"r"(s), "l"(from), "n"(BYTES), "l"(policy) : "memory");
 }
-__device__ __forceinline__ unsigned short load_hint(const unsigned short* p, unsigned long long policy) {
-  unsigned short v;
-  asm volatile("ld.global.nc.L2::cache_hint.u16 %0, [%1], %2;" : "=h"(v) : "l"(p), "l"(policy));
-  return v;
-}
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // V elements as they lie in memory; V * sizeof(T) is 2, 4, 8 or 16 bytes and the address a multiple of it.
 template <typename T, int V>
@@ -64,8 +66,6 @@ struct Raw {
   typedef typename Bits<V * (int)sizeof(T)>::type B;
   B b;
   __device__ __forceinline__ void load(const T* p) { b = __ldg(reinterpret_cast<const B*>(p)); }
-  __device__ __forceinline__ void load(const T* p, unsigned long long policy) { b = load_hint(reinterpret_cast<const B*>(p), policy); }
-  __device__ __forceinline__ void load_stream(const T* p) { b = __ldcs(reinterpret_cast<const B*>(p)); }
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<B*>(p) = b; }
   __device__ __forceinline__ void store_stream(T* p) const { __stcs(reinterpret_cast<B*>(p), b); }
   __device__ __forceinline__ void widen(float (&v)[V]) const {
