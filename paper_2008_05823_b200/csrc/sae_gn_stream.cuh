@@ -38,8 +38,8 @@ __device__ __forceinline__ int slice_count(const Args& a, const Stream& s, int i
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// How many of its pixels a thread has on their way: 64 KB of a block's shared memory, three blocks an SM.
-__host__ __device__ constexpr int ring_depth(int bytes, int tensors) { return bytes < 4 ? 8 : 256 / (bytes * tensors) < 24 ? 256 / (bytes * tensors) : 24; }
+// How many of its pixels a thread has on their way: up to 64 KB of a block's shared memory, three blocks an SM.
+__host__ __device__ constexpr int ring_depth(int bytes, int tensors) { return bytes == 16 ? (tensors == 3 ? 5 : 8) : bytes == 4 ? 16 : 8; }
 __host__ __device__ constexpr size_t ring_bytes(int bytes, int tensors) { return bytes < 4 ? 0 : (size_t)ring_depth(bytes, tensors) * tensors * bytes * GN_THREADS; }
 
 // A thread's walk over its pixels of NT tensors, first to last or (BACK) last to first: the second pass begins with what the
@@ -90,17 +90,17 @@ struct Walk {
   template <typename F>
   __device__ __forceinline__ void run(F use) {
     if constexpr (sizeof(B) >= 4) {
-      int to = D - 1, from = 0;
-#pragma unroll 2
-      for (int k = 0; k < turns; ++k) {
-        fetch(to);
-        to = to + 1 == D ? 0 : to + 1;
-        copies_wait<D - 1>();
-        Raw<T, V> r[NT];
+      for (int k = 0; k < turns; k += D) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) r[t].b = slots[(from * NT + t) * GN_THREADS];
-        from = from + 1 == D ? 0 : from + 1;
-        use(r, k);
+        for (int j = 0; j < D; ++j) {                       // slot j; the one before it has just been used
+          if (k + j >= turns) break;
+          fetch((j + D - 1) % D);
+          copies_wait<D - 1>();
+          Raw<T, V> r[NT];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) r[t].b = slots[(j * NT + t) * GN_THREADS];
+          use(r, k + j);
+        }
       }
       copies_wait<0>();
     } else {
@@ -198,7 +198,7 @@ template <typename T, int V, bool WHOLE>
 __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_statistics(const Args a, const Stream st) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int SL = WHOLE ? 1 : V;
-  float* const sh = (float*)(smem + ring_bytes(V * sizeof(T), 1));              // [rows][cvt * SL], then [tile_groups]
+  float* const sh = (float*)smem;         // after the walk: [rows][cvt * SL], then [tile_groups]
   let_next_start();
   const Place q = place<V>(a, st);
   const float inv_cg = 1.0f / (float)a.Cg;
@@ -244,6 +244,7 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_statistics(const Args a, c
     vfma<V>(s2, v, v, s2);
   });
   if (walk.turns > 0) join(((walk.turns - 1) & 31) + 1);
+  __syncthreads();                        // everybody is through with the ring
   // the block's mean of each group of its tile, then the squares about it
   const Tile tile = tile_of(a, st, blockIdx.y, V);
   const int pitch = st.cvt * SL, slot = q.row * pitch + (threadIdx.x - q.row * st.cvt) * SL;
@@ -343,7 +344,7 @@ template <typename T, int V, bool WHOLE, int ACT, bool RES>
 __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(const Args a, const Stream st) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int NT = RES ? 3 : 2;
-  float* const sh = (float*)(smem + ring_bytes(V * sizeof(T), NT));             // [2][rows][cvt * V]; the first rows take the sums, times the weight
+  float* const sh = (float*)smem;         // after the walk: [2][rows][cvt * V]; the first rows take the sums, times the weight
   let_next_start();
   const Place q = place<V>(a, st);
   const float inv_cg = 1.0f / (float)a.Cg;
@@ -354,33 +355,34 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(cons
   if constexpr (RES) walk.tensor(2, q, (const T*)a.res + q.n * a.r_n + q.c, a.r_p, st.held);
   walk.start();
   const int pitch = st.cvt * V, span = q.rows * pitch, slot = (threadIdx.x - q.row * st.cvt) * V;
+  float s[V], sx[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) { s[i] = 0.0f; sx[i] = 0.0f; }
+  if (q.on) {
+    float w[V], b[V], less[V], scale[V];
+    params<V>(a.w, a.ptype, q.c, 1.0f, w);
+    params<V>(a.b, a.ptype, q.c, 0.0f, b);
+    Per<V, WHOLE> mean, rstd;
+    const long long g = (long long)q.n * a.G;
+    mean.set([&](int i) { return __ldg(a.mean + g + quotient(q.c + i, inv_cg)); });
+    rstd.set([&](int i) { return __ldg(a.rstd + g + quotient(q.c + i, inv_cg)); });
+    mean.all(less);
+    rstd.all(scale);
+#pragma unroll
+    for (int i = 0; i < V; ++i) less[i] = -less[i];
+    T* dres = a.dres ? (T*)a.dres + ((long long)q.n * a.P + q.p) * a.C + q.c : nullptr;
+    const long long step = (long long)q.rows * a.C;
+    const int act = act_of<ACT>(a);
+    walk.run([&](const Raw<T, V> (&r)[NT], int) {
+      float xh[V], dz[V];
+      vector_grad<T, V>(r[0], r[1], RES ? &r[NT - 1] : nullptr, less, scale, w, b, act, xh, dz);
+      vadd<V>(s, s, dz);
+      vfma<V>(sx, dz, xh, sx);
+      if (dres) { Raw<T, V> o; o.round(dz); o.store(dres); dres += step; }
+    });
+  }
+  __syncthreads();                        // everybody is through with the ring
   if (q.row < q.rows) {
-    float s[V], sx[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) { s[i] = 0.0f; sx[i] = 0.0f; }
-    if (q.on) {
-      float w[V], b[V], less[V], scale[V];
-      params<V>(a.w, a.ptype, q.c, 1.0f, w);
-      params<V>(a.b, a.ptype, q.c, 0.0f, b);
-      Per<V, WHOLE> mean, rstd;
-      const long long g = (long long)q.n * a.G;
-      mean.set([&](int i) { return __ldg(a.mean + g + quotient(q.c + i, inv_cg)); });
-      rstd.set([&](int i) { return __ldg(a.rstd + g + quotient(q.c + i, inv_cg)); });
-      mean.all(less);
-      rstd.all(scale);
-#pragma unroll
-      for (int i = 0; i < V; ++i) less[i] = -less[i];
-      T* dres = a.dres ? (T*)a.dres + ((long long)q.n * a.P + q.p) * a.C + q.c : nullptr;
-      const long long step = (long long)q.rows * a.C;
-      const int act = act_of<ACT>(a);
-      walk.run([&](const Raw<T, V> (&r)[NT], int) {
-        float xh[V], dz[V];
-        vector_grad<T, V>(r[0], r[1], RES ? &r[NT - 1] : nullptr, less, scale, w, b, act, xh, dz);
-        vadd<V>(s, s, dz);
-        vfma<V>(sx, dz, xh, sx);
-        if (dres) { Raw<T, V> o; o.round(dz); o.store(dres); dres += step; }
-      });
-    }
 #pragma unroll
     for (int i = 0; i < V; ++i) { sh[q.row * pitch + slot + i] = s[i]; sh[span + q.row * pitch + slot + i] = sx[i]; }
   }

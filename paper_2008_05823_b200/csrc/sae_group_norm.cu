@@ -106,7 +106,7 @@ bool unit_plan(const sae_group_norm_desc* d, int vec, int tensors, bool backward
   return true;
 }
 
-// Two passes.  A portion of samples is what L2 keeps from the first pass to the second; a launch is about one wave of blocks.
+// Two passes, each of about one wave of blocks; a portion is what a grid's third dimension holds.
 void stream_plan(const sae_group_norm_desc* d, int vec, bool backward, bool residual, int sms, Plan& p) {
   const int cv = (int)((d->channels + vec - 1) / vec);
   Stream& s = p.s;
@@ -115,12 +115,9 @@ void stream_plan(const sae_group_norm_desc* d, int vec, bool backward, bool resi
   s.tiles = (cv + s.cvt - 1) / s.cvt;
   const int rows = GN_THREADS / s.cvt, tile_c = s.cvt * vec, cg_ = (int)(d->channels / d->groups);
   s.tile_groups = std::min(d->groups, tile_c / cg_ + 2);
-  const long long sample = d->pixels * d->channels * elem(d->type) * (backward ? 2 + (residual ? 2 : 0) : 1);
-  const long long keep = (long long)tune("GN_L2", 48) << 20;
-  p.portion = (int)std::max<long long>(1, std::min<long long>(std::min<long long>(d->samples, 32768), keep / std::max<long long>(1, sample)));
-  const long long parts = (d->samples + p.portion - 1) / p.portion;
-  p.portion = (int)((d->samples + parts - 1) / parts);
-  const long long wave = (long long)sms * tune("GN_WAVE", 3), blocks = (long long)p.portion * s.tiles;
+  p.portion = (int)std::min<long long>(d->samples, 32768);
+  const bool whole = cg_ % vec == 0;
+  const long long wave = (long long)sms * tune("GN_WAVE", backward && !whole ? 2 : 3), blocks = (long long)p.portion * s.tiles;
   // one wave of blocks, but at least eight vectors for a thread
   const long long most = std::max<long long>(1, d->pixels / ((long long)rows * 8));
   s.slices = (int)std::min<long long>(1024, std::min(std::max<long long>(1, wave / blocks), most));
@@ -231,7 +228,7 @@ int forward_as(const Args& a, const Plan& p, cudaStream_t st) {
   for (s.n0 = 0; s.n0 < a.N && rc == SAE_OK; s.n0 += p.portion) {
     const unsigned n = (unsigned)std::min(p.portion, a.N - s.n0);
     const dim3 grid((unsigned)s.slices, (unsigned)s.tiles, n);
-    rc = launch<k_gn_statistics<T, V, WHOLE>>(grid, ring_bytes(VB, 1) + (size_t)(rows * s.cvt * (WHOLE ? 1 : V) + s.tile_groups) * 4, st, s.n0 == 0, a, s);
+    rc = launch<k_gn_statistics<T, V, WHOLE>>(grid, std::max(ring_bytes(VB, 1), (size_t)(rows * s.cvt * (WHOLE ? 1 : V) + s.tile_groups) * 4), st, s.n0 == 0, a, s);
     if (rc != SAE_OK) break;
     if (a.res) rc = launch<k_gn_apply<T, V, WHOLE, true>>(grid, ring_bytes(VB, 2) + stat, st, false, a, s);
     else rc = launch<k_gn_apply<T, V, WHOLE, false>>(grid, ring_bytes(VB, 1) + stat, st, false, a, s);
@@ -241,7 +238,8 @@ int forward_as(const Args& a, const Plan& p, cudaStream_t st) {
 
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 int grad_sums(const Args& a, const Stream& s, dim3 grid, cudaStream_t st, bool first) {
-  return launch<k_gn_grad_sums<T, V, WHOLE, ACT, RES>>(grid, ring_bytes(V * sizeof(T), RES ? 3 : 2) + (size_t)2 * (GN_THREADS / s.cvt) * s.cvt * V * 4, st, first, a, s);
+  return launch<k_gn_grad_sums<T, V, WHOLE, ACT, RES>>(
+      grid, std::max(ring_bytes(V * sizeof(T), RES ? 3 : 2), (size_t)2 * (GN_THREADS / s.cvt) * s.cvt * V * 4), st, first, a, s);
 }
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 int grad_apply(const Args& a, const Stream& s, dim3 grid, cudaStream_t st, bool) {
