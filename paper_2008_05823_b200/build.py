@@ -35,7 +35,7 @@ def _host_command(out, sources):
     cmd += ["-o", out] + sources + ["-L" + HERE, "-l:libsae.so", "-Wl,-rpath,$ORIGIN"]
     for lib in cpp_extension.library_paths() + [os.path.join(cuda, "lib64")]:
         cmd.append("-L" + lib)
-    return cmd + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python", "-lcudart"]
+    return cmd + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch", "-ltorch_python", "-lcudart"]
 
 
 def _stale(out, deps):

@@ -4,11 +4,13 @@
 // No arithmetic happens here.
 #include "../../include/sae.h"
 
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <cuda_runtime_api.h>
 #include <torch/extension.h>
 
+#include <cstring>
 #include <vector>
 
 namespace py = pybind11;
@@ -21,6 +23,11 @@ int type_of(at::ScalarType t) {
 }
 
 [[noreturn]] void refuse(const std::string& why) { throw py::value_error(why); }
+
+// A new tensor, straight from the CUDA allocator (the dispatcher's way costs three times the time).
+Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, at::Device device) {
+  return at::detail::empty_cuda(sizes, type, device, std::nullopt);
+}
 
 const Tensor& tensor_of(PyObject* o) {
   if (!THPVariable_Check(o)) refuse("tensors are wanted");
@@ -51,7 +58,7 @@ class GradPlan {
     return {on_stream([&] { return sae_grads_clip(h_, const_cast<void* const*>(ptrs.data()), kind, max_norm, norms.data_ptr<float>()); }), norms};
   }
   std::tuple<int, Tensor, std::optional<Tensor>> pack(py::handle tensors, std::optional<Tensor> out, int kind, float max_norm) {
-    if (!out) out = at::empty({K_, d_}, options());
+    if (!out) out = fresh({K_, d_}, at::kFloat, device());
     const int64_t stride = vector(*out, "out", false);
     auto ptrs = pointers(tensors);
     std::optional<Tensor> norms;
@@ -68,8 +75,8 @@ class GradPlan {
   }
 
  private:
-  at::TensorOptions options() const { return at::TensorOptions().dtype(at::kFloat).device(at::Device(at::kCUDA, (c10::DeviceIndex)device_)); }
-  Tensor rows() const { return at::empty({K_}, options()); }
+  at::Device device() const { return at::Device(at::kCUDA, (c10::DeviceIndex)device_); }
+  Tensor rows() const { return fresh({K_}, at::kFloat, device()); }
 
   // The row stride of a [d] (one row, or the same for all) or [K, d] float32 tensor.
   int64_t vector(const Tensor& v, const char* what, bool same) const {
@@ -190,7 +197,8 @@ sae_group_norm_desc describe(const Tensor& x, int64_t groups, const Maybe& weigh
   if (!x.is_cuda() || type_of(x.scalar_type()) < 0 || x.dim() < 2) refuse("x must be a float32, bfloat16 or float16 CUDA tensor [n, c, *space]");
   const int64_t c = x.size(1);
   if (groups < 1 || c < 1 || c % groups || groups > INT32_MAX) refuse("the number of groups must divide the number of channels");
-  sae_group_norm_desc d = {};
+  sae_group_norm_desc d;
+  std::memset(&d, 0, sizeof(d));                 // padding too: descriptions are compared
   d.type = type_of(x.scalar_type());
   d.param_type = SAE_TYPE_FLOAT;
   for (int i = 0; i < 2; ++i) {
@@ -220,15 +228,24 @@ Tensor dense(const Tensor& x) {
   st[1] = 1;
   for (int64_t i = x.dim() - 1; i >= 2; --i) { st[i] = run; run *= std::max<int64_t>(1, x.size(i)); }
   st[0] = run;
-  return at::empty_strided(x.sizes(), st, x.options());
+  return at::detail::empty_strided_cuda(x.sizes(), st, x.scalar_type(), x.device());
 }
 
 void* ptr(const Maybe& t) { return t ? t->data_ptr() : nullptr; }
 
 Tensor workspace(const sae_group_norm_desc& d, const Tensor& x, int backward, size_t& bytes) {
-  const int64_t n = sae_group_norm_workspace(&d, backward);
-  bytes = n > 0 ? (size_t)n : 0;
-  return bytes ? at::empty({n}, x.options().dtype(at::kByte)) : Tensor();
+  // asked for once for a description: a layer's calls have the same one over and over
+  static thread_local sae_group_norm_desc last[2];
+  static thread_local int64_t last_bytes[2] = {-1, -1};
+  static thread_local int last_device[2] = {-1, -1};
+  const int device = x.get_device();
+  if (last_device[backward] != device || std::memcmp(&last[backward], &d, sizeof(d)) != 0) {
+    last_bytes[backward] = sae_group_norm_workspace(&d, backward);
+    last[backward] = d;
+    last_device[backward] = device;
+  }
+  bytes = last_bytes[backward] > 0 ? (size_t)last_bytes[backward] : 0;
+  return bytes ? fresh({(int64_t)bytes}, at::kByte, x.device()) : Tensor();
 }
 
 std::tuple<int, Tensor, Tensor, Tensor> group_norm_forward(const Tensor& x, int64_t groups, const Maybe& weight, const Maybe& bias,
@@ -236,7 +253,7 @@ std::tuple<int, Tensor, Tensor, Tensor> group_norm_forward(const Tensor& x, int6
   const sae_group_norm_desc d = describe(x, groups, weight, bias, eps, act, residual);
   c10::cuda::CUDAGuard guard(x.device());
   Tensor y = dense(x);
-  Tensor mean = at::empty({x.size(0), groups}, x.options().dtype(at::kFloat)), rstd = at::empty_like(mean);
+  Tensor mean = fresh({x.size(0), groups}, at::kFloat, x.device()), rstd = fresh({x.size(0), groups}, at::kFloat, x.device());
   size_t bytes;
   Tensor ws = workspace(d, x, 0, bytes);
   const int rc = sae_group_norm_forward(&d, x.data_ptr(), ptr(residual), ptr(weight), ptr(bias), y.data_ptr(), (float*)mean.data_ptr(),
@@ -257,8 +274,8 @@ std::tuple<int, Tensor, Maybe, Maybe, Maybe> group_norm_backward(const Tensor& d
   Tensor dx = dense(x);
   Maybe dres, dweight, dbias;
   if (residual && need_residual) dres = dense(x);
-  if (weight && need_params) dweight = at::empty_like(*weight);
-  if (bias && need_params) dbias = at::empty_like(*bias);
+  if (weight && need_params) dweight = fresh(weight->sizes(), weight->scalar_type(), x.device());
+  if (bias && need_params) dbias = fresh(bias->sizes(), bias->scalar_type(), x.device());
   size_t bytes;
   Tensor ws = workspace(d, x, 1, bytes);
   const int rc = sae_group_norm_backward(&d, dy.data_ptr(), x.data_ptr(), ptr(residual), (const float*)mean.data_ptr(), (const float*)rstd.data_ptr(),

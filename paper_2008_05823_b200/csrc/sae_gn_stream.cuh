@@ -31,7 +31,7 @@ __device__ __forceinline__ Place place(const Args& a, const Stream& s) {
   q.p1 = min(a.P, (q.slice + 1) * s.px);
   return q;
 }
-__device__ __forceinline__ int slice_count(const Args& a, const Stream& s, int i) { return min(s.px, a.P - i * s.px); }
+__device__ __forceinline__ int run_pixels(const Args& a, const Stream& s, int i) { return min(s.px, a.P - i * s.px); }
 
 // A stream kernel lets its successor start as soon as all its blocks run, and itself waits, before it touches what another
 // kernel of the call has written, for all of its predecessor.
@@ -148,15 +148,29 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
   return v;
 }
 
-// Sums of each group's values in sh[rows][pitch], SL of them a vector of V channels: out(j, sum, channels).
+// Sums of each group's values in sh[rows][pitch], SL of them a vector of V channels: out(j, sum, channels).  Where there are
+// more values than threads, columns are added up over the rows first.  Begins with a barrier.
 template <int SL, int V, typename F>
-__device__ __forceinline__ void fold_tile(const Args& a, const Tile& t, const float* sh, int rows, int pitch, F out) {
+__device__ __forceinline__ void fold_tile(const Args& a, const Tile& t, float* sh, int rows, int pitch, F out) {
+  __syncthreads();
+  if (rows > 1 && rows * pitch > GN_THREADS) {
+    for (int i = threadIdx.x; i < pitch; i += GN_THREADS) {
+      float s = 0.0f;
+#pragma unroll 4
+      for (int r = 0; r < rows; ++r) s += sh[r * pitch + i];
+      sh[i] = s;
+    }
+    rows = 1;
+    __syncthreads();
+  }
   each_group(t, rows * (a.Cg * SL / V), [&](int j, int lane, int lanes) {
     const int lo = max((t.g0 + j) * a.Cg, t.lo), hi = min((t.g0 + j + 1) * a.Cg, t.hi), len = (hi - lo) * SL / V;
     float s = 0.0f;
     if (j < t.groups) {
       const float* p = sh + (lo - t.lo) * SL / V;
-      if (len == 1) {
+      if (rows == 1) {
+        for (int e = lane; e < len; e += lanes) s += p[e];
+      } else if (len == 1) {
         for (int e = lane; e < rows; e += lanes) s += p[e * pitch];
       } else {
         const float inv = __frcp_rn((float)len);
@@ -171,20 +185,39 @@ __device__ __forceinline__ void fold_tile(const Args& a, const Tile& t, const fl
   });
 }
 
-// The runs' pairs of group g of sample n, dealt to the lanes that share it: f(pixels * channels of the run, pair).
-template <typename F>
-__device__ __forceinline__ void each_run(const Args& a, const Stream& s, int n, int g, int vec, int lane, int lanes, F f) {
+// Joins the runs' pairs of every group of a tile: the threads stand side by side over the groups and, as far as there are
+// more threads, over the runs.  add(sum, pixels * channels, pair, first pair) for each run; done(j, sum) for each group, from
+// one thread, before a barrier.  `sums` holds a pair for each thread.
+template <typename A, typename D>
+__device__ __forceinline__ void join_runs(const Args& a, const Stream& s, const Tile& tile, int n, int vec, float2* sums, A add, D done) {
+  const int tile_c = s.cvt * vec;
   const float2* part = a.part_s + (long long)n * s.slices * s.tiles * s.tile_groups;
-  if (s.tiles == 1) {
-    for (int i = lane; i < s.slices; i += lanes)
-      f((float)slice_count(a, s, i) * (float)a.Cg, __ldcg(part + i * s.tile_groups + g));
-    return;
-  }
-  const int tile_c = s.cvt * vec, t0 = g * a.Cg / tile_c, tiles = (g * a.Cg + a.Cg - 1) / tile_c - t0 + 1;
-  for (int e = lane; e < s.slices * tiles; e += lanes) {
-    const int i = tiles == 1 ? e : e / tiles, t = t0 + (e - i * tiles);
-    const int lo = max(g * a.Cg, t * tile_c), hi = min(min((g + 1) * a.Cg, (t + 1) * tile_c), a.C);
-    f((float)slice_count(a, s, i) * (float)(hi - lo), __ldcg(part + ((long long)i * s.tiles + t) * s.tile_groups + g - t * tile_c / a.Cg));
+  for (int j0 = 0; j0 < tile.groups; j0 += GN_THREADS) {
+    const int across = min(tile.groups - j0, GN_THREADS), subs = GN_THREADS / across, sub = quotient(threadIdx.x, __frcp_rn((float)across));
+    const int j = j0 + (int)threadIdx.x - sub * across, g = tile.g0 + j;
+    float2 t = make_float2(0.0f, 0.0f);
+    if (sub < subs) {
+      if (s.tiles == 1) {
+        const float2 first = __ldcg(part + g);
+#pragma unroll 4
+        for (int i = sub; i < s.slices; i += subs) add(t, (float)run_pixels(a, s, i) * (float)a.Cg, __ldcg(part + i * s.tile_groups + g), first);
+      } else {
+        const int t0 = g * a.Cg / tile_c, tiles = (g * a.Cg + a.Cg - 1) / tile_c - t0 + 1;
+        const float2 first = __ldcg(part + t0 * s.tile_groups + g - t0 * tile_c / a.Cg);
+        for (int e = sub; e < s.slices * tiles; e += subs) {
+          const int i = tiles == 1 ? e : e / tiles, k = t0 + (e - i * tiles);
+          const int lo = max(g * a.Cg, k * tile_c), hi = min(min((g + 1) * a.Cg, (k + 1) * tile_c), a.C);
+          add(t, (float)run_pixels(a, s, i) * (float)(hi - lo), __ldcg(part + ((long long)i * s.tiles + k) * s.tile_groups + g - k * tile_c / a.Cg), first);
+        }
+      }
+    }
+    sums[threadIdx.x] = t;
+    __syncthreads();
+    if (sub == 0) {
+      for (int k = 1; k < subs; ++k) { const float2 o = sums[k * across + (int)threadIdx.x]; t.x += o.x; t.y += o.y; }
+      done(j, t);
+    }
+    __syncthreads();
   }
 }
 __device__ __forceinline__ float2* run_out(const Args& a, const Stream& s, const Place& q) {
@@ -248,13 +281,12 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_statistics(const Args a, c
   // the block's mean of each group of its tile, then the squares about it
   const Tile tile = tile_of(a, st, blockIdx.y, V);
   const int pitch = st.cvt * SL, slot = q.row * pitch + (threadIdx.x - q.row * st.cvt) * SL;
-  const float inv_pixels = 1.0f / (float)slice_count(a, st, q.slice);
+  const float inv_pixels = 1.0f / (float)run_pixels(a, st, q.slice);
   float* const gmean = sh + q.rows * pitch;
   if (q.row < q.rows) {
 #pragma unroll
     for (int i = 0; i < SL; ++i) sh[slot + i] = q.on ? count * mean[i] : 0.0f;
   }
-  __syncthreads();
   fold_tile<SL, V>(a, tile, sh, q.rows, pitch, [&](int j, float s, int channels) { gmean[j] = s * inv_pixels * __frcp_rn((float)channels); });
   __syncthreads();
   if (q.row < q.rows) {
@@ -265,9 +297,8 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_statistics(const Args a, c
       sh[slot + i] = v;
     }
   }
-  __syncthreads();
-  wait_for_previous();
   float2* const out = run_out(a, st, q);
+  wait_for_previous();
   fold_tile<SL, V>(a, tile, sh, q.rows, pitch, [&](int j, float s, int) { out[j] = make_float2(gmean[j], s); });
 }
 
@@ -275,7 +306,7 @@ template <typename T, int V, bool WHOLE, bool RES>
 __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_apply(const Args a, const Stream st) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int NT = RES ? 2 : 1;
-  float2* const stat = (float2*)(smem + ring_bytes(V * sizeof(T), NT));         // [tile_groups]
+  float2* const stat = (float2*)(smem + ring_bytes(V * sizeof(T), NT));         // [tile_groups], then a pair for each thread
   let_next_start();
   const Place q = place<V>(a, st);
   Walk<T, V, NT, true> walk;
@@ -290,21 +321,19 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_apply(const Args a, const 
   // the tile's groups: their runs joined about the group's own mean
   const Tile tile = tile_of(a, st, blockIdx.y, V);
   const float inv_m = 1.0f / ((float)a.P * (float)a.Cg);
-  each_group(tile, st.slices, [&](int j, int lane, int lanes) {
-    const int g = tile.g0 + j;
-    const bool on = j < tile.groups;
-    float s = 0.0f, m2 = 0.0f;
-    if (on) each_run(a, st, q.n, g, V, lane, lanes, [&](float m, float2 v) { s = __fmaf_rn(m * inv_m, v.x, s); });
-    s = lanes_sum(s, lanes);
-    if (on) each_run(a, st, q.n, g, V, lane, lanes, [&](float m, float2 v) { const float d = v.x - s; m2 += __fmaf_rn(m * d, d, v.y); });
-    m2 = lanes_sum(m2, lanes);
-    if (on && lane == 0) {
-      const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(m2 * inv_m + a.eps));
-      stat[j] = make_float2(s, rstd);
-      if (q.slice == 0) { a.mean[(long long)q.n * a.G + g] = s; a.rstd[(long long)q.n * a.G + g] = rstd; }   // tiles that share a group agree
-    }
-  });
-  __syncthreads();
+  // (sums about the first run's mean: it is off by no more than the runs' spread, which the squares contain)
+  join_runs(a, st, tile, q.n, V, stat + st.tile_groups,
+            [&](float2& t, float m, float2 v, float2 first) { const float d = v.x - first.x; t.x = __fmaf_rn(m, d, t.x); t.y += __fmaf_rn(m * d, d, v.y); },
+            [&](int j, float2 t) {
+              const int g = tile.g0 + j;
+              const float d = t.x * inv_m;
+              const float2* part = a.part_s + (long long)q.n * st.slices * st.tiles * st.tile_groups;
+              const int t0 = st.tiles == 1 ? 0 : g * a.Cg / (st.cvt * V);
+              const float mean = __ldcg(part + t0 * st.tile_groups + g - (st.tiles == 1 ? 0 : t0 * (st.cvt * V) / a.Cg)).x + d;
+              const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fmaf_rn(-d, t.x, t.y) * inv_m + a.eps));
+              stat[j] = make_float2(mean, rstd);
+              if (q.slice == 0) { a.mean[(long long)q.n * a.G + g] = mean; a.rstd[(long long)q.n * a.G + g] = rstd; }   // tiles that share a group agree
+            });
   if (!q.on) return;
   {
     Per<V, WHOLE> mean, rstd;
@@ -397,7 +426,6 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(cons
     sh[i] = s * w;
     sh[span + i] = sx * w;
   }
-  __syncthreads();
   float2* const out = run_out(a, st, q);
   fold_tile<V, V>(a, tile, sh, 1, pitch, [&](int j, float s, int) { out[j].x = s; });
   fold_tile<V, V>(a, tile, sh + span, 1, pitch, [&](int j, float s, int) { out[j].y = s; });
@@ -429,7 +457,7 @@ template <typename T, int V, bool WHOLE, int ACT, bool RES>
 __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_apply(const Args a, const Stream st) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int NT = RES ? 3 : 2;
-  float2* const stat = (float2*)(smem + ring_bytes(V * sizeof(T), NT));         // [tile_groups]
+  float2* const stat = (float2*)(smem + ring_bytes(V * sizeof(T), NT));         // [tile_groups], then a pair for each thread
   let_next_start();
   if ((int)blockIdx.z < st.param_z) {     // dw and db, beside the rest
     wait_for_previous();
@@ -463,14 +491,8 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_apply(con
   // the tile's groups: mean(g) and mean(g * xhat), negated
   const Tile tile = tile_of(a, st, blockIdx.y, V);
   const float inv_m = 1.0f / ((float)a.P * (float)a.Cg);
-  each_group(tile, st.slices, [&](int j, int lane, int lanes) {
-    float s = 0.0f, sx = 0.0f;
-    if (j < tile.groups) each_run(a, st, q.n, tile.g0 + j, V, lane, lanes, [&](float, float2 v) { s += v.x; sx += v.y; });
-    s = lanes_sum(s, lanes);
-    sx = lanes_sum(sx, lanes);
-    if (j < tile.groups && lane == 0) stat[j] = make_float2(-s * inv_m, -sx * inv_m);
-  });
-  __syncthreads();
+  join_runs(a, st, tile, q.n, V, stat + st.tile_groups, [&](float2& t, float, float2 v, float2) { t.x += v.x; t.y += v.y; },
+            [&](int j, float2 t) { stat[j] = make_float2(-t.x * inv_m, -t.y * inv_m); });
   if (!q.on) return;
   {
     // dx = rstd * (dz * w - mean(g) - xhat * mean(g * xhat)) = dz * (w rstd) + (xhat * (-rstd mean(g xhat)) - rstd mean(g))

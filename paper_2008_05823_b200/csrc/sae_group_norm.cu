@@ -17,6 +17,7 @@
 #include "sae_gn_unit.cuh"
 
 #include <algorithm>
+#include <atomic>
 
 using namespace sae;
 
@@ -134,20 +135,23 @@ Plan make_plan(const sae_group_norm_desc* d, int vec, bool backward, bool residu
   const bool second = residual || (backward && elem(d->type) == 2 && d->activation >= SAE_ACT_SILU);
   const int tensors = (backward ? 2 : 1) + (second ? 1 : 0);
   const int segs[3] = {tune("GN_SEG", 128), 64, 32};
-  for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, (size_t)tune("GN_ROOM", 72) * 1024, sms, p);
-  for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, (size_t)SMEM_BLOCK / 2 - 1024, sms, p);
-  if (tune("GN_SPLIT", 0)) p.unit = false;
+  const long long traffic = d->samples * d->pixels * d->channels * elem(d->type) * (backward ? 3 + 2 * residual : 2 + residual);
+  if (traffic <= ((long long)tune("GN_UNIT_MB", 32) << 20)) {
+    for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, (size_t)tune("GN_ROOM", 72) * 1024, sms, p);
+    for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, (size_t)SMEM_MOST - 1024, sms, p);
+  }
   if (p.unit) p.bytes = backward ? (size_t)2 * 4 * d->samples * d->channels : 0;
   else stream_plan(d, vec, backward, residual, sms, p);
   return p;
 }
 
 int device_sms() {
+  static std::atomic<int> known[64];
   int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
-    cudaGetLastError();
-    return 0;
-  }
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 0; }
+  if (dev >= 0 && dev < 64 && (sms = known[dev].load(std::memory_order_relaxed)) > 0) return sms;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return 0; }
+  if (dev >= 0 && dev < 64) known[dev].store(sms, std::memory_order_relaxed);
   return sms;
 }
 
@@ -222,7 +226,7 @@ int forward_as(const Args& a, const Plan& p, cudaStream_t st) {
   if (p.unit) return launch_units<k_gn_unit<T, V, WHOLE>>(a, p, st);
   Stream s = p.s;
   const int rows = GN_THREADS / s.cvt;
-  const size_t stat = s.tile_groups * sizeof(float2);
+  const size_t stat = (s.tile_groups + GN_THREADS) * sizeof(float2);
   constexpr int VB = V * (int)sizeof(T);
   int rc = SAE_OK;
   for (s.n0 = 0; s.n0 < a.N && rc == SAE_OK; s.n0 += p.portion) {
@@ -239,11 +243,11 @@ int forward_as(const Args& a, const Plan& p, cudaStream_t st) {
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 int grad_sums(const Args& a, const Stream& s, dim3 grid, cudaStream_t st, bool first) {
   return launch<k_gn_grad_sums<T, V, WHOLE, ACT, RES>>(
-      grid, std::max(ring_bytes(V * sizeof(T), RES ? 3 : 2), (size_t)2 * (GN_THREADS / s.cvt) * s.cvt * V * 4), st, first, a, s);
+      grid, std::max(ring_bytes(V * sizeof(T), RES ? 3 : 2), (size_t)(2 * (GN_THREADS / s.cvt) * s.cvt * V) * 4), st, first, a, s);
 }
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 int grad_apply(const Args& a, const Stream& s, dim3 grid, cudaStream_t st, bool) {
-  return launch<k_gn_grad_apply<T, V, WHOLE, ACT, RES>>(grid, ring_bytes(V * sizeof(T), RES ? 3 : 2) + s.tile_groups * sizeof(float2), st, false, a, s);
+  return launch<k_gn_grad_apply<T, V, WHOLE, ACT, RES>>(grid, ring_bytes(V * sizeof(T), RES ? 3 : 2) + (s.tile_groups + GN_THREADS) * sizeof(float2), st, false, a, s);
 }
 #define GN_ACT(fn, ...)                                                                                              \
   (a.act == SAE_ACT_NONE ? fn<T, V, WHOLE, 0, false>(__VA_ARGS__)                                                     \
