@@ -21,7 +21,6 @@ typedef unsigned int u32;
 
 constexpr int GT_THREADS = 256;
 constexpr int GT_TILE = 8192;            // elements of one tensor that a block handles at a time
-constexpr int GT_VEC = 8;                // elements a thread takes in one piece
 constexpr int GT_BLOCKS_PER_SM = 8;      // 2048 resident threads
 constexpr int PTRS_SMALL = 64;           // tensor pointers that travel as kernel arguments
 constexpr int PTRS_LARGE = 448;
@@ -52,26 +51,6 @@ __global__ void k_upload_ptrs(const __grid_constant__ UploadChunk c, void** tabl
   const int i = blockIdx.x * blockDim.x + threadIdx.x;
   if (i < n) table[i] = c.p[i];
 }
-
-// Eight elements of any type: one piece of 16 bytes, or two.
-template <typename T> struct Eight {
-  Raw<T, 8> a;
-  __device__ __forceinline__ void load(const T* p) { a.load(p); }
-  __device__ __forceinline__ void store(T* p) const { a.store(p); }
-  __device__ __forceinline__ void widen(float (&v)[8]) const { a.widen(v); }
-  __device__ __forceinline__ void round(const float (&v)[8]) { a.round(v); }
-};
-template <> struct Eight<float> {
-  Raw<float, 4> a, b;
-  __device__ __forceinline__ void load(const float* p) { a.load(p); b.load(p + 4); }
-  __device__ __forceinline__ void store(float* p) const { a.store(p); b.store(p + 4); }
-  __device__ __forceinline__ void widen(float (&v)[8]) const {
-    a.widen(*reinterpret_cast<float (*)[4]>(&v[0])); b.widen(*reinterpret_cast<float (*)[4]>(&v[4]));
-  }
-  __device__ __forceinline__ void round(const float (&v)[8]) {
-    a.round(*reinterpret_cast<const float (*)[4]>(&v[0])); b.round(*reinterpret_cast<const float (*)[4]>(&v[4]));
-  }
-};
 
 // ---- the running value of a norm: a double (q = 1, 2), or the bits of the largest magnitude -------------------
 // Eight elements are added in float first and the sum goes to the double accumulator: the float part rounds at most
@@ -132,23 +111,34 @@ __device__ __forceinline__ void block_join(Running<KIND>& r, u64* sh) {
   }
 }
 
+// A thread's pieces are 16 bytes, neighbouring threads' pieces neighbours in memory.
 template <int KIND, typename T>
 __device__ __forceinline__ void tile_norm(Running<KIND>& r, const T* p, u32 cnt) {
+  constexpr int V = 16 / (int)sizeof(T), N = GT_TILE / (GT_THREADS * V);
+  const u32 tid = threadIdx.x;
   if ((reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-    if (cnt == GT_TILE) {
-      Eight<T> raw[GT_TILE / (GT_THREADS * GT_VEC)];
+    const u32 whole = cnt / V;
+    Raw<T, V> raw[N];
 #pragma unroll
-      for (int i = 0; i < GT_TILE / (GT_THREADS * GT_VEC); ++i) raw[i].load(p + (i * GT_THREADS + threadIdx.x) * GT_VEC);
+    for (int i = 0; i < N; ++i)
+      if (cnt == GT_TILE || i * GT_THREADS + tid < whole) raw[i].load(p + (i * GT_THREADS + tid) * V);
+      else raw[i].clear();
+    const u32 e = whole * V + tid;
+    const float last = cnt != GT_TILE && e < cnt ? to_f(p[e]) : 0.0f;
 #pragma unroll
-      for (int i = 0; i < GT_TILE / (GT_THREADS * GT_VEC); ++i) { float v[8]; raw[i].widen(v); r.eight(v); }
-    } else {
-      const u32 whole = cnt / GT_VEC;
-      for (u32 i = threadIdx.x; i < whole; i += GT_THREADS) { Eight<T> raw; raw.load(p + i * GT_VEC); float v[8]; raw.widen(v); r.eight(v); }
-      const u32 e = whole * GT_VEC + threadIdx.x;
-      if (e < cnt) r.one(to_f(p[e]));
+    for (int i = 0; i < N; i += 8 / V) {
+      float v[8];
+      if constexpr (V == 8) {
+        raw[i].widen(v);
+      } else {
+        raw[i].widen(*reinterpret_cast<float (*)[4]>(&v[0]));
+        raw[i + 1].widen(*reinterpret_cast<float (*)[4]>(&v[4]));
+      }
+      r.eight(v);
     }
+    r.one(last);
   } else {
-    for (u32 e = threadIdx.x; e < cnt; e += GT_THREADS) r.one(to_f(p[e]));
+    for (u32 e = tid; e < cnt; e += GT_THREADS) r.one(to_f(p[e]));
   }
 }
 
@@ -163,8 +153,11 @@ __global__ void __launch_bounds__(GT_THREADS) k_grads_norm(const __grid_constant
   const int row = blockIdx.y, B = gridDim.x;
   const int t0 = (int)((long long)ntiles * blockIdx.x / B), t1 = (int)((long long)ntiles * (blockIdx.x + 1) / B);
   Running<KIND> r; r.zero();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  Tile next = t0 < t1 ? tiles[t0] : Tile{};
   for (int t = t0; t < t1; ++t) {
-    const Tile ti = tiles[t];
+    const Tile ti = next;
+    if (t + 1 < t1) next = tiles[t + 1];
     void* base = ptrs.get(row * T + (int)ti.tensor);
     if (ti.type == SAE_TYPE_FLOAT) tile_norm<KIND, float>(r, (const float*)base + ti.start, ti.count);
     else if (ti.type == SAE_TYPE_BFLOAT) tile_norm<KIND, __nv_bfloat16>(r, (const __nv_bfloat16*)base + ti.start, ti.count);
@@ -193,48 +186,52 @@ __global__ void __launch_bounds__(GT_THREADS) k_grads_norm(const __grid_constant
 }
 
 // ---- scaled copies --------------------------------------------------------------------------------------------
-// coef = 1 multiplies exactly, so one form serves scaled and plain copies.  Sixteen bytes at a time where both sides
-// are aligned for it; else lane by lane, neighbours by neighbouring lanes, which any alignment coalesces.
+// coef = 1 multiplies exactly, so one form serves scaled and plain copies.  A piece is what makes the wider side 16 bytes, so
+// that stores fill whole sectors; where the sides are not aligned for it, lane by lane, neighbours by neighbouring lanes,
+// which any alignment coalesces.  In place each element is read and written by the same thread.
 template <typename S, typename D>
-__device__ __forceinline__ void tile_scale(const S* s, D* d, u32 cnt, float coef) {
-  if (((reinterpret_cast<uintptr_t>(s) | reinterpret_cast<uintptr_t>(d)) & 15) == 0) {
-    if (cnt == GT_TILE) {
-      Eight<S> raw[GT_TILE / (GT_THREADS * GT_VEC)];
+struct Moved {
+  static constexpr int V = 16 / (int)(sizeof(S) > sizeof(D) ? sizeof(S) : sizeof(D)), N = GT_TILE / (GT_THREADS * V);
+  Raw<S, V> raw[N];
+  bool aligned;
+  __device__ __forceinline__ void load(const S* s, const D* d, u32 cnt) {
+    aligned = (reinterpret_cast<uintptr_t>(s) & (V * sizeof(S) - 1)) == 0 && (reinterpret_cast<uintptr_t>(d) & (V * sizeof(D) - 1)) == 0;
+    if (!aligned) return;
+    const u32 whole = cnt / V;
 #pragma unroll
-      for (int i = 0; i < GT_TILE / (GT_THREADS * GT_VEC); ++i) raw[i].load(s + (i * GT_THREADS + threadIdx.x) * GT_VEC);
-#pragma unroll
-      for (int i = 0; i < GT_TILE / (GT_THREADS * GT_VEC); ++i) {
-        float v[8]; raw[i].widen(v);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = __fmul_rn(v[q], coef);
-        Eight<D> o; o.round(v);
-        o.store(d + (i * GT_THREADS + threadIdx.x) * GT_VEC);
-      }
-    } else {
-      const u32 whole = cnt / GT_VEC;
-      for (u32 i = threadIdx.x; i < whole; i += GT_THREADS) {
-        Eight<S> raw; raw.load(s + i * GT_VEC);
-        float v[8]; raw.widen(v);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = __fmul_rn(v[q], coef);
-        Eight<D> o; o.round(v);
-        o.store(d + i * GT_VEC);
-      }
-      const u32 e = whole * GT_VEC + threadIdx.x;
-      if (e < cnt) d[e] = from_f<D>(__fmul_rn(to_f(s[e]), coef));
-    }
-  } else {
-    u32 e = threadIdx.x;
-    for (; e + 7 * GT_THREADS < cnt; e += 8 * GT_THREADS) {
-      S v[8];
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] = s[e + q * GT_THREADS];
-#pragma unroll
-      for (int q = 0; q < 8; ++q) d[e + q * GT_THREADS] = from_f<D>(__fmul_rn(to_f(v[q]), coef));
-    }
-    for (; e < cnt; e += GT_THREADS) d[e] = from_f<D>(__fmul_rn(to_f(s[e]), coef));
+    for (int i = 0; i < N; ++i)
+      if (cnt == GT_TILE || i * GT_THREADS + threadIdx.x < whole) raw[i].load_once(s + (i * GT_THREADS + threadIdx.x) * V);
   }
-}
+  __device__ __forceinline__ void store(const S* s, D* d, u32 cnt, float coef) {
+    if (aligned) {
+      const u32 whole = cnt / V;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (cnt == GT_TILE || i * GT_THREADS + threadIdx.x < whole) {
+          float v[V];
+          raw[i].widen(v);
+#pragma unroll
+          for (int q = 0; q < V; ++q) v[q] = __fmul_rn(v[q], coef);
+          Raw<D, V> o;
+          o.round(v);
+          o.store_stream(d + (i * GT_THREADS + threadIdx.x) * V);
+        }
+      }
+      const u32 e = whole * V + threadIdx.x;
+      if (e < cnt) d[e] = from_f<D>(__fmul_rn(to_f(s[e]), coef));
+    } else {
+      u32 e = threadIdx.x;
+      for (; e + 7 * GT_THREADS < cnt; e += 8 * GT_THREADS) {
+        S v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = s[e + q * GT_THREADS];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) d[e + q * GT_THREADS] = from_f<D>(__fmul_rn(to_f(v[q]), coef));
+      }
+      for (; e < cnt; e += GT_THREADS) d[e] = from_f<D>(__fmul_rn(to_f(s[e]), coef));
+    }
+  }
+};
 
 enum { MODE_CLIP, MODE_PACK, MODE_UNPACK };
 
@@ -246,11 +243,33 @@ template <> __device__ __forceinline__ float coef_for<__nv_bfloat16>(float c) { 
 template <> __device__ __forceinline__ float coef_for<__half>(float c) { return c >= 6.103515625e-5f ? to_f(from_f<__half>(c)) : c; }
 
 template <int MODE, typename T>
-__device__ __forceinline__ void tile_move(void* base, const Tile& ti, float* vec, float coef) {
-  T* g = (T*)base + ti.start;
-  if (MODE == MODE_CLIP) tile_scale<T, T>(g, g, ti.count, coef_for<T>(coef));
-  else if (MODE == MODE_PACK) tile_scale<T, float>(g, vec + ti.at, ti.count, coef);
-  else tile_scale<float, T>(vec + ti.at, g, ti.count, 1.0f);
+__device__ __forceinline__ void tile_move(void* base, const Tile& ti, float* vec, const float* coefs, int row, bool& waited, float& coef) {
+  T* const g = (T*)base + ti.start;
+  auto wait = [&]() {                     // the norm's kernel, after this one's first loads are on their way
+    if (waited) return;
+    cudaGridDependencySynchronize();
+    coef = coefs ? *(volatile const float*)(coefs + row) : 1.0f;
+    waited = true;
+  };
+  if (MODE == MODE_PACK) {
+    Moved<T, float> m;
+    float* const d = vec + ti.at;
+    m.load(g, d, ti.count);
+    wait();
+    m.store(g, d, ti.count, coef);
+  } else if (MODE == MODE_CLIP) {
+    wait();
+    const float c = coef_for<T>(coef);
+    if (c == 1.0f) return;                // nothing would change
+    Moved<T, T> m;
+    m.load(g, g, ti.count);
+    m.store(g, g, ti.count, c);
+  } else {
+    Moved<float, T> m;
+    const float* const s = vec + ti.at;
+    m.load(s, g, ti.count);
+    m.store(s, g, ti.count, 1.0f);
+  }
 }
 
 // The tiles run backwards: the norm's pass went forwards, and what it read last is what L2 still holds.
@@ -259,16 +278,18 @@ __global__ void __launch_bounds__(GT_THREADS) k_grads_move(const __grid_constant
                                                            int ntiles, int T, const float* coefs, float* vec, long long stride) {
   const int row = (int)(gridDim.y - 1 - blockIdx.y), B = gridDim.x, b = B - 1 - (int)blockIdx.x;
   const int t0 = (int)((long long)ntiles * b / B), t1 = (int)((long long)ntiles * (b + 1) / B);
-  cudaGridDependencySynchronize();
-  const float coef = coefs ? *(volatile const float*)(coefs + row) : 1.0f;
-  if (MODE == MODE_CLIP && coef == 1.0f) return;      // nothing would change
-  float* v = MODE == MODE_CLIP ? nullptr : vec + row * stride;
+  bool waited = false;
+  float coef = 1.0f;
+  float* const v = MODE == MODE_CLIP ? nullptr : vec + row * stride;
+  Tile next = t0 < t1 ? tiles[t1 - 1] : Tile{};
   for (int t = t1 - 1; t >= t0; --t) {
-    const Tile ti = tiles[t];
+    const Tile ti = next;
+    if (t > t0) next = tiles[t - 1];
     void* base = ptrs.get(row * T + (int)ti.tensor);
-    if (ti.type == SAE_TYPE_FLOAT) tile_move<MODE, float>(base, ti, v, coef);
-    else if (ti.type == SAE_TYPE_BFLOAT) tile_move<MODE, __nv_bfloat16>(base, ti, v, coef);
-    else tile_move<MODE, __half>(base, ti, v, coef);
+    if (ti.type == SAE_TYPE_FLOAT) tile_move<MODE, float>(base, ti, v, coefs, row, waited, coef);
+    else if (ti.type == SAE_TYPE_BFLOAT) tile_move<MODE, __nv_bfloat16>(base, ti, v, coefs, row, waited, coef);
+    else tile_move<MODE, __half>(base, ti, v, coefs, row, waited, coef);
+    if (MODE == MODE_CLIP && coef == 1.0f) return;
   }
 }
 

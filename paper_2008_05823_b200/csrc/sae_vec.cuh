@@ -66,6 +66,8 @@ struct Raw {
   typedef typename Bits<V * (int)sizeof(T)>::type B;
   B b;
   __device__ __forceinline__ void load(const T* p) { b = __ldg(reinterpret_cast<const B*>(p)); }
+  __device__ __forceinline__ void load_once(const T* p) { b = __ldcs(reinterpret_cast<const B*>(p)); }
+  __device__ __forceinline__ void clear() { b = B{}; }
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<B*>(p) = b; }
   __device__ __forceinline__ void store_stream(T* p) const { __stcs(reinterpret_cast<B*>(p), b); }
   __device__ __forceinline__ void widen(float (&v)[V]) const {
