@@ -52,7 +52,6 @@ struct Walk {
   static constexpr int D = ring_depth(sizeof(B), NT);
   const T* next[NT];
   long long step[NT];
-  unsigned long long policy[NT];
   B* slots;
   int turns, ahead;
 
@@ -62,18 +61,17 @@ struct Walk {
     slots = (B*)smem + threadIdx.x;
   }
   __device__ __forceinline__ int first(const Place& q) const { return BACK ? q.p + (turns - 1) * q.rows : q.p; }
-  // Tensor t: element (n, c) of it and the stride of a pixel; `once`: nobody reads it again, so it goes from L2 first.
-  __device__ __forceinline__ void tensor(int t, const Place& q, const T* from, long long pixel, bool once) {
+  // Tensor t: element (n, c) of it and the stride of a pixel.
+  __device__ __forceinline__ void tensor(int t, const Place& q, const T* from, long long pixel) {
     next[t] = from + first(q) * pixel;
     step[t] = (BACK ? -q.rows : q.rows) * pixel;
-    policy[t] = l2_policy(once);
   }
   __device__ __forceinline__ void fetch(int slot) {
     if constexpr (sizeof(B) >= 4) {
       if (ahead < turns) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          copy_async<sizeof(B)>(slots + (slot * NT + t) * GN_THREADS, next[t], policy[t]);
+          copy_async<sizeof(B)>(slots + (slot * NT + t) * GN_THREADS, next[t]);
           next[t] += step[t];
         }
       }
@@ -240,7 +238,7 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_statistics(const Args a, c
   for (int i = 0; i < SL; ++i) { mean[i] = 0.0f; m2[i] = 0.0f; }
   Walk<T, V, 1, false> walk;
   walk.set(q, smem);
-  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p, false);
+  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p);
   walk.start();
   auto join = [&](int run) {
     float k1[SL], k2[SL];
@@ -311,8 +309,8 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_apply(const Args a, const 
   const Place q = place<V>(a, st);
   Walk<T, V, NT, true> walk;
   walk.set(q, smem);
-  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p, true);
-  if constexpr (RES) walk.tensor(1, q, (const T*)a.res + q.n * a.r_n + q.c, a.r_p, true);
+  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p);
+  if constexpr (RES) walk.tensor(1, q, (const T*)a.res + q.n * a.r_n + q.c, a.r_p);
   walk.start();                           // no kernel of the call has written these
   const float inv_cg = 1.0f / (float)a.Cg;
   float w[V], b[V], less[V], scale[V];
@@ -379,9 +377,9 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(cons
   const float inv_cg = 1.0f / (float)a.Cg;
   Walk<T, V, NT, false> walk;
   walk.set(q, smem);
-  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p, false);
-  walk.tensor(1, q, (const T*)a.dy + q.n * a.d_n + q.c, a.d_p, st.held);
-  if constexpr (RES) walk.tensor(2, q, (const T*)a.res + q.n * a.r_n + q.c, a.r_p, st.held);
+  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p);
+  walk.tensor(1, q, (const T*)a.dy + q.n * a.d_n + q.c, a.d_p);
+  if constexpr (RES) walk.tensor(2, q, (const T*)a.res + q.n * a.r_n + q.c, a.r_p);
   walk.start();
   const int pitch = st.cvt * V, span = q.rows * pitch, slot = (threadIdx.x - q.row * st.cvt) * V;
   float s[V], sx[V];
@@ -469,9 +467,9 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_apply(con
   const float inv_cg = 1.0f / (float)a.Cg;
   Walk<T, V, NT, true> walk;
   walk.set(q, smem);
-  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p, true);
-  walk.tensor(1, q, (const T*)a.dy + q.n * a.d_n + q.c, a.d_p, true);
-  if constexpr (RES) walk.tensor(2, q, (const T*)a.res + q.n * a.r_n + q.c, a.r_p, true);
+  walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p);
+  walk.tensor(1, q, (const T*)a.dy + q.n * a.d_n + q.c, a.d_p);
+  if constexpr (RES) walk.tensor(2, q, (const T*)a.res + q.n * a.r_n + q.c, a.r_p);
   if (!st.held) walk.start();             // held: the first pass writes what is read here
   float w[V], b[V], less[V], scale[V], p1[V], p2[V], gw[V];
   if (q.on) {

@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 using namespace sae;
@@ -20,17 +21,21 @@ typedef unsigned long long u64;
 typedef unsigned int u32;
 
 constexpr int GT_THREADS = 256;
-constexpr int GT_TILE = 8192;            // elements of one tensor that a block handles at a time
-constexpr int GT_BLOCKS_PER_SM = 8;      // 2048 resident threads
+constexpr int GT_TILE = 16384;           // bytes of one tensor that a block handles at a time
+constexpr int GT_STAGES = 3;             // tiles on their way or in use: 48 KB of shared memory
+constexpr int GT_BLOCKS_PER_SM = 4;
+constexpr int GT_SMEM = GT_STAGES * GT_TILE;
 constexpr int PTRS_SMALL = 64;           // tensor pointers that travel as kernel arguments
 constexpr int PTRS_LARGE = 448;
 constexpr int PTRS_UPLOAD = 3840;        // pointers one upload launch carries (30 KB of the 32 KB of arguments)
 constexpr double COEF_EPS = 1e-6;
 
-// One tile: `count` elements of tensor `tensor` from element `start`, at element `at` of a packed row.
-struct __align__(16) Tile {
-  u32 tensor, start, count, type;
-  long long at, pad;
+// One tile: elements of tensor `tensor` from element `start`, at element `at` of a packed row.
+struct Tile {
+  long long at;
+  u32 tensor, start, count_type, pad;     // count * 4 + type
+  __host__ __device__ u32 count() const { return count_type >> 2; }
+  __host__ __device__ u32 type() const { return count_type & 3u; }
 };
 
 // The tensors' addresses, row-major [rows][T].  N > 0: in the kernel's arguments; N = 0: in device memory.
@@ -111,32 +116,87 @@ __device__ __forceinline__ void block_join(Running<KIND>& r, u64* sh) {
   }
 }
 
-// A thread's pieces are 16 bytes, neighbouring threads' pieces neighbours in memory.
+// A block's tiles come through a ring of GT_STAGES shared-memory images, copied asynchronously in pieces of 16 bytes whatever
+// the type: two tiles are on their way while one is used, so the loads in flight (128 KB an SM) do not depend on registers.
+// A thread uses the pieces that it copied itself, so no barrier is needed.  A tensor that is not aligned to 16 bytes is not
+// copied but read in place.
+__device__ __forceinline__ int elem_size(u32 type) { return type == SAE_TYPE_FLOAT ? 4 : 2; }
+template <int N>
+struct Ring {
+  static constexpr int PIECES = GT_TILE / (16 * GT_THREADS);
+  unsigned char* smem;
+  const Tile* tiles;
+  const Ptrs<N>* ptrs;
+  int first;                              // the row's first pointer
+
+  __device__ __forceinline__ unsigned char* stage(int s) const { return smem + s * GT_TILE; }
+  __device__ __forceinline__ unsigned char* address(const Tile& t) const {
+    return (unsigned char*)ptrs->get(first + (int)t.tensor) + (size_t)t.start * elem_size(t.type());
+  }
+  __device__ __forceinline__ static bool copied(const unsigned char* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+  __device__ __forceinline__ void fetch(const Tile& t, int s) const {
+    const unsigned char* const p = address(t);
+    if (!copied(p)) return;
+    const u32 n = t.count() * elem_size(t.type()) / 16;
+    unsigned char* const to = stage(s);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const u32 e = i * GT_THREADS + threadIdx.x;
+      if (e < n) copy_async<16>(to + e * 16, p + (size_t)e * 16);
+    }
+  }
+  // use(tile, its address, its image) for count tiles from t0 on, dir = 1 or -1.
+  template <typename F>
+  __device__ __forceinline__ void run(int t0, int count, int dir, F use) const {
+    // the tiles' entries wait in registers: w[0] in use, w[1] and w[2] on their way, w[3] next
+    Tile w[GT_STAGES + 1] = {};
+#pragma unroll
+    for (int k = 0; k <= GT_STAGES; ++k)
+      if (k < count) w[k] = tiles[t0 + dir * k];
+#pragma unroll
+    for (int k = 0; k < GT_STAGES - 1; ++k) {
+      if (k < count) fetch(w[k], k);
+      copies_commit();
+    }
+    int from = 0;
+    for (int k = 0; k < count; ++k) {
+      const int to = from == 0 ? GT_STAGES - 1 : from - 1;                      // (from + GT_STAGES - 1) % GT_STAGES
+      if (k + GT_STAGES - 1 < count) fetch(w[GT_STAGES - 1], to);
+      copies_commit();
+      const Tile t = w[0];
+#pragma unroll
+      for (int i = 0; i < GT_STAGES; ++i) w[i] = w[i + 1];
+      if (k + GT_STAGES + 1 < count) w[GT_STAGES] = tiles[t0 + dir * (k + GT_STAGES + 1)];
+      copies_wait<GT_STAGES - 1>();
+      use(t, address(t), stage(from));
+      __syncwarp();                       // a warp's lanes may have used one another's pieces
+      from = from + 1 == GT_STAGES ? 0 : from + 1;
+    }
+    copies_wait<0>();
+  }
+};
+
 template <int KIND, typename T>
-__device__ __forceinline__ void tile_norm(Running<KIND>& r, const T* p, u32 cnt) {
-  constexpr int V = 16 / (int)sizeof(T), N = GT_TILE / (GT_THREADS * V);
+__device__ __forceinline__ void tile_norm(Running<KIND>& r, const T* p, const unsigned char* image, u32 cnt) {
+  constexpr int V = 16 / (int)sizeof(T), N = GT_TILE / (GT_THREADS * 16);
   const u32 tid = threadIdx.x;
   if ((reinterpret_cast<uintptr_t>(p) & 15) == 0) {
     const u32 whole = cnt / V;
-    Raw<T, V> raw[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (cnt == GT_TILE || i * GT_THREADS + tid < whole) raw[i].load(p + (i * GT_THREADS + tid) * V);
-      else raw[i].clear();
-    const u32 e = whole * V + tid;
-    const float last = cnt != GT_TILE && e < cnt ? to_f(p[e]) : 0.0f;
 #pragma unroll
     for (int i = 0; i < N; i += 8 / V) {
       float v[8];
-      if constexpr (V == 8) {
-        raw[i].widen(v);
-      } else {
-        raw[i].widen(*reinterpret_cast<float (*)[4]>(&v[0]));
-        raw[i + 1].widen(*reinterpret_cast<float (*)[4]>(&v[4]));
+#pragma unroll
+      for (int h = 0; h < 8 / V; ++h) {
+        const u32 e = (i + h) * GT_THREADS + tid;
+        Raw<T, V> raw;
+        raw.clear();
+        if (e < whole) raw.b = *reinterpret_cast<const uint4*>(image + e * 16);
+        raw.widen(*reinterpret_cast<float (*)[V]>(&v[h * V]));
       }
       r.eight(v);
     }
-    r.one(last);
+    const u32 e = whole * V + tid;
+    if (e < cnt) r.one(to_f(p[e]));
   } else {
     for (u32 e = tid; e < cnt; e += GT_THREADS) r.one(to_f(p[e]));
   }
@@ -145,24 +205,23 @@ __device__ __forceinline__ void tile_norm(Running<KIND>& r, const T* p, u32 cnt)
 // blockIdx.y: the row (worker).  The row's tiles are dealt out in runs of neighbours, one run a block.  The block
 // that comes last (a ticket a row, back at zero after it) joins the runs' values in their order.
 template <int KIND, int N>
-__global__ void __launch_bounds__(GT_THREADS) k_grads_norm(const __grid_constant__ Ptrs<N> ptrs, const Tile* __restrict__ tiles,
+__global__ void __launch_bounds__(GT_THREADS, GT_BLOCKS_PER_SM) k_grads_norm(const __grid_constant__ Ptrs<N> ptrs, const Tile* __restrict__ tiles,
                                                            int ntiles, int T, u64* partials, u32* tickets, float max_norm,
                                                            float* coefs, float* norms) {
-  __shared__ u64 sh[GT_THREADS / 32];
-  __shared__ int sh_last;
+  extern __shared__ __align__(16) unsigned char smem[];
+  u64* const sh = (u64*)smem;             // after the ring: a value for each warp, then whether this block is the last
+  int& sh_last = *(int*)(sh + GT_THREADS / 32);
   const int row = blockIdx.y, B = gridDim.x;
   const int t0 = (int)((long long)ntiles * blockIdx.x / B), t1 = (int)((long long)ntiles * (blockIdx.x + 1) / B);
   Running<KIND> r; r.zero();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  Tile next = t0 < t1 ? tiles[t0] : Tile{};
-  for (int t = t0; t < t1; ++t) {
-    const Tile ti = next;
-    if (t + 1 < t1) next = tiles[t + 1];
-    void* base = ptrs.get(row * T + (int)ti.tensor);
-    if (ti.type == SAE_TYPE_FLOAT) tile_norm<KIND, float>(r, (const float*)base + ti.start, ti.count);
-    else if (ti.type == SAE_TYPE_BFLOAT) tile_norm<KIND, __nv_bfloat16>(r, (const __nv_bfloat16*)base + ti.start, ti.count);
-    else tile_norm<KIND, __half>(r, (const __half*)base + ti.start, ti.count);
-  }
+  const Ring<N> ring = {smem, tiles, &ptrs, row * T};
+  ring.run(t0, t1 - t0, 1, [&](const Tile& t, const unsigned char* p, const unsigned char* image) {
+    if (t.type() == SAE_TYPE_FLOAT) tile_norm<KIND, float>(r, (const float*)p, image, t.count());
+    else if (t.type() == SAE_TYPE_BFLOAT) tile_norm<KIND, __nv_bfloat16>(r, (const __nv_bfloat16*)p, image, t.count());
+    else tile_norm<KIND, __half>(r, (const __half*)p, image, t.count());
+  });
+  __syncthreads();
   block_join<KIND>(r, sh);
   if (threadIdx.x == 0) {
     partials[(size_t)row * B + blockIdx.x] = r.bits();
@@ -186,54 +245,7 @@ __global__ void __launch_bounds__(GT_THREADS) k_grads_norm(const __grid_constant
 }
 
 // ---- scaled copies --------------------------------------------------------------------------------------------
-// coef = 1 multiplies exactly, so one form serves scaled and plain copies.  A piece is what makes the wider side 16 bytes, so
-// that stores fill whole sectors; where the sides are not aligned for it, lane by lane, neighbours by neighbouring lanes,
-// which any alignment coalesces.  In place each element is read and written by the same thread.
-template <typename S, typename D>
-struct Moved {
-  static constexpr int V = 16 / (int)(sizeof(S) > sizeof(D) ? sizeof(S) : sizeof(D)), N = GT_TILE / (GT_THREADS * V);
-  Raw<S, V> raw[N];
-  bool aligned;
-  __device__ __forceinline__ void load(const S* s, const D* d, u32 cnt) {
-    aligned = (reinterpret_cast<uintptr_t>(s) & (V * sizeof(S) - 1)) == 0 && (reinterpret_cast<uintptr_t>(d) & (V * sizeof(D) - 1)) == 0;
-    if (!aligned) return;
-    const u32 whole = cnt / V;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (cnt == GT_TILE || i * GT_THREADS + threadIdx.x < whole) raw[i].load_once(s + (i * GT_THREADS + threadIdx.x) * V);
-  }
-  __device__ __forceinline__ void store(const S* s, D* d, u32 cnt, float coef) {
-    if (aligned) {
-      const u32 whole = cnt / V;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        if (cnt == GT_TILE || i * GT_THREADS + threadIdx.x < whole) {
-          float v[V];
-          raw[i].widen(v);
-#pragma unroll
-          for (int q = 0; q < V; ++q) v[q] = __fmul_rn(v[q], coef);
-          Raw<D, V> o;
-          o.round(v);
-          o.store_stream(d + (i * GT_THREADS + threadIdx.x) * V);
-        }
-      }
-      const u32 e = whole * V + threadIdx.x;
-      if (e < cnt) d[e] = from_f<D>(__fmul_rn(to_f(s[e]), coef));
-    } else {
-      u32 e = threadIdx.x;
-      for (; e + 7 * GT_THREADS < cnt; e += 8 * GT_THREADS) {
-        S v[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = s[e + q * GT_THREADS];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) d[e + q * GT_THREADS] = from_f<D>(__fmul_rn(to_f(v[q]), coef));
-      }
-      for (; e < cnt; e += GT_THREADS) d[e] = from_f<D>(__fmul_rn(to_f(s[e]), coef));
-    }
-  }
-};
-
-enum { MODE_CLIP, MODE_PACK, MODE_UNPACK };
+enum { MODE_CLIP, MODE_PACK };
 
 // In place, a 16-bit tensor is scaled by the coefficient rounded to its own type, which is what torch's in-place product with
 // a scalar tensor does: replacing a torch clipping changes no bit.  Not below the type's normal numbers (a half's end at
@@ -242,54 +254,126 @@ template <typename T> __device__ __forceinline__ float coef_for(float c) { retur
 template <> __device__ __forceinline__ float coef_for<__nv_bfloat16>(float c) { return c >= 1.17549435e-38f ? to_f(from_f<__nv_bfloat16>(c)) : c; }
 template <> __device__ __forceinline__ float coef_for<__half>(float c) { return c >= 6.103515625e-5f ? to_f(from_f<__half>(c)) : c; }
 
-template <int MODE, typename T>
-__device__ __forceinline__ void tile_move(void* base, const Tile& ti, float* vec, const float* coefs, int row, bool& waited, float& coef) {
-  T* const g = (T*)base + ti.start;
-  auto wait = [&]() {                     // the norm's kernel, after this one's first loads are on their way
-    if (waited) return;
-    cudaGridDependencySynchronize();
-    coef = coefs ? *(volatile const float*)(coefs + row) : 1.0f;
-    waited = true;
-  };
-  if (MODE == MODE_PACK) {
-    Moved<T, float> m;
-    float* const d = vec + ti.at;
-    m.load(g, d, ti.count);
-    wait();
-    m.store(g, d, ti.count, coef);
-  } else if (MODE == MODE_CLIP) {
-    wait();
-    const float c = coef_for<T>(coef);
-    if (c == 1.0f) return;                // nothing would change
-    Moved<T, T> m;
-    m.load(g, g, ti.count);
-    m.store(g, g, ti.count, c);
-  } else {
-    Moved<float, T> m;
-    const float* const s = vec + ti.at;
-    m.load(s, g, ti.count);
-    m.store(s, g, ti.count, 1.0f);
+// A warp's 32 neighbouring pieces (`left` of them exist), scaled, to D at 16-byte aligned addresses.  Between types of one
+// size a lane stores its own piece.  16 bits to float doubles the bytes: lane after lane takes half a piece, so that a store
+// of the warp is one run of 512 bytes (a lane storing both halves of its own piece leaves every sector to two stores:
+// 35 against 25 us for a row of 25.6 M elements).
+template <typename S, typename D>
+__device__ __forceinline__ void store_pieces(const unsigned char* image, D* d, u32 left, float coef) {
+  constexpr int V = 16 / (int)sizeof(D), P = 16 / (int)sizeof(S) / V;           // elements a store takes, stores a piece takes
+  const u32 lane = threadIdx.x & 31;
+#pragma unroll
+  for (int h = 0; h < P; ++h) {
+    const u32 i = h * 32 + lane;
+    if (i < left * P) {
+      Raw<S, V> raw;
+      raw.b = *reinterpret_cast<const typename Raw<S, V>::B*>(image + i * (V * sizeof(S)));
+      float v[V];
+      raw.widen(v);
+#pragma unroll
+      for (int q = 0; q < V; ++q) v[q] = __fmul_rn(v[q], coef);
+      Raw<D, V> o;
+      o.round(v);
+      o.store_stream(d + i * V);
+    }
   }
+}
+
+// coef * a tile of S (clip: D = S, in place; pack: D = float).  coef = 1 multiplies exactly.
+template <typename S, typename D>
+__device__ __forceinline__ void tile_scale(const S* s, const unsigned char* image, D* d, u32 cnt, float coef) {
+  constexpr int V = 16 / (int)sizeof(S), N = GT_TILE / (GT_THREADS * 16);
+  const u32 tid = threadIdx.x;
+  if ((reinterpret_cast<uintptr_t>(s) & 15) != 0) {                             // not copied
+    for (u32 e = tid; e < cnt; e += GT_THREADS) d[e] = from_f<D>(__fmul_rn(to_f(s[e]), coef));
+    return;
+  }
+  const u32 whole = cnt / V;
+  if ((reinterpret_cast<uintptr_t>(d) & 15) == 0) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const u32 e = i * GT_THREADS + (tid & ~31u);
+      if (e < whole) store_pieces<S, D>(image + e * 16, d + e * V, min(32u, whole - e), coef);
+    }
+  } else {                                // neighbours by neighbouring threads, out of everybody's pieces
+    __syncthreads();
+    const S* const held = reinterpret_cast<const S*>(image);
+#pragma unroll 4
+    for (u32 e = tid; e < whole * V; e += GT_THREADS) d[e] = from_f<D>(__fmul_rn(to_f(held[e]), coef));
+    __syncthreads();                      // the image is not overwritten before
+  }
+  const u32 e = whole * V + tid;
+  if (e < cnt) d[e] = from_f<D>(__fmul_rn(to_f(s[e]), coef));
 }
 
 // The tiles run backwards: the norm's pass went forwards, and what it read last is what L2 still holds.
 template <int MODE, int N>
-__global__ void __launch_bounds__(GT_THREADS) k_grads_move(const __grid_constant__ Ptrs<N> ptrs, const Tile* __restrict__ tiles,
-                                                           int ntiles, int T, const float* coefs, float* vec, long long stride) {
+__global__ void __launch_bounds__(GT_THREADS, GT_BLOCKS_PER_SM) k_grads_scale(const __grid_constant__ Ptrs<N> ptrs, const Tile* __restrict__ tiles,
+                                                                              int ntiles, int T, const float* coefs, float* vec, long long stride) {
+  extern __shared__ __align__(16) unsigned char smem[];
   const int row = (int)(gridDim.y - 1 - blockIdx.y), B = gridDim.x, b = B - 1 - (int)blockIdx.x;
   const int t0 = (int)((long long)ntiles * b / B), t1 = (int)((long long)ntiles * (b + 1) / B);
-  bool waited = false;
   float coef = 1.0f;
+  bool waited = false;
+  if (MODE == MODE_CLIP) {
+    cudaGridDependencySynchronize();
+    coef = *(volatile const float*)(coefs + row);
+    if (coef == 1.0f) return;             // nothing would change
+  }
   float* const v = MODE == MODE_CLIP ? nullptr : vec + row * stride;
-  Tile next = t0 < t1 ? tiles[t1 - 1] : Tile{};
-  for (int t = t1 - 1; t >= t0; --t) {
-    const Tile ti = next;
-    if (t > t0) next = tiles[t - 1];
+  const Ring<N> ring = {smem, tiles, &ptrs, row * T};
+  ring.run(t1 - 1, t1 - t0, -1, [&](const Tile& t, unsigned char* p, const unsigned char* image) {
+    if (MODE == MODE_PACK && !waited) {   // for the norm's kernel, with this one's first loads on their way
+      cudaGridDependencySynchronize();
+      if (coefs) coef = *(volatile const float*)(coefs + row);
+      waited = true;
+    }
+    auto as = [&](auto* s) {
+      typedef typename std::remove_pointer<decltype(s)>::type S;
+      if (MODE == MODE_CLIP) tile_scale<S, S>(s, image, s, t.count(), coef_for<S>(coef));
+      else tile_scale<S, float>(s, image, v + t.at, t.count(), coef);
+    };
+    if (t.type() == SAE_TYPE_FLOAT) as((float*)p);
+    else if (t.type() == SAE_TYPE_BFLOAT) as((__nv_bfloat16*)p);
+    else as((__half*)p);
+  });
+}
+
+template <typename T>
+__device__ __forceinline__ void tile_unpack(const float* s, T* d, u32 cnt) {
+  if (((reinterpret_cast<uintptr_t>(s) & 15) | (reinterpret_cast<uintptr_t>(d) & (4 * sizeof(T) - 1))) == 0) {
+    const u32 whole = cnt / 4;
+#pragma unroll 4
+    for (u32 i = threadIdx.x; i < whole; i += GT_THREADS) {
+      Raw<float, 4> raw;
+      raw.load(s + i * 4);
+      float v[4];
+      raw.widen(v);
+      Raw<T, 4> o;
+      o.round(v);
+      o.store(d + i * 4);
+    }
+    const u32 e = whole * 4 + threadIdx.x;
+    if (e < cnt) d[e] = from_f<T>(s[e]);
+  } else {
+#pragma unroll 8
+    for (u32 e = threadIdx.x; e < cnt; e += GT_THREADS) d[e] = from_f<T>(s[e]);
+  }
+}
+
+template <int N>
+__global__ void __launch_bounds__(GT_THREADS) k_grads_unpack(const __grid_constant__ Ptrs<N> ptrs, const Tile* __restrict__ tiles, int ntiles,
+                                                             int T, const float* vec, long long stride) {
+  const int row = blockIdx.y;
+  const int t0 = (int)((long long)ntiles * blockIdx.x / gridDim.x), t1 = (int)((long long)ntiles * (blockIdx.x + 1) / gridDim.x);
+  for (int t = t0; t < t1; ++t) {
+    const Tile ti = tiles[t];
     void* base = ptrs.get(row * T + (int)ti.tensor);
-    if (ti.type == SAE_TYPE_FLOAT) tile_move<MODE, float>(base, ti, v, coefs, row, waited, coef);
-    else if (ti.type == SAE_TYPE_BFLOAT) tile_move<MODE, __nv_bfloat16>(base, ti, v, coefs, row, waited, coef);
-    else tile_move<MODE, __half>(base, ti, v, coefs, row, waited, coef);
-    if (MODE == MODE_CLIP && coef == 1.0f) return;
+    const float* const s = vec + row * stride + ti.at;
+    if (ti.type() == SAE_TYPE_FLOAT) tile_unpack(s, (float*)base + ti.start, ti.count());
+    else if (ti.type() == SAE_TYPE_BFLOAT) tile_unpack(s, (__nv_bfloat16*)base + ti.start, ti.count());
+    else tile_unpack(s, (__half*)base + ti.start, ti.count());
   }
 }
 
@@ -337,16 +421,16 @@ void release(sae_grads* h) {
 
 int elem_bytes(int type) { return type == SAE_TYPE_FLOAT ? 4 : 2; }
 
-// Blocks of one row when `rows` rows share a launch: every SM full once, one tile a block at least.
-int row_blocks(const sae_grads* h, int rows) {
-  const int want = (h->num_sms * GT_BLOCKS_PER_SM + rows - 1) / rows;
+// Blocks of one row: every SM full once, one tile a block at least.
+int row_blocks(const sae_grads* h) {
+  const int want = (h->num_sms * GT_BLOCKS_PER_SM + h->K - 1) / h->K;
   return std::max(1, std::min(std::min(h->ntiles, h->max_blocks), want));
 }
 
 template <int N>
-cudaError_t launch_norm(sae_grads* h, const Ptrs<N>& p, int rows, int kind, float max_norm, float* norms) {
-  const dim3 grid((unsigned)row_blocks(h, rows), (unsigned)rows);
-#define NORM(KIND) k_grads_norm<KIND, N><<<grid, GT_THREADS, 0, h->stream>>>(p, h->tiles, h->ntiles, h->T, h->partials, h->tickets, \
+cudaError_t launch_norm(sae_grads* h, const Ptrs<N>& p, int kind, float max_norm, float* norms) {
+  const dim3 grid((unsigned)row_blocks(h), (unsigned)h->K);
+#define NORM(KIND) k_grads_norm<KIND, N><<<grid, GT_THREADS, GT_SMEM, h->stream>>>(p, h->tiles, h->ntiles, h->T, h->partials, h->tickets, \
                                                                               max_norm, h->coefs, norms)
   if (kind == SAE_NORM_TWO) NORM(SAE_NORM_TWO);
   else if (kind == SAE_NORM_ONE) NORM(SAE_NORM_ONE);
@@ -356,31 +440,38 @@ cudaError_t launch_norm(sae_grads* h, const Ptrs<N>& p, int rows, int kind, floa
 }
 
 template <int MODE, int N>
-cudaError_t launch_move(sae_grads* h, const Ptrs<N>& p, int rows, bool scaled, float* vec, long long stride) {
+cudaError_t launch_scale(sae_grads* h, const Ptrs<N>& p, bool scaled, float* vec, long long stride) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)row_blocks(h, rows), (unsigned)rows);
+  cfg.gridDim = dim3((unsigned)row_blocks(h), (unsigned)h->K);
   cfg.blockDim = dim3(GT_THREADS);
+  cfg.dynamicSmemBytes = GT_SMEM;
   cfg.stream = h->stream;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = scaled ? 1 : 0;           // only behind this call's own norm kernel
-  return cudaLaunchKernelEx(&cfg, k_grads_move<MODE, N>, p, (const Tile*)h->tiles, h->ntiles, h->T,
+  return cudaLaunchKernelEx(&cfg, k_grads_scale<MODE, N>, p, (const Tile*)h->tiles, h->ntiles, h->T,
                             (const float*)(scaled ? h->coefs : nullptr), vec, stride);
 }
 
 enum { WITH_NORM = 1, WITH_CLIP = 2, WITH_PACK = 4, WITH_UNPACK = 8 };
 
+// All rows at once: one by one, so that L2 keeps a row of up to 48 MB from the first pass to the second, costs more in launches
+// than it saves (four ResNet-50 rows of 51 MB: 166 us against 152; four encoder rows of 219 MB: 635 against 620).
 template <int N>
-cudaError_t launch_all(sae_grads* h, const Ptrs<N>& p, int rows, int what, int kind, float max_norm, float* vec, long long stride, float* norms) {
+cudaError_t launch_all(sae_grads* h, const Ptrs<N>& p, int what, int kind, float max_norm, float* vec, long long stride, float* norms) {
   cudaError_t e = cudaSuccess;
   const bool scaled = (what & WITH_NORM) != 0;
-  if (scaled) e = launch_norm<N>(h, p, rows, kind, max_norm, norms);
+  if (scaled) e = launch_norm<N>(h, p, kind, max_norm, norms);
   if (e != cudaSuccess || h->ntiles == 0) return e;
-  if (what & WITH_CLIP) e = launch_move<MODE_CLIP, N>(h, p, rows, scaled, vec, stride);
-  if (what & WITH_PACK) e = launch_move<MODE_PACK, N>(h, p, rows, scaled, vec, stride);
-  if (what & WITH_UNPACK) e = launch_move<MODE_UNPACK, N>(h, p, rows, scaled, vec, stride);
+  if (what & WITH_CLIP) e = launch_scale<MODE_CLIP, N>(h, p, scaled, vec, stride);
+  if (what & WITH_PACK) e = launch_scale<MODE_PACK, N>(h, p, scaled, vec, stride);
+  if (what & WITH_UNPACK) {
+    const int blocks = std::max(1, std::min(h->ntiles, h->num_sms * 8 / h->K));
+    k_grads_unpack<N><<<dim3((unsigned)blocks, (unsigned)h->K), GT_THREADS, 0, h->stream>>>(p, h->tiles, h->ntiles, h->T, vec, stride);
+    e = cudaGetLastError();
+  }
   return e;
 }
 
@@ -397,11 +488,11 @@ int run(sae_grads* h, const void* const* tensors, int what, int kind, float max_
   if (n <= PTRS_SMALL) {
     Ptrs<PTRS_SMALL> p;
     for (size_t i = 0; i < n; ++i) p.p[i] = const_cast<void*>(tensors[i]);
-    e = launch_all<PTRS_SMALL>(h, p, h->K, what, kind, max_norm, vec, stride, norms);
+    e = launch_all<PTRS_SMALL>(h, p, what, kind, max_norm, vec, stride, norms);
   } else if (n <= PTRS_LARGE) {
     Ptrs<PTRS_LARGE> p;
     for (size_t i = 0; i < n; ++i) p.p[i] = const_cast<void*>(tensors[i]);
-    e = launch_all<PTRS_LARGE>(h, p, h->K, what, kind, max_norm, vec, stride, norms);
+    e = launch_all<PTRS_LARGE>(h, p, what, kind, max_norm, vec, stride, norms);
   } else {
     static thread_local UploadChunk chunk;
     for (size_t i = 0; i < n && e == cudaSuccess; i += PTRS_UPLOAD) {
@@ -412,7 +503,7 @@ int run(sae_grads* h, const void* const* tensors, int what, int kind, float max_
     }
     Ptrs<0> p;
     p.p = h->table;
-    if (e == cudaSuccess) e = launch_all<0>(h, p, h->K, what, kind, max_norm, vec, stride, norms);
+    if (e == cudaSuccess) e = launch_all<0>(h, p, what, kind, max_norm, vec, stride, norms);
   }
   return e == cudaSuccess ? SAE_OK : cuda_status(h, e);
 }
@@ -435,7 +526,7 @@ int sae_grads_init(const sae_grads_config* cfg, sae_grads** out) {
     const int32_t ty = cfg->tensor_types ? cfg->tensor_types[j] : SAE_TYPE_FLOAT;
     if (n < 0 || n > (1ll << 30) || (ty != SAE_TYPE_FLOAT && ty != SAE_TYPE_BFLOAT && ty != SAE_TYPE_HALF)) return SAE_ERR_INVALID_ARG;
     d += n;
-    nt += (n + GT_TILE - 1) / GT_TILE;
+    nt += (n * elem_bytes(ty) + GT_TILE - 1) / GT_TILE;
   }
   if (nt > (1ll << 30) || (long long)K * T > (1ll << 30)) return SAE_ERR_INVALID_ARG;
   sae_grads* h = new (std::nothrow) sae_grads();
@@ -449,10 +540,11 @@ int sae_grads_init(const sae_grads_config* cfg, sae_grads** out) {
     tiles.reserve((size_t)nt);
     long long at = 0;
     for (int j = 0; j < T; ++j) {
-      for (int64_t s = 0; s < h->sizes[j]; s += GT_TILE) {
+      const int64_t step = GT_TILE / elem_bytes(h->types[j]);
+      for (int64_t s = 0; s < h->sizes[j]; s += step) {
         Tile t = {};
-        t.tensor = (u32)j; t.start = (u32)s; t.count = (u32)std::min<int64_t>(GT_TILE, h->sizes[j] - s);
-        t.type = (u32)h->types[j]; t.at = at + s;
+        t.tensor = (u32)j; t.start = (u32)s; t.count_type = (u32)std::min<int64_t>(step, h->sizes[j] - s) * 4u + (u32)h->types[j];
+        t.at = at + s;
         tiles.push_back(t);
       }
       at += h->sizes[j];

@@ -57,15 +57,13 @@ int vector_width(const sae_group_norm_desc* d, const void* const* ptrs, int n) {
   return (m & 15) == 0 ? 16 / es : es == 2 && (m & 3) == 0 ? 2 : 1;
 }
 
-#ifdef SAE_GN_TUNE
-#include <cstdlib>
-int tune(const char* name, int otherwise) { const char* v = getenv(name); return v ? atoi(v) : otherwise; }
-#else
-int tune(const char*, int otherwise) { return otherwise; }
-#endif
-
-constexpr int SMEM_BLOCK = 227 * 1024;
-constexpr int SMEM_MOST = SMEM_BLOCK / 2;           // no kernel here takes more: two blocks an SM at least
+constexpr int SMEM_MOST = 113 * 1024;     // no kernel here takes more: two blocks an SM at least
+constexpr int SMEM_THIRD = 72 * 1024;    // three blocks an SM
+// One pass or two: the unit kernels read everything once but load, reduce and store in turns (2.4 to 3.3 TB/s); the streaming
+// kernels are two launches, and read once from HBM and once from L2 (4.2 to 5 TB/s).  Measured forwards / backwards, one pass
+// against two: 128x32x32x16 float (17, 25 MB of traffic) 8.5 / 14.8 us against 13 / 14; 32x14x14x1024 bf16 with a residual
+// (39, 64 MB) 13.5 / 22.9 against 14.6 / 24.5; 32x56x56x256 bf16 with a residual (154, 257 MB) 47 / 92 against 34 / 61.
+constexpr long long UNIT_TRAFFIC = 32ll << 20;
 
 // One pass over a unit of `seg` bytes a pixel or a little less (whole groups, whole vectors), in clusters of up to `most` blocks
 // of up to `room` bytes; false if the unit does not fit.
@@ -82,7 +80,7 @@ bool unit_plan(const sae_group_norm_desc* d, int vec, int tensors, bool backward
   if (cvt > GN_THREADS) return false;
   cc = std::min<long long>(d->channels, (long long)cvt * vec / step * step);      // fill the lanes
   const long long vectors = d->pixels * cvt;
-  int th = tune("GN_THREADS", 256);
+  int th = GN_THREADS;
   while (th > 64 && vectors < th * 2ll) th /= 2;
   th = std::max(th, cvt);
   if (th < 32) th = 32;
@@ -118,7 +116,7 @@ void stream_plan(const sae_group_norm_desc* d, int vec, bool backward, bool resi
   s.tile_groups = std::min(d->groups, tile_c / cg_ + 2);
   p.portion = (int)std::min<long long>(d->samples, 32768);
   const bool whole = cg_ % vec == 0;
-  const long long wave = (long long)sms * tune("GN_WAVE", backward && !whole ? 2 : 3), blocks = (long long)p.portion * s.tiles;
+  const long long wave = (long long)sms * (backward && !whole ? 2 : 3), blocks = (long long)p.portion * s.tiles;
   // one wave of blocks, but at least eight vectors for a thread
   const long long most = std::max<long long>(1, d->pixels / ((long long)rows * 8));
   s.slices = (int)std::min<long long>(1024, std::min(std::max<long long>(1, wave / blocks), most));
@@ -134,11 +132,13 @@ Plan make_plan(const sae_group_norm_desc* d, int vec, bool backward, bool residu
   // backward: a second slot for dz in float where its type cannot hold it
   const bool second = residual || (backward && elem(d->type) == 2 && d->activation >= SAE_ACT_SILU);
   const int tensors = (backward ? 2 : 1) + (second ? 1 : 0);
-  const int segs[3] = {tune("GN_SEG", 128), 64, 32};
+  const int segs[3] = {128, 64, 32};                               // shorter runs of a pixel where longer ones do not fit
   const long long traffic = d->samples * d->pixels * d->channels * elem(d->type) * (backward ? 3 + 2 * residual : 2 + residual);
-  if (traffic <= ((long long)tune("GN_UNIT_MB", 32) << 20)) {
-    for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, (size_t)tune("GN_ROOM", 72) * 1024, sms, p);
-    for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, (size_t)SMEM_MOST - 1024, sms, p);
+  if (traffic <= UNIT_TRAFFIC) {
+    unit_plan(d, vec, tensors, backward, segs[0], 1, SMEM_MOST, sms, p);
+    if (p.unit && d->samples * p.u.chunks < sms) p.unit = false;   // too few blocks without clusters
+    for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, SMEM_THIRD, sms, p);
+    for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, SMEM_MOST, sms, p);
   }
   if (p.unit) p.bytes = backward ? (size_t)2 * 4 * d->samples * d->channels : 0;
   else stream_plan(d, vec, backward, residual, sms, p);

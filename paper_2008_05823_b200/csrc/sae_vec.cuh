@@ -35,13 +35,6 @@ __device__ __forceinline__ unsigned int round2(float a, float b, const __half*) 
   return *reinterpret_cast<const unsigned int*>(&v);
 }
 
-// How a load is to be kept in L2: first to go, or as usual.
-__device__ __forceinline__ unsigned long long l2_policy(bool evict_first) {
-  unsigned long long first, usual;
-  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(first));
-  asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(usual));
-  return evict_first ? first : usual;
-}
 // Copies to shared memory that a thread waits for itself.  Two bytes have no asynchronous form.
 template <int BYTES>
 __device__ __forceinline__ void copy_async(void* to, const void* from) {
@@ -51,12 +44,6 @@ __device__ __forceinline__ void copy_async(void* to, const void* from) {
   else *(unsigned short*)to = __ldg((const unsigned short*)from);
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int BYTES>
-__device__ __forceinline__ void copy_async(void* to, const void* from, unsigned long long policy) {
-  const unsigned int s = (unsigned int)__cvta_generic_to_shared(to);
-  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(s), "l"(from), "l"(policy) : "memory");
-  else asm volatile("cp.async.ca.shared.global.L2::cache_hint [%0], [%1], %2, %3;" ::"r"(s), "l"(from), "n"(BYTES), "l"(policy) : "memory");
-}
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -66,7 +53,6 @@ struct Raw {
   typedef typename Bits<V * (int)sizeof(T)>::type B;
   B b;
   __device__ __forceinline__ void load(const T* p) { b = __ldg(reinterpret_cast<const B*>(p)); }
-  __device__ __forceinline__ void load_once(const T* p) { b = __ldcs(reinterpret_cast<const B*>(p)); }
   __device__ __forceinline__ void clear() { b = B{}; }
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<B*>(p) = b; }
   __device__ __forceinline__ void store_stream(T* p) const { __stcs(reinterpret_cast<B*>(p), b); }

@@ -399,6 +399,27 @@ def test_a_sample_past_31_bits():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(40000, 8, 1, 3), (40000, 64, 3, 3)])
+def test_more_samples_than_a_grid_dimension(shape):
+    from paper_2008_05823_b200 import group_norm as gn
+    n, c = shape[:2]
+    case = (shape, 2, BF16, "relu", False, 0, 0, 0.3)
+    x, w, b, _, dy = build(case, 5)
+    y, mean, rstd = gn.group_norm_forward(x, 2, w, b, 1e-5, "relu")
+    dx, _, dw, db = gn.group_norm_backward(dy, x, mean, rstd, 2, w, b, "relu")
+    some = [0, 1, 32767, 32768, 32769, n - 1]
+    wn, bn = w.double().cpu().numpy(), b.double().cpu().numpy()
+    want_y, want_mean, _ = forward64(last(x[some]), 2, wn, bn, 1e-5, "relu", 0.0, BF16)
+    close(last(y[some]), want_y, "y")
+    close(mean[some], want_mean, "mean")
+    m, r = mean.double().cpu().numpy(), rstd.double().cpu().numpy()
+    want_dx, _, want_dw, want_db = backward64(last(dy), last(x), m, r, 2, wn, bn, "relu", 0.0, BF16)
+    close(last(dx), want_dx, "dx")
+    close(dw, want_dw, "dweight")
+    close(db, want_db, "dbias")
+
+
+@pytest.mark.gpu
 def test_python_refusals():
     from paper_2008_05823_b200 import group_norm as gn
     x = torch.randn(2, 8, 4, 4, device="cuda").to(memory_format=torch.channels_last)
