@@ -34,24 +34,82 @@ __device__ __forceinline__ void put_param(void* p, int type, int c, float v) {
 }
 
 // ---- activations ------------------------------------------------------------------------------------------------
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
-// Exact enough for float32 results: expf and a true division.  (__expf's error grows with |z|.)
-__device__ __forceinline__ float sigmoid_exact(float z) { return __fdiv_rn(1.0f, 1.0f + expf(-z)); }
+// Results of 16 bits are computed with the special-function unit's 2^x and 1/x (errors of a few units of a float, and |z| more
+// in the exponent) two elements at a time where there is arithmetic; float results with expf, erff and true divisions.
+__device__ __forceinline__ float fast_exp2(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+__device__ __forceinline__ float fast_rcp(float v) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 
-template <typename T>
-__device__ __forceinline__ float sigmoid_for(float z) { return sizeof(T) == 4 ? sigmoid_exact(z) : sigmoid(z); }
+template <int V>
+__device__ __forceinline__ void vset(float (&o)[V], float v) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) o[i] = v;
+}
+
+// s = 1 / (1 + exp(-z))
+template <typename T, int V>
+__device__ __forceinline__ void sigmoid(float (&s)[V], const float (&z)[V]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[i] = __fdiv_rn(1.0f, 1.0f + expf(-z[i]));
+  } else {
+    float c[V], one[V];
+    vset<V>(c, -1.44269504f);
+    vset<V>(one, 1.0f);
+    vmul<V>(s, z, c);
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[i] = fast_exp2(s[i]);
+    vadd<V>(s, s, one);
+#pragma unroll
+    for (int i = 0; i < V; ++i) s[i] = fast_rcp(s[i]);
+  }
+}
+
+// The normal distribution's cdf and exp(-z^2 / 2).  16 bits: erf by formula 7.1.26 of Abramowitz and Stegun (within 1.5e-7),
+// whose exponential is the density's.
+template <typename T, int V>
+__device__ __forceinline__ void normal(float (&cdf)[V], float (&e)[V], const float (&z)[V]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) { cdf[i] = 0.5f * (1.0f + erff(z[i] * 0.70710678f)); e[i] = expf(-0.5f * z[i] * z[i]); }
+  } else {
+    float t[V], p[V], c[V];
+    vset<V>(c, -0.72134752f);                                                   // -log2(e) / 2
+    vmul<V>(e, z, z);
+    vmul<V>(e, e, c);
+    vset<V>(c, 1.0f);
+    vset<V>(p, 0.3275911f * 0.70710678f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) { e[i] = fast_exp2(e[i]); t[i] = fabsf(z[i]); }
+    vfma<V>(t, t, p, c);
+#pragma unroll
+    for (int i = 0; i < V; ++i) t[i] = fast_rcp(t[i]);
+    vset<V>(p, 1.061405429f);
+    vset<V>(c, -1.453152027f); vfma<V>(p, p, t, c);
+    vset<V>(c, 1.421413741f); vfma<V>(p, p, t, c);
+    vset<V>(c, -0.284496736f); vfma<V>(p, p, t, c);
+    vset<V>(c, 0.254829592f); vfma<V>(p, p, t, c);
+    vmul<V>(p, p, t);
+    vset<V>(c, 0.5f);
+    vmul<V>(t, e, c);
+    vmul<V>(p, p, t);                                                           // the tail beyond |z|
+#pragma unroll
+    for (int i = 0; i < V; ++i) cdf[i] = z[i] >= 0.0f ? 1.0f - p[i] : p[i];
+  }
+}
 
 template <typename T, int V>
 __device__ __forceinline__ void activate(float (&z)[V], int act) {
-  if (act == SAE_ACT_RELU) {
+  if (act == SAE_ACT_RELU) {                                                    // a NaN stays
 #pragma unroll
     for (int i = 0; i < V; ++i) asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(z[i]) : "f"(z[i]));
   } else if (act == SAE_ACT_SILU) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) z[i] *= sigmoid_for<T>(z[i]);
+    float s[V];
+    sigmoid<T, V>(s, z);
+    vmul<V>(z, z, s);
   } else if (act == SAE_ACT_GELU) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) z[i] *= 0.5f * (1.0f + erff(z[i] * 0.70710678f));
+    float cdf[V], e[V];
+    normal<T, V>(cdf, e, z);
+    vmul<V>(z, z, cdf);
   }
 }
 
@@ -61,18 +119,23 @@ __device__ __forceinline__ void slope(float (&dz)[V], const float (&z)[V], int a
   if (act == SAE_ACT_RELU) {
 #pragma unroll
     for (int i = 0; i < V; ++i) dz[i] = z[i] > 0.0f ? dz[i] : 0.0f;
-  } else if (act == SAE_ACT_SILU) {
+  } else if (act == SAE_ACT_SILU) {                                             // s (1 + z (1 - s))
+    float s[V], t[V], one[V];
+    sigmoid<T, V>(s, z);
+    vset<V>(one, 1.0f);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float s = sigmoid_for<T>(z[i]);
-      dz[i] *= s * (1.0f + z[i] * (1.0f - s));
-    }
-  } else if (act == SAE_ACT_GELU) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float cdf = 0.5f * (1.0f + erff(z[i] * 0.70710678f));
-      dz[i] *= cdf + z[i] * (0.39894228f * expf(-0.5f * z[i] * z[i]));
-    }
+    for (int i = 0; i < V; ++i) t[i] = -s[i];
+    vadd<V>(t, t, one);
+    vfma<V>(t, t, z, one);
+    vmul<V>(t, t, s);
+    vmul<V>(dz, dz, t);
+  } else if (act == SAE_ACT_GELU) {                                             // cdf + z exp(-z^2 / 2) / sqrt(2 pi)
+    float cdf[V], e[V], c[V];
+    normal<T, V>(cdf, e, z);
+    vset<V>(c, 0.39894228f);
+    vmul<V>(e, e, c);
+    vfma<V>(e, e, z, cdf);
+    vmul<V>(dz, dz, e);
   }
 }
 
