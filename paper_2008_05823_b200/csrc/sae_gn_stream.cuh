@@ -1,5 +1,8 @@
-// Group norm in two passes: streaming kernels for groups too large to stay on chip.  The second pass finds in L2 what the
-// first one read: the host cuts the samples into portions that fit there.
+// Group norm in two passes: streaming kernels for tensors too large to stay on chip.  The second pass runs backwards, so that
+// it begins with what the first one read last and L2 still holds.
+//
+// Where the channel count is no multiple of a 16-byte vector but the tensors have no gaps, `rep` neighbouring pixels make one
+// row of vectors: channel c of it is channel c mod C, and everything below works on rows of rep * C channels.
 #pragma once
 #include "sae_gn_common.cuh"
 
@@ -7,7 +10,8 @@ namespace sae {
 
 struct Stream {
   int n0;                                // first sample of this launch
-  int slices, px;                        // runs of pixels a sample is cut into, pixels of one
+  int rep, vc;                           // pixels of a row (Args::P and the pixel strides count rows), its channels rep * C
+  int slices, px;                        // runs of rows a sample is cut into, rows of one
   int cvt, tiles, tile_groups;           // vectors of a pixel a block takes, tiles of them in a pixel, groups a tile touches at most
   int param_z;                           // backward apply: leading layers of the grid that sum up dw and db
   bool held;                             // backward sums: the second pass reads dresidual instead of dy and the residual
@@ -26,12 +30,32 @@ __device__ __forceinline__ Place place(const Args& a, const Stream& s) {
   q.rows = GN_THREADS / s.cvt;
   q.row = threadIdx.x / s.cvt;
   q.c = (blockIdx.y * s.cvt + (threadIdx.x - q.row * s.cvt)) * V;
-  q.on = q.row < q.rows && q.c < a.C;
+  q.on = q.row < q.rows && q.c < s.vc;
   q.p = q.slice * s.px + q.row;
   q.p1 = min(a.P, (q.slice + 1) * s.px);
   return q;
 }
-__device__ __forceinline__ int run_pixels(const Args& a, const Stream& s, int i) { return min(s.px, a.P - i * s.px); }
+__device__ __forceinline__ int run_pixels(const Args& a, const Stream& s, int i) { return s.rep * min(s.px, a.P - i * s.px); }
+
+// Channels of a row and their groups.
+struct Channel {
+  float inv_c, inv_cg;
+  int C;
+  bool rows;
+  __device__ __forceinline__ Channel(const Args& a, const Stream& s) : inv_c(1.0f / (float)a.C), inv_cg(1.0f / (float)a.Cg), C(a.C), rows(s.rep > 1) {}
+  __device__ __forceinline__ int of(int c) const { return rows ? c - C * quotient(c, inv_c) : c; }
+  __device__ __forceinline__ int group(int c) const { return quotient(of(c), inv_cg); }
+};
+template <int V>
+__device__ __forceinline__ void row_params(const Args& a, const Channel& ch, int c, float (&w)[V], float (&b)[V]) {
+  if (!ch.rows) {
+    params<V>(a.w, a.ptype, c, 1.0f, w);
+    params<V>(a.b, a.ptype, c, 0.0f, b);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) { w[i] = param(a.w, a.ptype, ch.of(c + i), 1.0f); b[i] = param(a.b, a.ptype, ch.of(c + i), 0.0f); }
+  }
+}
 
 // A stream kernel lets its successor start as soon as all its blocks run, and itself waits, before it touches what another
 // kernel of the call has written, for all of its predecessor.
@@ -149,8 +173,18 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
 // Sums of each group's values in sh[rows][pitch], SL of them a vector of V channels: out(j, sum, channels).  Where there are
 // more values than threads, columns are added up over the rows first.  Begins with a barrier.
 template <int SL, int V, typename F>
-__device__ __forceinline__ void fold_tile(const Args& a, const Tile& t, float* sh, int rows, int pitch, F out) {
+__device__ __forceinline__ void fold_tile(const Args& a, const Tile& t, float* sh, int rows, int rep, int pitch, F out) {
   __syncthreads();
+  if (rep > 1) {                          // a channel's places in the row too
+    for (int i = threadIdx.x; i < a.C; i += GN_THREADS) {
+      float s = 0.0f;
+      for (int r = 0; r < rows; ++r)
+        for (int e = i; e < rep * a.C; e += a.C) s += sh[r * pitch + e];
+      sh[i] = s;
+    }
+    rows = 1;
+    __syncthreads();
+  }
   if (rows > 1 && rows * pitch > GN_THREADS) {
     for (int i = threadIdx.x; i < pitch; i += GN_THREADS) {
       float s = 0.0f;
@@ -232,7 +266,7 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_statistics(const Args a, c
   float* const sh = (float*)smem;         // after the walk: [rows][cvt * SL], then [tile_groups]
   let_next_start();
   const Place q = place<V>(a, st);
-  const float inv_cg = 1.0f / (float)a.Cg;
+  const Channel ch(a, st);
   float count = 0.0f, mean[SL], m2[SL], s1[V], s2[V], less[V];
 #pragma unroll
   for (int i = 0; i < SL; ++i) { mean[i] = 0.0f; m2[i] = 0.0f; }
@@ -285,19 +319,19 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_statistics(const Args a, c
 #pragma unroll
     for (int i = 0; i < SL; ++i) sh[slot + i] = q.on ? count * mean[i] : 0.0f;
   }
-  fold_tile<SL, V>(a, tile, sh, q.rows, pitch, [&](int j, float s, int channels) { gmean[j] = s * inv_pixels * __frcp_rn((float)channels); });
+  fold_tile<SL, V>(a, tile, sh, q.rows, st.rep, pitch, [&](int j, float s, int channels) { gmean[j] = s * inv_pixels * __frcp_rn((float)channels); });
   __syncthreads();
   if (q.row < q.rows) {
 #pragma unroll
     for (int i = 0; i < SL; ++i) {
       float v = 0.0f;
-      if (q.on) { const float d = mean[i] - gmean[quotient(q.c + i, inv_cg) - tile.g0]; v = __fmaf_rn(count * d, d, m2[i]); }
+      if (q.on) { const float d = mean[i] - gmean[ch.group(q.c + i) - tile.g0]; v = __fmaf_rn(count * d, d, m2[i]); }
       sh[slot + i] = v;
     }
   }
   float2* const out = run_out(a, st, q);
   wait_for_previous();
-  fold_tile<SL, V>(a, tile, sh, q.rows, pitch, [&](int j, float s, int) { out[j] = make_float2(gmean[j], s); });
+  fold_tile<SL, V>(a, tile, sh, q.rows, st.rep, pitch, [&](int j, float s, int) { out[j] = make_float2(gmean[j], s); });
 }
 
 template <typename T, int V, bool WHOLE, bool RES>
@@ -312,13 +346,13 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_apply(const Args a, const 
   walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p);
   if constexpr (RES) walk.tensor(1, q, (const T*)a.res + q.n * a.r_n + q.c, a.r_p);
   walk.start();                           // no kernel of the call has written these
-  const float inv_cg = 1.0f / (float)a.Cg;
+  const Channel ch(a, st);
   float w[V], b[V], less[V], scale[V];
-  if (q.on) { params<V>(a.w, a.ptype, q.c, 1.0f, w); params<V>(a.b, a.ptype, q.c, 0.0f, b); }
+  if (q.on) row_params<V>(a, ch, q.c, w, b);
   wait_for_previous();
   // the tile's groups: their runs joined about the group's own mean
   const Tile tile = tile_of(a, st, blockIdx.y, V);
-  const float inv_m = 1.0f / ((float)a.P * (float)a.Cg);
+  const float inv_m = 1.0f / ((float)a.P * (float)(st.rep * a.Cg));
   // (sums about the first run's mean: it is off by no more than the runs' spread, which the squares contain)
   join_runs(a, st, tile, q.n, V, stat + st.tile_groups,
             [&](float2& t, float m, float2 v, float2 first) { const float d = v.x - first.x; t.x = __fmaf_rn(m, d, t.x); t.y += __fmaf_rn(m * d, d, v.y); },
@@ -335,15 +369,15 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_apply(const Args a, const 
   if (!q.on) return;
   {
     Per<V, WHOLE> mean, rstd;
-    mean.set([&](int i) { return stat[quotient(q.c + i, inv_cg) - tile.g0].x; });
-    rstd.set([&](int i) { return stat[quotient(q.c + i, inv_cg) - tile.g0].y; });
+    mean.set([&](int i) { return stat[ch.group(q.c + i) - tile.g0].x; });
+    rstd.set([&](int i) { return stat[ch.group(q.c + i) - tile.g0].y; });
     mean.all(less);
     rstd.all(scale);
 #pragma unroll
     for (int i = 0; i < V; ++i) less[i] = -less[i];
   }
-  T* y = (T*)a.out + ((long long)q.n * a.P + walk.first(q)) * a.C + q.c;
-  const long long step = (long long)q.rows * a.C;
+  T* y = (T*)a.out + ((long long)q.n * a.P + walk.first(q)) * st.vc + q.c;
+  const long long step = (long long)q.rows * st.vc;
   const int act = a.act;
   walk.run([&](const Raw<T, V> (&r)[NT], int) {
     float z[V];
@@ -374,7 +408,7 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(cons
   float* const sh = (float*)smem;         // after the walk: [2][rows][cvt * V]; the first rows take the sums, times the weight
   let_next_start();
   const Place q = place<V>(a, st);
-  const float inv_cg = 1.0f / (float)a.Cg;
+  const Channel ch(a, st);
   Walk<T, V, NT, false> walk;
   walk.set(q, smem);
   walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p);
@@ -387,18 +421,17 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(cons
   for (int i = 0; i < V; ++i) { s[i] = 0.0f; sx[i] = 0.0f; }
   if (q.on) {
     float w[V], b[V], less[V], scale[V];
-    params<V>(a.w, a.ptype, q.c, 1.0f, w);
-    params<V>(a.b, a.ptype, q.c, 0.0f, b);
+    row_params<V>(a, ch, q.c, w, b);
     Per<V, WHOLE> mean, rstd;
     const long long g = (long long)q.n * a.G;
-    mean.set([&](int i) { return __ldg(a.mean + g + quotient(q.c + i, inv_cg)); });
-    rstd.set([&](int i) { return __ldg(a.rstd + g + quotient(q.c + i, inv_cg)); });
+    mean.set([&](int i) { return __ldg(a.mean + g + ch.group(q.c + i)); });
+    rstd.set([&](int i) { return __ldg(a.rstd + g + ch.group(q.c + i)); });
     mean.all(less);
     rstd.all(scale);
 #pragma unroll
     for (int i = 0; i < V; ++i) less[i] = -less[i];
-    T* dres = a.dres ? (T*)a.dres + ((long long)q.n * a.P + q.p) * a.C + q.c : nullptr;
-    const long long step = (long long)q.rows * a.C;
+    T* dres = a.dres ? (T*)a.dres + ((long long)q.n * a.P + q.p) * st.vc + q.c : nullptr;
+    const long long step = (long long)q.rows * st.vc;
     const int act = act_of<ACT>(a);
     walk.run([&](const Raw<T, V> (&r)[NT], int) {
       float xh[V], dz[V];
@@ -417,16 +450,17 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(cons
   wait_for_previous();
   const Tile tile = tile_of(a, st, blockIdx.y, V);
   const long long at = ((long long)q.n * st.slices + q.slice) * a.C + tile.lo;
-  for (int i = threadIdx.x; i < pitch; i += GN_THREADS) {
+  for (int i = threadIdx.x; i < (st.rep > 1 ? a.C : pitch); i += GN_THREADS) {
     float s = 0.0f, sx = 0.0f, w = 0.0f;
-    for (int r = 0; r < q.rows; ++r) { s += sh[r * pitch + i]; sx += sh[span + r * pitch + i]; }
+    for (int r = 0; r < q.rows; ++r)
+      for (int e = r * pitch + i, k = 0; k < st.rep; ++k, e += a.C) { s += sh[e]; sx += sh[span + e]; }
     if (tile.lo + i < tile.hi) { a.part_a[at + i] = s; a.part_b[at + i] = sx; w = param(a.w, a.ptype, tile.lo + i, 1.0f); }
     sh[i] = s * w;
     sh[span + i] = sx * w;
   }
   float2* const out = run_out(a, st, q);
-  fold_tile<V, V>(a, tile, sh, 1, pitch, [&](int j, float s, int) { out[j].x = s; });
-  fold_tile<V, V>(a, tile, sh + span, 1, pitch, [&](int j, float s, int) { out[j].y = s; });
+  fold_tile<V, V>(a, tile, sh, 1, 1, pitch, [&](int j, float s, int) { out[j].x = s; });
+  fold_tile<V, V>(a, tile, sh + span, 1, 1, pitch, [&](int j, float s, int) { out[j].y = s; });
 }
 
 // The channels' sums over `rows` runs, 32 channels a block of 256 threads, in a fixed order: dw and db.
@@ -464,7 +498,7 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_apply(con
     return;
   }
   const Place q = place<V>(a, st);
-  const float inv_cg = 1.0f / (float)a.Cg;
+  const Channel ch(a, st);
   Walk<T, V, NT, true> walk;
   walk.set(q, smem);
   walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p);
@@ -473,12 +507,11 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_apply(con
   if (!st.held) walk.start();             // held: the first pass writes what is read here
   float w[V], b[V], less[V], scale[V], p1[V], p2[V], gw[V];
   if (q.on) {
-    params<V>(a.w, a.ptype, q.c, 1.0f, w);
-    params<V>(a.b, a.ptype, q.c, 0.0f, b);
+    row_params<V>(a, ch, q.c, w, b);
     Per<V, WHOLE> mean, rstd;
     const long long g = (long long)q.n * a.G;
-    mean.set([&](int i) { return __ldg(a.mean + g + quotient(q.c + i, inv_cg)); });
-    rstd.set([&](int i) { return __ldg(a.rstd + g + quotient(q.c + i, inv_cg)); });
+    mean.set([&](int i) { return __ldg(a.mean + g + ch.group(q.c + i)); });
+    rstd.set([&](int i) { return __ldg(a.rstd + g + ch.group(q.c + i)); });
     mean.all(less);
     rstd.all(scale);
 #pragma unroll
@@ -488,21 +521,21 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_apply(con
   if (st.held) walk.start();
   // the tile's groups: mean(g) and mean(g * xhat), negated
   const Tile tile = tile_of(a, st, blockIdx.y, V);
-  const float inv_m = 1.0f / ((float)a.P * (float)a.Cg);
+  const float inv_m = 1.0f / ((float)a.P * (float)(st.rep * a.Cg));
   join_runs(a, st, tile, q.n, V, stat + st.tile_groups, [&](float2& t, float, float2 v, float2) { t.x += v.x; t.y += v.y; },
             [&](int j, float2 t) { stat[j] = make_float2(-t.x * inv_m, -t.y * inv_m); });
   if (!q.on) return;
   {
     // dx = rstd * (dz * w - mean(g) - xhat * mean(g * xhat)) = dz * (w rstd) + (xhat * (-rstd mean(g xhat)) - rstd mean(g))
     Per<V, WHOLE> m1, m2;
-    m1.set([&](int i) { return scale[i] * stat[quotient(q.c + i, inv_cg) - tile.g0].x; });
-    m2.set([&](int i) { return scale[i] * stat[quotient(q.c + i, inv_cg) - tile.g0].y; });
+    m1.set([&](int i) { return scale[i] * stat[ch.group(q.c + i) - tile.g0].x; });
+    m2.set([&](int i) { return scale[i] * stat[ch.group(q.c + i) - tile.g0].y; });
     m1.all(p1);
     m2.all(p2);
     vmul<V>(gw, w, scale);
   }
-  T* dx = (T*)a.out + ((long long)q.n * a.P + walk.first(q)) * a.C + q.c;
-  const long long step = (long long)q.rows * a.C;
+  T* dx = (T*)a.out + ((long long)q.n * a.P + walk.first(q)) * st.vc + q.c;
+  const long long step = (long long)q.rows * st.vc;
   const int act = act_of<ACT>(a);
   walk.run([&](const Raw<T, V> (&r)[NT], int) {
     float xh[V], dz[V];

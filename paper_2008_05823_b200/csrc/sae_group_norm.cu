@@ -47,14 +47,23 @@ bool desc_ok(const sae_group_norm_desc* d) {
   return true;
 }
 
-// Sixteen bytes at a time where every tensor of the call lets it (base, strides and the channel count), else four, else one element.
-int vector_width(const sae_group_norm_desc* d, const void* const* ptrs, int n) {
-  const int es = elem(d->type);
-  uintptr_t m = 0;
-  for (int i = 0; i < n; ++i) m |= reinterpret_cast<uintptr_t>(ptrs[i]);
-  const long long s = d->x_sample | d->x_pixel | d->residual_sample | d->residual_pixel | d->dy_sample | d->dy_pixel | d->channels;
-  m |= (uintptr_t)(s * es);
-  return (m & 15) == 0 ? 16 / es : es == 2 && (m & 3) == 0 ? 2 : 1;
+// Elements a thread takes at a time, and, where that is less than 16 bytes, the wider vector that rows of several pixels allow.
+struct Width { int vec, row_vec; };
+
+int common(long long a, long long b) { while (b) { const long long t = a % b; a = b; b = t; } return (int)a; }
+int row_pixels(const sae_group_norm_desc* d, int vec) { return vec / common(d->channels, vec); }
+
+// Sixteen bytes where every tensor of the call lets it (base, strides and the channel count), else four, else one element.
+Width vector_width(const sae_group_norm_desc* d, const void* const* ptrs, int n, bool residual, bool dy) {
+  const int es = elem(d->type), most = 16 / es;
+  uintptr_t base = 0;
+  for (int i = 0; i < n; ++i) base |= reinterpret_cast<uintptr_t>(ptrs[i]);
+  const long long samples = d->x_sample | d->residual_sample | d->dy_sample;
+  const uintptr_t m = base | (uintptr_t)((samples | d->x_pixel | d->residual_pixel | d->dy_pixel | d->channels) * es);
+  Width w = {(m & 15) == 0 ? most : es == 2 && (m & 3) == 0 ? 2 : 1, 0};
+  const bool gapless = d->x_pixel == d->channels && (!residual || d->residual_pixel == d->channels) && (!dy || d->dy_pixel == d->channels);
+  if (w.vec < most && gapless && (base & 15) == 0 && samples % most == 0) w.row_vec = most;
+  return w;
 }
 
 constexpr int SMEM_MOST = 113 * 1024;     // no kernel here takes more: two blocks an SM at least
@@ -64,6 +73,9 @@ constexpr int SMEM_THIRD = 72 * 1024;    // three blocks an SM
 // against two: 128x32x32x16 float (17, 25 MB of traffic) 8.5 / 14.8 us against 13 / 14; 32x14x14x1024 bf16 with a residual
 // (39, 64 MB) 13.5 / 22.9 against 14.6 / 24.5; 32x56x56x256 bf16 with a residual (154, 257 MB) 47 / 92 against 34 / 61.
 constexpr long long UNIT_TRAFFIC = 32ll << 20;
+// ... against vectors of less than 16 bytes, where two passes have whole ones over rows of pixels (8x100x100x35 bf16, 11 and 17 MB:
+// 23.8 / 46.5 us in one pass, 16.6 / 16.7 in two).
+constexpr long long ROW_TRAFFIC = 4ll << 20;
 
 // One pass over a unit of `seg` bytes a pixel or a little less (whole groups, whole vectors), in clusters of up to `most` blocks
 // of up to `room` bytes; false if the unit does not fit.
@@ -106,9 +118,12 @@ bool unit_plan(const sae_group_norm_desc* d, int vec, int tensors, bool backward
 }
 
 // Two passes, each of about one wave of blocks; a portion is what a grid's third dimension holds.
-void stream_plan(const sae_group_norm_desc* d, int vec, bool backward, bool residual, int sms, Plan& p) {
-  const int cv = (int)((d->channels + vec - 1) / vec);
+void stream_plan(const sae_group_norm_desc* d, int vec, int rep, bool backward, bool residual, int sms, Plan& p) {
   Stream& s = p.s;
+  s.rep = rep;
+  s.vc = rep * (int)d->channels;
+  const long long pixels = d->pixels / rep;                        // rows of them
+  const int cv = (s.vc + vec - 1) / vec;
   s.tiles = (cv + GN_THREADS - 1) / GN_THREADS;
   s.cvt = (cv + s.tiles - 1) / s.tiles;
   s.tiles = (cv + s.cvt - 1) / s.cvt;
@@ -118,23 +133,27 @@ void stream_plan(const sae_group_norm_desc* d, int vec, bool backward, bool resi
   const bool whole = cg_ % vec == 0;
   const long long wave = (long long)sms * (backward && !whole ? 2 : 3), blocks = (long long)p.portion * s.tiles;
   // one wave of blocks, but at least eight vectors for a thread
-  const long long most = std::max<long long>(1, d->pixels / ((long long)rows * 8));
+  const long long most = std::max<long long>(1, pixels / ((long long)rows * 8));
   s.slices = (int)std::min<long long>(1024, std::min(std::max<long long>(1, wave / blocks), most));
-  s.px = (int)((d->pixels + s.slices - 1) / s.slices);
-  s.slices = (int)((d->pixels + s.px - 1) / s.px);
+  s.px = (int)((pixels + s.slices - 1) / s.slices);
+  s.slices = (int)((pixels + s.px - 1) / s.px);
   const size_t runs = (size_t)d->samples * s.slices;
   p.bytes = runs * s.tiles * s.tile_groups * sizeof(float2) + (backward ? 2 * runs * d->channels * sizeof(float) : 0);
 }
 
-Plan make_plan(const sae_group_norm_desc* d, int vec, bool backward, bool residual, int sms) {
+Plan make_plan(const sae_group_norm_desc* d, Width w, bool backward, bool residual, int sms) {
   Plan p = {};
+  const int vec = w.vec;
   p.vec = vec;
+  // rows of several pixels: no pixels left over, one tile
+  int rep = w.row_vec ? row_pixels(d, w.row_vec) : 1;
+  if (rep > 1 && (d->pixels % rep || rep * d->channels / w.row_vec > GN_THREADS)) rep = 1;
   // backward: a second slot for dz in float where its type cannot hold it
   const bool second = residual || (backward && elem(d->type) == 2 && d->activation >= SAE_ACT_SILU);
   const int tensors = (backward ? 2 : 1) + (second ? 1 : 0);
   const int segs[3] = {128, 64, 32};                               // shorter runs of a pixel where longer ones do not fit
   const long long traffic = d->samples * d->pixels * d->channels * elem(d->type) * (backward ? 3 + 2 * residual : 2 + residual);
-  if (traffic <= UNIT_TRAFFIC) {
+  if (traffic <= (rep > 1 ? ROW_TRAFFIC : UNIT_TRAFFIC)) {
     // a unit a block, if that fills the SMs; else clusters, of narrower units where wide ones are too few to fill them and leave
     // a thread more than four vectors (3x33x47x90 float: 12.5 us with 72 blocks, 9.4 with 360)
     unit_plan(d, vec, tensors, backward, segs[0], 1, SMEM_MOST, sms, p);
@@ -148,7 +167,10 @@ Plan make_plan(const sae_group_norm_desc* d, int vec, bool backward, bool residu
     for (int i = 0; i < 3 && !p.unit; ++i) unit_plan(d, vec, tensors, backward, segs[i], 8, SMEM_MOST, sms, p);
   }
   if (p.unit) p.bytes = backward ? (size_t)2 * 4 * d->samples * d->channels : 0;
-  else stream_plan(d, vec, backward, residual, sms, p);
+  else {
+    if (rep > 1) p.vec = w.row_vec;
+    stream_plan(d, p.vec, rep, backward, residual, sms, p);
+  }
   return p;
 }
 
@@ -167,6 +189,7 @@ Args make_args(const sae_group_norm_desc* d, const Plan& p, void* ws) {
   a.x_n = d->x_sample; a.x_p = d->x_pixel; a.r_n = d->residual_sample; a.r_p = d->residual_pixel; a.d_n = d->dy_sample; a.d_p = d->dy_pixel;
   a.N = (int)d->samples; a.P = (int)d->pixels; a.C = (int)d->channels; a.G = d->groups; a.Cg = a.C / a.G;
   a.act = d->activation; a.ptype = d->param_type; a.eps = d->eps;
+  if (!p.unit && p.s.rep > 1) { a.P /= p.s.rep; a.x_p *= p.s.rep; a.r_p *= p.s.rep; a.d_p *= p.s.rep; }
   const size_t runs = (size_t)a.N * (p.unit ? 1 : p.s.slices);
   a.part_s = (float2*)ws;
   a.part_a = (float*)(a.part_s + (p.unit ? 0 : runs * p.s.tiles * p.s.tile_groups));
@@ -280,7 +303,7 @@ int backward_as(const Args& all, const Plan& p, cudaStream_t st) {
     s.param_z = 0;
     rc = GN_ACT(grad_sums, a, s, grid, st, s.n0 == 0);
     if (s.held) {
-      a.dy = a.dres; a.d_n = (long long)a.P * a.C; a.d_p = a.C;
+      a.dy = a.dres; a.d_n = (long long)a.P * s.vc; a.d_p = s.vc;
       a.act = SAE_ACT_NONE; a.res = nullptr;
     }
     if (s.n0 + p.portion >= all.N) s.param_z = (int)((param_blocks + grid.x * grid.y - 1) / (grid.x * grid.y));
@@ -323,7 +346,8 @@ int64_t sae_group_norm_workspace(const sae_group_norm_desc* d, int32_t backward)
   const int widths[3] = {16 / elem(d->type), 2, 1};
   for (int i = 0; i < 3; ++i) {
     if ((i == 1 && elem(d->type) == 4) || d->channels % widths[i]) continue;
-    for (int r = 0; r < 2; ++r) most = std::max(most, make_plan(d, widths[i], backward != 0, r != 0, sms).bytes);
+    for (int r = 0; r < 4; ++r)
+      most = std::max(most, make_plan(d, {widths[i], i && r >= 2 ? widths[0] : 0}, backward != 0, r & 1, sms).bytes);
   }
   return (int64_t)most;
 }
@@ -344,7 +368,7 @@ int sae_group_norm_forward(const sae_group_norm_desc* d, const void* x, const vo
   const int sms = device_sms();
   if (sms < 1) return SAE_ERR_CUDA;
   const void* ptrs[3] = {x, y, residual};
-  const Plan p = make_plan(d, vector_width(d, ptrs, 3), false, residual != nullptr, sms);
+  const Plan p = make_plan(d, vector_width(d, ptrs, 3, residual != nullptr, false), false, residual != nullptr, sms);
   if ((p.bytes && !workspace) || !aligned_to(workspace, 16) || workspace_bytes < p.bytes) return SAE_ERR_INVALID_ARG;
   Args a = make_args(d, p, workspace);
   a.x = x; a.res = residual; a.w = weight; a.b = bias; a.out = y; a.mean = mean; a.rstd = rstd;
@@ -369,7 +393,7 @@ int sae_group_norm_backward(const sae_group_norm_desc* d, const void* dy, const 
   const int sms = device_sms();
   if (sms < 1) return SAE_ERR_CUDA;
   const void* ptrs[5] = {dy, x, residual, dx, dresidual};
-  const Plan p = make_plan(d, vector_width(d, ptrs, 5), true, residual != nullptr, sms);
+  const Plan p = make_plan(d, vector_width(d, ptrs, 5, residual != nullptr, true), true, residual != nullptr, sms);
   if ((p.bytes && !workspace) || !aligned_to(workspace, 16) || workspace_bytes < p.bytes) return SAE_ERR_INVALID_ARG;
   Args a = make_args(d, p, workspace);
   a.x = x; a.dy = dy; a.res = residual; a.w = weight; a.b = bias; a.out = dx; a.dres = dresidual; a.dw = dweight; a.db = dbias;

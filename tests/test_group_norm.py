@@ -202,6 +202,13 @@ CASES = [
     ((1, 130, 100, 100), 13, F32, "relu", True, 2, 0, 0.0),
     ((9, 64, 56, 56), 8, F32, "silu", True, 0, 0, 0.0),
     ((2, 128, 40, 40), 32, BF16, "silu", True, 0, 0, 0.0),
+    # no multiple of a vector, without gaps: several pixels make a row (large enough for it), and beside them ones that do not
+    ((8, 35, 104, 100), 7, BF16, "relu", True, 0, 0, 0.3),
+    ((4, 90, 100, 60), 15, F16, "silu", False, 0, 0, 0.0),
+    ((2, 99, 120, 100), 3, F32, "gelu", True, 0, 0, 0.2),
+    ((3, 20, 200, 100), 20, BF16, "gelu", True, 0, 0, 0.0),
+    ((1, 111, 199, 101), 37, BF16, "relu", False, 0, 0, 0.0),
+    ((2, 35, 201, 200), 5, BF16, "none", True, 5, 0, 0.0),
 ]
 
 
