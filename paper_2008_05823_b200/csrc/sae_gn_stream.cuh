@@ -63,7 +63,7 @@ __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // How many of its pixels a thread has on their way: up to 64 KB of a block's shared memory, three blocks an SM.
-__host__ __device__ constexpr int ring_depth(int bytes, int tensors) { return bytes == 16 ? (tensors == 3 ? 5 : 8) : bytes == 4 ? 16 : 8; }
+__host__ __device__ constexpr int ring_depth(int bytes, int tensors) { return bytes == 16 ? (tensors == 3 ? 5 : 8) : bytes == 4 ? 16 : 24 / tensors; }
 __host__ __device__ constexpr size_t ring_bytes(int bytes, int tensors) { return bytes < 4 ? 0 : (size_t)ring_depth(bytes, tensors) * tensors * bytes * GN_THREADS; }
 
 // A thread's walk over its pixels of NT tensors, first to last or (BACK) last to first: the second pass begins with what the

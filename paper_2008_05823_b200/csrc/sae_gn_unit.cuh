@@ -22,8 +22,20 @@ struct Unit {
 // A thread's `turns` vectors, `step` elements apart, into its slots.
 template <typename T, int V>
 __device__ __forceinline__ void fetch(typename Raw<T, V>::B* to, const T* from, long long step, int pitch, int turns) {
+  if constexpr (V * sizeof(T) >= 4) {
 #pragma unroll 4
-  for (int k = 0; k < turns; ++k, from += step) copy_async<V * (int)sizeof(T)>(to + k * pitch, from);
+    for (int k = 0; k < turns; ++k, from += step) copy_async<V * (int)sizeof(T)>(to + k * pitch, from);
+  } else {                                // no asynchronous copy of two bytes: eight loads, then eight stores
+    for (int k = 0; k < turns; k += 8) {
+      typename Raw<T, V>::B b[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i, from += step)
+        if (k + i < turns) b[i] = __ldg((const typename Raw<T, V>::B*)from);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (k + i < turns) to[(k + i) * pitch] = b[i];
+    }
+  }
 }
 
 // A block's place: a cluster is one unit (chunk blockIdx.x / S of sample n), a block the rank-th run of its pixels.

@@ -73,9 +73,10 @@ constexpr int SMEM_THIRD = 72 * 1024;    // three blocks an SM
 // against two: 128x32x32x16 float (17, 25 MB of traffic) 8.5 / 14.8 us against 13 / 14; 32x14x14x1024 bf16 with a residual
 // (39, 64 MB) 13.5 / 22.9 against 14.6 / 24.5; 32x56x56x256 bf16 with a residual (154, 257 MB) 47 / 92 against 34 / 61.
 constexpr long long UNIT_TRAFFIC = 32ll << 20;
-// ... against vectors of less than 16 bytes, where two passes have whole ones over rows of pixels (8x100x100x35 bf16, 11 and 17 MB:
-// 23.8 / 46.5 us in one pass, 16.6 / 16.7 in two).
-constexpr long long ROW_TRAFFIC = 4ll << 20;
+// With vectors of less than 16 bytes a unit's threads hold little each: 8x100x100x35 bf16 (11 and 17 MB) 23.8 / 46.5 us in one
+// pass, 16.6 / 16.7 in two, which have whole vectors over rows of pixels; 14x54x55x72 bf16 of 109 channels (12 and 18 MB),
+// which have not, 28.8 / 25.3 against 19.4 / 22.7.
+constexpr long long NARROW_TRAFFIC = 4ll << 20;
 
 // One pass over a unit of `seg` bytes a pixel or a little less (whole groups, whole vectors), in clusters of up to `most` blocks
 // of up to `room` bytes; false if the unit does not fit.
@@ -153,7 +154,7 @@ Plan make_plan(const sae_group_norm_desc* d, Width w, bool backward, bool residu
   const int tensors = (backward ? 2 : 1) + (second ? 1 : 0);
   const int segs[3] = {128, 64, 32};                               // shorter runs of a pixel where longer ones do not fit
   const long long traffic = d->samples * d->pixels * d->channels * elem(d->type) * (backward ? 3 + 2 * residual : 2 + residual);
-  if (traffic <= (rep > 1 ? ROW_TRAFFIC : UNIT_TRAFFIC)) {
+  if (traffic <= (vec * elem(d->type) < 16 ? NARROW_TRAFFIC : UNIT_TRAFFIC)) {
     // a unit a block, if that fills the SMs; else clusters, of narrower units where wide ones are too few to fill them and leave
     // a thread more than four vectors (3x33x47x90 float: 12.5 us with 72 blocks, 9.4 with 360)
     unit_plan(d, vec, tensors, backward, segs[0], 1, SMEM_MOST, sms, p);

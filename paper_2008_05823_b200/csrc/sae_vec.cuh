@@ -40,8 +40,7 @@ template <int BYTES>
 __device__ __forceinline__ void copy_async(void* to, const void* from) {
   const unsigned int s = (unsigned int)__cvta_generic_to_shared(to);
   if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(from) : "memory");
-  else if constexpr (BYTES >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(s), "l"(from), "n"(BYTES) : "memory");
-  else *(unsigned short*)to = __ldg((const unsigned short*)from);
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(s), "l"(from), "n"(BYTES) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
