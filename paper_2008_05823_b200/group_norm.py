@@ -54,7 +54,7 @@ class _GroupNorm(torch.autograd.Function):
     def backward(ctx, dy):
         x, weight, bias, residual, mean, rstd = ctx.saved_tensors
         need = ctx.needs_input_grad
-        if x.dim() > 2 and not _channels_last(dy):          # a gradient in another order: laid out like x
+        if not _channels_last(dy):                          # a gradient in another order: laid out like x
             dy = dy.movedim(1, -1).contiguous().movedim(-1, 1)
         dx, dres, dweight, dbias = group_norm_backward(dy, x, mean, rstd, ctx.num_groups, weight, bias, ctx.activation, residual,
                                                        need[3], need[1] or need[2])

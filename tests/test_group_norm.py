@@ -209,6 +209,15 @@ CASES = [
     ((3, 20, 200, 100), 20, BF16, "gelu", True, 0, 0, 0.0),
     ((1, 111, 199, 101), 37, BF16, "relu", False, 0, 0, 0.0),
     ((2, 35, 201, 200), 5, BF16, "none", True, 5, 0, 0.0),
+    # groups wider than a block, and tensors too large for one pass: whole vectors in a group, and groups that cut them
+    ((2, 4100, 2), 1, F32, "relu", True, 0, 0, 0.0),
+    ((3, 9000, 5), 2, BF16, "silu", False, 0, 0, 0.2),
+    ((4, 3000, 30, 31), 3, BF16, "relu", False, 0, 0, 0.0),
+    ((7, 256, 56, 64), 32, BF16, "relu", True, 0, 0, 0.3),
+    ((7, 256, 56, 64), 16, F16, "silu", False, 8, 0, 0.0),
+    ((6, 128, 64, 64), 32, F32, "none", True, 0, 0, 0.0),
+    ((6, 128, 64, 64), 8, F32, "silu", True, 4, 0, 0.1),
+    ((3, 320, 100, 100), 32, BF16, "relu", True, 0, 0, 0.0),
 ]
 
 
@@ -331,6 +340,11 @@ def test_module_and_autograd():
     plain = gn.GroupNorm(4, 16, device="cuda")
     (plain(x, one.expand(3, 16, 6, 5)) * dy).sum().backward()
     assert torch.allclose(one.grad, dy.sum(0, keepdim=True), atol=1e-5)
+    # no pixels: [n, c], its gradient broadcast
+    flat = torch.randn(3, 16, device="cuda", requires_grad=True)
+    m(flat).sum().backward()
+    ref = torch.relu(torch.nn.functional.group_norm(flat.double(), 4, m.weight.double(), m.bias.double(), 1e-5))
+    assert torch.allclose(flat.grad.double(), torch.autograd.grad(ref.sum(), [flat])[0].double(), atol=1e-4)
     frozen = gn.group_norm(x, 4, m.weight.detach(), m.bias.detach(), 1e-5, "silu")
     (gx,) = torch.autograd.grad(frozen, [x], dy)
     assert torch.isfinite(gx).all()
