@@ -2,8 +2,8 @@
 in float64, gradients against differences too.
 
 Tolerances come with the reference, element by element, from u = 2^-24 and the number of roundings in sequence:
-a statistic passes at most L = 16 + P / (4 max(1, 256 // C)) of them (batches of a thread's pixels, a tree over the block's
-rows, the rest in double), a gradient sum S = 32 + P / max(1, 256 // C) + N.  mean is then within L u mean|x|, var within
+a statistic passes at most L = 16 + P / (4 max(1, 256 // C)) of them (runs of a thread's pixels, then a block's threads, then
+the blocks), a gradient sum S = 32 + P / max(1, 256 // C) + N.  mean is then within L u mean|x|, var within
 L u (2 + k) of itself with k = |mean| / std; x - mean, * rstd, * w, + b and the residual round once each.  A slope or
 activation costs 16 u in float32; in 16 bits it uses the fast exponential, whose error is 2 + 1.2 |z| units: 128 u up to the
 |z| < 40 that occur here.  relu's slope jumps at 0: where |z| is within its error, either value is right.  Outputs round once:
