@@ -69,7 +69,7 @@ __host__ __device__ constexpr size_t ring_bytes(int bytes, int tensors) { return
 // A thread's walk over its pixels of NT tensors, first to last or (BACK) last to first: the second pass begins with what the
 // first one read last.  Copies run ahead through a ring of slots of the thread's own in shared memory, so no barrier is
 // needed and the loads in flight do not depend on registers; single 16-bit elements, which have no asynchronous copy, are
-// loaded in batches instead.
+// loaded in batches instead, and not as constants: a backward apply that began early reads what the sums' kernel still wrote then.
 template <typename T, int V, int NT, bool BACK>
 struct Walk {
   typedef typename Raw<T, V>::B B;
@@ -132,7 +132,7 @@ struct Walk {
         for (int k = 0; k < D; ++k) {
           if (k0 + k < turns) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) { r[k][t].load(next[t]); next[t] += step[t]; }
+            for (int t = 0; t < NT; ++t) { r[k][t].load_written(next[t]); next[t] += step[t]; }
           }
         }
 #pragma unroll

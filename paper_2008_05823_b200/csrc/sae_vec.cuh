@@ -51,7 +51,8 @@ template <typename T, int V>
 struct Raw {
   typedef typename Bits<V * (int)sizeof(T)>::type B;
   B b;
-  __device__ __forceinline__ void load(const T* p) { b = __ldg(reinterpret_cast<const B*>(p)); }
+  __device__ __forceinline__ void load(const T* p) { b = __ldg(reinterpret_cast<const B*>(p)); }          // nobody writes there while the kernel lives
+  __device__ __forceinline__ void load_written(const T* p) { b = __ldcg(reinterpret_cast<const B*>(p)); } // another kernel of the call may
   __device__ __forceinline__ void clear() { b = B{}; }
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<B*>(p) = b; }
   __device__ __forceinline__ void store_stream(T* p) const { __stcs(reinterpret_cast<B*>(p), b); }

@@ -461,3 +461,21 @@ def test_python_refusals():
     for kw in ((3, 8), (0, 8)):
         with pytest.raises(ValueError):
             gn.GroupNorm(*kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("shape,groups,wide", [((2, 35, 201, 200), 5, 5), ((9, 33, 130, 131), 3, 0), ((70, 130, 30, 31), 13, 1)])
+def test_second_pass_reads_what_the_first_has_written(shape, groups, wide, dtype):
+    """Two passes over single 16-bit elements: with a residual the second one reads dresidual, without it dy.  Where there is no
+    activation both are the same values, so dx has the same bits, whatever was in dresidual's memory before."""
+    from paper_2008_05823_b200 import group_norm as gn
+    x, w, b, res, dy = build((shape, groups, dtype, "none", True, wide, 0, 0.1), 21)
+    _, mean, rstd = gn.group_norm_forward(x, groups, w, b)
+    want, none, dw, db = gn.group_norm_backward(dy, x, mean, rstd, groups, w, b)
+    assert none is None
+    for fill in (math.nan, 1.0, 1.0, 1.0):
+        junk = [torch.full_like(x, fill) for _ in range(3)]
+        del junk                                     # the next call's outputs lie there
+        dx, dres, dw2, db2 = gn.group_norm_backward(dy, x, mean, rstd, groups, w, b, "none", res)
+        assert torch.equal(dx, want) and torch.equal(dres, dy) and torch.equal(dw, dw2) and torch.equal(db, db2)
