@@ -170,8 +170,7 @@ __device__ __forceinline__ void vector_grad(const Raw<T, V>& x, const Raw<T, V>&
   vadd<V>(xh, xh, less);
   vmul<V>(xh, xh, scale);
   if (act == SAE_ACT_NONE) return;
-  vmul<V>(z, xh, w);
-  vadd<V>(z, z, b);
+  vmul_add<V>(z, xh, w, b);
   if (res) {
     float v[V];
     res->widen(v);

@@ -387,8 +387,7 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_apply(const Args a, const 
     r[0].widen(z);
     vadd<V>(z, z, less);
     vmul<V>(z, z, scale);
-    vmul<V>(z, z, w);
-    vadd<V>(z, z, b);
+    vmul_add<V>(z, z, w, b);
     if constexpr (RES) { float v[V]; r[1].widen(v); vadd<V>(z, z, v); }
     activate<T, V>(z, act);
     Raw<T, V> o;

@@ -191,8 +191,7 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_unit(const Args a, const U
     r.widen(z);
     vadd<V>(z, z, less);
     vmul<V>(z, z, scale);
-    vmul<V>(z, z, w);
-    vadd<V>(z, z, b);
+    vmul_add<V>(z, z, w, b);
     if (a.res) {
       float v[V];
       r.b = rs[k * TH];

@@ -479,3 +479,51 @@ def test_second_pass_reads_what_the_first_has_written(shape, groups, wide, dtype
         del junk                                     # the next call's outputs lie there
         dx, dres, dw2, db2 = gn.group_norm_backward(dy, x, mean, rstd, groups, w, b, "none", res)
         assert torch.equal(dx, want) and torch.equal(dres, dy) and torch.equal(dw, dw2) and torch.equal(db, db2)
+
+
+# ---- z's roundings: no tolerance ---------------------------------------------------------------------------------------------
+
+def plain_z(x, mean, rstd, w, b, res, groups):
+    """x - mean, * rstd, * w, + b, + residual, one float32 operation after the other, pixels before channels."""
+    c = x.shape[1]
+    at = lambda s: s.repeat_interleave(c // groups, 1).view(x.shape[0], *[1] * (x.dim() - 2), c)  # noqa: E731
+    z = (x.movedim(1, -1).float() - at(mean)) * at(rstd)
+    z = z * w + b
+    return z if res is None else z + res.movedim(1, -1).float()
+
+
+# (shape, groups, unread channels beside x): one pass and two, vectors of 16 bytes, of two elements and of one, rows of pixels
+Z_CASES = [((32, 256, 56, 56), 32, 0), ((128, 16, 32, 32), 4, 0), ((16, 256, 56, 56), 16, 2), ((16, 256, 56, 56), 256, 1), ((8, 35, 100, 100), 7, 0),
+           ((2, 64, 14, 14), 32, 0), ((2, 30, 9, 11), 5, 0), ((2, 30, 9, 11), 5, 3), ((2, 35, 9, 11), 5, 0), ((1, 2048, 7, 7), 32, 0), ((40, 24), 3, 0)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("has_res", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("case", range(len(Z_CASES)))
+def test_every_step_of_z_is_rounded(case, dtype, has_res):
+    """With the call's own statistics, y without an activation has the bits of the single operations; relu's mask in the
+    backward call is z > 0, also where the two calls read x in different layouts."""
+    from paper_2008_05823_b200 import group_norm as gn
+    shape, groups, wide = Z_CASES[case]
+    gen = torch.Generator(device="cuda").manual_seed(case)
+    n, c, *space = shape
+
+    def draw(beside):
+        return torch.randn((n, *space, c + beside), device="cuda", generator=gen).to(dtype)[..., :c].movedim(-1, 1)
+
+    x, res = draw(wide), draw(0).clamp(min=0) if has_res else None
+    w, b = 1 + 0.1 * torch.randn(c, device="cuda", generator=gen), 0.1 * torch.randn(c, device="cuda", generator=gen)
+    y, mean, rstd = gn.group_norm_forward(x, groups, w, b, 1e-5, "none", res)
+    z = plain_z(x, mean, rstd, w, b, res, groups)
+    assert torch.equal(y.movedim(1, -1), z.to(dtype))
+    y, _, _ = gn.group_norm_forward(x, groups, w, b, 1e-5, "relu", res)
+    assert torch.equal(y.movedim(1, -1), z.clamp(min=0).to(dtype))
+    # dy = 1: dz is the mask, dbias counts it (exactly: fewer than 2^24 a channel)
+    dense = x.movedim(1, -1).contiguous().movedim(-1, 1)
+    ones = torch.ones_like(dense)
+    for at in (x, dense):
+        _, dres, _, db = gn.group_norm_backward(ones, at, mean, rstd, groups, w, b, "relu", res)
+        assert torch.equal(db, (z > 0).sum(tuple(range(z.dim() - 1))).float())
+        if has_res:
+            assert torch.equal(dres.movedim(1, -1), (z > 0).to(dtype))
