@@ -217,24 +217,29 @@ __device__ __forceinline__ void fold_tile(const Args& a, const Tile& t, float* s
   });
 }
 
+// The tile in which a group begins.
+__device__ __forceinline__ int first_tile(const Args& a, const Stream& s, int g, int vec) { return s.tiles == 1 ? 0 : g * a.Cg / (s.cvt * vec); }
+
 // Joins the runs' pairs of every group of a tile: the threads stand side by side over the groups and, as far as there are
-// more threads, over the runs.  add(sum, pixels * channels, pair, first pair) for each run; done(j, sum) for each group, from
-// one thread, before a barrier.  `sums` holds a pair for each thread.
+// more threads, over the runs.  How many stand over the runs depends on the launch alone, not on the tile's own groups: tiles
+// that share a group add in the same order and get the same bits.  add(sum, pixels * channels, pair, first pair) for each run;
+// done(j, sum) for each group, from one thread, before a barrier.  `sums` holds a pair for each thread.
 template <typename A, typename D>
 __device__ __forceinline__ void join_runs(const Args& a, const Stream& s, const Tile& tile, int n, int vec, float2* sums, A add, D done) {
   const int tile_c = s.cvt * vec;
   const float2* part = a.part_s + (long long)n * s.slices * s.tiles * s.tile_groups;
-  for (int j0 = 0; j0 < tile.groups; j0 += GN_THREADS) {
-    const int across = min(tile.groups - j0, GN_THREADS), subs = GN_THREADS / across, sub = quotient(threadIdx.x, __frcp_rn((float)across));
+  const int across = min(s.tile_groups, GN_THREADS), subs = GN_THREADS / across, sub = quotient(threadIdx.x, __frcp_rn((float)across));
+  for (int j0 = 0; j0 < tile.groups; j0 += across) {
     const int j = j0 + (int)threadIdx.x - sub * across, g = tile.g0 + j;
     float2 t = make_float2(0.0f, 0.0f);
-    if (sub < subs) {
+    if (sub < subs && j < tile.groups) {
+      const int t0 = first_tile(a, s, g, vec);
       if (s.tiles == 1) {
         const float2 first = __ldcg(part + g);
 #pragma unroll 4
         for (int i = sub; i < s.slices; i += subs) add(t, (float)run_pixels(a, s, i) * (float)a.Cg, __ldcg(part + i * s.tile_groups + g), first);
       } else {
-        const int t0 = g * a.Cg / tile_c, tiles = (g * a.Cg + a.Cg - 1) / tile_c - t0 + 1;
+        const int tiles = (g * a.Cg + a.Cg - 1) / tile_c - t0 + 1;
         const float2 first = __ldcg(part + t0 * s.tile_groups + g - t0 * tile_c / a.Cg);
         for (int e = sub; e < s.slices * tiles; e += subs) {
           const int i = tiles == 1 ? e : e / tiles, k = t0 + (e - i * tiles);
@@ -245,7 +250,7 @@ __device__ __forceinline__ void join_runs(const Args& a, const Stream& s, const 
     }
     sums[threadIdx.x] = t;
     __syncthreads();
-    if (sub == 0) {
+    if (sub == 0 && j < tile.groups) {
       for (int k = 1; k < subs; ++k) { const float2 o = sums[k * across + (int)threadIdx.x]; t.x += o.x; t.y += o.y; }
       done(j, t);
     }
@@ -363,11 +368,11 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_apply(const Args a, const 
               const int g = tile.g0 + j;
               const float d = t.x * inv_m;
               const float2* part = a.part_s + (long long)q.n * st.slices * st.tiles * st.tile_groups;
-              const int t0 = st.tiles == 1 ? 0 : g * a.Cg / (st.cvt * V);
+              const int t0 = first_tile(a, st, g, V);
               const float mean = __ldcg(part + t0 * st.tile_groups + g - (st.tiles == 1 ? 0 : t0 * (st.cvt * V) / a.Cg)).x + d;
               const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fmaf_rn(-d, t.x, t.y) * inv_m + a.eps));
               stat[j] = make_float2(mean, rstd);
-              if (q.slice == 0) { a.mean[(long long)q.n * a.G + g] = mean; a.rstd[(long long)q.n * a.G + g] = rstd; }   // tiles that share a group agree
+              if (q.slice == 0 && (int)blockIdx.y == t0) { a.mean[(long long)q.n * a.G + g] = mean; a.rstd[(long long)q.n * a.G + g] = rstd; }
             });
   if (!q.on) return;
   {

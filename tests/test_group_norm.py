@@ -527,3 +527,29 @@ def test_every_step_of_z_is_rounded(case, dtype, has_res):
         assert torch.equal(db, (z > 0).sum(tuple(range(z.dim() - 1))).float())
         if has_res:
             assert torch.equal(dres.movedim(1, -1), (z > 0).to(dtype))
+
+
+# Two passes, tiles that share groups and touch different numbers of them, many runs of pixels
+TILED = [((1, 1152, 60, 60), 9, F32, 1), ((1, 2040, 1000), 85, F32, 1), ((2, 990, 3000), 99, F32, 1), ((1, 2560, 4000), 2, F32, 0), ((2, 2040, 1500), 85, BF16, 1),
+         ((1, 5000, 900), 5, F16, 0), ((1, 4104, 1000), 2, BF16, 0)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", range(len(TILED)))
+def test_tiles_that_share_a_group_agree(case):
+    """Every tile normalises with the statistics that the call returns (y without an activation has the bits that those give),
+    and they are the same bits on every call, forwards and backwards."""
+    from paper_2008_05823_b200 import group_norm as gn
+    shape, groups, dtype, wide = TILED[case]
+    x, w, b, _, dy = build((shape, groups, dtype, "none", False, wide, 0, 0.7), 31 + case)
+    y, mean, rstd = gn.group_norm_forward(x, groups, w, b)
+    assert torch.equal(y.movedim(1, -1), plain_z(x, mean, rstd, w, b, None, groups).to(dtype))
+    want_y, want_mean, want_rstd = forward64(last(x), groups, w.double().cpu().numpy(), b.double().cpu().numpy(), 1e-5, "none", 0.0, dtype)
+    close(mean, want_mean, "mean")
+    close(rstd, want_rstd, "rstd")
+    back = gn.group_norm_backward(dy, x, mean, rstd, groups, w, b)
+    for _ in range(30):
+        again = gn.group_norm_forward(x, groups, w, b)
+        assert all(torch.equal(p, q) for p, q in zip((y, mean, rstd), again))
+        more = gn.group_norm_backward(dy, x, mean, rstd, groups, w, b)
+        assert all(torch.equal(p, q) for p, q in zip(back, more) if p is not None)
