@@ -62,18 +62,24 @@ __device__ __forceinline__ void row_params(const Args& a, const Channel& ch, int
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// How many of its pixels a thread has on their way: up to 64 KB of a block's shared memory, three blocks an SM.
-__host__ __device__ constexpr int ring_depth(int bytes, int tensors) { return bytes == 16 ? (tensors == 3 ? 5 : 8) : bytes == 4 ? 16 : 24 / tensors; }
-__host__ __device__ constexpr size_t ring_bytes(int bytes, int tensors) { return bytes < 4 ? 0 : (size_t)ring_depth(bytes, tensors) * tensors * bytes * GN_THREADS; }
+// How many of its pixels a thread has on their way: up to 64 KB of a block's shared memory, with the bytes that the thread keeps
+// beside them 72 KB, three blocks an SM.
+__host__ __device__ constexpr int ring_depth(int bytes, int tensors, int kept = 0) {
+  const int most = bytes == 16 ? (tensors == 3 ? 5 : 8) : bytes == 4 ? 16 : 24 / tensors, fit = (288 - kept) / (tensors * bytes);
+  return most < fit ? most : fit;
+}
+__host__ __device__ constexpr size_t ring_bytes(int bytes, int tensors, int kept = 0) {
+  return bytes < 4 ? 0 : (size_t)ring_depth(bytes, tensors, kept) * tensors * bytes * GN_THREADS;
+}
 
 // A thread's walk over its pixels of NT tensors, first to last or (BACK) last to first: the second pass begins with what the
 // first one read last.  Copies run ahead through a ring of slots of the thread's own in shared memory, so no barrier is
 // needed and the loads in flight do not depend on registers; single 16-bit elements, which have no asynchronous copy, are
 // loaded in batches instead, and not as constants: a backward apply that began early reads what the sums' kernel still wrote then.
-template <typename T, int V, int NT, bool BACK>
+template <typename T, int V, int NT, bool BACK, int KEPT = 0>
 struct Walk {
   typedef typename Raw<T, V>::B B;
-  static constexpr int D = ring_depth(sizeof(B), NT);
+  static constexpr int D = ring_depth(sizeof(B), NT, KEPT);
   const T* next[NT];
   long long step[NT];
   B* slots;
@@ -109,9 +115,13 @@ struct Walk {
       for (int k = 0; k < D - 1; ++k) fetch(k);
     }
   }
+  // use(the tensors' vectors, turn) for each pixel; after every D of them after(turns so far / D).
   template <typename F>
-  __device__ __forceinline__ void run(F use) {
+  __device__ __forceinline__ void run(F use) { run(use, [](int) {}); }
+  template <typename F, typename G>
+  __device__ __forceinline__ void run(F use, G after) {
     if constexpr (sizeof(B) >= 4) {
+      int rounds = 0;
       for (int k = 0; k < turns; k += D) {
 #pragma unroll
         for (int j = 0; j < D; ++j) {                       // slot j; the one before it has just been used
@@ -123,9 +133,11 @@ struct Walk {
           for (int t = 0; t < NT; ++t) r[t].b = slots[(j * NT + t) * GN_THREADS];
           use(r, k + j);
         }
+        after(++rounds);
       }
       copies_wait<0>();
     } else {
+      int rounds = 0;
       for (int k0 = 0; k0 < turns; k0 += D) {
         Raw<T, V> r[D][NT];
 #pragma unroll
@@ -138,6 +150,7 @@ struct Walk {
 #pragma unroll
         for (int k = 0; k < D; ++k)
           if (k0 + k < turns) use(r[k], k0 + k);
+        after(++rounds);
       }
     }
   }
@@ -408,17 +421,23 @@ __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_apply(const Args a, const 
 template <int ACT>
 __device__ __forceinline__ int act_of(const Args& a) { return ACT == 2 ? a.act : ACT == 1 ? SAE_ACT_RELU : SAE_ACT_NONE; }
 
+// A thread's sums go to a second level, in shared memory, every eight rounds of its ring (32 to 128 pixels): no chain of additions is
+// as long as a run (a constant of 0.1 over 16384 pixels: 2590 units off in one chain, 38 in two levels of 64 and 256).
+__host__ __device__ constexpr int sums_kept(int vec) { return 2 * vec * (int)sizeof(float); }
+
 // Each channel's sum dz and sum dz * xhat over a run, dresidual = dz on the way.  Bound by HBM: 32x56x56x256 bf16, relu with a
 // residual, 206 MB in 36.7 us (5.6 TB/s); silu and gelu by the special-function unit (two operations an element).
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(const Args a, const Stream st) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int NT = RES ? 3 : 2;
+  constexpr int KEPT = sums_kept(V);
   float* const sh = (float*)smem;         // after the walk: [2][rows][cvt * V]; the first rows take the sums, times the weight
+  float* const kept = (float*)(smem + ring_bytes(V * sizeof(T), NT, KEPT)) + threadIdx.x;     // [2 V][threads]
   let_next_start();
   const Place q = place<V>(a, st);
   const Channel ch(a, st);
-  Walk<T, V, NT, false> walk;
+  Walk<T, V, NT, false, KEPT> walk;
   walk.set(q, smem);
   walk.tensor(0, q, (const T*)a.x + q.n * a.x_n + q.c, a.x_p);
   walk.tensor(1, q, (const T*)a.dy + q.n * a.d_n + q.c, a.d_p);
@@ -427,7 +446,7 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(cons
   const int pitch = st.cvt * V, span = q.rows * pitch, slot = (threadIdx.x - q.row * st.cvt) * V;
   float s[V], sx[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) { s[i] = 0.0f; sx[i] = 0.0f; }
+  for (int i = 0; i < V; ++i) { s[i] = 0.0f; sx[i] = 0.0f; kept[i * GN_THREADS] = 0.0f; kept[(V + i) * GN_THREADS] = 0.0f; }
   if (q.on) {
     float w[V], b[V], less[V], scale[V];
     row_params<V>(a, ch, q.c, w, b);
@@ -448,8 +467,18 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(cons
       vadd<V>(s, s, dz);
       vfma<V>(sx, dz, xh, sx);
       if (dres) { Raw<T, V> o; o.round(dz); o.store(dres); dres += step; }
+    }, [&](int rounds) {
+      if ((rounds & 7) == 0) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          kept[i * GN_THREADS] += s[i]; kept[(V + i) * GN_THREADS] += sx[i];
+          s[i] = 0.0f; sx[i] = 0.0f;
+        }
+      }
     });
   }
+#pragma unroll
+  for (int i = 0; i < V; ++i) { s[i] += kept[i * GN_THREADS]; sx[i] += kept[(V + i) * GN_THREADS]; }
   __syncthreads();                        // everybody is through with the ring
   if (q.row < q.rows) {
 #pragma unroll
@@ -472,21 +501,22 @@ __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(cons
   fold_tile<V, V>(a, tile, sh + span, 1, 1, pitch, [&](int j, float s, int) { out[j].y = s; });
 }
 
-// The channels' sums over `rows` runs, 32 channels a block of 256 threads, in a fixed order: dw and db.
+// The channels' sums over `rows` runs, 32 channels a block of 256 threads, in a fixed order: dw and db.  In double: there may be
+// millions of samples.
 __device__ __forceinline__ void param_grads(const Args& a, int block, long long rows) {
-  __shared__ float sa[8][33], sb[8][33];
+  __shared__ double sa[8][33], sb[8][33];
   const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5, c = block * 32 + cx;
-  float s = 0.0f, q = 0.0f;
+  double s = 0.0, q = 0.0;
   if (c < a.C) {
 #pragma unroll 4
-    for (long long r = ry; r < rows; r += 8) { s += __ldcg(a.part_a + r * a.C + c); q += __ldcg(a.part_b + r * a.C + c); }
+    for (long long r = ry; r < rows; r += 8) { s += (double)__ldcg(a.part_a + r * a.C + c); q += (double)__ldcg(a.part_b + r * a.C + c); }
   }
   sa[ry][cx] = s; sb[ry][cx] = q;
   __syncthreads();
   if (ry == 0 && c < a.C) {
     for (int i = 1; i < 8; ++i) { s += sa[i][cx]; q += sb[i][cx]; }
-    if (a.db) put_param(a.db, a.ptype, c, s);
-    if (a.dw) put_param(a.dw, a.ptype, c, q);
+    if (a.db) put_param(a.db, a.ptype, c, (float)s);
+    if (a.dw) put_param(a.dw, a.ptype, c, (float)q);
   }
 }
 __global__ void __launch_bounds__(GN_THREADS) k_gn_param_grads(const Args a, long long rows) {

@@ -273,8 +273,9 @@ int forward_as(const Args& a, const Plan& p, cudaStream_t st) {
 
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 int grad_sums(const Args& a, const Stream& s, dim3 grid, cudaStream_t st, bool first) {
+  constexpr int kept = sums_kept(V);
   return launch<k_gn_grad_sums<T, V, WHOLE, ACT, RES>>(
-      grid, std::max(ring_bytes(V * sizeof(T), RES ? 3 : 2), (size_t)(2 * (GN_THREADS / s.cvt) * s.cvt * V) * 4), st, first, a, s);
+      grid, std::max(ring_bytes(V * sizeof(T), RES ? 3 : 2, kept) + kept * GN_THREADS, (size_t)(2 * (GN_THREADS / s.cvt) * s.cvt * V) * 4), st, first, a, s);
 }
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 int grad_apply(const Args& a, const Stream& s, dim3 grid, cudaStream_t st, bool) {

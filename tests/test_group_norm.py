@@ -553,3 +553,24 @@ def test_tiles_that_share_a_group_agree(case):
         assert all(torch.equal(p, q) for p, q in zip((y, mean, rstd), again))
         more = gn.group_norm_backward(dy, x, mean, rstd, groups, w, b)
         assert all(torch.equal(p, q) for p, q in zip(back, more) if p is not None)
+
+
+# ---- long sums -------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,c,pixels", [(230, 250, 16384), (65536, 8, 4), (230, 256, 8192)])
+def test_long_sums_of_one_sign(n, c, pixels):
+    """dy = 0.1 everywhere: each addition to a long chain rounds the same way, so a chain of k is off by up to k u (one of 16384: 2590 u).
+    Here at most 128 + pixels / 32 of them follow one another in a thread, then 256 in a block and few more, and samples are
+    added in double.  dweight: the same chains over terms of both signs."""
+    from paper_2008_05823_b200 import group_norm as gn
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = (torch.randn((1, pixels, c), device="cuda", generator=gen) + 1).expand(n, pixels, c).movedim(-1, 1)
+    dy = torch.full((1, 1, c), 0.1, device="cuda").expand(n, pixels, c).movedim(-1, 1)
+    mean, rstd = torch.zeros(n, 2, device="cuda"), torch.ones(n, 2, device="cuda")
+    _, _, dw, db = gn.group_norm_backward(dy, x, mean, rstd, 2, torch.ones(c, device="cuda"), torch.zeros(c, device="cuda"))
+    depth = 128 + pixels / 32 + 16 if pixels > 1000 else pixels + 16
+    tenth = float(torch.tensor(0.1))
+    assert float((db.double() / (n * pixels * tenth) - 1).abs().max()) <= depth * U
+    one = x[0].double()
+    assert bool(((dw.double() - tenth * n * one.sum(1)).abs() <= (depth + 1) * U * tenth * n * one.abs().sum(1)).all())
