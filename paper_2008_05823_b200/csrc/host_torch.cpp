@@ -48,30 +48,30 @@ class GradPlan {
   }
 
   std::tuple<int, Tensor> norm(py::handle tensors, int kind) {
-    auto ptrs = pointers(tensors);
+    const Rows r = pointers(tensors);
     Tensor norms = rows();
-    return {on_stream([&] { return sae_grads_norm(h_, ptrs.data(), kind, norms.data_ptr<float>()); }), norms};
+    return {on_stream([&] { return sae_grads_norm(h_, r.ptrs.data(), kind, norms.data_ptr<float>()); }), norms};
   }
   std::tuple<int, Tensor> clip(py::handle tensors, int kind, float max_norm) {
-    auto ptrs = pointers(tensors);
+    const Rows r = pointers(tensors);
     Tensor norms = rows();
-    return {on_stream([&] { return sae_grads_clip(h_, const_cast<void* const*>(ptrs.data()), kind, max_norm, norms.data_ptr<float>()); }), norms};
+    return {on_stream([&] { return sae_grads_clip(h_, const_cast<void* const*>(r.ptrs.data()), kind, max_norm, norms.data_ptr<float>()); }), norms};
   }
   std::tuple<int, Tensor, std::optional<Tensor>> pack(py::handle tensors, std::optional<Tensor> out, int kind, float max_norm) {
     if (!out) out = fresh({K_, d_}, at::kFloat, device());
     const int64_t stride = vector(*out, "out", false);
-    auto ptrs = pointers(tensors);
+    const Rows r = pointers(tensors);
     std::optional<Tensor> norms;
     if (kind != SAE_NORM_NONE) norms = rows();
     const int rc = on_stream([&] {
-      return sae_grads_pack(h_, ptrs.data(), kind, max_norm, (float*)out->data_ptr(), stride, norms ? norms->data_ptr<float>() : nullptr);
+      return sae_grads_pack(h_, r.ptrs.data(), kind, max_norm, (float*)out->data_ptr(), stride, norms ? norms->data_ptr<float>() : nullptr);
     });
     return {rc, *out, norms};
   }
   int unpack(const Tensor& v, py::handle tensors) {
     const int64_t stride = vector(v, "vector", true);
-    auto ptrs = pointers(tensors);
-    return on_stream([&] { return sae_grads_unpack(h_, (const float*)v.data_ptr(), stride, const_cast<void* const*>(ptrs.data())); });
+    const Rows r = pointers(tensors);
+    return on_stream([&] { return sae_grads_unpack(h_, (const float*)v.data_ptr(), stride, const_cast<void* const*>(r.ptrs.data())); });
   }
 
  private:
@@ -92,9 +92,17 @@ class GradPlan {
     if (type_of(t.scalar_type()) != types_[j] || !t.is_cuda() || t.get_device() != device_) refuse("a tensor's dtype or device is not the set's");
   }
 
-  void row(py::handle tensors, std::vector<const void*>& out) const {
+  // A call's tensors: their addresses, and the sequences that hold them.  A generator's tensors may have no other owner; without
+  // one their memory would be the next allocation's (the norms') before the kernels have read it.
+  struct Rows {
+    std::vector<const void*> ptrs;
+    std::vector<py::object> held;
+  };
+
+  void row(py::handle tensors, Rows& out) const {
     py::object seq = py::reinterpret_steal<py::object>(PySequence_Fast(tensors.ptr(), "a row is a sequence of tensors"));
     if (!seq) throw py::error_already_set();
+    out.held.push_back(seq);
     if (PySequence_Fast_GET_SIZE(seq.ptr()) != T_)
       refuse("a row has " + std::to_string(T_) + " tensors, got " + std::to_string(PySequence_Fast_GET_SIZE(seq.ptr())));
     PyObject** items = PySequence_Fast_ITEMS(seq.ptr());
@@ -109,24 +117,25 @@ class GradPlan {
         for (size_t i = 0; same && i < s.sizes.size(); ++i) same = s.sizes[i] == 1 || t.stride((int64_t)i) == s.strides[i];
         if (!same) refuse("tensors must have the shapes and strides that the set was made like");
       }
-      out.push_back(t.data_ptr());
+      out.ptrs.push_back(t.data_ptr());
     }
   }
 
-  std::vector<const void*> pointers(py::handle tensors) const {
-    std::vector<const void*> out;
-    out.reserve((size_t)K_ * T_);
+  Rows pointers(py::handle tensors) const {
+    Rows out;
+    out.ptrs.reserve((size_t)K_ * T_);
     if (THPVariable_Check(tensors.ptr())) {
       const Tensor& t = THPVariable_Unpack(tensors.ptr());
       if (T_ != 1 || t.dim() != 2 || t.size(0) != K_ || t.size(1) != sizes_[0] || (t.size(1) > 1 && t.stride(1) != 1) ||
           (K_ > 1 && t.stride(0) < t.size(1)))
         refuse("one tensor stands for [num_rows, n] of a set of one tensor, rows without gaps");
       check_type(t, 0);
-      for (int k = 0; k < K_; ++k) out.push_back((const char*)t.data_ptr() + (int64_t)k * t.stride(0) * t.element_size());
+      for (int k = 0; k < K_; ++k) out.ptrs.push_back((const char*)t.data_ptr() + (int64_t)k * t.stride(0) * t.element_size());
       return out;
     }
     py::object seq = py::reinterpret_steal<py::object>(PySequence_Fast(tensors.ptr(), "tensors: a sequence of tensors, or of rows of tensors"));
     if (!seq) throw py::error_already_set();
+    out.held.push_back(seq);
     const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq.ptr());
     PyObject** items = PySequence_Fast_ITEMS(seq.ptr());
     if (K_ == 1 && n > 0 && THPVariable_Check(items[0])) {

@@ -381,3 +381,17 @@ def test_python_refusals():
         grads.GradSet(0, [4])
     with pytest.raises(ValueError):
         grads.GradSet.like([torch.zeros(4, 4, device="cuda")[:, :2]])
+
+
+@pytest.mark.gpu
+def test_tensors_that_only_a_generator_holds():
+    """The tensors of a generator live until the kernels that read them are enqueued: the call's own outputs are not in their place."""
+    sizes, dtypes = [1, 90, 3, 128, 7], [F32, BF16, F32, F32, F16]
+    rows = make(6, sizes, dtypes, 41)
+    s, one = gset(6, sizes, dtypes), gset(1, sizes, dtypes)
+    want, (out, _) = s.norm(rows), s.pack(rows, max_norm=0.5)
+    for _ in range(20):
+        assert torch.equal(s.norm((t * 1 for t in row) for row in rows), want)
+        got, norms = s.pack(((t * 1 for t in row) for row in rows), max_norm=0.5)
+        assert torch.equal(got, out) and torch.equal(norms, want)
+        assert torch.equal(one.norm(t * 1 for t in rows[2]), want[2:3])
