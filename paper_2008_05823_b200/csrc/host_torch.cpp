@@ -48,30 +48,35 @@ class GradPlan {
   }
 
   std::tuple<int, Tensor> norm(py::handle tensors, int kind) {
-    const Rows r = pointers(tensors);
+    const Rows r = pointers(tensors, false);
     Tensor norms = rows();
     return {on_stream([&] { return sae_grads_norm(h_, r.ptrs.data(), kind, norms.data_ptr<float>()); }), norms};
   }
   std::tuple<int, Tensor> clip(py::handle tensors, int kind, float max_norm) {
-    const Rows r = pointers(tensors);
+    const Rows r = pointers(tensors, true);
     Tensor norms = rows();
-    return {on_stream([&] { return sae_grads_clip(h_, const_cast<void* const*>(r.ptrs.data()), kind, max_norm, norms.data_ptr<float>()); }), norms};
+    const int rc = on_stream([&] { return sae_grads_clip(h_, const_cast<void* const*>(r.ptrs.data()), kind, max_norm, norms.data_ptr<float>()); });
+    if (rc == SAE_OK) written(r);
+    return {rc, norms};
   }
   std::tuple<int, Tensor, std::optional<Tensor>> pack(py::handle tensors, std::optional<Tensor> out, int kind, float max_norm) {
     if (!out) out = fresh({K_, d_}, at::kFloat, device());
     const int64_t stride = vector(*out, "out", false);
-    const Rows r = pointers(tensors);
+    const Rows r = pointers(tensors, false);
     std::optional<Tensor> norms;
     if (kind != SAE_NORM_NONE) norms = rows();
     const int rc = on_stream([&] {
       return sae_grads_pack(h_, r.ptrs.data(), kind, max_norm, (float*)out->data_ptr(), stride, norms ? norms->data_ptr<float>() : nullptr);
     });
+    if (rc == SAE_OK) written(*out);
     return {rc, *out, norms};
   }
   int unpack(const Tensor& v, py::handle tensors) {
     const int64_t stride = vector(v, "vector", true);
-    const Rows r = pointers(tensors);
-    return on_stream([&] { return sae_grads_unpack(h_, (const float*)v.data_ptr(), stride, const_cast<void* const*>(r.ptrs.data())); });
+    const Rows r = pointers(tensors, true);
+    const int rc = on_stream([&] { return sae_grads_unpack(h_, (const float*)v.data_ptr(), stride, const_cast<void* const*>(r.ptrs.data())); });
+    if (rc == SAE_OK) written(r);
+    return rc;
   }
 
  private:
@@ -92,20 +97,32 @@ class GradPlan {
     if (type_of(t.scalar_type()) != types_[j] || !t.is_cuda() || t.get_device() != device_) refuse("a tensor's dtype or device is not the set's");
   }
 
-  // A call's tensors: their addresses, and the sequences that hold them.  A generator's tensors may have no other owner; without
-  // one their memory would be the next allocation's (the norms') before the kernels have read it.
+  // A call's tensors: their addresses, the sequences that hold them, and themselves where the call writes them.  A generator's
+  // tensors may have no other owner; without one their memory would be the next allocation's (the norms') before the kernels have read it.
   struct Rows {
     std::vector<const void*> ptrs;
     std::vector<py::object> held;
+    std::vector<const Tensor*> tensors;
   };
 
-  void row(py::handle tensors, Rows& out) const {
+  // What a call has written counts as changed in place: autograd refuses a backward pass that would need the old values.
+  static void written(const Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  }
+  static void written(const Rows& r) {
+    for (const Tensor* t : r.tensors) written(*t);
+  }
+
+  void row(py::handle tensors, Rows& out, bool writes) const {
     py::object seq = py::reinterpret_steal<py::object>(PySequence_Fast(tensors.ptr(), "a row is a sequence of tensors"));
     if (!seq) throw py::error_already_set();
     out.held.push_back(seq);
     if (PySequence_Fast_GET_SIZE(seq.ptr()) != T_)
       refuse("a row has " + std::to_string(T_) + " tensors, got " + std::to_string(PySequence_Fast_GET_SIZE(seq.ptr())));
     PyObject** items = PySequence_Fast_ITEMS(seq.ptr());
+    const size_t at = out.ptrs.size();
+    out.ptrs.resize(at + (size_t)T_);
+    const void** const ptrs = out.ptrs.data() + at;
     for (int j = 0; j < T_; ++j) {
       const Tensor& t = tensor_of(items[j]);
       check_type(t, j);
@@ -117,19 +134,23 @@ class GradPlan {
         for (size_t i = 0; same && i < s.sizes.size(); ++i) same = s.sizes[i] == 1 || t.stride((int64_t)i) == s.strides[i];
         if (!same) refuse("tensors must have the shapes and strides that the set was made like");
       }
-      out.ptrs.push_back(t.data_ptr());
+      ptrs[j] = t.data_ptr();
+      if (writes) out.tensors.push_back(&t);
     }
   }
 
-  Rows pointers(py::handle tensors) const {
+  Rows pointers(py::handle tensors, bool writes) const {
     Rows out;
     out.ptrs.reserve((size_t)K_ * T_);
+    out.held.reserve((size_t)K_ + 1);
+    if (writes) out.tensors.reserve((size_t)K_ * T_);
     if (THPVariable_Check(tensors.ptr())) {
       const Tensor& t = THPVariable_Unpack(tensors.ptr());
       if (T_ != 1 || t.dim() != 2 || t.size(0) != K_ || t.size(1) != sizes_[0] || (t.size(1) > 1 && t.stride(1) != 1) ||
           (K_ > 1 && t.stride(0) < t.size(1)))
         refuse("one tensor stands for [num_rows, n] of a set of one tensor, rows without gaps");
       check_type(t, 0);
+      out.tensors.push_back(&t);
       for (int k = 0; k < K_; ++k) out.ptrs.push_back((const char*)t.data_ptr() + (int64_t)k * t.stride(0) * t.element_size());
       return out;
     }
@@ -139,12 +160,12 @@ class GradPlan {
     const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq.ptr());
     PyObject** items = PySequence_Fast_ITEMS(seq.ptr());
     if (K_ == 1 && n > 0 && THPVariable_Check(items[0])) {
-      row(seq, out);
+      row(seq, out, writes);
     } else {
       if (n != K_) refuse("tensors of " + std::to_string(K_) + " rows are wanted, got " + std::to_string(n));
       for (Py_ssize_t k = 0; k < n; ++k) {
         if (THPVariable_Check(items[k])) refuse("a row is a sequence of tensors");
-        row(items[k], out);
+        row(items[k], out, writes);
       }
     }
     return out;

@@ -41,6 +41,8 @@ class GradSet:
     they lie in memory, the same for parameters and gradients.
 
     `tensors` of a call: T tensors (num_rows = 1) or num_rows lists of T; with T = 1 also one [num_rows, n] tensor.
+    What a call writes (clip_'s and unpack's tensors, pack's out) counts as changed in place: a backward pass that needs the
+    old values raises.  Results take no part in autograd.
     Work is enqueued on the stream the set was made on (or `stream`); a call made while another stream is current
     orders the two, so that tensors of the current stream can be handed over."""
 

@@ -395,3 +395,41 @@ def test_tensors_that_only_a_generator_holds():
         got, norms = s.pack(((t * 1 for t in row) for row in rows), max_norm=0.5)
         assert torch.equal(got, out) and torch.equal(norms, want)
         assert torch.equal(one.norm(t * 1 for t in rows[2]), want[2:3])
+
+
+@pytest.mark.gpu
+def test_autograd_sees_what_is_written():
+    """unpack, clip_ and pack's out change tensors in place: a backward pass that needs what was there before raises, as it does
+    after torch's own in-place operations; what is only read counts as unchanged."""
+    s = gset(1, [12, 4], [F32, F32])
+    vec = torch.randn(16, device="cuda")
+
+    def forward():
+        w = torch.randn(12, device="cuda", requires_grad=True)
+        return w, torch.randn(4, device="cuda"), (w * w).sum()
+
+    w, b, loss = forward()
+    s.norm([w.detach(), b])
+    s.pack([w, b])
+    loss.backward()
+    assert torch.equal(w.grad, 2 * w.detach())
+    for write in (lambda w, b: s.unpack(vec, [w.detach(), b]), lambda w, b: s.clip_([w.detach(), b], 1e-3), lambda w, b: s.unpack(vec, [w, b])):
+        w, b, loss = forward()
+        before = w._version, b._version
+        write(w, b)
+        assert w._version > before[0] and b._version > before[1]
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    leaf = torch.ones(16, device="cuda", requires_grad=True)
+    out = torch.ones(16, device="cuda")
+    loss = (leaf * out).sum()
+    s.pack([w.detach(), b], out)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    buf = torch.ones(3, 5, device="cuda")
+    gset(3, [5], None).clip_(buf, 0.1)
+    assert buf._version == 1
+    with torch.inference_mode():
+        t = torch.ones(12, device="cuda"), torch.ones(4, device="cuda")
+        s.unpack(vec, t)
+    assert torch.equal(torch.cat(t), vec)
