@@ -343,9 +343,10 @@ int64_t sae_noalloc_max_elements(void);
  * out / in: DEVICE; row k starts at element k * stride.  in_stride = 0 gives every row the same vector.
  * SAE_NORM_NONE (sae_grads_pack only, norms NULL): no norm is taken and coef_k = 1.
  *
- * Squares and sums are accumulated in double (groups of eight in float), in a fixed order: the same input gives the
- * same bits, and no finite float row overflows.  As the formula has it, a row whose norm is infinite gets coef_k = 0
- * (its infinities become NaN) and a NaN anywhere makes the norm and the row NaN; sae_sync reports either after the step.
+ * Squares and sums are accumulated in double (groups of eight in float), in a fixed order that does not depend on where the
+ * tensors lie: the same values give the same bits, and no finite float row overflows.  As the formula has it, a row whose
+ * norm is infinite gets coef_k = 0 (its infinities become NaN) and a NaN anywhere makes the norm and the row NaN; sae_sync
+ * reports either after the step.
  * Where coef_k = 1, sae_grads_clip writes nothing.
  * All calls only enqueue kernels on the configuration's stream, allocate nothing, may be captured, and share the
  * handle's scratch: one handle is for one stream and one host thread at a time.

@@ -176,12 +176,13 @@ struct Ring {
   }
 };
 
+// Which eight values are added in float does not depend on the alignment: a tensor that is read in place is taken in the same pieces,
+// element by element, so equal values give equal bits wherever they lie.
 template <int KIND, typename T>
 __device__ __forceinline__ void tile_norm(Running<KIND>& r, const T* p, const unsigned char* image, u32 cnt) {
-  constexpr int V = 16 / (int)sizeof(T), N = GT_TILE / (GT_THREADS * 16);
-  const u32 tid = threadIdx.x;
+  constexpr int V = 16 / (int)sizeof(T), N = GT_TILE / (GT_THREADS * 16), L = 16;
+  const u32 tid = threadIdx.x, whole = cnt / V;
   if ((reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-    const u32 whole = cnt / V;
 #pragma unroll
     for (int i = 0; i < N; i += 8 / V) {
       float v[8];
@@ -195,11 +196,27 @@ __device__ __forceinline__ void tile_norm(Running<KIND>& r, const T* p, const un
       }
       r.eight(v);
     }
-    const u32 e = whole * V + tid;
-    if (e < cnt) r.one(to_f(p[e]));
   } else {
-    for (u32 e = tid; e < cnt; e += GT_THREADS) r.one(to_f(p[e]));
+#pragma unroll 1
+    for (int i = 0; i < N; i += L / V) {
+      T t[L];
+#pragma unroll
+      for (int q = 0; q < L; ++q) {
+        const u32 e = (i + q / V) * GT_THREADS + tid;
+        t[q] = from_f<T>(0.0f);
+        if (e < whole) t[q] = p[e * V + q % V];
+      }
+#pragma unroll
+      for (int h = 0; h < L; h += 8) {
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = to_f(t[h + q]);
+        r.eight(v);
+      }
+    }
   }
+  const u32 e = whole * V + tid;
+  if (e < cnt) r.one(to_f(p[e]));
 }
 
 // blockIdx.y: the row (worker).  The row's tiles are dealt out in runs of neighbours, one run a block.  The block

@@ -433,3 +433,23 @@ def test_autograd_sees_what_is_written():
         t = torch.ones(12, device="cuda"), torch.ones(4, device="cuda")
         s.unpack(vec, t)
     assert torch.equal(torch.cat(t), vec)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("q", [1, 2, math.inf])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_same_bits_at_every_alignment(dtype, q):
+    """Equal values have equal norms wherever they lie: eight are added in float and the rest in double, in one order."""
+    sizes = [5, 30011, 8192, 4099]
+    s = gset(1, sizes, [dtype] * 4)
+    row = make(1, sizes, [dtype] * 4, 12)[0]
+    want = s.norm(row, q)
+    out, _ = s.pack(row, max_norm=0.25, norm_type=q)
+    for offset in range(1, 9):
+        moved = [torch.cat([t[:offset], t])[min(offset, t.numel()):] for t in row]
+        assert torch.equal(s.norm(moved, q), want), offset
+        assert torch.equal(s.pack(moved, max_norm=0.25, norm_type=q)[0], out)
+    # the rows of a buffer whose length is odd against 16 bytes
+    one = torch.randn(16411, device="cuda").to(dtype)
+    norms = gset(9, [16411], dtype).norm(one.repeat(9, 1), q)
+    assert torch.equal(norms, norms[:1].expand(9))
