@@ -344,9 +344,10 @@ int64_t sae_noalloc_max_elements(void);
  * SAE_NORM_NONE (sae_grads_pack only, norms NULL): no norm is taken and coef_k = 1.
  *
  * Squares and sums are accumulated in double (groups of eight in float), in a fixed order that does not depend on where the
- * tensors lie: the same values give the same bits, and no finite float row overflows.  As the formula has it, a row whose
- * norm is infinite gets coef_k = 0 (its infinities become NaN) and a NaN anywhere makes the norm and the row NaN; sae_sync
- * reports either after the step.
+ * tensors lie: the same values give the same bits.  No finite row's sum overflows; a norm beyond the largest float is
+ * reported as infinity, coef_k is taken from it in double all the same.  As the formula has it, a row with an infinity gets
+ * coef_k = 0 (its infinities become NaN) and a NaN anywhere makes the norm and the row NaN; sae_sync reports either after
+ * the step.
  * Where coef_k = 1, sae_grads_clip writes nothing.
  * All calls only enqueue kernels on the configuration's stream, allocate nothing, may be captured, and share the
  * handle's scratch: one handle is for one stream and one host thread at a time.

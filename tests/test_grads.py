@@ -453,3 +453,15 @@ def test_same_bits_at_every_alignment(dtype, q):
     one = torch.randn(16411, device="cuda").to(dtype)
     norms = gset(9, [16411], dtype).norm(one.repeat(9, 1), q)
     assert torch.equal(norms, norms[:1].expand(9))
+
+
+@pytest.mark.gpu
+def test_a_norm_beyond_float_still_scales():
+    """Finite rows whose norm passes the largest float: it is reported as infinity, and the coefficient is right all the same."""
+    n = 20000
+    row = [torch.full((n,), 3e38, device="cuda"), torch.full((9,), -1e30, device="cuda")]
+    s = gset(1, [n, 9], None)
+    flat = flat64(row)
+    out, norms = s.pack(row, max_norm=1e38)
+    assert float(norms[0]) == math.inf
+    assert_scaled(out[0].double().cpu().numpy(), flat, coef64(norm64(flat, 2), 1e38), F32, 2)
