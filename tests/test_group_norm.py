@@ -574,3 +574,36 @@ def test_long_sums_of_one_sign(n, c, pixels):
     assert float((db.double() / (n * pixels * tenth) - 1).abs().max()) <= depth * U
     one = x[0].double()
     assert bool(((dw.double() - tenth * n * one.sum(1)).abs() <= (depth + 1) * U * tenth * n * one.abs().sum(1)).all())
+
+
+# ---- activations over their whole range -------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_activations_over_their_range(act, dtype):
+    """With weight 0, z is the bias.  y is act(z) rounded once: half a unit of the type, and the arithmetic's relative error: 16 u in
+    float32 (and u z^2 from an exponential's argument), 24 u + 4 u z^2 in 16 bits (ex2 and rcp 4 u, the tail's polynomial 8 u, products;
+    the exponent is rounded twice).  gelu in float32 is 1 + erf, whose error (two units of erf, one of its argument) is absolute.
+    dbias sums the slope over 64 pixels: the same error of each of its two terms, and of 64 additions."""
+    from paper_2008_05823_b200 import group_norm as gn
+    c, p = 4096, 64
+    z = np.linspace(-12.0, 12.0, c).astype(np.float32).astype(np.float64)
+    b = torch.tensor(z, dtype=F32, device="cuda")
+    x = torch.randn(1, p, c, device="cuda").to(dtype).movedim(-1, 1)
+    w = torch.zeros(c, device="cuda")
+    y, mean, rstd = gn.group_norm_forward(x, 32, w, b, 1e-5, act)
+    erfc = np.array([math.erfc(-v / math.sqrt(2)) for v in z])
+    cdf = 0.5 * erfc if act == "gelu" else 1 / (1 + np.exp(-z))
+    rel = (16 * U + U * z ** 2) if dtype == F32 else (24 * U + 4 * U * z ** 2)
+    off = 3 * U * np.abs(z) if dtype == F32 and act == "gelu" else 0.0
+    want = z * cdf
+    tol = np.abs(want) * (rel + ROUND[dtype]) * (1 + ROUND[dtype]) + off + TINY[dtype]
+    close(last(y), (np.broadcast_to(want, (1, p, c)), np.broadcast_to(tol, (1, p, c))), "y")
+    ones = torch.ones_like(x)
+    _, _, _, db = gn.group_norm_backward(ones, x, mean, rstd, 32, w, b, act)
+    other = z * np.exp(-z * z / 2) / math.sqrt(2 * math.pi) if act == "gelu" else z * cdf * (1 - cdf)
+    tol = p * ((np.abs(cdf) + np.abs(other)) * (rel + 80 * U) + (3 * U if dtype == F32 and act == "gelu" else 0.0))
+    if act == "silu":
+        tol = tol + p * cdf * np.abs(z) * 8 * U          # 1 - s loses the digits of s
+    close(db, (p * (cdf + other), tol), "dbias")
