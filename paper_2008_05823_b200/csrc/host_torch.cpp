@@ -131,7 +131,7 @@ class GradPlan {
       } else {
         const Shape& s = like_[j];
         bool same = t.sizes() == at::IntArrayRef(s.sizes);
-        for (size_t i = 0; same && i < s.sizes.size(); ++i) same = s.sizes[i] == 1 || t.stride((int64_t)i) == s.strides[i];
+        for (size_t i = 0; same && sizes_[j] && i < s.sizes.size(); ++i) same = s.sizes[i] == 1 || t.stride((int64_t)i) == s.strides[i];
         if (!same) refuse("tensors must have the shapes and strides that the set was made like");
       }
       ptrs[j] = t.data_ptr();

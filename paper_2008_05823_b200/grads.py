@@ -23,6 +23,8 @@ def _norm_kind(norm_type):
 
 def _fills_its_span(t):
     """Whether t's elements lie without gaps or overlap, in whatever order."""
+    if t.numel() == 0:
+        return True
     want = 1
     for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
         if stride != want:

@@ -465,3 +465,18 @@ def test_a_norm_beyond_float_still_scales():
     out, norms = s.pack(row, max_norm=1e38)
     assert float(norms[0]) == math.inf
     assert_scaled(out[0].double().cpu().numpy(), flat, coef64(norm64(flat, 2), 1e38), F32, 2)
+
+
+@pytest.mark.parametrize("shape", [(0,), (4, 0), (0, 4), (3, 0, 5)])
+def test_a_tensor_of_nothing_has_no_gaps(shape):
+    from paper_2008_05823_b200 import grads
+    assert grads._fills_its_span(torch.empty(shape)) and grads._fills_its_span(torch.empty(shape).t() if len(shape) == 2 else torch.empty(shape))
+
+
+@pytest.mark.gpu
+def test_a_set_like_empty_tensors():
+    from paper_2008_05823_b200 import grads
+    w = torch.randn(3, 4, device="cuda")
+    s = grads.GradSet.like([torch.empty(4, 0, device="cuda"), w, torch.empty(2, 0, 3, device="cuda")])
+    out, _ = s.pack([torch.empty(0, 4, device="cuda").t(), w, torch.empty(2, 0, 3, device="cuda")])
+    assert torch.equal(out[0], w.reshape(-1))
