@@ -2,7 +2,8 @@
 
   libsae.so        -- the C-ABI library declared in include/sae.h
   libsae_synth.so  -- the seeded synthetic-gradient generator used by tests and the benchmark
-  _host.so         -- the Python side of gradient sets and group norm (argument checks, allocation), C++ against torch
+  _host.so         -- the Python side of gradient sets and group norm (argument checks, allocation), C++ against torch;
+                      left out where torch is not installed
 
 Usage: python -m paper_2008_05823_b200.build [--force] [--verbose]
 """
@@ -55,7 +56,12 @@ def build(force: bool = False, verbose: bool = False):
         if force or _stale(out, dep_paths):
             extra = os.environ.get("SAE_NVCC_EXTRA", "").split()
             if src_paths[0].endswith(".cpp"):
-                subprocess.check_call(_host_command(out, src_paths))
+                try:
+                    cmd = _host_command(out, src_paths)
+                except ImportError:
+                    print(f"{name} is not built: torch is not installed", file=sys.stderr)
+                    continue
+                subprocess.check_call(cmd)
                 outs.append(out)
                 continue
             cmd = [nvcc] + NVCC_FLAGS + extra + (["-Xptxas", "-v"] if verbose else []) + ["-o", out] + src_paths
