@@ -33,6 +33,13 @@ def _fills_its_span(t):
     return True
 
 
+class _Closed:
+    """What a set has in place of its plan when it is closed: every call is refused."""
+
+    def __getattr__(self, name):
+        raise SaeError(binding.ERR_INVALID_ARG, f"{name} of a closed gradient set")
+
+
 class GradSet:
     """The plan of one parameter list: `num_rows` workers' gradients (or parameters) of T tensors each.
 
@@ -49,7 +56,7 @@ class GradSet:
     orders the two, so that tensors of the current stream can be handed over."""
 
     def __init__(self, num_rows, tensor_sizes, dtypes=None, device=None, stream=None, _like=None):
-        self.h = None
+        self.h, self._plan = None, _Closed()
         sizes = np.ascontiguousarray(tensor_sizes, dtype=np.int64)
         self.K, self.T = int(num_rows), len(sizes)
         self.sizes = sizes.tolist()
@@ -89,7 +96,7 @@ class GradSet:
 
     def close(self):
         if self.h:
-            self._plan = None
+            self._plan = _Closed()
             binding.lib().sae_grads_destroy(self.h)
             self.h = None
 

@@ -480,3 +480,14 @@ def test_a_set_like_empty_tensors():
     s = grads.GradSet.like([torch.empty(4, 0, device="cuda"), w, torch.empty(2, 0, 3, device="cuda")])
     out, _ = s.pack([torch.empty(0, 4, device="cuda").t(), w, torch.empty(2, 0, 3, device="cuda")])
     assert torch.equal(out[0], w.reshape(-1))
+
+
+@pytest.mark.gpu
+def test_a_closed_set_refuses():
+    row = make(1, [8], [F32], 1)[0]
+    s = gset(1, [8], None)
+    s.close()
+    s.close()
+    for call in (lambda: s.norm(row), lambda: s.clip_(row, 1.0), lambda: s.pack(row), lambda: s.unpack(torch.zeros(8, device="cuda"), row)):
+        with pytest.raises(sb.SaeError):
+            call()
