@@ -401,8 +401,9 @@ void sae_grads_destroy(sae_grads *h);
  *   values of type `param_type`; weight NULL = 1, bias NULL = 0.  residual NULL = none; dresidual, dweight, dbias NULL = not wanted.
  * mean, rstd: [samples][groups] floats, written by the forward call, read by the backward call.
  * workspace: at least sae_group_norm_workspace(desc, ..) bytes, 16-byte aligned, the call's own until it has run.
- * Arithmetic, statistics and sums are in float, one rounding to `type` at each output; z is the same bits
- * in both directions, so relu's mask (z > 0) is the forward call's.  The sums' order is fixed: same input, same bits.
+ * Arithmetic, statistics and sums are in float (dweight and dbias: over a sample's pixels; the samples are added in double), one
+ * rounding to `type` at each output.  x - mean, * rstd, * weight, + bias and + residual are rounded one by one, so z is the same
+ * bits in both directions and relu's mask (z > 0) is the forward call's.  The sums' order is fixed: same input, same bits.
  * samples or pixels = 0: mean and rstd are NaN (0 / 0), dweight and dbias 0.
  * Errors: SAE_ERR_INVALID_ARG for a null or misaligned pointer, groups that do not divide channels, a size out of range
  * (samples <= 2^24, pixels <= 2^30, channels <= 2^20, samples * groups < 2^31), a workspace too small; SAE_ERR_CUDA.

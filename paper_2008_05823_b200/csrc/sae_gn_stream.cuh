@@ -277,7 +277,7 @@ __device__ __forceinline__ float2* run_out(const Args& a, const Stream& s, const
 // ---- forward ------------------------------------------------------------------------------------------------------
 // A thread sums x - k and its square over at most 32 vectors, k being the first one's value (WHOLE: mean), then joins count, mean
 // and squares to what came before (Chan, Golub and LeVeque's update).
-// Bound by HBM and, below 100 MB, by its start and end: 51 MB of bf16 in 14 us, 7 of them before and after the loads flow.
+// Bound by HBM and, below 100 MB, by its start and end: 51 MB of bf16 in 15 us, 7 of them before and after the loads flow.
 template <typename T, int V, bool WHOLE>
 __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_statistics(const Args a, const Stream st) {
   extern __shared__ __align__(16) unsigned char smem[];
@@ -426,7 +426,8 @@ __device__ __forceinline__ int act_of(const Args& a) { return ACT == 2 ? a.act :
 __host__ __device__ constexpr int sums_kept(int vec) { return 2 * vec * (int)sizeof(float); }
 
 // Each channel's sum dz and sum dz * xhat over a run, dresidual = dz on the way.  Bound by HBM: 32x56x56x256 bf16, relu with a
-// residual, 206 MB in 36.7 us (5.6 TB/s); silu and gelu by the special-function unit (two operations an element).
+// residual, 206 MB in 36.7 us (5.6 TB/s); silu and gelu by the special-function unit (two operations an element):
+// without a residual 103 MB in 32.5 and 39 us.
 template <typename T, int V, bool WHOLE, int ACT, bool RES>
 __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_sums(const Args a, const Stream st) {
   extern __shared__ __align__(16) unsigned char smem[];

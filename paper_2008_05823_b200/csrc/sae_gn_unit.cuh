@@ -69,8 +69,8 @@ __device__ __forceinline__ Spot spot(const Args& a, const Unit& u) {
 // Statistics in one pass: a thread sums x - k and its square, k being its own first value (WHOLE: its first vector's mean).
 // As k is one of the values, (mean - k)^2 is at most their squares' sum about the mean, so taking the squares about the mean
 // from those about k loses at most the thread's count of values, in units of rounding: no large mean cancels.
-// Bound by latency (load, reduce, store in turns; two or three blocks an SM overlap them in part): 128x32x32x16 float, 17 MB
-// in 6.8 us; 32x14x14x1024 bf16 with a residual, 39 MB in 11.5.
+// Bound by latency (load, reduce, store in turns; two or three blocks an SM overlap them in part), inputs in L2: 128x32x32x16
+// float, 17 MB in 6.8 us; 16x14x14x1024 bf16 with a residual, 19 MB in 6.8.
 template <typename T, int V, bool WHOLE>
 __global__ void __launch_bounds__(GN_THREADS, 3) k_gn_unit(const Args a, const Unit u) {
   extern __shared__ __align__(16) unsigned char smem[];
@@ -238,7 +238,7 @@ __device__ __forceinline__ void held(const typename Raw<T, V>::B* lo, const type
 
 // After the first pass a thread's dz stays in its slots: a 16-bit dz that rounding does not change (relu's, none's) in dy's
 // place, else in float, which for 16-bit types takes a second slot (the residual's, if there is one).
-// Bound by latency as the forward kernel: 128x32x32x16 float, 25 MB in 8.2 us.
+// Bound by latency as the forward kernel: 128x32x32x16 float, 25 MB in 8.0 us; 16x14x14x1024 bf16 with a residual, 32 MB in 10.
 template <typename T, int V, bool WHOLE>
 __global__ void __launch_bounds__(GN_THREADS, WHOLE ? 3 : 2) k_gn_grad_unit(const Args a, const Unit u) {
   extern __shared__ __align__(16) unsigned char smem[];

@@ -69,13 +69,18 @@ Width vector_width(const sae_group_norm_desc* d, const void* const* ptrs, int n,
 constexpr int SMEM_MOST = 113 * 1024;     // no kernel here takes more: two blocks an SM at least
 constexpr int SMEM_THIRD = 72 * 1024;    // three blocks an SM
 // One pass or two: the unit kernels read everything once but load, reduce and store in turns (2.4 to 3.3 TB/s); the streaming
-// kernels are two launches, and read once from HBM and once from L2 (4.2 to 5 TB/s).  Measured forwards / backwards, one pass
-// against two: 128x32x32x16 float (17, 25 MB of traffic) 8.5 / 14.8 us against 13 / 14; 32x14x14x1024 bf16 with a residual
-// (39, 64 MB) 13.5 / 22.9 against 14.6 / 24.5; 32x56x56x256 bf16 with a residual (154, 257 MB) 47 / 92 against 34 / 61.
+// kernels are two launches, and read once from HBM and once from L2 (4.2 to 5 TB/s).  Both were measured over 92 calls forwards and
+// 88 backwards of 2 to 160 MB of traffic, 7x7 to 128x128 pixels, 16 to 2048 channels, bfloat16 and float.  Below 32 MB one pass wins
+// almost everywhere: 128x32x32x16 float (16 and 24 MB) 8.3 / 14.3 us against 10.3 / 18.4 forwards / backwards, 16x14x14x1024 bf16
+// with a residual (18 and 31 MB) 8.3 / 14.4 against 12.4 / 18.9.  Above it two passes win where a unit takes a whole
+// cluster: 16x56x56x256 bf16 with a residual (74 and 123 MB) 28.8 / 57.3 against 20.6 / 34.0; one pass still wins where a unit is small
+// (512x32x32x16 bf16 with a residual, 48 and 80 MB: 18.5 / 31.5 against 26.7 / 47.2).  Against the better form of each call the rule loses 2.6 % of
+// the time forwards and 3.7 % backwards, the best single number of each direction 2.4 % (64 and 48 MB).
 constexpr long long UNIT_TRAFFIC = 32ll << 20;
-// With vectors of less than 16 bytes a unit's threads hold little each: 8x100x100x35 bf16 (11 and 17 MB) 23.8 / 46.5 us in one
-// pass, 16.6 / 16.7 in two, which have whole vectors over rows of pixels; 14x54x55x72 bf16 of 109 channels (12 and 18 MB),
-// which have not, 28.8 / 25.3 against 19.4 / 22.7.
+// With vectors of less than 16 bytes a unit's threads hold little each; two passes have whole vectors over rows of pixels where those
+// have no gaps.  Over 57 such calls: 8x33x47x90 bf16 (4.3 and 6.4 MB) 8.3 / 12.1 us in one pass, 12.4 / 14.4 in two; 10x60x60x111
+// bf16 (15 and 23 MB) 27.4 / 38.6 against 16.4 / 18.5.  The number is a compromise: 35 channels are better off in two passes
+// from 1 MB on (22.6 / 28.8 against 14 / 12.4), 512 samples of 8x8x30 in one (10.3 / 18.5 against 26.7 / 24.6).
 constexpr long long NARROW_TRAFFIC = 4ll << 20;
 
 // One pass over a unit of `seg` bytes a pixel or a little less (whole groups, whole vectors), in clusters of up to `most` blocks
