@@ -435,6 +435,102 @@ int sae_group_norm_backward(const sae_group_norm_desc *desc, const void *dy, con
                             void *dresidual, void *dweight, void *dbias, void *workspace, size_t workspace_bytes,
                             void *stream);
 
+/*
+ * Linear cross entropy.  (Where a worker's stochastic gradient begins: the loss of a linear output layer over its classes, the
+ * logits of which would be the largest tensor of the training step.  They are never stored.)
+ *
+ *   z_ij = x_i . w_j + bias_j;  lse_i = log(sum_j exp(z_ij));  loss_i = lse_i - z_i,target(i)
+ *   p_ij = (exp(z_ij - lse_i) - [j = target(i)]) * g_i;  dx_i = sum_j p_ij w_j;  dw_j = sum_i p_ij x_i;  dbias_j = sum_i p_ij
+ *
+ * A row whose target is ignore_index takes no part: its loss, lse and dx are 0, its x may hold anything, and it costs nothing.
+ * Any other target outside 0 .. classes - 1 makes the row's loss NaN, and dx of the row, dw and dbias NaN.
+ * loss: SAE_REDUCE_NONE: `rows` floats; SAE_REDUCE_SUM, SAE_REDUCE_MEAN: one, the sum over the rows that take part or the
+ *   sum over their number (none: 0 / 0 = NaN).  lse: `rows` floats.  count: one int64, the number of rows that take part.
+ * dloss: SAE_REDUCE_NONE: `rows` floats; otherwise one.  g_i = dloss_i, dloss, or dloss / count.
+ * lse and count are read by the backward call as the forward call of the same inputs left them.
+ *
+ * All pointers are DEVICE pointers, all work goes to `stream` of the CURRENT device and is asynchronous; nothing is allocated
+ * and nothing is kept between calls, which may be captured.
+ * x: row i at i * x_pitch; weight: row j at j * weight_pitch (elements, at least `features` where there is more than one row), both of
+ *   type `type`; bias: `classes` values of type `bias_type` without gaps, NULL = none; target: `rows` int64 without gaps.
+ * dx [rows][features] and dweight [classes][features]: type `type`; dbias: type `bias_type`; all without gaps, NULL = not wanted, not
+ *   overlapping any input.
+ * workspace: at least sae_linear_ce_workspace(desc, ..) bytes, 256-byte aligned, the call's own until it has run.
+ *
+ * Arithmetic: 16-bit tensors are multiplied as they are, sums and everything about the softmax are float.  The backward call makes z
+ * again and holds p in pieces of the classes, rounded once to `type` (half a unit of that type for each p, which averages out in dx and
+ * dweight; a float16 p is scaled so that it does not vanish).  Float tensors are multiplied as three bfloat16 parts each, with about the
+ * error of float products.  The order of sums is fixed: same input, same bits.
+ * A bias of -inf takes a class out.  A row whose logits are all -inf, or that holds an infinity or a NaN, has a NaN loss.
+ * Errors: SAE_ERR_INVALID_ARG for a null or misaligned pointer, a size out of range (0 <= rows <= 2^24, 1 <= features <= 2^17,
+ *   1 <= classes <= 2^24), a workspace too small; SAE_ERR_CUDA.
+ */
+#define SAE_REDUCE_NONE 0
+#define SAE_REDUCE_SUM 1
+#define SAE_REDUCE_MEAN 2
+
+typedef struct {
+  int32_t type, bias_type;         /* SAE_TYPE_*                                                              */
+  int32_t reduction;               /* SAE_REDUCE_*                                                            */
+  int32_t has_bias;
+  int64_t rows, features, classes;
+  int64_t x_pitch, weight_pitch;   /* elements                                                                */
+  int64_t ignore_index;
+} sae_linear_ce_desc;
+
+/* Bytes of workspace the forward (backward = 0) or backward call needs on the current device, with these weights (their alignment counts,
+ * nothing is read); -1 for a bad description or without a device. */
+int64_t sae_linear_ce_workspace(const sae_linear_ce_desc *desc, const void *weight, int32_t backward);
+int sae_linear_ce_forward(const sae_linear_ce_desc *desc, const void *x, const void *weight, const void *bias,
+                          const int64_t *target, float *loss, float *lse, int64_t *count, void *workspace,
+                          size_t workspace_bytes, void *stream);
+int sae_linear_ce_backward(const sae_linear_ce_desc *desc, const float *dloss, const void *x, const void *weight,
+                           const void *bias, const int64_t *target, const float *lse, const int64_t *count, void *dx,
+                           void *dweight, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Orthogonalisation of many matrices.  (What a worker may do to its momentum or its model difference before it is compressed:
+ * every matrix of a model is replaced by one with the same singular vectors and singular values near 1.)
+ *
+ *   x = g / (|g| + eps), |g| the square root of the sum of squares;  then, for every step i:
+ *   x <- a_i x + b_i (x x') x + c_i (x x')^2 x
+ *
+ * A sae_ortho holds the shapes, the tables and the workspace (about 8 bytes an element and 8 more for each element of the square
+ * products) of one list of matrices: `num_rows` workers' lists of `num_matrices` each.
+ * matrices, results: HOST arrays of num_rows * num_matrices DEVICE pointers, row k's at [k * num_matrices .. ); read before the call
+ *   returns.  Matrix j is rows[j] x cols[j] of type types[j], neighbouring columns next to each other, its rows pitches[..] elements
+ *   apart (HOST, as the pointers; NULL: without gaps); its result is of type result_types[j].  A result may be its own
+ *   matrix; it must not overlap another.  An empty matrix may be NULL.
+ * Norms are taken in double.  x is held in 22 bits.  Products for a float or float16 result take all of them, which is about the error of float
+ *   products; for a bfloat16 result 11 bits of each operand, which is an error of about 2e-3 of the result's norm, that of its own rounding.
+ * A zero matrix stays zero (eps = 0: NaN); one with an infinity or a NaN becomes NaN.
+ * Coefficients that let a singular value grow beyond 16, or |b s + c s^2| beyond 4096, are refused.
+ * sae_ortho_run only enqueues kernels on the configuration's stream, allocates nothing, may be captured, and uses the handle's
+ *   workspace: one handle is for one stream and one host thread at a time.
+ * Returns SAE_OK or a sae_status; sae_ortho_last_cuda_error as sae_last_cuda_error (NULL: of the last sae_ortho_init).
+ */
+typedef struct sae_ortho sae_ortho; /* opaque, library-owned */
+
+typedef struct {
+  uint32_t abi_version;         /* must be SAE_ABI_VERSION                                                 */
+  int32_t num_rows;             /* 1..1024; num_rows * num_matrices <= 2^20                                */
+  int32_t num_matrices;         /* >= 1                                                                    */
+  const int64_t *rows, *cols;   /* HOST, num_matrices entries, 0..2^20, rows * cols <= 2^30; copied        */
+  const int32_t *types;         /* HOST, SAE_TYPE_* codes, copied; NULL = all SAE_TYPE_FLOAT               */
+  const int32_t *result_types;  /* HOST, copied; NULL = types                                              */
+  int32_t steps;                /* 1..64                                                                   */
+  const float *coefficients;    /* HOST, a, b, c of every step, copied                                     */
+  float eps;                    /* >= 0                                                                    */
+  int32_t device;               /* CUDA device ordinal                                                     */
+  void *stream;                 /* cudaStream_t (NULL = default stream)                                    */
+} sae_ortho_config;
+
+int sae_ortho_init(const sae_ortho_config *cfg, sae_ortho **out);
+int sae_ortho_run(sae_ortho *h, const void *const *matrices, const int64_t *pitches, void *const *results,
+                  const int64_t *result_pitches);
+int sae_ortho_last_cuda_error(const sae_ortho *h);
+void sae_ortho_destroy(sae_ortho *h);
+
 #ifdef __cplusplus
 }
 #endif

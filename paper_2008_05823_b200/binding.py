@@ -29,11 +29,13 @@ EXPORTS = ["sae_init", "sae_step", "sae_step_host", "sae_get_params", "sae_get_p
            "sae_num_padded", "sae_avg_local_sum", "sae_avg_set", "sae_set_local_steps",
            "sae_grads_init", "sae_grads_norm", "sae_grads_clip", "sae_grads_pack", "sae_grads_unpack",
            "sae_grads_last_cuda_error", "sae_grads_destroy", "sae_group_norm_workspace", "sae_group_norm_forward",
-           "sae_group_norm_backward"]
+           "sae_group_norm_backward", "sae_linear_ce_workspace", "sae_linear_ce_forward", "sae_linear_ce_backward",
+           "sae_ortho_init", "sae_ortho_run", "sae_ortho_last_cuda_error", "sae_ortho_destroy"]
 
 TYPE_FLOAT, TYPE_BFLOAT, TYPE_HALF = 0, 1, 2
 NORM_NONE, NORM_ONE, NORM_TWO, NORM_MAX = 0, 1, 2, 3
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
+REDUCE_NONE, REDUCE_SUM, REDUCE_MEAN = 0, 1, 2
 
 SHARD_BLOB_BYTES = 1024
 
@@ -56,6 +58,19 @@ class SaeGroupNormDesc(C.Structure):
                 ("samples", C.c_int64), ("pixels", C.c_int64), ("channels", C.c_int64), ("x_sample", C.c_int64),
                 ("x_pixel", C.c_int64), ("residual_sample", C.c_int64), ("residual_pixel", C.c_int64),
                 ("dy_sample", C.c_int64), ("dy_pixel", C.c_int64), ("eps", C.c_float)]
+
+
+class SaeLinearCeDesc(C.Structure):
+    _fields_ = [("type", C.c_int32), ("bias_type", C.c_int32), ("reduction", C.c_int32), ("has_bias", C.c_int32),
+                ("rows", C.c_int64), ("features", C.c_int64), ("classes", C.c_int64), ("x_pitch", C.c_int64),
+                ("weight_pitch", C.c_int64), ("ignore_index", C.c_int64)]
+
+
+class SaeOrthoConfig(C.Structure):
+    _fields_ = [("abi_version", C.c_uint32), ("num_rows", C.c_int32), ("num_matrices", C.c_int32),
+                ("rows", C.POINTER(C.c_int64)), ("cols", C.POINTER(C.c_int64)), ("types", C.POINTER(C.c_int32)),
+                ("result_types", C.POINTER(C.c_int32)), ("steps", C.c_int32), ("coefficients", C.POINTER(C.c_float)),
+                ("eps", C.c_float), ("device", C.c_int32), ("stream", C.c_void_p)]
 
 
 class SaeError(RuntimeError):
@@ -128,6 +143,15 @@ def lib():
         L.sae_grads_last_cuda_error.argtypes = [vp]
         L.sae_grads_destroy.argtypes = [vp]
         L.sae_grads_destroy.restype = None
+        L.sae_linear_ce_workspace.argtypes = [C.POINTER(SaeLinearCeDesc), vp, i32]
+        L.sae_linear_ce_workspace.restype = i64
+        L.sae_linear_ce_forward.argtypes = [C.POINTER(SaeLinearCeDesc)] + [vp] * 8 + [C.c_size_t, vp]
+        L.sae_linear_ce_backward.argtypes = [C.POINTER(SaeLinearCeDesc)] + [vp] * 11 + [C.c_size_t, vp]
+        L.sae_ortho_init.argtypes = [C.POINTER(SaeOrthoConfig), C.POINTER(vp)]
+        L.sae_ortho_run.argtypes = [vp] * 5
+        L.sae_ortho_last_cuda_error.argtypes = [vp]
+        L.sae_ortho_destroy.argtypes = [vp]
+        L.sae_ortho_destroy.restype = None
         L.sae_group_norm_workspace.argtypes = [C.POINTER(SaeGroupNormDesc), i32]
         L.sae_group_norm_workspace.restype = i64
         L.sae_group_norm_forward.argtypes = [C.POINTER(SaeGroupNormDesc)] + [vp] * 8 + [C.c_size_t, vp]
@@ -140,7 +164,7 @@ _host = None
 
 
 def host():
-    """The C++ side of `grads` and `group_norm` (argument checks and allocation against torch), built beside libsae.so."""
+    """The C++ side of `grads`, `group_norm`, `cross_entropy` and `orthogonal` (argument checks and allocation against torch), built beside libsae.so."""
     global _host
     if _host is None:
         lib()

@@ -1,4 +1,4 @@
-// What the Python side of the gradient sets and of group norm does per call, in C++: reading tensors (pointers, types,
+// What the Python side of the gradient sets, of orthogonalisation, of group norm and of the linear cross entropy does per call, in C++: reading tensors (pointers, types,
 // strides), refusing what does not fit, allocating outputs and calling the entry points of include/sae.h.  A model has
 // hundreds of gradient tensors, and looking at four properties of each in Python took 0.25 us a tensor, more than the kernels.
 // No arithmetic happens here.
@@ -10,6 +10,7 @@
 #include <cuda_runtime_api.h>
 #include <torch/extension.h>
 
+#include <algorithm>
 #include <cstring>
 #include <vector>
 
@@ -32,6 +33,27 @@ Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, at::Device device) {
 const Tensor& tensor_of(PyObject* o) {
   if (!THPVariable_Check(o)) refuse("tensors are wanted");
   return THPVariable_Unpack(o);
+}
+
+// A handle's work is on its own stream.  Where another is current, the two are ordered both ways, so that the call may
+// read what the current stream has made and the current stream may use what it gives.
+template <typename F>
+int ordered(int device, cudaStream_t stream, F call) {
+  cudaStream_t current = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device).stream();
+  if (current == stream) return call();
+  c10::cuda::CUDAGuard guard((c10::DeviceIndex)device);
+  cudaEvent_t e = nullptr;
+  if (cudaEventCreateWithFlags(&e, cudaEventDisableTiming) != cudaSuccess) return SAE_ERR_CUDA;
+  int rc = cudaEventRecord(e, current) == cudaSuccess && cudaStreamWaitEvent(stream, e, 0) == cudaSuccess ? SAE_OK : SAE_ERR_CUDA;
+  if (rc == SAE_OK) rc = call();
+  const bool back = cudaEventRecord(e, stream) == cudaSuccess && cudaStreamWaitEvent(current, e, 0) == cudaSuccess;
+  cudaEventDestroy(e);
+  return rc == SAE_OK && !back ? SAE_ERR_CUDA : rc;
+}
+
+// What a call has written counts as changed in place: autograd refuses a backward pass that would need the old values.
+void changed(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 
 // ---- gradient sets ----------------------------------------------------------------------------------------------------
@@ -105,10 +127,7 @@ class GradPlan {
     std::vector<const Tensor*> tensors;
   };
 
-  // What a call has written counts as changed in place: autograd refuses a backward pass that would need the old values.
-  static void written(const Tensor& t) {
-    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
-  }
+  static void written(const Tensor& t) { changed(t); }
   static void written(const Rows& r) {
     for (const Tensor* t : r.tensors) written(*t);
   }
@@ -171,21 +190,8 @@ class GradPlan {
     return out;
   }
 
-  // The set's work is on its own stream.  Where another is current, the two are ordered both ways, so that the call may
-  // read what the current stream has made and the current stream may use what it gives.
   template <typename F>
-  int on_stream(F call) const {
-    cudaStream_t current = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)device_).stream();
-    if (current == stream_) return call();
-    c10::cuda::CUDAGuard guard((c10::DeviceIndex)device_);
-    cudaEvent_t e = nullptr;
-    if (cudaEventCreateWithFlags(&e, cudaEventDisableTiming) != cudaSuccess) return SAE_ERR_CUDA;
-    int rc = cudaEventRecord(e, current) == cudaSuccess && cudaStreamWaitEvent(stream_, e, 0) == cudaSuccess ? SAE_OK : SAE_ERR_CUDA;
-    if (rc == SAE_OK) rc = call();
-    const bool back = cudaEventRecord(e, stream_) == cudaSuccess && cudaStreamWaitEvent(current, e, 0) == cudaSuccess;
-    cudaEventDestroy(e);
-    return rc == SAE_OK && !back ? SAE_ERR_CUDA : rc;
-  }
+  int on_stream(F call) const { return ordered(device_, stream_, call); }
 
   sae_grads* h_;
   int K_, T_;
@@ -195,6 +201,115 @@ class GradPlan {
   std::vector<int64_t> sizes_;
   std::vector<int> types_;
   std::vector<Shape> like_;
+};
+
+// ---- orthogonalisation --------------------------------------------------------------------------------------------------
+// A list of matrices: tensors of two dimensions or more, [first, all others].
+class OrthoPlan {
+ public:
+  OrthoPlan(int64_t handle, int K, std::vector<std::vector<int64_t>> shapes, std::vector<int> types, std::vector<int> result_types, int device, int64_t stream)
+      : h_(reinterpret_cast<sae_ortho*>(handle)), K_(K), T_((int)shapes.size()), device_(device), stream_(reinterpret_cast<cudaStream_t>(stream)),
+        shapes_(std::move(shapes)), types_(std::move(types)), result_types_(std::move(result_types)) {}
+
+  // (status, results): results is the given sequence, or a new one of the same form
+  std::tuple<int, py::object> run(py::handle matrices, py::object results) {
+    const size_t n = (size_t)K_ * T_;
+    std::vector<py::object> held;
+    std::vector<const Tensor*> in = tensors(matrices, held), out;
+    std::vector<Tensor> made;
+    for (size_t i = 0; i < n; ++i) check(*in[i], (int)(i % T_), types_[i % T_], "a matrix");
+    if (results.is_none()) {
+      made.reserve(n);
+      for (size_t i = 0; i < n; ++i) made.push_back(like(*in[i], result_types_[i % T_]));
+      for (Tensor& t : made) out.push_back(&t);
+      py::list rows;
+      for (int k = 0; k < K_; ++k) {
+        py::list row;
+        for (int j = 0; j < T_; ++j) row.append(py::cast(made[(size_t)k * T_ + j]));
+        rows.append(row);
+      }
+      results = K_ == 1 && flat_ ? py::object(rows[0]) : py::object(rows);
+    } else out = tensors(results, held);
+    std::vector<const void*> from(n);
+    std::vector<void*> to(n);
+    std::vector<int64_t> pitch(n), result_pitch(n);
+    for (size_t i = 0; i < n; ++i) {
+      const int j = (int)(i % T_);
+      check(*out[i], j, result_types_[j], "a result");
+      for (int64_t d = 1; d < in[i]->dim(); ++d)
+        if (in[i]->size(d) != 1 && in[i]->numel() && in[i]->stride(d) != out[i]->stride(d)) refuse("a matrix and its result must have their columns in the same order");
+      from[i] = in[i]->data_ptr();
+      to[i] = out[i]->data_ptr();
+      pitch[i] = pitch_of(*in[i]);
+      result_pitch[i] = pitch_of(*out[i]);
+    }
+    const int rc = ordered(device_, stream_, [&] { return sae_ortho_run(h_, from.data(), pitch.data(), to.data(), result_pitch.data()); });
+    if (rc == SAE_OK) for (const Tensor* t : out) changed(*t);
+    return {rc, results};
+  }
+
+ private:
+  static int64_t columns(const Tensor& t) {
+    int64_t n = 1;
+    for (int64_t d = 1; d < t.dim(); ++d) n *= t.size(d);
+    return n;
+  }
+  // Elements from a row to the next; refuses what is no matrix with neighbouring columns.
+  static int64_t pitch_of(const Tensor& t) {
+    const int64_t n = columns(t);
+    if (t.numel() == 0) return n;
+    c10::SmallVector<std::pair<int64_t, int64_t>, 6> dims;
+    for (int64_t d = 1; d < t.dim(); ++d) if (t.size(d) != 1) dims.push_back({t.stride(d), t.size(d)});
+    std::sort(dims.begin(), dims.end());
+    int64_t want = 1;
+    for (auto& d : dims) { if (d.first != want) refuse("a matrix has its columns next to each other"); want *= d.second; }
+    if (t.size(0) > 1 && t.stride(0) < n) refuse("a matrix has its rows one after another, without overlap");
+    return t.size(0) > 1 ? t.stride(0) : n;
+  }
+  Tensor like(const Tensor& t, int type) const {
+    c10::SmallVector<int64_t, 6> st(t.strides().begin(), t.strides().end());
+    st[0] = std::max<int64_t>(1, columns(t));
+    return at::detail::empty_strided_cuda(t.sizes(), st, type == SAE_TYPE_FLOAT ? at::kFloat : type == SAE_TYPE_BFLOAT ? at::kBFloat16 : at::kHalf, t.device());
+  }
+  void check(const Tensor& t, int j, int type, const char* what) const {
+    if (type_of(t.scalar_type()) != type || !t.is_cuda() || t.get_device() != device_) refuse(std::string(what) + "'s dtype or device is not the plan's");
+    if (t.sizes() != at::IntArrayRef(shapes_[j])) refuse(std::string(what) + " must have the plan's shape");
+  }
+  std::vector<const Tensor*> tensors(py::handle rows, std::vector<py::object>& held) {
+    std::vector<const Tensor*> out;
+    out.reserve((size_t)K_ * T_);
+    if (THPVariable_Check(rows.ptr())) refuse("matrices: a sequence of tensors, or of rows of tensors");
+    py::object seq = sequence(rows, held);
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq.ptr());
+    PyObject** items = PySequence_Fast_ITEMS(seq.ptr());
+    flat_ = K_ == 1 && n > 0 && THPVariable_Check(items[0]);
+    if (flat_) row(seq, out);
+    else {
+      if (n != K_) refuse("matrices of " + std::to_string(K_) + " rows are wanted, got " + std::to_string(n));
+      for (Py_ssize_t k = 0; k < n; ++k) {
+        if (THPVariable_Check(items[k])) refuse("a row is a sequence of tensors");
+        row(sequence(items[k], held), out);
+      }
+    }
+    return out;
+  }
+  static py::object sequence(py::handle o, std::vector<py::object>& held) {
+    py::object seq = py::reinterpret_steal<py::object>(PySequence_Fast(o.ptr(), "matrices: a sequence of tensors, or of rows of tensors"));
+    if (!seq) throw py::error_already_set();
+    held.push_back(seq);
+    return seq;
+  }
+  void row(const py::object& seq, std::vector<const Tensor*>& out) const {
+    if (PySequence_Fast_GET_SIZE(seq.ptr()) != T_) refuse("a row has " + std::to_string(T_) + " matrices, got " + std::to_string(PySequence_Fast_GET_SIZE(seq.ptr())));
+    for (int j = 0; j < T_; ++j) out.push_back(&tensor_of(PySequence_Fast_ITEMS(seq.ptr())[j]));
+  }
+
+  sae_ortho* h_;
+  int K_, T_, device_;
+  cudaStream_t stream_;
+  std::vector<std::vector<int64_t>> shapes_;
+  std::vector<int> types_, result_types_;
+  bool flat_ = false;
 };
 
 // ---- group norm -----------------------------------------------------------------------------------------------------------
@@ -314,6 +429,85 @@ std::tuple<int, Tensor, Maybe, Maybe, Maybe> group_norm_backward(const Tensor& d
   return {rc, dx, dres, dweight, dbias};
 }
 
+// ---- linear cross entropy ---------------------------------------------------------------------------------------------------
+// x as [rows, features] with neighbouring features, copied where no such view is there.
+Tensor as_rows(const Tensor& x) {
+  const int64_t d = x.size(-1);
+  Tensor v = x.dim() == 2 ? x : x.reshape({x.numel() / std::max<int64_t>(1, d), d});
+  if ((d > 1 && v.stride(1) != 1) || (v.size(0) > 1 && v.stride(0) < d)) v = v.contiguous();
+  return v;
+}
+
+struct LinearCe {
+  Tensor x, weight, target;
+  sae_linear_ce_desc d;
+};
+
+LinearCe describe_ce(const Tensor& x, const Tensor& weight, const Tensor& target, const Maybe& bias, int64_t ignore, int reduction) {
+  if (!x.is_cuda() || type_of(x.scalar_type()) < 0 || x.dim() < 1 || x.size(-1) < 1) refuse("x must be a float32, bfloat16 or float16 CUDA tensor [..., features]");
+  if (weight.dim() != 2 || weight.size(1) != x.size(-1) || weight.size(0) < 1 || weight.scalar_type() != x.scalar_type() || weight.device() != x.device())
+    refuse("weight must be a [classes, features] tensor of x's dtype and device");
+  if (target.scalar_type() != at::kLong || target.device() != x.device() || target.sizes() != x.sizes().slice(0, (size_t)x.dim() - 1))
+    refuse("target must be an int64 tensor on x's device, of x's shape without the features");
+  if (bias && (bias->dim() != 1 || bias->size(0) != weight.size(0) || type_of(bias->scalar_type()) < 0 || bias->device() != x.device() || !bias->is_contiguous()))
+    refuse("bias must be a contiguous [classes] tensor on x's device");
+  LinearCe c = {as_rows(x), as_rows(weight), target.is_contiguous() ? target : target.contiguous(), {}};
+  c.d.type = type_of(x.scalar_type());
+  c.d.has_bias = bias ? 1 : 0;
+  c.d.bias_type = bias ? type_of(bias->scalar_type()) : SAE_TYPE_FLOAT;
+  c.d.reduction = reduction;
+  c.d.rows = c.x.size(0);
+  c.d.features = x.size(-1);
+  c.d.classes = weight.size(0);
+  c.d.x_pitch = c.x.size(0) > 1 ? c.x.stride(0) : c.d.features;
+  c.d.weight_pitch = c.weight.size(0) > 1 ? c.weight.stride(0) : c.d.features;
+  c.d.ignore_index = ignore;
+  return c;
+}
+
+Tensor ce_workspace(const LinearCe& c, int backward, size_t& bytes) {
+  const int64_t n = sae_linear_ce_workspace(&c.d, c.weight.data_ptr(), backward);
+  bytes = n > 0 ? (size_t)n : 0;
+  return fresh({(int64_t)bytes}, at::kByte, c.x.device());
+}
+
+std::tuple<int, Tensor, Tensor, Tensor> linear_ce_forward(const Tensor& x, const Tensor& weight, const Tensor& target, const Maybe& bias, int64_t ignore,
+                                                          int reduction) {
+  const LinearCe c = describe_ce(x, weight, target, bias, ignore, reduction);
+  c10::cuda::CUDAGuard guard(x.device());
+  Tensor loss = fresh(reduction == SAE_REDUCE_NONE ? target.sizes() : at::IntArrayRef{}, at::kFloat, x.device());
+  Tensor lse = fresh(target.sizes(), at::kFloat, x.device()), count = fresh({}, at::kLong, x.device());
+  size_t bytes;
+  Tensor ws = ce_workspace(c, 0, bytes);
+  const int rc = sae_linear_ce_forward(&c.d, c.x.data_ptr(), c.weight.data_ptr(), ptr(bias), (const int64_t*)c.target.data_ptr(), (float*)loss.data_ptr(),
+                                       (float*)lse.data_ptr(), (int64_t*)count.data_ptr(), ws.data_ptr(), bytes,
+                                       c10::cuda::getCurrentCUDAStream(x.get_device()).stream());
+  return {rc, loss, lse, count};
+}
+
+std::tuple<int, Maybe, Maybe, Maybe> linear_ce_backward(const Tensor& dloss, const Tensor& x, const Tensor& weight, const Tensor& target, const Tensor& lse,
+                                                        const Tensor& count, const Maybe& bias, int64_t ignore, int reduction, bool need_x, bool need_weight,
+                                                        bool need_bias) {
+  const LinearCe c = describe_ce(x, weight, target, bias, ignore, reduction);
+  c10::cuda::CUDAGuard guard(x.device());
+  if (dloss.scalar_type() != at::kFloat || dloss.device() != x.device() || (reduction == SAE_REDUCE_NONE ? dloss.sizes() != target.sizes() : dloss.numel() != 1))
+    refuse("dloss must be a float32 tensor of the loss's shape on x's device");
+  if (lse.scalar_type() != at::kFloat || lse.device() != x.device() || lse.sizes() != target.sizes() || !lse.is_contiguous() || count.scalar_type() != at::kLong ||
+      count.device() != x.device() || count.numel() != 1)
+    refuse("lse and count must be what the forward call returned");
+  const Tensor dl = dloss.contiguous();
+  Maybe dx, dweight, dbias;
+  if (need_x) dx = fresh(x.sizes(), x.scalar_type(), x.device());
+  if (need_weight) dweight = fresh(weight.sizes(), weight.scalar_type(), x.device());
+  if (bias && need_bias) dbias = fresh(bias->sizes(), bias->scalar_type(), x.device());
+  size_t bytes;
+  Tensor ws = ce_workspace(c, 1, bytes);
+  const int rc = sae_linear_ce_backward(&c.d, (const float*)dl.data_ptr(), c.x.data_ptr(), c.weight.data_ptr(), ptr(bias), (const int64_t*)c.target.data_ptr(),
+                                        (const float*)lse.data_ptr(), (const int64_t*)count.data_ptr(), ptr(dx), ptr(dweight), ptr(dbias), ws.data_ptr(), bytes,
+                                        c10::cuda::getCurrentCUDAStream(x.get_device()).stream());
+  return {rc, dx, dweight, dbias};
+}
+
 }  // namespace
 
 PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
@@ -324,6 +518,11 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
       .def("clip", &GradPlan::clip)
       .def("pack", &GradPlan::pack)
       .def("unpack", &GradPlan::unpack);
+  py::class_<OrthoPlan>(m, "OrthoPlan")
+      .def(py::init<int64_t, int, std::vector<std::vector<int64_t>>, std::vector<int>, std::vector<int>, int, int64_t>())
+      .def("run", &OrthoPlan::run);
+  m.def("linear_ce_forward", &linear_ce_forward);
+  m.def("linear_ce_backward", &linear_ce_backward);
   m.def("group_norm_forward", &group_norm_forward);
   m.def("group_norm_backward", &group_norm_backward);
 }

@@ -1,0 +1,960 @@
+// Linear cross entropy (sae_linear_ce_* of include/sae.h): the loss of a linear output layer and its gradients, no logits kept.
+//
+// forward   rows that take part are gathered (k_ce_rows), then one product kernel makes z = x w' tile by tile and keeps of each row
+//           the running maximum, the sum of exp(z - maximum) and the target's z; the runs are joined (k_ce_join).
+// backward  z is made again, piece by piece of the classes, and leaves the tensor cores as p = (exp(z - lse) - [target]) g in 16 bits;
+//           p w is added to dx's float sums, p' x is the piece's dweight.  8 N D V operations in all, against 6 with all of z kept.
+//
+// A row without a target costs nothing: the gathered rows are counted on the device, and every kernel goes by that count.  Gathering is
+// also where rows get the 16-byte pitch that TMA wants and float rows become three bfloat16 parts.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "../../include/sae.h"
+#include "sae_mma.cuh"
+#include "sae_vec.cuh"
+
+using namespace sae;
+
+namespace {
+
+constexpr int CE_THREADS = 256;
+constexpr int CE_ROWS = 32;                   // rows of a block of k_ce_rows
+constexpr int CE_COUNT_ROWS = 4096;           // rows counted by a block of k_ce_count
+constexpr int CE_SCAN_ROWS = 16384;           // up to here every block counts the rows before its own by itself
+constexpr int CE_CHUNK = 2048;                // units that a block copies
+constexpr int64_t CE_PIECE_BYTES = 256ll << 20;
+constexpr float LOG2E = 1.44269504088896340736f;
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+int elem_bytes(int type) { return type == SAE_TYPE_FLOAT ? 4 : 2; }
+bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// ---- gathering ----------------------------------------------------------------------------------------------------------
+struct RowsArgs {
+  const void* x;
+  const int64_t* target;
+  int64_t x_pitch, rows, ignore;
+  int type, parts, features, classes, pitch;      // pitch of the gathered rows
+  unsigned short* xg;
+  int64_t xg_plane;
+  const int* before;                              // rows that take part in each CE_COUNT_ROWS, where there are many
+  int* index;                                     // of every gathered row: where it came from,
+  int* at;                                        // its target (-1: out of range),
+  int* counted;                                   // and how many there are
+  int64_t* count;                                 // forward: the caller's
+  float *loss, *lse;                              // forward: 0 for rows that take no part (loss NULL: reduced)
+  unsigned* ticket;
+  // backward
+  const float *lse_in, *dloss;
+  const int64_t* count_in;
+  int reduction;
+  float p_scale;
+  float *lse_g, *g, *alpha;                       // of every gathered row: lse, its factor in p;  the factor behind the sums
+  const float* g_top;                             // the largest |dloss|, for float16 p
+  void* dx;
+  // copies beside it
+  const void* w;
+  int64_t w_pitch, wg_plane;
+  unsigned short* wg;
+  const void* bias;
+  int bias_type, bias_room;
+  float* bias_out;
+  int row_blocks, w_blocks;
+};
+
+// A float as the exact sum of three bfloat16: each takes the leading 8 bits of what is left.
+__device__ __forceinline__ void three_parts(float v, float (&p)[3]) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    p[i] = __bfloat162float(__float2bfloat16_rz(v));
+    v = isfinite(p[i]) ? v - p[i] : 0.0f;
+  }
+}
+
+// One unit of a row to its place in every part.
+__device__ __forceinline__ void put_unit(const void* from, int type, int parts, int n, unsigned short* to, int64_t plane) {
+  u32 w[4];
+  if (parts == 1) {                     // 16 bits stay as they are
+    const unsigned short* p = (const unsigned short*)from;
+    if (n == UNIT && (reinterpret_cast<uintptr_t>(p) & 15) == 0) *reinterpret_cast<uint4*>(to) = __ldg(reinterpret_cast<const uint4*>(p));
+    else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (2 * i < n ? p[2 * i] : 0u) | (2 * i + 1 < n ? (u32)p[2 * i + 1] << 16 : 0u);
+      *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return;
+  }
+  float v[UNIT], p[UNIT][3];
+  load_unit((const float*)from, n, v);
+#pragma unroll
+  for (int i = 0; i < UNIT; ++i) three_parts(v[i], p[i]);
+#pragma unroll
+  for (int q = 0; q < 3; ++q) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = mma::pack_bfloat(p[2 * i][q], p[2 * i + 1][q]);
+    *reinterpret_cast<uint4*>(to + q * plane) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+__device__ __forceinline__ int block_total(int v, int* scratch) {
+  v = __reduce_add_sync(0xffffffffu, v);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+  __syncthreads();
+  int s = 0;
+  for (int i = 0; i < CE_THREADS / 32; ++i) s += scratch[i];
+  return s;
+}
+__device__ __forceinline__ int rows_with_target(const RowsArgs& a, int64_t from, int64_t to, int* scratch) {
+  int n = 0;
+  for (int64_t i = from + threadIdx.x; i < to; i += CE_THREADS) n += __ldg(a.target + i) != a.ignore;
+  return block_total(n, scratch);
+}
+
+__global__ void __launch_bounds__(CE_THREADS) k_ce_count(const __grid_constant__ RowsArgs a, int* before) {
+  __shared__ int scratch[CE_THREADS / 32];
+  const int64_t from = (int64_t)blockIdx.x * CE_COUNT_ROWS;
+  const int n = rows_with_target(a, from, min(from + CE_COUNT_ROWS, a.rows), scratch);
+  if (threadIdx.x == 0) before[blockIdx.x] = n;
+}
+
+// The largest |dloss| of the rows that take part, or 1 where that is 0 or not finite.
+__global__ void __launch_bounds__(1024) k_ce_top(const __grid_constant__ RowsArgs a, float* top) {
+  __shared__ float scratch[32];
+  float m = 0;
+  for (int64_t i = threadIdx.x; i < a.rows; i += 1024)
+    if (a.target[i] != a.ignore) { const float v = fabsf(a.dloss[i]); if (v <= 3.0e38f) m = fmaxf(m, v); }
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 32; ++i) m = fmaxf(m, scratch[i]);
+    *top = m > 0 ? m : 1.0f;
+  }
+}
+
+template <bool BACKWARD>
+__global__ void __launch_bounds__(CE_THREADS) k_ce_rows(const __grid_constant__ RowsArgs a) {
+  __shared__ int scratch[CE_THREADS / 32], place[CE_ROWS];
+  mma::let_next_start();
+  mma::wait_for_previous();
+  int b = blockIdx.x;
+  if (b >= a.row_blocks) {              // copies of the weights' rows and of the bias
+    b -= a.row_blocks;
+    if (b < a.w_blocks) {
+      const unsigned wide = (unsigned)a.pitch / UNIT;
+      for (int i = threadIdx.x; i < CE_CHUNK; i += CE_THREADS) {
+        const int64_t u = (int64_t)b * CE_CHUNK + i, r = u / wide;
+        const int c = (int)(u - r * wide) * UNIT;
+        if (r >= a.classes) break;
+        put_unit((const char*)a.w + (r * a.w_pitch + c) * (a.type == SAE_TYPE_FLOAT ? 4 : 2), a.type, a.parts, min(UNIT, a.features - c),
+                 a.wg + r * a.pitch + c, a.wg_plane);
+      }
+    } else {
+      const int j = (b - a.w_blocks) * CE_THREADS + threadIdx.x;
+      if (j < a.bias_room) {
+        float v = __int_as_float(0xff800000);                  // classes that there are not
+        if (j < a.classes)
+          v = a.bias_type == SAE_TYPE_FLOAT ? ((const float*)a.bias)[j]
+              : a.bias_type == SAE_TYPE_BFLOAT ? to_f(((const __nv_bfloat16*)a.bias)[j]) : to_f(((const __half*)a.bias)[j]);
+        a.bias_out[j] = v;
+      }
+    }
+    return;
+  }
+  const int64_t r0 = (int64_t)b * CE_ROWS;
+  int base = 0;
+  if (a.before) {
+    const int64_t whole = r0 / CE_COUNT_ROWS;
+    int n = 0;
+    for (int64_t i = threadIdx.x; i < whole; i += CE_THREADS) n += a.before[i];
+    base = block_total(n, scratch) + rows_with_target(a, whole * CE_COUNT_ROWS, r0, scratch);
+  } else base = rows_with_target(a, 0, r0, scratch);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (warp == 0) {
+    const int64_t r = r0 + lane;
+    const int64_t t = r < a.rows ? a.target[r] : a.ignore;
+    const bool part = r < a.rows && t != a.ignore;
+    const u32 mask = __ballot_sync(0xffffffffu, part);
+    const int to = base + __popc(mask & ((1u << lane) - 1));
+    place[lane] = part ? to : -1;
+    if (part) {
+      const int cls = t >= 0 && t < a.classes ? (int)t : -1;
+      a.index[to] = (int)r;
+      a.at[to] = cls;
+      if constexpr (BACKWARD) {
+        a.lse_g[to] = a.lse_in[r];
+        float f = a.reduction == SAE_REDUCE_NONE ? a.dloss[r] / (a.g_top ? *a.g_top : 1.0f) : 1.0f;
+        a.g[to] = (cls < 0 ? __int_as_float(0x7fc00000) : f) * a.p_scale;
+      }
+    } else if (r < a.rows) {
+      if constexpr (!BACKWARD) {
+        a.lse[r] = 0;
+        if (a.loss) a.loss[r] = 0;
+      }
+    }
+    if (b + 1 == a.row_blocks && lane == 0) {
+      const int n = base + __popc(mask);
+      *a.counted = n;
+      if constexpr (!BACKWARD) { *a.count = n; *a.ticket = 0; }
+      else {
+        float f = 1.0f;
+        if (n == 0) f = 0.0f;                                  // sums of nothing
+        else if (a.reduction == SAE_REDUCE_NONE) f = a.g_top ? *a.g_top : 1.0f;
+        else f = a.reduction == SAE_REDUCE_MEAN ? *a.dloss / (float)*a.count_in : *a.dloss;
+        *a.alpha = f / a.p_scale;
+      }
+    }
+  }
+  __syncthreads();
+  const int es = a.type == SAE_TYPE_FLOAT ? 4 : 2;
+  for (int i = warp; i < CE_ROWS; i += CE_THREADS / 32) {
+    const int64_t r = r0 + i;
+    if (r >= a.rows) break;
+    const int to = place[i];
+    if (to >= 0) {
+      const char* from = (const char*)a.x + r * a.x_pitch * es;
+      for (int c = lane * UNIT; c < a.pitch; c += 32 * UNIT)
+        put_unit(from + (int64_t)c * es, a.type, a.parts, min(UNIT, a.features - c), a.xg + (int64_t)to * a.pitch + c, a.xg_plane);
+    } else if constexpr (BACKWARD) {
+      if (a.dx) {
+        char* row = (char*)a.dx + r * a.features * es;
+        if (es == 4) for (int c = lane; c < a.features; c += 32) ((float*)row)[c] = 0.0f;
+        else for (int c = lane; c < a.features; c += 32) ((unsigned short*)row)[c] = 0;
+      }
+    }
+  }
+  if (BACKWARD && b + 1 == a.row_blocks) {          // the last block of k of dweight's product reads zeros behind the last row
+    int last = -1;
+    for (int i = 0; i < CE_ROWS; ++i) last = max(last, place[i]);
+    const int n = last >= 0 ? last + 1 : base, wide = a.pitch / UNIT;
+    const int end = (n + mma::BLOCK_K - 1) / mma::BLOCK_K * mma::BLOCK_K;
+    for (int q = 0; q < a.parts; ++q)
+      for (int64_t u = threadIdx.x; u < (int64_t)(end - n) * wide; u += CE_THREADS)
+        *reinterpret_cast<uint4*>(a.xg + q * a.xg_plane + (int64_t)n * a.pitch + u * UNIT) = make_uint4(0, 0, 0, 0);
+  }
+}
+
+// ---- the loss ------------------------------------------------------------------------------------------------------------
+// Runs of tiles: row blocks one after another, each over all classes; a cluster takes an equal share of this list and leaves one run
+// (maximum, sum) for each row block that it touches.
+struct LossJob {
+  int cols;
+  bool bfloat;
+  mma::Segments seg;
+  CUtensorMap x, w;
+  const int* counted;
+  int classes, features, rows;              // rows of a tile
+  const float* bias;
+  const int* at;
+  float* at_z;
+  float2* runs;
+
+  struct Local { long long first, last; int wide, blocks, clusters, id; };
+  __device__ __forceinline__ Local begin(int cluster, int clusters) const {
+    Local l;
+    l.id = cluster;
+    l.wide = (classes + cols - 1) / cols;
+    l.blocks = (*counted + rows - 1) / rows;
+    const long long total = (long long)l.blocks * l.wide;
+    l.clusters = (int)min((long long)clusters, total);
+    l.first = cluster < l.clusters ? total * cluster / l.clusters : 0;
+    l.last = cluster < l.clusters ? total * (cluster + 1) / l.clusters : 0;
+    return l;
+  }
+  __device__ __forceinline__ bool tile(Local& l, int i, mma::Tile& t) const {
+    const long long w = l.first + i;
+    if (w >= l.last) return false;
+    t.group = (int)(w / l.wide);
+    t.a = &x;
+    t.b = &this->w;
+    t.row = t.a_row = t.group * rows;
+    t.col = t.b_row = (int)(w - (long long)t.group * l.wide) * cols;
+    t.a_plane = t.b_plane = t.a_k = t.b_k = 0;
+    t.a_rows_first = t.b_rows_first = false;
+    t.blocks = (features + mma::BLOCK_K - 1) / mma::BLOCK_K;
+    return true;
+  }
+  // the cluster that has tile w
+  __device__ __host__ static int cluster_of(long long w, long long total, int clusters) { return (int)(((w + 1) * clusters - 1) / total); }
+  // most runs of a row block
+  __device__ __host__ static int runs_of(int blocks, int clusters) { return (clusters + blocks - 1) / blocks + 1; }
+
+  struct Epilogue {
+    const LossJob& job;
+    const Local l;
+    const int row, half;
+    int block, cls;
+    float m, s;
+    __device__ __forceinline__ Epilogue(const LossJob& j, const Local& l, int r, int h) : job(j), l(l), row(r), half(h), block(-1), cls(-1) {}
+    __device__ __forceinline__ void finish() {
+      if (block < 0 || block * job.rows + row >= *job.counted) return;
+      const long long total = (long long)l.blocks * l.wide;
+      const int run = l.id - cluster_of((long long)block * l.wide, total, l.clusters);
+      const long long at = ((long long)block * runs_of(l.blocks, l.clusters) + run) * 2 + half;
+      job.runs[at * job.rows + row] = make_float2(m, s);
+    }
+    __device__ __forceinline__ void tile(const mma::Tile& t, const mma::Sums& sums) {
+      if (t.group != block) {
+        finish();
+        block = t.group;
+        const int r = t.row + row;
+        cls = r < *job.counted ? job.at[r] : -1;
+        m = __int_as_float(0xff800000);
+        s = 0;
+      }
+      const int width = job.cols / 2;
+      for (int c = half * width; c < (half + 1) * width; c += 32) {
+        const int col = t.col + c;
+        if (col >= job.classes) break;                      // the same for the whole warp
+        float z[32];
+        mma::sums_of(sums, c, z);
+        if (job.bias) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 b = __ldg(reinterpret_cast<const float4*>(job.bias + col + i));
+            z[i] += b.x; z[i + 1] += b.y; z[i + 2] += b.z; z[i + 3] += b.w;
+          }
+        } else if (col + 32 > job.classes) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) if (col + i >= job.classes) z[i] = __int_as_float(0xff800000);
+        }
+        const unsigned mine = (unsigned)(cls - col);
+        if (mine < 32u) {
+          float v = z[0];
+#pragma unroll
+          for (int i = 1; i < 32; ++i) v = mine == (unsigned)i ? z[i] : v;
+          job.at_z[t.row + row] = v;
+        }
+        float top[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+        for (int i = 4; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], z[i]);
+        const float cm = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        if (cm > m) { s *= exp2_approx((m - cm) * LOG2E); m = cm; }
+        const float from = m == __int_as_float(0xff800000) ? 0.0f : m;      // subtracted first: large logits keep their differences
+        float part[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) part[i & 3] += exp2_approx((z[i] - from) * LOG2E);
+        s += (part[0] + part[1]) + (part[2] + part[3]);
+      }
+    }
+  };
+};
+
+struct JoinArgs {
+  const float2* runs;
+  const int *counted, *index, *at;
+  const float* at_z;
+  float *loss, *lse;
+  double* sums;
+  unsigned* ticket;
+  int rows, wide, clusters, reduction;
+};
+
+// A warp joins a row's runs; the last block adds the blocks' sums in their order.
+__global__ void __launch_bounds__(CE_THREADS) k_ce_join(const __grid_constant__ JoinArgs a) {
+  __shared__ double scratch[CE_THREADS / 32];
+  __shared__ bool final_block;
+  mma::let_next_start();
+  mma::wait_for_previous();
+  const int n = *a.counted, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int blocks = (n + a.rows - 1) / a.rows;
+  const long long total = (long long)blocks * a.wide;
+  const int clusters = (int)min((long long)a.clusters, total);
+  double sum = 0;
+  for (int i = blockIdx.x * CE_ROWS + warp; i < min(n, (int)(blockIdx.x + 1) * CE_ROWS); i += CE_THREADS / 32) {
+    const int block = i / a.rows, row = i - block * a.rows;
+    const int runs = LossJob::cluster_of((long long)(block + 1) * a.wide - 1, total, clusters) - LossJob::cluster_of((long long)block * a.wide, total, clusters) + 1;
+    const long long first = (long long)block * LossJob::runs_of(blocks, clusters) * 2;
+    float m = __int_as_float(0xff800000), s = 0;
+    for (int k = lane; k < 2 * runs; k += 32) {
+      const float2 v = a.runs[(first + k) * a.rows + row];
+      const float top = fmaxf(m, v.x);
+      if (top > __int_as_float(0xff800000)) s = s * exp2f((m - top) * LOG2E) + v.y * exp2f((v.x - top) * LOG2E);
+      else s += v.y;
+      m = top;
+    }
+    for (int o = 16; o; o >>= 1) {
+      const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o), top = fmaxf(m, om);
+      if (top > __int_as_float(0xff800000)) s = s * exp2f((m - top) * LOG2E) + os * exp2f((om - top) * LOG2E);
+      else s += os;
+      m = top;
+    }
+    if (lane == 0) {
+      const float lse = m + logf(s), z = a.at[i] >= 0 ? a.at_z[i] : __int_as_float(0x7fc00000);
+      // log s + (m - z): the same value with one rounding less where lse is large
+      const float loss = logf(s) + (m - z);
+      a.lse[a.index[i]] = lse;
+      if (a.reduction == SAE_REDUCE_NONE) a.loss[a.index[i]] = loss;
+      sum += loss;
+    }
+  }
+  if (a.reduction == SAE_REDUCE_NONE) return;
+  if (lane == 0) scratch[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    sum = 0;
+    for (int i = 0; i < CE_THREADS / 32; ++i) sum += scratch[i];
+    a.sums[blockIdx.x] = sum;
+    __threadfence();
+    final_block = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!final_block) return;
+  __threadfence();
+  sum = 0;
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += CE_THREADS) sum += __ldcg(a.sums + i);
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) scratch[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    sum = 0;
+    for (int i = 0; i < CE_THREADS / 32; ++i) sum += scratch[i];
+    *a.loss = (float)(a.reduction == SAE_REDUCE_MEAN ? sum / (double)n : sum);
+  }
+}
+
+// ---- the gradients --------------------------------------------------------------------------------------------------------
+// p of one piece of the classes.
+struct GradJob {
+  int cols;
+  bool bfloat;
+  mma::Segments seg;
+  CUtensorMap x, w;
+  const int* counted;
+  int classes, features, rows, start, tiles;     // first class of the piece, tiles across it
+  const float *bias, *lse, *g;
+  const int* at;
+  unsigned short* p;
+  int64_t p_plane;
+  int p_pitch, type;
+  float* bias_sums;                              // [rows / 32][p_pitch], NULL: not wanted
+
+  struct Local { int first, step, blocks; };
+  __device__ __forceinline__ Local begin(int cluster, int clusters) const { return {cluster, clusters, (*counted + rows - 1) / rows}; }
+  __device__ __forceinline__ bool tile(Local& l, int i, mma::Tile& t) const {
+    const long long n = l.first + (long long)i * l.step;
+    if (n >= (long long)l.blocks * tiles) return false;
+    const int v = (int)(n / l.blocks);
+    t.row = t.a_row = (int)(n - (long long)v * l.blocks) * rows;
+    t.col = v * cols;
+    t.b_row = start + t.col;
+    t.a = &x;
+    t.b = &w;
+    t.a_plane = t.b_plane = t.a_k = t.b_k = 0;
+    t.a_rows_first = t.b_rows_first = false;
+    t.blocks = (features + mma::BLOCK_K - 1) / mma::BLOCK_K;
+    return true;
+  }
+  struct Epilogue {
+    const GradJob& job;
+    const int row, half;
+    __device__ __forceinline__ Epilogue(const GradJob& j, const Local&, int r, int h) : job(j), row(r), half(h) {}
+    __device__ __forceinline__ void finish() {}
+    __device__ __forceinline__ void tile(const mma::Tile& t, const mma::Sums& sums) {
+      const int r = t.row + row;
+      const bool used = r < *job.counted;
+      const float lse = used ? job.lse[r] : 0.0f, g = used ? job.g[r] : 0.0f;
+      const int cls = used ? job.at[r] - job.start : -1;
+      const int width = job.cols / 2;
+      for (int c = half * width; c < (half + 1) * width; c += 32) {
+        const int col = t.col + c, cc = job.start + col;
+        float z[32];
+        mma::sums_of(sums, c, z);
+        if (job.bias) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const float4 b = __ldg(reinterpret_cast<const float4*>(job.bias + cc + i));
+            z[i] += b.x; z[i + 1] += b.y; z[i + 2] += b.z; z[i + 3] += b.w;
+          }
+        } else if (cc + 32 > job.classes) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) if (cc + i >= job.classes) z[i] = __int_as_float(0xff800000);
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) z[i] = exp2_approx((z[i] - lse) * LOG2E);
+        const unsigned mine = (unsigned)(cls - col);
+        if (mine < 32u) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) z[i] = mine == (unsigned)i ? z[i] - 1.0f : z[i];
+        }
+        // a row that is none stays exactly zero, whatever its sums are
+#pragma unroll
+        for (int i = 0; i < 32; ++i) z[i] = used ? z[i] * g : 0.0f;
+        unsigned short* const to = job.p + (int64_t)r * job.p_pitch + col;
+        u32 w[16];
+        if (job.type == SAE_TYPE_HALF) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[i] = mma::pack_half(z[2 * i], z[2 * i + 1]);
+          mma::store_words(to, w);
+        } else if (job.type == SAE_TYPE_BFLOAT) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[i] = mma::pack_bfloat(z[2 * i], z[2 * i + 1]);
+          mma::store_words(to, w);
+        } else {
+          u32 w1[16], w2[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float a[3], b[3];
+            three_parts(z[2 * i], a);
+            three_parts(z[2 * i + 1], b);
+            w[i] = mma::pack_bfloat(a[0], b[0]); w1[i] = mma::pack_bfloat(a[1], b[1]); w2[i] = mma::pack_bfloat(a[2], b[2]);
+          }
+          mma::store_words(to, w);
+          mma::store_words(to + job.p_plane, w1);
+          mma::store_words(to + 2 * job.p_plane, w2);
+        }
+        if (job.bias_sums) {                      // over the warp's 32 rows: halves are exchanged until each lane has one column
+          const int lane = threadIdx.x & 31;
+#pragma unroll
+          for (int o = 16; o; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < o; ++i) {
+              const float keep = lane & o ? z[i + o] : z[i], give = lane & o ? z[i] : z[i + o];
+              z[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+            }
+          job.bias_sums[(int64_t)((t.row + row) >> 5) * job.p_pitch + col + lane] = z[0];
+        }
+      }
+    }
+  };
+};
+
+// How often the classes of a piece are split for dx, where there are too few tiles for the clusters.
+__device__ __host__ inline int dx_splits(int blocks, int tiles_across, int clusters, int room) {
+  int best = 1;
+  float least = 0;
+  for (int s = 1; s <= 8 && s <= room; ++s) {
+    const long long t = (long long)blocks * tiles_across * s;
+    const float cost = (float)((t + clusters - 1) / clusters) / (float)s * (1.0f + 0.03f * (float)s);
+    if (s == 1 || cost < least) { least = cost; best = s; }
+  }
+  return best;
+}
+
+// dx's sums (p w, float, added up over the pieces) and dweight of a piece (p' x).
+struct ProductJob {
+  int cols;
+  bool bfloat;
+  mma::Segments seg;
+  CUtensorMap a, b;
+  const int* counted;
+  int rows, across, features;     // rows of a tile, tiles across the features
+  int start, width;               // the piece's first class and its classes, rounded up to 64
+  bool dx;
+  // dx
+  float* sums;
+  int sums_pitch, room, add;      // room: row blocks that the sums have place for
+  // dweight
+  void* out;
+  int type, classes;              // classes of the piece
+  const float* alpha;
+
+  struct Local { int first, step, blocks, splits, count; };
+  __device__ __forceinline__ Local begin(int cluster, int clusters) const {
+    Local l = {cluster, clusters, 0, 1, *counted};
+    l.blocks = ((dx ? l.count : classes) + rows - 1) / rows;
+    if (dx) l.splits = dx_splits(l.blocks, across, clusters, l.blocks ? room / l.blocks : 1);
+    return l;
+  }
+  __device__ __forceinline__ bool tile(Local& l, int i, mma::Tile& t) const {
+    const long long n = l.first + (long long)i * l.step;
+    if (n >= (long long)l.blocks * l.splits * across) return false;
+    const int q = (int)(n / across);
+    t.item = q / l.blocks;                        // the split
+    t.row = t.a_row = (q - t.item * l.blocks) * rows;
+    t.col = t.b_row = (int)(n - (long long)q * across) * cols;
+    t.a = &a;
+    t.b = &b;
+    t.a_plane = t.b_plane = 0;
+    t.b_rows_first = true;
+    t.a_rows_first = !dx;
+    const int all = ((dx ? width : l.count) + mma::BLOCK_K - 1) / mma::BLOCK_K;
+    const int from = (int)((long long)all * t.item / l.splits), to = (int)((long long)all * (t.item + 1) / l.splits);
+    t.a_k = from * mma::BLOCK_K;
+    t.b_k = t.a_k + (dx ? start : 0);
+    t.blocks = to - from;
+    t.group = l.blocks * rows;                    // rows of a split's sums
+    return true;
+  }
+  struct Epilogue {
+    const ProductJob& job;
+    const int row, half;
+    const float alpha;
+    const int limit;
+    __device__ __forceinline__ Epilogue(const ProductJob& j, const Local& l, int r, int h) : job(j), row(r), half(h), alpha(j.dx ? 1.0f : *j.alpha), limit(j.dx ? l.count : j.classes) {}
+    __device__ __forceinline__ void finish() {}
+    __device__ __forceinline__ void tile(const mma::Tile& t, const mma::Sums& sums) {
+      const int r = t.row + row, w = job.cols / 2;
+      for (int c = half * w; c < (half + 1) * w; c += 32) {
+        const int col = t.col + c;
+        if (col >= job.features) break;
+        float v[32];
+        mma::sums_of(sums, c, v);
+        if (r >= limit) continue;
+        if (job.dx) {
+          float* const to = job.sums + ((int64_t)t.item * t.group + r) * job.sums_pitch + col;
+          if (job.add) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              u32 old[16];
+              mma::load_words(to + 16 * h, old);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) v[16 * h + i] += __uint_as_float(old[i]);
+            }
+          }
+          mma::store_row(to, v, 32);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] *= alpha;
+          const int n = min(32, job.features - col);
+          const int64_t to = (int64_t)(job.start + r) * job.features + col;
+          if (job.type == SAE_TYPE_FLOAT) mma::store_row((float*)job.out + to, v, n);
+          else if (job.type == SAE_TYPE_BFLOAT) mma::store_row((__nv_bfloat16*)job.out + to, v, n);
+          else mma::store_row((__half*)job.out + to, v, n);
+        }
+      }
+    }
+  };
+};
+
+// dx = alpha * the sums over the splits, back to the rows that they belong to.
+struct DxArgs {
+  const float* sums;
+  const int *counted, *index;
+  const float* alpha;
+  void* dx;
+  int sums_pitch, features, type, rows, across, clusters, room;
+};
+template <typename T>
+__device__ __forceinline__ void put_row(T* to, const float (&v)[UNIT], int n) {
+  if (n == UNIT && (reinterpret_cast<uintptr_t>(to) & 15) == 0) {
+    if constexpr (sizeof(T) == 4) {
+      reinterpret_cast<float4*>(to)[0] = make_float4(v[0], v[1], v[2], v[3]);
+      reinterpret_cast<float4*>(to)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else {
+      Raw<T, 8> r;
+      r.round(v);
+      r.store(to);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < UNIT; ++i) if (i < n) to[i] = from_f<T>(v[i]);
+  }
+}
+__global__ void __launch_bounds__(CE_THREADS) k_ce_dx(const __grid_constant__ DxArgs a) {
+  mma::let_next_start();
+  mma::wait_for_previous();
+  const int count = *a.counted, blocks = (count + a.rows - 1) / a.rows;
+  if (!blocks) return;
+  const int splits = dx_splits(blocks, a.across, a.clusters, a.room / blocks);
+  const int64_t plane = (int64_t)blocks * a.rows * a.sums_pitch;
+  const float alpha = *a.alpha;
+  const unsigned wide = (unsigned)(a.features + UNIT - 1) / UNIT;
+  for (int i = threadIdx.x; i < CE_CHUNK; i += CE_THREADS) {
+    const int64_t u = (int64_t)blockIdx.x * CE_CHUNK + i, r = u / wide;
+    const int c = (int)(u - r * wide) * UNIT;
+    if (r >= count) break;
+    float v[UNIT] = {};
+    const float* from = a.sums + r * a.sums_pitch + c;
+    for (int s = 0; s < splits; ++s, from += plane) {
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(from)), y = __ldcg(reinterpret_cast<const float4*>(from) + 1);
+      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+    }
+#pragma unroll
+    for (int k = 0; k < UNIT; ++k) v[k] *= alpha;
+    const int n = min(UNIT, a.features - c);
+    const int64_t to = (int64_t)a.index[r] * a.features + c;
+    if (a.type == SAE_TYPE_FLOAT) put_row((float*)a.dx + to, v, n);
+    else if (a.type == SAE_TYPE_BFLOAT) put_row((__nv_bfloat16*)a.dx + to, v, n);
+    else put_row((__half*)a.dx + to, v, n);
+  }
+}
+
+// dbias of a piece: the sums of every 32 rows, added in order (double).
+__global__ void __launch_bounds__(CE_THREADS) k_ce_dbias(const float* sums, int pitch, const int* counted, const float* alpha, int classes, int type, void* out) {
+  __shared__ double scratch[CE_THREADS / 32][32];
+  mma::let_next_start();
+  mma::wait_for_previous();
+  const int j = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5, n = (*counted + 31) / 32;
+  double s = 0;
+  if (j < classes) for (int i = part; i < n; i += CE_THREADS / 32) s += __ldcg(sums + (int64_t)i * pitch + j);
+  scratch[part][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (part || j >= classes) return;
+  for (int i = 1; i < CE_THREADS / 32; ++i) s += scratch[i][threadIdx.x & 31];
+  const float v = (float)(s * *alpha);
+  if (type == SAE_TYPE_FLOAT) ((float*)out)[j] = v;
+  else if (type == SAE_TYPE_BFLOAT) ((__nv_bfloat16*)out)[j] = __float2bfloat16_rn(v);
+  else ((__half*)out)[j] = __float2half_rn(v);
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------------------
+bool type_ok(int t) { return t == SAE_TYPE_FLOAT || t == SAE_TYPE_BFLOAT || t == SAE_TYPE_HALF; }
+
+bool desc_ok(const sae_linear_ce_desc* d) {
+  return d && type_ok(d->type) && (!d->has_bias || type_ok(d->bias_type)) && d->reduction >= SAE_REDUCE_NONE && d->reduction <= SAE_REDUCE_MEAN &&
+         d->rows >= 0 && d->rows <= (1 << 24) && d->features >= 1 && d->features <= (1 << 17) && d->classes >= 1 && d->classes <= (1 << 24) &&
+         (d->rows < 2 || d->x_pitch >= d->features) && (d->classes < 2 || d->weight_pitch >= d->features);
+}
+
+int device_sms() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return -1; }
+  return sms;
+}
+
+struct TileShape { int cg, cols; };
+
+// Time in units of a block's k loop: waves of tiles over the SMs (or pairs) times what a tile costs.
+TileShape tile_shape(int64_t rows, int64_t cols, int parts, int sms) {
+  const struct { TileShape s; double cost; } shapes[3] = {{{2, parts == 1 ? 256 : 128}, parts == 1 ? 2.0 : 1.2}, {{1, 128}, 1.3}, {{1, 64}, 1.0}};
+  TileShape best = shapes[0].s;
+  double least = 0;
+  for (const auto& c : shapes) {
+    const double tiles = (double)((rows + 128 * c.s.cg - 1) / (128 * c.s.cg)) * (double)((cols + c.s.cols - 1) / c.s.cols);
+    const double t = c.cost * std::max(1.0, tiles / (sms / c.s.cg));
+    if (least == 0 || t < least) { least = t; best = c.s; }
+  }
+  return best;
+}
+
+struct CePlan {
+  int parts, pitch;
+  int64_t rows;                      // room for gathered rows
+  bool copy_w;
+  TileShape z, dx, dw;
+  int piece, pieces, p_pitch;        // classes of a piece
+  int sums_pitch, dx_room;
+  // offsets
+  size_t xg, wg, bias, index, at, at_z, counted, before, runs, sums, lse_g, g, alpha, top, p, bias_sums, dx_sums, bytes;
+};
+
+CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward, int sms) {
+  CePlan p = {};
+  p.parts = d->type == SAE_TYPE_FLOAT ? 3 : 1;
+  p.pitch = (int)up(d->features, 8);
+  p.rows = up(std::max<int64_t>(1, d->rows), 256);
+  // (one row of weights has no pitch of its own: any that TMA takes will do)
+  p.copy_w = p.parts > 1 || !aligned_to(weight, 16) || (d->classes > 1 && d->weight_pitch % 8);
+  size_t at = 0;
+  const auto take = [&](int64_t bytes) { const size_t o = at; at += (size_t)up(std::max<int64_t>(bytes, 1), 256); return o; };
+  p.xg = take((int64_t)p.parts * p.rows * p.pitch * 2);
+  p.wg = take(p.copy_w ? (int64_t)p.parts * d->classes * p.pitch * 2 : 0);
+  p.bias = take(d->has_bias ? up(d->classes, 256) * 4 + 1024 : 0);
+  p.index = take(p.rows * 4);
+  p.at = take(p.rows * 4);
+  p.counted = take(8);
+  p.before = take(d->rows > CE_SCAN_ROWS ? up(d->rows, CE_COUNT_ROWS) / CE_COUNT_ROWS * 4 : 0);
+  p.z = tile_shape(d->rows, d->classes, p.parts, sms);
+  if (!backward) {
+    const int rows = 128 * p.z.cg, clusters = sms / p.z.cg;
+    const int64_t blocks = up(p.rows, rows) / rows;
+    p.at_z = take(p.rows * 4);
+    p.runs = take((clusters + 2 * blocks + 2) * 2 * rows * (int64_t)sizeof(float2));
+    p.sums = take(up(p.rows, CE_ROWS) / CE_ROWS * 8);
+  } else {
+    p.lse_g = take(p.rows * 4);
+    p.g = take(p.rows * 4);
+    p.alpha = take(4);
+    p.top = take(4);
+    const int64_t most = std::max<int64_t>(256, CE_PIECE_BYTES / (p.rows * 2 * p.parts) / 256 * 256);
+    p.pieces = (int)((d->classes + most - 1) / most);
+    p.piece = (int)up((d->classes + p.pieces - 1) / p.pieces, 256);
+    p.pieces = (int)((d->classes + p.piece - 1) / p.piece);
+    p.p_pitch = p.piece;
+    p.dx = tile_shape(d->rows, d->features, p.parts, sms);
+    p.dw = tile_shape(p.piece, d->features, p.parts, sms);
+    p.sums_pitch = (int)up(d->features, 32);
+    const int rows = 128 * p.dx.cg, across = (int)up(d->features, p.dx.cols) / p.dx.cols, clusters = sms / p.dx.cg;
+    p.dx_room = (int)(up(p.rows, rows) / rows) + 4 * clusters / across;
+    p.p = take((int64_t)p.parts * p.rows * p.p_pitch * 2);
+    p.bias_sums = take(d->has_bias ? p.rows / 32 * p.p_pitch * 4 : 0);
+    p.dx_sums = take((int64_t)p.dx_room * rows * p.sums_pitch * 4);
+  }
+  p.bytes = at;
+  return p;
+}
+
+template <typename... P, typename... A>
+int launch(void (*kernel)(P...), int64_t blocks, int threads, cudaStream_t st, bool first, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = first ? 0 : 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
+  return SAE_OK;
+}
+
+template <class Job>
+int products(const Job& job, const TileShape& s, int64_t tiles, int sms, cudaStream_t st) {
+  const int units = (int)std::min<int64_t>(std::max<int64_t>(1, tiles), sms / s.cg);
+  const cudaError_t e = mma::launch_products(job, s.cg, units, st);
+  if (e != cudaSuccess) cudaGetLastError();
+  return e == cudaSuccess ? SAE_OK : SAE_ERR_CUDA;
+}
+
+mma::Segments segments(int parts) {
+  mma::Segments one = {1, {0}, {0}}, three = {6, {0, 2, 1, 0, 1, 0}, {2, 0, 1, 1, 0, 0}};
+  return parts == 1 ? one : three;
+}
+
+RowsArgs rows_args(const sae_linear_ce_desc* d, const CePlan& p, const void* x, const void* w, const void* bias, const int64_t* target, char* ws) {
+  RowsArgs a = {};
+  a.x = x; a.target = target; a.x_pitch = d->x_pitch; a.rows = d->rows; a.ignore = d->ignore_index;
+  a.type = d->type; a.parts = p.parts; a.features = (int)d->features; a.classes = (int)d->classes; a.pitch = p.pitch;
+  a.xg = (unsigned short*)(ws + p.xg); a.xg_plane = p.rows * p.pitch;
+  a.index = (int*)(ws + p.index); a.at = (int*)(ws + p.at); a.counted = (int*)(ws + p.counted); a.ticket = (unsigned*)(ws + p.counted + 4);
+  a.w = w; a.w_pitch = d->weight_pitch; a.wg = (unsigned short*)(ws + p.wg); a.wg_plane = d->classes * p.pitch;
+  a.bias = bias; a.bias_type = d->bias_type; a.bias_out = (float*)(ws + p.bias);
+  a.bias_room = d->has_bias ? (int)up(d->classes, 256) : 0;
+  a.row_blocks = (int)std::max<int64_t>(1, up(d->rows, CE_ROWS) / CE_ROWS);
+  a.w_blocks = p.copy_w ? (int)(up(d->classes * (p.pitch / UNIT), CE_CHUNK) / CE_CHUNK) : 0;
+  a.reduction = d->reduction;
+  return a;
+}
+
+// Gathers rows and whatever else must be laid out; its first launch is the call's first.
+template <bool BACKWARD>
+int gather(const sae_linear_ce_desc* d, const CePlan& p, RowsArgs& a, char* ws, cudaStream_t st) {
+  bool first = true;
+  int rc = SAE_OK;
+  if (d->rows > CE_SCAN_ROWS) {
+    rc = launch(k_ce_count, up(d->rows, CE_COUNT_ROWS) / CE_COUNT_ROWS, CE_THREADS, st, true, a, (int*)(ws + p.before));
+    a.before = (const int*)(ws + p.before);
+    first = false;
+  }
+  if (rc == SAE_OK && BACKWARD && d->type == SAE_TYPE_HALF && d->reduction == SAE_REDUCE_NONE) {
+    rc = launch(k_ce_top, 1, 1024, st, first, a, (float*)(ws + p.top));
+    a.g_top = (const float*)(ws + p.top);
+    first = false;
+  }
+  if (rc == SAE_OK) rc = launch(k_ce_rows<BACKWARD>, a.row_blocks + a.w_blocks + (a.bias_room + CE_THREADS - 1) / CE_THREADS, CE_THREADS, st, first, a);
+  return rc;
+}
+
+bool maps(const sae_linear_ce_desc* d, const CePlan& p, const void* weight, char* ws, CUtensorMap* x, CUtensorMap* w) {
+  const bool bfloat = d->type != SAE_TYPE_HALF;
+  return mma::encode_map(x, ws + p.xg, bfloat, d->features, p.rows, p.parts, p.pitch, p.rows * p.pitch) &&
+         (p.copy_w ? mma::encode_map(w, ws + p.wg, bfloat, d->features, d->classes, p.parts, p.pitch, d->classes * p.pitch)
+                   : mma::encode_map(w, weight, bfloat, d->features, d->classes, 1, d->classes > 1 ? d->weight_pitch : p.pitch, p.pitch));
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t sae_linear_ce_workspace(const sae_linear_ce_desc* d, const void* weight, int32_t backward) {
+  if (!desc_ok(d)) return -1;
+  const int sms = device_sms();
+  return sms < 2 ? -1 : (int64_t)make_plan(d, weight, backward != 0, sms).bytes;
+}
+
+int sae_linear_ce_forward(const sae_linear_ce_desc* d, const void* x, const void* weight, const void* bias, const int64_t* target, float* loss,
+                          float* lse, int64_t* count, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!desc_ok(d) || !weight || !count || (d->rows && (!x || !target || !lse)) || (!loss && (d->rows || d->reduction != SAE_REDUCE_NONE)) || (d->has_bias && !bias) || !workspace) return SAE_ERR_INVALID_ARG;
+  const int es = elem_bytes(d->type);
+  if (!aligned_to(x, es) || !aligned_to(weight, es) || !aligned_to(bias, d->has_bias ? elem_bytes(d->bias_type) : 1) || !aligned_to(target, 8) || !aligned_to(loss, 4) ||
+      !aligned_to(lse, 4) || !aligned_to(count, 8) || !aligned_to(workspace, 256)) return SAE_ERR_INVALID_ARG;
+  const int sms = device_sms();
+  if (sms < 2) return SAE_ERR_CUDA;
+  const CePlan p = make_plan(d, weight, false, sms);
+  if (workspace_bytes < p.bytes) return SAE_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  char* ws = (char*)workspace;
+  RowsArgs a = rows_args(d, p, x, weight, d->has_bias ? bias : nullptr, target, ws);
+  a.count = count; a.lse = lse; a.loss = d->reduction == SAE_REDUCE_NONE ? loss : nullptr;
+  LossJob job = {};
+  if (!maps(d, p, weight, ws, &job.x, &job.w)) return SAE_ERR_CUDA;
+  int rc = gather<false>(d, p, a, ws, st);
+  if (rc != SAE_OK) return rc;
+  job.cols = p.z.cols; job.bfloat = d->type != SAE_TYPE_HALF; job.seg = segments(p.parts);
+  job.counted = a.counted; job.classes = a.classes; job.features = a.features; job.rows = 128 * p.z.cg;
+  job.bias = d->has_bias ? a.bias_out : nullptr; job.at = a.at; job.at_z = (float*)(ws + p.at_z); job.runs = (float2*)(ws + p.runs);
+  const int64_t wide = up(d->classes, p.z.cols) / p.z.cols, tiles = up(d->rows, job.rows) / job.rows * wide;
+  if (tiles) rc = products(job, p.z, tiles, sms, st);
+  if (rc != SAE_OK) return rc;
+  JoinArgs j = {};
+  j.runs = job.runs; j.counted = a.counted; j.index = a.index; j.at = a.at; j.at_z = job.at_z; j.loss = loss; j.lse = lse; j.sums = (double*)(ws + p.sums);
+  j.ticket = a.ticket; j.rows = job.rows; j.wide = (int)wide; j.reduction = d->reduction;
+  j.clusters = (int)std::min<int64_t>(std::max<int64_t>(1, tiles), sms / p.z.cg);
+  return launch(k_ce_join, std::max<int64_t>(1, up(d->rows, CE_ROWS) / CE_ROWS), CE_THREADS, st, false, j);
+}
+
+int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, const void* x, const void* weight, const void* bias, const int64_t* target,
+                           const float* lse, const int64_t* count, void* dx, void* dweight, void* dbias, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  if (!desc_ok(d) || !weight || !count || (d->rows && (!x || !target || !lse)) || (!dloss && (d->rows || d->reduction != SAE_REDUCE_NONE)) || (d->has_bias && !bias) || (dbias && !d->has_bias) ||
+      !workspace) return SAE_ERR_INVALID_ARG;
+  const int es = elem_bytes(d->type), bs = d->has_bias ? elem_bytes(d->bias_type) : 1;
+  if (!aligned_to(x, es) || !aligned_to(weight, es) || !aligned_to(bias, bs) || !aligned_to(target, 8) || !aligned_to(dloss, 4) || !aligned_to(lse, 4) ||
+      !aligned_to(count, 8) || !aligned_to(dx, es) || !aligned_to(dweight, es) || !aligned_to(dbias, bs) || !aligned_to(workspace, 256)) return SAE_ERR_INVALID_ARG;
+  const int sms = device_sms();
+  if (sms < 2) return SAE_ERR_CUDA;
+  const CePlan p = make_plan(d, weight, true, sms);
+  if (workspace_bytes < p.bytes) return SAE_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (!dx && !dweight && !dbias) return SAE_OK;
+  char* ws = (char*)workspace;
+  RowsArgs a = rows_args(d, p, x, weight, d->has_bias ? bias : nullptr, target, ws);
+  a.lse_in = lse; a.dloss = dloss; a.count_in = count; a.dx = dx;
+  a.lse_g = (float*)(ws + p.lse_g); a.g = (float*)(ws + p.g); a.alpha = (float*)(ws + p.alpha);
+  a.p_scale = d->type == SAE_TYPE_HALF ? 32768.0f : 1.0f;
+  GradJob g = {};
+  if (!maps(d, p, weight, ws, &g.x, &g.w)) return SAE_ERR_CUDA;
+  const bool bfloat = d->type != SAE_TYPE_HALF;
+  CUtensorMap pm;
+  if (!mma::encode_map(&pm, ws + p.p, bfloat, p.p_pitch, p.rows, p.parts, p.p_pitch, p.rows * p.p_pitch)) return SAE_ERR_CUDA;
+  int rc = gather<true>(d, p, a, ws, st);
+  g.cols = p.z.cols; g.bfloat = bfloat; g.seg = segments(p.parts);
+  g.counted = a.counted; g.classes = a.classes; g.features = a.features; g.rows = 128 * p.z.cg;
+  g.bias = d->has_bias ? a.bias_out : nullptr; g.lse = a.lse_g; g.g = a.g; g.at = a.at;
+  g.p = (unsigned short*)(ws + p.p); g.p_plane = p.rows * p.p_pitch; g.p_pitch = p.p_pitch; g.type = d->type;
+  g.bias_sums = dbias ? (float*)(ws + p.bias_sums) : nullptr;
+  ProductJob job = {};
+  job.bfloat = bfloat; job.seg = g.seg; job.a = pm; job.counted = a.counted; job.features = a.features; job.alpha = a.alpha; job.type = d->type;
+  const int clusters = sms / p.dx.cg, dx_across = (int)(up(d->features, p.dx.cols) / p.dx.cols);
+  for (int i = 0; i < p.pieces && rc == SAE_OK; ++i) {
+    const int start = i * p.piece, classes = (int)std::min<int64_t>(p.piece, d->classes - start);
+    g.start = start;
+    g.tiles = (classes + g.cols - 1) / g.cols;
+    const int64_t z_tiles = up(d->rows, g.rows) / g.rows * g.tiles;
+    if (z_tiles) rc = products(g, p.z, z_tiles, sms, st);
+    job.start = start;
+    job.classes = classes;
+    job.width = classes;
+    if (dbias && rc == SAE_OK)
+      rc = launch(k_ce_dbias, (classes + 31) / 32, CE_THREADS, st, false, (const float*)g.bias_sums, p.p_pitch, (const int*)a.counted, (const float*)a.alpha, classes, d->bias_type,
+                  (void*)((char*)dbias + (int64_t)start * bs));
+    if (dx && d->rows && rc == SAE_OK) {
+      job.dx = true; job.b = g.w; job.cols = p.dx.cols; job.rows = 128 * p.dx.cg; job.across = dx_across;
+      job.sums = (float*)(ws + p.dx_sums); job.sums_pitch = p.sums_pitch; job.room = p.dx_room; job.add = i > 0;
+      rc = products(job, p.dx, clusters, sms, st);
+    }
+    if (dweight && rc == SAE_OK) {
+      job.dx = false; job.b = g.x; job.cols = p.dw.cols; job.rows = 128 * p.dw.cg; job.across = (int)(up(d->features, p.dw.cols) / p.dw.cols);
+      job.out = dweight;
+      rc = products(job, p.dw, up(classes, job.rows) / job.rows * job.across, sms, st);
+    }
+  }
+  if (dx && d->rows && rc == SAE_OK) {
+    DxArgs x2 = {(const float*)(ws + p.dx_sums), a.counted, a.index, a.alpha, dx, p.sums_pitch, a.features, d->type, 128 * p.dx.cg, dx_across, clusters, p.dx_room};
+    rc = launch(k_ce_dx, up(d->rows * ((d->features + UNIT - 1) / UNIT), CE_CHUNK) / CE_CHUNK, CE_THREADS, st, false, x2);
+  }
+  return rc;
+}
+
+}  // extern "C"

@@ -165,4 +165,29 @@ template <int V> struct Per<V, false> {
   }
 };
 
+// Eight elements of a row, at any address; what lies behind the first n is zero.
+constexpr int UNIT = 8;
+template <typename T>
+__device__ __forceinline__ void load_unit(const T* p, int n, float (&v)[UNIT]) {
+  if (n == UNIT && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+    if constexpr (sizeof(T) == 4) {
+      Raw<T, 4> a, b;
+      a.load(p);
+      b.load(p + 4);
+      float f[4], g[4];
+      a.widen(f);
+      b.widen(g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { v[i] = f[i]; v[4 + i] = g[i]; }
+    } else {
+      Raw<T, 8> a;
+      a.load(p);
+      a.widen(v);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < UNIT; ++i) v[i] = i < n ? to_f(p[i]) : 0.0f;
+  }
+}
+
 }  // namespace sae

@@ -1,0 +1,503 @@
+"""Linear cross entropy against the definition in float64: values, gradients, rows without a target, targets that are none, masks by
+the bias, infinities, layouts, streams, captured graphs, refusals."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+from paper_2008_05823_b200 import binding as sb
+from paper_2008_05823_b200 import cross_entropy as ce
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+IGNORE = -100
+
+
+# ---- refusals, without a GPU --------------------------------------------------------------------------------------------------
+
+def desc(**kw):
+    base = dict(type=sb.TYPE_BFLOAT, bias_type=sb.TYPE_FLOAT, reduction=sb.REDUCE_MEAN, has_bias=0, rows=4, features=8, classes=5,
+                x_pitch=8, weight_pitch=8, ignore_index=-100)
+    return sb.SaeLinearCeDesc(**(base | kw))
+
+
+@pytest.mark.parametrize("bad", [dict(type=3), dict(type=-1), dict(bias_type=7, has_bias=1), dict(reduction=3), dict(rows=-1), dict(rows=(1 << 24) + 1),
+                                 dict(features=0), dict(features=(1 << 17) + 1, x_pitch=1 << 18, weight_pitch=1 << 18), dict(classes=0),
+                                 dict(classes=(1 << 24) + 1), dict(x_pitch=7), dict(weight_pitch=7)])
+def test_bad_descriptions_are_refused(bad):
+    L, p = sb.lib(), C.c_void_p(256)                       # never dereferenced
+    d = desc(**bad)
+    assert L.sae_linear_ce_workspace(C.byref(d), p, 0) == -1
+    assert L.sae_linear_ce_forward(C.byref(d), p, p, None, p, p, p, p, p, 1 << 30, None) == sb.ERR_INVALID_ARG
+    assert L.sae_linear_ce_backward(C.byref(d), p, p, p, None, p, p, p, p, p, None, p, 1 << 30, None) == sb.ERR_INVALID_ARG
+
+
+def test_null_and_misaligned_pointers_are_refused():
+    L, p, odd = sb.lib(), C.c_void_p(256), C.c_void_p(257)
+    d, withbias = desc(), desc(has_bias=1)
+    good = [p, p, None, p, p, p, p, p]
+    for i in (0, 1, 3, 4, 5, 6, 7):
+        for v in (None, odd):
+            args = list(good)
+            args[i] = v
+            assert L.sae_linear_ce_forward(C.byref(d), *args, 1 << 30, None) == sb.ERR_INVALID_ARG, (i, v)
+    assert L.sae_linear_ce_forward(C.byref(withbias), *good, 1 << 30, None) == sb.ERR_INVALID_ARG
+    assert L.sae_linear_ce_forward(None, *good, 1 << 30, None) == sb.ERR_INVALID_ARG
+    good = [p, p, p, None, p, p, p, p, p, None, p]
+    for i in (0, 1, 2, 4, 5, 6, 10):
+        for v in (None, odd):
+            args = list(good)
+            args[i] = v
+            assert L.sae_linear_ce_backward(C.byref(d), *args, 1 << 30, None) == sb.ERR_INVALID_ARG, (i, v)
+    for i in (7, 8):
+        args = list(good)
+        args[i] = odd
+        assert L.sae_linear_ce_backward(C.byref(d), *args, 1 << 30, None) == sb.ERR_INVALID_ARG
+    args = list(good)
+    args[9] = p                                             # a bias gradient without a bias
+    assert L.sae_linear_ce_backward(C.byref(d), *args, 1 << 30, None) == sb.ERR_INVALID_ARG
+
+
+def test_module_arguments():
+    with pytest.raises(ValueError):
+        ce.LinearCrossEntropy(0, 3)
+    with pytest.raises(ValueError):
+        ce.LinearCrossEntropy(3, 3, reduction="max")
+    m = ce.LinearCrossEntropy(6, 3)
+    assert m.logits(torch.ones(2, 6)).shape == (2, 3) and ce.LinearCrossEntropy(6, 3, bias=False).bias is None
+
+
+def test_host_tensors_are_refused():
+    x, w, t = torch.ones(4, 8), torch.ones(5, 8), torch.zeros(4, dtype=torch.long)
+    with pytest.raises(ValueError):
+        ce.linear_cross_entropy_forward(x, w, t)
+    with pytest.raises(ValueError):
+        ce.linear_cross_entropy(x, w, t, reduction="max")
+
+
+# ---- the definition ---------------------------------------------------------------------------------------------------------------
+
+def data(n, d, v, dtype, bias=False, ignored=0.0, seed=0, scale=1.5):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((n, d), device="cuda", generator=gen).to(dtype)
+    w = (torch.randn((v, d), device="cuda", generator=gen) * scale / math.sqrt(d)).to(dtype)
+    b = (0.5 * torch.randn(v, device="cuda", generator=gen)).to(dtype) if bias else None
+    t = torch.randint(v, (n,), device="cuda", generator=gen)
+    t[torch.rand(n, device="cuda", generator=gen) < ignored] = IGNORE
+    return x, w, t, b
+
+
+class Exact:
+    """Everything in float64, and how far a result may be off.
+
+    u: half a step of the type.  dz: of a logit: every product of 16-bit values is exact in float; the sum of d terms loses at most one
+    step 2^-23 of the sum of magnitudes for each 16 terms and for the joins (float32: parts leave out terms below 2^-23 of a product).
+    The softmax adds the rounding of (z - m) log2(e) and of the exponential, 2^-22 (2 + |z|), and of the sums, 2^-24 for each
+    term that a thread adds.  p is rounded to the type once, the results once."""
+
+    def __init__(self, x, w, t, b, reduction, dloss=None):
+        self.dtype, used = x.dtype, t != IGNORE
+        x, w = x.double(), w.double()
+        b = None if b is None else b.double()
+        z = x @ w.t() + (0 if b is None else b)
+        self.lse = torch.where(used, torch.logsumexp(z, 1), 0.0)
+        rows = torch.where(used, self.lse - z.gather(1, torch.where(used, t, 0)[:, None])[:, 0], 0.0)
+        self.count = int(used.sum())
+        self.loss = {"none": rows, "sum": rows.sum(), "mean": rows.sum() / self.count if self.count else rows.sum() * math.nan}[reduction]
+        n, d = x.shape
+        v = len(w)
+        mags = (x.abs() @ w.abs().t() + (0 if b is None else b.abs())).amax(1)
+        self.dz = (d / 16 + 8) * 2.0 ** -23 * mags + 2.0 ** -22 * (2 + z.abs().amax(1)) + (v / 64 + 64) * 2.0 ** -24
+        self.dloss_rows = 2 * self.dz
+        self.loss_off = {"none": self.dloss_rows, "sum": self.dloss_rows[used].sum() + 2.0 ** -23 * rows.abs().sum(),
+                         "mean": (self.dloss_rows[used].sum() + 2.0 ** -23 * rows.abs().sum()) / max(1, self.count)}[reduction]
+        if dloss is None:
+            return
+        g = dloss.double() if reduction == "none" else dloss.double().expand(n) / (self.count if reduction == "mean" else 1)
+        p = torch.exp(z - self.lse[:, None])
+        both = p.clone()
+        r = torch.arange(n, device="cuda")[used]
+        p[r, t[used]] -= 1
+        both[r, t[used]] += 1                            # what rounding before the subtraction is relative to
+        g = torch.where(used, g, 0.0)[:, None]
+        p, both = p * g, both * g.abs()
+        u = 0.0 if self.dtype == torch.float32 else torch.finfo(self.dtype).eps / 2
+        # a float16 p is scaled by 2^15 over the largest factor: half of its smallest step is 2^-25
+        floor = 2.0 ** -40 * g.abs().max() if self.dtype == torch.float16 else 0.0
+        dp = p.abs() * u + both * (2 * self.dz[:, None] + 2.0 ** -21) + floor
+        dp = torch.where(used[:, None], dp, 0.0)
+        end = torch.finfo(self.dtype).eps / 2
+        tiny = torch.finfo(self.dtype).smallest_normal * torch.finfo(self.dtype).eps
+
+        def off(result, s):
+            return result.abs() * end + s * (1 + end) + tiny
+        self.dx, self.dw, self.db = p @ w, p.t() @ x, p.sum(0)
+        self.dx_off = off(self.dx, dp @ w.abs() + (v / 16 + 16) * 2.0 ** -23 * (p.abs() @ w.abs()))
+        self.dw_off = off(self.dw, dp.t() @ x.abs() + (n / 16 + 16) * 2.0 ** -23 * (p.abs().t() @ x.abs()))
+        self.db_off = off(self.db, dp.sum(0) + 40 * 2.0 ** -24 * p.abs().sum(0))
+
+
+def near(got, want, off, what):
+    assert got.shape == want.shape, what
+    bad = ~((got.double() - want).abs() <= off)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()}, worst {float(((got.double() - want).abs() / off).max())} of what is allowed"
+
+
+def check(x, w, t, b, reduction, dloss):
+    loss, lse, count = ce.linear_cross_entropy_forward(x, w, t, b, IGNORE, reduction)
+    e = Exact(x, w, t, b, reduction, dloss)
+    assert int(count) == e.count
+    near(loss, e.loss, e.loss_off, "loss")
+    near(lse, e.lse, torch.where(t != IGNORE, e.dloss_rows, 0.0), "lse")
+    dx, dw, db = ce.linear_cross_entropy_backward(dloss, x, w, t, lse, count, b, IGNORE, reduction)
+    assert dx.dtype == dw.dtype == x.dtype
+    near(dx, e.dx, e.dx_off, "dx")
+    near(dw, e.dw, e.dw_off, "dweight")
+    if b is not None:
+        off = e.db_off + e.db.abs() * (torch.finfo(b.dtype).eps / 2)
+        near(db, e.db, off, "dbias")
+    else:
+        assert db is None
+
+
+SIZES = [(1, 1, 1), (1, 8, 2), (2, 3, 5), (5, 64, 10), (31, 65, 63), (33, 40, 129), (127, 128, 64), (128, 64, 256), (129, 100, 257), (257, 77, 1000),
+         (512, 192, 2049), (1000, 515, 333), (64, 2048, 1000), (16, 4096, 70), (3, 24, 20000), (2100, 16, 40)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d,v", SIZES)
+def test_values_and_gradients(n, d, v, dtype):
+    for i, (bias, ignored, reduction) in enumerate([(False, 0.0, "mean"), (True, 0.3, "none"), (True, 0.0, "sum")]):
+        x, w, t, b = data(n, d, v, DTYPES[dtype], bias, ignored, seed=n + i)
+        dloss = torch.rand(n, device="cuda") - 0.3 if reduction == "none" else torch.tensor(0.7, device="cuda")
+        if int((t != IGNORE).sum()) == 0:
+            t[0] = v - 1
+        check(x, w, t, b, reduction, dloss)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,n,d,v,ignored", [("bf16", 4096, 256, 9000, 0.0), ("bf16", 20000, 64, 3000, 0.85), ("f16", 3000, 640, 7001, 0.1),
+                                                 ("f32", 2000, 256, 3000, 0.2), ("bf16", 40000, 32, 300, 0.5), ("bf16", 9000, 128, 20000, 0.0)])
+def test_large(dtype, n, d, v, ignored):
+    """Pairs of blocks with one tile, several pieces of the classes, rows counted in two steps."""
+    x, w, t, b = data(n, d, v, DTYPES[dtype], dtype != "bf16", ignored, seed=3)
+    check(x, w, t, b, "mean", torch.tensor(1.0, device="cuda"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_layouts(dtype):
+    """Slices of wider tensors, odd offsets, an expanded row, transposed storage, more dimensions: the bits of the plain tensors."""
+    x, w, t, b = data(96, 72, 200, DTYPES[dtype], True, 0.2, seed=5)
+    loss, lse, count = ce.linear_cross_entropy_forward(x, w, t, b)
+    one = torch.tensor(1.0, device="cuda")
+    grads = ce.linear_cross_entropy_backward(one, x, w, t, lse, count, b)
+
+    def wide(a, extra, at):
+        big = a.new_full((a.shape[0], a.shape[1] + extra), math.nan)
+        big[:, at:at + a.shape[1]] = a
+        return big[:, at:at + a.shape[1]]
+
+    def shifted(a):
+        flat = a.new_empty(a.numel() + 1)
+        flat[1:] = a.reshape(-1)
+        return flat[1:].view(a.shape)
+    for xx in (x, wide(x, 8, 0), wide(x, 37, 5), shifted(x), x.t().contiguous().t()):
+        for ww in (w, wide(w, 16, 8), wide(w, 3, 1), shifted(w), w.t().contiguous().t()):
+            got = ce.linear_cross_entropy_forward(xx, ww, t, b)
+            assert torch.equal(got[0], loss) and torch.equal(got[1], lse)
+            again = ce.linear_cross_entropy_backward(one, xx, ww, t, got[1], got[2], b)
+            assert all(torch.equal(p, q) for p, q in zip(grads, again))
+    t2 = torch.stack([t, t], 1)[:, 0]
+    assert torch.equal(ce.linear_cross_entropy_forward(x, w, t2, b)[0], loss)
+    x3 = x.view(4, 24, 72)
+    rows, lse3, count3 = ce.linear_cross_entropy_forward(x3, w, t.view(4, 24), b, reduction="none")
+    assert rows.shape == lse3.shape == (4, 24)
+    dx3 = ce.linear_cross_entropy_backward(torch.ones_like(rows), x3, w, t.view(4, 24), lse3, count3, b, reduction="none")[0]
+    assert dx3.shape == x3.shape
+    same = x[:1].expand(96, 72)
+    assert torch.equal(ce.linear_cross_entropy_forward(same, w, t, b)[0], ce.linear_cross_entropy_forward(same.contiguous(), w, t, b)[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_without_a_target_may_hold_anything(dtype):
+    """NaN and infinities there reach nothing; the results are the bits of the remaining rows alone."""
+    x, w, t, b = data(300, 40, 90, DTYPES[dtype], True, 0.5, seed=7)
+    used = t != IGNORE
+    one = torch.tensor(1.0, device="cuda")
+    small = ce.linear_cross_entropy_forward(x[used], w, t[used], b)
+    want = ce.linear_cross_entropy_backward(one, x[used], w, t[used], small[1], small[2], b)
+    bad = x.clone()
+    bad[~used] = torch.tensor([math.nan, math.inf, -math.inf, 1.0], device="cuda").to(x.dtype).repeat(10)
+    loss, lse, count = ce.linear_cross_entropy_forward(bad, w, t, b)
+    dx, dw, db = ce.linear_cross_entropy_backward(one, bad, w, t, lse, count, b)
+    assert torch.equal(loss, small[0]) and torch.equal(lse[used], small[1]) and not lse[~used].any()
+    assert torch.equal(dx[used], want[0]) and not dx[~used].any()
+    assert torch.equal(dw, want[1]) and torch.equal(db, want[2])
+    rows = ce.linear_cross_entropy_forward(bad, w, t, b, reduction="none")[0]
+    assert not rows[~used].any()
+
+
+@pytest.mark.gpu
+def test_nothing_to_count():
+    x, w, t, b = data(50, 16, 30, torch.bfloat16, True)
+    t.fill_(IGNORE)
+    one = torch.tensor(1.0, device="cuda")
+    for reduction, want in (("mean", math.nan), ("sum", 0.0)):
+        loss, lse, count = ce.linear_cross_entropy_forward(x, w, t, b, reduction=reduction)
+        assert int(count) == 0 and (math.isnan(float(loss)) if math.isnan(want) else float(loss) == want)
+        assert not any(g.any() for g in ce.linear_cross_entropy_backward(one, x, w, t, lse, count, b, reduction=reduction))
+        empty = ce.linear_cross_entropy_forward(x[:0], w, t[:0], b, reduction=reduction)
+        assert int(empty[2]) == 0 and (math.isnan(float(empty[0])) if math.isnan(want) else float(empty[0]) == want)
+        dx, dw, db = ce.linear_cross_entropy_backward(one, x[:0], w, t[:0], empty[1], empty[2], b, reduction=reduction)
+        assert dx.shape == (0, 16) and not dw.any() and not db.any()
+    rows = ce.linear_cross_entropy_forward(x[:0], w, t[:0], b, reduction="none")
+    assert rows[0].shape == (0,)
+    dx, dw, db = ce.linear_cross_entropy_backward(rows[0], x[:0], w, t[:0], rows[1], rows[2], b, reduction="none")
+    assert not dw.any() and not db.any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_targets_that_are_none(dtype):
+    """A target outside the classes makes its own loss and dx NaN and the sums over rows NaN; other rows stay."""
+    x, w, t, b = data(40, 24, 17, DTYPES[dtype], False)
+    want = ce.linear_cross_entropy_forward(x, w, t, reduction="none")[0]
+    ones = torch.ones(40, device="cuda")
+    good = ce.linear_cross_entropy_forward(x, w, t, reduction="none")
+    dx0 = ce.linear_cross_entropy_backward(ones, x, w, t, good[1], good[2], reduction="none")[0]
+    for value in (17, -1, 2 ** 40, -2 ** 40):
+        bad = t.clone()
+        bad[3] = value
+        loss, lse, count = ce.linear_cross_entropy_forward(x, w, bad, reduction="none")
+        others = torch.arange(40, device="cuda") != 3
+        assert int(count) == 40 and torch.isnan(loss[3]) and torch.equal(loss[others], want[others])
+        dx, dw, _ = ce.linear_cross_entropy_backward(ones, x, w, bad, lse, count, reduction="none")
+        assert torch.isnan(dx[3]).all() and torch.equal(dx[others], dx0[others]) and torch.isnan(dw).all()
+        assert torch.isnan(ce.linear_cross_entropy_forward(x, w, bad)[0])
+    assert torch.equal(ce.linear_cross_entropy_forward(x, w, t, ignore_index=10 ** 12, reduction="none")[0], want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_classes_masked_by_the_bias(dtype):
+    """A bias of -inf takes a class out: the others' results are those without it (whole tiles masked among them); a masked target's
+    loss is infinite; a row that loses every class is NaN."""
+    n, d, v = 70, 32, 700
+    x, w, t, b = data(n, d, v, DTYPES[dtype], True, seed=2)
+    keep = torch.ones(v, dtype=torch.bool, device="cuda")
+    keep[64:400] = False
+    keep[699] = False
+    masked = b.clone()
+    masked[~keep] = -math.inf
+    names = keep.nonzero()[:, 0]
+    t = names[t % len(names)]
+    small_t = torch.cumsum(keep, 0)[t] - 1
+    loss, lse, count = ce.linear_cross_entropy_forward(x, w, t, masked, reduction="none")
+    e = Exact(x, w[keep], small_t, b[keep], "none", torch.ones(n, device="cuda"))
+    near(loss, e.loss, e.loss_off, "loss")
+    dx, dw, db = ce.linear_cross_entropy_backward(torch.ones(n, device="cuda"), x, w, t, lse, count, masked, reduction="none")
+    near(dx, e.dx, e.dx_off, "dx")
+    near(dw[keep], e.dw, e.dw_off, "dweight")
+    assert not dw[~keep].any() and not db[~keep].any()
+    t[5] = 100
+    assert float(ce.linear_cross_entropy_forward(x, w, t, masked, reduction="none")[0][5]) == math.inf
+    masked.fill_(-math.inf)
+    assert torch.isnan(ce.linear_cross_entropy_forward(x, w, t, masked, reduction="none")[0]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+def test_values_that_are_not_finite_stay_in_their_row(dtype, value):
+    x, w, t, b = data(200, 24, 333, DTYPES[dtype], True, seed=4)
+    want = ce.linear_cross_entropy_forward(x, w, t, b, reduction="none")[0]
+    x[77, 5] = value
+    loss, lse, count = ce.linear_cross_entropy_forward(x, w, t, b, reduction="none")
+    others = torch.arange(200, device="cuda") != 77
+    assert torch.equal(loss[others], want[others]) and torch.isnan(loss[77])
+    dx = ce.linear_cross_entropy_backward(torch.ones(200, device="cuda"), x, w, t, lse, count, b, reduction="none")[0]
+    assert torch.isfinite(dx[others]).all() and torch.isnan(dx[77]).any()
+
+
+@pytest.mark.gpu
+def test_logits_far_apart():
+    """Differences of thousands: nothing overflows, the softmax is one of the largest logits alone; equal logits give log(classes).
+    511 and 512 are the same in bfloat16 (8 bits: steps of 2 from 256 on, 511 to the even 512), so the largest is there twice."""
+    v = 513
+    w = torch.zeros((v, 8), device="cuda", dtype=torch.bfloat16)
+    w[:, 0] = torch.arange(v, device="cuda").to(torch.bfloat16)
+    x = torch.zeros((4, 8), device="cuda", dtype=torch.bfloat16)
+    x[:, 0] = torch.tensor([64.0, -64.0, 0.0, 2.0 ** 100], device="cuda").to(torch.bfloat16)
+    t = torch.tensor([512, 0, 7, 512], device="cuda")
+    loss = ce.linear_cross_entropy_forward(x, w, t, reduction="none")[0]
+    two = (2 + math.log(2)) * 2.0 ** -22
+    assert float(w[511, 0]) == 512 and float(loss[1]) == 0
+    assert abs(float(loss[0]) - math.log(2)) <= two and abs(float(loss[3]) - math.log(2)) <= two
+    assert abs(float(loss[2]) - math.log(v)) <= (2 + math.log(v)) * 2.0 ** -22
+    t = torch.tensor([0, 512, 7, 0], device="cuda")
+    loss = ce.linear_cross_entropy_forward(x, w, t, reduction="none")[0]
+    assert abs(float(loss[0]) - 64.0 * 512 - math.log(2)) <= 64.0 * 512 * 2.0 ** -22
+    assert float(loss[1]) == 64.0 * 512 and float(loss[3]) == 512 * 2.0 ** 100
+
+
+@pytest.mark.gpu
+def test_same_bits_again():
+    for dtype, n in (("bf16", 3000), ("f32", 500)):
+        x, w, t, b = data(n, 200, 5000, DTYPES[dtype], True, 0.1, seed=9)
+        first = None
+        for _ in range(3):
+            out = ce.linear_cross_entropy_forward(x, w, t, b)
+            out += ce.linear_cross_entropy_backward(torch.tensor(1.0, device="cuda"), x, w, t, out[1], out[2], b)
+            first = first or out
+            assert all(torch.equal(p, q) for p, q in zip(first, out))
+
+
+@pytest.mark.gpu
+def test_wanted_gradients_only():
+    x, w, t, b = data(60, 40, 100, torch.bfloat16, True, 0.1)
+    one = torch.tensor(1.0, device="cuda")
+    loss, lse, count = ce.linear_cross_entropy_forward(x, w, t, b)
+    whole = ce.linear_cross_entropy_backward(one, x, w, t, lse, count, b)
+    for need in ((True, False, False), (False, True, False), (False, False, True), (False, False, False)):
+        got = ce.linear_cross_entropy_backward(one, x, w, t, lse, count, b, need_x=need[0], need_weight=need[1], need_bias=need[2])
+        for g, f, n in zip(got, whole, need):
+            assert (g is None) if not n else torch.equal(g, f)
+
+
+# ---- autograd -------------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
+def test_autograd_is_the_two_calls(reduction):
+    x, w, t, b = data(90, 48, 120, torch.float32, True, 0.2)
+    p = [v.clone().requires_grad_() for v in (x, w, b)]
+    loss = ce.linear_cross_entropy(p[0], p[1], t, p[2], reduction=reduction)
+    weights = torch.rand_like(loss)
+    (loss * weights).sum().backward()
+    fwd = ce.linear_cross_entropy_forward(x, w, t, b, reduction=reduction)
+    want = ce.linear_cross_entropy_backward(weights, x, w, t, fwd[1], fwd[2], b, reduction=reduction)
+    assert torch.equal(loss, fwd[0]) and all(torch.equal(a.grad, g) for a, g in zip(p, want))
+
+
+@pytest.mark.gpu
+def test_differences():
+    """The gradient along a random direction against central differences of the float64 loss's own value as the kernel gives it: step h
+    leaves h^2 / 6 of the third derivative (at most 2 |dz|^3 of the softmax) and the loss's own error over h."""
+    x, w, t, b = data(40, 32, 60, torch.float32, True, 0.1, seed=11)
+    one = torch.tensor(1.0, device="cuda")
+    loss, lse, count = ce.linear_cross_entropy_forward(x, w, t, b)
+    grads = ce.linear_cross_entropy_backward(one, x, w, t, lse, count, b)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    h = 2.0 ** -6
+    for i, base in enumerate((x, w, b)):
+        direction = torch.randn(base.shape, device="cuda", generator=gen) * (0.1 if i < 2 else 1.0)
+        values = []
+        for sign in (1, -1):
+            args = [x, w, b]
+            args[i] = base + sign * h * direction
+            values.append(float(ce.linear_cross_entropy_forward(args[0], args[1], t, args[2])[0]))
+        slope = (values[0] - values[1]) / (2 * h)
+        want = float((grads[i].double() * direction.double()).sum())
+        moved = (direction @ w.t() if i == 0 else x @ direction.t() if i == 1 else direction.expand(40, 60)).abs().amax(1).double()
+        e = Exact(x, w, t, b, "mean")
+        allowed = float((h * h / 6 * 2 * (2 * moved) ** 3).mean()) + float(e.loss_off) / h + abs(want) * 1e-4
+        assert abs(slope - want) <= allowed, (i, slope, want, allowed)
+
+
+@pytest.mark.gpu
+def test_module_under_autocast():
+    torch.manual_seed(0)
+    m = ce.LinearCrossEntropy(64, 50).cuda()
+    x, t = torch.randn(30, 64, device="cuda"), torch.randint(50, (30,), device="cuda")
+    with torch.autocast("cuda", torch.bfloat16):
+        loss = m(x, t)
+    loss.backward()
+    assert m.weight.grad.dtype == torch.float32 and loss.dtype == torch.float32
+    xb, wb = x.bfloat16(), m.weight.detach().bfloat16()
+    fwd = ce.linear_cross_entropy_forward(xb, wb, t, m.bias.detach())
+    want = ce.linear_cross_entropy_backward(torch.tensor(1.0, device="cuda"), xb, wb, t, fwd[1], fwd[2], m.bias.detach())
+    assert torch.equal(loss, fwd[0]) and torch.equal(m.weight.grad, want[1].float()) and torch.equal(m.bias.grad, want[2])
+
+
+@pytest.mark.gpu
+def test_a_changed_input_is_noticed():
+    x, w, t, _ = data(20, 16, 30, torch.float32)
+    w.requires_grad_()
+    loss = ce.linear_cross_entropy(x, w, t)
+    with torch.no_grad():
+        w.mul_(2)
+    with pytest.raises(RuntimeError):
+        loss.backward()
+
+
+# ---- streams, graphs, devices ------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+def test_on_another_stream_and_captured():
+    x, w, t, b = data(700, 96, 3000, torch.bfloat16, True, 0.3, seed=6)
+    one = torch.tensor(1.0, device="cuda")
+
+    def both():
+        loss, lse, count = ce.linear_cross_entropy_forward(x, w, t, b)
+        return (loss,) + ce.linear_cross_entropy_backward(one, x, w, t, lse, count, b)
+    want = both()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = both()
+    torch.cuda.current_stream().wait_stream(s)
+    assert all(torch.equal(p, q) for p, q in zip(want, got))
+    graphs, outs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    for g in graphs:
+        with torch.cuda.graph(g):
+            outs.append(both())
+    x2, w2, t2, b2 = data(700, 96, 3000, torch.bfloat16, True, 0.6, seed=16)       # other rows take part
+    for a, c in ((x, x2), (w, w2), (t, t2), (b, b2)):
+        a.copy_(c)
+    for g in graphs + graphs:
+        g.replay()
+    want = both()
+    for out in outs:
+        assert all(torch.equal(p, q) for p, q in zip(want, out))
+
+
+@pytest.mark.gpu
+def test_two_calls_at_once():
+    a, c = data(2000, 128, 4000, torch.bfloat16, True, 0.1, seed=1), data(1500, 256, 3000, torch.bfloat16, False, 0.2, seed=2)
+    want = [ce.linear_cross_entropy_forward(*d)[0] for d in (a, c)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, d in enumerate((a, c)):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(ce.linear_cross_entropy_forward(*d)[0])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, want[i]) for g in got[i])
+
+
+@pytest.mark.gpu
+def test_bad_calls_are_refused():
+    x, w, t, b = data(8, 16, 10, torch.bfloat16, True)
+    f = ce.linear_cross_entropy_forward
+    for args in ((x.cpu(), w, t), (x, w.cpu(), t), (x, w, t.cpu()), (x.double(), w.double(), t), (x, w.float(), t), (x, w[:, :8], t), (x, w, t.int()), (x, w, t[:4]),
+                 (x, w, t, b[:4]), (x, w, t, b.double()), (x, w, t, b.cpu()), (x, w, t, b.repeat(2)[::2]), (x, w[0], t), (x[:, :0], w[:, :0], t), (x, w[:0], t)):
+        with pytest.raises(ValueError):
+            f(*args)
+    loss, lse, count = f(x, w, t, b)
+    one = torch.ones((), device="cuda")
+    g = ce.linear_cross_entropy_backward
+    for args in ((one.double(), x, w, t, lse, count, b), (torch.ones(8, device="cuda"), x, w, t, lse, count, b), (one, x, w, t, lse[:4], count, b),
+                 (one, x, w, t, lse.double(), count, b), (one, x, w, t, lse, count.float(), b), (one.cpu(), x, w, t, lse, count, b)):
+        with pytest.raises(ValueError):
+            g(*args)
+    L = sb.lib()
+    d = desc(rows=8, features=16, classes=10, x_pitch=16, weight_pitch=16)
+    need = L.sae_linear_ce_workspace(C.byref(d), w.data_ptr(), 0)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    args = [x.data_ptr(), w.data_ptr(), None, t.data_ptr(), loss.data_ptr(), lse.data_ptr(), count.data_ptr(), ws.data_ptr()]
+    assert need > 0 and L.sae_linear_ce_forward(C.byref(d), *args, need - 1, None) == sb.ERR_INVALID_ARG
