@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_rows(const __grid_constant__ 
 // ---- the loss ------------------------------------------------------------------------------------------------------------
 // Runs of tiles: row blocks one after another, each over all classes; a cluster takes an equal share of this list and leaves one run
 // (maximum, sum) for each row block that it touches.
-struct LossJob {
+struct LossJob : mma::Plain {
   int cols;
   bool bfloat;
   mma::Segments seg;
@@ -259,7 +259,7 @@ struct LossJob {
   float2* runs;
 
   struct Local { long long first, last; int wide, blocks, clusters, id; };
-  __device__ __forceinline__ Local begin(int cluster, int clusters) const {
+  __device__ __forceinline__ Local begin(const Shared&, int cluster, int clusters) const {
     Local l;
     l.id = cluster;
     l.wide = (classes + cols - 1) / cols;
@@ -278,7 +278,7 @@ struct LossJob {
     t.b = &this->w;
     t.row = t.a_row = t.group * rows;
     t.col = t.b_row = (int)(w - (long long)t.group * l.wide) * cols;
-    t.a_plane = t.b_plane = t.a_k = t.b_k = 0;
+    t.a_plane = t.b_plane = t.a_k = t.b_k = t.a_turn = t.b_turn = 0;
     t.a_rows_first = t.b_rows_first = false;
     t.blocks = (features + mma::BLOCK_K - 1) / mma::BLOCK_K;
     return true;
@@ -294,7 +294,8 @@ struct LossJob {
     const int row, half;
     int block, cls;
     float m, s;
-    __device__ __forceinline__ Epilogue(const LossJob& j, const Local& l, int r, int h) : job(j), l(l), row(r), half(h), block(-1), cls(-1) {}
+    __device__ __forceinline__ Epilogue(const LossJob& j, const Local& l, int r, int h, u32) : job(j), l(l), row(r), half(h), block(-1), cls(-1) {}
+    __device__ __forceinline__ void prepare(const mma::Tile&, int, mma::Control*) {}
     __device__ __forceinline__ void finish() {
       if (block < 0 || block * job.rows + row >= *job.counted) return;
       const long long total = (long long)l.blocks * l.wide;
@@ -424,7 +425,7 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_join(const __grid_constant__ 
 
 // ---- the gradients --------------------------------------------------------------------------------------------------------
 // p of one piece of the classes.
-struct GradJob {
+struct GradJob : mma::Plain {
   int cols;
   bool bfloat;
   mma::Segments seg;
@@ -439,7 +440,7 @@ struct GradJob {
   float* bias_sums;                              // [rows / 32][p_pitch], NULL: not wanted
 
   struct Local { int first, step, blocks; };
-  __device__ __forceinline__ Local begin(int cluster, int clusters) const { return {cluster, clusters, (*counted + rows - 1) / rows}; }
+  __device__ __forceinline__ Local begin(const Shared&, int cluster, int clusters) const { return {cluster, clusters, (*counted + rows - 1) / rows}; }
   __device__ __forceinline__ bool tile(Local& l, int i, mma::Tile& t) const {
     const long long n = l.first + (long long)i * l.step;
     if (n >= (long long)l.blocks * tiles) return false;
@@ -449,7 +450,7 @@ struct GradJob {
     t.b_row = start + t.col;
     t.a = &x;
     t.b = &w;
-    t.a_plane = t.b_plane = t.a_k = t.b_k = 0;
+    t.a_plane = t.b_plane = t.a_k = t.b_k = t.a_turn = t.b_turn = 0;
     t.a_rows_first = t.b_rows_first = false;
     t.blocks = (features + mma::BLOCK_K - 1) / mma::BLOCK_K;
     return true;
@@ -457,7 +458,8 @@ struct GradJob {
   struct Epilogue {
     const GradJob& job;
     const int row, half;
-    __device__ __forceinline__ Epilogue(const GradJob& j, const Local&, int r, int h) : job(j), row(r), half(h) {}
+    __device__ __forceinline__ Epilogue(const GradJob& j, const Local&, int r, int h, u32) : job(j), row(r), half(h) {}
+    __device__ __forceinline__ void prepare(const mma::Tile&, int, mma::Control*) {}
     __device__ __forceinline__ void finish() {}
     __device__ __forceinline__ void tile(const mma::Tile& t, const mma::Sums& sums) {
       const int r = t.row + row;
@@ -541,7 +543,7 @@ __device__ __host__ inline int dx_splits(int blocks, int tiles_across, int clust
 }
 
 // dx's sums (p w, float, added up over the pieces) and dweight of a piece (p' x).
-struct ProductJob {
+struct ProductJob : mma::Plain {
   int cols;
   bool bfloat;
   mma::Segments seg;
@@ -559,7 +561,7 @@ struct ProductJob {
   const float* alpha;
 
   struct Local { int first, step, blocks, splits, count; };
-  __device__ __forceinline__ Local begin(int cluster, int clusters) const {
+  __device__ __forceinline__ Local begin(const Shared&, int cluster, int clusters) const {
     Local l = {cluster, clusters, 0, 1, *counted};
     l.blocks = ((dx ? l.count : classes) + rows - 1) / rows;
     if (dx) l.splits = dx_splits(l.blocks, across, clusters, l.blocks ? room / l.blocks : 1);
@@ -574,7 +576,7 @@ struct ProductJob {
     t.col = t.b_row = (int)(n - (long long)q * across) * cols;
     t.a = &a;
     t.b = &b;
-    t.a_plane = t.b_plane = 0;
+    t.a_plane = t.b_plane = t.a_turn = t.b_turn = 0;
     t.b_rows_first = true;
     t.a_rows_first = !dx;
     const int all = ((dx ? width : l.count) + mma::BLOCK_K - 1) / mma::BLOCK_K;
@@ -590,7 +592,8 @@ struct ProductJob {
     const int row, half;
     const float alpha;
     const int limit;
-    __device__ __forceinline__ Epilogue(const ProductJob& j, const Local& l, int r, int h) : job(j), row(r), half(h), alpha(j.dx ? 1.0f : *j.alpha), limit(j.dx ? l.count : j.classes) {}
+    __device__ __forceinline__ Epilogue(const ProductJob& j, const Local& l, int r, int h, u32) : job(j), row(r), half(h), alpha(j.dx ? 1.0f : *j.alpha), limit(j.dx ? l.count : j.classes) {}
+    __device__ __forceinline__ void prepare(const mma::Tile&, int, mma::Control*) {}
     __device__ __forceinline__ void finish() {}
     __device__ __forceinline__ void tile(const mma::Tile& t, const mma::Sums& sums) {
       const int r = t.row + row, w = job.cols / 2;

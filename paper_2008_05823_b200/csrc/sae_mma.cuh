@@ -9,9 +9,9 @@
 //
 // Tile: 128 * CG rows by 64, 128 or 256 columns.  CG = 2: the two thread blocks of a cluster share one tile; each loads its 128 rows of
 // A and its half of B, the tensor cores of both read both halves, so a byte that comes from L2 is used twice as often.
-// Warp 0 loads (TMA, boxes of 64 x 64 elements in 128-byte swizzled rows, a ring of six 32 KB stages), warp 1 issues the
-// products (one thread; in block 0 of a pair), warps 4 to 11 take the sums: warp w the lanes 32 (w % 4) .. + 31, which are the
-// tile's rows, and one half of the columns.  Sums are held twice (2 x 256 columns of the 512), so the products
+// Warps 0 and 3 load (TMA, boxes of 64 x 64 elements in 128-byte swizzled rows, a ring of 32 KB stages; warp 0 A, warp 3 B), warp 1 issues the
+// products (one thread; in block 0 of a pair), warps 4 and up take the sums: warp w the lanes 32 (w % 4) .. + 31, which are
+// the tile's rows, and one half of the columns.  Sums are held twice (2 x 256 columns of the 512), so the products
 // of the next tile run while a tile is taken out.
 //
 // The tensor cores cut off what a sum has below its last bit, at each of the products that it is made of, and a sum of a few
@@ -40,11 +40,16 @@ namespace mma {
 constexpr int BLOCK_K = 64;
 constexpr int BOX_ROWS = 64;
 constexpr u32 BOX_BYTES = BLOCK_K * BOX_ROWS * 2;
-constexpr int STAGES = 6;
 constexpr u32 STAGE_BYTES = 4 * BOX_BYTES;      // 128 rows of A, up to 128 of B
-constexpr u32 SMEM_BYTES = STAGES * STAGE_BYTES + 1024;
-constexpr int THREADS = 384;
 constexpr int EPI_WARP = 4, EPI_WARPS = 8;
+constexpr int MAX_STAGES = 6;
+// 8 warps take the sums out (16 were no faster).  A job that brings values in by copies has STAGING bytes for each of them, at the cost of stages.
+template <class Job>
+struct Room {
+  static constexpr int STAGES = Job::STAGING ? 4 : MAX_STAGES;
+  static constexpr int THREADS = 32 * (EPI_WARP + EPI_WARPS + Job::REPORTS);
+  static constexpr u32 BYTES = STAGES * STAGE_BYTES + EPI_WARPS * Job::STAGING + 1024;
+};
 constexpr u32 TMEM_COLUMNS = 512;
 constexpr u64 WAIT_NS = 2000000000ull, DRAIN_NS = 100000000ull;
 constexpr int MAX_SEGMENTS = 6;
@@ -63,6 +68,7 @@ struct Tile {
   int a_plane, b_plane;    // planes of part 0
   int a_k, b_k, blocks;    // first k in A and in B, blocks of 64 of them (0: all sums are zero)
   bool a_rows_first, b_rows_first;
+  int a_turn, b_turn;      // this many first blocks of k come from the transpose instead: (row, k) from (k, row), the other of K and rows first
   // for the epilogue
   int row, col;            // first output row and column
   int group, item;
@@ -76,8 +82,9 @@ struct Sums {
 };
 
 struct Control {
-  u64 full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drain;
+  u64 full[MAX_STAGES], empty[MAX_STAGES], acc_full[2], acc_empty[2], drain;
   u32 tmem, dead;
+  u32 ready, stored[EPI_WARPS];       // tiles whose operands were found ready; tiles that each epilogue warp has written
 };
 
 // ---- PTX --------------------------------------------------------------------------------------------------------------
@@ -94,13 +101,62 @@ __device__ __forceinline__ bool wait(u64* bar, u32 parity, u32* dead) {
   if (mbar_try(addr, parity)) return true;
   return wait_slow(addr, parity, dead, WAIT_NS);
 }
+// Waits until a counter that other blocks of the grid add to has reached a value.  (Polled by relaxed loads, one fence at the end: an
+// acquiring load throws L1 away each time and holds up the loads and stores of the whole SM.)
+__device__ __forceinline__ bool counter_reached(const u32* counter, u32 least) {
+  u32 v;
+  asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(counter) : "memory");
+  return (int)(v - least) >= 0;
+}
+static __device__ __noinline__ bool wait_counter(const u32* counter, u32 least, volatile u32* dead) {
+  const u64 t0 = global_ns();
+  while (!counter_reached(counter, least)) {
+    __nanosleep(64);
+    if (*dead) return false;
+    if (global_ns() - t0 > WAIT_NS) { *dead = 1; return false; }
+  }
+  asm volatile("fence.acq_rel.gpu;" ::: "memory");
+  return true;
+}
+__device__ __forceinline__ void add_counter(u32* counter) { asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory"); }
+// The same within a block.
+__device__ __forceinline__ void set_shared(u32* to, u32 v) { asm volatile("st.release.cta.shared::cta.u32 [%0], %1;" ::"r"(smem_u32(to)), "r"(v) : "memory"); }
+__device__ __forceinline__ bool shared_reached(u32* at, u32 least) {
+  u32 v;
+  asm volatile("ld.acquire.cta.shared::cta.u32 %0, [%1];" : "=r"(v) : "r"(smem_u32(at)) : "memory");
+  return (int)(v - least) >= 0;
+}
+static __device__ __noinline__ bool wait_shared_slow(u32* at, u32 least, volatile u32* dead) {
+  const u64 t0 = global_ns();
+  for (;;) {
+    for (int i = 0; i < 16; ++i) {
+      if (shared_reached(at, least)) return true;
+      __nanosleep(40);
+    }
+    if (*dead) return false;
+    if (global_ns() - t0 > WAIT_NS) { *dead = 1; return false; }
+  }
+}
+__device__ __forceinline__ bool wait_shared(u32* at, u32 least, u32* dead) { return shared_reached(at, least) || wait_shared_slow(at, least, dead); }
+// Between plain accesses and TMA's: whoever wrote, and whoever is going to load.
+__device__ __forceinline__ void fence_copies() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+// One lane of a warp whose lanes run together.  The roles that issue copies and products are whole warps with this around what
+// one thread does: a loop that only one lane runs has its operands moved one by one to the registers these instructions take
+// (890 cycles for the four products of a stage, of which the tensor cores need 512).
+__device__ __forceinline__ bool one_lane() {
+  u32 r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
 __device__ __forceinline__ u32 of_block0(u32 addr) {      // the address of block 0's copy of a shared variable
   u32 r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
   return r;
 }
+// (Relaxed: what it orders is tensor memory, read before; a release would first wait for the thread's stores to memory.)
 __device__ __forceinline__ void arrive_cluster(u32 addr) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -203,26 +259,39 @@ __device__ __forceinline__ void sums_of(const Sums& s, int c, float (&v)[32]) {
   }
 }
 
+// The columns of a tile that an epilogue warp takes.
+__device__ __forceinline__ int epilogue_width(int cols) { return cols / 2; }
+
 // ---- the kernel -----------------------------------------------------------------------------------------------------------
 // Job: int cols; bool bfloat; Segments seg;
-//      Local begin(cluster, clusters): a role's place in the list of tiles;  bool tile(local, i, Tile&): this cluster's i-th tile,
-//      asked for in order;  Epilogue(job, local, row of the tile, column half): tile(t, sums), finish()
+//      Shared, fill(shared): what the roles look up, in shared memory
+//      Local begin(shared, cluster, clusters): a role's place in the list of tiles;  bool tile(local, i, Tile&): this cluster's i-th
+//      tile, asked for in order
+//      Epilogue(job, local, row of the tile, which part of the columns, the warp's staging): prepare(t, number, control), while the sums are
+//      made;  tile(t, sums);  finish(), behind the last tile
+//      REPORTS: tiles depend on one another.  A warp of its own, the last, runs ahead with ready(local, t, dead), which waits until a tile's
+//      operands are there (false: gave up); report(local, t) is called by warp 2 when the block has written its part of a
+//      tile.  Both wait a microsecond or two for the memory; with the loading warps waiting themselves, 12 encoder layers took 1702 us, not 1601.
 // JOINED: sums are taken out every JOIN_BLOCKS blocks of k (job.cols <= 128).
 template <class Job, int CG, bool JOINED>
-__global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__ Job job) {
+__global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid_constant__ Job job) {
+  constexpr int STAGES = Room<Job>::STAGES;
   extern __shared__ unsigned char smem_raw[];
   __shared__ Control ctl;
+  __shared__ typename Job::Shared shared;
   const u32 tiles = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const u32 rank = CG == 2 ? cluster_rank() : 0;
   const int cluster = blockIdx.x / CG, clusters = gridDim.x / CG;
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(&ctl.full[i], 1); mbar_init(&ctl.empty[i], 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(&ctl.acc_full[i], 1); mbar_init(&ctl.acc_empty[i], EPI_WARPS * CG); }
     mbar_init(&ctl.drain, 1);
-    ctl.dead = 0;
+    ctl.dead = ctl.ready = 0;
+    for (int i = 0; i < EPI_WARPS; ++i) ctl.stored[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  job.fill(shared);
   if (warp == 2) tmem_alloc<CG>(&ctl.tmem);
   fence_before();
   __syncthreads();
@@ -231,15 +300,18 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
   let_next_start();
   wait_for_previous();
   const u32 tmem = ctl.tmem;
-  typename Job::Local local = job.begin(cluster, clusters);
+  typename Job::Local local = job.begin(shared, cluster, clusters);
   const int b_rows = job.cols / CG;               // rows of B that a block loads
 
-  if (warp == 0 && lane == 0) {
+  if (warp == 0 || warp == 3) {
     const u32 bytes = CG * (2 * BOX_BYTES + (u32)b_rows * BLOCK_K * 2);
     u32 n = 0;
     Tile t;
     bool ok = true;
     for (int i = 0; ok && job.tile(local, i, t); ++i) {
+      if constexpr (Job::REPORTS) {
+        if (!__all_sync(0xffffffffu, wait_shared(&ctl.ready, (u32)i + 1, &ctl.dead))) { ok = false; break; }
+      }
       const int a_row = t.a_row + (int)rank * 128, b_row = t.b_row + (int)rank * b_rows, run = JOINED ? JOIN_BLOCKS : t.blocks;
       for (int k0 = 0; k0 < t.blocks && ok; k0 += run) {
         const int k1 = JOINED ? min(k0 + run, t.blocks) : t.blocks;
@@ -247,66 +319,100 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
           const int za = t.a_plane + job.seg.a[s], zb = t.b_plane + job.seg.b[s];
           for (int kb = k0; kb < k1; ++kb, ++n) {
             const u32 stage = n % STAGES;
-            if (!wait(&ctl.empty[stage], ((n / STAGES) & 1) ^ 1, &ctl.dead)) { ok = false; break; }
+            if (!__all_sync(0xffffffffu, wait(&ctl.empty[stage], ((n / STAGES) & 1) ^ 1, &ctl.dead))) { ok = false; break; }
             const u32 at = tiles + stage * STAGE_BYTES;
             u32 bar = smem_u32(&ctl.full[stage]);
-            if (rank == 0) mbar_arrive_expect_tx(&ctl.full[stage], bytes);
             if constexpr (CG == 2) bar = of_block0(bar);
             const int ka = t.a_k + kb * BLOCK_K, kw = t.b_k + kb * BLOCK_K;
+            const bool a_rows_first = t.a_rows_first != (kb < t.a_turn), b_rows_first = t.b_rows_first != (kb < t.b_turn);
+            if (one_lane()) {
+              if (warp == 0) {
+                if (rank == 0) mbar_arrive_expect_tx(&ctl.full[stage], bytes);
 #pragma unroll
-            for (int r = 0; r < 128; r += BOX_ROWS)
-              load_box<CG>(at + r * BLOCK_K * 2, t.a, t.a_rows_first ? a_row + r : ka, t.a_rows_first ? ka : a_row + r, za, bar);
-            for (int r = 0; r < b_rows; r += BOX_ROWS)
-              load_box<CG>(at + 2 * BOX_BYTES + r * BLOCK_K * 2, t.b, t.b_rows_first ? b_row + r : kw, t.b_rows_first ? kw : b_row + r, zb, bar);
+                for (int r = 0; r < 128; r += BOX_ROWS)
+                  load_box<CG>(at + r * BLOCK_K * 2, t.a, a_rows_first ? a_row + r : ka, a_rows_first ? ka : a_row + r, za, bar);
+              } else {
+#pragma unroll
+                for (int r = 0; r < 128; r += BOX_ROWS)
+                  if (r < b_rows)
+                    load_box<CG>(at + 2 * BOX_BYTES + r * BLOCK_K * 2, t.b, b_rows_first ? b_row + r : kw, b_rows_first ? kw : b_row + r, zb, bar);
+              }
+            }
+            __syncwarp();
           }
         }
       }
     }
-    if (!ok && rank == 0)                          // copies in flight land before the block ends
+    if (!ok && rank == 0 && warp == 0)             // copies in flight land before the block ends
       for (u32 m = n > STAGES ? n - STAGES : 0; m < n; ++m) wait_slow(smem_u32(&ctl.full[m % STAGES]), (m / STAGES) & 1, nullptr, DRAIN_NS);
-  } else if (warp == 1 && lane == 0 && rank == 0) {
+  } else if (warp == 1 && rank == 0) {
     u32 n = 0, taken = 0;
     Tile t;
     bool ok = true;
     for (int i = 0; ok && job.tile(local, i, t); ++i) {
-      const u32 idesc = instruction(128 * CG, job.cols, job.bfloat, t.a_rows_first, t.b_rows_first);
-      const u32 a_step = (t.a_rows_first ? 2048 : 32) >> 4, b_step = (t.b_rows_first ? 2048 : 32) >> 4;
       int left = t.blocks;
       do {
         const int blocks = JOINED ? min(left, JOIN_BLOCKS) : left;
         const u32 buf = taken & 1;
-        if (!wait(&ctl.acc_empty[buf], ((taken >> 1) & 1) ^ 1, &ctl.dead)) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, wait(&ctl.acc_empty[buf], ((taken >> 1) & 1) ^ 1, &ctl.dead))) { ok = false; break; }
         fence_after();
         const u32 acc = tmem + buf * 256;
         u32 add = 0;
-        for (int j = job.seg.n * blocks; j > 0; --j, ++n) {
+        const int k0 = t.blocks - left;
+        for (int j = 0; j < job.seg.n * blocks; ++j, ++n) {
           const u32 stage = n % STAGES;
-          if (!wait(&ctl.full[stage], (n / STAGES) & 1, &ctl.dead)) { ok = false; break; }
+          if (!__all_sync(0xffffffffu, wait(&ctl.full[stage], (n / STAGES) & 1, &ctl.dead))) { ok = false; break; }
           fence_after();
           const u32 at = tiles + stage * STAGE_BYTES;
-          const u64 a = smem_desc(at, t.a_rows_first), b = smem_desc(at + 2 * BOX_BYTES, t.b_rows_first);
+          const int kb = k0 + (JOINED && JOIN_BLOCKS == 1 ? 0 : (JOINED ? j % blocks : j));
+          const bool a_rows_first = t.a_rows_first != (kb < t.a_turn), b_rows_first = t.b_rows_first != (kb < t.b_turn);
+          const u32 idesc = instruction(128 * CG, job.cols, job.bfloat, a_rows_first, b_rows_first);
+          const u32 a_step = (a_rows_first ? 2048 : 32) >> 4, b_step = (b_rows_first ? 2048 : 32) >> 4;
+          const u64 a = smem_desc(at, a_rows_first), b = smem_desc(at + 2 * BOX_BYTES, b_rows_first);
+          if (one_lane()) {
 #pragma unroll
-          for (u32 k = 0; k < BLOCK_K / 16; ++k) { product<CG>(acc, a + k * a_step, b + k * b_step, idesc, add); add = 1; }
-          commit<CG>(&ctl.empty[stage]);
+            for (u32 k = 0; k < BLOCK_K / 16; ++k) product<CG>(acc, a + k * a_step, b + k * b_step, idesc, k ? 1 : add);
+            commit<CG>(&ctl.empty[stage]);
+          }
+          __syncwarp();
+          add = 1;
         }
         if (!ok) break;
-        commit<CG>(&ctl.acc_full[buf]);
+        if (one_lane()) commit<CG>(&ctl.acc_full[buf]);
+        __syncwarp();
         ++taken;
         left -= blocks;
       } while (left > 0);
     }
     if (*(volatile u32*)&ctl.dead) {               // products in flight end before the tensor memory is given back
-      asm volatile("tcgen05.commit.cta_group::%1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&ctl.drain)), "n"(CG) : "memory");
+      if (one_lane()) asm volatile("tcgen05.commit.cta_group::%1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&ctl.drain)), "n"(CG) : "memory");
       wait_slow(smem_u32(&ctl.drain), 0, nullptr, DRAIN_NS);
     }
+  } else if (Job::REPORTS && warp == 2) {
+    Tile t;
+    for (int i = 0; job.tile(local, i, t); ++i) {
+      if (!__all_sync(0xffffffffu, wait_shared(&ctl.stored[lane % EPI_WARPS], (u32)i + 1, &ctl.dead))) break;
+      if constexpr (Job::REPORTS) if (one_lane()) job.report(local, t);
+      __syncwarp();
+    }
+  } else if (Job::REPORTS && warp == EPI_WARP + EPI_WARPS) {
+    Tile t;
+    for (int i = 0; job.tile(local, i, t); ++i) {
+      bool there = true;
+      if constexpr (Job::REPORTS) if (lane == 0) there = job.ready(local, t, &ctl.dead);
+      if (!__shfl_sync(0xffffffffu, there, 0)) break;
+      if (lane == 0) set_shared(&ctl.ready, (u32)i + 1);
+      __syncwarp();
+    }
   } else if (warp >= EPI_WARP) {
-    const int quarter = warp & 3, half = (warp - EPI_WARP) >> 2;
-    typename Job::Epilogue epi(job, local, (int)rank * 128 + quarter * 32 + lane, half);
+    const int quarter = warp & 3, part = (warp - EPI_WARP) >> 2;
+    typename Job::Epilogue epi(job, local, (int)rank * 128 + quarter * 32 + lane, part, tiles + STAGES * STAGE_BYTES + (warp - EPI_WARP) * Job::STAGING);
     Tile t;
     bool ok = true;
     u32 taken = 0;
     const u32 lanes = tmem + ((u32)quarter * 32 << 16);
     for (int i = 0; job.tile(local, i, t); ++i) {
+      epi.prepare(t, i, &ctl);
       int left = t.blocks;
       bool first = true;
       for (;;) {
@@ -318,8 +424,8 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
         Sums s = {!ok ? SUMS_NAN : job.seg.n * t.blocks == 0 ? SUMS_ZERO : first ? SUMS_HELD : SUMS_JOINED, lanes + buf * 256, lanes + HELD_COLUMN};
         if (last) epi.tile(t, s);
         else if constexpr (JOINED) {
-          const int width = job.cols / 2;
-          for (int c = half * width; c < (half + 1) * width; c += 32) {
+          const int width = epilogue_width(job.cols);
+          for (int c = part * width; c < (part + 1) * width; c += 32) {
             float v[32];
             sums_of(s, c, v);
             tmem_store(s.held + (u32)c, v);
@@ -331,6 +437,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_products(const __grid_constant__
           const u32 bar = smem_u32(&ctl.acc_empty[buf]);
           if constexpr (CG == 2) arrive_cluster(of_block0(bar));
           else mbar_arrive(&ctl.acc_empty[buf]);
+        }
+        if constexpr (Job::REPORTS) {
+          if (last) {
+            __syncwarp();
+            if (lane == 0) set_shared(&ctl.stored[warp - EPI_WARP], (u32)i + 1);
+          }
         }
         ++taken;
         if (last) break;
@@ -369,6 +481,35 @@ __device__ __forceinline__ void load_words(const void* from, u32 (&w)[16]) {
     asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7]) : "l"((const char*)from + i * 4)
                  : "memory");
 }
+// Rows of 16-byte pieces in shared memory, `wide` (a power of two, 4 at least) a row.  Pieces change places with the row, so that a lane
+// that takes pieces of its own row and lanes that take the pieces of one row both meet different banks.
+template <int WIDE>
+__device__ __forceinline__ u32 staged_at(u32 base, int r, int piece) {
+  return base + (u32)(r * WIDE + (piece ^ (WIDE == 4 ? (r >> 1) & 3 : r & 7))) * 16;
+}
+template <int WIDE>
+__device__ __forceinline__ void staged_store(u32 base, int r, int piece, const u32 (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(staged_at<WIDE>(base, r, piece + i)), "r"(w[4 * i]), "r"(w[4 * i + 1]), "r"(w[4 * i + 2]), "r"(w[4 * i + 3]) : "memory");
+}
+__device__ __forceinline__ uint4 staged_piece(u32 at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+template <int WIDE>
+__device__ __forceinline__ void staged_load(u32 base, int r, int piece, u32 (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint4 v = staged_piece(staged_at<WIDE>(base, r, piece + i));
+    w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+  }
+}
+// 16 bytes to shared memory, past L1 (which does not see what other SMs write).
+__device__ __forceinline__ void piece_in(u32 to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void pieces_arrived() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 __device__ __forceinline__ float2 unpack_half(u32 w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
 // `n` <= 32 values of a row, rounded to a type, to any aligned address.
@@ -418,7 +559,7 @@ inline bool encode_map(CUtensorMap* map, const void* base, bool bfloat, int64_t 
 }
 
 template <class Job, int CG, bool JOINED>
-cudaError_t launch_products(const Job& job, int blocks, cudaStream_t st, bool first) {
+cudaError_t launch_products(const Job& job, int blocks, cudaStream_t st, bool together) {
   // the attribute belongs to a device's context: set once for each
   static std::atomic<unsigned long long> ready{0};
   int device = 0;
@@ -426,30 +567,40 @@ cudaError_t launch_products(const Job& job, int blocks, cudaStream_t st, bool fi
   if (e != cudaSuccess) return e;
   const unsigned long long bit = device < 64 ? 1ull << device : 0;
   if (!(ready.load(std::memory_order_acquire) & bit)) {
-    e = cudaFuncSetAttribute(k_products<Job, CG, JOINED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES);
+    e = cudaFuncSetAttribute(k_products<Job, CG, JOINED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Room<Job>::BYTES);
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks);
-  cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = SMEM_BYTES;
+  cfg.blockDim = dim3(Room<Job>::THREADS);
+  cfg.dynamicSmemBytes = Room<Job>::BYTES;
   cfg.stream = st;
   cudaLaunchAttribute at[2];
   int n = 0;
   if (CG == 2) { at[n].id = cudaLaunchAttributeClusterDimension; at[n].val.clusterDim.x = 2; at[n].val.clusterDim.y = 1; at[n].val.clusterDim.z = 1; ++n; }
-  if (!first) { at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization; at[n].val.programmaticStreamSerializationAllowed = 1; ++n; }
+  if (together) { at[n].id = cudaLaunchAttributeCooperative; at[n].val.cooperative = 1; ++n; }
+  else { at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization; at[n].val.programmaticStreamSerializationAllowed = 1; ++n; }
   cfg.attrs = at;
   cfg.numAttrs = (unsigned)n;
   return cudaLaunchKernelEx(&cfg, k_products<Job, CG, JOINED>, job);
 }
 
-// Sums of several parts are joined on the way.
+// together: blocks wait for one another, so all of them have to run at once.  Otherwise the kernel may start while the one before it
+// still runs.  Sums of several parts are joined on the way.
 template <class Job>
-cudaError_t launch_products(const Job& job, int cg, int tiles_at_once, cudaStream_t st) {
-  if (job.seg.n > 1) return cg == 2 ? launch_products<Job, 2, true>(job, 2 * tiles_at_once, st, false) : launch_products<Job, 1, true>(job, tiles_at_once, st, false);
-  return cg == 2 ? launch_products<Job, 2, false>(job, 2 * tiles_at_once, st, false) : launch_products<Job, 1, false>(job, tiles_at_once, st, false);
+cudaError_t launch_products(const Job& job, int cg, int tiles_at_once, cudaStream_t st, bool together = false) {
+  if (job.seg.n > 1) return cg == 2 ? launch_products<Job, 2, true>(job, 2 * tiles_at_once, st, together) : launch_products<Job, 1, true>(job, tiles_at_once, st, together);
+  return cg == 2 ? launch_products<Job, 2, false>(job, 2 * tiles_at_once, st, together) : launch_products<Job, 1, false>(job, tiles_at_once, st, together);
 }
+
+// For jobs whose operands are there before the kernel runs, and that look up nothing.
+struct Plain {
+  static constexpr int STAGING = 0;
+  static constexpr bool REPORTS = false;
+  struct Shared {};
+  __device__ __forceinline__ void fill(Shared&) const {}
+};
 
 }  // namespace mma
 }  // namespace sae

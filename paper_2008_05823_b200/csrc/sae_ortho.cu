@@ -2,13 +2,18 @@
 //
 //   x <- g / (|g| + eps), then `steps` times  x <- a x + (b s + c s s) x  with s = x x' (x' x where a matrix is taller than wide)
 //
-// One call is a kernel for the norms, one that lays g out as two float16 parts, and three product kernels a step, each over
-// the tiles of all matrices:  S = s;  B = b S + c S S;  x = a x + B x.
+// One call is a kernel for the norms, one that lays g out as two float16 parts, and ONE kernel for all products of all steps:
+// S = s;  B = a + b S + c S S;  x = B x, tile by tile.  Its tiles are one list; a tile starts when the tiles of its
+// matrix's product before are all written, which a counter of each matrix says.  Every cluster takes every n-th tile of the list in
+// order, and all clusters run at once (cooperative launch), so the first tile that is not done can always be worked on.
+// Against a launch for each product (15 of them): no gaps and no partly filled last wave between products.
+// S and B are symmetric: only tiles on and above the diagonal are made and kept.  Blocks of k that lie below it are loaded from
+// above it, with rows and k in exchanged order, which the matrix descriptors undo.
 //
-// Precision.  x is held as hi + lo, two float16 of a value scaled by a power of two (22 bits).  For results of 16 bits in bfloat16
-// the products read hi alone (11 bits), and a x in the last product's epilogue reads both: a rounding of x itself to 11
+// Precision.  x is held as hi + lo, two float16 of a value scaled by a power of two (22 bits).  For results in bfloat16
+// the products read hi alone (11 bits), and a lo is added in the last product's epilogue: a rounding of x itself to 11
 // bits in every step would be multiplied by a^5 = 485 in the directions of small singular values (errors of 1.4e-2 for a gradient of a few
-// strong directions over noise, 2e-4 this way).  Float32 and float16 results take hi and lo in all three products (hi lo + lo hi +
+// strong directions over noise, 8e-4 this way).  Float32 and float16 results take hi and lo in all three products (hi lo + lo hi +
 // hi hi): about the error of float32 products.
 // Scales: singular values stay below a bound that follows from the coefficients, so no element of x, S or B leaves
 // float16's range, and each is scaled up to near its top to keep small elements from becoming subnormal.
@@ -31,23 +36,31 @@ namespace {
 
 constexpr int OT_THREADS = 256;
 constexpr int OT_CHUNK = 2048;                // units of a row that a block takes
+// Bytes of the matrices that go through all steps together, one such portion after another.  Portions that L2 holds (64 or 128 MB) have too few
+// tiles to cover the wait from one product to the next: the 12-layer encoder takes 4070 and 2020 us with them, 1850 with 256 MB, 1800 with
+// 512, 1880 with all at once.
+constexpr int64_t OT_PORTION = 512ll << 20;
 constexpr int OT_ARGS = 448;                  // matrices whose addresses travel as kernel arguments
 
-// All matrices of one shape and precision.
-struct Group {
-  CUtensorMap x[2], s, b;
-  __half *xp[2], *sp, *bp;
+constexpr int OT_SHAPES = 32, OT_BATCHES = 800;   // as many are looked up in shared memory
+constexpr int OT_STEPS = 64;
+
+// All matrices of one shape and precision: its maps, and what else a tile needs to know.
+struct Maps { CUtensorMap x[2], s, b; };
+struct Shape {
+  __half *x[2], *s, *b;
   long long x_plane, s_plane;                 // elements of a part
   int rows, cols, small, tall;
   int x_pitch, s_pitch;
-  int s_parts;
-  int x_tiles, x_tile_cols, s_tiles, s_tile_cols;   // tiles of one matrix
-  int x_end, s_end;                           // tiles of all groups up to and with this one
+  int s_parts, plain;                         // plain: 16-bit matrices, whose x0 is hi alone, exactly
+  int x_tiles, x_tile_cols, s_tiles;          // tiles of one matrix's products
   int first;                                  // its first matrix in the class's order
 };
+// One product of some neighbouring matrices of a shape: tiles begin .. end - 1 of the list.
+struct Batch { int begin, end, first; unsigned short shape; unsigned char phase, step; };
 
 struct Matrix { const void* in; void* out; long long in_ld, out_ld; };
-struct Place { int rows, cols, x_pitch, in_type, out_type, first_chunk, chunks; __half* x; long long x_plane; };
+struct Place { int rows, cols, x_pitch, in_type, out_type, first_chunk, chunks; __half* x; long long x_plane; u32* done; float* ratio; int plain; };
 struct Chunk { int matrix, unit; };
 
 struct Table { int n; Matrix m[OT_ARGS]; };
@@ -105,9 +118,18 @@ __global__ void __launch_bounds__(OT_THREADS) k_ortho_split(const Matrix* mats, 
   const Place p = places[ch.matrix];
   mma::wait_for_previous();
   const Matrix m = mats[ch.matrix];
+  if (ch.unit == 0 && threadIdx.x == 0) *p.done = 0;
   double s = 0;
   for (int i = threadIdx.x; i < p.chunks; i += OT_THREADS) s += sums[p.first_chunk + i];
-  const double factor = scale / (sqrt(block_sum(s, scratch)) + eps);
+  // 16-bit elements times a power of two are float16 exactly (but for what is 2^-25 of the norm); the rest of the factor, from 1/2
+  // to 1, goes into the first step's products
+  double factor = scale / (sqrt(block_sum(s, scratch)) + eps), ratio = 1.0;
+  if (p.plain && factor > 0 && factor < 1e300) {
+    int e;
+    ratio = frexp(factor, &e);
+    factor = ldexp(1.0, e);
+  }
+  if (ch.unit == 0 && threadIdx.x == 0) *p.ratio = (float)ratio;
   const unsigned wide = (unsigned)(p.cols + UNIT - 1) / UNIT;
   for (int i = threadIdx.x; i < OT_CHUNK; i += OT_THREADS) {
     const unsigned u = (unsigned)ch.unit + (unsigned)i, r = u / wide, c = (u - r * wide) * UNIT;
@@ -124,140 +146,226 @@ __global__ void __launch_bounds__(OT_THREADS) k_ortho_split(const Matrix* mats, 
     }
     __half* const to = p.x + (long long)r * p.x_pitch + c;
     *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-    *reinterpret_cast<uint4*>(to + p.x_plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    if (!p.plain) *reinterpret_cast<uint4*>(to + p.x_plane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
   }
 }
 
 // ---- products ---------------------------------------------------------------------------------------------------------
 enum Phase { PHASE_S, PHASE_B, PHASE_X };
+// S = s_sum acc;  B = b_diag 1 + b_own S + b_sum acc;  x = x_own lo + x_sum acc
+struct Factors { float s_sum, b_diag, b_own, b_sum, x_own, x_sum; };
 
 struct OrthoJob {
+  static constexpr bool REPORTS = true;
+  static constexpr int STAGING = 32 * 256;      // 32 rows of 128 elements
   int cols;
   bool bfloat;
   mma::Segments seg;
-  const Group* groups;
-  int phase, rows, total, from, last;
-  float own, sum;                   // result = own * (the matrix's present value) + sum * acc
-  const Matrix* mats;               // in the class's order, for the last step
+  const Maps* maps;
+  const Shape* shapes;
+  const Batch* batches;
+  int num_shapes, num_batches, total, rows, steps, arrivals;   // rows of a tile; blocks that write one
+  u32* done;                        // in the class's order
+  const Matrix* mats;
   const Place* places;
   const int* order;
+  const float* ratios;
+  Factors factors[OT_STEPS];
 
-  struct Local { int first, step, g; };
-  __device__ __forceinline__ Local begin(int cluster, int clusters) const { return {cluster, clusters, 0}; }
+  struct Shared {
+    Shape shapes[OT_SHAPES];
+    Batch batches[OT_BATCHES];
+  };
+  __device__ __forceinline__ void fill(Shared& s) const {
+    if (num_shapes <= OT_SHAPES)
+      for (int i = threadIdx.x; i < num_shapes * (int)(sizeof(Shape) / 4); i += (int)blockDim.x) reinterpret_cast<u32*>(s.shapes)[i] = reinterpret_cast<const u32*>(shapes)[i];
+    if (num_batches <= OT_BATCHES)
+      for (int i = threadIdx.x; i < num_batches * (int)(sizeof(Batch) / 4); i += (int)blockDim.x) reinterpret_cast<u32*>(s.batches)[i] = reinterpret_cast<const u32*>(batches)[i];
+  }
+  struct Local { const Shape* shapes; const Batch* batch; int first, step; };
+  __device__ __forceinline__ Local begin(const Shared& s, int cluster, int clusters) const {
+    return {num_shapes <= OT_SHAPES ? s.shapes : shapes, num_batches <= OT_BATCHES ? s.batches : batches, cluster, clusters};
+  }
+  // The tile (row, column) of a symmetric product that is number q of those not wholly below the diagonal.
+  __device__ __host__ static void above(int q, int rows, int cols, int small, int& r, int& c) {
+    const int wide = (small + cols - 1) / cols, per = rows / cols;
+    for (r = 0; q >= wide - r * per; ++r) q -= wide - r * per;
+    c = r * per + q;
+  }
+  // the first block of k that S and B have for a row (the rows of a tile have the same)
+  __device__ __forceinline__ int kept_from(int row) const { return row / rows * rows / mma::BLOCK_K; }
   __device__ __forceinline__ bool tile(Local& l, int i, mma::Tile& t) const {
     const int w = l.first + i * l.step;
     if (w >= total) return false;
-    const bool px = phase == PHASE_X;
-    while (w >= (px ? groups[l.g].x_end : groups[l.g].s_end)) ++l.g;
-    const Group& g = groups[l.g];
-    const int per = px ? g.x_tiles : g.s_tiles, wide = px ? g.x_tile_cols : g.s_tile_cols;
-    const int before = l.g ? (px ? groups[l.g - 1].x_end : groups[l.g - 1].s_end) : 0;
-    t.item = (w - before) / per;
-    const int q = (w - before) % per;
-    t.group = l.g;
-    t.row = q / wide * rows;
-    t.col = q % wide * cols;
-    t.a_row = t.row;
-    t.b_row = t.col;
-    t.a_k = t.b_k = 0;
-    const int zx = t.item * 2, zs = t.item * g.s_parts;
-    int k;
-    if (phase == PHASE_S) {
-      t.a = t.b = &g.x[from];
+    while (w >= l.batch->end) ++l.batch;
+    const Batch b = *l.batch;
+    const Shape& g = l.shapes[b.shape];
+    const Maps& m = maps[b.shape];
+    const bool px = b.phase == PHASE_X;
+    const int per = px ? g.x_tiles : g.s_tiles, n = (w - b.begin) / per, q = (w - b.begin) - n * per;
+    t.item = b.first + n;
+    t.group = b.shape;
+    int r, c;
+    if (px) { r = q / g.x_tile_cols; c = q - r * g.x_tile_cols; }
+    else above(q, rows, cols, g.small, r, c);
+    t.a_row = t.row = r * rows;
+    t.b_row = t.col = c * cols;
+    t.a_k = t.b_k = t.a_turn = t.b_turn = 0;
+    const int zx = t.item * 2, zs = t.item * g.s_parts, from = b.step & 1;
+    int k = g.small;
+    t.a_rows_first = t.b_rows_first = false;
+    if (b.phase == PHASE_S) {
+      t.a = t.b = &m.x[from];
       t.a_plane = t.b_plane = zx;
       t.a_rows_first = t.b_rows_first = g.tall;
       k = g.tall ? g.rows : g.cols;
-    } else if (phase == PHASE_B) {
-      t.a = t.b = &g.s;
+    } else if (b.phase == PHASE_B) {
+      t.a = t.b = &m.s;
       t.a_plane = t.b_plane = zs;
-      t.a_rows_first = t.b_rows_first = false;
-      k = g.small;
+      t.a_turn = kept_from(t.row);
+      t.b_turn = kept_from(t.col);
     } else {
-      t.a = g.tall ? &g.x[from] : &g.b;
-      t.b = g.tall ? &g.b : &g.x[from];
+      t.a = g.tall ? &m.x[from] : &m.b;
+      t.b = g.tall ? &m.b : &m.x[from];
       t.a_plane = g.tall ? zx : zs;
       t.b_plane = g.tall ? zs : zx;
-      t.a_rows_first = false;
       t.b_rows_first = !g.tall;
-      k = g.small;
+      if (g.tall) t.b_turn = kept_from(t.col);
+      else t.a_turn = kept_from(t.row);
     }
     t.blocks = (k + mma::BLOCK_K - 1) / mma::BLOCK_K;
     return true;
   }
+  // Whether x has a lo when step s begins.  Where products read hi alone, the last step needs none: a rounding is multiplied by a at most there.
+  __device__ __forceinline__ bool has_lo(const Shape& g, int s) const { return g.s_parts == 2 || (s ? s + 1 < steps : !g.plain); }
+  // the matrix's counter, and what it shows when every product before this tile's is written
+  __device__ __forceinline__ u32* counter(const Shape& g, const mma::Tile& t) const { return done + g.first + t.item; }
+  __device__ __forceinline__ u32 before(const Shape& g, const Batch& b) const { return (u32)((b.step * (2 * g.s_tiles + g.x_tiles) + b.phase * g.s_tiles) * arrivals); }
+  __device__ __forceinline__ bool ready(const Local& l, const mma::Tile& t, u32* dead) const {
+    const Shape& g = l.shapes[t.group];
+    if (!mma::wait_counter(counter(g, t), before(g, *l.batch), dead)) return false;
+    mma::fence_copies();
+    return true;
+  }
 
+  __device__ __forceinline__ void report(const Local& l, const mma::Tile& t) const {
+    mma::fence_copies();
+    mma::add_counter(counter(l.shapes[t.group], t));
+  }
+
+  // A warp takes its rows 32 columns at a time.  Present values come in through shared memory, whole lines at a time, while the tile's products
+  // run; a thread that reads 64 bytes of its own row keeps the load and store unit busy for 32 lines with every instruction.  Results go out
+  // straight from the registers, 32 bytes a store: an SM's stores pass at 32 bytes a cycle, and lines put together in shared memory first
+  // did not pass faster.  Copies by TMA, in or out, hold up those of the operands (16000 cycles a tile of 256 x 256, whose products take
+  // 6144 at 768 rows).
   struct Epilogue {
     const OrthoJob& job;
-    int row, half;
-    __device__ __forceinline__ Epilogue(const OrthoJob& j, const Local&, int r, int h) : job(j), row(r), half(h) {}
-    __device__ __forceinline__ void finish() {}
+    const Local& l;                   // the role's own: its batch is the tile's
+    const int row, part;
+    const u32 in;                     // shared memory, 16 pieces of 16 bytes a row
+    int chunks;                       // of 32 columns that this warp has of the tile
+    int own;                          // parts of present values that come in for a chunk
+    bool here;                        // they do come in
+    __device__ __forceinline__ Epilogue(const OrthoJob& j, const Local& l, int r, int p, u32 at)
+        : job(j), l(l), row(r), part(p), in(at), chunks(0), own(0), here(false) {}
 
-    // own * (hi + lo of `from`) + sum * acc, `from` null: nothing of its own
-    __device__ __forceinline__ void value(float (&v)[32], const __half* from, long long lo_at) const {
-      if (from) {
-        u32 w[16], u[16];
-        mma::load_words(from, w);
-        if (lo_at) mma::load_words(from + lo_at, u);
+    __device__ __forceinline__ void finish() {}
+    __device__ __forceinline__ void prepare(const mma::Tile& t, int number, mma::Control* ctl) {
+      const Batch b = *l.batch;
+      const Shape& g = l.shapes[t.group];
+      const bool px = b.phase == PHASE_X, two = g.s_parts == 2;
+      const int lane = threadIdx.x & 31, width = mma::epilogue_width(job.cols), row0 = t.row + (row & ~31), col0 = t.col + part * width;
+      const int rows = px ? g.rows : g.small, cols = px ? g.cols : g.small;
+      chunks = row0 >= rows ? 0 : (max(0, min(width, cols - col0)) + 31) / 32;
+      own = b.phase == PHASE_S ? 0 : b.phase == PHASE_B ? g.s_parts : two ? 0 : job.has_lo(g, b.step);
+      here = true;
+      if (own && chunks) {
+        here = __all_sync(0xffffffffu, mma::wait_shared(&ctl->ready, (u32)number + 1, &ctl->dead));      // (without them the tile is NaN)
+        if (here) {
+          const int pitch = px ? g.x_pitch : g.s_pitch, p = lane & 15;
+          const long long plane = px ? g.x_plane : g.s_plane;
+          const __half* from = (px ? g.x[b.step & 1] + (t.item * 2ll + 1) * plane : g.s + (long long)t.item * g.s_parts * plane) + (long long)row0 * pitch + col0;
+          if (own == 2) from += (p >> 3) * plane + (p & 7) * 8;          // pieces 8 .. 15 are lo's
+          else from += p * 8;
+          if ((own == 2 ? p & 7 : p) < chunks * 4)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float2 h = mma::unpack_half(w[i]);
-          if (lo_at) { const float2 l = mma::unpack_half(u[i]); h.x += l.x; h.y += l.y; }
-          v[2 * i] = __fmaf_rn(job.own, h.x, job.sum * v[2 * i]);
-          v[2 * i + 1] = __fmaf_rn(job.own, h.y, job.sum * v[2 * i + 1]);
+            for (int r = lane >> 4; r < 32; r += 2)
+              if (row0 + r < rows) mma::piece_in(mma::staged_at<16>(in, r, p), from + (long long)r * pitch);
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= job.sum;
-      }
-    }
-    __device__ __forceinline__ void split(const float (&v)[32], __half* to, long long lo_at) const {
-      u32 w[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w[i] = mma::pack_half(v[2 * i], v[2 * i + 1]);
-      mma::store_words(to, w);
-      if (lo_at) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float2 h = mma::unpack_half(w[i]);
-          w[i] = mma::pack_half(v[2 * i] - h.x, v[2 * i + 1] - h.y);
-        }
-        mma::store_words(to + lo_at, w);
       }
     }
     __device__ __forceinline__ void tile(const mma::Tile& t, const mma::Sums& sums) {
-      const Group& g = job.groups[t.group];
-      const bool px = job.phase == PHASE_X;
-      const int r = t.row + row, rows = px ? g.rows : g.small, cols = px ? g.cols : g.small, pitch = px ? g.x_pitch : g.s_pitch;
-      const int width = job.cols / 2;
+      if (!chunks) return;
+      const Batch b = *l.batch;
+      const Shape& g = l.shapes[t.group];
+      const Factors f = job.factors[b.step];
+      const bool px = b.phase == PHASE_X, last = px && b.step + 1 == job.steps;
+      const int r = t.row + row, cols = px ? g.cols : g.small, parts = px ? 1 + job.has_lo(g, b.step + 1) : g.s_parts;
+      const float mine = px ? f.x_own : f.b_own;
+      float sum = px ? f.x_sum : b.phase == PHASE_B ? f.b_sum : f.s_sum;
+      if (b.step == 0 && b.phase != PHASE_B) {              // x0 is hi times this
+        const float ratio = job.ratios[g.first + t.item];
+        sum *= px ? ratio : ratio * ratio;
+      }
+      if (!here) sum = __int_as_float(0x7fc00000);
+      const int lane_row = row & 31, rows = px ? g.rows : g.small, pitch = px ? g.x_pitch : g.s_pitch;
+      const long long plane = px ? g.x_plane : g.s_plane;
+      __half* const to = (px ? g.x[(b.step & 1) ^ 1] : b.phase == PHASE_B ? g.b : g.s) + t.item * (long long)(px ? 2 : g.s_parts) * plane + (long long)r * pitch;
       Matrix m = {};
       int type = 0;
-      if (px && job.last) {
+      if (last) {
         const int i = job.order[g.first + t.item];
         m = job.mats[i];
         type = job.places[i].out_type;
       }
-      for (int c = half * width; c < (half + 1) * width; c += 32) {
-        const int col = t.col + c;
-        if (col >= cols) break;                       // the same for the whole warp
+      if (own) {
+        mma::pieces_arrived();
+        __syncwarp();
+      }
+      for (int k = 0; k < chunks; ++k) {
+        const int col = t.col + part * mma::epilogue_width(job.cols) + k * 32;
         float v[32];
-        mma::sums_of(sums, c, v);
-        if (r >= rows) continue;
-        const long long at = (long long)r * pitch + col;
-        if (!px) {
-          const long long plane = (long long)t.item * g.s_parts * g.s_plane, lo = g.s_parts == 2 ? g.s_plane : 0;
-          value(v, job.phase == PHASE_B ? g.sp + plane + at : nullptr, lo);
-          split(v, (job.phase == PHASE_B ? g.bp : g.sp) + plane + at, lo);
-        } else {
-          const long long plane = (long long)t.item * 2 * g.x_plane;
-          value(v, g.xp[job.from] + plane + at, g.x_plane);
-          if (!job.last) split(v, g.xp[job.from ^ 1] + plane + at, g.x_plane);
-          else {
-            const int n = min(32, cols - col);
-            const long long to = r * m.out_ld + col;
-            if (type == SAE_TYPE_FLOAT) mma::store_row((float*)m.out + to, v, n);
-            else if (type == SAE_TYPE_BFLOAT) mma::store_row((__nv_bfloat16*)m.out + to, v, n);
-            else mma::store_row((__half*)m.out + to, v, n);
+        mma::sums_of(sums, col - t.col, v);
+        if (sum != 1.0f) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] *= sum;
+        }
+        u32 hi[16], lo[16];
+        if (own) {
+          mma::staged_load<16>(in, lane_row, 4 * k, hi);
+          if (own == 2) mma::staged_load<16>(in, lane_row, 8 + 4 * k, lo);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float2 x = mma::unpack_half(hi[i]);
+            if (own == 2) { const float2 y = mma::unpack_half(lo[i]); x.x += y.x; x.y += y.y; }
+            v[2 * i] = __fmaf_rn(mine, x.x, v[2 * i]);
+            v[2 * i + 1] = __fmaf_rn(mine, x.y, v[2 * i + 1]);
           }
         }
+        if (b.phase == PHASE_B && (unsigned)(r - col) < 32u) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] += r - col == i ? f.b_diag : 0.0f;
+        }
+        if (last) {
+          if (r < g.rows) {
+            const int w = min(32, cols - col);
+            const long long out = r * m.out_ld + col;
+            if (type == SAE_TYPE_FLOAT) mma::store_row((float*)m.out + out, v, w);
+            else if (type == SAE_TYPE_BFLOAT) mma::store_row((__nv_bfloat16*)m.out + out, v, w);
+            else mma::store_row((__half*)m.out + out, v, w);
+          }
+          continue;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) hi[i] = mma::pack_half(v[2 * i], v[2 * i + 1]);
+        if (r < rows) mma::store_words(to + col, hi);
+        if (parts == 1) continue;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float2 h = mma::unpack_half(hi[i]);
+          lo[i] = mma::pack_half(v[2 * i] - h.x, v[2 * i + 1] - h.y);
+        }
+        if (r < rows) mma::store_words(to + plane + col, lo);
       }
     }
   };
@@ -280,19 +388,19 @@ int elem_bytes(int type) { return type == SAE_TYPE_FLOAT ? 4 : 2; }
 bool type_ok(int type) { return type == SAE_TYPE_FLOAT || type == SAE_TYPE_BFLOAT || type == SAE_TYPE_HALF; }
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-// Groups whose products have the same number of parts: one launch a phase.
+// Shapes whose products have the same number of parts: one launch.
 struct Class {
   int parts, cg, cols;
-  int first, n;                  // groups
-  int s_total, x_total;
+  int first, n;                  // shapes
+  int first_batch, batches, total;
 };
 
-// The largest |p(v)| and |b v^2 + c v^4| over 0 <= v <= top.
+// The largest |p(v)| and |a + b v^2 + c v^4| over 0 <= v <= top.
 void bounds(const float* k, double top, double& p, double& q) {
   p = q = 0;
   for (int i = 0; i <= 4096; ++i) {
-    const double v = top * i / 4096, s = v * v, e = k[1] * s + k[2] * s * s;
-    p = std::max(p, std::fabs(v * (k[0] + e)));
+    const double v = top * i / 4096, s = v * v, e = k[0] + k[1] * s + k[2] * s * s;
+    p = std::max(p, std::fabs(v * e));
     q = std::max(q, std::fabs(e));
   }
 }
@@ -310,7 +418,11 @@ struct sae_ortho {
   double x_scale;
   std::vector<Class> classes;
   char* arena;
-  Group* groups;
+  Maps* maps;
+  Shape* shapes;
+  Batch* batches;
+  u32* done;
+  float* ratios;
   Matrix* mats;
   Place* places;
   Chunk* chunk_list;
@@ -327,7 +439,7 @@ int cuda_status(sae_ortho* h, cudaError_t e) {
 }
 
 void release(sae_ortho* h) {
-  cudaFree(h->arena); cudaFree(h->groups); cudaFree(h->mats); cudaFree(h->places); cudaFree(h->chunk_list); cudaFree(h->order); cudaFree(h->sums);
+  cudaFree(h->arena); cudaFree(h->maps); cudaFree(h->shapes); cudaFree(h->batches); cudaFree(h->done); cudaFree(h->ratios); cudaFree(h->mats); cudaFree(h->places); cudaFree(h->chunk_list); cudaFree(h->order); cudaFree(h->sums);
   delete h;
 }
 
@@ -338,30 +450,75 @@ cudaError_t upload(T** to, const std::vector<T>& v, cudaStream_t st) {
   return e;
 }
 
+// Tiles of a symmetric product that are not wholly below the diagonal.
+int tiles_above(int small, int rows, int cols) {
+  const int wide = (small + cols - 1) / cols, per = rows / cols;
+  int n = 0;
+  for (int r = 0; r * per < wide; ++r) n += wide - r * per;
+  return n;
+}
+
+void count_tiles(Shape& g, int rows, int cols) {
+  g.x_tile_cols = (g.cols + cols - 1) / cols;
+  g.x_tiles = (g.rows + rows - 1) / rows * g.x_tile_cols;
+  g.s_tiles = tiles_above(g.small, rows, cols);
+}
+
 // Tile shape of a class: time in units of a block's k loop, waves of tiles over the SMs (or pairs).
-void choose_tiles(Class& c, const std::vector<Group>& groups, const std::vector<int>& count, int sms) {
-  struct Shape { int cg, cols; double cost; };
-  const Shape shapes[3] = {{2, c.parts == 1 ? 256 : 128, c.parts == 1 ? 2.0 : 1.2}, {1, 128, 1.3}, {1, 64, 1.0}};
+void choose_tiles(Class& c, std::vector<Shape>& shapes, const std::vector<int>& count, int sms) {
+  struct Form { int cg, cols; double cost; };
+  const Form forms[3] = {{2, c.parts == 1 ? 256 : 128, c.parts == 1 ? 2.0 : 1.2}, {1, 128, 1.3}, {1, 64, 1.0}};
   double best = 0;
-  for (const Shape& s : shapes) {
-    const int rows = 128 * s.cg, units = sms / s.cg;
+  for (const Form& f : forms) {
+    const int units = sms / f.cg;
     double work_s = 0, work_x = 0, longest_s = 0, longest_x = 0;
     for (int i = c.first; i < c.first + c.n; ++i) {
-      const Group& g = groups[i];
-      const auto tiles = [&](int r, int q) { return (double)((r + rows - 1) / rows) * ((q + s.cols - 1) / s.cols); };
+      Shape g = shapes[i];
+      count_tiles(g, 128 * f.cg, f.cols);
       const int big = g.tall ? g.rows : g.cols;
-      work_s += tiles(g.small, g.small) * big * count[i];
-      work_x += (tiles(g.rows, g.cols) + tiles(g.small, g.small)) * g.small * count[i];
+      work_s += (double)g.s_tiles * big * count[i];
+      work_x += (double)(g.x_tiles + g.s_tiles) * g.small * count[i];
       longest_s = std::max(longest_s, (double)big);
       longest_x = std::max(longest_x, (double)g.small);
     }
-    const double t = s.cost * (std::max(work_s / units, longest_s) + std::max(work_x / units, 2 * longest_x));
-    if (best == 0 || t < best) { best = t; c.cg = s.cg; c.cols = s.cols; }
+    const double t = f.cost * (std::max(work_s / units, longest_s) + std::max(work_x / units, 2 * longest_x));
+    if (best == 0 || t < best) { best = t; c.cg = f.cg; c.cols = f.cols; }
   }
+  for (int i = c.first; i < c.first + c.n; ++i) count_tiles(shapes[i], 128 * c.cg, c.cols);
 }
 
-cudaError_t products(const sae_ortho* h, const Class& c, const OrthoJob& job) {
-  return mma::launch_products(job, c.cg, std::min(job.total, h->num_sms / c.cg), h->stream);
+// The list of a class's products.  Portions of matrices that L2 holds go through all steps, one portion after another.
+void list_products(Class& c, const std::vector<Shape>& shapes, const std::vector<int>& count, int steps, std::vector<Batch>& batches) {
+  struct Piece { int shape, first, n; };
+  std::vector<std::vector<Piece>> portions;
+  int64_t room = 0;
+  for (int i = c.first; i < c.first + c.n; ++i) {
+    const Shape& g = shapes[i];
+    const int64_t bytes = 8 * g.x_plane + 4 * g.s_parts * g.s_plane;
+    for (int m = 0; m < count[i]; ++m) {
+      if (portions.empty() || room < bytes) { portions.emplace_back(); room = OT_PORTION; }
+      room -= bytes;
+      auto& p = portions.back();
+      if (!p.empty() && p.back().shape == i) ++p.back().n;
+      else p.push_back({i, m, 1});
+    }
+  }
+  c.first_batch = (int)batches.size();
+  int64_t at = 0;
+  for (const auto& p : portions)
+    for (int s = 0; s < steps; ++s)
+      for (int phase = 0; phase < 3; ++phase)
+        for (const Piece& q : p) {
+          const Shape& g = shapes[q.shape];
+          Batch b = {};
+          b.begin = (int)at;
+          b.end = (int)(at += (int64_t)q.n * (phase == PHASE_X ? g.x_tiles : g.s_tiles));
+          b.first = q.first; b.shape = (unsigned short)(q.shape - c.first); b.phase = (unsigned char)phase; b.step = (unsigned char)s;
+          batches.push_back(b);
+        }
+  c.batches = (int)batches.size() - c.first_batch;
+  if (at > (1 << 30)) throw std::bad_alloc();       // (more tiles than an int counts: no list of matrices that memory holds)
+  c.total = (int)at;
 }
 
 template <typename... P, typename... A>
@@ -413,14 +570,17 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
   if (!h) return SAE_ERR_NOMEM;
   h->K = K; h->T = T; h->device = cfg->device; h->stream = (cudaStream_t)cfg->stream; h->steps = cfg->steps; h->eps = cfg->eps;
   h->x_scale = std::exp2(std::floor(std::log2(32768.0 / widest)));
-  std::vector<Group> groups;
+  std::vector<Maps> maps;
+  std::vector<Shape> shapes;
   std::vector<int> count, order;
   std::vector<Place> places;
   std::vector<Chunk> chunks;
-  std::vector<std::vector<int>> members;
+  std::vector<Batch> batches;
   DeviceGuard guard(cfg->device);
   cudaError_t e = guard.ok ? cudaSuccess : cudaGetLastError();
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, cfg->device);
+  if (e == cudaSuccess) e = cudaMalloc((void**)&h->done, (size_t)K * T * sizeof(u32));
+  if (e == cudaSuccess) e = cudaMalloc((void**)&h->ratios, (size_t)K * T * sizeof(float));
   bool mapped = true;
   if (e == cudaSuccess) {
     try {
@@ -432,20 +592,21 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
         h->in_types.push_back(cfg->types ? cfg->types[j] : SAE_TYPE_FLOAT);
         h->out_types.push_back(cfg->result_types ? cfg->result_types[j] : h->in_types[j]);
       }
-      // groups: parts first (a class), then long sums before short ones
-      std::map<std::tuple<int, int64_t, int64_t, int64_t>, std::vector<int>> by;
+      // shapes: by parts (a class), then long sums before short ones
+      std::map<std::tuple<int, int64_t, int64_t, int64_t, bool>, std::vector<int>> by;
       for (int k = 0; k < K; ++k)
         for (int j = 0; j < T; ++j)
           if (h->rows[j] && h->cols[j]) {
             // bfloat16 results of a few rows or columns take both parts too: such products are short, and their roundings average out less
             const bool one = h->out_types[j] == SAE_TYPE_BFLOAT && std::min(h->rows[j], h->cols[j]) > 128;
-            by[{one ? 1 : 2, -std::max(h->rows[j], h->cols[j]), h->rows[j], h->cols[j]}].push_back(k * T + j);
+            by[{one ? 1 : 2, -std::max(h->rows[j], h->cols[j]), h->rows[j], h->cols[j], one && h->in_types[j] != SAE_TYPE_FLOAT}].push_back(k * T + j);
           }
       places.resize((size_t)K * T);
       int64_t bytes = 0;
       for (auto& kv : by) {
-        Group g = {};
+        Shape g = {};
         g.s_parts = std::get<0>(kv.first);
+        g.plain = std::get<4>(kv.first);
         g.rows = (int)std::get<2>(kv.first); g.cols = (int)std::get<3>(kv.first);
         g.tall = g.rows > g.cols;
         g.small = std::min(g.rows, g.cols);
@@ -454,32 +615,33 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
         g.first = (int)order.size();
         for (int i : kv.second) order.push_back(i);
         count.push_back((int)kv.second.size());
-        members.push_back(kv.second);
-        if (h->classes.empty() || h->classes.back().parts != g.s_parts) h->classes.push_back({g.s_parts, 1, 64, (int)groups.size(), 0, 0, 0});
+        if (h->classes.empty() || h->classes.back().parts != g.s_parts) h->classes.push_back({g.s_parts, 1, 64, (int)shapes.size(), 0, 0, 0, 0});
         ++h->classes.back().n;
-        groups.push_back(g);
+        shapes.push_back(g);
         bytes += 2 * up(2 * g.x_plane * count.back() * 2, 1024) + 2 * up(g.s_parts * g.s_plane * count.back() * 2, 1024);
       }
       if (bytes) e = cudaMalloc((void**)&h->arena, (size_t)bytes);
       if (e == cudaSuccess) {
         char* at = h->arena;
-        for (size_t i = 0; i < groups.size(); ++i) {
-          Group& g = groups[i];
+        maps.resize(shapes.size());
+        for (size_t i = 0; i < shapes.size(); ++i) {
+          Shape& g = shapes[i];
           const int n = count[i];
           const auto take = [&](int64_t elements) { __half* p = (__half*)at; at += up(elements * 2, 1024); return p; };
           for (int q = 0; q < 2; ++q) {
-            g.xp[q] = take(2 * g.x_plane * n);
-            mapped = mapped && mma::encode_map(&g.x[q], g.xp[q], false, g.cols, g.rows, 2ll * n, g.x_pitch, g.x_plane);
+            g.x[q] = take(2 * g.x_plane * n);
+            mapped = mapped && mma::encode_map(&maps[i].x[q], g.x[q], false, g.cols, g.rows, 2ll * n, g.x_pitch, g.x_plane);
           }
-          g.sp = take(g.s_parts * g.s_plane * n);
-          g.bp = take(g.s_parts * g.s_plane * n);
-          mapped = mapped && mma::encode_map(&g.s, g.sp, false, g.small, g.small, (int64_t)g.s_parts * n, g.s_pitch, g.s_plane);
-          mapped = mapped && mma::encode_map(&g.b, g.bp, false, g.small, g.small, (int64_t)g.s_parts * n, g.s_pitch, g.s_plane);
+          g.s = take(g.s_parts * g.s_plane * n);
+          g.b = take(g.s_parts * g.s_plane * n);
+          mapped = mapped && mma::encode_map(&maps[i].s, g.s, false, g.small, g.small, (int64_t)g.s_parts * n, g.s_pitch, g.s_plane);
+          mapped = mapped && mma::encode_map(&maps[i].b, g.b, false, g.small, g.small, (int64_t)g.s_parts * n, g.s_pitch, g.s_plane);
           for (int q = 0; q < n; ++q) {
-            const int i2 = members[i][q], j = i2 % T;
+            const int i2 = order[g.first + q], j = i2 % T;
             Place& p = places[i2];
             p.rows = g.rows; p.cols = g.cols; p.x_pitch = g.x_pitch; p.in_type = h->in_types[j]; p.out_type = h->out_types[j];
-            p.x = g.xp[0] + (long long)q * 2 * g.x_plane; p.x_plane = g.x_plane;
+            p.x = g.x[0] + (long long)q * 2 * g.x_plane; p.x_plane = g.x_plane;
+            p.done = h->done + g.first + q; p.ratio = h->ratios + g.first + q; p.plain = g.plain;
             p.first_chunk = (int)chunks.size();
             const int64_t units = (int64_t)g.rows * ((g.cols + UNIT - 1) / UNIT);
             for (int64_t u = 0; u < units; u += OT_CHUNK) chunks.push_back({i2, (int)u});
@@ -487,15 +649,8 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
           }
         }
         for (Class& c : h->classes) {
-          choose_tiles(c, groups, count, h->num_sms);
-          for (int i = c.first; i < c.first + c.n; ++i) {
-            Group& g = groups[i];
-            const int r = 128 * c.cg;
-            g.x_tile_cols = (g.cols + c.cols - 1) / c.cols; g.x_tiles = (g.rows + r - 1) / r * g.x_tile_cols;
-            g.s_tile_cols = (g.small + c.cols - 1) / c.cols; g.s_tiles = (g.small + r - 1) / r * g.s_tile_cols;
-            c.x_total += g.x_tiles * count[i]; c.s_total += g.s_tiles * count[i];
-            g.x_end = c.x_total; g.s_end = c.s_total;
-          }
+          choose_tiles(c, shapes, count, h->num_sms);
+          list_products(c, shapes, count, cfg->steps, batches);
         }
         h->chunks = (int)chunks.size();
       }
@@ -505,7 +660,9 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
     }
   }
   if (e == cudaSuccess && !mapped) e = cudaErrorUnknown;
-  if (e == cudaSuccess) e = upload(&h->groups, groups, h->stream);
+  if (e == cudaSuccess) e = upload(&h->maps, maps, h->stream);
+  if (e == cudaSuccess) e = upload(&h->shapes, shapes, h->stream);
+  if (e == cudaSuccess) e = upload(&h->batches, batches, h->stream);
   if (e == cudaSuccess) e = upload(&h->places, places, h->stream);
   if (e == cudaSuccess) e = upload(&h->chunk_list, chunks, h->stream);
   if (e == cudaSuccess) e = upload(&h->order, order, h->stream);
@@ -551,29 +708,28 @@ int sae_ortho_run(sae_ortho* h, const void* const* matrices, const int64_t* pitc
   if (e == cudaSuccess) e = launch(k_ortho_norm, h->chunks, h->stream, first, (const Matrix*)h->mats, (const Place*)h->places, (const Chunk*)h->chunk_list, h->sums);
   if (e == cudaSuccess) e = launch(k_ortho_split, h->chunks, h->stream, false, (const Matrix*)h->mats, (const Place*)h->places, (const Chunk*)h->chunk_list, (const double*)h->sums, h->eps, h->x_scale);
   for (const Class& c : h->classes) {
-    OrthoJob job = {};
+    static thread_local OrthoJob job;
+    job = {};
     job.cols = c.cols;
     job.rows = 128 * c.cg;
-    job.groups = h->groups + c.first;
+    if (c.parts == 2) job.seg = {3, {0, 1, 0}, {1, 0, 0}};
+    else job.seg = {1, {0}, {0}};
+    job.maps = h->maps + c.first;
+    job.shapes = h->shapes + c.first;
+    job.batches = h->batches + c.first_batch;
+    job.num_shapes = c.n; job.num_batches = c.batches; job.total = c.total; job.steps = h->steps; job.arrivals = c.cg;
+    job.done = h->done;
+    job.ratios = h->ratios;
     job.mats = h->mats;
     job.places = h->places;
     job.order = h->order;
-    if (c.parts == 2) job.seg = {3, {0, 1, 0}, {1, 0, 0}};
-    else job.seg = {1, {0}, {0}};
-    for (int i = 0; i < h->steps && e == cudaSuccess; ++i) {
+    for (int i = 0; i < h->steps; ++i) {
       const float* k = h->coef.data() + 3 * i;
-      const double sx = h->x_scale, ss = h->s_scale[i], sb = h->b_scale[i];
-      job.from = i & 1;
-      job.phase = PHASE_S; job.total = c.s_total; job.own = 0; job.sum = (float)(ss / (sx * sx));
-      e = products(h, c, job);
-      job.phase = PHASE_B; job.own = (float)(k[1] * sb / ss); job.sum = (float)(k[2] * sb / (ss * ss));
-      if (e == cudaSuccess) e = products(h, c, job);
-      job.last = i + 1 == h->steps;
-      job.phase = PHASE_X; job.total = c.x_total;
-      const double to = job.last ? 1.0 / sx : 1.0;
-      job.own = (float)(k[0] * to); job.sum = (float)(to / sb);
-      if (e == cudaSuccess) e = products(h, c, job);
+      const double sx = h->x_scale, ss = h->s_scale[i], sb = c.parts == 2 ? h->b_scale[i] : 1.0,      // (one part: B hi is added to x hi times 1)
+                   to = i + 1 == h->steps ? 1.0 / sx : 1.0;
+      job.factors[i] = {(float)(ss / (sx * sx)), (float)(k[0] * sb), (float)(k[1] * sb / ss), (float)(k[2] * sb / (ss * ss)), (float)(k[0] * to), (float)(to / sb)};
     }
+    if (e == cudaSuccess) e = mma::launch_products(job, c.cg, std::min(c.total, h->num_sms / c.cg), h->stream, true);
   }
   return e == cudaSuccess ? SAE_OK : cuda_status(h, e);
 }
