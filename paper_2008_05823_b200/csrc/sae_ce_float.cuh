@@ -1,0 +1,287 @@
+// The linear cross entropy of float tensors in small problems: ordinary float arithmetic.  Three bfloat16 parts cost a pass over the weights
+// and six products each, which pays only when there is enough of them (32 x 2048 x 1000, loss and gradients: 199 us there, see
+// CE_FLOAT_WORK for where the two meet).  Products are tiles of 32 x 64 by 128 threads, split along k until the SMs are
+// filled; whoever reads a product adds its splits in their order.
+#pragma once
+
+namespace {
+
+constexpr int CF_ROWS = 32, CF_COLS = 64, CF_K = 32, CF_THREADS = 128, CF_LOSS_THREADS = 512;
+
+enum FloatProduct { CF_Z, CF_DX, CF_DW };     // x w',  p w,  p' x
+
+struct FloatArgs {
+  const float *x, *w, *p;
+  const int *index, *counted;
+  int64_t x_pitch, w_pitch;
+  int p_pitch, features, classes;
+  int splits;
+  float* out;                                 // [splits][room][out_pitch]
+  int64_t room;
+  int out_pitch;
+  bool vector;                                // rows of x and w start on 16 bytes
+  // dweight in one split goes straight to the caller
+  float* dweight;
+  void* dbias;
+  int bias_type;
+  const float* alpha;
+};
+
+__device__ __forceinline__ void store_bias(void* out, int type, int64_t j, float v) {
+  if (type == SAE_TYPE_FLOAT) ((float*)out)[j] = v;
+  else if (type == SAE_TYPE_BFLOAT) ((__nv_bfloat16*)out)[j] = __float2bfloat16_rn(v);
+  else ((__half*)out)[j] = __float2half_rn(v);
+}
+
+// Four neighbours of a row to shared memory, those behind the first `n` as zeros.
+__device__ __forceinline__ void four_in(float* to, const float* from, int n, bool vector, const void* any) {      // any: an address, where nothing is read
+  const u32 at = smem_u32(to);
+  n = max(0, min(n, 4));
+  if (vector) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(n ? (const void*)from : any), "r"(4 * n) : "memory");
+  else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(at + 4 * i), "l"(i < n ? (const void*)(from + i) : any), "r"(i < n ? 4 : 0) : "memory");
+  }
+}
+
+constexpr int CF_STAGES = 4;
+// A and B as they lie in memory: rows of CF_K k, or rows of tile rows (columns) for each k; 4 more words a row, against bank conflicts.
+template <FloatProduct KIND>
+struct FloatTile {
+  static constexpr bool A_ROWS = KIND == CF_DW, B_ROWS = KIND != CF_Z;         // k is the slow direction
+  static constexpr int A_PITCH = (A_ROWS ? CF_ROWS : CF_K) + 4, B_PITCH = (B_ROWS ? CF_COLS : CF_K) + 4;
+  static constexpr int A_SIZE = A_PITCH * (A_ROWS ? CF_K : CF_ROWS), B_SIZE = B_PITCH * (B_ROWS ? CF_K : CF_COLS);
+  static constexpr int BYTES = CF_STAGES * (A_SIZE + B_SIZE) * 4;
+};
+
+template <FloatProduct KIND>
+__global__ void __launch_bounds__(CF_THREADS) k_cf_product(const __grid_constant__ FloatArgs a) {
+  typedef FloatTile<KIND> F;
+  extern __shared__ __align__(16) float smem[];
+  mma::let_next_start();
+  mma::wait_for_previous();
+  const int count = *a.counted, t = threadIdx.x;
+  const int rows = KIND == CF_DW ? a.classes : count, cols = KIND == CF_Z ? a.classes : a.features;
+  const int depth = KIND == CF_Z ? a.features : KIND == CF_DX ? a.classes : count;
+  const int row0 = blockIdx.y * CF_ROWS, col0 = blockIdx.x * CF_COLS;
+  if (row0 >= rows) return;
+  const int chunks = (depth + CF_K - 1) / CF_K, c0 = (int)((int64_t)chunks * blockIdx.z / a.splits), c1 = (int)((int64_t)chunks * (blockIdx.z + 1) / a.splits);
+  const auto fetch = [&](int chunk) {
+    if (chunk < c1) {
+      const int k0 = chunk * CF_K;
+      float* const sa = smem + (chunk - c0) % CF_STAGES * (F::A_SIZE + F::B_SIZE);
+      float* const sb = sa + F::A_SIZE;
+#pragma unroll
+      for (int u = t; u < CF_ROWS * CF_K / 4; u += CF_THREADS) {
+        if constexpr (KIND == CF_DW) {
+          const int k = u / (CF_ROWS / 4), r = u % (CF_ROWS / 4) * 4;
+          four_in(sa + k * F::A_PITCH + r, a.p + (int64_t)(k0 + k) * a.p_pitch + row0 + r, k0 + k < depth ? rows - row0 - r : 0, true, a.counted);
+        } else {
+          const int r = u / (CF_K / 4), k = u % (CF_K / 4) * 4;
+          const bool there = row0 + r < rows;
+          if constexpr (KIND == CF_Z) four_in(sa + r * F::A_PITCH + k, a.x + (there ? (int64_t)a.index[row0 + r] * a.x_pitch : 0) + k0 + k, there ? depth - k0 - k : 0, a.vector, a.counted);
+          else four_in(sa + r * F::A_PITCH + k, a.p + (int64_t)(row0 + r) * a.p_pitch + k0 + k, there ? depth - k0 - k : 0, true, a.counted);
+        }
+      }
+#pragma unroll
+      for (int u = t; u < CF_COLS * CF_K / 4; u += CF_THREADS) {
+        if constexpr (KIND == CF_Z) {
+          const int c = u / (CF_K / 4), k = u % (CF_K / 4) * 4;
+          four_in(sb + c * F::B_PITCH + k, a.w + (int64_t)(col0 + c) * a.w_pitch + k0 + k, col0 + c < cols ? depth - k0 - k : 0, a.vector, a.counted);
+        } else {
+          const int k = u / (CF_COLS / 4), c = u % (CF_COLS / 4) * 4;
+          const bool there = k0 + k < depth;
+          const float* const row = KIND == CF_DX ? a.w + (int64_t)(k0 + k) * a.w_pitch : a.x + (there ? (int64_t)a.index[k0 + k] * a.x_pitch : 0);
+          four_in(sb + k * F::B_PITCH + c, row + col0 + c, there ? cols - col0 - c : 0, a.vector, a.counted);
+        }
+      }
+    }
+    copies_commit();
+  };
+  // this thread's rows and columns of the tile
+  const int tr = t / 16, tc = t % 16;
+  const auto row_of = [&](int i) { return F::A_ROWS ? tr * 4 + i : tr + 8 * i; };
+  const auto col_of = [&](int j) { return F::B_ROWS ? tc * 4 + j : tc + 16 * j; };
+  float acc[4][4] = {};
+#pragma unroll
+  for (int i = 0; i < CF_STAGES - 1; ++i) fetch(c0 + i);
+  for (int c = c0; c < c1; ++c) {
+    copies_wait<CF_STAGES - 2>();
+    __syncthreads();
+    fetch(c + CF_STAGES - 1);
+    const float* const sa = smem + (c - c0) % CF_STAGES * (F::A_SIZE + F::B_SIZE);
+    const float* const sb = sa + F::A_SIZE;
+#pragma unroll
+    for (int k = 0; k < CF_K; k += 4) {
+      float x[4][4], y[4][4];             // [row or column][k]
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 v = *reinterpret_cast<const float4*>(F::A_ROWS ? sa + (k + i) * F::A_PITCH + tr * 4 : sa + row_of(i) * F::A_PITCH + k);
+        const float4 w = *reinterpret_cast<const float4*>(F::B_ROWS ? sb + (k + i) * F::B_PITCH + tc * 4 : sb + col_of(i) * F::B_PITCH + k);
+        const float vs[4] = {v.x, v.y, v.z, v.w}, ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (F::A_ROWS) x[q][i] = vs[q]; else x[i][q] = vs[q];
+          if (F::B_ROWS) y[q][i] = ws[q]; else y[i][q] = ws[q];
+        }
+      }
+      if (KIND == CF_DW) {                // dbias: a feature that is always 1
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (col0 + col_of(j) == a.features) y[j][0] = y[j][1] = y[j][2] = y[j][3] = 1.0f;
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[i][j] = __fmaf_rn(x[i][q], y[j][q], acc[i][j]);
+    }
+  }
+  copies_wait<0>();
+  if (KIND == CF_DW && a.splits == 1) {
+    const float alpha = *a.alpha;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t r = row0 + row_of(i);
+      if (r >= rows) continue;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = col0 + col_of(j);
+        if (c < a.features) { if (a.dweight) a.dweight[r * a.features + c] = acc[i][j] * alpha; }
+        else if (c == a.features && a.dbias) store_bias(a.dbias, a.bias_type, r, acc[i][j] * alpha);
+      }
+    }
+    return;
+  }
+  float* const out = a.out + (int64_t)blockIdx.z * a.room * a.out_pitch;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = row0 + row_of(i);
+    if (r >= rows) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = col0 + col_of(j);
+      if (c < a.out_pitch) out[(int64_t)r * a.out_pitch + c] = acc[i][j];
+    }
+  }
+}
+
+struct FloatRowArgs {
+  const float* z;                             // [splits][room][pitch]
+  const void* bias;
+  const int *index, *at, *counted;
+  int64_t room;
+  int splits, pitch, classes, bias_type, reduction;
+  // loss
+  float *loss, *lse;
+  double* sums;
+  unsigned* ticket;
+  // p
+  const float *lse_g, *g;
+  float* p;
+};
+__device__ __forceinline__ float bias_of(const FloatRowArgs& a, int j) {
+  if (!a.bias) return 0.0f;
+  return a.bias_type == SAE_TYPE_FLOAT ? ((const float*)a.bias)[j]
+         : a.bias_type == SAE_TYPE_BFLOAT ? to_f(((const __nv_bfloat16*)a.bias)[j]) : to_f(((const __half*)a.bias)[j]);
+}
+__device__ __forceinline__ float logit_of(const FloatRowArgs& a, int64_t row, int j) {
+  float v = 0;
+#pragma unroll 8
+  for (int s = 0; s < a.splits; ++s) v += __ldcg(a.z + (s * a.room + row) * a.pitch + j);
+  return v + bias_of(a, j);
+}
+__device__ __forceinline__ void join_runs(float& m, float& s, float om, float os) {
+  const float top = fmaxf(m, om);
+  if (top > __int_as_float(0xff800000)) s = s * exp2f((m - top) * LOG2E) + os * exp2f((om - top) * LOG2E);
+  else s += os;
+  m = top;
+}
+
+// A block a row: maximum and sum, then the loss; the last block adds the rows' losses in their order.
+__global__ void __launch_bounds__(CF_LOSS_THREADS) k_cf_loss(const __grid_constant__ FloatRowArgs a) {
+  __shared__ float sm[CF_LOSS_THREADS / 32], ss[CF_LOSS_THREADS / 32];
+  __shared__ double sd[CF_LOSS_THREADS / 32];
+  __shared__ bool final_block;
+  mma::let_next_start();
+  mma::wait_for_previous();
+  const int count = *a.counted, i = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  double loss_d = 0;
+  if (i < count) {
+    float m = __int_as_float(0xff800000), s = 0;
+    for (int j = threadIdx.x; j < a.classes; j += CF_LOSS_THREADS) {
+      const float z = logit_of(a, i, j);
+      if (z > m) { s *= exp2f((m - z) * LOG2E); m = z; }
+      s += m == __int_as_float(0xff800000) ? (z != z ? z : 0.0f) : exp2f((z - m) * LOG2E);
+    }
+    for (int o = 16; o; o >>= 1) {
+      const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o);
+      join_runs(m, s, om, os);
+    }
+    if (lane == 0) { sm[warp] = m; ss[warp] = s; }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int k = 1; k < CF_LOSS_THREADS / 32; ++k) join_runs(m, s, sm[k], ss[k]);
+      const int t = a.at[i];
+      const float z = t >= 0 ? logit_of(a, i, t) : __int_as_float(0x7fc00000), loss = logf(s) + (m - z);
+      a.lse[a.index[i]] = m + logf(s);
+      if (a.reduction == SAE_REDUCE_NONE) a.loss[a.index[i]] = loss;
+      loss_d = loss;
+    }
+  }
+  if (a.reduction == SAE_REDUCE_NONE) return;
+  if (threadIdx.x == 0) {
+    a.sums[i] = loss_d;
+    __threadfence();
+    final_block = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!final_block) return;
+  __threadfence();
+  double sum = 0;
+  for (int k = threadIdx.x; k < (int)gridDim.x; k += CF_LOSS_THREADS) sum += __ldcg(a.sums + k);
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) sd[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int k = 1; k < CF_LOSS_THREADS / 32; ++k) sum += sd[k];
+    *a.loss = (float)(a.reduction == SAE_REDUCE_MEAN ? sum / (double)count : sum);
+  }
+}
+
+__global__ void __launch_bounds__(CF_THREADS) k_cf_p(const __grid_constant__ FloatRowArgs a) {
+  mma::let_next_start();
+  mma::wait_for_previous();
+  const int i = blockIdx.y, j = blockIdx.x * CF_THREADS + threadIdx.x;
+  if (i >= *a.counted || j >= a.classes) return;
+  const float p = exp2f((logit_of(a, i, j) - a.lse_g[i]) * LOG2E);
+  a.p[(int64_t)i * a.pitch + j] = (j == a.at[i] ? p - 1.0f : p) * a.g[i];
+}
+
+// out = alpha * the sum of the splits; rows to where they belong, the column behind the features to dbias.
+struct FloatSumArgs {
+  const float* sums;
+  const int *counted, *index;
+  const float* alpha;
+  float* out;
+  void* dbias;
+  int64_t room;
+  int splits, pitch, features, bias_type, rows;      // rows < 0: those that are counted
+};
+__global__ void __launch_bounds__(CF_THREADS) k_cf_sum(const __grid_constant__ FloatSumArgs a) {
+  mma::let_next_start();
+  mma::wait_for_previous();
+  const int64_t r = blockIdx.y;
+  const int c = blockIdx.x * CF_THREADS + threadIdx.x;
+  if (r >= (a.rows < 0 ? *a.counted : a.rows) || c > a.features) return;
+  if (c == a.features && !a.dbias) return;
+  float v = 0;
+#pragma unroll 8
+  for (int s = 0; s < a.splits; ++s) v += __ldcg(a.sums + (s * a.room + r) * a.pitch + c);
+  v *= *a.alpha;
+  if (c == a.features) store_bias(a.dbias, a.bias_type, r, v);
+  else if (a.out) a.out[(a.index ? (int64_t)a.index[r] : r) * a.features + c] = v;
+}
+
+}  // namespace

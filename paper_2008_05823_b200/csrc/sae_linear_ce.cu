@@ -23,7 +23,7 @@ constexpr int CE_THREADS = 256;
 constexpr int CE_ROWS = 32;                   // rows of a block of k_ce_rows
 constexpr int CE_COUNT_ROWS = 4096;           // rows counted by a block of k_ce_count
 constexpr int CE_SCAN_ROWS = 16384;           // up to here every block counts the rows before its own by itself
-constexpr int CE_CHUNK = 2048;                // units that a block copies
+constexpr int CE_CHUNK = 1024;                // units that a block copies
 constexpr int64_t CE_PIECE_BYTES = 256ll << 20;
 constexpr float LOG2E = 1.44269504088896340736f;
 
@@ -221,6 +221,7 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_rows(const __grid_constant__ 
     if (r >= a.rows) break;
     const int to = place[i];
     if (to >= 0) {
+      if (!a.xg) continue;
       const char* from = (const char*)a.x + r * a.x_pitch * es;
       for (int c = lane * UNIT; c < a.pitch; c += 32 * UNIT)
         put_unit(from + (int64_t)c * es, a.type, a.parts, min(UNIT, a.features - c), a.xg + (int64_t)to * a.pitch + c, a.xg_plane);
@@ -232,7 +233,7 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_rows(const __grid_constant__ 
       }
     }
   }
-  if (BACKWARD && b + 1 == a.row_blocks) {          // the last block of k of dweight's product reads zeros behind the last row
+  if (BACKWARD && a.xg && b + 1 == a.row_blocks) {  // the last block of k of dweight's product reads zeros behind the last row
     int last = -1;
     for (int i = 0; i < CE_ROWS; ++i) last = max(last, place[i]);
     const int n = last >= 0 ? last + 1 : base, wide = a.pitch / UNIT;
@@ -544,6 +545,7 @@ __device__ __host__ inline int dx_splits(int blocks, int tiles_across, int clust
 
 // dx's sums (p w, float, added up over the pieces) and dweight of a piece (p' x).
 struct ProductJob : mma::Plain {
+  static constexpr int STAGING = mma::SQUARE_BYTES;
   int cols;
   bool bfloat;
   mma::Segments seg;
@@ -553,18 +555,20 @@ struct ProductJob : mma::Plain {
   int start, width;               // the piece's first class and its classes, rounded up to 64
   bool dx;
   // dx
-  float* sums;
+  float* sums;                    // dweight: those of its splits, where it has more than one
   int sums_pitch, room, add;      // room: row blocks that the sums have place for
+  int dw_splits;
   // dweight
   void* out;
   int type, classes;              // classes of the piece
+  bool whole_rows;                // every row starts on 32 bytes
   const float* alpha;
 
   struct Local { int first, step, blocks, splits, count; };
   __device__ __forceinline__ Local begin(const Shared&, int cluster, int clusters) const {
     Local l = {cluster, clusters, 0, 1, *counted};
     l.blocks = ((dx ? l.count : classes) + rows - 1) / rows;
-    if (dx) l.splits = dx_splits(l.blocks, across, clusters, l.blocks ? room / l.blocks : 1);
+    l.splits = dx ? dx_splits(l.blocks, across, clusters, l.blocks ? room / l.blocks : 1) : dw_splits;
     return l;
   }
   __device__ __forceinline__ bool tile(Local& l, int i, mma::Tile& t) const {
@@ -592,7 +596,8 @@ struct ProductJob : mma::Plain {
     const int row, half;
     const float alpha;
     const int limit;
-    __device__ __forceinline__ Epilogue(const ProductJob& j, const Local& l, int r, int h, u32) : job(j), row(r), half(h), alpha(j.dx ? 1.0f : *j.alpha), limit(j.dx ? l.count : j.classes) {}
+    const u32 staging;
+    __device__ __forceinline__ Epilogue(const ProductJob& j, const Local& l, int r, int h, u32 at) : job(j), row(r), half(h), alpha(j.dx || j.dw_splits > 1 ? 1.0f : *j.alpha), limit(j.dx ? l.count : j.classes), staging(at) {}
     __device__ __forceinline__ void prepare(const mma::Tile&, int, mma::Control*) {}
     __device__ __forceinline__ void finish() {}
     __device__ __forceinline__ void tile(const mma::Tile& t, const mma::Sums& sums) {
@@ -602,8 +607,21 @@ struct ProductJob : mma::Plain {
         if (col >= job.features) break;
         float v[32];
         mma::sums_of(sums, c, v);
+        const bool apart = job.dx || job.dw_splits > 1;
+        if (!apart && !job.whole_rows) {
+          const int row0 = t.row + (row & ~31);
+          if (row0 >= limit) continue;                    // the whole warp's
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] *= alpha;
+          const int64_t to = (int64_t)(job.start + row0) * job.features + col;
+          const int m = min(32, limit - row0), n = min(32, job.features - col);
+          if (job.type == SAE_TYPE_FLOAT) mma::store_square((float*)job.out + to, job.features, v, m, n, staging);
+          else if (job.type == SAE_TYPE_BFLOAT) mma::store_square((__nv_bfloat16*)job.out + to, job.features, v, m, n, staging);
+          else mma::store_square((__half*)job.out + to, job.features, v, m, n, staging);
+          continue;
+        }
         if (r >= limit) continue;
-        if (job.dx) {
+        if (apart) {
           float* const to = job.sums + ((int64_t)t.item * t.group + r) * job.sums_pitch + col;
           if (job.add) {
 #pragma unroll
@@ -629,13 +647,14 @@ struct ProductJob : mma::Plain {
   };
 };
 
-// dx = alpha * the sums over the splits, back to the rows that they belong to.
+// dx = alpha * the sums over the splits, back to the rows that they belong to; dweight likewise.
 struct DxArgs {
   const float* sums;
   const int *counted, *index;
   const float* alpha;
   void* dx;
   int sums_pitch, features, type, rows, across, clusters, room;
+  int dw_rows, dw_splits;           // dweight: its rows and splits (0: this is dx)
 };
 template <typename T>
 __device__ __forceinline__ void put_row(T* to, const float (&v)[UNIT], int n) {
@@ -656,9 +675,9 @@ __device__ __forceinline__ void put_row(T* to, const float (&v)[UNIT], int n) {
 __global__ void __launch_bounds__(CE_THREADS) k_ce_dx(const __grid_constant__ DxArgs a) {
   mma::let_next_start();
   mma::wait_for_previous();
-  const int count = *a.counted, blocks = (count + a.rows - 1) / a.rows;
+  const int count = a.dw_splits ? a.dw_rows : *a.counted, blocks = (count + a.rows - 1) / a.rows;
   if (!blocks) return;
-  const int splits = dx_splits(blocks, a.across, a.clusters, a.room / blocks);
+  const int splits = a.dw_splits ? a.dw_splits : dx_splits(blocks, a.across, a.clusters, a.room / blocks);
   const int64_t plane = (int64_t)blocks * a.rows * a.sums_pitch;
   const float alpha = *a.alpha;
   const unsigned wide = (unsigned)(a.features + UNIT - 1) / UNIT;
@@ -675,7 +694,7 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_dx(const __grid_constant__ Dx
 #pragma unroll
     for (int k = 0; k < UNIT; ++k) v[k] *= alpha;
     const int n = min(UNIT, a.features - c);
-    const int64_t to = (int64_t)a.index[r] * a.features + c;
+    const int64_t to = (a.dw_splits ? r : (int64_t)a.index[r]) * a.features + c;
     if (a.type == SAE_TYPE_FLOAT) put_row((float*)a.dx + to, v, n);
     else if (a.type == SAE_TYPE_BFLOAT) put_row((__nv_bfloat16*)a.dx + to, v, n);
     else put_row((__half*)a.dx + to, v, n);
@@ -700,6 +719,12 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_dbias(const float* sums, int 
   else ((__half*)out)[j] = __float2half_rn(v);
 }
 
+}  // namespace
+
+#include "sae_ce_float.cuh"
+
+namespace {
+
 // ---- host ---------------------------------------------------------------------------------------------------------------------
 bool type_ok(int t) { return t == SAE_TYPE_FLOAT || t == SAE_TYPE_BFLOAT || t == SAE_TYPE_HALF; }
 
@@ -713,6 +738,21 @@ int device_sms() {
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return -1; }
   return sms;
+}
+
+// Float tensors take float arithmetic up to so many rows and products (rows * classes * features).  Loss and gradients, us, there and in
+// bfloat16 parts: 32 x 2048 x 1000 69 and 202, 128 x 2048 x 1000 125 and 199, 256 x 2048 x 1000 197 and 215, 512 x 2048 x 1000 362 and
+// 241, 8 x 768 x 30522 353 and 361, 128 x 768 x 30522 936 and 437.
+constexpr int64_t CE_FLOAT_ROWS = 256, CE_FLOAT_WORK = 1ll << 29;
+bool in_float(const sae_linear_ce_desc* d) {
+  return d->type == SAE_TYPE_FLOAT && d->rows <= CE_FLOAT_ROWS && d->classes <= (1 << 20) && d->rows * d->classes <= CE_FLOAT_WORK / d->features;
+}
+// Splits of k, from what does not depend on the rows, so that a row's result does not either: four blocks an SM for a single block of
+// rows, and no split of less than 64 k (least k unknown: 0).
+int float_splits(int64_t tiles, int64_t depth, int most, int sms) {
+  int64_t s = std::min<int64_t>(4ll * sms / tiles, most);
+  if (depth) s = std::min<int64_t>(s, depth / 64);
+  return (int)std::max<int64_t>(1, s);
 }
 
 struct TileShape { int cg, cols; };
@@ -737,9 +777,36 @@ struct CePlan {
   TileShape z, dx, dw;
   int piece, pieces, p_pitch;        // classes of a piece
   int sums_pitch, dx_room;
+  size_t dw_sums;
   // offsets
+  // in float arithmetic (dw_splits: in the other too)
+  bool in_float;
+  int z_splits, dx_splits, dw_splits, z_pitch, dx_pitch, dw_pitch;
+  size_t fz, fdx, fdw;
   size_t xg, wg, bias, index, at, at_z, counted, before, runs, sums, lse_g, g, alpha, top, p, bias_sums, dx_sums, bytes;
 };
+
+// Classes of a piece, in blocks of 256: as many as the bytes allow, or fewer where the tiles of its products then come out as
+// whole waves.  Time in units of a tile's k: waves of p, of dweight, of dx (in splits), and what three more launches cost.
+// 8192 rows of 768, 30522 classes: 24 blocks at a time instead of 60, 72 tiles of dweight on 74 pairs instead of 180.
+int piece_blocks(const sae_linear_ce_desc* d, int64_t rows, int parts, int sms) {
+  const int64_t all = (d->classes + 255) / 256, most = std::max<int64_t>(1, std::min(all, CE_PIECE_BYTES / (rows * 2 * parts) / 256));
+  const int64_t units = sms / 2, down = (d->rows + 255) / 256, across = (d->features + 255) / 256;
+  const auto waves = [&](int64_t tiles) { return (double)((tiles + units - 1) / units); };
+  int64_t best = most;
+  double least = 0;
+  for (int64_t b = most; b >= std::max<int64_t>(1, most / 4); --b) {
+    double dx = 0;
+    for (int s = 1; s <= 8; ++s) {
+      const double t = waves(down * across * s) / s * (1.0 + 0.03 * s);
+      if (s == 1 || t < dx) dx = t;
+    }
+    const double pieces = (double)((all + b - 1) / b);
+    const double t = pieces * (parts * (waves(down * b) * (double)d->features + waves(b * across) * (double)d->rows + dx * 256.0 * (double)b) + 2500.0);
+    if (least == 0 || t < 0.99 * least) { least = t; best = b; }
+  }
+  return (int)best;
+}
 
 CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward, int sms) {
   CePlan p = {};
@@ -748,8 +815,35 @@ CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward,
   p.rows = up(std::max<int64_t>(1, d->rows), 256);
   // (one row of weights has no pitch of its own: any that TMA takes will do)
   p.copy_w = p.parts > 1 || !aligned_to(weight, 16) || (d->classes > 1 && d->weight_pitch % 8);
+  p.in_float = in_float(d);
+  if (p.in_float) p.parts = 1;
   size_t at = 0;
   const auto take = [&](int64_t bytes) { const size_t o = at; at += (size_t)up(std::max<int64_t>(bytes, 1), 256); return o; };
+  if (p.in_float) {
+    const int64_t n = std::max<int64_t>(1, d->rows);
+    p.index = take(n * 4);
+    p.at = take(n * 4);
+    p.counted = take(8);
+    p.before = take(d->rows > CE_SCAN_ROWS ? up(d->rows, CE_COUNT_ROWS) / CE_COUNT_ROWS * 4 : 0);
+    p.z_pitch = (int)up(d->classes, 4);
+    p.z_splits = float_splits((d->classes + CF_COLS - 1) / CF_COLS, d->features, 8, sms);
+    p.fz = take((int64_t)p.z_splits * n * p.z_pitch * 4);
+    p.sums = take(n * 8);
+    if (backward) {
+      p.lse_g = take(n * 4);
+      p.g = take(n * 4);
+      p.alpha = take(4);
+      p.p = take(n * p.z_pitch * 4);
+      p.dx_pitch = (int)up(d->features, 4);
+      p.dx_splits = float_splits((d->features + CF_COLS - 1) / CF_COLS, d->classes, 32, sms);
+      p.fdx = take((int64_t)p.dx_splits * n * p.dx_pitch * 4);
+      p.dw_pitch = (int)up(d->features + 1, 4);
+      p.dw_splits = float_splits((d->classes + CF_ROWS - 1) / CF_ROWS * ((d->features + CF_COLS) / CF_COLS), 0, 32, sms);
+      p.fdw = take(p.dw_splits > 1 ? (int64_t)p.dw_splits * d->classes * p.dw_pitch * 4 : 0);
+    }
+    p.bytes = at;
+    return p;
+  }
   p.xg = take((int64_t)p.parts * p.rows * p.pitch * 2);
   p.wg = take(p.copy_w ? (int64_t)p.parts * d->classes * p.pitch * 2 : 0);
   p.bias = take(d->has_bias ? up(d->classes, 256) * 4 + 1024 : 0);
@@ -769,9 +863,7 @@ CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward,
     p.g = take(p.rows * 4);
     p.alpha = take(4);
     p.top = take(4);
-    const int64_t most = std::max<int64_t>(256, CE_PIECE_BYTES / (p.rows * 2 * p.parts) / 256 * 256);
-    p.pieces = (int)((d->classes + most - 1) / most);
-    p.piece = (int)up((d->classes + p.pieces - 1) / p.pieces, 256);
+    p.piece = 256 * piece_blocks(d, p.rows, p.parts, sms);
     p.pieces = (int)((d->classes + p.piece - 1) / p.piece);
     p.p_pitch = p.piece;
     p.dx = tile_shape(d->rows, d->features, p.parts, sms);
@@ -782,16 +874,23 @@ CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward,
     p.p = take((int64_t)p.parts * p.rows * p.p_pitch * 2);
     p.bias_sums = take(d->has_bias ? p.rows / 32 * p.p_pitch * 4 : 0);
     p.dx_sums = take((int64_t)p.dx_room * rows * p.sums_pitch * 4);
+    // A head of few classes has a tile or two of dweight, and all rows to add up in it (16384 x 64 x 10 float: 470 us on one SM).  In two
+    // launches more where that leaves half of the SMs idle; no split of less than 512 rows.
+    const int dw_rows = 128 * p.dw.cg;
+    const int64_t dw_tiles = up(p.piece, dw_rows) / dw_rows * (up(d->features, p.dw.cols) / p.dw.cols);
+    p.dw_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(sms / p.dw.cg / dw_tiles, d->rows / 512), 32));
+    p.dw_sums = take(p.dw_splits > 1 ? (int64_t)p.dw_splits * up(p.piece, dw_rows) * p.sums_pitch * 4 : 0);
   }
   p.bytes = at;
   return p;
 }
 
 template <typename... P, typename... A>
-int launch(void (*kernel)(P...), int64_t blocks, int threads, cudaStream_t st, bool first, A... args) {
+int launch_shared(void (*kernel)(P...), dim3 grid, int threads, size_t shared, cudaStream_t st, bool first, A... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = shared;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -800,6 +899,10 @@ int launch(void (*kernel)(P...), int64_t blocks, int threads, cudaStream_t st, b
   cfg.numAttrs = first ? 0 : 1;
   if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
   return SAE_OK;
+}
+template <typename... P, typename... A>
+int launch(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t st, bool first, A... args) {
+  return launch_shared(kernel, grid, threads, 0, st, first, args...);
 }
 
 template <class Job>
@@ -819,13 +922,14 @@ RowsArgs rows_args(const sae_linear_ce_desc* d, const CePlan& p, const void* x, 
   RowsArgs a = {};
   a.x = x; a.target = target; a.x_pitch = d->x_pitch; a.rows = d->rows; a.ignore = d->ignore_index;
   a.type = d->type; a.parts = p.parts; a.features = (int)d->features; a.classes = (int)d->classes; a.pitch = p.pitch;
-  a.xg = (unsigned short*)(ws + p.xg); a.xg_plane = p.rows * p.pitch;
+  a.xg = p.in_float ? nullptr : (unsigned short*)(ws + p.xg);      // (float arithmetic reads rows where they are)
+  a.xg_plane = p.rows * p.pitch;
   a.index = (int*)(ws + p.index); a.at = (int*)(ws + p.at); a.counted = (int*)(ws + p.counted); a.ticket = (unsigned*)(ws + p.counted + 4);
   a.w = w; a.w_pitch = d->weight_pitch; a.wg = (unsigned short*)(ws + p.wg); a.wg_plane = d->classes * p.pitch;
   a.bias = bias; a.bias_type = d->bias_type; a.bias_out = (float*)(ws + p.bias);
-  a.bias_room = d->has_bias ? (int)up(d->classes, 256) : 0;
+  a.bias_room = d->has_bias && !p.in_float ? (int)up(d->classes, 256) : 0;
   a.row_blocks = (int)std::max<int64_t>(1, up(d->rows, CE_ROWS) / CE_ROWS);
-  a.w_blocks = p.copy_w ? (int)(up(d->classes * (p.pitch / UNIT), CE_CHUNK) / CE_CHUNK) : 0;
+  a.w_blocks = p.copy_w && !p.in_float ? (int)(up(d->classes * (p.pitch / UNIT), CE_CHUNK) / CE_CHUNK) : 0;
   a.reduction = d->reduction;
   return a;
 }
@@ -856,6 +960,76 @@ bool maps(const sae_linear_ce_desc* d, const CePlan& p, const void* weight, char
                    : mma::encode_map(w, weight, bfloat, d->features, d->classes, 1, d->classes > 1 ? d->weight_pitch : p.pitch, p.pitch));
 }
 
+template <FloatProduct KIND>
+int float_product(FloatArgs a, int64_t rows, int64_t cols, int splits, float* out, int64_t room, int pitch, cudaStream_t st) {
+  a.splits = splits; a.out = out; a.room = room; a.out_pitch = pitch;
+  const dim3 grid((unsigned)((cols + CF_COLS - 1) / CF_COLS), (unsigned)((rows + CF_ROWS - 1) / CF_ROWS), (unsigned)splits);
+  // (55 KB of shared memory at most: more than a kernel has unasked)
+  static std::atomic<unsigned long long> ready{0};
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
+  const unsigned long long bit = device < 64 ? 1ull << device : 0;
+  if (!(ready.load(std::memory_order_acquire) & bit)) {
+    if (cudaFuncSetAttribute(k_cf_product<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, FloatTile<KIND>::BYTES) != cudaSuccess) { cudaGetLastError(); return SAE_ERR_CUDA; }
+    ready.fetch_or(bit, std::memory_order_release);
+  }
+  return launch_shared(k_cf_product<KIND>, grid, CF_THREADS, FloatTile<KIND>::BYTES, st, false, a);
+}
+
+FloatArgs float_args(const sae_linear_ce_desc* d, const CePlan& p, const RowsArgs& a, char* ws) {
+  FloatArgs f = {};
+  f.x = (const float*)a.x; f.w = (const float*)a.w; f.p = (const float*)(ws + p.p);
+  f.index = a.index; f.counted = a.counted;
+  f.x_pitch = d->x_pitch; f.w_pitch = d->weight_pitch;
+  f.p_pitch = p.z_pitch; f.features = a.features; f.classes = a.classes;
+  f.vector = aligned_to(a.x, 16) && aligned_to(a.w, 16) && (d->rows < 2 || d->x_pitch % 4 == 0) && (d->classes < 2 || d->weight_pitch % 4 == 0);
+  f.alpha = a.alpha;
+  return f;
+}
+FloatRowArgs float_rows(const sae_linear_ce_desc* d, const CePlan& p, const RowsArgs& a, char* ws) {
+  FloatRowArgs r = {};
+  r.z = (const float*)(ws + p.fz); r.bias = a.bias; r.index = a.index; r.at = a.at; r.counted = a.counted;
+  r.room = std::max<int64_t>(1, d->rows); r.splits = p.z_splits; r.pitch = p.z_pitch; r.classes = a.classes; r.bias_type = a.bias_type; r.reduction = d->reduction;
+  r.sums = (double*)(ws + p.sums); r.ticket = a.ticket;
+  return r;
+}
+
+int float_forward(const sae_linear_ce_desc* d, const CePlan& p, RowsArgs& a, float* loss, float* lse, char* ws, int, cudaStream_t st) {
+  int rc = gather<false>(d, p, a, ws, st);
+  if (rc == SAE_OK && d->rows) rc = float_product<CF_Z>(float_args(d, p, a, ws), d->rows, d->classes, p.z_splits, (float*)(ws + p.fz), d->rows, p.z_pitch, st);
+  FloatRowArgs r = float_rows(d, p, a, ws);
+  r.loss = loss; r.lse = lse;
+  if (rc == SAE_OK) rc = launch(k_cf_loss, dim3((unsigned)std::max<int64_t>(1, d->rows)), CF_LOSS_THREADS, st, false, r);
+  return rc;
+}
+
+int float_backward(const sae_linear_ce_desc* d, const CePlan& p, RowsArgs& a, void* dx, void* dweight, void* dbias, char* ws, cudaStream_t st) {
+  int rc = gather<true>(d, p, a, ws, st);
+  FloatArgs f = float_args(d, p, a, ws);
+  if (rc == SAE_OK && d->rows) rc = float_product<CF_Z>(f, d->rows, d->classes, p.z_splits, (float*)(ws + p.fz), d->rows, p.z_pitch, st);
+  FloatRowArgs r = float_rows(d, p, a, ws);
+  r.lse_g = a.lse_g; r.g = a.g; r.p = (float*)(ws + p.p);
+  if (rc == SAE_OK && d->rows) rc = launch(k_cf_p, dim3((unsigned)((d->classes + CF_THREADS - 1) / CF_THREADS), (unsigned)d->rows), CF_THREADS, st, false, r);
+  FloatSumArgs s = {};
+  s.counted = a.counted; s.alpha = a.alpha; s.features = a.features; s.bias_type = d->bias_type;
+  if (dx && d->rows) {
+    if (rc == SAE_OK) rc = float_product<CF_DX>(f, d->rows, d->features, p.dx_splits, (float*)(ws + p.fdx), d->rows, p.dx_pitch, st);
+    s.sums = (const float*)(ws + p.fdx); s.index = a.index; s.out = (float*)dx; s.room = d->rows; s.splits = p.dx_splits; s.pitch = p.dx_pitch; s.rows = -1;
+    if (rc == SAE_OK) rc = launch(k_cf_sum, dim3((unsigned)((d->features + CF_THREADS) / CF_THREADS), (unsigned)d->rows), CF_THREADS, st, false, s);
+  }
+  if (dweight || dbias) {
+    f.dweight = (float*)dweight; f.dbias = dbias; f.bias_type = d->bias_type;
+    if (rc == SAE_OK) rc = float_product<CF_DW>(f, d->classes, d->features + (dbias ? 1 : 0), p.dw_splits, (float*)(ws + p.fdw), d->classes, p.dw_pitch, st);
+    if (p.dw_splits > 1) {
+      // (only few classes are split: far fewer than a grid has rows)
+      s.sums = (const float*)(ws + p.fdw); s.index = nullptr; s.out = (float*)dweight; s.dbias = dbias; s.room = d->classes; s.splits = p.dw_splits; s.pitch = p.dw_pitch;
+      s.rows = (int)d->classes;
+      if (rc == SAE_OK) rc = launch(k_cf_sum, dim3((unsigned)((d->features + 1 + CF_THREADS - 1) / CF_THREADS), (unsigned)d->classes), CF_THREADS, st, false, s);
+    }
+  }
+  return rc;
+}
+
 }  // namespace
 
 extern "C" {
@@ -880,6 +1054,7 @@ int sae_linear_ce_forward(const sae_linear_ce_desc* d, const void* x, const void
   char* ws = (char*)workspace;
   RowsArgs a = rows_args(d, p, x, weight, d->has_bias ? bias : nullptr, target, ws);
   a.count = count; a.lse = lse; a.loss = d->reduction == SAE_REDUCE_NONE ? loss : nullptr;
+  if (p.in_float) return float_forward(d, p, a, loss, lse, ws, sms, st);
   LossJob job = {};
   if (!maps(d, p, weight, ws, &job.x, &job.w)) return SAE_ERR_CUDA;
   int rc = gather<false>(d, p, a, ws, st);
@@ -916,6 +1091,7 @@ int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, cons
   a.lse_in = lse; a.dloss = dloss; a.count_in = count; a.dx = dx;
   a.lse_g = (float*)(ws + p.lse_g); a.g = (float*)(ws + p.g); a.alpha = (float*)(ws + p.alpha);
   a.p_scale = d->type == SAE_TYPE_HALF ? 32768.0f : 1.0f;
+  if (p.in_float) return float_backward(d, p, a, dx, dweight, dbias, ws, st);
   GradJob g = {};
   if (!maps(d, p, weight, ws, &g.x, &g.w)) return SAE_ERR_CUDA;
   const bool bfloat = d->type != SAE_TYPE_HALF;
@@ -950,11 +1126,17 @@ int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, cons
     if (dweight && rc == SAE_OK) {
       job.dx = false; job.b = g.x; job.cols = p.dw.cols; job.rows = 128 * p.dw.cg; job.across = (int)(up(d->features, p.dw.cols) / p.dw.cols);
       job.out = dweight;
-      rc = products(job, p.dw, up(classes, job.rows) / job.rows * job.across, sms, st);
+      job.dw_splits = p.dw_splits; job.sums = (float*)(ws + p.dw_sums); job.sums_pitch = p.sums_pitch; job.add = 0;
+      job.whole_rows = aligned_to(dweight, 32) && d->features * es % 32 == 0;
+      rc = products(job, p.dw, up(classes, job.rows) / job.rows * job.across * p.dw_splits, sms, st);
+      if (rc == SAE_OK && p.dw_splits > 1) {
+        DxArgs x1 = {job.sums, a.counted, nullptr, a.alpha, (char*)dweight + (int64_t)start * d->features * es, p.sums_pitch, a.features, d->type, job.rows, 0, 0, 0, classes, p.dw_splits};
+        rc = launch(k_ce_dx, (unsigned)(up((int64_t)classes * ((d->features + UNIT - 1) / UNIT), CE_CHUNK) / CE_CHUNK), CE_THREADS, st, false, x1);
+      }
     }
   }
   if (dx && d->rows && rc == SAE_OK) {
-    DxArgs x2 = {(const float*)(ws + p.dx_sums), a.counted, a.index, a.alpha, dx, p.sums_pitch, a.features, d->type, 128 * p.dx.cg, dx_across, clusters, p.dx_room};
+    DxArgs x2 = {(const float*)(ws + p.dx_sums), a.counted, a.index, a.alpha, dx, p.sums_pitch, a.features, d->type, 128 * p.dx.cg, dx_across, clusters, p.dx_room, 0, 0};
     rc = launch(k_ce_dx, up(d->rows * ((d->features + UNIT - 1) / UNIT), CE_CHUNK) / CE_CHUNK, CE_THREADS, st, false, x2);
   }
   return rc;

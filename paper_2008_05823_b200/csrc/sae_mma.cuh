@@ -33,6 +33,7 @@
 #include <type_traits>
 
 #include "sae_device.cuh"
+#include "sae_vec.cuh"
 
 namespace sae {
 namespace mma {
@@ -46,7 +47,8 @@ constexpr int MAX_STAGES = 6;
 // 8 warps take the sums out (16 were no faster).  A job that brings values in by copies has STAGING bytes for each of them, at the cost of stages.
 template <class Job>
 struct Room {
-  static constexpr int STAGES = Job::STAGING ? 4 : MAX_STAGES;
+  static constexpr int STAGES = (int)((227 * 1024 - 1024 - sizeof(typename Job::Shared) - 512 - EPI_WARPS * Job::STAGING) / STAGE_BYTES) < MAX_STAGES
+                                    ? (int)((227 * 1024 - 1024 - sizeof(typename Job::Shared) - 512 - EPI_WARPS * Job::STAGING) / STAGE_BYTES) : MAX_STAGES;
   static constexpr int THREADS = 32 * (EPI_WARP + EPI_WARPS + Job::REPORTS);
   static constexpr u32 BYTES = STAGES * STAGE_BYTES + EPI_WARPS * Job::STAGING + 1024;
 };
@@ -540,6 +542,24 @@ __device__ __forceinline__ void store_row(T* to, const float (&v)[32], int n) {
       }
   }
 }
+
+// A warp's 32 x 32 values to a matrix whose rows start anywhere: through shared memory (`at`, 32 rows of 33 words), so that a store
+// covers a row's neighbouring columns.  rows, cols: how many of each there are.
+template <typename T>
+__device__ __forceinline__ void store_square(T* to, int64_t pitch, const float (&v)[32], int rows, int cols, u32 at) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + (u32)(lane * 33 + i) * 4), "f"(v[i]) : "memory");
+  __syncwarp();
+#pragma unroll 8
+  for (int r = 0; r < rows; ++r) {
+    float x;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(at + (u32)(r * 33 + lane) * 4) : "memory");
+    if (lane < cols) to[r * pitch + lane] = from_f<T>(x);
+  }
+  __syncwarp();
+}
+constexpr int SQUARE_BYTES = 32 * 33 * 4;
 
 // ---- host -------------------------------------------------------------------------------------------------------------------
 // A map of `planes` matrices of `rows` rows of `inner` 16-bit elements; pitches in elements, multiples of 8.
