@@ -742,8 +742,8 @@ int device_sms() {
 
 // Float tensors take float arithmetic up to so many rows and products (rows * classes * features).  Loss and gradients, us, there and in
 // bfloat16 parts: 32 x 2048 x 1000 69 and 202, 128 x 2048 x 1000 125 and 199, 256 x 2048 x 1000 197 and 215, 512 x 2048 x 1000 362 and
-// 241, 8 x 768 x 30522 353 and 361, 128 x 768 x 30522 936 and 437.
-constexpr int64_t CE_FLOAT_ROWS = 256, CE_FLOAT_WORK = 1ll << 29;
+// 241 (they meet near 300 rows), 8 x 768 x 30522 353 and 361, 128 x 768 x 30522 936 and 437.
+constexpr int64_t CE_FLOAT_ROWS = 320, CE_FLOAT_WORK = 1ll << 29;
 bool in_float(const sae_linear_ce_desc* d) {
   return d->type == SAE_TYPE_FLOAT && d->rows <= CE_FLOAT_ROWS && d->classes <= (1 << 20) && d->rows * d->classes <= CE_FLOAT_WORK / d->features;
 }
