@@ -19,7 +19,7 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC", "-shared"]
 
 TARGETS = {
-    "libsae.so": (["sae.cu", "sae_noalloc.cu", "sae_grads.cu", "sae_group_norm.cu", "sae_linear_ce.cu", "sae_ortho.cu"], ["sae_vec.cuh", "sae_mma.cuh", "sae_gn_common.cuh", "sae_gn_unit.cuh", "sae_gn_stream.cuh", "sae_kernels.cuh", "sae_worker_tma.cuh", "sae_worker_fused.cuh", "sae_worker_small.cuh", "sae_topk.cuh", "sae_shard_topk.cuh", "sae_device.cuh", os.path.join(INCLUDE, "sae.h")]),
+    "libsae.so": (["sae.cu", "sae_noalloc.cu", "sae_grads.cu", "sae_group_norm.cu", "sae_linear_ce.cu", "sae_ortho.cu"], ["sae_vec.cuh", "sae_mma.cuh", "sae_ce_float.cuh", "sae_ortho_small.cuh", "sae_gn_common.cuh", "sae_gn_unit.cuh", "sae_gn_stream.cuh", "sae_kernels.cuh", "sae_worker_tma.cuh", "sae_worker_fused.cuh", "sae_worker_small.cuh", "sae_topk.cuh", "sae_shard_topk.cuh", "sae_device.cuh", os.path.join(INCLUDE, "sae.h")]),
     "libsae_synth.so": (["synth_gen.cu"], []),
     "_host.so": (["host_torch.cpp"], [os.path.join(INCLUDE, "sae.h")]),
 }

@@ -371,6 +371,12 @@ struct OrthoJob {
   };
 };
 
+}  // namespace
+
+#include "sae_ortho_small.cuh"
+
+namespace {
+
 thread_local int g_ortho_cuda_error = 0;
 
 struct DeviceGuard {
@@ -414,9 +420,10 @@ struct sae_ortho {
   std::vector<int64_t> rows, cols;
   std::vector<int> in_types, out_types;
   std::vector<float> coef;
-  std::vector<double> s_scale, b_scale;          // of every step
+  std::vector<double> s_scale, b_scale, ones;    // of every step
   double x_scale;
   std::vector<Class> classes;
+  int small_n[2], small_first[2];                // matrices that one SM holds, of up to 64 and up to 128 rows, and where they begin in `order`
   char* arena;
   Maps* maps;
   Shape* shapes;
@@ -521,6 +528,14 @@ void list_products(Class& c, const std::vector<Shape>& shapes, const std::vector
   c.total = (int)at;
 }
 
+void factors(const sae_ortho* h, const std::vector<double>& b_scale, Factors* f) {
+  for (int i = 0; i < h->steps; ++i) {
+    const float* k = h->coef.data() + 3 * i;
+    const double sx = h->x_scale, ss = h->s_scale[i], sb = b_scale[i], to = i + 1 == h->steps ? 1.0 / sx : 1.0;
+    f[i] = {(float)(ss / (sx * sx)), (float)(k[0] * sb), (float)(k[1] * sb / ss), (float)(k[2] * sb / (ss * ss)), (float)(k[0] * to), (float)(to / sb)};
+  }
+}
+
 template <typename... P, typename... A>
 cudaError_t launch(void (*kernel)(P...), int blocks, cudaStream_t st, bool first, A... args) {
   cudaLaunchConfig_t cfg = {};
@@ -587,7 +602,7 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
       h->rows.assign(cfg->rows, cfg->rows + T);
       h->cols.assign(cfg->cols, cfg->cols + T);
       h->coef.assign(cfg->coefficients, cfg->coefficients + 3 * cfg->steps);
-      h->s_scale = s_scale; h->b_scale = b_scale;
+      h->s_scale = s_scale; h->b_scale = b_scale; h->ones.assign((size_t)cfg->steps, 1.0);
       for (int j = 0; j < T; ++j) {
         h->in_types.push_back(cfg->types ? cfg->types[j] : SAE_TYPE_FLOAT);
         h->out_types.push_back(cfg->result_types ? cfg->result_types[j] : h->in_types[j]);
@@ -596,7 +611,7 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
       std::map<std::tuple<int, int64_t, int64_t, int64_t, bool>, std::vector<int>> by;
       for (int k = 0; k < K; ++k)
         for (int j = 0; j < T; ++j)
-          if (h->rows[j] && h->cols[j]) {
+          if (h->rows[j] && h->cols[j] && !small_rows(std::min(h->rows[j], h->cols[j]), std::max(h->rows[j], h->cols[j]))) {
             // bfloat16 results of a few rows or columns take both parts too: such products are short, and their roundings average out less
             const bool one = h->out_types[j] == SAE_TYPE_BFLOAT && std::min(h->rows[j], h->cols[j]) > 128;
             by[{one ? 1 : 2, -std::max(h->rows[j], h->cols[j]), h->rows[j], h->cols[j], one && h->in_types[j] != SAE_TYPE_FLOAT}].push_back(k * T + j);
@@ -619,6 +634,23 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
         ++h->classes.back().n;
         shapes.push_back(g);
         bytes += 2 * up(2 * g.x_plane * count.back() * 2, 1024) + 2 * up(g.s_parts * g.s_plane * count.back() * 2, 1024);
+      }
+      for (int f = 0; f < 2; ++f) {
+        h->small_first[f] = (int)order.size();
+        // the longest first
+        std::vector<std::pair<int64_t, int>> found;
+        for (int k = 0; k < K; ++k)
+          for (int j = 0; j < T; ++j)
+            if (h->rows[j] && h->cols[j] && small_rows(std::min(h->rows[j], h->cols[j]), std::max(h->rows[j], h->cols[j])) == (f ? 128 : 64))
+              found.push_back({-std::max(h->rows[j], h->cols[j]), k * T + j});
+        std::sort(found.begin(), found.end());
+        for (const auto& q : found) {
+          const int j = q.second % T;
+          Place& p = places[q.second];
+          p.rows = (int)h->rows[j]; p.cols = (int)h->cols[j]; p.in_type = h->in_types[j]; p.out_type = h->out_types[j];
+          order.push_back(q.second);
+        }
+        h->small_n[f] = (int)found.size();
       }
       if (bytes) e = cudaMalloc((void**)&h->arena, (size_t)bytes);
       if (e == cudaSuccess) {
@@ -690,7 +722,7 @@ int sae_ortho_run(sae_ortho* h, const void* const* matrices, const int64_t* pitc
         (pitches && h->rows[j] > 1 && pitches[i] < h->cols[j]) || (result_pitches && h->rows[j] > 1 && result_pitches[i] < h->cols[j]))
       return SAE_ERR_INVALID_ARG;
   }
-  if (!h->chunks) return SAE_OK;
+  if (!h->chunks && !h->small_n[0] && !h->small_n[1]) return SAE_OK;
   DeviceGuard guard(h->device);
   if (!guard.ok) return cuda_status(h, cudaGetLastError());
   cudaError_t e = cudaSuccess;
@@ -705,8 +737,17 @@ int sae_ortho_run(sae_ortho* h, const void* const* matrices, const int64_t* pitc
     e = launch(k_ortho_table, 1, h->stream, true, table, h->mats + i);
     first = false;
   }
-  if (e == cudaSuccess) e = launch(k_ortho_norm, h->chunks, h->stream, first, (const Matrix*)h->mats, (const Place*)h->places, (const Chunk*)h->chunk_list, h->sums);
-  if (e == cudaSuccess) e = launch(k_ortho_split, h->chunks, h->stream, false, (const Matrix*)h->mats, (const Place*)h->places, (const Chunk*)h->chunk_list, (const double*)h->sums, h->eps, h->x_scale);
+  static thread_local SmallJob one;
+  one.mats = h->mats; one.places = h->places; one.steps = h->steps; one.eps = h->eps; one.scale = h->x_scale;
+  factors(h, h->b_scale, one.factors);
+  for (int f = 0; f < 2 && e == cudaSuccess; ++f) {
+    one.order = h->order + h->small_first[f];
+    if (h->small_n[f]) e = f ? launch_small<128>(one, h->small_n[f], h->stream) : launch_small<64>(one, h->small_n[f], h->stream);
+  }
+  if (h->chunks && e == cudaSuccess)
+    e = launch(k_ortho_norm, h->chunks, h->stream, first, (const Matrix*)h->mats, (const Place*)h->places, (const Chunk*)h->chunk_list, h->sums);
+  if (h->chunks && e == cudaSuccess)
+    e = launch(k_ortho_split, h->chunks, h->stream, false, (const Matrix*)h->mats, (const Place*)h->places, (const Chunk*)h->chunk_list, (const double*)h->sums, h->eps, h->x_scale);
   for (const Class& c : h->classes) {
     static thread_local OrthoJob job;
     job = {};
@@ -723,12 +764,8 @@ int sae_ortho_run(sae_ortho* h, const void* const* matrices, const int64_t* pitc
     job.mats = h->mats;
     job.places = h->places;
     job.order = h->order;
-    for (int i = 0; i < h->steps; ++i) {
-      const float* k = h->coef.data() + 3 * i;
-      const double sx = h->x_scale, ss = h->s_scale[i], sb = c.parts == 2 ? h->b_scale[i] : 1.0,      // (one part: B hi is added to x hi times 1)
-                   to = i + 1 == h->steps ? 1.0 / sx : 1.0;
-      job.factors[i] = {(float)(ss / (sx * sx)), (float)(k[0] * sb), (float)(k[1] * sb / ss), (float)(k[2] * sb / (ss * ss)), (float)(k[0] * to), (float)(to / sb)};
-    }
+    // (one part: B hi is added to x hi times 1)
+    factors(h, c.parts == 2 ? h->b_scale : h->ones, job.factors);
     if (e == cudaSuccess) e = mma::launch_products(job, c.cg, std::min(c.total, h->num_sms / c.cg), h->stream, true);
   }
   return e == cudaSuccess ? SAE_OK : cuda_status(h, e);
