@@ -234,9 +234,9 @@ __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.
 
 // ---- descriptors --------------------------------------------------------------------------------------------------------
 // 128-byte swizzled rows.  K first: 8 rows of 128 bytes (64 k) are one kilobyte, groups of 8 rows follow one another.  Rows
-// first: 64 rows of the matrix are the 128 bytes, 8 k are one kilobyte, and the next 64 rows are the next box.
-__device__ __forceinline__ u64 smem_desc(u32 addr, bool rows_first) {
-  const u64 lead = rows_first ? BOX_BYTES >> 4 : 1, stride = 1024 >> 4;
+// first: 64 rows of the matrix are the 128 bytes, 8 k are one kilobyte, and the next 64 rows are `next` bytes on.
+__device__ __forceinline__ u64 smem_desc(u32 addr, bool rows_first, u32 next = BOX_BYTES) {
+  const u64 lead = rows_first ? next >> 4 : 1, stride = 1024 >> 4;
   return (u64)((addr >> 4) & 0x3fff) | lead << 16 | stride << 32 | 1ull << 46 | 2ull << 61;
 }
 constexpr u32 FLOAT_SUMS = 1u << 4, BFLOAT_OPERANDS = 1u << 7 | 1u << 10;

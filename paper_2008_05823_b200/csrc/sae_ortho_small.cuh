@@ -3,7 +3,8 @@
 // With x as `small` rows of `big` columns (a matrix taller than wide is read and written transposed), x and S lie in shared memory as two
 // float16 parts in blocks of 64 columns, R = 64 or 128 swizzled rows of 128 bytes each.  Such a block is an operand
 // either way: its rows the matrix's rows and 64 k (S = x x'), or its rows k and 64 columns (x = B x), so nothing is laid out anew.
-// S becomes B in its place, x is replaced block by block.  Sums over more than two blocks are joined in float, rounded to nearest.
+// S becomes B in its place, x is replaced block by block.  S and B are added up in as many sums as tensor memory has room for, joined in
+// float: each product of 16 k cuts off what a sum has below its last bit.
 // 64 rows go through products of 128 rows, whose second half is not looked at.
 // What bounds it is the chain of 3 products and 3 epilogues a step (about 8 us); tiles of a matrix spread over SMs wait for one another through
 // memory instead, 7 us a product: 64 x 576 took 130 us that way.
@@ -53,10 +54,22 @@ __device__ __forceinline__ void small_put(const float (&v)[32], u32 hi, u32 lo, 
   }
 }
 
+// The sum of `n` sums, R columns apart.
+template <int R>
+__device__ __forceinline__ void joined(float (&v)[32], u32 at, int n) {
+  mma::tmem_load(at, v);
+  for (int g = 1; g < n; ++g) {
+    float w[32];
+    mma::tmem_load(at + (u32)(g * R), w);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] += w[i];
+  }
+}
+
 template <int R>
 __global__ void __launch_bounds__(OS_THREADS, 1) k_ortho_small(const __grid_constant__ SmallJob job) {
   constexpr u32 BLOCK = R * 128;                         // bytes
-  constexpr int GROUP = 2;                               // blocks of a sum
+  constexpr int SUMS = 512 / R;                          // S is added up in so many sums, which are joined in float
   extern __shared__ unsigned char raw[];
   __shared__ u64 bar;
   __shared__ u32 tmem_at, dead;
@@ -141,7 +154,7 @@ __global__ void __launch_bounds__(OS_THREADS, 1) k_ortho_small(const __grid_cons
     ++phase;
     mma::fence_after();
   };
-  const u32 square = mma::instruction(128, R, false, false, false), wide = mma::instruction(128, 64, false, false, true);
+  const u32 square = mma::instruction(128, R, false, false, false);
   constexpr int seg[3][2] = {{0, 1}, {1, 0}, {0, 0}};
   const int quarter = warp & 3, half = warp >> 2, r = quarter * 32 + lane;
   const bool mine = quarter * 32 < R;                    // this warp's rows are looked at
@@ -151,40 +164,30 @@ __global__ void __launch_bounds__(OS_THREADS, 1) k_ortho_small(const __grid_cons
   for (int step = 0; step < job.steps; ++step) {
     const Factors f = job.factors[step];
     products([&] {
-      for (int b0 = 0; b0 < blocks; b0 += GROUP) {
-        u32 add = 0;
-        for (int q = 0; q < 3; ++q)
-          for (int b = b0; b < min(b0 + GROUP, blocks); ++b) {
-            const u64 a = mma::smem_desc(x[seg[q][0]] + (u32)b * BLOCK, false), c = mma::smem_desc(x[seg[q][1]] + (u32)b * BLOCK, false);
+      for (int q = 0; q < 3; ++q)
+        for (int b = 0; b < blocks; ++b) {
+          const u64 a = mma::smem_desc(x[seg[q][0]] + (u32)b * BLOCK, false), c = mma::smem_desc(x[seg[q][1]] + (u32)b * BLOCK, false);
 #pragma unroll
-            for (u32 k = 0; k < 4; ++k) { mma::product<1>(tmem + (u32)(b0 / GROUP) * R, a + 2 * k, c + 2 * k, square, add); add = 1; }
-          }
-      }
+          for (u32 k = 0; k < 4; ++k) mma::product<1>(tmem + (u32)(b * 4 + k) % SUMS * R, a + 2 * k, c + 2 * k, square, q || b * 4 + (int)k >= SUMS);
+        }
     });
     float own[CHUNKS][32];
     if (mine) {
 #pragma unroll
       for (int k = 0; k < CHUNKS; ++k) {
         const int col = half * (R / 2) + k * 32;
-        mma::tmem_load(lanes + (u32)col, own[k]);
-        for (int g = 1; g < (blocks + GROUP - 1) / GROUP; ++g) {
-          float v[32];
-          mma::tmem_load(lanes + (u32)(g * R + col), v);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) own[k][i] += v[i];
-        }
+        joined<R>(own[k], lanes + (u32)col, min(4 * blocks, SUMS));
 #pragma unroll
         for (int i = 0; i < 32; ++i) own[k][i] *= f.s_sum;
         small_put<R>(own[k], s[0], s[1], r, col);
       }
     }
     products([&] {
-      u32 add = 0;
       for (int q = 0; q < 3; ++q)
         for (int b = 0; b < R / 64; ++b) {
           const u64 a = mma::smem_desc(s[seg[q][0]] + (u32)b * BLOCK, false), c = mma::smem_desc(s[seg[q][1]] + (u32)b * BLOCK, false);
 #pragma unroll
-          for (u32 k = 0; k < 4; ++k) { mma::product<1>(tmem, a + 2 * k, c + 2 * k, square, add); add = 1; }
+          for (u32 k = 0; k < 4; ++k) mma::product<1>(tmem + k * R, a + 2 * k, c + 2 * k, square, q || b);
         }
     });
     if (mine) {
@@ -192,7 +195,7 @@ __global__ void __launch_bounds__(OS_THREADS, 1) k_ortho_small(const __grid_cons
       for (int k = 0; k < CHUNKS; ++k) {
         const int col = half * (R / 2) + k * 32;
         float v[32];
-        mma::tmem_load(lanes + (u32)col, v);
+        joined<R>(v, lanes + (u32)col, 4);
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
           v[i] = __fmaf_rn(f.b_own, own[k][i], f.b_sum * v[i]);
@@ -204,10 +207,11 @@ __global__ void __launch_bounds__(OS_THREADS, 1) k_ortho_small(const __grid_cons
     for (int b0 = 0; b0 < blocks; b0 += 8) {
       const int b1 = min(b0 + 8, blocks);
       products([&] {
-        for (int b = b0; b < b1; ++b) {
+        for (int b = b0; b < b1; b += 4) {               // four blocks, 256 columns, at a time
+          const u32 wide = mma::instruction(128, 64 * min(4, b1 - b), false, false, true);
           u32 add = 0;
           for (int q = 0; q < 3; ++q) {
-            const u64 c = mma::smem_desc(x[seg[q][1]] + (u32)b * BLOCK, true);
+            const u64 c = mma::smem_desc(x[seg[q][1]] + (u32)b * BLOCK, true, BLOCK);
 #pragma unroll
             for (u32 k = 0; k < R / 16; ++k) {
               const u64 a = mma::smem_desc(s[seg[q][0]] + k / 4 * BLOCK, false) + 2 * (k % 4);
