@@ -531,15 +531,17 @@ struct GradJob : mma::Plain {
   };
 };
 
-// How often the classes of a piece are split for dx, where there are too few tiles for the clusters.
-__device__ __host__ inline int dx_splits(int blocks, int tiles_across, int clusters, int room) {
+// How often the classes of a piece are split for dx, where there are too few tiles for the clusters.  Time in units of a tile's k; a tile's own
+// sums, read and written in float, are about 500 of them (2458 x 768 and 6144 classes: 2 splits 25 us, 7 splits, which fill three waves
+// to 95 %, 44 us).
+__device__ __host__ inline float dx_time(int blocks, int tiles_across, int clusters, int depth, int s) {
+  const long long t = (long long)blocks * tiles_across * s;
+  return (float)((t + clusters - 1) / clusters) * ((float)depth / (float)s + 500.0f);
+}
+__device__ __host__ inline int dx_splits(int blocks, int tiles_across, int clusters, int depth, int room) {
   int best = 1;
-  float least = 0;
-  for (int s = 1; s <= 8 && s <= room; ++s) {
-    const long long t = (long long)blocks * tiles_across * s;
-    const float cost = (float)((t + clusters - 1) / clusters) / (float)s * (1.0f + 0.03f * (float)s);
-    if (s == 1 || cost < least) { least = cost; best = s; }
-  }
+  for (int s = 2; s <= 8 && s <= room; ++s)
+    if (dx_time(blocks, tiles_across, clusters, depth, s) < dx_time(blocks, tiles_across, clusters, depth, best)) best = s;
   return best;
 }
 
@@ -556,6 +558,7 @@ struct ProductJob : mma::Plain {
   bool dx;
   // dx
   float* sums;                    // dweight: those of its splits, where it has more than one
+  int depth;                      // classes of a whole piece
   int sums_pitch, room, add;      // room: row blocks that the sums have place for
   int dw_splits;
   // dweight
@@ -568,7 +571,7 @@ struct ProductJob : mma::Plain {
   __device__ __forceinline__ Local begin(const Shared&, int cluster, int clusters) const {
     Local l = {cluster, clusters, 0, 1, *counted};
     l.blocks = ((dx ? l.count : classes) + rows - 1) / rows;
-    l.splits = dx ? dx_splits(l.blocks, across, clusters, l.blocks ? room / l.blocks : 1) : dw_splits;
+    l.splits = dx ? dx_splits(l.blocks, across, clusters, depth, l.blocks ? room / l.blocks : 1) : dw_splits;
     return l;
   }
   __device__ __forceinline__ bool tile(Local& l, int i, mma::Tile& t) const {
@@ -653,7 +656,7 @@ struct DxArgs {
   const int *counted, *index;
   const float* alpha;
   void* dx;
-  int sums_pitch, features, type, rows, across, clusters, room;
+  int sums_pitch, features, type, rows, across, clusters, depth, room;
   int dw_rows, dw_splits;           // dweight: its rows and splits (0: this is dx)
 };
 template <typename T>
@@ -677,7 +680,7 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_dx(const __grid_constant__ Dx
   mma::wait_for_previous();
   const int count = a.dw_splits ? a.dw_rows : *a.counted, blocks = (count + a.rows - 1) / a.rows;
   if (!blocks) return;
-  const int splits = a.dw_splits ? a.dw_splits : dx_splits(blocks, a.across, a.clusters, a.room / blocks);
+  const int splits = a.dw_splits ? a.dw_splits : dx_splits(blocks, a.across, a.clusters, a.depth, a.room / blocks);
   const int64_t plane = (int64_t)blocks * a.rows * a.sums_pitch;
   const float alpha = *a.alpha;
   const unsigned wide = (unsigned)(a.features + UNIT - 1) / UNIT;
@@ -796,13 +799,10 @@ int piece_blocks(const sae_linear_ce_desc* d, int64_t rows, int parts, int sms) 
   int64_t best = most;
   double least = 0;
   for (int64_t b = most; b >= std::max<int64_t>(1, most / 4); --b) {
-    double dx = 0;
-    for (int s = 1; s <= 8; ++s) {
-      const double t = waves(down * across * s) / s * (1.0 + 0.03 * s);
-      if (s == 1 || t < dx) dx = t;
-    }
+    const int s = dx_splits((int)down, (int)across, (int)units, (int)(256 * b), 8);
+    const double dx = dx_time((int)down, (int)across, (int)units, (int)(256 * b), s);
     const double pieces = (double)((all + b - 1) / b);
-    const double t = pieces * (parts * (waves(down * b) * (double)d->features + waves(b * across) * (double)d->rows + dx * 256.0 * (double)b) + 2500.0);
+    const double t = pieces * (parts * (waves(down * b) * (double)d->features + waves(b * across) * (double)d->rows + dx) + 2500.0);
     if (least == 0 || t < 0.99 * least) { least = t; best = b; }
   }
   return (int)best;
@@ -1120,7 +1120,7 @@ int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, cons
                   (void*)((char*)dbias + (int64_t)start * bs));
     if (dx && d->rows && rc == SAE_OK) {
       job.dx = true; job.b = g.w; job.cols = p.dx.cols; job.rows = 128 * p.dx.cg; job.across = dx_across;
-      job.sums = (float*)(ws + p.dx_sums); job.sums_pitch = p.sums_pitch; job.room = p.dx_room; job.add = i > 0;
+      job.sums = (float*)(ws + p.dx_sums); job.sums_pitch = p.sums_pitch; job.room = p.dx_room; job.depth = p.piece; job.add = i > 0;
       rc = products(job, p.dx, clusters, sms, st);
     }
     if (dweight && rc == SAE_OK) {
@@ -1130,13 +1130,13 @@ int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, cons
       job.whole_rows = aligned_to(dweight, 32) && d->features * es % 32 == 0;
       rc = products(job, p.dw, up(classes, job.rows) / job.rows * job.across * p.dw_splits, sms, st);
       if (rc == SAE_OK && p.dw_splits > 1) {
-        DxArgs x1 = {job.sums, a.counted, nullptr, a.alpha, (char*)dweight + (int64_t)start * d->features * es, p.sums_pitch, a.features, d->type, job.rows, 0, 0, 0, classes, p.dw_splits};
+        DxArgs x1 = {job.sums, a.counted, nullptr, a.alpha, (char*)dweight + (int64_t)start * d->features * es, p.sums_pitch, a.features, d->type, job.rows, 0, 0, 0, 0, classes, p.dw_splits};
         rc = launch(k_ce_dx, (unsigned)(up((int64_t)classes * ((d->features + UNIT - 1) / UNIT), CE_CHUNK) / CE_CHUNK), CE_THREADS, st, false, x1);
       }
     }
   }
   if (dx && d->rows && rc == SAE_OK) {
-    DxArgs x2 = {(const float*)(ws + p.dx_sums), a.counted, a.index, a.alpha, dx, p.sums_pitch, a.features, d->type, 128 * p.dx.cg, dx_across, clusters, p.dx_room, 0, 0};
+    DxArgs x2 = {(const float*)(ws + p.dx_sums), a.counted, a.index, a.alpha, dx, p.sums_pitch, a.features, d->type, 128 * p.dx.cg, dx_across, clusters, p.piece, p.dx_room, 0, 0};
     rc = launch(k_ce_dx, up(d->rows * ((d->features + UNIT - 1) / UNIT), CE_CHUNK) / CE_CHUNK, CE_THREADS, st, false, x2);
   }
   return rc;
