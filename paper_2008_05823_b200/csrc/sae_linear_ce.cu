@@ -684,24 +684,22 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_dx(const __grid_constant__ Dx
   const int64_t plane = (int64_t)blocks * a.rows * a.sums_pitch;
   const float alpha = *a.alpha;
   const unsigned wide = (unsigned)(a.features + UNIT - 1) / UNIT;
-  for (int i = threadIdx.x; i < CE_CHUNK; i += CE_THREADS) {
-    const int64_t u = (int64_t)blockIdx.x * CE_CHUNK + i, r = u / wide;
-    const int c = (int)(u - r * wide) * UNIT;
-    if (r >= count) break;
-    float v[UNIT] = {};
-    const float* from = a.sums + r * a.sums_pitch + c;
-    for (int s = 0; s < splits; ++s, from += plane) {
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(from)), y = __ldcg(reinterpret_cast<const float4*>(from) + 1);
-      v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
-    }
-#pragma unroll
-    for (int k = 0; k < UNIT; ++k) v[k] *= alpha;
-    const int n = min(UNIT, a.features - c);
-    const int64_t to = (a.dw_splits ? r : (int64_t)a.index[r]) * a.features + c;
-    if (a.type == SAE_TYPE_FLOAT) put_row((float*)a.dx + to, v, n);
-    else if (a.type == SAE_TYPE_BFLOAT) put_row((__nv_bfloat16*)a.dx + to, v, n);
-    else put_row((__half*)a.dx + to, v, n);
+  const int64_t u = (int64_t)blockIdx.x * CE_THREADS + threadIdx.x, r = u / wide;
+  const int c = (int)(u - r * wide) * UNIT;
+  if (r >= count) return;
+  float v[UNIT] = {};
+  const float* from = a.sums + r * a.sums_pitch + c;
+  for (int s = 0; s < splits; ++s, from += plane) {
+    const float4 x = __ldcg(reinterpret_cast<const float4*>(from)), y = __ldcg(reinterpret_cast<const float4*>(from) + 1);
+    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
   }
+#pragma unroll
+  for (int k = 0; k < UNIT; ++k) v[k] *= alpha;
+  const int n = min(UNIT, a.features - c);
+  const int64_t to = (a.dw_splits ? r : (int64_t)a.index[r]) * a.features + c;
+  if (a.type == SAE_TYPE_FLOAT) put_row((float*)a.dx + to, v, n);
+  else if (a.type == SAE_TYPE_BFLOAT) put_row((__nv_bfloat16*)a.dx + to, v, n);
+  else put_row((__half*)a.dx + to, v, n);
 }
 
 // dbias of a piece: the sums of every 32 rows, added in order (double).
@@ -1131,13 +1129,13 @@ int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, cons
       rc = products(job, p.dw, up(classes, job.rows) / job.rows * job.across * p.dw_splits, sms, st);
       if (rc == SAE_OK && p.dw_splits > 1) {
         DxArgs x1 = {job.sums, a.counted, nullptr, a.alpha, (char*)dweight + (int64_t)start * d->features * es, p.sums_pitch, a.features, d->type, job.rows, 0, 0, 0, 0, classes, p.dw_splits};
-        rc = launch(k_ce_dx, (unsigned)(up((int64_t)classes * ((d->features + UNIT - 1) / UNIT), CE_CHUNK) / CE_CHUNK), CE_THREADS, st, false, x1);
+        rc = launch(k_ce_dx, (unsigned)(up((int64_t)classes * ((d->features + UNIT - 1) / UNIT), CE_THREADS) / CE_THREADS), CE_THREADS, st, false, x1);
       }
     }
   }
   if (dx && d->rows && rc == SAE_OK) {
     DxArgs x2 = {(const float*)(ws + p.dx_sums), a.counted, a.index, a.alpha, dx, p.sums_pitch, a.features, d->type, 128 * p.dx.cg, dx_across, clusters, p.piece, p.dx_room, 0, 0};
-    rc = launch(k_ce_dx, up(d->rows * ((d->features + UNIT - 1) / UNIT), CE_CHUNK) / CE_CHUNK, CE_THREADS, st, false, x2);
+    rc = launch(k_ce_dx, (unsigned)(up(d->rows * ((d->features + UNIT - 1) / UNIT), CE_THREADS) / CE_THREADS), CE_THREADS, st, false, x2);
   }
   return rc;
 }

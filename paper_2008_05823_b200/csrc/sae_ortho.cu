@@ -559,7 +559,7 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
   *out = nullptr;
   if (cfg->abi_version != SAE_ABI_VERSION) return SAE_ERR_ABI;
   const int K = cfg->num_rows, T = cfg->num_matrices;
-  if (K < 1 || K > 1024 || T < 1 || !cfg->rows || !cfg->cols || !cfg->coefficients || cfg->device < 0 || cfg->steps < 1 || cfg->steps > 64 ||
+  if (K < 1 || K > 1024 || T < 1 || !cfg->rows || !cfg->cols || !cfg->coefficients || cfg->device < 0 || cfg->steps < 1 || cfg->steps > OT_STEPS ||
       !(cfg->eps >= 0.0f) || !std::isfinite(cfg->eps) || (long long)K * T > (1 << 20)) return SAE_ERR_INVALID_ARG;
   for (int j = 0; j < T; ++j) {
     const int it = cfg->types ? cfg->types[j] : SAE_TYPE_FLOAT, ot = cfg->result_types ? cfg->result_types[j] : it;
@@ -567,8 +567,7 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
         !type_ok(it) || !type_ok(ot)) return SAE_ERR_INVALID_ARG;
   }
   // Where the singular values can get to decides how far x, S and B may be scaled up in float16.
-  std::vector<double> s_scale, b_scale;
-  double top = 1.0, widest = 1.0;
+  double s_scale[OT_STEPS], b_scale[OT_STEPS], top = 1.0, widest = 1.0;
   for (int i = 0; i < cfg->steps; ++i) {
     const float* k = cfg->coefficients + 3 * i;
     if (!std::isfinite(k[0]) || !std::isfinite(k[1]) || !std::isfinite(k[2])) return SAE_ERR_INVALID_ARG;
@@ -576,8 +575,8 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
     const double t = top * 1.01;                 // roundings
     bounds(k, t, p, q);
     if (!(p <= 16.0) || !(q <= 4096.0)) return SAE_ERR_INVALID_ARG;
-    s_scale.push_back(std::exp2(std::floor(std::log2(32768.0 / (t * t)))));
-    b_scale.push_back(std::exp2(std::min(14.0, std::floor(std::log2(32768.0 / std::max(q, 1e-6))))));
+    s_scale[i] = std::exp2(std::floor(std::log2(32768.0 / (t * t))));
+    b_scale[i] = std::exp2(std::min(14.0, std::floor(std::log2(32768.0 / std::max(q, 1e-6)))));
     top = std::max(p, 1e-3);
     widest = std::max(widest, top * 1.01);
   }
@@ -602,7 +601,7 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
       h->rows.assign(cfg->rows, cfg->rows + T);
       h->cols.assign(cfg->cols, cfg->cols + T);
       h->coef.assign(cfg->coefficients, cfg->coefficients + 3 * cfg->steps);
-      h->s_scale = s_scale; h->b_scale = b_scale; h->ones.assign((size_t)cfg->steps, 1.0);
+      h->s_scale.assign(s_scale, s_scale + cfg->steps); h->b_scale.assign(b_scale, b_scale + cfg->steps); h->ones.assign((size_t)cfg->steps, 1.0);
       for (int j = 0; j < T; ++j) {
         h->in_types.push_back(cfg->types ? cfg->types[j] : SAE_TYPE_FLOAT);
         h->out_types.push_back(cfg->result_types ? cfg->result_types[j] : h->in_types[j]);
