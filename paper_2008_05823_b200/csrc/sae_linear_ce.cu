@@ -758,15 +758,19 @@ int float_splits(int64_t tiles, int64_t depth, int most, int sms) {
 
 struct TileShape { int cg, cols; };
 
-// Time in units of a block's k loop: waves of tiles over the SMs (or pairs) times what a tile costs.
-TileShape tile_shape(int64_t rows, int64_t cols, int parts, int sms) {
-  const struct { TileShape s; double cost; } shapes[3] = {{{2, parts == 1 ? 256 : 128}, parts == 1 ? 2.0 : 1.2}, {{1, 128}, 1.3}, {{1, 64}, 1.0}};
+// The tile shape of a product of `depth` k: waves of tiles over the SMs (or pairs) times what a tile costs for each k.  A block of 64 k takes a pair
+// 588 cycles for 256 x 256, one SM 630 for 128 x 128 (shared memory: the tensor cores read and TMA writes 64 KB in it) and about 500
+// for 128 x 64.  splits: where sums may be added up in several parts of k, at 500 k for each, the best number of them counts.
+TileShape tile_shape(int64_t rows, int64_t cols, int64_t depth, int splits, int parts, int sms) {
+  const struct { TileShape s; double cost; } shapes[3] = {{{2, parts == 1 ? 256 : 128}, parts == 1 ? 2.0 : 1.6}, {{1, 128}, 2.1}, {{1, 64}, 1.7}};
   TileShape best = shapes[0].s;
   double least = 0;
   for (const auto& c : shapes) {
-    const double tiles = (double)((rows + 128 * c.s.cg - 1) / (128 * c.s.cg)) * (double)((cols + c.s.cols - 1) / c.s.cols);
-    const double t = c.cost * std::max(1.0, tiles / (sms / c.s.cg));
-    if (least == 0 || t < least) { least = t; best = c.s; }
+    const int64_t tiles = (rows + 128 * c.s.cg - 1) / (128 * c.s.cg) * ((cols + c.s.cols - 1) / c.s.cols), units = sms / c.s.cg;
+    for (int s = 1; s <= splits; ++s) {
+      const double t = c.cost * (double)((tiles * s + units - 1) / units) * ((double)depth / s + (splits > 1 ? 500.0 : 0.0));
+      if (least == 0 || t < least) { least = t; best = c.s; }
+    }
   }
   return best;
 }
@@ -849,7 +853,7 @@ CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward,
   p.at = take(p.rows * 4);
   p.counted = take(8);
   p.before = take(d->rows > CE_SCAN_ROWS ? up(d->rows, CE_COUNT_ROWS) / CE_COUNT_ROWS * 4 : 0);
-  p.z = tile_shape(d->rows, d->classes, p.parts, sms);
+  p.z = tile_shape(d->rows, d->classes, d->features, 1, p.parts, sms);
   if (!backward) {
     const int rows = 128 * p.z.cg, clusters = sms / p.z.cg;
     const int64_t blocks = up(p.rows, rows) / rows;
@@ -864,8 +868,8 @@ CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward,
     p.piece = 256 * piece_blocks(d, p.rows, p.parts, sms);
     p.pieces = (int)((d->classes + p.piece - 1) / p.piece);
     p.p_pitch = p.piece;
-    p.dx = tile_shape(d->rows, d->features, p.parts, sms);
-    p.dw = tile_shape(p.piece, d->features, p.parts, sms);
+    p.dx = tile_shape(d->rows, d->features, p.piece, 8, p.parts, sms);
+    p.dw = tile_shape(std::min<int64_t>(p.piece, d->classes), d->features, d->rows, 1, p.parts, sms);
     p.sums_pitch = (int)up(d->features, 32);
     const int rows = 128 * p.dx.cg, across = (int)up(d->features, p.dx.cols) / p.dx.cols, clusters = sms / p.dx.cg;
     p.dx_room = (int)(up(p.rows, rows) / rows) + 4 * clusters / across;

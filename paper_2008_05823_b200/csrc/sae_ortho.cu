@@ -474,7 +474,7 @@ void count_tiles(Shape& g, int rows, int cols) {
 // Tile shape of a class: time in units of a block's k loop, waves of tiles over the SMs (or pairs).
 void choose_tiles(Class& c, std::vector<Shape>& shapes, const std::vector<int>& count, int sms) {
   struct Form { int cg, cols; double cost; };
-  const Form forms[3] = {{2, c.parts == 1 ? 256 : 128, c.parts == 1 ? 2.0 : 1.2}, {1, 128, 1.3}, {1, 64, 1.0}};
+  const Form forms[3] = {{2, c.parts == 1 ? 256 : 128, c.parts == 1 ? 2.0 : 1.75}, {1, 128, 2.1}, {1, 64, 1.7}};
   double best = 0;
   for (const Form& f : forms) {
     const int units = sms / f.cg;
