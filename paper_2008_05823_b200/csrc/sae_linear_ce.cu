@@ -191,9 +191,9 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_rows(const __grid_constant__ 
       a.index[to] = (int)r;
       a.at[to] = cls;
       if constexpr (BACKWARD) {
-        a.lse_g[to] = a.lse_in[r];
+        a.lse_g[to] = cls < 0 ? __int_as_float(0x7fc00000) : a.lse_in[r];
         float f = a.reduction == SAE_REDUCE_NONE ? a.dloss[r] / (a.g_top ? *a.g_top : 1.0f) : 1.0f;
-        a.g[to] = (cls < 0 ? __int_as_float(0x7fc00000) : f) * a.p_scale;
+        a.g[to] = f * a.p_scale;
       }
     } else if (r < a.rows) {
       if constexpr (!BACKWARD) {
@@ -438,6 +438,7 @@ struct GradJob : mma::Plain {
   unsigned short* p;
   int64_t p_plane;
   int p_pitch, type;
+  bool scaled;                                   // a row's factor may be another than 1
   float* bias_sums;                              // [rows / 32][p_pitch], NULL: not wanted
 
   struct Local { int first, step, blocks; };
@@ -489,9 +490,14 @@ struct GradJob : mma::Plain {
 #pragma unroll
           for (int i = 0; i < 32; ++i) z[i] = mine == (unsigned)i ? z[i] - 1.0f : z[i];
         }
-        // a row that is none stays exactly zero, whatever its sums are
+        if (job.scaled) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) z[i] = used ? z[i] * g : 0.0f;
+          for (int i = 0; i < 32; ++i) z[i] *= g;
+        }
+        if (!used) {                              // a row that is none stays exactly zero, whatever its sums are
+#pragma unroll
+          for (int i = 0; i < 32; ++i) z[i] = 0.0f;
+        }
         unsigned short* const to = job.p + (int64_t)r * job.p_pitch + col;
         u32 w[16];
         if (job.type == SAE_TYPE_HALF) {
@@ -1104,6 +1110,7 @@ int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, cons
   g.counted = a.counted; g.classes = a.classes; g.features = a.features; g.rows = 128 * p.z.cg;
   g.bias = d->has_bias ? a.bias_out : nullptr; g.lse = a.lse_g; g.g = a.g; g.at = a.at;
   g.p = (unsigned short*)(ws + p.p); g.p_plane = p.rows * p.p_pitch; g.p_pitch = p.p_pitch; g.type = d->type;
+  g.scaled = d->reduction == SAE_REDUCE_NONE || a.p_scale != 1.0f;
   g.bias_sums = dbias ? (float*)(ws + p.bias_sums) : nullptr;
   ProductJob job = {};
   job.bfloat = bfloat; job.seg = g.seg; job.a = pm; job.counted = a.counted; job.features = a.features; job.alpha = a.alpha; job.type = d->type;
