@@ -3,6 +3,7 @@
 // CE_FLOAT_WORK for where the two meet).  Products are tiles of 32 x 64 by 128 threads, split along k until the SMs are
 // filled; whoever reads a product adds its splits in their order.
 #pragma once
+#include <cooperative_groups.h>
 
 namespace {
 
@@ -25,6 +26,7 @@ struct FloatArgs {
   void* dbias;
   int bias_type;
   const float* alpha;
+  const void* any;                            // an address that copies of nothing may name
 };
 
 __device__ __forceinline__ void store_bias(void* out, int type, int64_t j, float v) {
@@ -52,20 +54,17 @@ struct FloatTile {
   static constexpr int A_PITCH = (A_ROWS ? CF_ROWS : CF_K) + 4, B_PITCH = (B_ROWS ? CF_COLS : CF_K) + 4;
   static constexpr int A_SIZE = A_PITCH * (A_ROWS ? CF_K : CF_ROWS), B_SIZE = B_PITCH * (B_ROWS ? CF_K : CF_COLS);
   static constexpr int BYTES = CF_STAGES * (A_SIZE + B_SIZE) * 4;
+  // a thread's rows and columns of the tile
+  __device__ __forceinline__ static int row(int tr, int i) { return A_ROWS ? tr * 4 + i : tr + 8 * i; }
+  __device__ __forceinline__ static int col(int tc, int j) { return B_ROWS ? tc * 4 + j : tc + 16 * j; }
 };
 
-template <FloatProduct KIND>
-__global__ void __launch_bounds__(CF_THREADS) k_cf_product(const __grid_constant__ FloatArgs a) {
+// One tile: acc[i][j] for rows tr + 8 i (tr * 4 + i where A's rows are its fast direction) and columns tc + 16 j (tc * 4 + j).
+// row_at(i): where in memory the i-th row of x is, -1: nowhere (a row of zeros).
+template <FloatProduct KIND, typename RowAt>
+__device__ __forceinline__ void float_tile(const FloatArgs& a, float* smem, int row0, int col0, int rows, int cols, int depth, int c0, int c1, RowAt row_at, float (&acc)[4][4]) {
   typedef FloatTile<KIND> F;
-  extern __shared__ __align__(16) float smem[];
-  mma::let_next_start();
-  mma::wait_for_previous();
-  const int count = *a.counted, t = threadIdx.x;
-  const int rows = KIND == CF_DW ? a.classes : count, cols = KIND == CF_Z ? a.classes : a.features;
-  const int depth = KIND == CF_Z ? a.features : KIND == CF_DX ? a.classes : count;
-  const int row0 = blockIdx.y * CF_ROWS, col0 = blockIdx.x * CF_COLS;
-  if (row0 >= rows) return;
-  const int chunks = (depth + CF_K - 1) / CF_K, c0 = (int)((int64_t)chunks * blockIdx.z / a.splits), c1 = (int)((int64_t)chunks * (blockIdx.z + 1) / a.splits);
+  const int t = threadIdx.x;
   const auto fetch = [&](int chunk) {
     if (chunk < c1) {
       const int k0 = chunk * CF_K;
@@ -75,34 +74,31 @@ __global__ void __launch_bounds__(CF_THREADS) k_cf_product(const __grid_constant
       for (int u = t; u < CF_ROWS * CF_K / 4; u += CF_THREADS) {
         if constexpr (KIND == CF_DW) {
           const int k = u / (CF_ROWS / 4), r = u % (CF_ROWS / 4) * 4;
-          four_in(sa + k * F::A_PITCH + r, a.p + (int64_t)(k0 + k) * a.p_pitch + row0 + r, k0 + k < depth ? rows - row0 - r : 0, true, a.counted);
+          four_in(sa + k * F::A_PITCH + r, a.p + (int64_t)(k0 + k) * a.p_pitch + row0 + r, k0 + k < depth ? rows - row0 - r : 0, true, a.any);
         } else {
           const int r = u / (CF_K / 4), k = u % (CF_K / 4) * 4;
-          const bool there = row0 + r < rows;
-          if constexpr (KIND == CF_Z) four_in(sa + r * F::A_PITCH + k, a.x + (there ? (int64_t)a.index[row0 + r] * a.x_pitch : 0) + k0 + k, there ? depth - k0 - k : 0, a.vector, a.counted);
-          else four_in(sa + r * F::A_PITCH + k, a.p + (int64_t)(row0 + r) * a.p_pitch + k0 + k, there ? depth - k0 - k : 0, true, a.counted);
+          if constexpr (KIND == CF_Z) {
+            const int at = row0 + r < rows ? row_at(row0 + r) : -1;
+            four_in(sa + r * F::A_PITCH + k, a.x + (at >= 0 ? (int64_t)at * a.x_pitch : 0) + k0 + k, at >= 0 ? depth - k0 - k : 0, a.vector, a.any);
+          } else four_in(sa + r * F::A_PITCH + k, a.p + (int64_t)(row0 + r) * a.p_pitch + k0 + k, row0 + r < rows ? depth - k0 - k : 0, true, a.any);
         }
       }
 #pragma unroll
       for (int u = t; u < CF_COLS * CF_K / 4; u += CF_THREADS) {
         if constexpr (KIND == CF_Z) {
           const int c = u / (CF_K / 4), k = u % (CF_K / 4) * 4;
-          four_in(sb + c * F::B_PITCH + k, a.w + (int64_t)(col0 + c) * a.w_pitch + k0 + k, col0 + c < cols ? depth - k0 - k : 0, a.vector, a.counted);
+          four_in(sb + c * F::B_PITCH + k, a.w + (int64_t)(col0 + c) * a.w_pitch + k0 + k, col0 + c < cols ? depth - k0 - k : 0, a.vector, a.any);
         } else {
           const int k = u / (CF_COLS / 4), c = u % (CF_COLS / 4) * 4;
           const bool there = k0 + k < depth;
-          const float* const row = KIND == CF_DX ? a.w + (int64_t)(k0 + k) * a.w_pitch : a.x + (there ? (int64_t)a.index[k0 + k] * a.x_pitch : 0);
-          four_in(sb + k * F::B_PITCH + c, row + col0 + c, there ? cols - col0 - c : 0, a.vector, a.counted);
+          const float* const row = KIND == CF_DX ? a.w + (int64_t)(k0 + k) * a.w_pitch : a.x + (there ? (int64_t)row_at(k0 + k) * a.x_pitch : 0);
+          four_in(sb + k * F::B_PITCH + c, row + col0 + c, there ? cols - col0 - c : 0, a.vector, a.any);
         }
       }
     }
     copies_commit();
   };
-  // this thread's rows and columns of the tile
   const int tr = t / 16, tc = t % 16;
-  const auto row_of = [&](int i) { return F::A_ROWS ? tr * 4 + i : tr + 8 * i; };
-  const auto col_of = [&](int j) { return F::B_ROWS ? tc * 4 + j : tc + 16 * j; };
-  float acc[4][4] = {};
 #pragma unroll
   for (int i = 0; i < CF_STAGES - 1; ++i) fetch(c0 + i);
   for (int c = c0; c < c1; ++c) {
@@ -116,8 +112,8 @@ __global__ void __launch_bounds__(CF_THREADS) k_cf_product(const __grid_constant
       float x[4][4], y[4][4];             // [row or column][k]
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float4 v = *reinterpret_cast<const float4*>(F::A_ROWS ? sa + (k + i) * F::A_PITCH + tr * 4 : sa + row_of(i) * F::A_PITCH + k);
-        const float4 w = *reinterpret_cast<const float4*>(F::B_ROWS ? sb + (k + i) * F::B_PITCH + tc * 4 : sb + col_of(i) * F::B_PITCH + k);
+        const float4 v = *reinterpret_cast<const float4*>(F::A_ROWS ? sa + (k + i) * F::A_PITCH + tr * 4 : sa + F::row(tr, i) * F::A_PITCH + k);
+        const float4 w = *reinterpret_cast<const float4*>(F::B_ROWS ? sb + (k + i) * F::B_PITCH + tc * 4 : sb + F::col(tc, i) * F::B_PITCH + k);
         const float vs[4] = {v.x, v.y, v.z, v.w}, ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -128,7 +124,7 @@ __global__ void __launch_bounds__(CF_THREADS) k_cf_product(const __grid_constant
       if (KIND == CF_DW) {                // dbias: a feature that is always 1
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (col0 + col_of(j) == a.features) y[j][0] = y[j][1] = y[j][2] = y[j][3] = 1.0f;
+          if (col0 + F::col(tc, j) == a.features) y[j][0] = y[j][1] = y[j][2] = y[j][3] = 1.0f;
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q)
@@ -139,6 +135,25 @@ __global__ void __launch_bounds__(CF_THREADS) k_cf_product(const __grid_constant
     }
   }
   copies_wait<0>();
+}
+
+template <FloatProduct KIND>
+__global__ void __launch_bounds__(CF_THREADS) k_cf_product(const __grid_constant__ FloatArgs a) {
+  typedef FloatTile<KIND> F;
+  extern __shared__ __align__(16) float smem[];
+  mma::let_next_start();
+  mma::wait_for_previous();
+  const int count = *a.counted;
+  const int rows = KIND == CF_DW ? a.classes : count, cols = KIND == CF_Z ? a.classes : a.features;
+  const int depth = KIND == CF_Z ? a.features : KIND == CF_DX ? a.classes : count;
+  const int row0 = blockIdx.y * CF_ROWS, col0 = blockIdx.x * CF_COLS;
+  if (row0 >= rows) return;
+  const int chunks = (depth + CF_K - 1) / CF_K, c0 = (int)((int64_t)chunks * blockIdx.z / a.splits), c1 = (int)((int64_t)chunks * (blockIdx.z + 1) / a.splits);
+  float acc[4][4] = {};
+  float_tile<KIND>(a, smem, row0, col0, rows, cols, depth, c0, c1, [&](int i) { return a.index[i]; }, acc);
+  const int tr = threadIdx.x / 16, tc = threadIdx.x % 16;
+  const auto row_of = [&](int i) { return F::row(tr, i); };
+  const auto col_of = [&](int j) { return F::col(tc, j); };
   if (KIND == CF_DW && a.splits == 1) {
     const float alpha = *a.alpha;
 #pragma unroll
@@ -282,6 +297,88 @@ __global__ void __launch_bounds__(CF_THREADS) k_cf_sum(const __grid_constant__ F
   v *= *a.alpha;
   if (c == a.features) store_bias(a.dbias, a.bias_type, r, v);
   else if (a.out) a.out[(a.index ? (int64_t)a.index[r] : r) * a.features + c] = v;
+}
+
+// The whole forward pass of a head of up to 64 classes, few features and up to 256 rows: a block for 32 rows, the blocks one cluster, which
+// adds up the loss.
+struct TinyArgs {
+  FloatArgs f;
+  const int64_t* target;
+  int64_t ignore, *count;
+  const void* bias;
+  float *loss, *lse;
+  int rows, bias_type, reduction;
+};
+__global__ void __launch_bounds__(CF_THREADS) k_cf_tiny(const __grid_constant__ TinyArgs a) {
+  extern __shared__ __align__(16) float smem[];
+  __shared__ int at[CF_ROWS], cls[CF_ROWS];
+  __shared__ double sums[CF_THREADS / 32], total;
+  __shared__ int number;
+  namespace cg = cooperative_groups;
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int row0 = blockIdx.x * CF_ROWS, t = threadIdx.x, tr = t / 16, tc = t % 16;
+  if (t < CF_ROWS) {
+    const int64_t c = row0 + t < a.rows ? a.target[row0 + t] : a.ignore;
+    at[t] = row0 + t < a.rows && c != a.ignore ? row0 + t : -1;
+    cls[t] = c >= 0 && c < a.f.classes ? (int)c : -1;
+    const u32 used = __ballot_sync(0xffffffffu, at[t] >= 0);
+    if (t == 0) number = __popc(used);
+  }
+  __syncthreads();
+  float acc[4][4] = {};
+  float_tile<CF_Z>(a.f, smem, row0, 0, a.rows, a.f.classes, a.f.features, 0, (a.f.features + CF_K - 1) / CF_K, [&](int i) { return at[i - row0]; }, acc);
+  double sum = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = tr + 8 * i;
+    float m = __int_as_float(0xff800000), s = 0, z_at = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int c = tc + 16 * j;
+      if (c >= a.f.classes) { acc[i][j] = __int_as_float(0xff800000); continue; }
+      if (a.bias)
+        acc[i][j] += a.bias_type == SAE_TYPE_FLOAT ? ((const float*)a.bias)[c]
+                     : a.bias_type == SAE_TYPE_BFLOAT ? to_f(((const __nv_bfloat16*)a.bias)[c]) : to_f(((const __half*)a.bias)[c]);
+      m = fmaxf(m, acc[i][j]);
+      if (c == cls[r]) z_at = acc[i][j];
+    }
+    // over the 16 lanes of a row
+#pragma unroll
+    for (int o = 8; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s += exp2f((acc[i][j] - (m == __int_as_float(0xff800000) ? 0.0f : m)) * LOG2E);
+#pragma unroll
+    for (int o = 8; o; o >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, o);
+      z_at += __shfl_xor_sync(0xffffffffu, z_at, o);
+    }
+    if (tc == 0 && row0 + r < a.rows) {
+      const bool used = at[r] >= 0;
+      const float loss = used ? logf(s) + (m - (cls[r] >= 0 ? z_at : __int_as_float(0x7fc00000))) : 0.0f;
+      a.lse[row0 + r] = used ? m + logf(s) : 0.0f;
+      if (a.reduction == SAE_REDUCE_NONE) a.loss[row0 + r] = loss;
+      sum += loss;
+    }
+  }
+  sum += __shfl_xor_sync(0xffffffffu, sum, 16);          // lanes 0 and 16 have the sums of their rows
+  if (t % 32 == 0) sums[t / 32] = sum;
+  __syncthreads();
+  if (t == 0) {
+    total = 0;
+    for (int i = 0; i < CF_THREADS / 32; ++i) total += sums[i];
+  }
+  cluster.sync();
+  if (cluster.block_rank() == 0 && t == 0) {
+    double all = 0;
+    int n = 0;
+    for (unsigned i = 0; i < cluster.num_blocks(); ++i) {
+      all += *cluster.map_shared_rank(&total, i);
+      n += *cluster.map_shared_rank(&number, i);
+    }
+    *a.count = n;
+    if (a.reduction != SAE_REDUCE_NONE) *a.loss = (float)(a.reduction == SAE_REDUCE_MEAN ? all / (double)n : all);
+  }
+  cluster.sync();                                        // no block leaves while its sums are read
 }
 
 }  // namespace

@@ -489,12 +489,6 @@ template <int WIDE>
 __device__ __forceinline__ u32 staged_at(u32 base, int r, int piece) {
   return base + (u32)(r * WIDE + (piece ^ (WIDE == 4 ? (r >> 1) & 3 : r & 7))) * 16;
 }
-template <int WIDE>
-__device__ __forceinline__ void staged_store(u32 base, int r, int piece, const u32 (&w)[16]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(staged_at<WIDE>(base, r, piece + i)), "r"(w[4 * i]), "r"(w[4 * i + 1]), "r"(w[4 * i + 2]), "r"(w[4 * i + 3]) : "memory");
-}
 __device__ __forceinline__ uint4 staged_piece(u32 at) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");

@@ -57,7 +57,7 @@ struct Shape {
   int first;                                  // its first matrix in the class's order
 };
 // One product of some neighbouring matrices of a shape: tiles begin .. end - 1 of the list.
-struct Batch { int begin, end, first; unsigned short shape; unsigned char phase, step; };
+struct Batch { int begin, end, first; u32 shape : 24, phase : 2, step : 6; };     // (up to 2^20 shapes, 64 steps)
 
 struct Matrix { const void* in; void* out; long long in_ld, out_ld; };
 struct Place { int rows, cols, x_pitch, in_type, out_type, first_chunk, chunks; __half* x; long long x_plane; u32* done; float* ratio; int plain; };
@@ -520,7 +520,7 @@ void list_products(Class& c, const std::vector<Shape>& shapes, const std::vector
           Batch b = {};
           b.begin = (int)at;
           b.end = (int)(at += (int64_t)q.n * (phase == PHASE_X ? g.x_tiles : g.s_tiles));
-          b.first = q.first; b.shape = (unsigned short)(q.shape - c.first); b.phase = (unsigned char)phase; b.step = (unsigned char)s;
+          b.first = q.first; b.shape = (u32)(q.shape - c.first); b.phase = (u32)phase; b.step = (u32)s;
           batches.push_back(b);
         }
   c.batches = (int)batches.size() - c.first_batch;

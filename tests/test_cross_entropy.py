@@ -187,6 +187,64 @@ def test_large(dtype, n, d, v, ignored):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_factors_of_their_own_in_large_problems(dtype):
+    """A dloss of its own for every row, of both signs and far apart, where tiles are shared by pairs of blocks."""
+    x, w, t, b = data(3000, 512, 6001, DTYPES[dtype], True, 0.3, seed=21)
+    dloss = torch.randn(3000, device="cuda") * 2.0 ** (torch.arange(3000, device="cuda") % 24 - 12)
+    check(x, w, t, b, "none", dloss)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,d,v", [(256, 192, 64), (257, 192, 64), (256, 193, 64), (256, 192, 65), (255, 191, 63), (33, 20, 64), (32, 1, 1), (256, 512, 64), (255, 511, 63)])
+def test_small_float_heads(n, d, v):
+    """Where one launch takes them and just beyond: every reduction and type of bias, weights that start anywhere, an infinity, a masked
+    class, a target that is none, nothing to count."""
+    for i, reduction in enumerate(("mean", "sum", "none")):
+        x, w, t, _ = data(n, d, v, torch.float32, False, 0.2, seed=n + i)
+        t[0] = v - 1
+        b = torch.randn(v, device="cuda").to(list(DTYPES.values())[i])
+        dloss = torch.rand(n, device="cuda") - 0.3 if reduction == "none" else torch.tensor(0.7, device="cuda")
+        check(x, w, t, b, reduction, dloss)
+        want = ce.linear_cross_entropy_forward(x, w, t, b, reduction=reduction)
+        flat = w.new_empty(w.numel() + 1)
+        flat[1:] = w.reshape(-1)
+        wide = x.new_full((n, d + 5), math.nan)
+        wide[:, 3:3 + d] = x
+        got = ce.linear_cross_entropy_forward(wide[:, 3:3 + d], flat[1:].view(v, d), t, b, reduction=reduction)
+        assert all(torch.equal(p, q) for p, q in zip(want, got))
+    rows = want[0]
+    used = t != IGNORE
+    bad = x.clone()
+    bad[~used] = math.nan
+    assert torch.equal(ce.linear_cross_entropy_forward(bad, w, t, b, reduction="none")[0], rows)
+    others = torch.arange(n, device="cuda") != 0
+    for value in (math.nan, math.inf):
+        bad = x.clone()
+        bad[0, d - 1] = value
+        got = ce.linear_cross_entropy_forward(bad, w, t, b, reduction="none")[0]
+        assert torch.equal(got[others], rows[others]) and torch.isnan(got[0])
+    for value in (v, -1, 2 ** 40):
+        wrong = t.clone()
+        wrong[0] = value
+        got = ce.linear_cross_entropy_forward(x, w, wrong, b, reduction="none")
+        assert torch.equal(got[0][others], rows[others]) and torch.isnan(got[0][0]) and torch.equal(got[1], want[1])
+        assert torch.isnan(ce.linear_cross_entropy_forward(x, w, wrong, b)[0])
+    masked = b.float()
+    masked[v - 1] = -math.inf
+    got = ce.linear_cross_entropy_forward(x, w, t, masked, reduction="none")[0]
+    assert float(got[0]) == math.inf if v > 1 else torch.isnan(got[0])
+    if v > 1:
+        keep = used & (t != v - 1)
+        less = ce.linear_cross_entropy_forward(x, w[:-1], torch.where(keep, t, IGNORE), masked[:-1], reduction="none")[0]
+        e = Exact(x, w[:-1], torch.where(keep, t, IGNORE), masked[:-1], "none")
+        near(got[keep], e.loss[keep], e.loss_off[keep], "masked")
+        near(less, e.loss, e.loss_off, "fewer classes")
+    none = torch.full_like(t, IGNORE)
+    assert float(ce.linear_cross_entropy_forward(x, w, none, b, reduction="sum")[0]) == 0 and torch.isnan(ce.linear_cross_entropy_forward(x, w, none, b)[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_layouts(dtype):
     """Slices of wider tensors, odd offsets, an expanded row, transposed storage, more dimensions: the bits of the plain tensors."""
     x, w, t, b = data(96, 72, 200, DTYPES[dtype], True, 0.2, seed=5)
@@ -462,6 +520,33 @@ def test_on_another_stream_and_captured():
     want = both()
     for out in outs:
         assert all(torch.equal(p, q) for p, q in zip(want, out))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,n,d,v", [("f32", 100, 64, 10), ("bf16", 300, 64, 500)])
+def test_captured_training(dtype, n, d, v):
+    """Loss and gradients by autograd inside a graph, replayed on other data; eager calls of other leaves go on beside it."""
+    x, w, t, b = data(n, d, v, DTYPES[dtype], True, 0.2, seed=8)
+    leaves = [a.clone().requires_grad_() for a in (x, w, b)]
+
+    def both(p, t):
+        loss = ce.linear_cross_entropy(p[0], p[1], t, p[2])
+        return (loss.detach(),) + torch.autograd.grad(loss * 3, p)
+    both(leaves, t)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = both(leaves, t)
+    x2, w2, t2, b2 = data(n, d, v, DTYPES[dtype], True, 0.5, seed=18)
+    with torch.no_grad():
+        for p, q in zip(leaves, (x2, w2, b2)):
+            p.copy_(q)
+    t.copy_(t2)
+    want = both([a.clone().requires_grad_() for a in (x2, w2, b2)], t2)
+    for _ in range(2):
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want))
 
 
 @pytest.mark.gpu

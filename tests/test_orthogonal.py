@@ -9,6 +9,7 @@ import torch
 
 from paper_2008_05823_b200 import binding as sb
 from paper_2008_05823_b200 import orthogonal
+from paper_2008_05823_b200.cross_entropy import linear_cross_entropy_forward
 from paper_2008_05823_b200.orthogonal import COEFFICIENTS, Orthogonalizer
 
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
@@ -280,6 +281,31 @@ def test_streams_and_graphs():
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(out, plan(gs)))
+
+
+@pytest.mark.gpu
+def test_two_plans_at_once():
+    """On two streams, beside a loss on a third: all their blocks have to share the SMs."""
+    shapes = [(300, 500), (140, 900), (100, 64)]
+    kinds = [torch.bfloat16, torch.float32]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    gs = [[gradient(s, k, i + 10 * q) for i, s in enumerate(shapes)] for q, k in enumerate(kinds)]
+    want = [Orthogonalizer(shapes, k)(g) for k, g in zip(kinds, gs)]
+    x, w, t = torch.randn((2000, 128), device="cuda").bfloat16(), torch.randn((5000, 128), device="cuda").bfloat16(), torch.randint(5000, (2000,), device="cuda")
+    loss = linear_cross_entropy_forward(x, w, t)[0]
+    plans = [Orthogonalizer(shapes, k, stream=s.cuda_stream) for k, s in zip(kinds, streams)]
+    torch.cuda.synchronize()
+    got, losses = [[], []], []
+    for _ in range(10):
+        for q in range(2):
+            with torch.cuda.stream(streams[q]):
+                got[q].append(plans[q](gs[q]))
+        with torch.cuda.stream(streams[2]):
+            losses.append(linear_cross_entropy_forward(x, w, t)[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(v, loss) for v in losses)
+    for q in range(2):
+        assert all(torch.equal(a, b) for run in got[q] for a, b in zip(run, want[q]))
 
 
 @pytest.mark.gpu
