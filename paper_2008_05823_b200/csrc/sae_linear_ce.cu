@@ -37,6 +37,57 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+// ---- pieces and splits ----------------------------------------------------------------------------------------------------
+// Pieces of the classes.  p has room for all rows times `piece` classes; where fewer rows take part, a piece has as many times more classes, up
+// to CE_WIDER, and the launches for the last pieces find nothing to do (16384 x 768 x 30522, 15 % of the targets: one piece in place of five).
+constexpr int CE_WIDER = 8;
+struct Pieces {
+  int piece, number, classes, most;     // most: times wider at most
+  int64_t rows;
+  __device__ __host__ __forceinline__ int times(int count) const {
+    const int64_t taken = ((int64_t)count + 255) / 256 * 256;
+    const int can = (int)(taken ? (rows / taken < most ? rows / taken : most) : most);
+    const int left = (number + can - 1) / can;                       // pieces
+    return (number + left - 1) / left;
+  }
+};
+
+// Time of a list of tiles that the clusters take in turn: n1 of them, then n2, in units of a tile's k.
+__device__ __host__ inline float list_time(u32 n1, float t1, u32 n2, float t2, u32 clusters) {
+  const u32 whole1 = n1 / clusters, left1 = n1 - whole1 * clusters, whole = (n1 + n2) / clusters, left = n1 + n2 - whole * clusters;
+  float most = 0;
+  for (int i = 0; i < 3; ++i) {                   // the loads are the same between these clusters
+    const u32 at = i == 0 ? 0 : i == 1 ? left1 : left, a = whole1 + (at < left1), b = whole + (at < left) - a;
+    const float t = (float)a * t1 + (float)b * t2;
+    most = t > most ? t : most;
+  }
+  return most;
+}
+// How often the classes of a piece are split for dx, where there are too few tiles for the clusters, or tiles of dweight beside them.  A tile's
+// own sums, read and written in float, are about 500 k (2458 x 768 and 6144 classes: 2 splits 25 us, 7 splits, which fill three waves
+// to 95 %, 44 us).
+struct Product {
+  int dx_blocks, across, clusters, depth, room;   // blocks of rows, tiles across the features; classes of a whole piece; row blocks that the sums have place for
+  int dw_tiles, count;
+  __device__ __host__ inline float time(int s) const {
+    const u32 n = (u32)(dx_blocks * across * s);
+    const float dx = (float)depth / (float)s + 500.0f, dw = (float)count;
+    return dx > dw ? list_time(n, dx, dw_tiles, dw, clusters) : list_time(dw_tiles, dw, n, dx, clusters);
+  }
+  __device__ __host__ inline int splits() const {
+    int best = 1;
+    float least = 0;
+    for (int s = 1; s <= 8 && (s == 1 || (int64_t)s * dx_blocks <= room); ++s) {
+      const float t = time(s);
+      if (s == 1 || t < least) { least = t; best = s; }
+    }
+    return best;
+  }
+};
+
+// What the gathering kernel leaves for those behind it: the rows that take part, a ticket of the forward pass, and what their number decides.
+enum Counted { COUNT_ROWS, COUNT_TICKET, COUNT_TIMES, COUNT_SPLITS, COUNT_WORDS };      // how much wider pieces are; splits of dx
+
 // ---- gathering ----------------------------------------------------------------------------------------------------------
 struct RowsArgs {
   const void* x;
@@ -48,11 +99,14 @@ struct RowsArgs {
   const int* before;                              // rows that take part in each CE_COUNT_ROWS, where there are many
   int* index;                                     // of every gathered row: where it came from,
   int* at;                                        // its target (-1: out of range),
-  int* counted;                                   // and how many there are
+  int* counted;                                   // and how many there are: [COUNT_WORDS]
   int64_t* count;                                 // forward: the caller's
   float *loss, *lse;                              // forward: 0 for rows that take no part (loss NULL: reduced)
-  unsigned* ticket;
   // backward
+  Pieces pieces;
+  Product product;                                // of a piece, but for what the count gives
+  bool both;                                      // dx and dweight in one list
+  int product_rows;                               // rows of a tile of it
   const float *lse_in, *dloss;
   const int64_t* count_in;
   int reduction;
@@ -204,7 +258,7 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_rows(const __grid_constant__ 
     if (b + 1 == a.row_blocks && lane == 0) {
       const int n = base + __popc(mask);
       *a.counted = n;
-      if constexpr (!BACKWARD) { *a.count = n; *a.ticket = 0; }
+      if constexpr (!BACKWARD) { *a.count = n; a.counted[COUNT_TICKET] = 0; }
       else {
         float f = 1.0f;
         if (n == 0) f = 0.0f;                                  // sums of nothing
@@ -232,6 +286,17 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_rows(const __grid_constant__ 
         else for (int c = lane; c < a.features; c += 32) ((unsigned short*)row)[c] = 0;
       }
     }
+  }
+  // (here, where other warps still copy: 0.5 us; in the kernels that need it, it took them 1 to 4 us each)
+  if (BACKWARD && a.xg && b + 1 == a.row_blocks && threadIdx.x == 0) {
+    const int n = a.counted[COUNT_ROWS], times = a.pieces.times(n), piece = a.pieces.piece * times;
+    Product q = a.product;
+    q.count = n;
+    q.dx_blocks = (n + a.product_rows - 1) / a.product_rows;
+    q.depth = piece;
+    q.dw_tiles = a.both ? (min(piece, a.classes) + a.product_rows - 1) / a.product_rows * q.across : 0;
+    a.counted[COUNT_TIMES] = times;
+    a.counted[COUNT_SPLITS] = q.splits();
   }
   if (BACKWARD && a.xg && b + 1 == a.row_blocks) {  // the last block of k of dweight's product reads zeros behind the last row
     int last = -1;
@@ -432,24 +497,33 @@ struct GradJob : mma::Plain {
   mma::Segments seg;
   CUtensorMap x, w;
   const int* counted;
-  int classes, features, rows, start, tiles;     // first class of the piece, tiles across it
+  Pieces pieces;
+  int classes, features, rows, index;            // index: of the piece
   const float *bias, *lse, *g;
   const int* at;
   unsigned short* p;
   int64_t p_plane;
-  int p_pitch, type;
+  int type;
   bool scaled;                                   // a row's factor may be another than 1
-  float* bias_sums;                              // [rows / 32][p_pitch], NULL: not wanted
+  float* bias_sums;                              // of every 32 rows, as p; NULL: not wanted
 
-  struct Local { int first, step, blocks; };
-  __device__ __forceinline__ Local begin(const Shared&, int cluster, int clusters) const { return {cluster, clusters, (*counted + rows - 1) / rows}; }
+  struct Local { int first, step, blocks, start, tiles, pitch, count; };        // first class of the piece, tiles across it
+  __device__ __forceinline__ Local begin(const Shared&, int cluster, int clusters) const {
+    Local l = {cluster, clusters, 0, 0, 0, 0, *counted};
+    l.blocks = (l.count + rows - 1) / rows;
+    l.pitch = pieces.piece * counted[COUNT_TIMES];
+    const int64_t start = (int64_t)index * l.pitch;
+    l.start = (int)(start < classes ? start : classes);
+    l.tiles = (min(l.pitch, classes - l.start) + cols - 1) / cols;
+    return l;
+  }
   __device__ __forceinline__ bool tile(Local& l, int i, mma::Tile& t) const {
     const long long n = l.first + (long long)i * l.step;
-    if (n >= (long long)l.blocks * tiles) return false;
+    if (n >= (long long)l.blocks * l.tiles) return false;
     const int v = (int)(n / l.blocks);
     t.row = t.a_row = (int)(n - (long long)v * l.blocks) * rows;
     t.col = v * cols;
-    t.b_row = start + t.col;
+    t.b_row = l.start + t.col;
     t.a = &x;
     t.b = &w;
     t.a_plane = t.b_plane = t.a_k = t.b_k = t.a_turn = t.b_turn = 0;
@@ -459,18 +533,19 @@ struct GradJob : mma::Plain {
   }
   struct Epilogue {
     const GradJob& job;
+    const Local& l;
     const int row, half;
-    __device__ __forceinline__ Epilogue(const GradJob& j, const Local&, int r, int h, u32) : job(j), row(r), half(h) {}
+    __device__ __forceinline__ Epilogue(const GradJob& j, const Local& l, int r, int h, u32) : job(j), l(l), row(r), half(h) {}
     __device__ __forceinline__ void prepare(const mma::Tile&, int, mma::Control*) {}
     __device__ __forceinline__ void finish() {}
     __device__ __forceinline__ void tile(const mma::Tile& t, const mma::Sums& sums) {
       const int r = t.row + row;
-      const bool used = r < *job.counted;
+      const bool used = r < l.count;
       const float lse = used ? job.lse[r] : 0.0f, g = used ? job.g[r] : 0.0f;
-      const int cls = used ? job.at[r] - job.start : -1;
+      const int cls = used ? job.at[r] - l.start : -1;
       const int width = job.cols / 2;
       for (int c = half * width; c < (half + 1) * width; c += 32) {
-        const int col = t.col + c, cc = job.start + col;
+        const int col = t.col + c, cc = l.start + col;
         float z[32];
         mma::sums_of(sums, c, z);
         if (job.bias) {
@@ -498,7 +573,7 @@ struct GradJob : mma::Plain {
 #pragma unroll
           for (int i = 0; i < 32; ++i) z[i] = 0.0f;
         }
-        unsigned short* const to = job.p + (int64_t)r * job.p_pitch + col;
+        unsigned short* const to = job.p + (int64_t)r * l.pitch + col;
         u32 w[16];
         if (job.type == SAE_TYPE_HALF) {
 #pragma unroll
@@ -530,99 +605,100 @@ struct GradJob : mma::Plain {
               const float keep = lane & o ? z[i + o] : z[i], give = lane & o ? z[i] : z[i + o];
               z[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
             }
-          job.bias_sums[(int64_t)((t.row + row) >> 5) * job.p_pitch + col + lane] = z[0];
+          job.bias_sums[(int64_t)((t.row + row) >> 5) * l.pitch + col + lane] = z[0];
         }
       }
     }
   };
 };
 
-// How often the classes of a piece are split for dx, where there are too few tiles for the clusters.  Time in units of a tile's k; a tile's own
-// sums, read and written in float, are about 500 of them (2458 x 768 and 6144 classes: 2 splits 25 us, 7 splits, which fill three waves
-// to 95 %, 44 us).
-__device__ __host__ inline float dx_time(int blocks, int tiles_across, int clusters, int depth, int s) {
-  const long long t = (long long)blocks * tiles_across * s;
-  return (float)((t + clusters - 1) / clusters) * ((float)depth / (float)s + 500.0f);
-}
-__device__ __host__ inline int dx_splits(int blocks, int tiles_across, int clusters, int depth, int room) {
-  int best = 1;
-  for (int s = 2; s <= 8 && s <= room; ++s)
-    if (dx_time(blocks, tiles_across, clusters, depth, s) < dx_time(blocks, tiles_across, clusters, depth, best)) best = s;
-  return best;
-}
-
-// dx's sums (p w, float, added up over the pieces) and dweight of a piece (p' x).
+// dx's sums (p w, float, added up over the pieces) and dweight of a piece (p' x): one list of tiles, the longer ones first, or either alone.
 struct ProductJob : mma::Plain {
   static constexpr int STAGING = mma::SQUARE_BYTES;
   int cols;
   bool bfloat;
   mma::Segments seg;
-  CUtensorMap a, b;
+  CUtensorMap p[CE_WIDER], w, x;  // p: for pieces of 1, 2 .. times the classes
   const int* counted;
+  Pieces pieces;
   int rows, across, features;     // rows of a tile, tiles across the features
-  int start, width;               // the piece's first class and its classes, rounded up to 64
-  bool dx;
+  int classes, index;             // index: of the piece
+  bool dx, dweight;
   // dx
-  float* sums;                    // dweight: those of its splits, where it has more than one
-  int depth;                      // classes of a whole piece
-  int sums_pitch, room, add;      // room: row blocks that the sums have place for
-  int dw_splits;
+  float* dx_sums;
+  int sums_pitch;
   // dweight
+  float* dw_sums;                 // of its splits, where it has more than one
+  int dw_splits;
   void* out;
-  int type, classes;              // classes of the piece
+  int type;
   bool whole_rows;                // every row starts on 32 bytes
   const float* alpha;
 
-  struct Local { int first, step, blocks, splits, count; };
+  struct Local { int first, step, count, times, start, width, dx_blocks, splits, dx_tiles, dw_blocks, dw_tiles; bool dx_first; };
   __device__ __forceinline__ Local begin(const Shared&, int cluster, int clusters) const {
-    Local l = {cluster, clusters, 0, 1, *counted};
-    l.blocks = ((dx ? l.count : classes) + rows - 1) / rows;
-    l.splits = dx ? dx_splits(l.blocks, across, clusters, depth, l.blocks ? room / l.blocks : 1) : dw_splits;
+    Local l = {};
+    l.first = cluster; l.step = clusters; l.count = *counted; l.splits = 1;
+    l.times = counted[COUNT_TIMES];
+    const int piece = pieces.piece * l.times;
+    const int64_t start = (int64_t)index * piece;
+    if (start >= classes) return l;
+    l.start = (int)start;
+    l.width = min(piece, classes - l.start);
+    if (dx) l.dx_blocks = (l.count + rows - 1) / rows;
+    if (dweight) l.dw_blocks = (l.width + rows - 1) / rows;
+    l.dw_tiles = l.dw_blocks * across * dw_splits;
+    if (dx) l.splits = counted[COUNT_SPLITS];
+    l.dx_tiles = l.dx_blocks * across * l.splits;
+    l.dx_first = l.width / l.splits + 500 > l.count;
     return l;
   }
   __device__ __forceinline__ bool tile(Local& l, int i, mma::Tile& t) const {
-    const long long n = l.first + (long long)i * l.step;
-    if (n >= (long long)l.blocks * l.splits * across) return false;
-    const int q = (int)(n / across);
-    t.item = q / l.blocks;                        // the split
-    t.row = t.a_row = (q - t.item * l.blocks) * rows;
-    t.col = t.b_row = (int)(n - (long long)q * across) * cols;
-    t.a = &a;
-    t.b = &b;
+    const long long at = l.first + (long long)i * l.step;
+    if (at >= (long long)l.dx_tiles + l.dw_tiles) return false;
+    const bool is_dx = l.dx_first ? at < l.dx_tiles : at >= l.dw_tiles;
+    const int n = (int)at - (is_dx == l.dx_first ? 0 : is_dx ? l.dw_tiles : l.dx_tiles), blocks = is_dx ? l.dx_blocks : l.dw_blocks, q = n / across;
+    t.item = q / blocks;                          // the split
+    t.row = t.a_row = (q - t.item * blocks) * rows;
+    t.col = t.b_row = (n - q * across) * cols;
+    t.a = &p[l.times - 1];
+    t.b = is_dx ? &w : &x;
     t.a_plane = t.b_plane = t.a_turn = t.b_turn = 0;
     t.b_rows_first = true;
-    t.a_rows_first = !dx;
-    const int all = ((dx ? width : l.count) + mma::BLOCK_K - 1) / mma::BLOCK_K;
-    const int from = (int)((long long)all * t.item / l.splits), to = (int)((long long)all * (t.item + 1) / l.splits);
+    t.a_rows_first = !is_dx;                      // (what the epilogue knows them by, too)
+    const int all = ((is_dx ? l.width : l.count) + mma::BLOCK_K - 1) / mma::BLOCK_K, splits = is_dx ? l.splits : dw_splits;
+    const int from = (int)((long long)all * t.item / splits), to = (int)((long long)all * (t.item + 1) / splits);
     t.a_k = from * mma::BLOCK_K;
-    t.b_k = t.a_k + (dx ? start : 0);
+    t.b_k = t.a_k + (is_dx ? l.start : 0);
     t.blocks = to - from;
-    t.group = l.blocks * rows;                    // rows of a split's sums
+    t.group = blocks * rows;                      // rows of a split's sums
     return true;
   }
   struct Epilogue {
     const ProductJob& job;
+    const Local& l;
     const int row, half;
     const float alpha;
-    const int limit;
     const u32 staging;
-    __device__ __forceinline__ Epilogue(const ProductJob& j, const Local& l, int r, int h, u32 at) : job(j), row(r), half(h), alpha(j.dx || j.dw_splits > 1 ? 1.0f : *j.alpha), limit(j.dx ? l.count : j.classes), staging(at) {}
+    __device__ __forceinline__ Epilogue(const ProductJob& j, const Local& l, int r, int h, u32 at)
+        : job(j), l(l), row(r), half(h), alpha(j.dweight && j.dw_splits == 1 ? *j.alpha : 1.0f), staging(at) {}
     __device__ __forceinline__ void prepare(const mma::Tile&, int, mma::Control*) {}
     __device__ __forceinline__ void finish() {}
     __device__ __forceinline__ void tile(const mma::Tile& t, const mma::Sums& sums) {
-      const int r = t.row + row, w = job.cols / 2;
+      const bool dx = !t.a_rows_first, apart = dx || job.dw_splits > 1, add = dx && job.index;
+      const int r = t.row + row, w = job.cols / 2, limit = dx ? l.count : l.width;
       for (int c = half * w; c < (half + 1) * w; c += 32) {
         const int col = t.col + c;
         if (col >= job.features) break;
+        __syncwarp();
         float v[32];
         mma::sums_of(sums, c, v);
-        const bool apart = job.dx || job.dw_splits > 1;
         if (!apart && !job.whole_rows) {
           const int row0 = t.row + (row & ~31);
           if (row0 >= limit) continue;                    // the whole warp's
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] *= alpha;
-          const int64_t to = (int64_t)(job.start + row0) * job.features + col;
+          const int64_t to = (int64_t)(l.start + row0) * job.features + col;
           const int m = min(32, limit - row0), n = min(32, job.features - col);
           if (job.type == SAE_TYPE_FLOAT) mma::store_square((float*)job.out + to, job.features, v, m, n, staging);
           else if (job.type == SAE_TYPE_BFLOAT) mma::store_square((__nv_bfloat16*)job.out + to, job.features, v, m, n, staging);
@@ -631,8 +707,8 @@ struct ProductJob : mma::Plain {
         }
         if (r >= limit) continue;
         if (apart) {
-          float* const to = job.sums + ((int64_t)t.item * t.group + r) * job.sums_pitch + col;
-          if (job.add) {
+          float* const to = (dx ? job.dx_sums : job.dw_sums) + ((int64_t)t.item * t.group + r) * job.sums_pitch + col;
+          if (add) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               u32 old[16];
@@ -646,7 +722,7 @@ struct ProductJob : mma::Plain {
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] *= alpha;
           const int n = min(32, job.features - col);
-          const int64_t to = (int64_t)(job.start + r) * job.features + col;
+          const int64_t to = (int64_t)(l.start + r) * job.features + col;
           if (job.type == SAE_TYPE_FLOAT) mma::store_row((float*)job.out + to, v, n);
           else if (job.type == SAE_TYPE_BFLOAT) mma::store_row((__nv_bfloat16*)job.out + to, v, n);
           else mma::store_row((__half*)job.out + to, v, n);
@@ -662,7 +738,7 @@ struct DxArgs {
   const int *counted, *index;
   const float* alpha;
   void* dx;
-  int sums_pitch, features, type, rows, across, clusters, depth, room;
+  int sums_pitch, features, type, rows;
   int dw_rows, dw_splits;           // dweight: its rows and splits (0: this is dx)
 };
 template <typename T>
@@ -686,7 +762,7 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_dx(const __grid_constant__ Dx
   mma::wait_for_previous();
   const int count = a.dw_splits ? a.dw_rows : *a.counted, blocks = (count + a.rows - 1) / a.rows;
   if (!blocks) return;
-  const int splits = a.dw_splits ? a.dw_splits : dx_splits(blocks, a.across, a.clusters, a.depth, a.room / blocks);
+  const int splits = a.dw_splits ? a.dw_splits : a.counted[COUNT_SPLITS];
   const int64_t plane = (int64_t)blocks * a.rows * a.sums_pitch;
   const float alpha = *a.alpha;
   const unsigned wide = (unsigned)(a.features + UNIT - 1) / UNIT;
@@ -709,21 +785,27 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_dx(const __grid_constant__ Dx
 }
 
 // dbias of a piece: the sums of every 32 rows, added in order (double).
-__global__ void __launch_bounds__(CE_THREADS) k_ce_dbias(const float* sums, int pitch, const int* counted, const float* alpha, int classes, int type, void* out) {
+__global__ void __launch_bounds__(CE_THREADS) k_ce_dbias(const float* sums, const Pieces pieces, int index, const int* counted, const float* alpha, int type, void* out) {
   __shared__ double scratch[CE_THREADS / 32][32];
   mma::let_next_start();
   mma::wait_for_previous();
-  const int j = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5, n = (*counted + 31) / 32;
-  double s = 0;
-  if (j < classes) for (int i = part; i < n; i += CE_THREADS / 32) s += __ldcg(sums + (int64_t)i * pitch + j);
-  scratch[part][threadIdx.x & 31] = s;
-  __syncthreads();
-  if (part || j >= classes) return;
-  for (int i = 1; i < CE_THREADS / 32; ++i) s += scratch[i][threadIdx.x & 31];
-  const float v = (float)(s * *alpha);
-  if (type == SAE_TYPE_FLOAT) ((float*)out)[j] = v;
-  else if (type == SAE_TYPE_BFLOAT) ((__nv_bfloat16*)out)[j] = __float2bfloat16_rn(v);
-  else ((__half*)out)[j] = __float2half_rn(v);
+  const int count = *counted, pitch = pieces.piece * counted[COUNT_TIMES], part = threadIdx.x >> 5, n = (count + 31) / 32;
+  const int64_t start = (int64_t)index * pitch;
+  for (int64_t block = blockIdx.x; block * 32 < pitch && start + block * 32 < pieces.classes; block += gridDim.x) {
+    const int j = (int)block * 32 + (threadIdx.x & 31);
+    const int64_t to = start + j;
+    double s = 0;
+    if (to < pieces.classes) for (int i = part; i < n; i += CE_THREADS / 32) s += __ldcg(sums + (int64_t)i * pitch + j);
+    __syncthreads();
+    scratch[part][threadIdx.x & 31] = s;
+    __syncthreads();
+    if (part || to >= pieces.classes) continue;
+    for (int i = 1; i < CE_THREADS / 32; ++i) s += scratch[i][threadIdx.x & 31];
+    const float v = (float)(s * *alpha);
+    if (type == SAE_TYPE_FLOAT) ((float*)out)[to] = v;
+    else if (type == SAE_TYPE_BFLOAT) ((__nv_bfloat16*)out)[to] = __float2bfloat16_rn(v);
+    else ((__half*)out)[to] = __float2half_rn(v);
+  }
 }
 
 }  // namespace
@@ -767,18 +849,40 @@ struct TileShape { int cg, cols; };
 // The tile shape of a product of `depth` k: waves of tiles over the SMs (or pairs) times what a tile costs for each k.  A block of 64 k takes a pair
 // 588 cycles for 256 x 256, one SM 630 for 128 x 128 (shared memory: the tensor cores read and TMA writes 64 KB in it) and about 500
 // for 128 x 64.  splits: where sums may be added up in several parts of k, at 500 k for each, the best number of them counts.
-TileShape tile_shape(int64_t rows, int64_t cols, int64_t depth, int splits, int parts, int sms) {
-  const struct { TileShape s; double cost; } shapes[3] = {{{2, parts == 1 ? 256 : 128}, parts == 1 ? 2.0 : 1.6}, {{1, 128}, 2.1}, {{1, 64}, 1.7}};
-  TileShape best = shapes[0].s;
+struct CostedShape { TileShape s; double cost; };
+CostedShape costed_shape(int i, int parts) {
+  const CostedShape shapes[3] = {{{2, parts == 1 ? 256 : 128}, parts == 1 ? 2.0 : 1.6}, {{1, 128}, 2.1}, {{1, 64}, 1.7}};
+  return shapes[i];
+}
+TileShape tile_shape(int64_t rows, int64_t cols, int64_t depth, int splits, int parts, int sms, double* time = nullptr) {
+  TileShape best = {};
   double least = 0;
-  for (const auto& c : shapes) {
+  for (int i = 0; i < 3; ++i) {
+    const CostedShape c = costed_shape(i, parts);
     const int64_t tiles = (rows + 128 * c.s.cg - 1) / (128 * c.s.cg) * ((cols + c.s.cols - 1) / c.s.cols), units = sms / c.s.cg;
     for (int s = 1; s <= splits; ++s) {
       const double t = c.cost * (double)((tiles * s + units - 1) / units) * ((double)depth / s + (splits > 1 ? 500.0 : 0.0));
       if (least == 0 || t < least) { least = t; best = c.s; }
     }
   }
+  if (time) *time = least;
   return best;
+}
+// Row blocks that dx's sums have place for: four splits where there are few of them.
+int sums_room(int64_t blocks, int64_t across, int64_t clusters) { return (int)(blocks + 4 * clusters / across); }
+// One shape for dx and dweight in one list, where that takes no longer than two launches with a shape for each.
+bool shape_of_both(int64_t rows, int64_t features, int64_t classes, int64_t piece, int parts, int sms, double apart, TileShape* to) {
+  double least = apart;
+  bool found = false;
+  for (int i = 0; i < 3; ++i) {
+    const CostedShape c = costed_shape(i, parts);
+    const int64_t across = (features + c.s.cols - 1) / c.s.cols, down = 128 * c.s.cg;
+    const int64_t blocks = (rows + down - 1) / down;
+    const Product q = {(int)blocks, (int)across, sms / c.s.cg, (int)piece, sums_room(blocks, across, sms / c.s.cg), (int)((std::min(piece, classes) + down - 1) / down * across), (int)rows};
+    const double t = c.cost * q.time(q.splits());
+    if (t <= least) { least = t; *to = c.s; found = true; }
+  }
+  return found;
 }
 
 struct CePlan {
@@ -786,7 +890,8 @@ struct CePlan {
   int64_t rows;                      // room for gathered rows
   bool copy_w;
   TileShape z, dx, dw;
-  int piece, pieces, p_pitch;        // classes of a piece
+  Pieces pieces;
+  bool both;                         // dx and dweight in one list
   int sums_pitch, dx_room;
   size_t dw_sums;
   // offsets
@@ -798,7 +903,7 @@ struct CePlan {
 };
 
 // Classes of a piece, in blocks of 256: as many as the bytes allow, or fewer where the tiles of its products then come out as
-// whole waves.  Time in units of a tile's k: waves of p, of dweight, of dx (in splits), and what three more launches cost.
+// whole waves.  Time in units of a tile's k: waves of p, the list of dx and dweight, and what two more launches cost.
 // 8192 rows of 768, 30522 classes: 24 blocks at a time instead of 60, 72 tiles of dweight on 74 pairs instead of 180.
 int piece_blocks(const sae_linear_ce_desc* d, int64_t rows, int parts, int sms) {
   const int64_t all = (d->classes + 255) / 256, most = std::max<int64_t>(1, std::min(all, CE_PIECE_BYTES / (rows * 2 * parts) / 256));
@@ -807,10 +912,9 @@ int piece_blocks(const sae_linear_ce_desc* d, int64_t rows, int parts, int sms) 
   int64_t best = most;
   double least = 0;
   for (int64_t b = most; b >= std::max<int64_t>(1, most / 4); --b) {
-    const int s = dx_splits((int)down, (int)across, (int)units, (int)(256 * b), 8);
-    const double dx = dx_time((int)down, (int)across, (int)units, (int)(256 * b), s);
+    const Product q = {(int)down, (int)across, (int)units, (int)(256 * b), sums_room(down, across, units), (int)(b * across), (int)d->rows};
     const double pieces = (double)((all + b - 1) / b);
-    const double t = pieces * (parts * (waves(down * b) * (double)d->features + waves(b * across) * (double)d->rows + dx) + 2500.0);
+    const double t = pieces * (parts * (waves(down * b) * (double)d->features + q.time(q.splits())) + 1700.0);
     if (least == 0 || t < 0.99 * least) { least = t; best = b; }
   }
   return (int)best;
@@ -831,7 +935,7 @@ CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward,
     const int64_t n = std::max<int64_t>(1, d->rows);
     p.index = take(n * 4);
     p.at = take(n * 4);
-    p.counted = take(8);
+    p.counted = take(COUNT_WORDS * 4);
     p.before = take(d->rows > CE_SCAN_ROWS ? up(d->rows, CE_COUNT_ROWS) / CE_COUNT_ROWS * 4 : 0);
     p.z_pitch = (int)up(d->classes, 4);
     p.z_splits = float_splits((d->classes + CF_COLS - 1) / CF_COLS, d->features, 8, sms);
@@ -857,7 +961,7 @@ CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward,
   p.bias = take(d->has_bias ? up(d->classes, 256) * 4 + 1024 : 0);
   p.index = take(p.rows * 4);
   p.at = take(p.rows * 4);
-  p.counted = take(8);
+  p.counted = take(COUNT_WORDS * 4);
   p.before = take(d->rows > CE_SCAN_ROWS ? up(d->rows, CE_COUNT_ROWS) / CE_COUNT_ROWS * 4 : 0);
   p.z = tile_shape(d->rows, d->classes, d->features, 1, p.parts, sms);
   if (!backward) {
@@ -871,23 +975,26 @@ CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward,
     p.g = take(p.rows * 4);
     p.alpha = take(4);
     p.top = take(4);
-    p.piece = 256 * piece_blocks(d, p.rows, p.parts, sms);
-    p.pieces = (int)((d->classes + p.piece - 1) / p.piece);
-    p.p_pitch = p.piece;
-    p.dx = tile_shape(d->rows, d->features, p.piece, 8, p.parts, sms);
-    p.dw = tile_shape(std::min<int64_t>(p.piece, d->classes), d->features, d->rows, 1, p.parts, sms);
-    p.sums_pitch = (int)up(d->features, 32);
-    const int rows = 128 * p.dx.cg, across = (int)up(d->features, p.dx.cols) / p.dx.cols, clusters = sms / p.dx.cg;
-    p.dx_room = (int)(up(p.rows, rows) / rows) + 4 * clusters / across;
-    p.p = take((int64_t)p.parts * p.rows * p.p_pitch * 2);
-    p.bias_sums = take(d->has_bias ? p.rows / 32 * p.p_pitch * 4 : 0);
-    p.dx_sums = take((int64_t)p.dx_room * rows * p.sums_pitch * 4);
+    const int piece = 256 * piece_blocks(d, p.rows, p.parts, sms);
+    double dx_time = 0, dw_time = 0;
+    p.dx = tile_shape(d->rows, d->features, piece, 8, p.parts, sms, &dx_time);
+    p.dw = tile_shape(std::min<int64_t>(piece, d->classes), d->features, d->rows, 1, p.parts, sms, &dw_time);
     // A head of few classes has a tile or two of dweight, and all rows to add up in it (16384 x 64 x 10 float: 470 us on one SM).  In two
     // launches more where that leaves half of the SMs idle; no split of less than 512 rows.
-    const int dw_rows = 128 * p.dw.cg;
-    const int64_t dw_tiles = up(p.piece, dw_rows) / dw_rows * (up(d->features, p.dw.cols) / p.dw.cols);
+    const int64_t dw_tiles = up(piece, 128 * p.dw.cg) / (128 * p.dw.cg) * (up(d->features, p.dw.cols) / p.dw.cols);
     p.dw_splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(sms / p.dw.cg / dw_tiles, d->rows / 512), 32));
-    p.dw_sums = take(p.dw_splits > 1 ? (int64_t)p.dw_splits * up(p.piece, dw_rows) * p.sums_pitch * 4 : 0);
+    TileShape one;
+    p.both = p.dw_splits == 1 && shape_of_both(d->rows, d->features, d->classes, piece, p.parts, sms, dx_time + dw_time + 800.0, &one);
+    if (p.both) p.dx = p.dw = one;
+    p.pieces = {piece, (int)((d->classes + piece - 1) / piece), (int)d->classes, 1, p.rows};
+    if (p.dw_splits == 1) p.pieces.most = std::min(CE_WIDER, p.pieces.number);
+    p.sums_pitch = (int)up(d->features, 32);
+    const int rows = 128 * p.dx.cg, across = (int)up(d->features, p.dx.cols) / p.dx.cols, clusters = sms / p.dx.cg;
+    p.dx_room = sums_room(up(p.rows, rows) / rows, across, clusters);
+    p.p = take((int64_t)p.parts * p.rows * piece * 2);
+    p.bias_sums = take(d->has_bias ? p.rows / 32 * piece * 4 : 0);
+    p.dx_sums = take((int64_t)p.dx_room * rows * p.sums_pitch * 4);
+    p.dw_sums = take(p.dw_splits > 1 ? (int64_t)p.dw_splits * up(piece, 128 * p.dw.cg) * p.sums_pitch * 4 : 0);
   }
   p.bytes = at;
   return p;
@@ -926,19 +1033,25 @@ mma::Segments segments(int parts) {
   return parts == 1 ? one : three;
 }
 
-RowsArgs rows_args(const sae_linear_ce_desc* d, const CePlan& p, const void* x, const void* w, const void* bias, const int64_t* target, char* ws) {
+RowsArgs rows_args(const sae_linear_ce_desc* d, const CePlan& p, const void* x, const void* w, const void* bias, const int64_t* target, char* ws, int sms) {
   RowsArgs a = {};
   a.x = x; a.target = target; a.x_pitch = d->x_pitch; a.rows = d->rows; a.ignore = d->ignore_index;
   a.type = d->type; a.parts = p.parts; a.features = (int)d->features; a.classes = (int)d->classes; a.pitch = p.pitch;
   a.xg = p.in_float ? nullptr : (unsigned short*)(ws + p.xg);      // (float arithmetic reads rows where they are)
   a.xg_plane = p.rows * p.pitch;
-  a.index = (int*)(ws + p.index); a.at = (int*)(ws + p.at); a.counted = (int*)(ws + p.counted); a.ticket = (unsigned*)(ws + p.counted + 4);
+  a.index = (int*)(ws + p.index); a.at = (int*)(ws + p.at); a.counted = (int*)(ws + p.counted);
   a.w = w; a.w_pitch = d->weight_pitch; a.wg = (unsigned short*)(ws + p.wg); a.wg_plane = d->classes * p.pitch;
   a.bias = bias; a.bias_type = d->bias_type; a.bias_out = (float*)(ws + p.bias);
   a.bias_room = d->has_bias && !p.in_float ? (int)up(d->classes, 256) : 0;
   a.row_blocks = (int)std::max<int64_t>(1, up(d->rows, CE_ROWS) / CE_ROWS);
   a.w_blocks = p.copy_w && !p.in_float ? (int)(up(d->classes * (p.pitch / UNIT), CE_CHUNK) / CE_CHUNK) : 0;
   a.reduction = d->reduction;
+  if (!p.in_float && p.pieces.number) {            // backwards
+    a.pieces = p.pieces;
+    a.product_rows = 128 * p.dx.cg;
+    a.product.across = (int)(up(d->features, p.dx.cols) / p.dx.cols); a.product.clusters = sms / p.dx.cg; a.product.room = p.dx_room;
+    a.both = p.both;
+  }
   return a;
 }
 
@@ -1003,7 +1116,7 @@ FloatRowArgs float_rows(const sae_linear_ce_desc* d, const CePlan& p, const Rows
   FloatRowArgs r = {};
   r.z = (const float*)(ws + p.fz); r.bias = a.bias; r.index = a.index; r.at = a.at; r.counted = a.counted;
   r.room = std::max<int64_t>(1, d->rows); r.splits = p.z_splits; r.pitch = p.z_pitch; r.classes = a.classes; r.bias_type = a.bias_type; r.reduction = d->reduction;
-  r.sums = (double*)(ws + p.sums); r.ticket = a.ticket;
+  r.sums = (double*)(ws + p.sums); r.ticket = (unsigned*)a.counted + COUNT_TICKET;
   return r;
 }
 
@@ -1087,7 +1200,7 @@ int sae_linear_ce_forward(const sae_linear_ce_desc* d, const void* x, const void
   if (workspace_bytes < p.bytes) return SAE_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
   char* ws = (char*)workspace;
-  RowsArgs a = rows_args(d, p, x, weight, d->has_bias ? bias : nullptr, target, ws);
+  RowsArgs a = rows_args(d, p, x, weight, d->has_bias ? bias : nullptr, target, ws, sms);
   a.count = count; a.lse = lse; a.loss = d->reduction == SAE_REDUCE_NONE ? loss : nullptr;
   if (p.in_float) return float_forward(d, p, a, loss, lse, ws, st);
   LossJob job = {};
@@ -1102,7 +1215,7 @@ int sae_linear_ce_forward(const sae_linear_ce_desc* d, const void* x, const void
   if (rc != SAE_OK) return rc;
   JoinArgs j = {};
   j.runs = job.runs; j.counted = a.counted; j.index = a.index; j.at = a.at; j.at_z = job.at_z; j.loss = loss; j.lse = lse; j.sums = (double*)(ws + p.sums);
-  j.ticket = a.ticket; j.rows = job.rows; j.wide = (int)wide; j.reduction = d->reduction;
+  j.ticket = (unsigned*)a.counted + COUNT_TICKET; j.rows = job.rows; j.wide = (int)wide; j.reduction = d->reduction;
   j.clusters = (int)std::min<int64_t>(std::max<int64_t>(1, tiles), sms / p.z.cg);
   return launch(k_ce_join, std::max<int64_t>(1, up(d->rows, CE_ROWS) / CE_ROWS), CE_THREADS, st, false, j);
 }
@@ -1122,7 +1235,7 @@ int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, cons
   cudaStream_t st = (cudaStream_t)stream;
   if (!dx && !dweight && !dbias) return SAE_OK;
   char* ws = (char*)workspace;
-  RowsArgs a = rows_args(d, p, x, weight, d->has_bias ? bias : nullptr, target, ws);
+  RowsArgs a = rows_args(d, p, x, weight, d->has_bias ? bias : nullptr, target, ws, sms);
   a.lse_in = lse; a.dloss = dloss; a.count_in = count; a.dx = dx;
   a.lse_g = (float*)(ws + p.lse_g); a.g = (float*)(ws + p.g); a.alpha = (float*)(ws + p.alpha);
   a.p_scale = d->type == SAE_TYPE_HALF ? 32768.0f : 1.0f;
@@ -1130,49 +1243,47 @@ int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, cons
   GradJob g = {};
   if (!maps(d, p, weight, ws, &g.x, &g.w)) return SAE_ERR_CUDA;
   const bool bfloat = d->type != SAE_TYPE_HALF;
-  CUtensorMap pm;
-  if (!mma::encode_map(&pm, ws + p.p, bfloat, p.p_pitch, p.rows, p.parts, p.p_pitch, p.rows * p.p_pitch)) return SAE_ERR_CUDA;
+  ProductJob job = {};
+  for (int i = 0; i < p.pieces.most; ++i)
+    if (!mma::encode_map(&job.p[i], ws + p.p, bfloat, (int64_t)p.pieces.piece * (i + 1), p.rows / (i + 1), p.parts, (int64_t)p.pieces.piece * (i + 1), p.rows * p.pieces.piece))
+      return SAE_ERR_CUDA;
   int rc = gather<true>(d, p, a, ws, st);
   g.cols = p.z.cols; g.bfloat = bfloat; g.seg = segments(p.parts);
   g.counted = a.counted; g.classes = a.classes; g.features = a.features; g.rows = 128 * p.z.cg;
   g.bias = d->has_bias ? a.bias_out : nullptr; g.lse = a.lse_g; g.g = a.g; g.at = a.at;
-  g.p = (unsigned short*)(ws + p.p); g.p_plane = p.rows * p.p_pitch; g.p_pitch = p.p_pitch; g.type = d->type;
+  g.p = (unsigned short*)(ws + p.p); g.p_plane = p.rows * p.pieces.piece; g.type = d->type; g.pieces = p.pieces;
   g.scaled = d->reduction == SAE_REDUCE_NONE || a.p_scale != 1.0f;
   g.bias_sums = dbias ? (float*)(ws + p.bias_sums) : nullptr;
-  ProductJob job = {};
-  job.bfloat = bfloat; job.seg = g.seg; job.a = pm; job.counted = a.counted; job.features = a.features; job.alpha = a.alpha; job.type = d->type;
-  const int clusters = sms / p.dx.cg, dx_across = (int)(up(d->features, p.dx.cols) / p.dx.cols);
-  for (int i = 0; i < p.pieces && rc == SAE_OK; ++i) {
-    const int start = i * p.piece, classes = (int)std::min<int64_t>(p.piece, d->classes - start);
-    g.start = start;
-    g.tiles = (classes + g.cols - 1) / g.cols;
-    const int64_t z_tiles = up(d->rows, g.rows) / g.rows * g.tiles;
+  job.bfloat = bfloat; job.seg = g.seg; job.w = g.w; job.x = g.x; job.counted = a.counted; job.pieces = p.pieces; job.features = a.features; job.classes = a.classes;
+  job.dx_sums = (float*)(ws + p.dx_sums); job.dw_sums = (float*)(ws + p.dw_sums); job.sums_pitch = p.sums_pitch; job.dw_splits = p.dw_splits;
+  job.out = dweight; job.type = d->type; job.alpha = a.alpha; job.whole_rows = aligned_to(dweight, 32) && d->features * es % 32 == 0;
+  const auto across = [&](const TileShape& s) { return (int)(up(d->features, s.cols) / s.cols); };
+  // (launches are sized for all rows and for pieces of any width)
+  const auto product = [&](const TileShape& s, bool for_x, bool for_weight) {
+    job.cols = s.cols; job.rows = 128 * s.cg; job.across = across(s); job.dx = for_x; job.dweight = for_weight;
+    const int64_t classes = std::min<int64_t>((int64_t)p.pieces.piece * p.pieces.most, d->classes);
+    return products(job, s, for_x ? sms : up(classes, job.rows) / job.rows * job.across * p.dw_splits, sms, st);
+  };
+  const bool want_x = dx && d->rows, both = p.both && want_x && dweight;
+  for (int i = 0; i < p.pieces.number && rc == SAE_OK; ++i) {
+    g.index = job.index = i;
+    const int64_t z_tiles = up(d->rows, g.rows) / g.rows * (up(std::min<int64_t>((int64_t)p.pieces.piece * p.pieces.most, d->classes), g.cols) / g.cols);
     if (z_tiles) rc = products(g, p.z, z_tiles, sms, st);
-    job.start = start;
-    job.classes = classes;
-    job.width = classes;
     if (dbias && rc == SAE_OK)
-      rc = launch(k_ce_dbias, (classes + 31) / 32, CE_THREADS, st, false, (const float*)g.bias_sums, p.p_pitch, (const int*)a.counted, (const float*)a.alpha, classes, d->bias_type,
-                  (void*)((char*)dbias + (int64_t)start * bs));
-    if (dx && d->rows && rc == SAE_OK) {
-      job.dx = true; job.b = g.w; job.cols = p.dx.cols; job.rows = 128 * p.dx.cg; job.across = dx_across;
-      job.sums = (float*)(ws + p.dx_sums); job.sums_pitch = p.sums_pitch; job.room = p.dx_room; job.depth = p.piece; job.add = i > 0;
-      rc = products(job, p.dx, clusters, sms, st);
-    }
-    if (dweight && rc == SAE_OK) {
-      job.dx = false; job.b = g.x; job.cols = p.dw.cols; job.rows = 128 * p.dw.cg; job.across = (int)(up(d->features, p.dw.cols) / p.dw.cols);
-      job.out = dweight;
-      job.dw_splits = p.dw_splits; job.sums = (float*)(ws + p.dw_sums); job.sums_pitch = p.sums_pitch; job.add = 0;
-      job.whole_rows = aligned_to(dweight, 32) && d->features * es % 32 == 0;
-      rc = products(job, p.dw, up(classes, job.rows) / job.rows * job.across * p.dw_splits, sms, st);
+      rc = launch(k_ce_dbias, (p.pieces.piece + 31) / 32, CE_THREADS, st, false, (const float*)g.bias_sums, p.pieces, i, (const int*)a.counted, (const float*)a.alpha, d->bias_type, dbias);
+    if (both && rc == SAE_OK) rc = product(p.dx, true, true);
+    if (!both && want_x && rc == SAE_OK) rc = product(p.dx, true, false);
+    if (!both && dweight && rc == SAE_OK) {
+      rc = product(p.dw, false, true);
       if (rc == SAE_OK && p.dw_splits > 1) {
-        DxArgs x1 = {job.sums, a.counted, nullptr, a.alpha, (char*)dweight + (int64_t)start * d->features * es, p.sums_pitch, a.features, d->type, job.rows, 0, 0, 0, 0, classes, p.dw_splits};
+        const int start = i * p.pieces.piece, classes = std::min(p.pieces.piece, a.classes - start);
+        DxArgs x1 = {job.dw_sums, a.counted, nullptr, a.alpha, (char*)dweight + (int64_t)start * d->features * es, p.sums_pitch, a.features, d->type, job.rows, classes, p.dw_splits};
         rc = launch(k_ce_dx, (unsigned)(up((int64_t)classes * ((d->features + UNIT - 1) / UNIT), CE_THREADS) / CE_THREADS), CE_THREADS, st, false, x1);
       }
     }
   }
-  if (dx && d->rows && rc == SAE_OK) {
-    DxArgs x2 = {(const float*)(ws + p.dx_sums), a.counted, a.index, a.alpha, dx, p.sums_pitch, a.features, d->type, 128 * p.dx.cg, dx_across, clusters, p.piece, p.dx_room, 0, 0};
+  if (want_x && rc == SAE_OK) {
+    DxArgs x2 = {job.dx_sums, a.counted, a.index, a.alpha, dx, p.sums_pitch, a.features, d->type, 128 * p.dx.cg, 0, 0};
     rc = launch(k_ce_dx, (unsigned)(up(d->rows * ((d->features + UNIT - 1) / UNIT), CE_THREADS) / CE_THREADS), CE_THREADS, st, false, x2);
   }
   return rc;
