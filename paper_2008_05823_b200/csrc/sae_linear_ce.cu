@@ -313,6 +313,7 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_rows(const __grid_constant__ 
 // Runs of tiles: row blocks one after another, each over all classes; a cluster takes an equal share of this list and leaves one run
 // (maximum, sum) for each row block that it touches.
 struct LossJob : mma::Plain {
+  static constexpr bool LONG = true;
   int cols;
   bool bfloat;
   mma::Segments seg;

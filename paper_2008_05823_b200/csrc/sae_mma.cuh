@@ -55,8 +55,9 @@ struct Room {
 constexpr u32 TMEM_COLUMNS = 512;
 constexpr u64 WAIT_NS = 2000000000ull, DRAIN_NS = 100000000ull;
 constexpr int MAX_SEGMENTS = 6;
-constexpr int JOIN_BLOCKS = 64 / BLOCK_K;
-constexpr u32 HELD_COLUMN = 384;
+// Blocks of k after which sums are taken out and joined, rounded to nearest: sums of several parts, and long sums of one (Job::LONG).  The tensor
+// cores truncate a sum at every 16 k: by 4e-6 of a loss at 4096 features, 6e-7 with joins (loss of 2048 x 4096 x 32000 418 us, 477 with).
+constexpr int JOIN_PARTS = 1, JOIN_LONG = 8, JOIN_FROM = 768;      // (sums of up to JOIN_FROM k are as exact as joined ones of 4096)
 
 struct Segments {
   int n;
@@ -274,8 +275,9 @@ __device__ __forceinline__ int epilogue_width(int cols) { return cols / 2; }
 //      REPORTS: tiles depend on one another.  A warp of its own, the last, runs ahead with ready(local, t, dead), which waits until a tile's
 //      operands are there (false: gave up); report(local, t) is called by warp 2 when the block has written its part of a
 //      tile.  Both wait a microsecond or two for the memory; with the loading warps waiting themselves, 12 encoder layers took 1702 us, not 1601.
-// JOINED: sums are taken out every JOIN_BLOCKS blocks of k (job.cols <= 128).
-template <class Job, int CG, bool JOINED>
+// JOIN: sums are taken out after so many blocks of k and held (0: not).  Up to 128 columns there is room for two sums beside the held ones;
+// of 256 columns there is one, taken out for good before the next tile's first block of k, and the epilogue reads the held ones.
+template <class Job, int CG, int JOIN>
 __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid_constant__ Job job) {
   constexpr int STAGES = Room<Job>::STAGES;
   extern __shared__ unsigned char smem_raw[];
@@ -304,6 +306,8 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
   const u32 tmem = ctl.tmem;
   typename Job::Local local = job.begin(shared, cluster, clusters);
   const int b_rows = job.cols / CG;               // rows of B that a block loads
+  const bool single = JOIN > 1 && job.cols > 128;
+  const u32 buffers = single ? 0 : 1;             // (a mask)
 
   if (warp == 0 || warp == 3) {
     const u32 bytes = CG * (2 * BOX_BYTES + (u32)b_rows * BLOCK_K * 2);
@@ -314,9 +318,9 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
       if constexpr (Job::REPORTS) {
         if (!__all_sync(0xffffffffu, wait_shared(&ctl.ready, (u32)i + 1, &ctl.dead))) { ok = false; break; }
       }
-      const int a_row = t.a_row + (int)rank * 128, b_row = t.b_row + (int)rank * b_rows, run = JOINED ? JOIN_BLOCKS : t.blocks;
+      const int a_row = t.a_row + (int)rank * 128, b_row = t.b_row + (int)rank * b_rows, run = JOIN ? JOIN : t.blocks;
       for (int k0 = 0; k0 < t.blocks && ok; k0 += run) {
-        const int k1 = JOINED ? min(k0 + run, t.blocks) : t.blocks;
+        const int k1 = JOIN ? min(k0 + run, t.blocks) : t.blocks;
         for (int s = 0; s < job.seg.n && ok; ++s) {
           const int za = t.a_plane + job.seg.a[s], zb = t.b_plane + job.seg.b[s];
           for (int kb = k0; kb < k1; ++kb, ++n) {
@@ -354,9 +358,9 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
     for (int i = 0; ok && job.tile(local, i, t); ++i) {
       int left = t.blocks;
       do {
-        const int blocks = JOINED ? min(left, JOIN_BLOCKS) : left;
-        const u32 buf = taken & 1;
-        if (!__all_sync(0xffffffffu, wait(&ctl.acc_empty[buf], ((taken >> 1) & 1) ^ 1, &ctl.dead))) { ok = false; break; }
+        const int blocks = JOIN ? min(left, JOIN) : left;
+        const u32 buf = taken & buffers;
+        if (!__all_sync(0xffffffffu, wait(&ctl.acc_empty[buf], ((taken >> buffers) & 1) ^ 1, &ctl.dead))) { ok = false; break; }
         fence_after();
         const u32 acc = tmem + buf * 256;
         u32 add = 0;
@@ -366,7 +370,7 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
           if (!__all_sync(0xffffffffu, wait(&ctl.full[stage], (n / STAGES) & 1, &ctl.dead))) { ok = false; break; }
           fence_after();
           const u32 at = tiles + stage * STAGE_BYTES;
-          const int kb = k0 + (JOINED && JOIN_BLOCKS == 1 ? 0 : (JOINED ? j % blocks : j));
+          const int kb = k0 + (JOIN == 1 ? 0 : j);        // (several segments: no join, or one after each block)
           const bool a_rows_first = t.a_rows_first != (kb < t.a_turn), b_rows_first = t.b_rows_first != (kb < t.b_turn);
           const u32 idesc = instruction(128 * CG, job.cols, job.bfloat, a_rows_first, b_rows_first);
           const u32 a_step = (a_rows_first ? 2048 : 32) >> 4, b_step = (b_rows_first ? 2048 : 32) >> 4;
@@ -418,21 +422,25 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
       int left = t.blocks;
       bool first = true;
       for (;;) {
-        const u32 buf = taken & 1;
-        if (ok && !wait(&ctl.acc_full[buf], (taken >> 1) & 1, &ctl.dead)) ok = false;
+        const u32 buf = taken & buffers;
+        if (ok && !wait(&ctl.acc_full[buf], (taken >> buffers) & 1, &ctl.dead)) ok = false;
         ok = __all_sync(0xffffffffu, ok);
         fence_after();
-        const bool last = !JOINED || left <= JOIN_BLOCKS || !ok;
-        Sums s = {!ok ? SUMS_NAN : job.seg.n * t.blocks == 0 ? SUMS_ZERO : first ? SUMS_HELD : SUMS_JOINED, lanes + buf * 256, lanes + HELD_COLUMN};
-        if (last) epi.tile(t, s);
-        else if constexpr (JOINED) {
-          const int width = epilogue_width(job.cols);
-          for (int c = part * width; c < (part + 1) * width; c += 32) {
-            float v[32];
-            sums_of(s, c, v);
-            tmem_store(s.held + (u32)c, v);
+        const bool last = !JOIN || left <= JOIN || !ok;
+        const u32 held = lanes + (single ? 256 : 384);
+        Sums s = {!ok ? SUMS_NAN : job.seg.n * t.blocks == 0 ? SUMS_ZERO : first ? SUMS_HELD : SUMS_JOINED, lanes + buf * 256, held};
+        const bool join = JOIN && s.state <= SUMS_JOINED && (single || !last);
+        if constexpr (JOIN > 0) {
+          if (join) {
+            const int width = epilogue_width(job.cols);
+            for (int c = part * width; c < (part + 1) * width; c += 32) {
+              float v[32];
+              sums_of(s, c, v);
+              tmem_store(s.held + (u32)c, v);
+            }
           }
         }
+        if (last && !join) epi.tile(t, s);
         fence_before();
         __syncwarp();
         if (lane == 0 && ok) {
@@ -440,6 +448,7 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
           if constexpr (CG == 2) arrive_cluster(of_block0(bar));
           else mbar_arrive(&ctl.acc_empty[buf]);
         }
+        if (JOIN > 1 && last && join) epi.tile(t, {SUMS_HELD, held, held});
         if constexpr (Job::REPORTS) {
           if (last) {
             __syncwarp();
@@ -449,7 +458,7 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
         ++taken;
         if (last) break;
         first = false;
-        left -= JOIN_BLOCKS;
+        left -= JOIN;
       }
     }
     epi.finish();
@@ -572,7 +581,7 @@ inline bool encode_map(CUtensorMap* map, const void* base, bool bfloat, int64_t 
                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class Job, int CG, bool JOINED>
+template <class Job, int CG, int JOIN>
 cudaError_t launch_products(const Job& job, int blocks, cudaStream_t st, bool together) {
   // the attribute belongs to a device's context: set once for each
   static std::atomic<unsigned long long> ready{0};
@@ -581,7 +590,7 @@ cudaError_t launch_products(const Job& job, int blocks, cudaStream_t st, bool to
   if (e != cudaSuccess) return e;
   const unsigned long long bit = device < 64 ? 1ull << device : 0;
   if (!(ready.load(std::memory_order_acquire) & bit)) {
-    e = cudaFuncSetAttribute(k_products<Job, CG, JOINED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Room<Job>::BYTES);
+    e = cudaFuncSetAttribute(k_products<Job, CG, JOIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Room<Job>::BYTES);
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_release);
   }
@@ -597,21 +606,26 @@ cudaError_t launch_products(const Job& job, int blocks, cudaStream_t st, bool to
   else { at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization; at[n].val.programmaticStreamSerializationAllowed = 1; ++n; }
   cfg.attrs = at;
   cfg.numAttrs = (unsigned)n;
-  return cudaLaunchKernelEx(&cfg, k_products<Job, CG, JOINED>, job);
+  return cudaLaunchKernelEx(&cfg, k_products<Job, CG, JOIN>, job);
 }
 
 // together: blocks wait for one another, so all of them have to run at once.  Otherwise the kernel may start while the one before it
 // still runs.  Sums of several parts are joined on the way.
 template <class Job>
 cudaError_t launch_products(const Job& job, int cg, int tiles_at_once, cudaStream_t st, bool together = false) {
-  if (job.seg.n > 1) return cg == 2 ? launch_products<Job, 2, true>(job, 2 * tiles_at_once, st, together) : launch_products<Job, 1, true>(job, tiles_at_once, st, together);
-  return cg == 2 ? launch_products<Job, 2, false>(job, 2 * tiles_at_once, st, together) : launch_products<Job, 1, false>(job, tiles_at_once, st, together);
+  const auto with = [&](auto join) {
+    return cg == 2 ? launch_products<Job, 2, decltype(join)::value>(job, 2 * tiles_at_once, st, together) : launch_products<Job, 1, decltype(join)::value>(job, tiles_at_once, st, together);
+  };
+  if (job.seg.n > 1) return with(std::integral_constant<int, JOIN_PARTS>());
+  if constexpr (Job::LONG)
+    if (job.features > JOIN_FROM) return with(std::integral_constant<int, JOIN_LONG>());
+  return with(std::integral_constant<int, 0>());
 }
 
 // For jobs whose operands are there before the kernel runs, and that look up nothing.
 struct Plain {
   static constexpr int STAGING = 0;
-  static constexpr bool REPORTS = false;
+  static constexpr bool REPORTS = false, LONG = false;
   struct Shared {};
   __device__ __forceinline__ void fill(Shared&) const {}
 };

@@ -156,7 +156,7 @@ enum Phase { PHASE_S, PHASE_B, PHASE_X };
 struct Factors { float s_sum, b_diag, b_own, b_sum, x_own, x_sum; };
 
 struct OrthoJob {
-  static constexpr bool REPORTS = true;
+  static constexpr bool REPORTS = true, LONG = false;
   static constexpr int STAGING = 32 * 256;      // 32 rows of 128 elements
   int cols;
   bool bfloat;

@@ -178,9 +178,11 @@ def test_values_and_gradients(n, d, v, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,n,d,v,ignored", [("bf16", 4096, 256, 9000, 0.0), ("bf16", 20000, 64, 3000, 0.85), ("f16", 3000, 640, 7001, 0.1),
-                                                 ("f32", 2000, 256, 3000, 0.2), ("bf16", 40000, 32, 300, 0.5), ("bf16", 9000, 128, 20000, 0.0)])
+                                                 ("f32", 2000, 256, 3000, 0.2), ("bf16", 40000, 32, 300, 0.5), ("bf16", 9000, 128, 20000, 0.0),
+                                                 ("bf16", 2500, 1100, 9000, 0.1), ("f16", 1500, 2048, 12000, 0.0), ("bf16", 16384, 96, 9000, 0.97)])
 def test_large(dtype, n, d, v, ignored):
-    """Pairs of blocks with one tile, several pieces of the classes, rows counted in two steps."""
+    """Pairs of blocks with one tile, several pieces of the classes, pieces wider for fewer rows, rows counted in two steps, sums long enough
+    to be joined."""
     x, w, t, b = data(n, d, v, DTYPES[dtype], dtype != "bf16", ignored, seed=3)
     check(x, w, t, b, "mean", torch.tensor(1.0, device="cuda"))
 
