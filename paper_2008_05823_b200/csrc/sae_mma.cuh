@@ -74,7 +74,7 @@ struct Tile {
   int a_turn, b_turn;      // this many first blocks of k come from the transpose instead: (row, k) from (k, row), the other of K and rows first
   // for the epilogue
   int row, col;            // first output row and column
-  int group, item;
+  int group, item, part;
 };
 
 // Where a tile's sums are: in tensor memory, there in two places to be added, all zero, or lost.
@@ -490,6 +490,13 @@ __device__ __forceinline__ void load_words(const void* from, u32 (&w)[16]) {
 #pragma unroll
   for (int i = 0; i < 16; i += 8)
     asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7]) : "l"((const char*)from + i * 4)
+                 : "memory");
+}
+// The same past L1, which does not see what other SMs have written during the kernel.
+__device__ __forceinline__ void load_written(const void* from, u32 (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; i += 8)
+    asm volatile("ld.relaxed.gpu.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7]) : "l"((const char*)from + i * 4)
                  : "memory");
 }
 // Rows of 16-byte pieces in shared memory, `wide` (a power of two, 4 at least) a row.  Pieces change places with the row, so that a lane

@@ -42,6 +42,7 @@ constexpr int OT_CHUNK = 2048;                // units of a row that a block tak
 constexpr int64_t OT_PORTION = 512ll << 20;
 constexpr int OT_ARGS = 448;                  // matrices whose addresses travel as kernel arguments
 
+constexpr int OT_SPLITS = 16;                 // of S's sums
 constexpr int OT_SHAPES = 32, OT_BATCHES = 800;   // as many are looked up in shared memory
 constexpr int OT_STEPS = 64;
 
@@ -56,11 +57,17 @@ struct Shape {
   int x_tiles, x_tile_cols, s_tiles;          // tiles of one matrix's products
   int first;                                  // its first matrix in the class's order
 };
+// Of a shape whose S has too few tiles, and is made in parts.
+struct Parts {
+  int n;                                      // of k
+  float* sums;                                // [matrix][s_tile][n][rows of a tile][columns]
+  u32* arrived;                               // [matrix][s_tile][16]: parts that the warp of this place has written
+};
 // One product of some neighbouring matrices of a shape: tiles begin .. end - 1 of the list.
 struct Batch { int begin, end, first; u32 shape : 24, phase : 2, step : 6; };     // (up to 2^20 shapes, 64 steps)
 
 struct Matrix { const void* in; void* out; long long in_ld, out_ld; };
-struct Place { int rows, cols, x_pitch, in_type, out_type, first_chunk, chunks; __half* x; long long x_plane; u32* done; float* ratio; int plain; };
+struct Place { int rows, cols, x_pitch, in_type, out_type, first_chunk, chunks; __half* x; long long x_plane; u32 *done, *arrived; int num_arrived; float* ratio; int plain; };
 struct Chunk { int matrix, unit; };
 
 struct Table { int n; Matrix m[OT_ARGS]; };
@@ -118,7 +125,10 @@ __global__ void __launch_bounds__(OT_THREADS) k_ortho_split(const Matrix* mats, 
   const Place p = places[ch.matrix];
   mma::wait_for_previous();
   const Matrix m = mats[ch.matrix];
-  if (ch.unit == 0 && threadIdx.x == 0) *p.done = 0;
+  if (ch.unit == 0) {
+    if (threadIdx.x == 0) *p.done = 0;
+    for (int i = threadIdx.x; i < p.num_arrived; i += OT_THREADS) p.arrived[i] = 0;
+  }
   double s = 0;
   for (int i = threadIdx.x; i < p.chunks; i += OT_THREADS) s += sums[p.first_chunk + i];
   // 16-bit elements times a power of two are float16 exactly (but for what is 2^-25 of the norm); the rest of the factor, from 1/2
@@ -155,6 +165,54 @@ enum Phase { PHASE_S, PHASE_B, PHASE_X };
 // S = s_sum acc;  B = b_diag 1 + b_own S + b_sum acc;  x = x_own lo + x_sum acc
 struct Factors { float s_sum, b_diag, b_own, b_sum, x_own, x_sum; };
 
+// A part of S's sums: left in memory, and the warp that finds itself the last of its place in the tile adds all parts up in their order, the same bits
+// whoever that is, and writes S.
+__device__ __forceinline__ void join_sums(const Shape& g, const Parts& parts_of, const mma::Tile& t, const mma::Sums sums, int tile_rows, int tile_cols, int row, int half, int chunks, float scale) {
+  const int split = t.part / g.s_tiles, q = t.part - split * g.s_tiles, first = half * mma::epilogue_width(tile_cols), next = tile_rows * tile_cols, r = t.row + row;
+  const long long tile = (long long)t.item * g.s_tiles + q;
+  float* const parts = parts_of.sums + (tile * parts_of.n * tile_rows + row) * tile_cols + first;
+  const bool there = r < g.small;
+  for (int k = 0; k < chunks; ++k) {
+    float v[32];
+    __syncwarp();
+    mma::sums_of(sums, first + k * 32, v);
+    if (there) mma::store_row(parts + (long long)split * next + k * 32, v, 32);
+  }
+  __threadfence();
+  __syncwarp();
+  u32* const arrived = parts_of.arrived + tile * 16 + (row >> 5) * 2 + half;
+  u32 before = 0;
+  if ((threadIdx.x & 31) == 0) before = atomicAdd(arrived, 1u);
+  if (__shfl_sync(0xffffffffu, before, 0) + 1 != (u32)parts_of.n) return;
+  __threadfence();
+  if ((threadIdx.x & 31) == 0) *arrived = 0;               // for the next step
+  if (!there) return;
+  __half* const to = g.s + (t.item * (long long)g.s_parts) * g.s_plane + (long long)r * g.s_pitch + t.col + first;
+  for (int k = 0; k < chunks; ++k) {
+    float v[32] = {};
+#pragma unroll 2
+    for (int s = 0; s < parts_of.n; ++s) {
+      u32 w[2][16];
+      mma::load_written(parts + (long long)s * next + k * 32, w[0]);
+      mma::load_written(parts + (long long)s * next + k * 32 + 16, w[1]);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(w[i >> 4][i & 15]);
+    }
+    u32 hi[16], lo[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float x = v[2 * i] * scale, y = v[2 * i + 1] * scale;
+      hi[i] = mma::pack_half(x, y);
+      const float2 h = mma::unpack_half(hi[i]);
+      lo[i] = mma::pack_half(x - h.x, y - h.y);
+    }
+    mma::store_words(to + k * 32, hi);
+    if (g.s_parts > 1) mma::store_words(to + g.s_plane + k * 32, lo);
+  }
+}
+
+// SPLIT: some shape's S is made in parts (a kernel of its own: asking took 15 products of 512 x 512 3 % longer).
+template <bool SPLIT>
 struct OrthoJob {
   static constexpr bool REPORTS = true, LONG = false;
   static constexpr int STAGING = 32 * 256;      // 32 rows of 128 elements
@@ -163,6 +221,7 @@ struct OrthoJob {
   mma::Segments seg;
   const Maps* maps;
   const Shape* shapes;
+  const Parts* parts;             // of S
   const Batch* batches;
   int num_shapes, num_batches, total, rows, steps, arrivals;   // rows of a tile; blocks that write one
   u32* done;                        // in the class's order
@@ -202,7 +261,10 @@ struct OrthoJob {
     const Shape& g = l.shapes[b.shape];
     const Maps& m = maps[b.shape];
     const bool px = b.phase == PHASE_X;
-    const int per = px ? g.x_tiles : g.s_tiles, n = (w - b.begin) / per, q = (w - b.begin) - n * per;
+    const int splits = SPLIT && b.phase == PHASE_S ? parts[b.shape].n : 1, per = px ? g.x_tiles : g.s_tiles * splits, n = (w - b.begin) / per;
+    int q = (w - b.begin) - n * per, split = 0;
+    if (SPLIT) t.part = q;
+    if (SPLIT && splits > 1) { split = q / g.s_tiles; q -= split * g.s_tiles; }
     t.item = b.first + n;
     t.group = b.shape;
     int r, c;
@@ -234,13 +296,21 @@ struct OrthoJob {
       else t.a_turn = kept_from(t.row);
     }
     t.blocks = (k + mma::BLOCK_K - 1) / mma::BLOCK_K;
+    if (SPLIT && splits > 1) {
+      const int from = t.blocks * split / splits;
+      t.a_k = t.b_k = from * mma::BLOCK_K;
+      t.blocks = t.blocks * (split + 1) / splits - from;
+    }
     return true;
   }
   // Whether x has a lo when step s begins.  Where products read hi alone, the last step needs none: a rounding is multiplied by a at most there.
   __device__ __forceinline__ bool has_lo(const Shape& g, int s) const { return g.s_parts == 2 || (s ? s + 1 < steps : !g.plain); }
   // the matrix's counter, and what it shows when every product before this tile's is written
   __device__ __forceinline__ u32* counter(const Shape& g, const mma::Tile& t) const { return done + g.first + t.item; }
-  __device__ __forceinline__ u32 before(const Shape& g, const Batch& b) const { return (u32)((b.step * (2 * g.s_tiles + g.x_tiles) + b.phase * g.s_tiles) * arrivals); }
+  __device__ __forceinline__ u32 before(const Shape& g, const Batch& b) const {
+    const int s = SPLIT ? g.s_tiles * parts[b.shape].n : g.s_tiles;
+    return (u32)((b.step * (s + g.s_tiles + g.x_tiles) + (b.phase > PHASE_S ? s : 0) + (b.phase > PHASE_B ? g.s_tiles : 0)) * arrivals);
+  }
   __device__ __forceinline__ bool ready(const Local& l, const mma::Tile& t, u32* dead) const {
     const Shape& g = l.shapes[t.group];
     if (!mma::wait_counter(counter(g, t), before(g, *l.batch), dead)) return false;
@@ -308,6 +378,10 @@ struct OrthoJob {
         sum *= px ? ratio : ratio * ratio;
       }
       if (!here) sum = __int_as_float(0x7fc00000);
+      if (SPLIT && b.phase == PHASE_S && job.parts[b.shape].n > 1) {
+        join_sums(g, job.parts[b.shape], t, sums, job.rows, job.cols, row, part, chunks, sum);
+        return;
+      }
       const int lane_row = row & 31, rows = px ? g.rows : g.small, pitch = px ? g.x_pitch : g.s_pitch;
       const long long plane = px ? g.x_plane : g.s_plane;
       __half* const to = (px ? g.x[(b.step & 1) ^ 1] : b.phase == PHASE_B ? g.b : g.s) + t.item * (long long)(px ? 2 : g.s_parts) * plane + (long long)r * pitch;
@@ -399,6 +473,7 @@ struct Class {
   int parts, cg, cols;
   int first, n;                  // shapes
   int first_batch, batches, total;
+  bool split;                    // some S is made in parts
 };
 
 // The largest |p(v)| and |a + b v^2 + c v^4| over 0 <= v <= top.
@@ -427,6 +502,7 @@ struct sae_ortho {
   char* arena;
   Maps* maps;
   Shape* shapes;
+  Parts* parts;
   Batch* batches;
   u32* done;
   float* ratios;
@@ -435,6 +511,8 @@ struct sae_ortho {
   Chunk* chunk_list;
   int* order;
   double* sums;
+  float* split_sums;                             // of S, where it is made in parts
+  u32* arrived;
 };
 
 namespace {
@@ -446,7 +524,7 @@ int cuda_status(sae_ortho* h, cudaError_t e) {
 }
 
 void release(sae_ortho* h) {
-  cudaFree(h->arena); cudaFree(h->maps); cudaFree(h->shapes); cudaFree(h->batches); cudaFree(h->done); cudaFree(h->ratios); cudaFree(h->mats); cudaFree(h->places); cudaFree(h->chunk_list); cudaFree(h->order); cudaFree(h->sums);
+  cudaFree(h->arena); cudaFree(h->maps); cudaFree(h->shapes); cudaFree(h->parts); cudaFree(h->batches); cudaFree(h->done); cudaFree(h->ratios); cudaFree(h->mats); cudaFree(h->places); cudaFree(h->chunk_list); cudaFree(h->order); cudaFree(h->sums); cudaFree(h->split_sums); cudaFree(h->arrived);
   delete h;
 }
 
@@ -471,31 +549,59 @@ void count_tiles(Shape& g, int rows, int cols) {
   g.s_tiles = tiles_above(g.small, rows, cols);
 }
 
+// Parts of k that S's sums are made in, where a class has fewer tiles than SMs (or pairs): time in the units of choose_tiles.  A warp that joins
+// sums waits about 3 us, and 0.5 us for 32 columns of each part.
+int splits_of(const Class& c, const Shape& g, int64_t tiles, int units, int cols, double cost, double* time) {
+  const int k = g.tall ? g.rows : g.cols, most = (int)std::min<int64_t>(units / std::max<int64_t>(1, tiles), OT_SPLITS);
+  const double us = c.parts == 1 ? 400.0 : 130.0;
+  int best = 1;
+  *time = cost * k;
+  for (int s = 2; s <= most; ++s) {
+    const double t = cost * k / s + us * (3.0 + 0.5 * s * cols / 64);
+    if (t < *time) { *time = t; best = s; }
+  }
+  return best;
+}
+
 // Tile shape of a class: time in units of a block's k loop, waves of tiles over the SMs (or pairs).
-void choose_tiles(Class& c, std::vector<Shape>& shapes, const std::vector<int>& count, int sms) {
+void choose_tiles(Class& c, std::vector<Shape>& shapes, std::vector<Parts>& parts, const std::vector<int>& count, int sms) {
   struct Form { int cg, cols; double cost; };
   const Form forms[3] = {{2, c.parts == 1 ? 256 : 128, c.parts == 1 ? 2.0 : 1.75}, {1, 128, 2.1}, {1, 64, 1.7}};
   double best = 0;
+  const Form* form = forms;
   for (const Form& f : forms) {
     const int units = sms / f.cg;
     double work_s = 0, work_x = 0, longest_s = 0, longest_x = 0;
+    int64_t tiles = 0;
+    for (int i = c.first; i < c.first + c.n; ++i) {
+      Shape g = shapes[i];
+      count_tiles(g, 128 * f.cg, f.cols);
+      tiles += (int64_t)g.s_tiles * count[i];
+    }
     for (int i = c.first; i < c.first + c.n; ++i) {
       Shape g = shapes[i];
       count_tiles(g, 128 * f.cg, f.cols);
       const int big = g.tall ? g.rows : g.cols;
       work_s += (double)g.s_tiles * big * count[i];
       work_x += (double)(g.x_tiles + g.s_tiles) * g.small * count[i];
-      longest_s = std::max(longest_s, (double)big);
+      double alone;
+      splits_of(c, g, tiles, units, f.cols, f.cost, &alone);
+      longest_s = std::max(longest_s, alone / f.cost);
       longest_x = std::max(longest_x, (double)g.small);
     }
     const double t = f.cost * (std::max(work_s / units, longest_s) + std::max(work_x / units, 2 * longest_x));
-    if (best == 0 || t < best) { best = t; c.cg = f.cg; c.cols = f.cols; }
+    if (best == 0 || t < best) { best = t; c.cg = f.cg; c.cols = f.cols; form = &f; }
   }
-  for (int i = c.first; i < c.first + c.n; ++i) count_tiles(shapes[i], 128 * c.cg, c.cols);
+  int64_t tiles = 0;
+  for (int i = c.first; i < c.first + c.n; ++i) {
+    count_tiles(shapes[i], 128 * c.cg, c.cols);
+    tiles += (int64_t)shapes[i].s_tiles * count[i];
+  }
+  for (int i = c.first; i < c.first + c.n; ++i) parts[i].n = splits_of(c, shapes[i], tiles, sms / c.cg, c.cols, form->cost, &best);
 }
 
 // The list of a class's products.  Portions of matrices that L2 holds go through all steps, one portion after another.
-void list_products(Class& c, const std::vector<Shape>& shapes, const std::vector<int>& count, int steps, std::vector<Batch>& batches) {
+void list_products(Class& c, const std::vector<Shape>& shapes, const std::vector<Parts>& parts, const std::vector<int>& count, int steps, std::vector<Batch>& batches) {
   struct Piece { int shape, first, n; };
   std::vector<std::vector<Piece>> portions;
   int64_t room = 0;
@@ -519,7 +625,7 @@ void list_products(Class& c, const std::vector<Shape>& shapes, const std::vector
           const Shape& g = shapes[q.shape];
           Batch b = {};
           b.begin = (int)at;
-          b.end = (int)(at += (int64_t)q.n * (phase == PHASE_X ? g.x_tiles : g.s_tiles));
+          b.end = (int)(at += (int64_t)q.n * (phase == PHASE_X ? g.x_tiles : phase == PHASE_S ? g.s_tiles * parts[q.shape].n : g.s_tiles));
           b.first = q.first; b.shape = (u32)(q.shape - c.first); b.phase = (u32)phase; b.step = (u32)s;
           batches.push_back(b);
         }
@@ -548,6 +654,29 @@ cudaError_t launch(void (*kernel)(P...), int blocks, cudaStream_t st, bool first
   cfg.attrs = at;
   cfg.numAttrs = first ? 0 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <bool SPLIT>
+cudaError_t launch_class(const sae_ortho* h, const Class& c) {
+  static thread_local OrthoJob<SPLIT> job;
+  job = {};
+  job.cols = c.cols;
+  job.rows = 128 * c.cg;
+  if (c.parts == 2) job.seg = {3, {0, 1, 0}, {1, 0, 0}};
+  else job.seg = {1, {0}, {0}};
+  job.maps = h->maps + c.first;
+  job.shapes = h->shapes + c.first;
+  job.parts = h->parts + c.first;
+  job.batches = h->batches + c.first_batch;
+  job.num_shapes = c.n; job.num_batches = c.batches; job.total = c.total; job.steps = h->steps; job.arrivals = c.cg;
+  job.done = h->done;
+  job.ratios = h->ratios;
+  job.mats = h->mats;
+  job.places = h->places;
+  job.order = h->order;
+  // (one part: B hi is added to x hi times 1)
+  factors(h, c.parts == 2 ? h->b_scale : h->ones, job.factors);
+  return mma::launch_products(job, c.cg, std::min(c.total, h->num_sms / c.cg), h->stream, true);
 }
 
 }  // namespace
@@ -586,6 +715,7 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
   h->x_scale = std::exp2(std::floor(std::log2(32768.0 / widest)));
   std::vector<Maps> maps;
   std::vector<Shape> shapes;
+  std::vector<Parts> parts;
   std::vector<int> count, order;
   std::vector<Place> places;
   std::vector<Chunk> chunks;
@@ -629,7 +759,7 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
         g.first = (int)order.size();
         for (int i : kv.second) order.push_back(i);
         count.push_back((int)kv.second.size());
-        if (h->classes.empty() || h->classes.back().parts != g.s_parts) h->classes.push_back({g.s_parts, 1, 64, (int)shapes.size(), 0, 0, 0, 0});
+        if (h->classes.empty() || h->classes.back().parts != g.s_parts) h->classes.push_back({g.s_parts, 1, 64, (int)shapes.size(), 0, 0, 0, 0, false});
         ++h->classes.back().n;
         shapes.push_back(g);
         bytes += 2 * up(2 * g.x_plane * count.back() * 2, 1024) + 2 * up(g.s_parts * g.s_plane * count.back() * 2, 1024);
@@ -679,9 +809,37 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
             p.chunks = (int)chunks.size() - p.first_chunk;
           }
         }
+        parts.resize(shapes.size());
+        int64_t split_sums = 0, arrived = 0;
+        const auto sums_size = [&](const Class& c, int i) { return parts[i].n > 1 ? (int64_t)count[i] * shapes[i].s_tiles * parts[i].n * 128 * c.cg * c.cols : 0; };
         for (Class& c : h->classes) {
-          choose_tiles(c, shapes, count, h->num_sms);
-          list_products(c, shapes, count, cfg->steps, batches);
+          choose_tiles(c, shapes, parts, count, h->num_sms);
+          list_products(c, shapes, parts, count, cfg->steps, batches);
+          for (int i = c.first; i < c.first + c.n; ++i) {
+            split_sums += sums_size(c, i);
+            c.split = c.split || parts[i].n > 1;
+            if (parts[i].n > 1) arrived += (int64_t)count[i] * shapes[i].s_tiles * 16;
+          }
+        }
+        if (split_sums) {
+          e = cudaMalloc((void**)&h->split_sums, (size_t)split_sums * sizeof(float));
+          if (e == cudaSuccess) e = cudaMalloc((void**)&h->arrived, (size_t)arrived * sizeof(u32));
+          float* sums_at = h->split_sums;
+          u32* arrived_at = h->arrived;
+          for (const Class& c : h->classes)
+            for (int i = c.first; i < c.first + c.n && e == cudaSuccess; ++i) {
+              const Shape& g = shapes[i];
+              if (parts[i].n == 1) continue;
+              parts[i].sums = sums_at;
+              parts[i].arrived = arrived_at;
+              for (int q = 0; q < count[i]; ++q) {
+                Place& p = places[order[g.first + q]];
+                p.arrived = arrived_at + (int64_t)q * g.s_tiles * 16;
+                p.num_arrived = g.s_tiles * 16;
+              }
+              sums_at += sums_size(c, i);
+              arrived_at += (int64_t)count[i] * g.s_tiles * 16;
+            }
         }
         h->chunks = (int)chunks.size();
       }
@@ -693,6 +851,7 @@ int sae_ortho_init(const sae_ortho_config* cfg, sae_ortho** out) {
   if (e == cudaSuccess && !mapped) e = cudaErrorUnknown;
   if (e == cudaSuccess) e = upload(&h->maps, maps, h->stream);
   if (e == cudaSuccess) e = upload(&h->shapes, shapes, h->stream);
+  if (e == cudaSuccess) e = upload(&h->parts, parts, h->stream);
   if (e == cudaSuccess) e = upload(&h->batches, batches, h->stream);
   if (e == cudaSuccess) e = upload(&h->places, places, h->stream);
   if (e == cudaSuccess) e = upload(&h->chunk_list, chunks, h->stream);
@@ -747,26 +906,8 @@ int sae_ortho_run(sae_ortho* h, const void* const* matrices, const int64_t* pitc
     e = launch(k_ortho_norm, h->chunks, h->stream, first, (const Matrix*)h->mats, (const Place*)h->places, (const Chunk*)h->chunk_list, h->sums);
   if (h->chunks && e == cudaSuccess)
     e = launch(k_ortho_split, h->chunks, h->stream, false, (const Matrix*)h->mats, (const Place*)h->places, (const Chunk*)h->chunk_list, (const double*)h->sums, h->eps, h->x_scale);
-  for (const Class& c : h->classes) {
-    static thread_local OrthoJob job;
-    job = {};
-    job.cols = c.cols;
-    job.rows = 128 * c.cg;
-    if (c.parts == 2) job.seg = {3, {0, 1, 0}, {1, 0, 0}};
-    else job.seg = {1, {0}, {0}};
-    job.maps = h->maps + c.first;
-    job.shapes = h->shapes + c.first;
-    job.batches = h->batches + c.first_batch;
-    job.num_shapes = c.n; job.num_batches = c.batches; job.total = c.total; job.steps = h->steps; job.arrivals = c.cg;
-    job.done = h->done;
-    job.ratios = h->ratios;
-    job.mats = h->mats;
-    job.places = h->places;
-    job.order = h->order;
-    // (one part: B hi is added to x hi times 1)
-    factors(h, c.parts == 2 ? h->b_scale : h->ones, job.factors);
-    if (e == cudaSuccess) e = mma::launch_products(job, c.cg, std::min(c.total, h->num_sms / c.cg), h->stream, true);
-  }
+  for (const Class& c : h->classes)
+    if (e == cudaSuccess) e = c.split ? launch_class<true>(h, c) : launch_class<false>(h, c);
   return e == cudaSuccess ? SAE_OK : cuda_status(h, e);
 }
 

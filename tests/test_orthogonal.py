@@ -146,6 +146,21 @@ def test_large_batches(result):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,result", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16")])
+def test_long_sums(dtype, result):
+    """Matrices whose square products are few and long are made in parts: wide, tall, odd, beside others that are not; the same bits again."""
+    shapes = [(25, 3770), (3001, 140), (168, 2518), (129, 1001), (333, 1001), (200, 200), (300, 9000), (70, 50)]
+    for group in ([s] for s in shapes), [shapes[:3] + shapes[5:]], [shapes]:
+        for some in group:
+            gs = [gradient(s, DTYPES[dtype], i) for i, s in enumerate(some)]
+            plan = Orthogonalizer(some, DTYPES[dtype], result_dtypes=DTYPES[result])
+            out = plan(gs)
+            for g, x in zip(gs, out):
+                assert rel(x, exact(g)) <= allowed(g, DTYPES[result]), tuple(g.shape)
+            assert all(torch.equal(a, b) for _ in range(3) for a, b in zip(out, plan(gs)))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("steps", [1, 2, 7])
 def test_steps_and_coefficients(steps):
     g = gradient((150, 210), torch.float32, 3, "noise")
