@@ -1,13 +1,12 @@
 // The linear cross entropy of float tensors in small problems: ordinary float arithmetic.  Three bfloat16 parts cost a pass over the weights
-// and six products each, which pays only when there is enough of them (32 x 2048 x 1000, loss and gradients: 199 us there, see
-// CE_FLOAT_WORK for where the two meet).  Products are tiles of 32 x 64 by 128 threads, split along k until the SMs are
-// filled; whoever reads a product adds its splits in their order.
+// and six products each, which pays only when there is enough of them (in_float says where the two meet).  Products are tiles of 32 x 64 by
+// 128 threads, split along k until the SMs are filled; whoever reads a product adds its splits in their order.
 #pragma once
 #include <cooperative_groups.h>
 
 namespace {
 
-constexpr int CF_ROWS = 32, CF_COLS = 64, CF_K = 32, CF_THREADS = 128, CF_LOSS_THREADS = 512;
+constexpr int CF_ROWS = 32, CF_COLS = 64, CF_K = 32, CF_THREADS = 128, CF_LOSS_THREADS = 512, CF_LOSS_CLASSES = 2048;
 
 enum FloatProduct { CF_Z, CF_DX, CF_DW };     // x w',  p w,  p' x
 
@@ -20,7 +19,8 @@ struct FloatArgs {
   float* out;                                 // [splits][room][out_pitch]
   int64_t room;
   int out_pitch;
-  bool vector;                                // rows of x and w start on 16 bytes
+  bool x_vector, w_vector;                    // rows start on 16 bytes
+  bool dw_vector;                             // and dweight's
   // dweight in one split goes straight to the caller
   float* dweight;
   void* dbias;
@@ -60,8 +60,8 @@ struct FloatTile {
 };
 
 // One tile: acc[i][j] for rows tr + 8 i (tr * 4 + i where A's rows are its fast direction) and columns tc + 16 j (tc * 4 + j).
-// row_at(i): where in memory the i-th row of x is, -1: nowhere (a row of zeros).
-template <FloatProduct KIND, typename RowAt>
+// row_at(i): where in memory the i-th row of x is, -1: nowhere (a row of zeros).  I: rows of a thread, 1 where the tile has no more than 8.
+template <FloatProduct KIND, int I, typename RowAt>
 __device__ __forceinline__ void float_tile(const FloatArgs& a, float* smem, int row0, int col0, int rows, int cols, int depth, int c0, int c1, RowAt row_at, float (&acc)[4][4]) {
   typedef FloatTile<KIND> F;
   const int t = threadIdx.x;
@@ -79,7 +79,7 @@ __device__ __forceinline__ void float_tile(const FloatArgs& a, float* smem, int 
           const int r = u / (CF_K / 4), k = u % (CF_K / 4) * 4;
           if constexpr (KIND == CF_Z) {
             const int at = row0 + r < rows ? row_at(row0 + r) : -1;
-            four_in(sa + r * F::A_PITCH + k, a.x + (at >= 0 ? (int64_t)at * a.x_pitch : 0) + k0 + k, at >= 0 ? depth - k0 - k : 0, a.vector, a.any);
+            four_in(sa + r * F::A_PITCH + k, a.x + (at >= 0 ? (int64_t)at * a.x_pitch : 0) + k0 + k, at >= 0 ? depth - k0 - k : 0, a.x_vector, a.any);
           } else four_in(sa + r * F::A_PITCH + k, a.p + (int64_t)(row0 + r) * a.p_pitch + k0 + k, row0 + r < rows ? depth - k0 - k : 0, true, a.any);
         }
       }
@@ -87,12 +87,12 @@ __device__ __forceinline__ void float_tile(const FloatArgs& a, float* smem, int 
       for (int u = t; u < CF_COLS * CF_K / 4; u += CF_THREADS) {
         if constexpr (KIND == CF_Z) {
           const int c = u / (CF_K / 4), k = u % (CF_K / 4) * 4;
-          four_in(sb + c * F::B_PITCH + k, a.w + (int64_t)(col0 + c) * a.w_pitch + k0 + k, col0 + c < cols ? depth - k0 - k : 0, a.vector, a.any);
+          four_in(sb + c * F::B_PITCH + k, a.w + (int64_t)(col0 + c) * a.w_pitch + k0 + k, col0 + c < cols ? depth - k0 - k : 0, a.w_vector, a.any);
         } else {
           const int k = u / (CF_COLS / 4), c = u % (CF_COLS / 4) * 4;
           const bool there = k0 + k < depth;
           const float* const row = KIND == CF_DX ? a.w + (int64_t)(k0 + k) * a.w_pitch : a.x + (there ? (int64_t)row_at(k0 + k) * a.x_pitch : 0);
-          four_in(sb + k * F::B_PITCH + c, row + col0 + c, there ? cols - col0 - c : 0, a.vector, a.any);
+          four_in(sb + k * F::B_PITCH + c, row + col0 + c, there ? cols - col0 - c : 0, KIND == CF_DX ? a.w_vector : a.x_vector, a.any);
         }
       }
     }
@@ -109,15 +109,22 @@ __device__ __forceinline__ void float_tile(const FloatArgs& a, float* smem, int 
     const float* const sb = sa + F::A_SIZE;
 #pragma unroll
     for (int k = 0; k < CF_K; k += 4) {
+      if (KIND == CF_DW && c * CF_K + k >= depth) break;      // a few rows of x
       float x[4][4], y[4][4];             // [row or column][k]
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float4 v = *reinterpret_cast<const float4*>(F::A_ROWS ? sa + (k + i) * F::A_PITCH + tr * 4 : sa + F::row(tr, i) * F::A_PITCH + k);
+        if (F::A_ROWS || i < I) {
+          const float4 v = *reinterpret_cast<const float4*>(F::A_ROWS ? sa + (k + i) * F::A_PITCH + tr * 4 : sa + F::row(tr, i) * F::A_PITCH + k);
+          const float vs[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            if (F::A_ROWS) x[q][i] = vs[q]; else x[i][q] = vs[q];
+          }
+        }
         const float4 w = *reinterpret_cast<const float4*>(F::B_ROWS ? sb + (k + i) * F::B_PITCH + tc * 4 : sb + F::col(tc, i) * F::B_PITCH + k);
-        const float vs[4] = {v.x, v.y, v.z, v.w}, ws[4] = {w.x, w.y, w.z, w.w};
+        const float ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          if (F::A_ROWS) x[q][i] = vs[q]; else x[i][q] = vs[q];
           if (F::B_ROWS) y[q][i] = ws[q]; else y[i][q] = ws[q];
         }
       }
@@ -129,7 +136,7 @@ __device__ __forceinline__ void float_tile(const FloatArgs& a, float* smem, int 
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < I; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j) acc[i][j] = __fmaf_rn(x[i][q], y[j][q], acc[i][j]);
     }
@@ -150,7 +157,9 @@ __global__ void __launch_bounds__(CF_THREADS) k_cf_product(const __grid_constant
   if (row0 >= rows) return;
   const int chunks = (depth + CF_K - 1) / CF_K, c0 = (int)((int64_t)chunks * blockIdx.z / a.splits), c1 = (int)((int64_t)chunks * (blockIdx.z + 1) / a.splits);
   float acc[4][4] = {};
-  float_tile<KIND>(a, smem, row0, col0, rows, cols, depth, c0, c1, [&](int i) { return a.index[i]; }, acc);
+  const auto row_at = [&](int i) { return a.index[i]; };
+  if (KIND != CF_DW && rows - row0 <= 8) float_tile<KIND, 1>(a, smem, row0, col0, rows, cols, depth, c0, c1, row_at, acc);
+  else float_tile<KIND, 4>(a, smem, row0, col0, rows, cols, depth, c0, c1, row_at, acc);
   const int tr = threadIdx.x / 16, tc = threadIdx.x % 16;
   const auto row_of = [&](int i) { return F::row(tr, i); };
   const auto col_of = [&](int j) { return F::col(tc, j); };
@@ -160,6 +169,10 @@ __global__ void __launch_bounds__(CF_THREADS) k_cf_product(const __grid_constant
     for (int i = 0; i < 4; ++i) {
       const int64_t r = row0 + row_of(i);
       if (r >= rows) continue;
+      if (a.dw_vector && col0 + col_of(3) < a.features) {
+        *reinterpret_cast<float4*>(a.dweight + r * a.features + col0 + col_of(0)) = make_float4(acc[i][0] * alpha, acc[i][1] * alpha, acc[i][2] * alpha, acc[i][3] * alpha);
+        continue;
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int c = col0 + col_of(j);
@@ -174,10 +187,14 @@ __global__ void __launch_bounds__(CF_THREADS) k_cf_product(const __grid_constant
   for (int i = 0; i < 4; ++i) {
     const int r = row0 + row_of(i);
     if (r >= rows) continue;
+    if constexpr (F::B_ROWS) {                    // four neighbours, of a pitch that is a multiple of 4
+      if (col0 + col_of(0) < a.out_pitch) *reinterpret_cast<float4*>(out + (int64_t)r * a.out_pitch + col0 + col_of(0)) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int c = col0 + col_of(j);
-      if (c < a.out_pitch) out[(int64_t)r * a.out_pitch + c] = acc[i][j];
+      for (int j = 0; j < 4; ++j) {
+        const int c = col0 + col_of(j);
+        if (c < a.out_pitch) out[(int64_t)r * a.out_pitch + c] = acc[i][j];
+      }
     }
   }
 }
@@ -190,7 +207,8 @@ struct FloatRowArgs {
   int splits, pitch, classes, bias_type, reduction;
   // loss
   float *loss, *lse;
-  double* sums;
+  float2* runs;                               // [rows][blocks of a row]: maximum, sum
+  float* at_z;                                // the target's logit
   unsigned* ticket;
   // p
   const float *lse_g, *g;
@@ -214,21 +232,29 @@ __device__ __forceinline__ void join_runs(float& m, float& s, float om, float os
   m = top;
 }
 
-// A block a row: maximum and sum, then the loss; the last block adds the rows' losses in their order.
+// Maximum and sum of up to CF_LOSS_CLASSES of a row by each block (30522 classes by one block: 64 us); the last block joins them and adds the rows'
+// losses, all in their order.
 __global__ void __launch_bounds__(CF_LOSS_THREADS) k_cf_loss(const __grid_constant__ FloatRowArgs a) {
   __shared__ float sm[CF_LOSS_THREADS / 32], ss[CF_LOSS_THREADS / 32];
   __shared__ double sd[CF_LOSS_THREADS / 32];
   __shared__ bool final_block;
   mma::let_next_start();
   mma::wait_for_previous();
-  const int count = *a.counted, i = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  double loss_d = 0;
+  const int count = *a.counted, i = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, blocks = gridDim.y;
+  constexpr float NONE = -INFINITY;
   if (i < count) {
-    float m = __int_as_float(0xff800000), s = 0;
-    for (int j = threadIdx.x; j < a.classes; j += CF_LOSS_THREADS) {
-      const float z = logit_of(a, i, j);
-      if (z > m) { s *= exp2f((m - z) * LOG2E); m = z; }
-      s += m == __int_as_float(0xff800000) ? (z != z ? z : 0.0f) : exp2f((z - m) * LOG2E);
+    float m = NONE, s = 0;
+    const int end = min(a.classes, ((int)blockIdx.y + 1) * CF_LOSS_CLASSES), target = a.at[i];
+    for (int j0 = blockIdx.y * CF_LOSS_CLASSES + threadIdx.x; j0 < end; j0 += 4 * CF_LOSS_THREADS) {
+      float z[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) z[q] = j0 + q * CF_LOSS_THREADS < end ? logit_of(a, i, j0 + q * CF_LOSS_THREADS) : NONE;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (j0 + q * CF_LOSS_THREADS == target) a.at_z[i] = z[q];
+        if (z[q] > m) { s *= exp2f((m - z[q]) * LOG2E); m = z[q]; }
+        s += m == NONE ? (z[q] != z[q] ? z[q] : 0.0f) : exp2f((z[q] - m) * LOG2E);
+      }
     }
     for (int o = 16; o; o >>= 1) {
       const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o);
@@ -238,24 +264,33 @@ __global__ void __launch_bounds__(CF_LOSS_THREADS) k_cf_loss(const __grid_consta
     __syncthreads();
     if (threadIdx.x == 0) {
       for (int k = 1; k < CF_LOSS_THREADS / 32; ++k) join_runs(m, s, sm[k], ss[k]);
-      const int t = a.at[i];
-      const float z = t >= 0 ? logit_of(a, i, t) : __int_as_float(0x7fc00000), loss = logf(s) + (m - z);
-      a.lse[a.index[i]] = m + logf(s);
-      if (a.reduction == SAE_REDUCE_NONE) a.loss[a.index[i]] = loss;
-      loss_d = loss;
+      a.runs[(int64_t)i * blocks + blockIdx.y] = make_float2(m, s);
     }
   }
-  if (a.reduction == SAE_REDUCE_NONE) return;
+  __threadfence();
+  __syncthreads();
   if (threadIdx.x == 0) {
-    a.sums[i] = loss_d;
     __threadfence();
-    final_block = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+    final_block = atomicAdd(a.ticket, 1u) == gridDim.x * gridDim.y - 1;
   }
   __syncthreads();
   if (!final_block) return;
   __threadfence();
   double sum = 0;
-  for (int k = threadIdx.x; k < (int)gridDim.x; k += CF_LOSS_THREADS) sum += __ldcg(a.sums + k);
+  for (int r = threadIdx.x; r < count; r += CF_LOSS_THREADS) {
+    const float z = a.at[r] >= 0 ? __ldcg(a.at_z + r) : __int_as_float(0x7fc00000);
+    float m = NONE, s = 0;
+#pragma unroll 4
+    for (int k = 0; k < blocks; ++k) {
+      const float2 run = __ldcg(a.runs + (int64_t)r * blocks + k);
+      join_runs(m, s, run.x, run.y);
+    }
+    const float loss = logf(s) + (m - z);
+    a.lse[a.index[r]] = m + logf(s);
+    if (a.reduction == SAE_REDUCE_NONE) a.loss[a.index[r]] = loss;
+    sum += loss;
+  }
+  if (a.reduction == SAE_REDUCE_NONE) return;
   for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) sd[warp] = sum;
   __syncthreads();
@@ -284,18 +319,25 @@ struct FloatSumArgs {
   int64_t room;
   int splits, pitch, features, bias_type, rows;      // rows < 0: those that are counted
 };
+// A block has 32 columns; each of its warps takes every fourth split.
 __global__ void __launch_bounds__(CF_THREADS) k_cf_sum(const __grid_constant__ FloatSumArgs a) {
+  __shared__ float parts[CF_THREADS / 32][32];
   mma::let_next_start();
   mma::wait_for_previous();
   const int64_t r = blockIdx.y;
-  const int c = blockIdx.x * CF_THREADS + threadIdx.x;
-  if (r >= (a.rows < 0 ? *a.counted : a.rows) || c > a.features) return;
-  if (c == a.features && !a.dbias) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  if (r >= (a.rows < 0 ? *a.counted : a.rows)) return;
   float v = 0;
+  if (c < a.pitch) {
 #pragma unroll 8
-  for (int s = 0; s < a.splits; ++s) v += __ldcg(a.sums + (s * a.room + r) * a.pitch + c);
+    for (int s = warp; s < a.splits; s += CF_THREADS / 32) v += __ldcg(a.sums + (s * a.room + r) * a.pitch + c);
+  }
+  parts[warp][lane] = v;
+  __syncthreads();
+  if (warp || c > a.features) return;
+  v = (parts[0][lane] + parts[1][lane]) + (parts[2][lane] + parts[3][lane]);
   v *= *a.alpha;
-  if (c == a.features) store_bias(a.dbias, a.bias_type, r, v);
+  if (c == a.features) { if (a.dbias) store_bias(a.dbias, a.bias_type, r, v); }
   else if (a.out) a.out[(a.index ? (int64_t)a.index[r] : r) * a.features + c] = v;
 }
 
@@ -326,7 +368,7 @@ __global__ void __launch_bounds__(CF_THREADS) k_cf_tiny(const __grid_constant__ 
   }
   __syncthreads();
   float acc[4][4] = {};
-  float_tile<CF_Z>(a.f, smem, row0, 0, a.rows, a.f.classes, a.f.features, 0, (a.f.features + CF_K - 1) / CF_K, [&](int i) { return at[i - row0]; }, acc);
+  float_tile<CF_Z, 4>(a.f, smem, row0, 0, a.rows, a.f.classes, a.f.features, 0, (a.f.features + CF_K - 1) / CF_K, [&](int i) { return at[i - row0]; }, acc);
   double sum = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {

@@ -830,12 +830,15 @@ int device_sms() {
   return sms;
 }
 
-// Float tensors take float arithmetic up to so many rows and products (rows * classes * features).  Loss and gradients, us, there and in
-// bfloat16 parts: 32 x 2048 x 1000 69 and 202, 128 x 2048 x 1000 125 and 199, 256 x 2048 x 1000 197 and 215, 512 x 2048 x 1000 362 and
-// 241 (they meet near 300 rows), 8 x 768 x 30522 353 and 361, 128 x 768 x 30522 936 and 437.
-constexpr int64_t CE_FLOAT_ROWS = 320, CE_FLOAT_WORK = 1ll << 29;
+// Float tensors of up to CE_FLOAT_ROWS rows take float arithmetic where that is faster than bfloat16 parts, by these fits (us).  Float: whole blocks of
+// 32 rows, and a logit's way through memory.  Parts: w is read, laid out and read again; long sums of six products in few tiles.  Loss and gradients, there
+// and in parts: 32 x 2048 x 1000 58 and 165, 128 x 2048 x 1000 121 and 166, 256 x 2048 x 1000 198 and 169; 8 x 768 x 30522 203 and 322, 32 rows 285 and 338,
+// 64 rows 478 and 341; 17 x 1152 x 39231 460 and 572; 320 x 64 x 20000 259 and 147, 300 x 64 x 1000 43 and 53.
+constexpr int64_t CE_FLOAT_ROWS = 320;
 bool in_float(const sae_linear_ce_desc* d) {
-  return d->type == SAE_TYPE_FLOAT && d->rows <= CE_FLOAT_ROWS && d->classes <= (1 << 20) && d->rows * d->classes <= CE_FLOAT_WORK / d->features;
+  if (d->type != SAE_TYPE_FLOAT || d->rows > CE_FLOAT_ROWS || d->classes > (1 << 20)) return false;
+  const double n = (double)d->rows, v = (double)d->classes, k = (double)d->features;
+  return 35 + 2.6e-7 * (double)up(std::max<int64_t>(1, d->rows), 32) * v * k + 1.9e-5 * n * v < 40 + 7e-6 * v * k + 3e-3 * v + 4.5e-2 * k;
 }
 // Splits of k, from what does not depend on the rows, so that a row's result does not either: four blocks an SM for a single block of
 // rows, and no split of less than 64 k (least k unknown: 0).
@@ -941,7 +944,8 @@ CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward,
     p.z_pitch = (int)up(d->classes, 4);
     p.z_splits = float_splits((d->classes + CF_COLS - 1) / CF_COLS, d->features, 8, sms);
     p.fz = take((int64_t)p.z_splits * n * p.z_pitch * 4);
-    p.sums = take(n * 8);
+    p.at_z = take(n * 4);
+    p.sums = take(n * ((d->classes + CF_LOSS_CLASSES - 1) / CF_LOSS_CLASSES) * 8);
     if (backward) {
       p.lse_g = take(n * 4);
       p.g = take(n * 4);
@@ -1108,7 +1112,8 @@ FloatArgs float_args(const sae_linear_ce_desc* d, const CePlan& p, const RowsArg
   f.index = a.index; f.counted = a.counted;
   f.x_pitch = d->x_pitch; f.w_pitch = d->weight_pitch;
   f.p_pitch = p.z_pitch; f.features = a.features; f.classes = a.classes;
-  f.vector = aligned_to(a.x, 16) && aligned_to(a.w, 16) && (d->rows < 2 || d->x_pitch % 4 == 0) && (d->classes < 2 || d->weight_pitch % 4 == 0);
+  f.x_vector = aligned_to(a.x, 16) && (d->rows < 2 || d->x_pitch % 4 == 0);
+  f.w_vector = aligned_to(a.w, 16) && (d->classes < 2 || d->weight_pitch % 4 == 0);
   f.alpha = a.alpha;
   f.any = a.counted;
   return f;
@@ -1117,7 +1122,7 @@ FloatRowArgs float_rows(const sae_linear_ce_desc* d, const CePlan& p, const Rows
   FloatRowArgs r = {};
   r.z = (const float*)(ws + p.fz); r.bias = a.bias; r.index = a.index; r.at = a.at; r.counted = a.counted;
   r.room = std::max<int64_t>(1, d->rows); r.splits = p.z_splits; r.pitch = p.z_pitch; r.classes = a.classes; r.bias_type = a.bias_type; r.reduction = d->reduction;
-  r.sums = (double*)(ws + p.sums); r.ticket = (unsigned*)a.counted + COUNT_TICKET;
+  r.runs = (float2*)(ws + p.sums); r.at_z = (float*)(ws + p.at_z); r.ticket = (unsigned*)a.counted + COUNT_TICKET;
   return r;
 }
 
@@ -1148,7 +1153,7 @@ int float_forward(const sae_linear_ce_desc* d, const CePlan& p, RowsArgs& a, flo
   if (rc == SAE_OK && d->rows) rc = float_product<CF_Z>(float_args(d, p, a, ws), d->rows, d->classes, p.z_splits, (float*)(ws + p.fz), d->rows, p.z_pitch, st);
   FloatRowArgs r = float_rows(d, p, a, ws);
   r.loss = loss; r.lse = lse;
-  if (rc == SAE_OK) rc = launch(k_cf_loss, dim3((unsigned)std::max<int64_t>(1, d->rows)), CF_LOSS_THREADS, st, false, r);
+  if (rc == SAE_OK) rc = launch(k_cf_loss, dim3((unsigned)std::max<int64_t>(1, d->rows), (unsigned)((d->classes + CF_LOSS_CLASSES - 1) / CF_LOSS_CLASSES)), CF_LOSS_THREADS, st, false, r);
   return rc;
 }
 
@@ -1164,16 +1169,16 @@ int float_backward(const sae_linear_ce_desc* d, const CePlan& p, RowsArgs& a, vo
   if (dx && d->rows) {
     if (rc == SAE_OK) rc = float_product<CF_DX>(f, d->rows, d->features, p.dx_splits, (float*)(ws + p.fdx), d->rows, p.dx_pitch, st);
     s.sums = (const float*)(ws + p.fdx); s.index = a.index; s.out = (float*)dx; s.room = d->rows; s.splits = p.dx_splits; s.pitch = p.dx_pitch; s.rows = -1;
-    if (rc == SAE_OK) rc = launch(k_cf_sum, dim3((unsigned)((d->features + CF_THREADS) / CF_THREADS), (unsigned)d->rows), CF_THREADS, st, false, s);
+    if (rc == SAE_OK) rc = launch(k_cf_sum, dim3((unsigned)(d->features / 32 + 1), (unsigned)d->rows), CF_THREADS, st, false, s);
   }
   if (dweight || dbias) {
-    f.dweight = (float*)dweight; f.dbias = dbias; f.bias_type = d->bias_type;
+    f.dweight = (float*)dweight; f.dw_vector = dweight && aligned_to(dweight, 16) && d->features % 4 == 0; f.dbias = dbias; f.bias_type = d->bias_type;
     if (rc == SAE_OK) rc = float_product<CF_DW>(f, d->classes, d->features + (dbias ? 1 : 0), p.dw_splits, (float*)(ws + p.fdw), d->classes, p.dw_pitch, st);
     if (p.dw_splits > 1) {
       // (only few classes are split: far fewer than a grid has rows)
       s.sums = (const float*)(ws + p.fdw); s.index = nullptr; s.out = (float*)dweight; s.dbias = dbias; s.room = d->classes; s.splits = p.dw_splits; s.pitch = p.dw_pitch;
       s.rows = (int)d->classes;
-      if (rc == SAE_OK) rc = launch(k_cf_sum, dim3((unsigned)((d->features + 1 + CF_THREADS - 1) / CF_THREADS), (unsigned)d->classes), CF_THREADS, st, false, s);
+      if (rc == SAE_OK) rc = launch(k_cf_sum, dim3((unsigned)(d->features / 32 + 1), (unsigned)d->classes), CF_THREADS, st, false, s);
     }
   }
   return rc;

@@ -246,6 +246,28 @@ def test_small_float_heads(n, d, v):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,d,v", [(1, 40, 6000), (8, 64, 5001), (9, 61, 4099), (40, 132, 2049), (33, 1000, 2048)])
+def test_few_float_rows(n, d, v):
+    """A row's classes in several blocks, up to 8 rows in a tile and more; x that starts on no 16 bytes beside weights that do, and the
+    other way round: the bits of the plain tensors."""
+    for i, reduction in enumerate(("mean", "sum", "none")):
+        x, w, t, b = data(n, d, v, torch.float32, i > 0, 0.2, seed=n + i)
+        t[0] = v - 1
+        dloss = torch.rand(n, device="cuda") - 0.3 if reduction == "none" else torch.tensor(0.7, device="cuda")
+        check(x, w, t, b, reduction, dloss)
+        want = ce.linear_cross_entropy_forward(x, w, t, b, reduction=reduction)
+        grads = ce.linear_cross_entropy_backward(dloss, x, w, t, want[1], want[2], b, reduction=reduction)
+
+        def off(a):
+            return torch.cat([a.new_zeros((len(a), 3)), a], 1)[:, 3:]
+        for xx, ww in ((off(x), w), (x, off(w))):
+            got = ce.linear_cross_entropy_forward(xx, ww, t, b, reduction=reduction)
+            again = ce.linear_cross_entropy_backward(dloss, xx, ww, t, got[1], got[2], b, reduction=reduction)
+            assert all(torch.equal(p, q) for p, q in zip(want, got))
+            assert all(p is q is None or torch.equal(p, q) for p, q in zip(grads, again))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_layouts(dtype):
     """Slices of wider tensors, odd offsets, an expanded row, transposed storage, more dimensions: the bits of the plain tensors."""
