@@ -496,7 +496,7 @@ int sae_linear_ce_backward(const sae_linear_ce_desc *desc, const float *dloss, c
  *   x <- a_i x + b_i (x x') x + c_i (x x')^2 x
  *
  * A sae_ortho holds the shapes, the tables and the workspace (about 8 bytes an element and 8 more for each element of the square
- * products) of one list of matrices: `num_rows` workers' lists of `num_matrices` each.
+ * products, and up to 20 MB of sums) of one list of matrices: `num_rows` workers' lists of `num_matrices` each.
  * matrices, results: HOST arrays of num_rows * num_matrices DEVICE pointers, row k's at [k * num_matrices .. ); read before the call
  *   returns.  Matrix j is rows[j] x cols[j] of type types[j], neighbouring columns next to each other, its rows pitches[..] elements
  *   apart (HOST, as the pointers; NULL: without gaps); its result is of type result_types[j].  A result may be its own
