@@ -183,6 +183,7 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_count(const __grid_constant__
 // The largest |dloss| of the rows that take part, or 1 where that is 0 or not finite.
 __global__ void __launch_bounds__(1024) k_ce_top(const __grid_constant__ RowsArgs a, float* top) {
   __shared__ float scratch[32];
+  mma::wait_for_previous();             // the gathering kernel waits for this one alone, and reads what k_ce_count wrote before it
   float m = 0;
   for (int64_t i = threadIdx.x; i < a.rows; i += 1024)
     if (a.target[i] != a.ignore) { const float v = fabsf(a.dloss[i]); if (v <= 3.0e38f) m = fmaxf(m, v); }

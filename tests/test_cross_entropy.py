@@ -197,6 +197,17 @@ def test_factors_of_their_own_in_large_problems(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("ignored", [0.0, 0.3, 0.95])
+def test_factors_of_their_own_for_rows_counted_in_two_steps(ignored):
+    """float16 rows beyond what one block counts, each with its own dloss: three kernels in a chain before the first product, the last of which reads
+    what the first has written.  Rows without a target in every run of 4096."""
+    x, w, t, b = data(20000, 48, 300, torch.float16, True, ignored, seed=31)
+    dloss = torch.randn(20000, device="cuda") * 2.0 ** (torch.arange(20000, device="cuda") % 16 - 8)
+    for _ in range(3):
+        check(x, w, t, b, "none", dloss)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n,d,v", [(256, 192, 64), (257, 192, 64), (256, 193, 64), (256, 192, 65), (255, 191, 63), (33, 20, 64), (32, 1, 1), (256, 512, 64), (255, 511, 63)])
 def test_small_float_heads(n, d, v):
     """Where one launch takes them and just beyond: every reduction and type of bias, weights that start anywhere, an infinity, a masked
