@@ -448,6 +448,9 @@ int sae_group_norm_backward(const sae_group_norm_desc *desc, const void *dy, con
  *   sum over their number (none: 0 / 0 = NaN).  lse: `rows` floats.  count: one int64, the number of rows that take part.
  * dloss: SAE_REDUCE_NONE: `rows` floats; otherwise one.  g_i = dloss_i, dloss, or dloss / count.
  * lse and count are read by the backward call as the forward call of the same inputs left them.
+ * rest: `rows` floats, what rounding to a float left out of lse (0 where lse is 0; NaN where it is not finite).  With it the gradients are as exact at
+ *   logits of 30000, where a float's last bit is 0.2 % of p, as at small ones.  A backward call without it (NULL, or sae_linear_ce_backward) makes the rows'
+ *   sums again, for a fourth more work; a forward call without it does not store it.
  *
  * All pointers are DEVICE pointers, all work goes to `stream` of the CURRENT device and is asynchronous; nothing is allocated
  * and nothing is kept between calls, which may be captured.
@@ -487,6 +490,14 @@ int sae_linear_ce_forward(const sae_linear_ce_desc *desc, const void *x, const v
 int sae_linear_ce_backward(const sae_linear_ce_desc *desc, const float *dloss, const void *x, const void *weight,
                            const void *bias, const int64_t *target, const float *lse, const int64_t *count, void *dx,
                            void *dweight, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+/* The same with rest behind lse. */
+int sae_linear_ce_forward_with_rest(const sae_linear_ce_desc *desc, const void *x, const void *weight, const void *bias,
+                                    const int64_t *target, float *loss, float *lse, float *rest, int64_t *count,
+                                    void *workspace, size_t workspace_bytes, void *stream);
+int sae_linear_ce_backward_with_rest(const sae_linear_ce_desc *desc, const float *dloss, const void *x, const void *weight,
+                                     const void *bias, const int64_t *target, const float *lse, const float *rest,
+                                     const int64_t *count, void *dx, void *dweight, void *dbias, void *workspace,
+                                     size_t workspace_bytes, void *stream);
 
 /*
  * Orthogonalisation of many matrices.  (What a worker may do to its momentum or its model difference before it is compressed:

@@ -30,6 +30,7 @@ EXPORTS = ["sae_init", "sae_step", "sae_step_host", "sae_get_params", "sae_get_p
            "sae_grads_init", "sae_grads_norm", "sae_grads_clip", "sae_grads_pack", "sae_grads_unpack",
            "sae_grads_last_cuda_error", "sae_grads_destroy", "sae_group_norm_workspace", "sae_group_norm_forward",
            "sae_group_norm_backward", "sae_linear_ce_workspace", "sae_linear_ce_forward", "sae_linear_ce_backward",
+           "sae_linear_ce_forward_with_rest", "sae_linear_ce_backward_with_rest",
            "sae_ortho_init", "sae_ortho_run", "sae_ortho_last_cuda_error", "sae_ortho_destroy"]
 
 TYPE_FLOAT, TYPE_BFLOAT, TYPE_HALF = 0, 1, 2
@@ -147,6 +148,8 @@ def lib():
         L.sae_linear_ce_workspace.restype = i64
         L.sae_linear_ce_forward.argtypes = [C.POINTER(SaeLinearCeDesc)] + [vp] * 8 + [C.c_size_t, vp]
         L.sae_linear_ce_backward.argtypes = [C.POINTER(SaeLinearCeDesc)] + [vp] * 11 + [C.c_size_t, vp]
+        L.sae_linear_ce_forward_with_rest.argtypes = [C.POINTER(SaeLinearCeDesc)] + [vp] * 9 + [C.c_size_t, vp]
+        L.sae_linear_ce_backward_with_rest.argtypes = [C.POINTER(SaeLinearCeDesc)] + [vp] * 12 + [C.c_size_t, vp]
         L.sae_ortho_init.argtypes = [C.POINTER(SaeOrthoConfig), C.POINTER(vp)]
         L.sae_ortho_run.argtypes = [vp] * 5
         L.sae_ortho_last_cuda_error.argtypes = [vp]

@@ -22,39 +22,51 @@ def _reduction(name):
 def linear_cross_entropy_forward(x, weight, target, bias=None, ignore_index=-100, reduction="mean"):
     """The cross entropy of x @ weight.T + bias ([..., classes], never stored) against target [...].
     Returns (loss, lse, count): the loss in float32, of target's shape for "none"; the logarithm of every row's sum of
-    exponentials, 0 for a row whose target is ignore_index; the number of the other rows, int64."""
-    status, loss, lse, count = binding.host().linear_ce_forward(x, weight, target, bias, ignore_index, _reduction(reduction))
+    exponentials, 0 for a row whose target is ignore_index; the number of the other rows, int64.
+    lse.rest is what rounding to float32 left out of lse: the backward call reads it.  A copy of lse does not have it."""
+    loss, lse, rest, count = _forward(x, weight, target, bias, ignore_index, reduction)
+    lse.rest = rest
+    return loss, lse, count
+
+
+def _forward(x, weight, target, bias, ignore_index, reduction):
+    status, *out = binding.host().linear_ce_forward(x, weight, target, bias, ignore_index, _reduction(reduction))
     if status:
         raise SaeError(status, "sae_linear_ce_forward")
-    return loss, lse, count
+    return out
 
 
 def linear_cross_entropy_backward(dloss, x, weight, target, lse, count, bias=None, ignore_index=-100, reduction="mean",
                                   need_x=True, need_weight=True, need_bias=True):
     """The gradients of linear_cross_entropy_forward's loss: (dx, dweight, dbias), None where there is no such input or it is not
-    wanted.  lse and count are what the forward call returned; dloss is float32, of the loss's shape."""
-    status, dx, dweight, dbias = binding.host().linear_ce_backward(dloss, x, weight, target, lse, count, bias, ignore_index,
-                                                                   _reduction(reduction), need_x, need_weight, need_bias)
+    wanted.  lse and count are what the forward call returned; with a copy of lse the rows' sums are made again, for a fourth more work.
+    dloss is float32, of the loss's shape."""
+    return _backward(dloss, x, weight, target, lse, getattr(lse, "rest", None), count, bias, ignore_index, reduction, need_x, need_weight, need_bias)
+
+
+def _backward(dloss, x, weight, target, lse, rest, count, bias, ignore_index, reduction, need_x, need_weight, need_bias):
+    status, *out = binding.host().linear_ce_backward(dloss, x, weight, target, lse, rest, count, bias, ignore_index, _reduction(reduction),
+                                                     need_x, need_weight, need_bias)
     if status:
         raise SaeError(status, "sae_linear_ce_backward")
-    return dx, dweight, dbias
+    return tuple(out)
 
 
 class _LinearCrossEntropy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, target, ignore_index, reduction):
-        loss, lse, count = linear_cross_entropy_forward(x, weight, target, bias, ignore_index, reduction)
-        ctx.save_for_backward(x, weight, bias, target, lse, count)
+        loss, lse, rest, count = _forward(x, weight, target, bias, ignore_index, reduction)
+        ctx.save_for_backward(x, weight, bias, target, lse, rest, count)
         ctx.ignore_index, ctx.reduction = ignore_index, reduction
         return loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dloss):
-        x, weight, bias, target, lse, count = ctx.saved_tensors
+        x, weight, bias, target, lse, rest, count = ctx.saved_tensors
         need = ctx.needs_input_grad
-        return linear_cross_entropy_backward(dloss, x, weight, target, lse, count, bias, ctx.ignore_index, ctx.reduction,
-                                             need[0], need[1], need[2]) + (None, None, None)
+        return _backward(dloss, x, weight, target, lse, rest, count, bias, ctx.ignore_index, ctx.reduction,
+                         need[0], need[1], need[2]) + (None, None, None)
 
 
 def linear_cross_entropy(x, weight, target, bias=None, ignore_index=-100, reduction="mean"):

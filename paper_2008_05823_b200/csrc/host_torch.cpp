@@ -471,29 +471,30 @@ Tensor ce_workspace(const LinearCe& c, int backward, size_t& bytes) {
   return fresh({(int64_t)bytes}, at::kByte, c.x.device());
 }
 
-std::tuple<int, Tensor, Tensor, Tensor> linear_ce_forward(const Tensor& x, const Tensor& weight, const Tensor& target, const Maybe& bias, int64_t ignore,
+std::tuple<int, Tensor, Tensor, Tensor, Tensor> linear_ce_forward(const Tensor& x, const Tensor& weight, const Tensor& target, const Maybe& bias, int64_t ignore,
                                                           int reduction) {
   const LinearCe c = describe_ce(x, weight, target, bias, ignore, reduction);
   c10::cuda::CUDAGuard guard(x.device());
   Tensor loss = fresh(reduction == SAE_REDUCE_NONE ? target.sizes() : at::IntArrayRef{}, at::kFloat, x.device());
-  Tensor lse = fresh(target.sizes(), at::kFloat, x.device()), count = fresh({}, at::kLong, x.device());
+  Tensor lse = fresh(target.sizes(), at::kFloat, x.device()), rest = fresh(target.sizes(), at::kFloat, x.device()), count = fresh({}, at::kLong, x.device());
   size_t bytes;
   Tensor ws = ce_workspace(c, 0, bytes);
-  const int rc = sae_linear_ce_forward(&c.d, c.x.data_ptr(), c.weight.data_ptr(), ptr(bias), (const int64_t*)c.target.data_ptr(), (float*)loss.data_ptr(),
-                                       (float*)lse.data_ptr(), (int64_t*)count.data_ptr(), ws.data_ptr(), bytes,
-                                       c10::cuda::getCurrentCUDAStream(x.get_device()).stream());
-  return {rc, loss, lse, count};
+  const int rc = sae_linear_ce_forward_with_rest(&c.d, c.x.data_ptr(), c.weight.data_ptr(), ptr(bias), (const int64_t*)c.target.data_ptr(), (float*)loss.data_ptr(),
+                                                 (float*)lse.data_ptr(), (float*)rest.data_ptr(), (int64_t*)count.data_ptr(), ws.data_ptr(), bytes,
+                                                 c10::cuda::getCurrentCUDAStream(x.get_device()).stream());
+  return {rc, loss, lse, rest, count};
 }
 
 std::tuple<int, Maybe, Maybe, Maybe> linear_ce_backward(const Tensor& dloss, const Tensor& x, const Tensor& weight, const Tensor& target, const Tensor& lse,
-                                                        const Tensor& count, const Maybe& bias, int64_t ignore, int reduction, bool need_x, bool need_weight,
+                                                        const Maybe& rest, const Tensor& count, const Maybe& bias, int64_t ignore, int reduction, bool need_x, bool need_weight,
                                                         bool need_bias) {
   const LinearCe c = describe_ce(x, weight, target, bias, ignore, reduction);
   c10::cuda::CUDAGuard guard(x.device());
   if (dloss.scalar_type() != at::kFloat || dloss.device() != x.device() || (reduction == SAE_REDUCE_NONE ? dloss.sizes() != target.sizes() : dloss.numel() != 1))
     refuse("dloss must be a float32 tensor of the loss's shape on x's device");
   if (lse.scalar_type() != at::kFloat || lse.device() != x.device() || lse.sizes() != target.sizes() || !lse.is_contiguous() || count.scalar_type() != at::kLong ||
-      count.device() != x.device() || count.numel() != 1)
+      count.device() != x.device() || count.numel() != 1 ||
+      (rest && (rest->scalar_type() != at::kFloat || rest->device() != x.device() || rest->sizes() != target.sizes() || !rest->is_contiguous())))
     refuse("lse and count must be what the forward call returned");
   const Tensor dl = dloss.contiguous();
   Maybe dx, dweight, dbias;
@@ -502,9 +503,9 @@ std::tuple<int, Maybe, Maybe, Maybe> linear_ce_backward(const Tensor& dloss, con
   if (bias && need_bias) dbias = fresh(bias->sizes(), bias->scalar_type(), x.device());
   size_t bytes;
   Tensor ws = ce_workspace(c, 1, bytes);
-  const int rc = sae_linear_ce_backward(&c.d, (const float*)dl.data_ptr(), c.x.data_ptr(), c.weight.data_ptr(), ptr(bias), (const int64_t*)c.target.data_ptr(),
-                                        (const float*)lse.data_ptr(), (const int64_t*)count.data_ptr(), ptr(dx), ptr(dweight), ptr(dbias), ws.data_ptr(), bytes,
-                                        c10::cuda::getCurrentCUDAStream(x.get_device()).stream());
+  const int rc = sae_linear_ce_backward_with_rest(&c.d, (const float*)dl.data_ptr(), c.x.data_ptr(), c.weight.data_ptr(), ptr(bias), (const int64_t*)c.target.data_ptr(),
+                                                  (const float*)lse.data_ptr(), (const float*)ptr(rest), (const int64_t*)count.data_ptr(), ptr(dx), ptr(dweight),
+                                                  ptr(dbias), ws.data_ptr(), bytes, c10::cuda::getCurrentCUDAStream(x.get_device()).stream());
   return {rc, dx, dweight, dbias};
 }
 

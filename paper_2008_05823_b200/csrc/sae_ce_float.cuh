@@ -205,13 +205,13 @@ struct FloatRowArgs {
   const int *index, *at, *counted;
   int64_t room;
   int splits, pitch, classes, bias_type, reduction;
-  // loss
-  float *loss, *lse;
+  // loss (index NULL: lse and rest of the gathered rows alone, for the gradients)
+  float *loss, *lse, *rest;
   float2* runs;                               // [rows][blocks of a row]: maximum, sum
   float* at_z;                                // the target's logit
   unsigned* ticket;
   // p
-  const float *lse_g, *g;
+  const float *lse_g, *rest_g, *g;
   float* p;
 };
 __device__ __forceinline__ float bias_of(const FloatRowArgs& a, int j) {
@@ -285,9 +285,12 @@ __global__ void __launch_bounds__(CF_LOSS_THREADS) k_cf_loss(const __grid_consta
       const float2 run = __ldcg(a.runs + (int64_t)r * blocks + k);
       join_runs(m, s, run.x, run.y);
     }
-    const float loss = logf(s) + (m - z);
-    a.lse[a.index[r]] = m + logf(s);
-    if (a.reduction == SAE_REDUCE_NONE) a.loss[a.index[r]] = loss;
+    float rest;
+    const float loss = logf(s) + (m - z), lse = lse_of(m, s, rest);
+    const int to = a.index ? a.index[r] : r;
+    a.lse[to] = a.index || a.at[r] >= 0 ? lse : z;
+    if (a.rest) a.rest[to] = rest;
+    if (a.loss && a.reduction == SAE_REDUCE_NONE) a.loss[to] = loss;
     sum += loss;
   }
   if (a.reduction == SAE_REDUCE_NONE) return;
@@ -305,7 +308,7 @@ __global__ void __launch_bounds__(CF_THREADS) k_cf_p(const __grid_constant__ Flo
   mma::wait_for_previous();
   const int i = blockIdx.y, j = blockIdx.x * CF_THREADS + threadIdx.x;
   if (i >= *a.counted || j >= a.classes) return;
-  const float p = exp2f((logit_of(a, i, j) - a.lse_g[i]) * LOG2E);
+  const float p = exp2f(log2_p(logit_of(a, i, j), a.lse_g[i], a.rest_g[i] * LOG2E));
   a.p[(int64_t)i * a.pitch + j] = (j == a.at[i] ? p - 1.0f : p) * a.g[i];
 }
 
@@ -348,7 +351,7 @@ struct TinyArgs {
   const int64_t* target;
   int64_t ignore, *count;
   const void* bias;
-  float *loss, *lse;
+  float *loss, *lse, *rest;
   int rows, bias_type, reduction;
 };
 __global__ void __launch_bounds__(CF_THREADS) k_cf_tiny(const __grid_constant__ TinyArgs a) {
@@ -397,7 +400,10 @@ __global__ void __launch_bounds__(CF_THREADS) k_cf_tiny(const __grid_constant__ 
     if (tc == 0 && row0 + r < a.rows) {
       const bool used = at[r] >= 0;
       const float loss = used ? logf(s) + (m - (cls[r] >= 0 ? z_at : __int_as_float(0x7fc00000))) : 0.0f;
-      a.lse[row0 + r] = used ? m + logf(s) : 0.0f;
+      float rest;
+      const float lse = lse_of(m, s, rest);
+      a.lse[row0 + r] = used ? lse : 0.0f;
+      if (a.rest) a.rest[row0 + r] = used ? rest : 0.0f;
       if (a.reduction == SAE_REDUCE_NONE) a.loss[row0 + r] = loss;
       sum += loss;
     }

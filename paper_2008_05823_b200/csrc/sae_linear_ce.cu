@@ -2,7 +2,8 @@
 //
 // forward   rows that take part are gathered (k_ce_rows), then one product kernel makes z = x w' tile by tile and keeps of each row
 //           the running maximum, the sum of exp(z - maximum) and the target's z; the runs are joined (k_ce_join).
-// backward  z is made again, piece by piece of the classes, and leaves the tensor cores as p = (exp(z - lse) - [target]) g in 16 bits;
+// backward  z is made again, to the last bit as it was, piece by piece of the classes, and leaves the tensor cores as p = (exp(z - lse) - [target]) g
+//           in 16 bits; lse is a float and what its rounding left out, so that p of a row adds up to 0 however large its logits are;
 //           p w is added to dx's float sums, p' x is the piece's dweight.  8 N D V operations in all, against 6 with all of z kept.
 //
 // A row without a target costs nothing: the gathered rows are counted on the device, and every kernel goes by that count.  Gathering is
@@ -36,6 +37,15 @@ __device__ __forceinline__ float exp2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+
+// log(sum) + maximum as a float and what that leaves out (the sum's error, exactly).  Behind a logit of 30000 a float's last bit is 0.2 % of p.
+__device__ __forceinline__ float lse_of(float m, float s, float& rest) {
+  const float l = logf(s), lse = m + l, back = lse - m;
+  rest = (m - (lse - back)) + (l - back);
+  return lse;
+}
+// exp(z - lse), the exponent for base 2: both subtractions before they are rounded to much.
+__device__ __forceinline__ float log2_p(float z, float lse, float rest_log2e) { return __fmaf_rn(z - lse, LOG2E, -rest_log2e); }
 
 // ---- pieces and splits ----------------------------------------------------------------------------------------------------
 // Pieces of the classes.  p has room for all rows times `piece` classes; where fewer rows take part, a piece has as many times more classes, up
@@ -101,17 +111,17 @@ struct RowsArgs {
   int* at;                                        // its target (-1: out of range),
   int* counted;                                   // and how many there are: [COUNT_WORDS]
   int64_t* count;                                 // forward: the caller's
-  float *loss, *lse;                              // forward: 0 for rows that take no part (loss NULL: reduced)
+  float *loss, *lse, *rest;                       // forward: 0 for rows that take no part (loss NULL: reduced; rest NULL: not wanted)
   // backward
   Pieces pieces;
   Product product;                                // of a piece, but for what the count gives
   bool both;                                      // dx and dweight in one list
   int product_rows;                               // rows of a tile of it
-  const float *lse_in, *dloss;
+  const float *lse_in, *rest_in, *dloss;
   const int64_t* count_in;
   int reduction;
   float p_scale;
-  float *lse_g, *g, *alpha;                       // of every gathered row: lse, its factor in p;  the factor behind the sums
+  float *lse_g, *rest_g, *g, *alpha;              // of every gathered row: lse and the rest of it, its factor in p;  the factor behind the sums
   const float* g_top;                             // the largest |dloss|, for float16 p
   void* dx;
   // copies beside it
@@ -247,19 +257,22 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_rows(const __grid_constant__ 
       a.at[to] = cls;
       if constexpr (BACKWARD) {
         a.lse_g[to] = cls < 0 ? __int_as_float(0x7fc00000) : a.lse_in[r];
+        a.rest_g[to] = a.rest_in ? a.rest_in[r] : 0.0f;
         float f = a.reduction == SAE_REDUCE_NONE ? a.dloss[r] / (a.g_top ? *a.g_top : 1.0f) : 1.0f;
         a.g[to] = f * a.p_scale;
       }
     } else if (r < a.rows) {
       if constexpr (!BACKWARD) {
         a.lse[r] = 0;
+        if (a.rest) a.rest[r] = 0;
         if (a.loss) a.loss[r] = 0;
       }
     }
     if (b + 1 == a.row_blocks && lane == 0) {
       const int n = base + __popc(mask);
       *a.counted = n;
-      if constexpr (!BACKWARD) { *a.count = n; a.counted[COUNT_TICKET] = 0; }
+      a.counted[COUNT_TICKET] = 0;
+      if constexpr (!BACKWARD) *a.count = n;
       else {
         float f = 1.0f;
         if (n == 0) f = 0.0f;                                  // sums of nothing
@@ -420,9 +433,9 @@ struct LossJob : mma::Plain {
 
 struct JoinArgs {
   const float2* runs;
-  const int *counted, *index, *at;
+  const int *counted, *index, *at;            // index NULL: lse and rest of the gathered rows, for the gradients
   const float* at_z;
-  float *loss, *lse;
+  float *loss, *lse, *rest;
   double* sums;
   unsigned* ticket;
   int rows, wide, clusters, reduction;
@@ -458,11 +471,14 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_join(const __grid_constant__ 
       m = top;
     }
     if (lane == 0) {
-      const float lse = m + logf(s), z = a.at[i] >= 0 ? a.at_z[i] : __int_as_float(0x7fc00000);
+      float rest;
+      const float lse = lse_of(m, s, rest), z = a.at[i] >= 0 ? a.at_z[i] : __int_as_float(0x7fc00000);
       // log s + (m - z): the same value with one rounding less where lse is large
       const float loss = logf(s) + (m - z);
-      a.lse[a.index[i]] = lse;
-      if (a.reduction == SAE_REDUCE_NONE) a.loss[a.index[i]] = loss;
+      const int to = a.index ? a.index[i] : i;
+      a.lse[to] = a.index || a.at[i] >= 0 ? lse : z;
+      if (a.rest) a.rest[to] = rest;
+      if (a.loss && a.reduction == SAE_REDUCE_NONE) a.loss[to] = loss;
       sum += loss;
     }
   }
@@ -494,6 +510,7 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_join(const __grid_constant__ 
 // ---- the gradients --------------------------------------------------------------------------------------------------------
 // p of one piece of the classes.
 struct GradJob : mma::Plain {
+  static constexpr bool LONG = true;             // (as LossJob: lse goes with the very z that it was made from)
   int cols;
   bool bfloat;
   mma::Segments seg;
@@ -501,7 +518,7 @@ struct GradJob : mma::Plain {
   const int* counted;
   Pieces pieces;
   int classes, features, rows, index;            // index: of the piece
-  const float *bias, *lse, *g;
+  const float *bias, *lse, *rest, *g;
   const int* at;
   unsigned short* p;
   int64_t p_plane;
@@ -543,7 +560,7 @@ struct GradJob : mma::Plain {
     __device__ __forceinline__ void tile(const mma::Tile& t, const mma::Sums& sums) {
       const int r = t.row + row;
       const bool used = r < l.count;
-      const float lse = used ? job.lse[r] : 0.0f, g = used ? job.g[r] : 0.0f;
+      const float lse = used ? job.lse[r] : 0.0f, rest = used ? job.rest[r] * LOG2E : 0.0f, g = used ? job.g[r] : 0.0f;
       const int cls = used ? job.at[r] - l.start : -1;
       const int width = job.cols / 2;
       for (int c = half * width; c < (half + 1) * width; c += 32) {
@@ -561,7 +578,7 @@ struct GradJob : mma::Plain {
           for (int i = 0; i < 32; ++i) if (cc + i >= job.classes) z[i] = __int_as_float(0xff800000);
         }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) z[i] = exp2_approx((z[i] - lse) * LOG2E);
+        for (int i = 0; i < 32; ++i) z[i] = exp2_approx(log2_p(z[i], lse, rest));
         const unsigned mine = (unsigned)(cls - col);
         if (mine < 32u) {
 #pragma unroll
@@ -849,6 +866,10 @@ int float_splits(int64_t tiles, int64_t depth, int most, int sms) {
   return (int)std::max<int64_t>(1, s);
 }
 
+// Whether the loss of a float head takes one launch in place of three.  A block has all k of its rows there, at 1.06 us for 32: 128 x 64 x 10 6.4 us
+// (11.6 with three), 256 x 512 x 64 21.7 (12.8); they meet at 7 blocks of k.
+bool in_one_launch(const sae_linear_ce_desc* d) { return d->rows && d->rows <= 8 * CF_ROWS && d->classes <= CF_COLS && d->features <= 6 * CF_K; }
+
 struct TileShape { int cg, cols; };
 
 // The tile shape of a product of `depth` k: waves of tiles over the SMs (or pairs) times what a tile costs for each k.  A block of 64 k takes a pair
@@ -904,7 +925,7 @@ struct CePlan {
   bool in_float;
   int z_splits, dx_splits, dw_splits, z_pitch, dx_pitch, dw_pitch;
   size_t fz, fdx, fdw;
-  size_t xg, wg, bias, index, at, at_z, counted, before, runs, sums, lse_g, g, alpha, top, p, bias_sums, dx_sums, bytes;
+  size_t xg, wg, bias, index, at, at_z, counted, before, runs, sums, lse_g, rest_g, g, alpha, top, p, bias_sums, dx_sums, bytes;
 };
 
 // Classes of a piece, in blocks of 256: as many as the bytes allow, or fewer where the tiles of its products then come out as
@@ -943,12 +964,14 @@ CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward,
     p.counted = take(COUNT_WORDS * 4);
     p.before = take(d->rows > CE_SCAN_ROWS ? up(d->rows, CE_COUNT_ROWS) / CE_COUNT_ROWS * 4 : 0);
     p.z_pitch = (int)up(d->classes, 4);
-    p.z_splits = float_splits((d->classes + CF_COLS - 1) / CF_COLS, d->features, 8, sms);
+    // (not split where the loss was made in one launch: the gradients take the very z that lse was made from)
+    p.z_splits = in_one_launch(d) ? 1 : float_splits((d->classes + CF_COLS - 1) / CF_COLS, d->features, 8, sms);
     p.fz = take((int64_t)p.z_splits * n * p.z_pitch * 4);
     p.at_z = take(n * 4);
     p.sums = take(n * ((d->classes + CF_LOSS_CLASSES - 1) / CF_LOSS_CLASSES) * 8);
     if (backward) {
       p.lse_g = take(n * 4);
+      p.rest_g = take(n * 4);
       p.g = take(n * 4);
       p.alpha = take(4);
       p.p = take(n * p.z_pitch * 4);
@@ -970,14 +993,14 @@ CePlan make_plan(const sae_linear_ce_desc* d, const void* weight, bool backward,
   p.counted = take(COUNT_WORDS * 4);
   p.before = take(d->rows > CE_SCAN_ROWS ? up(d->rows, CE_COUNT_ROWS) / CE_COUNT_ROWS * 4 : 0);
   p.z = tile_shape(d->rows, d->classes, d->features, 1, p.parts, sms);
-  if (!backward) {
-    const int rows = 128 * p.z.cg, clusters = sms / p.z.cg;
-    const int64_t blocks = up(p.rows, rows) / rows;
-    p.at_z = take(p.rows * 4);
-    p.runs = take((clusters + 2 * blocks + 2) * 2 * rows * (int64_t)sizeof(float2));
-    p.sums = take(up(p.rows, CE_ROWS) / CE_ROWS * 8);
-  } else {
+  const int z_rows = 128 * p.z.cg, z_clusters = sms / p.z.cg;
+  const int64_t z_blocks = up(p.rows, z_rows) / z_rows;
+  p.at_z = take(p.rows * 4);
+  p.runs = take((z_clusters + 2 * z_blocks + 2) * 2 * z_rows * (int64_t)sizeof(float2));
+  p.sums = take(up(p.rows, CE_ROWS) / CE_ROWS * 8);
+  if (backward) {
     p.lse_g = take(p.rows * 4);
+    p.rest_g = take(p.rows * 4);
     p.g = take(p.rows * 4);
     p.alpha = take(4);
     p.top = take(4);
@@ -1127,13 +1150,15 @@ FloatRowArgs float_rows(const sae_linear_ce_desc* d, const CePlan& p, const Rows
   return r;
 }
 
-int float_forward(const sae_linear_ce_desc* d, const CePlan& p, RowsArgs& a, float* loss, float* lse, char* ws, cudaStream_t st) {
-  // One launch in place of three.  A block has all k of its rows there, at 1.06 us for 32: 128 x 64 x 10 6.4 us (11.6 with three), 256 x 512 x 64
-  // 21.7 (12.8); they meet at 7 blocks of k.
-  if (d->rows && d->rows <= 8 * CF_ROWS && d->classes <= CF_COLS && d->features <= 6 * CF_K) {
+int float_sums(const sae_linear_ce_desc* d, const FloatRowArgs& r, cudaStream_t st) {
+  return launch(k_cf_loss, dim3((unsigned)std::max<int64_t>(1, d->rows), (unsigned)((d->classes + CF_LOSS_CLASSES - 1) / CF_LOSS_CLASSES)), CF_LOSS_THREADS, st, false, r);
+}
+
+int float_forward(const sae_linear_ce_desc* d, const CePlan& p, RowsArgs& a, float* loss, char* ws, cudaStream_t st) {
+  if (in_one_launch(d)) {
     TinyArgs t = {};
     t.f = float_args(d, p, a, ws);
-    t.target = a.target; t.ignore = a.ignore; t.count = a.count; t.bias = a.bias; t.bias_type = d->bias_type; t.loss = loss; t.lse = lse; t.rows = (int)d->rows;
+    t.target = a.target; t.ignore = a.ignore; t.count = a.count; t.bias = a.bias; t.bias_type = d->bias_type; t.loss = loss; t.lse = a.lse; t.rest = a.rest; t.rows = (int)d->rows;
     t.reduction = d->reduction;
     static std::atomic<unsigned long long> ready{0};
     if (!allow_shared((const void*)k_cf_tiny, FloatTile<CF_Z>::BYTES, ready)) return SAE_ERR_CUDA;
@@ -1153,9 +1178,8 @@ int float_forward(const sae_linear_ce_desc* d, const CePlan& p, RowsArgs& a, flo
   int rc = gather<false>(d, p, a, ws, st);
   if (rc == SAE_OK && d->rows) rc = float_product<CF_Z>(float_args(d, p, a, ws), d->rows, d->classes, p.z_splits, (float*)(ws + p.fz), d->rows, p.z_pitch, st);
   FloatRowArgs r = float_rows(d, p, a, ws);
-  r.loss = loss; r.lse = lse;
-  if (rc == SAE_OK) rc = launch(k_cf_loss, dim3((unsigned)std::max<int64_t>(1, d->rows), (unsigned)((d->classes + CF_LOSS_CLASSES - 1) / CF_LOSS_CLASSES)), CF_LOSS_THREADS, st, false, r);
-  return rc;
+  r.loss = loss; r.lse = a.lse; r.rest = a.rest;
+  return rc == SAE_OK ? float_sums(d, r, st) : rc;
 }
 
 int float_backward(const sae_linear_ce_desc* d, const CePlan& p, RowsArgs& a, void* dx, void* dweight, void* dbias, char* ws, cudaStream_t st) {
@@ -1163,7 +1187,12 @@ int float_backward(const sae_linear_ce_desc* d, const CePlan& p, RowsArgs& a, vo
   FloatArgs f = float_args(d, p, a, ws);
   if (rc == SAE_OK && d->rows) rc = float_product<CF_Z>(f, d->rows, d->classes, p.z_splits, (float*)(ws + p.fz), d->rows, p.z_pitch, st);
   FloatRowArgs r = float_rows(d, p, a, ws);
-  r.lse_g = a.lse_g; r.g = a.g; r.p = (float*)(ws + p.p);
+  r.lse_g = a.lse_g; r.rest_g = a.rest_g; r.g = a.g; r.p = (float*)(ws + p.p);
+  if (rc == SAE_OK && d->rows && !a.rest_in) {     // z is there: its sums once more
+    FloatRowArgs again = r;
+    again.index = nullptr; again.lse = a.lse_g; again.rest = a.rest_g; again.reduction = SAE_REDUCE_NONE;
+    rc = float_sums(d, again, st);
+  }
   if (rc == SAE_OK && d->rows) rc = launch(k_cf_p, dim3((unsigned)((d->classes + CF_THREADS - 1) / CF_THREADS), (unsigned)d->rows), CF_THREADS, st, false, r);
   FloatSumArgs s = {};
   s.counted = a.counted; s.alpha = a.alpha; s.features = a.features; s.bias_type = d->bias_type;
@@ -1185,6 +1214,23 @@ int float_backward(const sae_linear_ce_desc* d, const CePlan& p, RowsArgs& a, vo
   return rc;
 }
 
+// The rows' sums of exponentials, from gathered rows: loss, lse and the rest of it; without a loss, lse and rest of the gathered rows.
+int sums_of_rows(const sae_linear_ce_desc* d, const CePlan& p, const RowsArgs& a, const CUtensorMap& x, const CUtensorMap& w, float* loss, float* lse, float* rest, char* ws, int sms, cudaStream_t st) {
+  LossJob job = {};
+  job.x = x; job.w = w;
+  job.cols = p.z.cols; job.bfloat = d->type != SAE_TYPE_HALF; job.seg = segments(p.parts);
+  job.counted = a.counted; job.classes = a.classes; job.features = a.features; job.rows = 128 * p.z.cg;
+  job.bias = d->has_bias ? a.bias_out : nullptr; job.at = a.at; job.at_z = (float*)(ws + p.at_z); job.runs = (float2*)(ws + p.runs);
+  const int64_t wide = up(d->classes, p.z.cols) / p.z.cols, tiles = up(d->rows, job.rows) / job.rows * wide;
+  const int rc = tiles ? products(job, p.z, tiles, sms, st) : SAE_OK;
+  if (rc != SAE_OK) return rc;
+  JoinArgs j = {};
+  j.runs = job.runs; j.counted = a.counted; j.index = loss ? a.index : nullptr; j.at = a.at; j.at_z = job.at_z; j.loss = loss; j.lse = lse; j.rest = rest; j.sums = (double*)(ws + p.sums);
+  j.ticket = (unsigned*)a.counted + COUNT_TICKET; j.rows = job.rows; j.wide = (int)wide; j.reduction = loss ? d->reduction : SAE_REDUCE_NONE;
+  j.clusters = (int)std::min<int64_t>(std::max<int64_t>(1, tiles), sms / p.z.cg);
+  return launch(k_ce_join, std::max<int64_t>(1, up(d->rows, CE_ROWS) / CE_ROWS), CE_THREADS, st, false, j);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1195,12 +1241,12 @@ int64_t sae_linear_ce_workspace(const sae_linear_ce_desc* d, const void* weight,
   return sms < 2 ? -1 : (int64_t)make_plan(d, weight, backward != 0, sms).bytes;
 }
 
-int sae_linear_ce_forward(const sae_linear_ce_desc* d, const void* x, const void* weight, const void* bias, const int64_t* target, float* loss,
-                          float* lse, int64_t* count, void* workspace, size_t workspace_bytes, void* stream) {
+int sae_linear_ce_forward_with_rest(const sae_linear_ce_desc* d, const void* x, const void* weight, const void* bias, const int64_t* target, float* loss,
+                                    float* lse, float* rest, int64_t* count, void* workspace, size_t workspace_bytes, void* stream) {
   if (!desc_ok(d) || !weight || !count || (d->rows && (!x || !target || !lse)) || (!loss && (d->rows || d->reduction != SAE_REDUCE_NONE)) || (d->has_bias && !bias) || !workspace) return SAE_ERR_INVALID_ARG;
   const int es = elem_bytes(d->type);
   if (!aligned_to(x, es) || !aligned_to(weight, es) || !aligned_to(bias, d->has_bias ? elem_bytes(d->bias_type) : 1) || !aligned_to(target, 8) || !aligned_to(loss, 4) ||
-      !aligned_to(lse, 4) || !aligned_to(count, 8) || !aligned_to(workspace, 256)) return SAE_ERR_INVALID_ARG;
+      !aligned_to(lse, 4) || !aligned_to(rest, 4) || !aligned_to(count, 8) || !aligned_to(workspace, 256)) return SAE_ERR_INVALID_ARG;
   const int sms = device_sms();
   if (sms < 2) return SAE_ERR_CUDA;
   const CePlan p = make_plan(d, weight, false, sms);
@@ -1208,33 +1254,33 @@ int sae_linear_ce_forward(const sae_linear_ce_desc* d, const void* x, const void
   cudaStream_t st = (cudaStream_t)stream;
   char* ws = (char*)workspace;
   RowsArgs a = rows_args(d, p, x, weight, d->has_bias ? bias : nullptr, target, ws, sms);
-  a.count = count; a.lse = lse; a.loss = d->reduction == SAE_REDUCE_NONE ? loss : nullptr;
-  if (p.in_float) return float_forward(d, p, a, loss, lse, ws, st);
-  LossJob job = {};
-  if (!maps(d, p, weight, ws, &job.x, &job.w)) return SAE_ERR_CUDA;
-  int rc = gather<false>(d, p, a, ws, st);
-  if (rc != SAE_OK) return rc;
-  job.cols = p.z.cols; job.bfloat = d->type != SAE_TYPE_HALF; job.seg = segments(p.parts);
-  job.counted = a.counted; job.classes = a.classes; job.features = a.features; job.rows = 128 * p.z.cg;
-  job.bias = d->has_bias ? a.bias_out : nullptr; job.at = a.at; job.at_z = (float*)(ws + p.at_z); job.runs = (float2*)(ws + p.runs);
-  const int64_t wide = up(d->classes, p.z.cols) / p.z.cols, tiles = up(d->rows, job.rows) / job.rows * wide;
-  if (tiles) rc = products(job, p.z, tiles, sms, st);
-  if (rc != SAE_OK) return rc;
-  JoinArgs j = {};
-  j.runs = job.runs; j.counted = a.counted; j.index = a.index; j.at = a.at; j.at_z = job.at_z; j.loss = loss; j.lse = lse; j.sums = (double*)(ws + p.sums);
-  j.ticket = (unsigned*)a.counted + COUNT_TICKET; j.rows = job.rows; j.wide = (int)wide; j.reduction = d->reduction;
-  j.clusters = (int)std::min<int64_t>(std::max<int64_t>(1, tiles), sms / p.z.cg);
-  return launch(k_ce_join, std::max<int64_t>(1, up(d->rows, CE_ROWS) / CE_ROWS), CE_THREADS, st, false, j);
+  a.count = count; a.lse = lse; a.rest = rest; a.loss = d->reduction == SAE_REDUCE_NONE ? loss : nullptr;
+  if (p.in_float) return float_forward(d, p, a, loss, ws, st);
+  CUtensorMap xm, wm;
+  if (!maps(d, p, weight, ws, &xm, &wm)) return SAE_ERR_CUDA;
+  const int rc = gather<false>(d, p, a, ws, st);
+  return rc == SAE_OK ? sums_of_rows(d, p, a, xm, wm, loss, lse, rest, ws, sms, st) : rc;
+}
+
+int sae_linear_ce_forward(const sae_linear_ce_desc* d, const void* x, const void* weight, const void* bias, const int64_t* target, float* loss,
+                          float* lse, int64_t* count, void* workspace, size_t workspace_bytes, void* stream) {
+  return sae_linear_ce_forward_with_rest(d, x, weight, bias, target, loss, lse, nullptr, count, workspace, workspace_bytes, stream);
 }
 
 int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, const void* x, const void* weight, const void* bias, const int64_t* target,
                            const float* lse, const int64_t* count, void* dx, void* dweight, void* dbias, void* workspace, size_t workspace_bytes,
                            void* stream) {
+  return sae_linear_ce_backward_with_rest(d, dloss, x, weight, bias, target, lse, nullptr, count, dx, dweight, dbias, workspace, workspace_bytes, stream);
+}
+
+int sae_linear_ce_backward_with_rest(const sae_linear_ce_desc* d, const float* dloss, const void* x, const void* weight, const void* bias, const int64_t* target,
+                                     const float* lse, const float* rest, const int64_t* count, void* dx, void* dweight, void* dbias, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
   if (!desc_ok(d) || !weight || !count || (d->rows && (!x || !target || !lse)) || (!dloss && (d->rows || d->reduction != SAE_REDUCE_NONE)) || (d->has_bias && !bias) || (dbias && !d->has_bias) ||
       !workspace) return SAE_ERR_INVALID_ARG;
   const int es = elem_bytes(d->type), bs = d->has_bias ? elem_bytes(d->bias_type) : 1;
   if (!aligned_to(x, es) || !aligned_to(weight, es) || !aligned_to(bias, bs) || !aligned_to(target, 8) || !aligned_to(dloss, 4) || !aligned_to(lse, 4) ||
-      !aligned_to(count, 8) || !aligned_to(dx, es) || !aligned_to(dweight, es) || !aligned_to(dbias, bs) || !aligned_to(workspace, 256)) return SAE_ERR_INVALID_ARG;
+      !aligned_to(rest, 4) || !aligned_to(count, 8) || !aligned_to(dx, es) || !aligned_to(dweight, es) || !aligned_to(dbias, bs) || !aligned_to(workspace, 256)) return SAE_ERR_INVALID_ARG;
   const int sms = device_sms();
   if (sms < 2) return SAE_ERR_CUDA;
   const CePlan p = make_plan(d, weight, true, sms);
@@ -1243,8 +1289,8 @@ int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, cons
   if (!dx && !dweight && !dbias) return SAE_OK;
   char* ws = (char*)workspace;
   RowsArgs a = rows_args(d, p, x, weight, d->has_bias ? bias : nullptr, target, ws, sms);
-  a.lse_in = lse; a.dloss = dloss; a.count_in = count; a.dx = dx;
-  a.lse_g = (float*)(ws + p.lse_g); a.g = (float*)(ws + p.g); a.alpha = (float*)(ws + p.alpha);
+  a.lse_in = lse; a.rest_in = rest; a.dloss = dloss; a.count_in = count; a.dx = dx;
+  a.lse_g = (float*)(ws + p.lse_g); a.rest_g = (float*)(ws + p.rest_g); a.g = (float*)(ws + p.g); a.alpha = (float*)(ws + p.alpha);
   a.p_scale = d->type == SAE_TYPE_HALF ? 32768.0f : 1.0f;
   if (p.in_float) return float_backward(d, p, a, dx, dweight, dbias, ws, st);
   GradJob g = {};
@@ -1255,9 +1301,10 @@ int sae_linear_ce_backward(const sae_linear_ce_desc* d, const float* dloss, cons
     if (!mma::encode_map(&job.p[i], ws + p.p, bfloat, (int64_t)p.pieces.piece * (i + 1), p.rows / (i + 1), p.parts, (int64_t)p.pieces.piece * (i + 1), p.rows * p.pieces.piece))
       return SAE_ERR_CUDA;
   int rc = gather<true>(d, p, a, ws, st);
+  if (rc == SAE_OK && !rest && d->rows) rc = sums_of_rows(d, p, a, g.x, g.w, nullptr, a.lse_g, a.rest_g, ws, sms, st);
   g.cols = p.z.cols; g.bfloat = bfloat; g.seg = segments(p.parts);
   g.counted = a.counted; g.classes = a.classes; g.features = a.features; g.rows = 128 * p.z.cg;
-  g.bias = d->has_bias ? a.bias_out : nullptr; g.lse = a.lse_g; g.g = a.g; g.at = a.at;
+  g.bias = d->has_bias ? a.bias_out : nullptr; g.lse = a.lse_g; g.rest = a.rest_g; g.g = a.g; g.at = a.at;
   g.p = (unsigned short*)(ws + p.p); g.p_plane = p.rows * p.pieces.piece; g.type = d->type; g.pieces = p.pieces;
   g.scaled = d->reduction == SAE_REDUCE_NONE || a.p_scale != 1.0f;
   g.bias_sums = dbias ? (float*)(ws + p.bias_sums) : nullptr;

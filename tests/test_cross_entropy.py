@@ -58,6 +58,14 @@ def test_null_and_misaligned_pointers_are_refused():
     assert L.sae_linear_ce_backward(C.byref(d), *args, 1 << 30, None) == sb.ERR_INVALID_ARG
 
 
+def test_misaligned_rests_are_refused():
+    L, p, odd = sb.lib(), C.c_void_p(256), C.c_void_p(257)
+    d = desc()
+    assert L.sae_linear_ce_forward_with_rest(C.byref(d), p, p, None, p, p, p, odd, p, p, 1 << 30, None) == sb.ERR_INVALID_ARG
+    assert L.sae_linear_ce_backward_with_rest(C.byref(d), p, p, p, None, p, p, odd, p, p, p, None, p, 1 << 30, None) == sb.ERR_INVALID_ARG
+    assert L.sae_linear_ce_backward_with_rest(C.byref(d), p, p, p, None, p, None, p, p, p, p, None, p, 1 << 30, None) == sb.ERR_INVALID_ARG
+
+
 def test_module_arguments():
     with pytest.raises(ValueError):
         ce.LinearCrossEntropy(0, 3)
@@ -434,6 +442,96 @@ def test_logits_far_apart():
     loss = ce.linear_cross_entropy_forward(x, w, t, reduction="none")[0]
     assert abs(float(loss[0]) - 64.0 * 512 - math.log(2)) <= 64.0 * 512 * 2.0 ** -22
     assert float(loss[1]) == 64.0 * 512 and float(loss[3]) == 512 * 2.0 ** 100
+
+
+def gradients(x, w, t, b, reduction, dloss, how):
+    """By the two calls, with lse as it came, or as a copy; and by autograd."""
+    if how == "autograd":
+        p = [None if a is None else a.clone().requires_grad_() for a in (x, w, b)]
+        loss = ce.linear_cross_entropy(p[0], p[1], t, p[2], reduction=reduction)
+        grads = torch.autograd.grad(loss, [a for a in p if a is not None], dloss)
+        return tuple(grads) + (None,) * (3 - len(grads))
+    _, lse, count = ce.linear_cross_entropy_forward(x, w, t, b, reduction=reduction)
+    return ce.linear_cross_entropy_backward(dloss, x, w, t, lse.clone() if how == "copy" else lse, count, b, reduction=reduction)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("how", ["calls", "autograd", "copy"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d,v", [(1, 8, 50), (70, 20, 64), (300, 24, 1000), (600, 40, 3000)])
+@pytest.mark.parametrize("offset", [256.0, 2992.0, 29952.0])
+def test_gradients_at_large_logits(offset, n, d, v, dtype, how):
+    """All logits of a row moved by the same number: the gradients are those without it, and so is what they may be off.  x and w are multiples
+    of 1/4 and 1/8, offsets and their sums multiples of 1/32 below 2^15: every logit is exact in 20 bits.  Half of the rows have the largest logit's class
+    for a target: there p - 1 is a small difference."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.randint(-16, 17, (n, d), device="cuda", generator=gen).div(4).to(DTYPES[dtype])
+    w = torch.randint(-16, 17, (v, d), device="cuda", generator=gen).div(8).to(DTYPES[dtype])
+    b = torch.randint(-32, 33, (v,), device="cuda", generator=gen).div(32)
+    x[:, 0], w[:, 0] = 1, offset
+    t = torch.randint(v, (n,), device="cuda", generator=gen)
+    t[::2] = (x[:, 1:].double() @ w[:, 1:].double().t() + b.double()).argmax(1)[::2]
+    dloss = torch.rand(n, device="cuda", generator=gen) + 0.5
+    e = Exact(x[:, 1:], w[:, 1:], t, b, "none", dloss)
+    dx, dw, db = gradients(x, w, t, b, "none", dloss, how)
+    near(dx[:, 1:], e.dx, e.dx_off, "dx")
+    near(dw[:, 1:], e.dw, e.dw_off, "dweight")
+    near(db, e.db, e.db_off + 2.0 ** -24 * e.db.abs(), "dbias")
+
+
+@pytest.mark.gpu
+def test_the_rest_of_lse():
+    """What comes beside lse: a float's half step at most, their sum the exact value (log of a sum of 1000 terms within 2^-20, on exact logits); 0 where
+    lse is; refused where it is none of this call's."""
+    x, w, t, _ = data(100, 8, 1000, torch.bfloat16, False, 0.3)
+    x, w = (x * 4).round() / 4, (w * 8).round() / 8
+    x[:, 0], w[:, 0] = 1, 29952
+    _, lse, count = ce.linear_cross_entropy_forward(x, w, t)
+    want = torch.where(t != IGNORE, torch.logsumexp(x.double() @ w.double().t(), 1), 0.0)
+    assert float((lse.double() + lse.rest.double() - want).abs().max()) <= 2.0 ** -20
+    assert float(lse.rest.abs().max()) <= 2.0 ** -10 and not lse.rest[t == IGNORE].any()
+    one = torch.ones((), device="cuda")
+    whole = lse.rest
+    for bad in (whole[:50], whole.double(), whole.cpu(), whole.repeat(2)[::2]):
+        lse.rest = bad
+        with pytest.raises(ValueError):
+            ce.linear_cross_entropy_backward(one, x, w, t, lse, count)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("how", ["calls", "autograd", "copy"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [3, 700])
+def test_gradients_of_tied_classes(n, dtype, how):
+    """Two classes at 2^25, 3998 at 0: p is 1/2 and 1/2 (half a step of the type and the few roundings of a softmax)."""
+    x, w = torch.zeros((n, 16), device="cuda", dtype=DTYPES[dtype]), torch.zeros((4000, 16), device="cuda", dtype=DTYPES[dtype])
+    x[:, 0], w[5, 0], w[3007, 0] = 4096, 8192, 8192
+    w[5, 1], w[3007, 2] = 1, 1
+    t = torch.full((n,), 5, device="cuda")
+    dx = gradients(x, w, t, None, "sum", torch.tensor(1.0, device="cuda"), how)[0]
+    want = torch.zeros_like(dx[0], dtype=torch.float64)
+    want[1], want[2] = -0.5, 0.5
+    assert float((dx.double() - want)[:, 1:].abs().max()) <= 2.0 ** -20
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("how", ["calls", "autograd", "copy"])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,d,v", [(1, 100, 60), (7, 192, 64), (256, 192, 64), (40, 700, 500), (300, 769, 900), (700, 1100, 2000), (2000, 2500, 700)])
+def test_p_of_a_row_adds_up_to_nothing(n, d, v, dtype, how):
+    """Logits of tens of thousands whose sums are not exact: the backward pass has to meet the logits that lse was made from, to the last bit.
+    A feature that is 0 in x and 1 in every class has dx = the sum of a row's p, which is 0.  The softmax is one class (differences of thousands), so
+    that is p of it and of the target, each off by half a step of the type and 2^-21 of its own, and the largest sum of exponentials by
+    (v / 64 + 64) 2^-24."""
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    x = torch.randn((n, d), device="cuda", generator=gen).to(DTYPES[dtype])
+    w = (torch.randn((v, d), device="cuda", generator=gen) * (20000 / math.sqrt(d))).to(DTYPES[dtype])
+    x[:, d - 1], w[:, d - 1] = 0, 1
+    t = torch.randint(v, (n,), device="cuda", generator=gen)
+    t[::2] = (x.double() @ w.double().t()).argmax(1)[::2]
+    dx = gradients(x, w, t, None, "none", torch.ones(n, device="cuda"), how)[0]
+    u = 0.0 if dtype == "f32" else torch.finfo(DTYPES[dtype]).eps / 2
+    assert float(dx[:, d - 1].abs().max()) <= 2 * (u + 2 * (2.0 ** -21 + (v / 64 + 64) * 2.0 ** -24))
 
 
 @pytest.mark.gpu
