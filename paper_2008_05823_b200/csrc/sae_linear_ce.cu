@@ -327,7 +327,8 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_rows(const __grid_constant__ 
 // Runs of tiles: row blocks one after another, each over all classes; a cluster takes an equal share of this list and leaves one run
 // (maximum, sum) for each row block that it touches.
 struct LossJob : mma::Plain {
-  static constexpr bool LONG = true;
+  static constexpr int run = mma::JOIN_LONG;
+  bool joins() const { return features > run * mma::BLOCK_K; }
   int cols;
   bool bfloat;
   mma::Segments seg;
@@ -510,7 +511,8 @@ __global__ void __launch_bounds__(CE_THREADS) k_ce_join(const __grid_constant__ 
 // ---- the gradients --------------------------------------------------------------------------------------------------------
 // p of one piece of the classes.
 struct GradJob : mma::Plain {
-  static constexpr bool LONG = true;             // (as LossJob: lse goes with the very z that it was made from)
+  static constexpr int run = LossJob::run;       // (lse goes with the very z that it was made from)
+  bool joins() const { return features > run * mma::BLOCK_K; }
   int cols;
   bool bfloat;
   mma::Segments seg;
@@ -634,6 +636,8 @@ struct GradJob : mma::Plain {
 // dx's sums (p w, float, added up over the pieces) and dweight of a piece (p' x): one list of tiles, the longer ones first, or either alone.
 struct ProductJob : mma::Plain {
   static constexpr int STAGING = mma::SQUARE_BYTES;
+  int run, longest;               // blocks of k: of a sum, most of a tile as far as the host knows
+  bool joins() const { return longest > run; }
   int cols;
   bool bfloat;
   mma::Segments seg;
@@ -655,6 +659,9 @@ struct ProductJob : mma::Plain {
   const float* alpha;
 
   struct Local { int first, step, count, times, start, width, dx_blocks, splits, dx_tiles, dw_blocks, dw_tiles; bool dx_first; };
+  __device__ __forceinline__ bool joined(const Local& l) const {
+    return (dx && l.width > l.splits * (run * mma::BLOCK_K)) || (dweight && l.count > dw_splits * (run * mma::BLOCK_K));
+  }
   __device__ __forceinline__ Local begin(const Shared&, int cluster, int clusters) const {
     Local l = {};
     l.first = cluster; l.step = clusters; l.count = *counted; l.splits = 1;
@@ -1308,6 +1315,7 @@ int sae_linear_ce_backward_with_rest(const sae_linear_ce_desc* d, const float* d
   g.p = (unsigned short*)(ws + p.p); g.p_plane = p.rows * p.pieces.piece; g.type = d->type; g.pieces = p.pieces;
   g.scaled = d->reduction == SAE_REDUCE_NONE || a.p_scale != 1.0f;
   g.bias_sums = dbias ? (float*)(ws + p.bias_sums) : nullptr;
+  job.run = bfloat ? mma::JOIN_BFLOAT : mma::JOIN_HALF;
   job.bfloat = bfloat; job.seg = g.seg; job.w = g.w; job.x = g.x; job.counted = a.counted; job.pieces = p.pieces; job.features = a.features; job.classes = a.classes;
   job.dx_sums = (float*)(ws + p.dx_sums); job.dw_sums = (float*)(ws + p.dw_sums); job.sums_pitch = p.sums_pitch; job.dw_splits = p.dw_splits;
   job.out = dweight; job.type = d->type; job.alpha = a.alpha; job.whole_rows = aligned_to(dweight, 32) && d->features * es % 32 == 0;
@@ -1316,6 +1324,7 @@ int sae_linear_ce_backward_with_rest(const sae_linear_ce_desc* d, const float* d
   const auto product = [&](const TileShape& s, bool for_x, bool for_weight) {
     job.cols = s.cols; job.rows = 128 * s.cg; job.across = across(s); job.dx = for_x; job.dweight = for_weight;
     const int64_t classes = std::min<int64_t>((int64_t)p.pieces.piece * p.pieces.most, d->classes);
+    job.longest = (int)(std::max(for_x ? classes : 0, for_weight ? d->rows / p.dw_splits : 0) / mma::BLOCK_K) + 1;
     return products(job, s, for_x ? sms : up(classes, job.rows) / job.rows * job.across * p.dw_splits, sms, st);
   };
   const bool want_x = dx && d->rows, both = p.both && want_x && dweight;

@@ -55,10 +55,12 @@ struct Room {
 constexpr u32 TMEM_COLUMNS = 512;
 constexpr u64 WAIT_NS = 2000000000ull, DRAIN_NS = 100000000ull;
 constexpr int MAX_SEGMENTS = 6;
-// Blocks of k after which sums are taken out and joined, rounded to nearest: sums of several parts, and long sums of one (Job::LONG).  The tensor
+// Blocks of k after which sums are taken out and joined, rounded to nearest: sums of several parts, and long sums of one.  The tensor
 // cores truncate a sum at every 16 k: by 4e-6 of a loss at 4096 features.  2048 x 4096 x 32000, joined every 512, 768 or 1024 k: the rows' losses off by
 // 1.1e-7, 1.6e-7, 2.2e-7; loss 464, 450, 434 us (418 unjoined), gradients 1136, 1115, 1103 (1080).  768 features unjoined: 2.3e-7.
-constexpr int JOIN_PARTS = 1, JOIN_LONG = 12, JOIN_FROM = JOIN_LONG * BLOCK_K;
+// A sum of terms of one sign is short by 6e-9 for each of its terms (65536 of them: 4e-4): sums that end in 16 bits are joined where they would lose more than a
+// tenth of the type's smallest half step.
+constexpr int JOIN_PARTS = 1, JOIN_LONG = 12, JOIN_HALF = 4096 / BLOCK_K, JOIN_BFLOAT = 32768 / BLOCK_K;
 
 struct Segments {
   int n;
@@ -276,7 +278,9 @@ __device__ __forceinline__ int epilogue_width(int cols) { return cols / 2; }
 //      REPORTS: tiles depend on one another.  A warp of its own, the last, runs ahead with ready(local, t, dead), which waits until a tile's
 //      operands are there (false: gave up); report(local, t) is called by warp 2 when the block has written its part of a
 //      tile.  Both wait a microsecond or two for the memory; with the loading warps waiting themselves, 12 encoder layers took 1702 us, not 1601.
-// JOIN: sums are taken out after so many blocks of k and held (0: not).  Up to 128 columns there is room for two sums beside the held ones;
+//      LONG: sums of one part may be joined: after `run` blocks of k, in this call (joins(), on the host) and this kernel (joined(local): false only where
+//      none is longer)
+// JOIN: how sums are taken out and held on the way: not (0), after each block (1, sums of parts), after `run` blocks (2).  Up to 128 columns there is room for two sums beside the held ones;
 // of 256 columns there is one, taken out for good before the next tile's first block of k, and the epilogue reads the held ones.
 template <class Job, int CG, int JOIN>
 __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid_constant__ Job job) {
@@ -307,8 +311,11 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
   const u32 tmem = ctl.tmem;
   typename Job::Local local = job.begin(shared, cluster, clusters);
   const int b_rows = job.cols / CG;               // rows of B that a block loads
-  const bool single = JOIN > 1 && job.cols > 128;
+  bool single = false;
+  if constexpr (JOIN > 1) single = job.cols > 128 && job.joined(local);
   const u32 buffers = single ? 0 : 1;             // (a mask)
+  int length = JOIN;                              // blocks of k of a sum
+  if constexpr (JOIN > 1) length = job.run;
 
   if (warp == 0 || warp == 3) {
     const u32 bytes = CG * (2 * BOX_BYTES + (u32)b_rows * BLOCK_K * 2);
@@ -319,7 +326,7 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
       if constexpr (Job::REPORTS) {
         if (!__all_sync(0xffffffffu, wait_shared(&ctl.ready, (u32)i + 1, &ctl.dead))) { ok = false; break; }
       }
-      const int a_row = t.a_row + (int)rank * 128, b_row = t.b_row + (int)rank * b_rows, run = JOIN ? JOIN : t.blocks;
+      const int a_row = t.a_row + (int)rank * 128, b_row = t.b_row + (int)rank * b_rows, run = JOIN ? length : t.blocks;
       for (int k0 = 0; k0 < t.blocks && ok; k0 += run) {
         const int k1 = JOIN ? min(k0 + run, t.blocks) : t.blocks;
         for (int s = 0; s < job.seg.n && ok; ++s) {
@@ -359,7 +366,7 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
     for (int i = 0; ok && job.tile(local, i, t); ++i) {
       int left = t.blocks;
       do {
-        const int blocks = JOIN ? min(left, JOIN) : left;
+        const int blocks = JOIN ? min(left, length) : left;
         const u32 buf = taken & buffers;
         if (!__all_sync(0xffffffffu, wait(&ctl.acc_empty[buf], ((taken >> buffers) & 1) ^ 1, &ctl.dead))) { ok = false; break; }
         fence_after();
@@ -371,7 +378,7 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
           if (!__all_sync(0xffffffffu, wait(&ctl.full[stage], (n / STAGES) & 1, &ctl.dead))) { ok = false; break; }
           fence_after();
           const u32 at = tiles + stage * STAGE_BYTES;
-          const int kb = k0 + (JOIN == 1 ? 0 : j);        // (several segments: no join, or one after each block)
+          const int kb = k0 + (JOIN == 1 ? 0 : j);        // (JOIN 1: the segments of one block; otherwise there is one segment)
           const bool a_rows_first = t.a_rows_first != (kb < t.a_turn), b_rows_first = t.b_rows_first != (kb < t.b_turn);
           const u32 idesc = instruction(128 * CG, job.cols, job.bfloat, a_rows_first, b_rows_first);
           const u32 a_step = (a_rows_first ? 2048 : 32) >> 4, b_step = (b_rows_first ? 2048 : 32) >> 4;
@@ -427,7 +434,7 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
         if (ok && !wait(&ctl.acc_full[buf], (taken >> buffers) & 1, &ctl.dead)) ok = false;
         ok = __all_sync(0xffffffffu, ok);
         fence_after();
-        const bool last = !JOIN || left <= JOIN || !ok;
+        const bool last = !JOIN || left <= length || !ok;
         const u32 held = lanes + (single ? 256 : 384);
         Sums s = {!ok ? SUMS_NAN : job.seg.n * t.blocks == 0 ? SUMS_ZERO : first ? SUMS_HELD : SUMS_JOINED, lanes + buf * 256, held};
         const bool join = JOIN && s.state <= SUMS_JOINED && (single || !last);
@@ -459,7 +466,7 @@ __global__ void __launch_bounds__(Room<Job>::THREADS, 1) k_products(const __grid
         ++taken;
         if (last) break;
         first = false;
-        left -= JOIN;
+        left -= length;
       }
     }
     epi.finish();
@@ -626,16 +633,17 @@ cudaError_t launch_products(const Job& job, int cg, int tiles_at_once, cudaStrea
   };
   if (job.seg.n > 1) return with(std::integral_constant<int, JOIN_PARTS>());
   if constexpr (Job::LONG)
-    if (job.features > JOIN_FROM) return with(std::integral_constant<int, JOIN_LONG>());
+    if (job.joins()) return with(std::integral_constant<int, 2>());
   return with(std::integral_constant<int, 0>());
 }
 
 // For jobs whose operands are there before the kernel runs, and that look up nothing.
 struct Plain {
   static constexpr int STAGING = 0;
-  static constexpr bool REPORTS = false, LONG = false;
+  static constexpr bool REPORTS = false, LONG = true;
   struct Shared {};
   __device__ __forceinline__ void fill(Shared&) const {}
+  template <class Local> __device__ __forceinline__ bool joined(const Local&) const { return true; }
 };
 
 }  // namespace mma

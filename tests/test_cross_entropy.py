@@ -535,6 +535,49 @@ def test_p_of_a_row_adds_up_to_nothing(n, d, v, dtype, how):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_long_sums_of_one_sign(dtype):
+    """x and every p that is looked at are positive, so whatever the products cut off of their sums is of one sign, and shows in the mean over all elements of
+    dweight, where the roundings of p and of the result (2^-11 or 2^-8, of both signs) leave 2^-8 / sqrt(127 * 4096), below 1e-5.  Sums are joined every 4096
+    terms (float16) or 32768 at the latest: 256 or 2048 products of 16, each of which may cut off two steps, 2^-22, of a sum that grows evenly: 2^-23 for each."""
+    n, d, v = 1 << 18, 4096, 128
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = (torch.rand((n, d), device="cuda", generator=gen, dtype=torch.float16) + 0.5).to(DTYPES[dtype])
+    w = torch.randn((v, d), device="cuda", generator=gen).mul_(0.3 / math.sqrt(d)).to(DTYPES[dtype])
+    t = torch.zeros(n, device="cuda", dtype=torch.long)
+    loss, lse, count = ce.linear_cross_entropy_forward(x, w, t)
+    dw = ce.linear_cross_entropy_backward(torch.tensor(1000.0, device="cuda"), x, w, t, lse, count, need_x=False)[1]
+    want = torch.zeros((v, d), device="cuda", dtype=torch.float64)
+    for part in x.split(1 << 14):
+        p = torch.softmax(part.double() @ w.double().t(), 1)
+        p[:, 0] -= 1
+        want += p.t() @ part.double()
+    want *= 1000.0 / n
+    off = ((dw.double() - want) / want)[1:].mean()
+    assert abs(float(off)) <= (256 if dtype == "f16" else 2048) * 2.0 ** -23 + 1e-5, float(off)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [64, 1200])
+def test_long_sums_over_the_classes(n):
+    """The same of dx: weights between 1/2 and 3/2, the target's own part (its weights, exactly) taken out again."""
+    d, v = 256, 1 << 19
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    w = torch.rand((v, d), device="cuda", generator=gen, dtype=torch.float16) + 0.5
+    x = torch.randn((n, d), device="cuda", generator=gen).mul_(0.02).half()
+    t = torch.randint(v, (n,), device="cuda", generator=gen)
+    w[t] = 0                                            # the target's p - 1 then adds nothing
+    loss, lse, count = ce.linear_cross_entropy_forward(x, w, t, reduction="sum")
+    dx = ce.linear_cross_entropy_backward(torch.tensor(1.0, device="cuda"), x, w, t, lse, count, reduction="sum", need_weight=False)[0]
+    top, total, want = (x.double() @ w.double().t()).amax(1, keepdim=True), 0.0, 0.0
+    for part in w.split(1 << 16):
+        q = torch.exp(x.double() @ part.double().t() - top)
+        total, want = total + q.sum(1, keepdim=True), want + q @ part.double()
+    off = ((dx.double() - want / total) / (want / total)).mean()
+    assert abs(float(off)) <= 256 * 2.0 ** -23 + 1e-5, float(off)
+
+
+@pytest.mark.gpu
 def test_same_bits_again():
     for dtype, n in (("bf16", 3000), ("f32", 500)):
         x, w, t, b = data(n, 200, 5000, DTYPES[dtype], True, 0.1, seed=9)
