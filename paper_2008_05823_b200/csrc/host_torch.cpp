@@ -229,7 +229,11 @@ class OrthoPlan {
         rows.append(row);
       }
       results = K_ == 1 && flat_ ? py::object(rows[0]) : py::object(rows);
-    } else out = tensors(results, held);
+    } else {
+      const size_t first = held.size();
+      out = tensors(results, held);
+      results = given(results, held, first);
+    }
     std::vector<const void*> from(n);
     std::vector<void*> to(n);
     std::vector<int64_t> pitch(n), result_pitch(n);
@@ -292,6 +296,17 @@ class OrthoPlan {
       }
     }
     return out;
+  }
+  // What a call was given as results; an iterator, which has been used up, as the list of what it gave.
+  py::object given(const py::object& results, const std::vector<py::object>& held, size_t first) const {
+    py::object outer = PyIter_Check(results.ptr()) ? held[first] : results;
+    if (flat_) return outer;
+    bool used = false;
+    for (Py_ssize_t k = 0; k < PySequence_Fast_GET_SIZE(held[first].ptr()); ++k) used = used || PyIter_Check(PySequence_Fast_GET_ITEM(held[first].ptr(), k));
+    if (!used) return outer;
+    py::list rows;
+    for (size_t k = first + 1; k < held.size(); ++k) rows.append(held[k]);
+    return rows;
   }
   static py::object sequence(py::handle o, std::vector<py::object>& held) {
     py::object seq = py::reinterpret_steal<py::object>(PySequence_Fast(o.ptr(), "matrices: a sequence of tensors, or of rows of tensors"));

@@ -334,6 +334,24 @@ def test_what_a_call_writes_counts_as_changed():
 
 
 @pytest.mark.gpu
+def test_results_by_iterators():
+    """What is returned can be read again: the lists of what iterators gave, otherwise the very objects."""
+    shapes = [(20, 30), (9, 4)]
+    gs = [[gradient(s, torch.float32, 10 * k + i) for i, s in enumerate(shapes)] for k in range(2)]
+    one, two = Orthogonalizer(shapes), Orthogonalizer(shapes, num_rows=2)
+    want = two(gs)
+    for make in (lambda o: o, tuple, iter, lambda o: (t for t in o), lambda o: dict(enumerate(o)).values()):
+        out = [[torch.empty_like(g) for g in row] for row in gs]
+        given = make(out[0])
+        got = one(gs[0], given)
+        assert got is given or not isinstance(given, (list, tuple))
+        assert all(a is b for a, b in zip(list(got), out[0])) and len(list(got)) == 2
+        for outer in (list, iter):
+            got = two(gs, outer([make(row) for row in out]))
+            assert len(got) == 2 and all(a is b and torch.equal(b, c) for r, o, w in zip(got, out, want) for a, b, c in zip(list(r), o, w)) and len(list(got[1])) == 2
+
+
+@pytest.mark.gpu
 def test_bad_calls_are_refused():
     plan = Orthogonalizer([(8, 6), (4, 4, 3)])
     a, b = torch.ones((8, 6), device="cuda"), torch.ones((4, 4, 3), device="cuda")
