@@ -507,22 +507,18 @@ __device__ __forceinline__ void load_written(const void* from, u32 (&w)[16]) {
     asm volatile("ld.relaxed.gpu.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]), "=r"(w[i + 4]), "=r"(w[i + 5]), "=r"(w[i + 6]), "=r"(w[i + 7]) : "l"((const char*)from + i * 4)
                  : "memory");
 }
-// Rows of 16-byte pieces in shared memory, `wide` (a power of two, 4 at least) a row.  Pieces change places with the row, so that a lane
-// that takes pieces of its own row and lanes that take the pieces of one row both meet different banks.
-template <int WIDE>
-__device__ __forceinline__ u32 staged_at(u32 base, int r, int piece) {
-  return base + (u32)(r * WIDE + (piece ^ (WIDE == 4 ? (r >> 1) & 3 : r & 7))) * 16;
-}
+// Rows of 16 pieces of 16 bytes in shared memory.  Pieces change places with the row, so that a lane that takes pieces of its own row and
+// lanes that take the pieces of one row both meet different banks.
+__device__ __forceinline__ u32 staged_at(u32 base, int r, int piece) { return base + (u32)(r * 16 + (piece ^ (r & 7))) * 16; }
 __device__ __forceinline__ uint4 staged_piece(u32 at) {
   uint4 v;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
   return v;
 }
-template <int WIDE>
 __device__ __forceinline__ void staged_load(u32 base, int r, int piece, u32 (&w)[16]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint4 v = staged_piece(staged_at<WIDE>(base, r, piece + i));
+    const uint4 v = staged_piece(staged_at(base, r, piece + i));
     w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
   }
 }

@@ -360,7 +360,7 @@ struct OrthoJob {
           if ((own == 2 ? p & 7 : p) < chunks * 4)
 #pragma unroll
             for (int r = lane >> 4; r < 32; r += 2)
-              if (row0 + r < rows) mma::piece_in(mma::staged_at<16>(in, r, p), from + (long long)r * pitch);
+              if (row0 + r < rows) mma::piece_in(mma::staged_at(in, r, p), from + (long long)r * pitch);
         }
       }
     }
@@ -406,8 +406,8 @@ struct OrthoJob {
         }
         u32 hi[16], lo[16];
         if (own) {
-          mma::staged_load<16>(in, lane_row, 4 * k, hi);
-          if (own == 2) mma::staged_load<16>(in, lane_row, 8 + 4 * k, lo);
+          mma::staged_load(in, lane_row, 4 * k, hi);
+          if (own == 2) mma::staged_load(in, lane_row, 8 + 4 * k, lo);
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             float2 x = mma::unpack_half(hi[i]);

@@ -241,6 +241,49 @@ def test_more_matrices_than_travel_as_arguments():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_more_shapes_and_batches_than_shared_memory_holds(dtype):
+    """40 shapes and 7 steps, 840 products: both tables are read from memory.  33 shapes and 3 steps: one of them is."""
+    kind = DTYPES[dtype]
+    for count, steps in ((40, 7), (33, 3), (40, 6), (12, 23)):
+        shapes = [(131 + 5 * i, 420 - 7 * i) if i % 2 else (300 - 3 * i, 140 + 9 * i) for i in range(count)]
+        gs = [gradient(s, kind, i, "noise") for i, s in enumerate(shapes)]
+        coefs = [(1.875, -1.25, 0.375)] * steps
+        for g, y in zip(gs, Orthogonalizer(shapes, kind, steps=steps, coefficients=coefs)(gs)):
+            one = 1 if kind == torch.bfloat16 else 2
+            off = 2 * rel(rounded(g, one, steps, coefs), exact(g, steps, coefs)) + torch.finfo(kind).eps / 2 + 20 * 36 * 2.0 ** -24
+            assert rel(y, exact(g, steps, coefs)) <= off, (count, steps, tuple(g.shape))
+
+
+@pytest.mark.gpu
+def test_many_small_and_large_matrices_in_one_list():
+    """More than travel as arguments, of every kind: held by one SM or made tile by tile, in one part or two, their addresses in two tables."""
+    small, large = [(8, 12), (64, 70), (100, 40), (128, 300)], [(200, 300), (131, 1100), (333, 140)]
+    shapes = [large[i // 40 % 3] if i % 40 == 7 else small[i % 4] for i in range(470)]
+    kinds = [(torch.float32, torch.bfloat16, torch.float16)[i % 3] for i in range(470)]
+    results = [(torch.bfloat16, torch.float32)[i // 47 % 2] for i in range(470)]
+    gs = [gradient(s, k, i) for i, (s, k) in enumerate(zip(shapes, kinds))]
+    plan = Orthogonalizer(shapes, kinds, result_dtypes=results)
+    out = plan(gs)
+    for i, (g, y, k) in enumerate(zip(gs, out, results)):
+        assert rel(y, exact(g)) <= allowed(g, k), (i, tuple(g.shape))
+    assert all(torch.equal(a, b) for a, b in zip(out, plan(gs)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("result", ["bf16", "f32"])
+def test_lists_of_several_portions(result):
+    """About 1.2 GB of workspace, gone through in portions of half a GB: shapes that begin in one and end in the next, whose S is made in parts or not."""
+    shapes = [(2048, 1900)] * 14 + [(140, 9000)] * 6 + [(1000, 3000)] * 14
+    gs = [gradient(s, torch.bfloat16, i) for i, s in enumerate(shapes)]
+    plan = Orthogonalizer(shapes, torch.bfloat16, result_dtypes=DTYPES[result])
+    out = plan(gs)
+    for i, (g, y) in enumerate(zip(gs, out)):
+        assert rel(y, exact(g)) <= allowed(g, DTYPES[result]), (i, tuple(g.shape))
+    assert all(torch.equal(a, b) for a, b in zip(out, plan(gs)))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_scales_and_special_values(dtype):
     """Norms from the smallest to the largest that the type holds; zeros; a matrix that is not finite is NaN and its neighbours stay."""
