@@ -578,6 +578,51 @@ def test_long_sums_over_the_classes(n):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("left", [0, 1, 300, 9000])
+def test_few_rows_left_of_many(left, dtype):
+    """Launches made for 9000 rows and 40000 classes, whose sums would be joined, where few rows take part, or none."""
+    x, w, t, b = data(9000, 40, 40000, DTYPES[dtype], True, 0.0, seed=12)
+    t[torch.randperm(9000, device="cuda")[left:]] = IGNORE
+    if left:
+        check(x, w, t, b, "mean", torch.tensor(1.0, device="cuda"))
+    one = torch.tensor(1.0, device="cuda")
+    loss, lse, count = ce.linear_cross_entropy_forward(x, w, t, b, reduction="sum")
+    for some in (lse, lse.clone()):
+        dx, dw, db = ce.linear_cross_entropy_backward(one, x, w, t, some, count, b, reduction="sum")
+        assert int(count) == left and not dx[t == IGNORE].any() and torch.isfinite(dx).all() and torch.isfinite(dw).all()
+        if not left:
+            assert float(loss) == 0 and not dw.any() and not db.any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,n,d,v", [("f32", 20, 64, 10), ("f32", 20, 300, 500), ("f32", 700, 64, 900), ("bf16", 700, 900, 3000), ("f16", 300, 65, 200)])
+def test_the_entry_points_without_rest(dtype, n, d, v):
+    """Loss and lse to the bit; the gradients those of a call with a copy of lse, and within the bounds of the ones with rest."""
+    x, w, t, b = data(n, d, v, DTYPES[dtype], True, 0.2, seed=13)
+    L, one = sb.lib(), torch.tensor(1.0, device="cuda")
+    kind = {"f32": sb.TYPE_FLOAT, "bf16": sb.TYPE_BFLOAT, "f16": sb.TYPE_HALF}[dtype]
+    s = desc(type=kind, bias_type=kind, has_bias=1, rows=n, features=d, classes=v, x_pitch=d, weight_pitch=d)
+    loss, lse, count = ce.linear_cross_entropy_forward(x, w, t, b)
+    want = ce.linear_cross_entropy_backward(one, x, w, t, lse.clone(), count, b)
+    loss2, lse2, count2 = torch.full_like(loss, 7), torch.full_like(lse, 7), torch.full_like(count, 7)
+    got = [torch.full_like(a, 7) for a in (x, w, b)]
+    stream = torch.cuda.current_stream().cuda_stream
+    need = [L.sae_linear_ce_workspace(C.byref(s), w.data_ptr(), k) for k in (0, 1)]
+    ws = torch.empty(max(need), dtype=torch.uint8, device="cuda")
+    assert L.sae_linear_ce_forward(C.byref(s), x.data_ptr(), w.data_ptr(), b.data_ptr(), t.data_ptr(), loss2.data_ptr(), lse2.data_ptr(), count2.data_ptr(),
+                                   ws.data_ptr(), need[0], stream) == sb.OK
+    assert torch.equal(loss, loss2) and torch.equal(lse, lse2) and torch.equal(count, count2)
+    assert L.sae_linear_ce_backward(C.byref(s), one.data_ptr(), x.data_ptr(), w.data_ptr(), b.data_ptr(), t.data_ptr(), lse2.data_ptr(), count2.data_ptr(),
+                                    got[0].data_ptr(), got[1].data_ptr(), got[2].data_ptr(), ws.data_ptr(), need[1], stream) == sb.OK
+    assert all(torch.equal(p, q) for p, q in zip(want, got))
+    e = Exact(x, w, t, b, "mean", one)
+    near(got[0], e.dx, e.dx_off, "dx")
+    near(got[1], e.dw, e.dw_off, "dweight")
+    near(got[2], e.db, e.db_off + e.db.abs() * (torch.finfo(b.dtype).eps / 2), "dbias")
+
+
+@pytest.mark.gpu
 def test_same_bits_again():
     for dtype, n in (("bf16", 3000), ("f32", 500)):
         x, w, t, b = data(n, 200, 5000, DTYPES[dtype], True, 0.1, seed=9)

@@ -305,6 +305,29 @@ def test_scales_and_special_values(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(200, 300), (420, 150), (140, 5000), (131, 131), (64, 900)])
+@pytest.mark.parametrize("dtype,result", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("f32", "bf16")])
+def test_special_values_tile_by_tile(shape, dtype, result):
+    """The same where a matrix is made tile by tile, its square product in parts or not: small and large norms, zeros, one value that is not finite at either
+    end; neighbours keep their bits."""
+    dt = DTYPES[dtype]
+    base = gradient(shape, torch.float32, 4, "noise") * 1e3
+    top, low = (1e3, 1e-2) if dt == torch.float16 else (1e36, 1e-30)
+    gs = [(base * top).to(dt), (base * low).to(dt), torch.zeros(shape, device="cuda", dtype=dt)] + [base.to(dt).clone() for _ in range(4)]
+    want = Orthogonalizer([shape], dt, result_dtypes=DTYPES[result])([gs[3]])[0]
+    gs[4][0, 0] = math.nan
+    gs[5][-1, -1] = math.inf
+    gs[6][shape[0] // 2, shape[1] - 1] = -math.inf
+    y = Orthogonalizer([shape] * 7, dt, result_dtypes=DTYPES[result])(gs)
+    for i in (0, 1, 3):
+        assert rel(y[i], exact(gs[i])) <= allowed(gs[i], DTYPES[result]), i
+    assert not y[2].any() and rel(y[3], want.double()) <= 2 * allowed(gs[3], DTYPES[result])
+    assert all(torch.isnan(y[i]).all() for i in (4, 5, 6))
+    zero = Orthogonalizer([shape] * 2, dt, eps=0.0, result_dtypes=DTYPES[result])([gs[2], gs[1]])
+    assert torch.isnan(zero[0]).all() and rel(zero[1], exact(gs[1], eps=0.0)) <= allowed(gs[1], DTYPES[result])
+
+
+@pytest.mark.gpu
 def test_same_bits_wherever_it_stands():
     """A matrix has the same result again, and beside others of its shape."""
     g, other = gradient((300, 400), torch.bfloat16, 1), gradient((300, 400), torch.bfloat16, 2)
