@@ -57,10 +57,11 @@ constexpr u64 WAIT_NS = 2000000000ull, DRAIN_NS = 100000000ull;
 constexpr int MAX_SEGMENTS = 6;
 // Blocks of k after which sums are taken out and joined, rounded to nearest: sums of several parts, and long sums of one.  The tensor
 // cores truncate a sum at every 16 k: by 4e-6 of a loss at 4096 features.  2048 x 4096 x 32000, joined every 512, 768 or 1024 k: the rows' losses off by
-// 1.1e-7, 1.6e-7, 2.2e-7; loss 464, 450, 434 us (418 unjoined), gradients 1136, 1115, 1103 (1080).  768 features unjoined: 2.3e-7.
+// 1.1e-7, 1.6e-7, 2.2e-7; loss 464, 450, 434 us (418 unjoined), gradients 1136, 1115, 1103 (1080); the
+// plain form in float32 7e-7 at 2048 features.  Every 1024: a join waits 1000 cycles for a sum of 16 blocks, which takes 9400.
 // A sum of terms of one sign is short by 6e-9 for each of its terms (65536 of them: 4e-4): sums that end in 16 bits are joined where they would lose more than a
 // tenth of the type's smallest half step.
-constexpr int JOIN_PARTS = 1, JOIN_LONG = 12, JOIN_HALF = 4096 / BLOCK_K, JOIN_BFLOAT = 32768 / BLOCK_K;
+constexpr int JOIN_PARTS = 1, JOIN_LONG = 16, JOIN_HALF = 4096 / BLOCK_K, JOIN_BFLOAT = 32768 / BLOCK_K;
 
 struct Segments {
   int n;
