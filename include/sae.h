@@ -437,7 +437,8 @@ int sae_group_norm_backward(const sae_group_norm_desc *desc, const void *dy, con
 
 /*
  * Linear cross entropy.  (Where a worker's stochastic gradient begins: the loss of a linear output layer over its classes, the
- * logits of which would be the largest tensor of the training step.  They are never stored.)
+ * logits of which would be the largest tensor of the training step.  They are not kept.  What a call holds in its workspace is p of a piece of the classes,
+ * 256 MB or 256 classes; with float tensors of up to 320 rows all logits, up to 8 parts of each, and p.)
  *
  *   z_ij = x_i . w_j + bias_j;  lse_i = log(sum_j exp(z_ij));  loss_i = lse_i - z_i,target(i)
  *   p_ij = (exp(z_ij - lse_i) - [j = target(i)]) * g_i;  dx_i = sum_j p_ij w_j;  dw_j = sum_i p_ij x_i;  dbias_j = sum_i p_ij
@@ -463,7 +464,8 @@ int sae_group_norm_backward(const sae_group_norm_desc *desc, const void *dy, con
  * Arithmetic: 16-bit tensors are multiplied as they are, sums and everything about the softmax are float.  The backward call makes z
  * again and holds p in pieces of the classes, rounded once to `type` (half a unit of that type for each p, which averages out in dx and
  * dweight; a float16 p is scaled so that it does not vanish).  Float tensors are multiplied as three bfloat16 parts each, with about the
- * error of float products.  The order of sums is fixed: same input, same bits.
+ * error of float products.  What the tensor cores cut off of a long sum of 16-bit products of one sign stays below 3e-5 (float16) or 2e-4 of it.  The order
+ * of sums is fixed: same input, same bits.
  * A bias of -inf takes a class out.  A row whose logits are all -inf, or that holds an infinity or a NaN, has a NaN loss.
  * Errors: SAE_ERR_INVALID_ARG for a null or misaligned pointer, a size out of range (0 <= rows <= 2^24, 1 <= features <= 2^17,
  *   1 <= classes <= 2^24), a workspace too small; SAE_ERR_CUDA.
@@ -500,20 +502,24 @@ int sae_linear_ce_backward_with_rest(const sae_linear_ce_desc *desc, const float
                                      size_t workspace_bytes, void *stream);
 
 /*
- * Orthogonalisation of many matrices.  (What a worker may do to its momentum or its model difference before it is compressed:
- * every matrix of a model is replaced by one with the same singular vectors and singular values near 1.)
+ * Orthogonalisation of many matrices.  (What a worker may do to its gradients or its model difference before they are compressed:
+ * every matrix of a model is replaced by one with the same singular vectors and singular values near 1.  The momentum of sae_step lies behind this, where no
+ * call reaches it: who wants a momentum made orthogonal keeps it outside and gives the step none.)
  *
  *   x = g / (|g| + eps), |g| the square root of the sum of squares;  then, for every step i:
  *   x <- a_i x + b_i (x x') x + c_i (x x')^2 x
  *
- * A sae_ortho holds the shapes, the tables and the workspace (about 8 bytes an element and 8 more for each element of the square
- * products, and up to 20 MB of sums) of one list of matrices: `num_rows` workers' lists of `num_matrices` each.
+ * A sae_ortho holds the shapes, the tables and the workspace of one list of matrices: `num_rows` workers' lists of `num_matrices` each.  That is, for
+ * matrices that are too large for one SM (64 rows of 768 or 128 of 320, either way round), 8 bytes an element and 8 more for each element of the square product, the
+ * columns of both counted up to a multiple of 64 (a matrix of 1000000 x 8: 64 bytes an element), and up to 30 MB of sums.  A captured graph uses
+ * it too: the handle has to outlive the graph.
  * matrices, results: HOST arrays of num_rows * num_matrices DEVICE pointers, row k's at [k * num_matrices .. ); read before the call
  *   returns.  Matrix j is rows[j] x cols[j] of type types[j], neighbouring columns next to each other, its rows pitches[..] elements
  *   apart (HOST, as the pointers; NULL: without gaps); its result is of type result_types[j].  A result may be its own
  *   matrix; it must not overlap another.  An empty matrix may be NULL.
  * Norms are taken in double.  x is held in 22 bits.  Products for a float or float16 result take all of them, which is about the error of float
- *   products; for a bfloat16 result 11 bits of each operand, which is an error of about 2e-3 of the result's norm, that of its own rounding.
+ *   products; for a bfloat16 result 11 bits of each operand (more than 128 rows and columns), which is an error of about 2e-3 of the result's norm, that of its
+ *   own rounding, and up to 3e-3 where one side is a thousand times the other.
  * A zero matrix stays zero (eps = 0: NaN); one with an infinity or a NaN becomes NaN.
  * Coefficients that let a singular value grow beyond 16, or |b s + c s^2| beyond 4096, are refused.
  * sae_ortho_run only enqueues kernels on the configuration's stream, allocates nothing, may be captured, and uses the handle's

@@ -20,7 +20,7 @@ def _reduction(name):
 
 
 def linear_cross_entropy_forward(x, weight, target, bias=None, ignore_index=-100, reduction="mean"):
-    """The cross entropy of x @ weight.T + bias ([..., classes], never stored) against target [...].
+    """The cross entropy of x @ weight.T + bias ([..., classes], not kept) against target [...].
     Returns (loss, lse, count): the loss in float32, of target's shape for "none"; the logarithm of every row's sum of
     exponentials, 0 for a row whose target is ignore_index; the number of the other rows, int64.
     lse.rest is what rounding to float32 left out of lse: the backward call reads it.  A copy of lse does not have it."""

@@ -16,7 +16,8 @@
 //
 // The tensor cores cut off what a sum has below its last bit, at each of the products that it is made of, and a sum of a few
 // thousand terms of one sign ends up short by some 1e-5.  For operands of several parts the sums are therefore taken out every
-// 64 of k, rounded to nearest where they are joined (in the 128 columns that tiles of up to 128 columns leave free).
+// 64 of k, rounded to nearest where they are joined (in the 128 columns that tiles of up to 128 columns leave free); for operands of one part
+// where sums are long.
 //
 // Operands lie in memory either way: k neighbouring ("K first", what x w' wants of x and w) or the rows neighbouring ("rows
 // first", what p' x wants); the matrix descriptors say which, nothing is transposed.

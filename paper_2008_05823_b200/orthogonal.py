@@ -1,5 +1,6 @@
 """Orthogonalisation of a model's matrices by Newton-Schulz products, all of them in one call: what a worker may do to its
-momentum, its gradients or its model difference before they are packed.  `Orthogonalizer` mirrors the `sae_ortho_*` entry points of
+gradients or its model difference before they are packed.  (The momentum of Sae.step lies behind that.  A momentum that is to be made orthogonal is kept
+outside, and the step is made with momentum 0.)  `Orthogonalizer` mirrors the `sae_ortho_*` entry points of
 include/sae.h; what looks at the tensors is csrc/host_torch.cpp, and there is no CPU fallback.
 """
 import ctypes as C
@@ -12,7 +13,8 @@ from . import binding
 from .binding import ABI_VERSION, ERR_INVALID_ARG, OK, SaeError, SaeOrthoConfig
 from .grads import TYPE_OF
 
-# Five steps of these bring every singular value above about 0.01 of the norm to within 0.7 .. 1.2.
+# Five steps of these bring every singular value above about 0.01 of the norm to within 0.7 .. 1.2 (a published choice: K. Jordan et al., "Muon: an optimizer
+# for hidden layers in neural networks", 2024).
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 
@@ -42,10 +44,11 @@ class Orthogonalizer:
     plan(tensors, results=None): T tensors (num_rows = 1) or num_rows lists of T; returns results, new tensors where none are
     given.  A tensor may be its own result.  Its columns are neighbours in memory, its rows may have gaps between them.  What a call
     writes counts as changed in place; results take no part in autograd.
-    bfloat16 results have an error of about their own rounding, 2e-3 of the norm; float32 and float16 results that of float32
+    bfloat16 results have an error of about their own rounding, 2e-3 of the norm (3e-3 where a matrix is a thousand times as long as wide); float32 and float16 results that of float32
     products, for three times the work.
     Work is enqueued on the stream the plan was made on (or `stream`); a call made while another stream is current orders the
-    two.  One plan is for one stream and one host thread at a time."""
+    two.  One plan is for one stream and one host thread at a time.  Making one takes 0.5 to 1.5 ms (allocations, tables, a synchronisation): it is kept for a
+    model, and outlives the graphs that captured its calls."""
 
     def __init__(self, shapes, dtypes=torch.float32, num_rows=1, steps=5, coefficients=COEFFICIENTS, eps=1e-7, result_dtypes=None,
                  device=None, stream=None):
